@@ -246,6 +246,109 @@ lq_status lq_linear_forward_host_async(const lq_layer* layer, lq_act* act, const
 lq_status lq_linear_forward_static(const lq_layer* layer, const void* X_f16_dev, int32_t M, void* Y_dev,
                                    lq_out_dtype dtype, void* cuda_stream);
 
+/* ---- low-rank adapters of many requests beside a shared projection ----------------------------------------------
+ * (The paper has one low-rank branch per layer, fixed at calibration.  A server that answers many requests with one
+ * quantized layer adds each request's own fp16 branch to the shared output.)
+ *
+ *     Y[m] = Y0[m] + scale_a ( X[m] A_a ) B_a,     a = the adapter of row m, or none: Y[m] = Y0[m]
+ *
+ * lq_adapters holds up to `slots` adapters (A_a [K][r_a], B_a [r_a][N], scale_a) of projections of one shape on one
+ * device; lq_rowmap says which adapter each row of a batch uses.  One map serves every projection of a step.        */
+typedef struct lq_adapters lq_adapters;
+typedef struct lq_rowmap lq_rowmap;
+
+/* A set of `slots` empty adapters of rank up to max_rank for projections of K inputs and N outputs (allocates
+ * 2 * slots * r * (K + N) bytes of device memory, r = max_rank rounded up to 16 or a multiple of 32; synchronous).
+ * 1 <= slots <= 1023, 1 <= max_rank <= 128, K <= 8192, N <= 2^20, K and N multiples of 8; anything else is UNSUPPORTED. */
+lq_status lq_adapters_create(int32_t K, int32_t N, int32_t max_rank, int32_t slots, int device, lq_adapters** out);
+lq_status lq_adapters_free(lq_adapters* set);
+
+/* Puts an adapter into a slot, or another one in its place; rank 0 empties the slot (A and B are then ignored).
+ *   A_f16_dev  [K][rank] row-major half bits, device        B_f16_dev  [rank][N] row-major half bits, device
+ *   scale      finite; applied to the product in fp32
+ * The set keeps its own copy.  Asynchronous on `cuda_stream`: forwards queued there earlier use what was there before,
+ * later ones the new adapter; forwards on other streams must be ordered by the caller.  May be captured. */
+lq_status lq_adapters_set(lq_adapters* set, int32_t slot, int32_t rank, const void* A_f16_dev, const void* B_f16_dev, float scale,
+                          void* cuda_stream);
+
+/* A map of up to M_max rows to the slots 0 .. slots - 1 (1 <= slots <= 1023, M_max <= 2^24), with the workspace of the forwards
+ * that use it (synchronous). */
+lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, lq_rowmap** out);
+lq_status lq_rowmap_free(lq_rowmap* map);
+
+/* Sorts the rows by adapter (stable; on the device, so a captured graph sorts anew on each replay what the array then holds).
+ *   row_adapter_dev  [M] int32, device: the slot of each row; anything outside 0 .. slots - 1 means none
+ *   M                1 <= M <= M_max; the rows of every forward until the next call
+ * Asynchronous on `cuda_stream`. */
+lq_status lq_rowmap_set(lq_rowmap* map, const int32_t* row_adapter_dev, int32_t M, void* cuda_stream);
+
+/* Y = Y0 + the rows' adapters.  Products and sums in fp32; the rank-r intermediate travels as two halves under a power-of-two
+ * scale of its row (22 bits); rounded once to `dtype`.
+ *   X_f16_dev  [M][K] row-major half, device, 16-byte aligned, finite
+ *   Y0_dev     [M][N] row-major half or float per `dtype`, device, 16-byte aligned: the projection's output
+ *   Y_dev      the same shape and type: Y0_dev itself (rows without an adapter are then left alone) or memory apart from it
+ *              and from X
+ * The map's slots must not be more than the set's, and map and set must be on one device.  No sum depends on the order of execution, so
+ * equal calls give equal bits; a row may differ by rounding between calls of other M or other maps.
+ * Calls that use one map, lq_rowmap_set among them, share its workspace: they must not overlap on the GPU (one stream, or events;
+ * graphs that were captured with one map must not run side by side).  Asynchronous on `cuda_stream`. */
+lq_status lq_adapters_forward(const lq_adapters* set, const lq_rowmap* map, const void* X_f16_dev, const void* Y0_dev, void* Y_dev,
+                              lq_out_dtype dtype, void* cuda_stream);
+
+/* ---- queries and keys behind a projection: norm of each head and rotation by position, in one pass ---------------
+ * (Outside the paper's layer: what an attention block does with the output of its qkv projection.)                  */
+typedef enum {
+  LQ_NORM_NONE = 0,
+  LQ_NORM_RMS = 1,        /* x / sqrt(mean x^2 + eps) * weight                       */
+  LQ_NORM_LAYER = 2       /* (x - mean) / sqrt(var + eps) * weight + bias            */
+} lq_norm;
+
+#define LQ_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t axes;                    /* 0 (no rotation) .. LQ_ROPE_MAX_AXES: e.g. 1 = text, 2 = rows and columns, 3 = time, height, width */
+  int32_t dims[LQ_ROPE_MAX_AXES];  /* entries of a head that turn with each axis: even, >= 0; their sum, rot_dim, is what is rotated;
+                                      the head's other entries, behind them, only see the norm                        */
+  int32_t halves;                  /* 0: pair i is entries (2 i, 2 i + 1); 1: (i, i + rot_dim / 2), rot_dim a multiple of 8 */
+  int32_t shared;                  /* 0: each axis has its own frequencies theta^(-2 j / dims[axis]), j from 0;
+                                      1: pair i has theta^(-2 i / rot_dim), and the axes take dims[axis] / 2 pairs each in turn */
+  double theta;                    /* > 0                                                                             */
+} lq_rope_config;
+
+typedef struct lq_rope lq_rope;    /* opaque: axis and frequency of each pair, on one device                          */
+
+/* Fill *cfg: `axes` axes of dims[0 .. axes - 1] entries (host), neighbouring pairs, frequencies of each axis its own, theta 10000. */
+lq_status lq_rope_config_default(lq_rope_config* cfg, int32_t axes, const int32_t* dims);
+
+/* A table of rotations (synchronous).  freq_host: NULL (frequencies as the configuration says) or rot_dim / 2 finite doubles, radians
+ * a position, pair by pair: scaled or interpolated frequencies.  axis_host: NULL or rot_dim / 2 axes, pair by pair (the configuration's
+ * dims then only give rot_dim).  Frequencies are kept as 64-bit fractions of a turn and multiplied by the position in integers, so an angle is
+ * right to 1e-9 radians at any position. */
+lq_status lq_rope_create(const lq_rope_config* cfg, const double* freq_host, const int32_t* axis_host, int device, lq_rope** out);
+lq_status lq_rope_free(lq_rope* rope);
+
+/* The queries or the keys of a call.  Entry d of head h of row s of sequence b lies at b * seq + s * row + h * head + d elements. */
+typedef struct {
+  const void* in;                          /* device, 16-byte aligned; half or float per in_dtype                     */
+  void* out;                               /* device, 16-byte aligned; half or float per out_dtype; `in` itself, with its strides and
+                                              type, or memory apart from all inputs                                   */
+  int64_t in_seq, in_row, in_head;         /* strides in elements, multiples of 8                                     */
+  int64_t out_seq, out_row, out_head;
+  const float* weight;                     /* [head_dim] device, 16-byte aligned, or NULL (ones); NULL without a norm */
+  const float* bias;                       /* [head_dim] device, 16-byte aligned, or NULL (zeros); LQ_NORM_LAYER only */
+  int32_t heads;                           /* 1 .. 4096                                                               */
+} lq_heads;
+
+/* Norm of each head, then the rotation of its leading rot_dim entries: entries (u, v) of a pair become
+ * (u cos - v sin, v cos + u sin) of the row's angle.  In fp32, rounded once to out_dtype.
+ *   q, k       either may be NULL (no such heads)
+ *   head_dim   a multiple of 8 up to 256, >= rot_dim
+ *   sequences, seq_len   >= 1; rows = sequences * seq_len < 2^31
+ *   pos_dev    [sequences][seq_len][axes] int32, any value, device; ignored (may be NULL) if the table has no axes
+ * Writes nothing but the heads' entries: what lies between them (values of the same rows, say) stays.
+ * Runs on the table's device.  Asynchronous on `cuda_stream`. */
+lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32_t head_dim, int32_t sequences, int32_t seq_len, lq_norm norm, float eps,
+                          const lq_rope* rope, const int32_t* pos_dev, lq_out_dtype in_dtype, lq_out_dtype out_dtype, void* cuda_stream);
+
 /* Decode the activation record of the last lq_quantize_act into plain host arrays (for
  * parity checks); NULL skips a part.  qx int8 [M][K], sx half bits [M][G] (MXINT4: the block
  * exponents e as int16 [M][G], since 2^e may lie below the fp16 range), qb int8 [M][K],

@@ -21,6 +21,7 @@ MAIN_AUTO, MAIN_MXFP4, MAIN_MXINT4_A8 = 0, 2, 3
 ACT_DEFAULT, ACT_MXFP6 = 0, 6
 BRANCH_NAME = {v: k for k, v in BRANCH.items()}
 OUT_F16, OUT_F32 = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 GROUP = 64
 
 
@@ -29,6 +30,16 @@ class LqConfig(C.Structure):
                 ("branch", C.c_int32), ("steps", C.c_int32), ("lr", C.c_float), ("beta1", C.c_float),
                 ("beta2", C.c_float), ("eps", C.c_float), ("rot_steps", C.c_int32), ("rot_lr", C.c_float),
                 ("seed", C.c_uint64), ("main_fmt", C.c_int32), ("act_fmt", C.c_int32)]
+
+
+class LqRopeConfig(C.Structure):
+    _fields_ = [("axes", C.c_int32), ("dims", C.c_int32 * 4), ("halves", C.c_int32), ("shared", C.c_int32), ("theta", C.c_double)]
+
+
+class LqHeads(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("in_seq", C.c_int64), ("in_row", C.c_int64), ("in_head", C.c_int64),
+                ("out_seq", C.c_int64), ("out_row", C.c_int64), ("out_head", C.c_int64), ("weight", C.c_void_p), ("bias", C.c_void_p),
+                ("heads", C.c_int32)]
 
 
 class LqError(RuntimeError):
@@ -56,6 +67,18 @@ _SIGNATURES = {
     "lq_linear_forward_host": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int, C.c_void_p],
     "lq_linear_forward_host_async": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int, C.c_void_p],
     "lq_linear_forward_static": [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int, C.c_void_p],
+    "lq_adapters_create": [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int, C.POINTER(C.c_void_p)],
+    "lq_adapters_set": [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p],
+    "lq_adapters_free": [C.c_void_p],
+    "lq_rowmap_create": [C.c_int32, C.c_int32, C.c_int, C.POINTER(C.c_void_p)],
+    "lq_rowmap_set": [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p],
+    "lq_rowmap_free": [C.c_void_p],
+    "lq_adapters_forward": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p],
+    "lq_rope_config_default": [C.POINTER(LqRopeConfig), C.c_int32, C.c_void_p],
+    "lq_rope_create": [C.POINTER(LqRopeConfig), C.c_void_p, C.c_void_p, C.c_int, C.POINTER(C.c_void_p)],
+    "lq_rope_free": [C.c_void_p],
+    "lq_qk_norm_rope": [C.POINTER(LqHeads), C.POINTER(LqHeads), C.c_int32, C.c_int32, C.c_int32, C.c_int, C.c_float, C.c_void_p,
+                        C.c_void_p, C.c_int, C.c_int, C.c_void_p],
     "lq_act_export": [C.c_void_p] * 8,
     "lq_get_device_status": [C.c_int, C.POINTER(C.c_int32), C.POINTER(C.c_int32)],
     "lq_set_option": [C.c_char_p, C.c_int32],
@@ -251,6 +274,78 @@ def lq_linear_forward_static(layer, X_dev_ptr: int, M: int, Y_dev_ptr: int, dtyp
     Raises LqError(code 2) when M x K does not fit the array; calls must not overlap on the GPU."""
     _check(lib().lq_linear_forward_static(layer, C.c_void_p(X_dev_ptr), M, C.c_void_p(Y_dev_ptr), dtype,
                                           C.c_void_p(stream)), "lq_linear_forward_static")
+
+
+def lq_adapters_create(K: int, N: int, max_rank: int, slots: int, device: int = 0):
+    h = C.c_void_p()
+    _check(lib().lq_adapters_create(K, N, max_rank, slots, device, C.byref(h)), "lq_adapters_create")
+    return h
+
+
+def lq_adapters_set(adapters, slot: int, rank: int, A_dev_ptr: int | None, B_dev_ptr: int | None, scale: float = 1.0, stream: int = 0):
+    """A fp16 [K, rank] and B fp16 [rank, N] on the device; rank 0 empties the slot."""
+    _check(lib().lq_adapters_set(adapters, slot, rank, C.c_void_p(A_dev_ptr), C.c_void_p(B_dev_ptr), scale, C.c_void_p(stream)),
+           "lq_adapters_set")
+
+
+def lq_adapters_free(adapters):
+    _check(lib().lq_adapters_free(adapters), "lq_adapters_free")
+
+
+def lq_rowmap_create(M_max: int, slots: int, device: int = 0):
+    h = C.c_void_p()
+    _check(lib().lq_rowmap_create(M_max, slots, device, C.byref(h)), "lq_rowmap_create")
+    return h
+
+
+def lq_rowmap_set(rowmap, row_adapter_dev_ptr: int, M: int, stream: int = 0):
+    _check(lib().lq_rowmap_set(rowmap, C.c_void_p(row_adapter_dev_ptr), M, C.c_void_p(stream)), "lq_rowmap_set")
+
+
+def lq_rowmap_free(rowmap):
+    _check(lib().lq_rowmap_free(rowmap), "lq_rowmap_free")
+
+
+def lq_adapters_forward(adapters, rowmap, X_dev_ptr: int, Y0_dev_ptr: int, Y_dev_ptr: int, dtype: int = OUT_F16, stream: int = 0):
+    """Y = Y0 + each row's adapter on X; Y may be Y0 itself."""
+    _check(lib().lq_adapters_forward(adapters, rowmap, C.c_void_p(X_dev_ptr), C.c_void_p(Y0_dev_ptr), C.c_void_p(Y_dev_ptr), dtype,
+                                     C.c_void_p(stream)), "lq_adapters_forward")
+
+
+def lq_rope_config_default(dims, theta: float = 10000.0, halves: bool = False, shared: bool = False) -> LqRopeConfig:
+    cfg = LqRopeConfig()
+    d = np.ascontiguousarray(dims, dtype=np.int32)
+    _check(lib().lq_rope_config_default(C.byref(cfg), d.size, _np_ptr(d)), "lq_rope_config_default")
+    cfg.theta, cfg.halves, cfg.shared = theta, int(halves), int(shared)
+    return cfg
+
+
+def lq_rope_create(cfg: LqRopeConfig, device: int = 0, freq: np.ndarray | None = None, axis: np.ndarray | None = None):
+    """freq, axis: host arrays with an entry for each rotated pair, in place of the configuration's."""
+    pairs = sum(cfg.dims[: max(0, min(cfg.axes, 4))]) // 2
+    f = None if freq is None else np.ascontiguousarray(freq, dtype=np.float64)
+    a = None if axis is None else np.ascontiguousarray(axis, dtype=np.int32)
+    assert all(v is None or v.shape == (pairs,) for v in (f, a))
+    h = C.c_void_p()
+    _check(lib().lq_rope_create(C.byref(cfg), _np_ptr(f), _np_ptr(a), device, C.byref(h)), "lq_rope_create")
+    return h
+
+
+def lq_rope_free(rope):
+    _check(lib().lq_rope_free(rope), "lq_rope_free")
+
+
+def lq_heads(in_ptr: int, in_strides, out_ptr: int, out_strides, heads: int, weight_ptr: int | None = None,
+             bias_ptr: int | None = None) -> LqHeads:
+    """The queries or keys of a call; strides of sequence, row and head in elements."""
+    return LqHeads(in_ptr, out_ptr, *in_strides, *out_strides, weight_ptr, bias_ptr, heads)
+
+
+def lq_qk_norm_rope(q: LqHeads | None, k: LqHeads | None, head_dim: int, sequences: int, seq_len: int, norm: int, eps: float, rope,
+                    pos_dev_ptr: int | None, in_dtype: int = OUT_F16, out_dtype: int = OUT_F16, stream: int = 0):
+    ref = lambda h: None if h is None else C.byref(h)
+    _check(lib().lq_qk_norm_rope(ref(q), ref(k), head_dim, sequences, seq_len, norm, eps, rope, C.c_void_p(pos_dev_ptr), in_dtype, out_dtype,
+                                 C.c_void_p(stream)), "lq_qk_norm_rope")
 
 
 def lq_act_export(act, M: int, cfg: LqConfig, stream: int = 0) -> dict:

@@ -1,0 +1,440 @@
+// Low-rank adapters of many requests beside a shared projection:  Y[m] = Y0[m] + scale_a (X[m] A_a) B_a,  a = the adapter of row m.
+//
+// A map sorts the rows of a batch by adapter (stable) and cuts them into tiles of rows of one adapter; every projection of a step
+// uses it.
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+
+#include "lq_device.cuh"
+#include "lq_internal.h"
+
+using namespace lqdev;
+
+namespace {
+
+constexpr int MAX_SLOTS = 1023;      // bins of the sort: the slots and "none"
+constexpr int TILE_ROWS = 16;
+constexpr int CLUSTER = 8, WARPS = 8;
+
+struct Tile {
+  int adapter, begin, rows, pad;     // adapter -1: none; rows are perm[begin] .. perm[begin + rows - 1]
+};
+struct Meta {
+  int rank;                          // 0: empty slot
+  float scale;
+};
+
+}  // namespace
+
+struct lq_adapters {
+  int K, N, Npad, max_rank, rp, slots, device;  // rp: ranks are stored in rows of so many (16, or a multiple of 32); Npad: N rounded up to 32
+  __half* d_down;                    // [slots][rp][K]     column j of A as a row
+  __half* d_up;                      // [slots][Npad][rp]  column n of B as row lq_col32_slot(n)
+  Meta* d_meta;                      // [slots]
+};
+struct lq_rowmap {
+  int M_max, slots, device, M, tiles_max;
+  int* d_ntiles;
+  Tile* d_tiles;                     // [tiles_max]
+  int* d_perm;                       // [M_max]
+};
+
+namespace {
+
+// ---- the map: a stable counting sort in one block ------------------------------------------------------------------------
+// Each of the 32 warps counts the adapters of its own run of rows, then places them behind those of the warps before it.
+__global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int M, int slots, int tile_rows, int* perm, Tile* tiles, int* ntiles) {
+  extern __shared__ int count[];     // [32][slots + 1]
+  __shared__ int scan_rows[32], scan_tiles[32];
+  const int bins = slots + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  for (int i = tid; i < 32 * bins; i += 1024) count[i] = 0;
+  grid_launch_dependents();
+  grid_dependency_wait();
+  __syncthreads();
+  const int run = ((M + 31) / 32 + 31) & ~31;                  // rows a warp: whole loads
+  const long long first = (long long)warp * run;
+  const int last = (int)min((long long)M, first + run);
+  int* mine = count + warp * bins;
+  for (long long r0 = first; r0 < last; r0 += 32) {
+    const int r = (int)r0 + lane;
+    const bool in = r0 + lane < last;
+    const int id = in ? ids[r] : 0, bin = id >= 0 && id < slots ? id : slots;
+    const unsigned live = __ballot_sync(0xffffffffu, in);
+    const unsigned same = __match_any_sync(0xffffffffu, in ? bin : -1) & live;
+    if (in && lane == __ffs(same) - 1) mine[bin] += __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  // thread b: rows and tiles of bin b, and where they begin
+  int rows = 0, nt = 0;
+  if (tid < bins) {
+    for (int w = 0; w < 32; ++w) rows += count[w * bins + tid];
+    nt = (rows + tile_rows - 1) / tile_rows;
+  }
+  int a = rows, b = nt;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int u = __shfl_up_sync(0xffffffffu, a, d), v = __shfl_up_sync(0xffffffffu, b, d);
+    if (lane >= d) { a += u; b += v; }
+  }
+  if (lane == 31) { scan_rows[warp] = a; scan_tiles[warp] = b; }
+  __syncthreads();
+  if (warp == 0) {
+    int u = scan_rows[lane], v = scan_tiles[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int x = __shfl_up_sync(0xffffffffu, u, d), y = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) { u += x; v += y; }
+    }
+    scan_rows[lane] = u; scan_tiles[lane] = v;
+  }
+  __syncthreads();
+  if (tid == 0) *ntiles = scan_tiles[31];
+  if (tid < bins) {
+    int at = a - rows + (warp > 0 ? scan_rows[warp - 1] : 0);
+    const int tile0 = b - nt + (warp > 0 ? scan_tiles[warp - 1] : 0);
+    for (int i = 0; i < nt; ++i)
+      tiles[tile0 + i] = Tile{tid < slots ? tid : -1, at + i * tile_rows, min(tile_rows, rows - i * tile_rows), 0};
+    for (int w = 0; w < 32; ++w) {
+      const int n = count[w * bins + tid];
+      count[w * bins + tid] = at;
+      at += n;
+    }
+  }
+  __syncthreads();
+  for (long long r0 = first; r0 < last; r0 += 32) {
+    const int r = (int)r0 + lane;
+    const bool in = r0 + lane < last;
+    const int id = in ? ids[r] : 0, bin = id >= 0 && id < slots ? id : slots;
+    const unsigned live = __ballot_sync(0xffffffffu, in);
+    const unsigned same = __match_any_sync(0xffffffffu, in ? bin : -1) & live;
+    const int at = in ? mine[bin] + __popc(same & ((1u << lane) - 1)) : 0;
+    __syncwarp();
+    if (in) {
+      perm[at] = r;
+      if (lane == __ffs(same) - 1) mine[bin] += __popc(same);
+    }
+    __syncwarp();
+  }
+}
+
+// ---- a slot's new adapter in the forwards' layouts ----------------------------------------------------------------------
+__global__ void __launch_bounds__(256) lq_adapters_set_kernel(__half* down, __half* up, Meta* meta, const __half* A, const __half* B, int K, int N, int Npad,
+                                                              int rp, int rank, float scale) {
+  grid_dependency_wait();            // (no launch_dependents: what follows sees the adapter whole)
+  const long long n_down = (long long)rp * K, n_up = (long long)Npad * rp, step = (long long)gridDim.x * blockDim.x;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n_down + n_up; i += step) {
+    if (i < n_down) {
+      const int j = (int)(i / K), k = (int)(i - (long long)j * K);
+      down[i] = j < rank ? A[(long long)k * rank + j] : __half(0.f);
+    } else {
+      const long long e = i - n_down;
+      const int s = (int)(e / rp), j = (int)(e - (long long)s * rp);
+      const int n = (s & ~31) | (((s >> 3) & 3) << 1) | (((s >> 1) & 3) << 3) | (s & 1);      // the column whose slot is s: the map is its own inverse
+      up[e] = j < rank && n < N ? B[(long long)j * N + n] : __half(0.f);
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *meta = Meta{rank, scale};
+}
+
+// ---- fragments ---------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The order of a product's inner index is free as long as both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7
+// of each 32, so that a fragment of either operand is one 16-byte load from rows that run along the inner index.
+template <int RP>
+__global__ void __launch_bounds__(32 * WARPS) lq_adapters_kernel(const Tile* tiles, const int* ntiles, const int* perm, const __half* X, const void* Y0,
+                                                                 void* Y, const __half* down, const __half* up, const Meta* meta, int K, int N, int Npad,
+                                                                 int out_f32) {
+  constexpr int NT = RP / 8, KB = (RP + 31) / 32;
+  extern __shared__ __align__(16) float smem[];
+  float* red = smem;                                      // [WARPS][16][RP]
+  float* part = red + WARPS * 16 * RP;                    // [16][RP] this CTA's share of K
+  __half* tq = reinterpret_cast<__half*>(part + 16 * RP); // [2][16][KB * 32]: hi, lo
+  float* row_scale = reinterpret_cast<float*>(tq + 2 * 16 * KB * 32);   // [16]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int rank_in_cluster = blockIdx.x % CLUSTER, ti = blockIdx.x / CLUSTER;
+  grid_launch_dependents();
+  grid_dependency_wait();
+  if (ti >= *ntiles) return;                              // (the whole cluster)
+  const Tile tile = tiles[ti];
+  const Meta m = tile.adapter >= 0 ? meta[tile.adapter] : Meta{0, 0.f};
+  const int unit = warp * CLUSTER + rank_in_cluster, units = WARPS * CLUSTER;
+  const bool has0 = g < tile.rows, has1 = g + 8 < tile.rows;
+  const long long row0 = has0 ? perm[tile.begin + g] : 0, row1 = has1 ? perm[tile.begin + g + 8] : 0;
+  if (m.rank == 0 && Y == Y0) return;
+
+  float c[NT][4];
+  if (m.rank > 0) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
+    const __half* A = down + (long long)tile.adapter * RP * K;
+    for (int kb = unit; kb * 32 < K; kb += units) {
+      const int k = kb * 32 + 8 * t;
+      const uint4 zero = make_uint4(0, 0, 0, 0);
+      const bool in = k < K;
+      const uint4 x0 = in && has0 ? *reinterpret_cast<const uint4*>(X + row0 * K + k) : zero;
+      const uint4 x1 = in && has1 ? *reinterpret_cast<const uint4*>(X + row1 * K + k) : zero;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        if (n * 8 < m.rank) {
+          const uint4 b = in ? *reinterpret_cast<const uint4*>(A + (long long)(8 * n + g) * K + k) : zero;
+          mma_16816(c[n], x0.x, x1.x, x0.y, x1.y, b.x, b.y);
+          mma_16816(c[n], x0.z, x1.z, x0.w, x1.w, b.z, b.w);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      *reinterpret_cast<float2*>(red + (warp * 16 + g) * RP + 8 * n + 2 * t) = make_float2(c[n][0], c[n][1]);
+      *reinterpret_cast<float2*>(red + (warp * 16 + g + 8) * RP + 8 * n + 2 * t) = make_float2(c[n][2], c[n][3]);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * RP; i += 32 * WARPS) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) s += red[w * 16 * RP + i];
+      part[i] = s;
+    }
+    cluster_sync();
+    // every CTA adds up the whole intermediate, always in the same order, two rows a warp
+    for (int r = 2 * warp; r < 2 * warp + 2; ++r) {
+      float v[KB];
+      float top = 0.f;
+#pragma unroll
+      for (int q = 0; q < KB; ++q) {
+        const int j = 32 * q + lane;
+        v[q] = 0.f;
+        if (j < RP)
+#pragma unroll
+          for (int w = 0; w < CLUSTER; ++w) {
+            float u;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(peer_smem(smem_u32(part + r * RP + j), w)) : "memory");
+            v[q] += u;
+          }
+        top = fmaxf(top, fabsf(v[q]));
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      // the row's largest magnitude comes to lie in [2^14, 2^15): no half overflows, and hi + lo keep 22 bits of it
+      int e = 0;
+      if (top > 0.f && top < INFINITY) frexpf(top, &e);
+      e = max(-100, min(100, 15 - e));
+      if (lane == 0) row_scale[r] = ldexpf(m.scale, -e);
+#pragma unroll
+      for (int q = 0; q < KB; ++q) {
+        const float u = ldexpf(v[q], e);
+        const __half hi = __float2half_rn(u);
+        tq[r * KB * 32 + 32 * q + lane] = hi;
+        tq[(16 + r) * KB * 32 + 32 * q + lane] = __float2half_rn(u - __half2float(hi));
+      }
+    }
+    cluster_arrive<false>();                              // this CTA has read the others' shares
+    __syncthreads();
+  }
+  const float s0 = m.rank > 0 ? row_scale[g] : 0.f, s1 = m.rank > 0 ? row_scale[g + 8] : 0.f;
+  const __half* Bu = up + (long long)max(tile.adapter, 0) * Npad * RP;
+  for (int cg = unit; cg * 32 < N; cg += units) {
+    float d[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
+    if (m.rank > 0) {
+#pragma unroll
+      for (int q = 0; q < KB; ++q)
+        if (32 * q < m.rank) {
+          uint4 b[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const __half* src = Bu + (long long)(32 * cg + 8 * j + g) * RP + 32 * q;
+            if constexpr (RP == 16) {                     // half a block: four neighbours a lane
+              const uint2 v = *reinterpret_cast<const uint2*>(src + 4 * t);
+              b[j] = make_uint4(v.x, v.y, 0, 0);
+            } else {
+              b[j] = *reinterpret_cast<const uint4*>(src + 8 * t);
+            }
+          }
+#pragma unroll
+          for (int part_of = 0; part_of < 2; ++part_of) {
+            const __half* a0p = tq + (16 * part_of + g) * KB * 32 + 32 * q + (RP == 16 ? 4 : 8) * t;
+            const __half* a1p = a0p + 8 * KB * 32;
+            if constexpr (RP == 16) {
+              const uint2 a0 = *reinterpret_cast<const uint2*>(a0p), a1 = *reinterpret_cast<const uint2*>(a1p);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma_16816(d[j], a0.x, a1.x, a0.y, a1.y, b[j].x, b[j].y);
+            } else {
+              const uint4 a0 = *reinterpret_cast<const uint4*>(a0p), a1 = *reinterpret_cast<const uint4*>(a1p);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                mma_16816(d[j], a0.x, a1.x, a0.y, a1.y, b[j].x, b[j].y);
+                mma_16816(d[j], a0.z, a1.z, a0.w, a1.w, b[j].z, b[j].w);
+              }
+            }
+          }
+        }
+    }
+    const int n = 32 * cg + 8 * t;                        // this lane's eight columns
+    if (n < N)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (h ? has1 : has0) {
+          const long long at = (h ? row1 : row0) * N + n;
+          const float s = h ? s1 : s0;
+          if (out_f32) {
+            const float4* y0 = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(Y0) + at);
+            float4 a = y0[0], b = y0[1];
+            if (m.rank > 0) {                             // (a row without an adapter keeps its bits)
+              a.x = fmaf(s, d[0][2 * h], a.x); a.y = fmaf(s, d[0][2 * h + 1], a.y); a.z = fmaf(s, d[1][2 * h], a.z); a.w = fmaf(s, d[1][2 * h + 1], a.w);
+              b.x = fmaf(s, d[2][2 * h], b.x); b.y = fmaf(s, d[2][2 * h + 1], b.y); b.z = fmaf(s, d[3][2 * h], b.z); b.w = fmaf(s, d[3][2 * h + 1], b.w);
+            }
+            float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(Y) + at);
+            o[0] = a; o[1] = b;
+          } else {
+            uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(Y0) + at);
+            __half2* w = reinterpret_cast<__half2*>(&v);
+            if (m.rank > 0)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float2 f = __half22float2(w[j]);
+                w[j] = __floats2half2_rn(fmaf(s, d[j][2 * h], f.x), fmaf(s, d[j][2 * h + 1], f.y));
+              }
+            *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(Y) + at) = v;
+          }
+        }
+  }
+  if (m.rank > 0) cluster_wait();                         // the others have read this CTA's share
+}
+
+size_t forward_smem(int rp) {
+  const int kb = (rp + 31) / 32;
+  return (size_t)(WARPS + 1) * 16 * rp * 4 + 2 * 16 * kb * 32 * 2 + 16 * 4;
+}
+template <int RP>
+cudaError_t launch_forward(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
+  const int tiles = std::min(R->M, lq_ceil_div(R->M, TILE_ROWS) + R->slots);
+  return lq_launch_cluster(lq_adapters_kernel<RP>, tiles * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st, (const Tile*)R->d_tiles, (const int*)R->d_ntiles,
+                           (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up, (const Meta*)S->d_meta, S->K,
+                           S->N, S->Npad, dt == LQ_OUT_F32 ? 1 : 0);
+}
+
+}  // namespace
+
+extern "C" lq_status lq_adapters_create(int32_t K, int32_t N, int32_t max_rank, int32_t slots, int device, lq_adapters** out) {
+  if (!out || K <= 0 || N <= 0 || max_rank <= 0 || slots <= 0) return LQ_ERR_INVALID_ARG;
+  if (K > LQ_MAX_K || K % 8 != 0 || N % 8 != 0 || N > (1 << 20) || max_rank > LQ_MAX_RANK || slots > MAX_SLOTS) return LQ_ERR_UNSUPPORTED;
+  int ndev = 0;
+  if (lq_note_cuda(cudaGetDeviceCount(&ndev)) != cudaSuccess || device < 0 || device >= ndev) return LQ_ERR_CUDA;
+  LqDeviceGuard guard(device);
+  if (!guard.ok) return LQ_ERR_CUDA;
+  lq_adapters* S = new (std::nothrow) lq_adapters();
+  if (!S) return LQ_ERR_ALLOC;
+  S->K = K; S->N = N; S->Npad = lq_round_up(N, 32); S->max_rank = max_rank; S->slots = slots; S->device = device;
+  S->rp = max_rank <= 16 ? 16 : lq_round_up(max_rank, 32);
+  const size_t n_down = (size_t)slots * S->rp * K, n_up = (size_t)slots * S->Npad * S->rp;
+  if (lq_note_cuda(cudaMalloc((void**)&S->d_down, n_down * 2)) != cudaSuccess || lq_note_cuda(cudaMalloc((void**)&S->d_up, n_up * 2)) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&S->d_meta, slots * sizeof(Meta))) != cudaSuccess) {
+    lq_adapters_free(S);
+    return LQ_ERR_ALLOC;
+  }
+  // (what the factors of an empty slot hold is never read)
+  if (lq_note_cuda(cudaMemset(S->d_meta, 0, slots * sizeof(Meta))) != cudaSuccess || lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess) {
+    lq_adapters_free(S);
+    return LQ_ERR_CUDA;
+  }
+  *out = S;
+  return LQ_OK;
+}
+
+extern "C" lq_status lq_adapters_free(lq_adapters* S) {
+  if (!S) return LQ_ERR_INVALID_ARG;
+  LqDeviceGuard guard(S->device);
+  cudaFree(S->d_down); cudaFree(S->d_up); cudaFree(S->d_meta);
+  delete S;
+  return LQ_OK;
+}
+
+extern "C" lq_status lq_adapters_set(lq_adapters* S, int32_t slot, int32_t rank, const void* A, const void* B, float scale, void* stream) {
+  if (!S || slot < 0 || slot >= S->slots || rank < 0) return LQ_ERR_INVALID_ARG;
+  if (rank > S->max_rank) return LQ_ERR_UNSUPPORTED;
+  if (rank > 0 && (!A || !B || (((uintptr_t)A | (uintptr_t)B) & 1) != 0)) return LQ_ERR_INVALID_ARG;
+  if (!isfinite(scale)) return LQ_ERR_NUMERIC;
+  LqDeviceGuard guard(S->device);
+  if (!guard.ok) return LQ_ERR_CUDA;
+  if (rank == 0)                     // nothing to lay out
+    return lq_note_cuda(cudaMemsetAsync(S->d_meta + slot, 0, sizeof(Meta), (cudaStream_t)stream)) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+  const int blocks = (int)std::min(((long long)S->rp * (S->K + S->Npad) + 255) / 256, 4096ll);
+  const size_t at = (size_t)slot * S->rp;
+  const cudaError_t e = lq_launch(lq_adapters_set_kernel, blocks, 256, 0, (cudaStream_t)stream, S->d_down + at * S->K, S->d_up + at * S->Npad, S->d_meta + slot,
+                                  (const __half*)A, (const __half*)B, S->K, S->N, S->Npad, S->rp, rank, scale);
+  return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+}
+
+extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, lq_rowmap** out) {
+  if (!out || M_max <= 0 || slots <= 0) return LQ_ERR_INVALID_ARG;
+  if (slots > MAX_SLOTS || M_max > (1 << 24)) return LQ_ERR_UNSUPPORTED;
+  int ndev = 0;
+  if (lq_note_cuda(cudaGetDeviceCount(&ndev)) != cudaSuccess || device < 0 || device >= ndev) return LQ_ERR_CUDA;
+  LqDeviceGuard guard(device);
+  if (!guard.ok) return LQ_ERR_CUDA;
+  lq_rowmap* R = new (std::nothrow) lq_rowmap();
+  if (!R) return LQ_ERR_ALLOC;
+  R->M_max = M_max; R->slots = slots; R->device = device; R->M = 0;
+  R->tiles_max = lq_ceil_div(M_max, TILE_ROWS) + slots + 1;
+  if (lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, sizeof(int))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_tiles, (size_t)R->tiles_max * sizeof(Tile))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_perm, (size_t)M_max * sizeof(int))) != cudaSuccess) {
+    lq_rowmap_free(R);
+    return LQ_ERR_ALLOC;
+  }
+  if (lq_note_cuda(cudaFuncSetAttribute(lq_rowmap_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * (MAX_SLOTS + 1) * 4)) != cudaSuccess ||
+      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(16))) != cudaSuccess ||
+      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(32))) != cudaSuccess ||
+      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(64))) != cudaSuccess ||
+      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<96>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(96))) != cudaSuccess ||
+      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(128))) != cudaSuccess) {
+    lq_rowmap_free(R);
+    return LQ_ERR_CUDA;
+  }
+  *out = R;
+  return LQ_OK;
+}
+
+extern "C" lq_status lq_rowmap_free(lq_rowmap* R) {
+  if (!R) return LQ_ERR_INVALID_ARG;
+  LqDeviceGuard guard(R->device);
+  cudaFree(R->d_ntiles); cudaFree(R->d_tiles); cudaFree(R->d_perm);
+  delete R;
+  return LQ_OK;
+}
+
+extern "C" lq_status lq_rowmap_set(lq_rowmap* R, const int32_t* ids, int32_t M, void* stream) {
+  if (!R || !ids || M <= 0 || M > R->M_max || ((uintptr_t)ids & 3) != 0) return LQ_ERR_INVALID_ARG;
+  LqDeviceGuard guard(R->device);
+  if (!guard.ok) return LQ_ERR_CUDA;
+  const cudaError_t e = lq_launch(lq_rowmap_kernel, 1, 1024, (size_t)32 * (R->slots + 1) * 4, (cudaStream_t)stream, ids, M, R->slots, TILE_ROWS, R->d_perm,
+                                  R->d_tiles, R->d_ntiles);
+  if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
+  R->M = M;
+  return LQ_OK;
+}
+
+extern "C" lq_status lq_adapters_forward(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, void* stream) {
+  if (!S || !R || !X || !Y0 || !Y) return LQ_ERR_INVALID_ARG;
+  if (S->device != R->device || R->slots > S->slots || R->M <= 0) return LQ_ERR_INVALID_ARG;
+  if (dt != LQ_OUT_F16 && dt != LQ_OUT_F32) return LQ_ERR_INVALID_ARG;
+  if ((((uintptr_t)X | (uintptr_t)Y0 | (uintptr_t)Y) & 15) != 0) return LQ_ERR_INVALID_ARG;
+  LqDeviceGuard guard(S->device);
+  if (!guard.ok) return LQ_ERR_CUDA;
+  cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = S->rp == 16   ? launch_forward<16>(S, R, X, Y0, Y, dt, st)
+                        : S->rp == 32 ? launch_forward<32>(S, R, X, Y0, Y, dt, st)
+                        : S->rp == 64 ? launch_forward<64>(S, R, X, Y0, Y, dt, st)
+                        : S->rp == 96 ? launch_forward<96>(S, R, X, Y0, Y, dt, st)
+                                      : launch_forward<128>(S, R, X, Y0, Y, dt, st);
+  return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+}

@@ -160,6 +160,19 @@ struct lq_act {
 // remembers the last failing CUDA runtime code (per host thread) for lq_last_cuda_error(); returns its argument
 cudaError_t lq_note_cuda(cudaError_t e);
 
+// Makes `device` the calling thread's current one and puts the one before back at the end of the scope.
+struct LqDeviceGuard {
+  int before = -1;
+  bool ok;
+  explicit LqDeviceGuard(int device) {
+    ok = lq_note_cuda(cudaGetDevice(&before)) == cudaSuccess && (before == device || lq_note_cuda(cudaSetDevice(device)) == cudaSuccess);
+    if (before == device) before = -1;
+  }
+  ~LqDeviceGuard() { if (before >= 0) cudaSetDevice(before); }
+  LqDeviceGuard(const LqDeviceGuard&) = delete;
+  LqDeviceGuard& operator=(const LqDeviceGuard&) = delete;
+};
+
 // device status word (one per device, allocated on first use): {code, stage}
 int32_t* lq_device_status_ptr(int device);
 

@@ -1,0 +1,281 @@
+"""Low-rank adapters of many requests beside a projection, against the formula in 64 bits."""
+import numpy as np
+import pytest
+
+from paper_2604_18117_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+class Set:
+    """Adapters on the GPU (scales and ranks of their own) with the same factors on the host."""
+
+    def __init__(self, rng, K, N, max_rank, ranks, scales=None, slots=None):
+        import torch
+        self.K, self.N, self.ranks = K, N, list(ranks)
+        self.scales = [1.0 + 0.25 * i for i in range(len(ranks))] if scales is None else scales
+        self.h = B.lq_adapters_create(K, N, max_rank, slots or len(ranks), 0)
+        self.A = [(rng.standard_normal((K, r)) * 0.2 / np.sqrt(K)).astype(np.float16) for r in ranks]
+        self.B = [(rng.standard_normal((r, N)) * 0.3).astype(np.float16) for r in ranks]
+        st = torch.cuda.current_stream().cuda_stream
+        for s, r in enumerate(ranks):
+            self.put(s, self.A[s], self.B[s], self.scales[s], st)
+        torch.cuda.synchronize()
+
+    def put(self, slot, A, Bf, scale, stream):
+        import torch
+        self.A[slot], self.B[slot], self.scales[slot], self.ranks[slot] = A, Bf, scale, A.shape[1]
+        self.kept = [torch.from_numpy(A).cuda(), torch.from_numpy(Bf).cuda()]
+        B.lq_adapters_set(self.h, slot, A.shape[1], self.kept[0].data_ptr(), self.kept[1].data_ptr(), scale, stream)
+        torch.cuda.synchronize()
+
+    def free(self):
+        B.lq_adapters_free(self.h)
+
+
+def reference(S, X, Y0, ids, f32):
+    """Y in 64 bits and how far an element may be from it.  Steps of the path, each with its roundings: sums over K on the tensor core (an addition may
+    cut 2^-23 of the partial sum; ceil(K / 16) of them and 24 more where warps and blocks are joined), two halves of the intermediate (2^-22 of the row's
+    largest), sums over the rank (two products a 16), the scale and the last sum in fp32, one rounding to the output's type."""
+    X64, Y = X.astype(np.float64), Y0.astype(np.float64)
+    err = np.zeros_like(Y)
+    for a, r in enumerate(S.ranks):
+        rows = np.nonzero(ids == a)[0]
+        if r == 0 or rows.size == 0:
+            continue
+        A, Bf, s = S.A[a].astype(np.float64), S.B[a].astype(np.float64), float(np.float32(S.scales[a]))
+        T = X64[rows] @ A
+        dT = (np.ceil(S.K / 16) + 24) * 2.0 ** -23 * (np.abs(X64[rows]) @ np.abs(A)) + 2.0 ** -22 * np.abs(T).max(1, keepdims=True)
+        Y[rows] += s * (T @ Bf)
+        err[rows] = abs(s) * (dT @ np.abs(Bf) + (2 * np.ceil(r / 16) + 4) * 2.0 ** -23 * (np.abs(T) @ np.abs(Bf)))
+    err += 2.0 ** -23 * np.abs(Y)
+    return Y, err + ((np.abs(Y) + err) * 2.0 ** -24 if f32 else (np.abs(Y) + err) * 2.0 ** -11 + 2.0 ** -25)
+
+
+def forward(S, ids, X, Y0, f32, in_place=False, slots=None, M_max=None, rowmap=None):
+    import torch
+    M = X.shape[0]
+    m = rowmap or B.lq_rowmap_create(M_max or M, slots or len(S.ranks), 0)
+    st = torch.cuda.current_stream().cuda_stream
+    i, x, y0 = torch.from_numpy(ids.astype(np.int32)).cuda(), torch.from_numpy(X).cuda(), torch.from_numpy(Y0).cuda()
+    room = torch.full((M + 3, S.N), 7.0, dtype=y0.dtype, device="cuda")       # rows behind the last one are left alone
+    if in_place:
+        room[:M] = y0
+        y0 = room
+    B.lq_rowmap_set(m, i.data_ptr(), M, st)
+    B.lq_adapters_forward(S.h, m, x.data_ptr(), y0.data_ptr(), room.data_ptr(), B.OUT_F32 if f32 else B.OUT_F16, st)
+    torch.cuda.synchronize()
+    if rowmap is None:
+        B.lq_rowmap_free(m)
+    out = room.cpu().numpy()
+    assert (out[M:] == 7).all()
+    assert B.lq_get_device_status(0)[0] == 0
+    return out[:M]
+
+
+def inputs(rng, M, K, N, f32):
+    X = rng.standard_normal((M, K)).astype(np.float32)
+    X[:, rng.permutation(K)[:8]] *= 20
+    return X.astype(np.float16), rng.standard_normal((M, N)).astype(np.float32 if f32 else np.float16)
+
+
+@pytest.mark.parametrize("M,K,N,ranks,runs,f32", [
+    (1, 8, 8, [1], 1, True),
+    (1, 1152, 1152, [16, 16], 1, False),
+    (2, 40, 24, [3], 0, True),
+    (15, 1160, 2312, [24, 7, 1], 0, True),
+    (16, 256, 32, [128, 64], 1, False),
+    (17, 264, 40, [128, 100], 0, True),
+    (33, 8192, 64, [96, 33], 0, False),
+    (64, 512, 1000, [32] * 64, 0, False),
+    (127, 1152, 136, [16], 1, True),
+    (129, 640, 8192, [13, 48], 3, False),
+    (300, 72, 520, [64, 17, 128], 2, True),
+    (1000, 1152, 1152, [32, 8, 32], 5, False),
+    (1365, 1160, 2312, [24, 12, 18, 1], 0, True),
+    (2500, 96, 72, [32] * 40, 0, False),
+    (4096, 2240, 256, [128, 64], 4, True),
+    (5000, 136, 344, [16, 1], 7, False),
+])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rows_against_64_bits(M, K, N, ranks, runs, f32, in_place):
+    rng = np.random.default_rng(M * 7 + K)
+    S = Set(rng, K, N, max(ranks), ranks)
+    X, Y0 = inputs(rng, M, K, N, f32)
+    ids = np.arange(M) * runs // M % len(ranks) if runs else rng.permutation(np.arange(M) % len(ranks))
+    if M > 10 and M % 2:                                   # some rows without an adapter
+        ids[rng.random(M) < 0.2] = -1
+        ids[rng.random(M) < 0.05] = len(ranks) + 3         # outside the slots: none either
+    Y = forward(S, ids, X, Y0, f32, in_place)
+    S.free()
+    ref, bound = reference(S, X, Y0, ids, f32)
+    none = (ids < 0) | (ids >= len(ranks))
+    assert np.array_equal(Y[none], Y0[none])               # to the bit
+    over = np.abs(Y - ref) - bound
+    assert over.max() <= 0, (over.max(), np.unravel_index(over.argmax(), Y.shape))
+
+
+def test_every_element_is_where_it_belongs():
+    """Factors with one entry each pick a single input for a single output: no permutation of either inner order may show."""
+    import torch
+    K, N, r = 264, 200, 40
+    rng = np.random.default_rng(5)
+    S = Set(rng, K, N, r, [r], scales=[2.0])
+    X = rng.integers(-30, 30, (70, K)).astype(np.float16)
+    Y0 = np.zeros((70, N), np.float32)
+    for k, j, n in [(0, 0, 0), (263, 39, 199), (31, 8, 33), (32, 31, 7), (100, 32, 64), (7, 17, 95)]:
+        A, Bf = np.zeros((K, r), np.float16), np.zeros((r, N), np.float16)
+        A[k, j], Bf[j, n] = 1, 1
+        S.put(0, A, Bf, 2.0, torch.cuda.current_stream().cuda_stream)
+        Y = forward(S, np.zeros(70, int), X, Y0, True)
+        want = np.zeros_like(Y0)
+        want[:, n] = 2 * X[:, k]
+        assert np.array_equal(Y, want), (k, j, n)
+    S.free()
+
+
+def test_wide_magnitudes_neither_overflow_nor_vanish():
+    """An intermediate beyond the halves' range, and one far below it: the row's power of two carries both."""
+    import torch
+    rng = np.random.default_rng(11)
+    K, N = 1024, 64
+    for f in (1.0, 2.0 ** -20):
+        S = Set(rng, K, N, 16, [16], scales=[2.0 ** -8])
+        S.put(0, (rng.standard_normal((K, 16)) * 40 * f).astype(np.float16), S.B[0], 2.0 ** -8, torch.cuda.current_stream().cuda_stream)
+        X = (rng.standard_normal((40, K)) * 200).astype(np.float16)
+        X[7] = np.clip(X[7].astype(np.float32) * 100, -60000, 60000)      # rows side by side, each with its own scale
+        X[8] = 0
+        Y0 = np.zeros((40, N), np.float32)
+        Y = forward(S, np.zeros(40, int), X, Y0, True)
+        ref, bound = reference(S, X, Y0, np.zeros(40, int), True)
+        assert np.abs(X.astype(np.float64) @ S.A[0].astype(np.float64)).max() > 65504 * f
+        assert (np.abs(Y - ref) <= bound).all() and not Y[8].any()
+        S.free()
+
+
+def test_a_slot_is_replaced_and_emptied_in_stream_order():
+    import torch
+    rng = np.random.default_rng(2)
+    K, N, M = 128, 96, 50
+    S = Set(rng, K, N, 32, [32, 8], slots=5)
+    X, Y0 = inputs(rng, M, K, N, True)
+    ids = np.arange(M) % 4                                 # slots 2 and 3 have never been filled
+    first = forward(S, ids, X, Y0, True, slots=5)
+    assert np.array_equal(first[ids >= 2], Y0[ids >= 2])
+    A, Bf = (rng.standard_normal((K, 20)) * 0.1).astype(np.float16), rng.standard_normal((20, N)).astype(np.float16)
+    S.put(1, A, Bf, -0.5, torch.cuda.current_stream().cuda_stream)      # a lower and then a higher rank than before
+    again = forward(S, ids, X, Y0, True, slots=5)
+    ref, bound = reference(S, X, Y0, ids, True)
+    assert np.array_equal(again[ids != 1], first[ids != 1]) and (np.abs(again - ref) <= bound).all()
+    B.lq_adapters_set(S.h, 0, 0, None, None, 1.0, torch.cuda.current_stream().cuda_stream)
+    S.ranks[0] = 0
+    last = forward(S, ids, X, Y0, True, slots=5)
+    assert np.array_equal(last[ids != 1], Y0[ids != 1]) and np.array_equal(last[ids == 1], again[ids == 1])
+    S.free()
+
+
+def test_equal_calls_give_equal_bits_and_a_map_is_used_again():
+    rng = np.random.default_rng(3)
+    S = Set(rng, 1152, 576, 32, [32, 16, 8])
+    m = B.lq_rowmap_create(3000, 3, 0)
+    got = []
+    for M in (3000, 70, 1, 2000, 70, 3000):
+        r = np.random.default_rng(M)
+        X, Y0 = inputs(r, M, 1152, 576, False)
+        ids = r.integers(-1, 3, M)
+        Y = forward(S, ids, X, Y0, False, rowmap=m)
+        ref, bound = reference(S, X, Y0, ids, False)
+        assert (np.abs(Y - ref) <= bound).all(), M
+        got.append(Y)
+    assert np.array_equal(got[0], got[5]) and np.array_equal(got[1], got[4])
+    B.lq_rowmap_free(m)
+    S.free()
+
+
+def test_captured_calls_follow_the_array_that_they_read():
+    """A graph that sorts and adds: each replay goes by what the row array and the inputs hold by then."""
+    import torch
+    rng = np.random.default_rng(4)
+    K, N, M = 640, 320, 600
+    S = Set(rng, K, N, 32, [32, 16, 24])
+    m = B.lq_rowmap_create(M, 3, 0)
+    ids = torch.zeros(M, dtype=torch.int32, device="cuda")
+    x, y0, y = (torch.zeros(M, c, dtype=torch.float16, device="cuda") for c in (K, N, N))
+    side = torch.cuda.Stream()
+
+    def call(st):
+        B.lq_rowmap_set(m, ids.data_ptr(), M, st)
+        B.lq_adapters_forward(S.h, m, x.data_ptr(), y0.data_ptr(), y.data_ptr(), B.OUT_F16, st)
+
+    side.wait_stream(torch.cuda.current_stream())
+    call(side.cuda_stream)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(torch.cuda.current_stream().cuda_stream)
+    for seed in range(3):
+        r = np.random.default_rng(seed)
+        X, Y0 = inputs(r, M, K, N, False)
+        i = r.integers(-1, 3, M) if seed else np.zeros(M, int)
+        ids.copy_(torch.from_numpy(i.astype(np.int32)))
+        x.copy_(torch.from_numpy(X))
+        y0.copy_(torch.from_numpy(Y0))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        ref, bound = reference(S, X, Y0, i, False)
+        assert (np.abs(y.cpu().numpy() - ref) <= bound).all(), seed
+    del graph
+    B.lq_rowmap_free(m)
+    S.free()
+
+
+def test_a_nan_in_one_row_stays_there():
+    rng = np.random.default_rng(6)
+    S = Set(rng, 320, 160, 16, [16])
+    for M in (20, 700):
+        X, Y0 = inputs(rng, M, 320, 160, True)
+        ids = np.zeros(M, int)
+        ids[3] = -1
+        X[5, 100] = np.nan
+        X[3] = np.inf                                      # no adapter: never looked at
+        Y = forward(S, ids, X, Y0, True)
+        bad = ~np.isfinite(Y).all(1)
+        assert bad[5] and bad.sum() == 1
+    S.free()
+
+
+def test_refusals():
+    import torch
+    S = Set(np.random.default_rng(1), 64, 64, 20, [8, 8])
+    m, big = B.lq_rowmap_create(10, 2, 0), B.lq_rowmap_create(10, 3, 0)
+    x = torch.zeros(64, 64, dtype=torch.float16, device="cuda")
+    i = torch.zeros(16, dtype=torch.int32, device="cuda")
+    P = x.data_ptr()
+
+    def code(f, *a):
+        with pytest.raises(B.LqError) as e:
+            f(*a)
+        return e.value.code
+
+    assert code(B.lq_adapters_forward, S.h, m, P, P, P, B.OUT_F16, 0) == 1            # the map holds no rows yet
+    assert code(B.lq_rowmap_set, m, i.data_ptr(), 11, 0) == 1                         # more rows than it was made for
+    assert code(B.lq_rowmap_set, m, i.data_ptr(), 0, 0) == 1
+    assert code(B.lq_rowmap_set, m, i.data_ptr() + 2, 4, 0) == 1
+    assert code(B.lq_rowmap_set, m, None, 4, 0) == 1
+    for r in (m, big):
+        B.lq_rowmap_set(r, i.data_ptr(), 4, 0)
+    assert code(B.lq_adapters_forward, S.h, big, P, P, P, B.OUT_F16, 0) == 1          # a map of more slots than the set has
+    assert code(B.lq_adapters_forward, S.h, m, P, P, P, 2, 0) == 1
+    for bad in ((P + 8, P, P), (P, P + 2, P), (P, P, P + 4), (None, P, P), (P, None, P), (P, P, None)):
+        assert code(B.lq_adapters_forward, S.h, m, *bad, B.OUT_F16, 0) == 1
+    assert code(B.lq_adapters_set, S.h, 2, 8, P, P, 1.0, 0) == 1                      # no such slot
+    assert code(B.lq_adapters_set, S.h, -1, 8, P, P, 1.0, 0) == 1
+    assert code(B.lq_adapters_set, S.h, 0, -1, P, P, 1.0, 0) == 1
+    assert code(B.lq_adapters_set, S.h, 0, 21, P, P, 1.0, 0) == 2                     # above max_rank
+    assert code(B.lq_adapters_set, S.h, 0, 8, None, P, 1.0, 0) == 1
+    assert code(B.lq_adapters_set, S.h, 0, 8, P, P, float("nan"), 0) == 6
+    torch.cuda.synchronize()
+    for r in (m, big):
+        B.lq_rowmap_free(r)
+    S.free()

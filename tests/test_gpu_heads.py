@@ -1,0 +1,238 @@
+"""Norms of queries and keys with the rotation by position, against the formulas in 64 bits."""
+import numpy as np
+import pytest
+
+from paper_2604_18117_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+NORMS = {"none": B.NORM_NONE, "rms": B.NORM_RMS, "layer": B.NORM_LAYER}
+
+
+def frequencies(dims, theta, shared):
+    rot = sum(dims)
+    axis = np.concatenate([np.full(d // 2, a, int) for a, d in enumerate(dims)]) if rot else np.zeros(0, int)
+    if shared:
+        return axis, theta ** (-2.0 * np.arange(rot // 2) / max(rot, 1))
+    return axis, np.concatenate([theta ** (-2.0 * np.arange(d // 2) / max(d, 1)) for d in dims]) if rot else np.zeros(0)
+
+
+def reference(x, w, b, norm, eps, axis, freq, halves, pos, f32_out):
+    """x [B, S, H, D], pos [B, S, axes] -> (y in 64 bits, how far an element may be from it).  With u = 2^-24: a sum of D squares is within D u, so a
+    normed value within (D / 2 + 8) u of itself (and, with a mean, that much of the mean magnitude, times the scale); cosine and sine are within 4 u of
+    theirs; a turned value is two products and a sum."""
+    u, D = 2.0 ** -24, x.shape[-1]
+    x = x.astype(np.float64)
+    err = np.zeros_like(x)
+    if norm != "none":
+        w64 = np.ones(D) if w is None else w.astype(np.float64)
+        m = x.mean(-1, keepdims=True) if norm == "layer" else 0.0
+        rstd = 1 / np.sqrt(np.square(x - m).mean(-1, keepdims=True) + eps)
+        if norm == "layer":
+            err = 2 * D * u * np.abs(x).mean(-1, keepdims=True) * rstd * np.abs(w64) * np.ones_like(x)
+            # (the mean's error moves the variance only in second order)
+        x = (x - m) * rstd * w64
+        err = err + (D / 2 + 8) * u * np.abs(x)
+        if b is not None:
+            x = x + b
+            err = err + u * np.abs(x)
+    P = freq.size
+    y, e = x.copy(), err.copy()
+    if P:
+        t = pos.astype(np.float64)[..., axis] * freq
+        c, s = np.cos(t)[:, :, None], np.sin(t)[:, :, None]
+        lo = slice(0, P) if halves else slice(0, 2 * P, 2)
+        hi = slice(P, 2 * P) if halves else slice(1, 2 * P, 2)
+        y[..., lo], y[..., hi] = x[..., lo] * c - x[..., hi] * s, x[..., hi] * c + x[..., lo] * s
+        both = np.abs(x[..., lo]) + np.abs(x[..., hi])
+        # the reference's own angle: 2^-52 of pos * freq
+        off = (8 * u + 2.0 ** -51 * np.abs(t)[:, :, None]) * both + err[..., lo] + err[..., hi]
+        e[..., lo] = e[..., hi] = off
+    return y, e + (np.abs(y) + e) * (u if f32_out else 2.0 ** -11) + (0 if f32_out else 2.0 ** -25)
+
+
+class Case:
+    def __init__(self, Bn, S, hq, hk, D, norm, dims, halves=False, shared=False, theta=10000.0, far=1000, fin="f16", fout="f16",
+                 weight=True, in_place=False, bhsd=False, seed=0, freq=None, axis=None):
+        import torch
+        rng = np.random.default_rng(seed + D + S)
+        self.norm, self.halves, self.fout = norm, halves, fout
+        ti, to = (torch.float32 if f == "f32" else torch.float16 for f in (fin, fout))
+        hv = 1                                             # a head of other values behind the keys
+        x = rng.standard_normal((Bn, S, hq + hk + hv, D)).astype(np.float32) * np.exp(rng.standard_normal((1, 1, hq + hk + hv, 1)))
+        self.x = x.astype(np.float32 if fin == "f32" else np.float16)
+        self.pos = rng.integers(-far, far + 1, (Bn, S, max(1, len(dims)))).astype(np.int32)
+        self.axis, self.freq = frequencies(dims, theta, shared)
+        cfg = B.lq_rope_config_default(dims, theta=theta, halves=halves, shared=shared)
+        if freq is not None:
+            self.freq = freq
+        if axis is not None:
+            self.axis = axis
+        self.rope = B.lq_rope_create(cfg, 0, freq, axis)
+        vec = lambda: (1 + 0.3 * rng.standard_normal(D)).astype(np.float32)
+        self.w = [vec() if weight and norm != "none" else None for _ in range(2)]
+        self.b = [vec() if weight and norm == "layer" else None for _ in range(2)]
+        put = lambda a: None if a is None else torch.from_numpy(a).cuda()
+        self.wd, self.bd = [put(v) for v in self.w], [put(v) for v in self.b]
+        rows = torch.from_numpy(self.x).cuda().to(ti)
+        posd = torch.from_numpy(self.pos).cuda()
+        sides, self.out, at = [], [], 0
+        for i, h in enumerate((hq, hk)):
+            src = rows[:, :, at:at + h]
+            at += h
+            if h == 0:
+                sides.append(None)
+                self.out.append(None)
+                continue
+            if in_place:
+                dst, strides = src, src.stride()[:3]
+            elif bhsd:
+                dst = torch.full((Bn, h, S, D), 9.0, dtype=to, device="cuda")
+                strides = [dst.stride(0), dst.stride(2), dst.stride(1)]
+            else:
+                dst = torch.full((Bn, S, h, D), 9.0, dtype=to, device="cuda")
+                strides = dst.stride()[:3]
+            self.out.append(dst)
+            sides.append(B.lq_heads(src.data_ptr(), src.stride()[:3], dst.data_ptr(), strides, h,
+                                    None if self.wd[i] is None else self.wd[i].data_ptr(), None if self.bd[i] is None else self.bd[i].data_ptr()))
+        code = {"f16": B.OUT_F16, "f32": B.OUT_F32}
+        self.kept = [rows, posd]
+        self.call = lambda st: B.lq_qk_norm_rope(sides[0], sides[1], D, Bn, S, NORMS[norm], 1e-6, self.rope, posd.data_ptr() if dims else None,
+                                                 code[fin], code[fout], st)
+        self.h, self.rows, self.in_place, self.bhsd = (hq, hk), rows, in_place, bhsd
+
+    def check(self):
+        at = 0
+        for i, h in enumerate(self.h):
+            if h:
+                y = self.out[i].float().cpu().numpy()
+                y = y.transpose(0, 2, 1, 3) if self.bhsd and not self.in_place else y
+                ref, bound = reference(self.x[:, :, at:at + h], self.w[i], self.b[i], self.norm, 1e-6, self.axis, self.freq, self.halves, self.pos,
+                                       self.fout == "f32")
+                over = np.abs(y - ref) - bound
+                assert over.max() <= 0, ("qk"[i], over.max(), np.unravel_index(over.argmax(), y.shape))
+            at += h
+        assert np.array_equal(self.rows[:, :, at:].cpu().numpy(), self.x[:, :, at:])       # what lies beside the heads stays
+        B.lq_rope_free(self.rope)
+
+    def run(self):
+        import torch
+        self.call(torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        self.check()
+
+
+@pytest.mark.parametrize("norm", ["none", "rms", "layer"])
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("D,dims", [(8, (8,)), (32, (32,)), (40, (16,)), (64, (24, 40)), (72, (72,)), (72, (36, 36)), (80, ()), (96, (32, 32, 32)),
+                                    (112, (96,)), (128, (44, 42, 42)), (160, (40, 40, 40, 40)), (248, (8,)), (256, (256,))])
+def test_head_sizes_against_64_bits(norm, halves, D, dims):
+    Case(2, 37, 3, 2, D, norm, dims, halves=halves).run()
+
+
+@pytest.mark.parametrize("fin,fout", [("f16", "f16"), ("f16", "f32"), ("f32", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("Bn,S,hq,hk", [(1, 1, 1, 0), (1, 1, 0, 3), (1, 1, 16, 16), (5, 1, 32, 8), (1, 513, 1, 1), (3, 455, 20, 5), (2, 300, 64, 1)])
+@pytest.mark.parametrize("D,halves", [(72, True), (128, False), (128, True)])
+def test_rows_heads_and_types(fin, fout, Bn, S, hq, hk, D, halves):
+    Case(Bn, S, hq, hk, D, "rms", (D - 8,), halves=halves, fin=fin, fout=fout, bhsd=S % 2 == 1).run()
+
+
+@pytest.mark.parametrize("fin", ["f16", "f32"])
+@pytest.mark.parametrize("halves", [False, True])
+def test_in_place(fin, halves):
+    Case(2, 130, 4, 4, 72, "rms", (24, 24, 24), halves=halves, fin=fin, fout=fin, in_place=True).run()
+    Case(1, 77, 6, 2, 64, "layer", (32,), halves=halves, fin=fin, fout=fin, in_place=True, weight=False).run()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("halves", [False, True])
+def test_axes_share_or_own_their_frequencies(shared, halves):
+    Case(2, 60, 2, 1, 128, "none", (32, 48, 48), halves=halves, shared=shared, theta=1e6, fin="f32", fout="f32").run()
+    Case(1, 9, 2, 1, 64, "rms", (0, 64, 0, 0), halves=halves, shared=shared).run()
+
+
+def test_angles_of_far_positions_are_exact():
+    """2^31 - 1 positions away an angle in 32 bits would be off by hundreds of radians."""
+    for far in (10 ** 6, 2 ** 31 - 1):
+        Case(1, 200, 1, 1, 64, "none", (64,), far=far, fin="f32", fout="f32").run()
+
+
+def test_frequencies_and_axes_of_the_caller():
+    rng = np.random.default_rng(0)
+    freq = np.concatenate([[0.0, 1.0, np.pi, -0.5, 2 * np.pi, 100.0], rng.random(26)])
+    Case(1, 50, 2, 2, 64, "none", (64, 0, 0), freq=freq, axis=rng.integers(0, 3, 32), fin="f32", fout="f32").run()
+
+
+def test_zero_heads_and_large_values():
+    """A head of zeros stays zero; fp32 entries whose squares are large or tiny."""
+    import torch
+    c = Case(1, 40, 2, 2, 72, "rms", (72,), fin="f32", fout="f32")
+    c.x[0, 3, 0] = 0
+    c.x[0, 4, 1] *= 1e15
+    c.x[0, 5, 2] *= 1e-15
+    c.rows.copy_(torch.from_numpy(c.x))
+    c.run()
+    assert not c.out[0][0, 3, 0].any()
+
+
+def test_a_nan_stays_in_its_head():
+    import torch
+    for D in (72, 128):
+        c = Case(1, 20, 3, 1, D, "rms", (D,), halves=True)
+        c.rows[0, 5, 1, 7] = float("nan")
+        c.call(torch.cuda.current_stream().cuda_stream)
+        bad = ~torch.isfinite(c.out[0].float()).all(-1)
+        assert bad[0, 5, 1] and bad.sum() == 1 and torch.isfinite(c.out[1]).all()
+        B.lq_rope_free(c.rope)
+
+
+def test_captured_and_replayed_on_another_stream():
+    import torch
+    c = Case(2, 100, 4, 2, 72, "rms", (36, 36))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c.call(side.cuda_stream)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.call(torch.cuda.current_stream().cuda_stream)
+    c.x = (c.x * 0.5 + 1).astype(np.float16)
+    c.pos[:] += 17
+    c.kept[0].copy_(torch.from_numpy(c.x))
+    c.kept[1].copy_(torch.from_numpy(c.pos))
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    c.check()
+
+
+def test_refusals():
+    import torch
+    x = torch.zeros(1 << 14, dtype=torch.float16, device="cuda")
+    P = x.data_ptr()
+    w = torch.ones(64, device="cuda").data_ptr()
+    rope, none = B.lq_rope_create(B.lq_rope_config_default([64]), 0), B.lq_rope_create(B.lq_rope_config_default([]), 0)
+    pos = torch.zeros(64, dtype=torch.int32, device="cuda").data_ptr()
+    good = dict(in_ptr=P, in_strides=(0, 128, 64), out_ptr=P + 16384, out_strides=(0, 128, 64), heads=2)
+
+    def code(side=None, q=True, D=64, Bn=1, S=4, norm=B.NORM_RMS, eps=1e-6, r=rope, at=pos, fin=0, fout=0):
+        h = B.lq_heads(**{**good, **(side or {})})
+        try:
+            B.lq_qk_norm_rope(h if q else None, None, D, Bn, S, norm, eps, r, at, fin, fout, 0)
+        except B.LqError as e:
+            return e.code
+        return 0
+
+    assert code() == 0 and code(r=none, at=None) == 0
+    assert code(dict(in_strides=(3, 128, 64))) == 0                                       # one sequence: its stride means nothing
+    for side in (dict(in_ptr=None), dict(out_ptr=None), dict(in_ptr=P + 8), dict(out_ptr=P + 8), dict(heads=0), dict(in_strides=(0, 124, 64)),
+                 dict(out_strides=(0, 128, 60)), dict(out_strides=(0, 0, 64)), dict(out_strides=(0, 128, 0)), dict(bias_ptr=w), dict(weight_ptr=w + 4)):
+        assert code(side) == 1, side
+    assert code(dict(weight_ptr=w), norm=B.NORM_NONE) == 1 and code(dict(weight_ptr=w, bias_ptr=w), norm=B.NORM_LAYER) == 0
+    assert code(q=False) == 1 and code(Bn=0) == 1 and code(S=0) == 1 and code(norm=3) == 1 and code(eps=-1.0) == 1 and code(eps=float("nan")) == 1
+    assert code(fin=2) == 1 and code(fout=2) == 1 and code(at=None) == 1 and code(at=pos + 2) == 1 and code(D=0) == 1
+    assert code(D=60) == 2 and code(D=264) == 2 and code(dict(heads=5000)) == 2
+    assert code(D=56, side=dict(in_strides=(0, 128, 56), out_strides=(0, 128, 56))) == 1   # fewer entries than are rotated
+    torch.cuda.synchronize()
+    B.lq_rope_free(rope)
+    B.lq_rope_free(none)
