@@ -9,6 +9,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -25,7 +26,7 @@ struct lq_rope {
 
 namespace {
 
-constexpr int MAX_D = 256, NTHREADS = 256, ITER = 2;
+constexpr int MAX_D = 256, WARPS = 8;
 enum { ROT_NONE = 0, ROT_PAIRS = 1, ROT_HALVES = 2 };
 
 struct Side {
@@ -36,38 +37,56 @@ struct Side {
 };
 struct HeadsParams {
   Side side[2];
-  long long items;              // rows * heads
-  int heads, q_heads, seq_len, axes, pairs;
+  int tasks;                    // rows * parts: a warp's work is a row's heads of one part
+  int heads, q_heads, parts, part_heads, seq_len, lanes, groups, axes, pairs;
   float eps, inv_d;
   const uint64_t* turn;
   const uint8_t* axis;
   const int32_t* pos;
 };
 
-// eight neighbouring entries
-__device__ __forceinline__ void load8(const __half* p, float (&x)[8]) {
+// eight entries: two runs of four neighbours, `apart` entries from the first to the second (4: one run of eight)
+template <typename T> struct Raw;
+template <> struct Raw<__half> { uint2 a, b; };
+template <> struct Raw<float> { float4 a, b; };
+template <bool SPLIT>
+__device__ __forceinline__ Raw<__half> load_raw(const __half* p, int apart) {
+  if constexpr (SPLIT) return {*reinterpret_cast<const uint2*>(p), *reinterpret_cast<const uint2*>(p + apart)};
   const uint4 v = *reinterpret_cast<const uint4*>(p);
-  const __half2* h = reinterpret_cast<const __half2*>(&v);
+  return {make_uint2(v.x, v.y), make_uint2(v.z, v.w)};
+}
+template <bool SPLIT>
+__device__ __forceinline__ Raw<float> load_raw(const float* p, int apart) {
+  return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + (SPLIT ? apart : 4))};
+}
+__device__ __forceinline__ void open8(const Raw<__half>& r, float (&x)[8]) {
+  const uint32_t w[4] = {r.a.x, r.a.y, r.b.x, r.b.y};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(h[i]);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
     x[2 * i] = f.x; x[2 * i + 1] = f.y;
   }
 }
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+__device__ __forceinline__ void open8(const Raw<float>& r, float (&x)[8]) {
+  x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w; x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
 }
-__device__ __forceinline__ void store8(__half* p, const float (&x)[8]) {
+template <bool SPLIT>
+__device__ __forceinline__ void store8(__half* p, int apart, const float (&x)[8]) {
   uint4 v;
   __half2* h = reinterpret_cast<__half2*>(&v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
-  *reinterpret_cast<uint4*>(p) = v;
+  if constexpr (SPLIT) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(v.x, v.y);
+    *reinterpret_cast<uint2*>(p + apart) = make_uint2(v.z, v.w);
+  } else {
+    *reinterpret_cast<uint4*>(p) = v;
+  }
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+template <bool SPLIT>
+__device__ __forceinline__ void store8(float* p, int apart, const float (&x)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + (SPLIT ? apart : 4)) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
 __device__ __forceinline__ float2 cos_sin(uint64_t turn, int32_t pos) {
@@ -81,160 +100,131 @@ __device__ __forceinline__ float2 cos_sin(uint64_t turn, int32_t pos) {
   return r;
 }
 
-// Block: V = D / 8 threads to a head, as many heads as fit 256 threads, ITER of those one behind the other.  Heads of a row are
-// neighbours, so a block sees few rows and forms their angles once.
+// Sum over the `lanes` neighbours of a group, in every lane of it.  lanes is a power of two (then xor steps do) or not.
+__device__ __forceinline__ float group_sum(float a, int lanes, int at, int lane) {
+  if ((lanes & (lanes - 1)) == 0) {
+    for (int d = lanes >> 1; d > 0; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
+    return a;
+  }
+  for (int d = 1; d < lanes; d *= 2) {
+    const float u = __shfl_down_sync(0xffffffffu, a, d);
+    if (at + d < lanes) a += u;
+  }
+  return __shfl_sync(0xffffffffu, a, lane - at);
+}
+
+// A warp takes a row and walks over its heads (or over a part of them, where rows are few): D / 8 lanes hold a head, 32 / (D / 8) heads are in
+// hand at once.  A lane's eight entries are the two sides of the same four pairs in every head, so the row's angles are formed once, in the lane
+// that needs them, and nothing passes through shared memory; the norm's sum crosses the head's lanes by shuffles.
 template <typename TIN, typename TOUT, int NORM, int ROT>
-__global__ void __launch_bounds__(NTHREADS) lq_heads_kernel(const __grid_constant__ HeadsParams p) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  const int V = blockDim.x, HB = blockDim.y, v = threadIdx.x, y = threadIdx.y, tid = y * V + v;
-  float2* red = reinterpret_cast<float2*>(smem);                          // [HB][V]
-  float* xbuf = reinterpret_cast<float*>(red + ((HB * V + 1) & ~1));      // [HB][8 V] (ROT_HALVES), on 16 bytes
-  float2* trig = reinterpret_cast<float2*>(xbuf + (ROT == ROT_HALVES ? HB * V * 8 : 0));   // [rows][pairs]
-  const long long item0 = (long long)blockIdx.x * (HB * ITER);
-  const long long items = min((long long)(HB * ITER), p.items - item0);
-  const long long row0 = item0 / p.heads;
+__global__ void __launch_bounds__(32 * WARPS) lq_heads_kernel(const __grid_constant__ HeadsParams p) {
+  constexpr bool SPLIT = ROT == ROT_HALVES;
+  constexpr int U = sizeof(TIN) == 4 ? 2 : 4;             // heads of a lane whose loads are in flight together
+  const int lane = threadIdx.x & 31, V = p.lanes;
+  const int task = blockIdx.x * WARPS + (threadIdx.x >> 5);
+  const int grp = lane / V, v = lane - grp * V;
+  const bool works = grp < p.groups;
+  // pairs 4 v .. 4 v + 3: entries 8 v .. 8 v + 7, or (halves) 4 v .. 4 v + 3 and as many half of the rotated part further; what is not rotated lies
+  // behind, eight neighbours a lane
+  const bool turned = ROT != ROT_NONE && 4 * v < p.pairs;
+  const int first = SPLIT && turned ? 4 * v : 8 * v, apart = SPLIT && turned ? p.pairs : 4;
+  uint64_t turn[4];
+  int axis[4];
+  if constexpr (ROT != ROT_NONE) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = min(4 * v + j, p.pairs - 1);
+      turn[j] = p.turn[i];
+      axis[j] = p.axis[i];
+    }
+  }
   grid_launch_dependents();
   grid_dependency_wait();
-
-  float x[ITER][8];
-  const Side* side[ITER];
-  long long out[ITER];
-  int row_at[ITER];
-#pragma unroll
-  for (int i = 0; i < ITER; ++i) {
-    const long long at = (long long)i * HB + y;
-    if (at < items) {
-      const long long item = item0 + at, row = item / p.heads;
-      const int head = (int)(item - row * p.heads);
-      const bool is_k = head >= p.q_heads;
-      const Side& s = p.side[is_k];
-      const int h = is_k ? head - p.q_heads : head;
-      const long long b = row / p.seq_len, r = row - b * p.seq_len;
-      side[i] = &s;
-      row_at[i] = (int)(row - row0);
-      load8(reinterpret_cast<const TIN*>(s.in) + b * s.in_seq + r * s.in_row + h * s.in_head + 8 * v, x[i]);
-      out[i] = b * s.out_seq + r * s.out_row + h * s.out_head + 8 * v;
-    }
-  }
-  if constexpr (ROT != ROT_NONE) {
-    const int rows = (int)((item0 + items - 1) / p.heads - row0) + 1;
-    for (int e = tid; e < rows * p.pairs; e += HB * V) {
-      const int r = e / p.pairs, j = e - r * p.pairs;
-      trig[e] = cos_sin(p.turn[j], p.pos[(row0 + r) * p.axes + p.axis[j]]);
-    }
-    if constexpr (NORM == LQ_NORM_NONE) __syncthreads();
-  }
-#pragma unroll
-  for (int i = 0; i < ITER; ++i) {
-    const bool live = (long long)i * HB + y < items;
+  if (task >= p.tasks) return;
+  const int row = task / p.parts, part = task - row * p.parts;
+  const int seq = row / p.seq_len, at = row - seq * p.seq_len;
+  const int h_begin = part * p.part_heads, h_end = min(p.heads, h_begin + p.part_heads);
+  float2 cs[4];
+  bool have_angles = false;
+  for (int side = 0; side < 2; ++side) {
+    const Side& s = p.side[side];
+    const int begin = max(h_begin - (side ? p.q_heads : 0), 0), end = min(h_end, side ? p.heads : p.q_heads) - (side ? p.q_heads : 0);
+    if (begin >= end) continue;
+    const TIN* in = reinterpret_cast<const TIN*>(s.in) + seq * s.in_seq + at * s.in_row + first;
+    TOUT* out = reinterpret_cast<TOUT*>(s.out) + seq * s.out_seq + at * s.out_row + first;
+    float w[8], b[8];
     if constexpr (NORM != LQ_NORM_NONE) {
-      if (live) {
-        float a = 0.f, m = 0.f;
-        if constexpr (NORM == LQ_NORM_LAYER) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) m += x[i][j];
-          m *= 0.125f;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) a = fmaf(x[i][j] - m, x[i][j] - m, a);
-        red[tid] = make_float2(a, m);
-      }
-      __syncthreads();
-      if (live) {
-        float a = 0.f, m = 0.f;
-        for (int j = 0; j < V; ++j) { a += red[y * V + j].x; m += red[y * V + j].y; }
-        if constexpr (NORM == LQ_NORM_LAYER) {
-          m *= 8.f * p.inv_d;
-          float d = 0.f;
-          for (int j = 0; j < V; ++j) d = fmaf(red[y * V + j].y - m, red[y * V + j].y - m, d);
-          a = fmaf(8.f, d, a);
-        }
-        const float rstd = 1.f / sqrtf(fmaf(a, p.inv_d, p.eps));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[i][j] = (x[i][j] - m) * rstd;
-        if (side[i]->weight) {
-          float w[8];
-          load8(side[i]->weight + 8 * v, w);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[i][j] *= w[j];
-        }
-        if (NORM == LQ_NORM_LAYER && side[i]->bias) {
-          float w[8];
-          load8(side[i]->bias + 8 * v, w);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[i][j] += w[j];
-        }
-      }
+      for (int j = 0; j < 8; ++j) { w[j] = 1.f; b[j] = 0.f; }
+      if (works && s.weight) open8(load_raw<SPLIT>(s.weight + first, apart), w);
+      if (NORM == LQ_NORM_LAYER && works && s.bias) open8(load_raw<SPLIT>(s.bias + first, apart), b);
     }
-    if constexpr (ROT == ROT_HALVES) {
-      if (live) {
-        float4* b = reinterpret_cast<float4*>(xbuf + 8 * tid);
-        b[0] = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
-        b[1] = make_float4(x[i][4], x[i][5], x[i][6], x[i][7]);
-      }
-    }
-    __syncthreads();      // the partners' entries are there; the sums of this heads' group have been read
-    if (live) {
-      if constexpr (ROT == ROT_PAIRS) {
-        const float2* cs = trig + row_at[i] * p.pairs + 4 * v;
+    for (int h0 = begin; h0 < end; h0 += U * p.groups) {
+      Raw<TIN> raw[U] = {};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (4 * v + j < p.pairs) {
-            const float2 t = cs[j];
-            const float u = x[i][2 * j], w = x[i][2 * j + 1];
-            x[i][2 * j] = u * t.x - w * t.y;
-            x[i][2 * j + 1] = w * t.x + u * t.y;
+      for (int u = 0; u < U; ++u) {
+        const int h = h0 + u * p.groups + grp;
+        if (works && h < end) raw[u] = load_raw<SPLIT>(in + h * s.in_head, apart);
+      }
+      if constexpr (ROT != ROT_NONE) {
+        if (!have_angles) {                               // under the first loads
+#pragma unroll
+          for (int j = 0; j < 4; ++j) cs[j] = cos_sin(turn[j], p.pos[(long long)row * p.axes + axis[j]]);
+          have_angles = true;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (h0 + u * p.groups >= end) break;              // (the whole warp)
+        const int h = h0 + u * p.groups + grp;
+        float x[8];
+        open8(raw[u], x);
+        if constexpr (NORM != LQ_NORM_NONE) {
+          float m = 0.f, a = 0.f;
+          if constexpr (NORM == LQ_NORM_LAYER) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m += x[j];
+            m = group_sum(m, V, v, lane) * p.inv_d;
           }
-      }
-      if constexpr (ROT == ROT_HALVES) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {                     // half of the rotated part is a multiple of four entries
-          const int d = 8 * v + 4 * q;
-          if (d < 2 * p.pairs) {
-            const bool first = d < p.pairs;
-            const float4 o = *reinterpret_cast<const float4*>(xbuf + 8 * V * y + (first ? d + p.pairs : d - p.pairs));
-            const float2* cs = trig + row_at[i] * p.pairs + (first ? d : d - p.pairs);
-            const float other[4] = {o.x, o.y, o.z, o.w};
+          for (int j = 0; j < 8; ++j) {
+            x[j] -= m;
+            a = fmaf(x[j], x[j], a);
+          }
+          a = group_sum(a, V, v, lane);
+          const float rstd = rsqrtf(fmaf(a, p.inv_d, p.eps));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float2 t = cs[j];
-              x[i][4 * q + j] = x[i][4 * q + j] * t.x + (first ? -other[j] : other[j]) * t.y;
+          for (int j = 0; j < 8; ++j) x[j] = NORM == LQ_NORM_LAYER ? fmaf(x[j] * rstd, w[j], b[j]) : x[j] * rstd * w[j];
+        }
+        if (ROT != ROT_NONE && turned) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int lo = SPLIT ? j : 2 * j, hi = SPLIT ? j + 4 : 2 * j + 1;
+            const float a = x[lo], c = x[hi];
+            if (SPLIT || 4 * v + j < p.pairs) {           // (halves turn whole lanes)
+              x[lo] = a * cs[j].x - c * cs[j].y;
+              x[hi] = c * cs[j].x + a * cs[j].y;
             }
           }
         }
+        if (works && h < end) store8<SPLIT>(out + h * s.out_head, apart, x);
       }
-      store8(reinterpret_cast<TOUT*>(side[i]->out) + out[i], x[i]);
     }
-    if constexpr (ROT == ROT_HALVES)
-      if (i + 1 < ITER) __syncthreads();
   }
 }
 
 template <typename TIN, typename TOUT, int NORM, int ROT>
-cudaError_t launch(const HeadsParams& p, int D, cudaStream_t st) {
-  const int V = D / 8, HB = NTHREADS / V;
-  const long long blocks = (p.items + HB * ITER - 1) / (HB * ITER);
-  if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  const int rows = (HB * ITER - 1) / p.heads + 2;         // a block's items touch no more rows
-  const size_t smem = (size_t)((HB * V + 1) & ~1) * sizeof(float2) + (ROT == ROT_HALVES ? (size_t)HB * V * 32 : 0) +
-                      (ROT != ROT_NONE ? (size_t)rows * p.pairs * sizeof(float2) : 0);
-  cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3((unsigned)blocks); lc.blockDim = dim3((unsigned)V, (unsigned)HB); lc.dynamicSmemBytes = smem; lc.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  lc.attrs = at; lc.numAttrs = g_lq_overlap ? 1 : 0;
-  return cudaLaunchKernelEx(&lc, lq_heads_kernel<TIN, TOUT, NORM, ROT>, p);
+cudaError_t launch(const HeadsParams& p, cudaStream_t st) {
+  return lq_launch(lq_heads_kernel<TIN, TOUT, NORM, ROT>, (p.tasks + WARPS - 1) / WARPS, 32 * WARPS, 0, st, p);
 }
 template <typename TIN, typename TOUT, int NORM>
-cudaError_t launch_rot(const HeadsParams& p, int D, int rot, cudaStream_t st) {
-  return rot == ROT_NONE ? launch<TIN, TOUT, NORM, ROT_NONE>(p, D, st)
-         : rot == ROT_PAIRS ? launch<TIN, TOUT, NORM, ROT_PAIRS>(p, D, st) : launch<TIN, TOUT, NORM, ROT_HALVES>(p, D, st);
+cudaError_t launch_rot(const HeadsParams& p, int rot, cudaStream_t st) {
+  return rot == ROT_NONE ? launch<TIN, TOUT, NORM, ROT_NONE>(p, st) : rot == ROT_PAIRS ? launch<TIN, TOUT, NORM, ROT_PAIRS>(p, st) : launch<TIN, TOUT, NORM, ROT_HALVES>(p, st);
 }
 template <typename TIN, typename TOUT>
-cudaError_t launch_norm(const HeadsParams& p, int D, int norm, int rot, cudaStream_t st) {
-  return norm == LQ_NORM_NONE ? launch_rot<TIN, TOUT, LQ_NORM_NONE>(p, D, rot, st)
-         : norm == LQ_NORM_RMS ? launch_rot<TIN, TOUT, LQ_NORM_RMS>(p, D, rot, st) : launch_rot<TIN, TOUT, LQ_NORM_LAYER>(p, D, rot, st);
+cudaError_t launch_norm(const HeadsParams& p, int norm, int rot, cudaStream_t st) {
+  return norm == LQ_NORM_NONE ? launch_rot<TIN, TOUT, LQ_NORM_NONE>(p, rot, st)
+         : norm == LQ_NORM_RMS ? launch_rot<TIN, TOUT, LQ_NORM_RMS>(p, rot, st) : launch_rot<TIN, TOUT, LQ_NORM_LAYER>(p, rot, st);
 }
 
 // Strides over dimensions of one entry mean nothing; the others keep entries on 16-byte boundaries, and no two outputs on one place.
@@ -342,7 +332,15 @@ extern "C" lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32
   if (k && (s = take_side(k, sequences, seq_len, norm, &p.side[1])) != LQ_OK) return s;
   p.q_heads = q ? q->heads : 0;
   p.heads = p.q_heads + (k ? k->heads : 0);
-  p.items = rows * p.heads;
+  p.lanes = head_dim / 8;
+  p.groups = 32 / p.lanes;
+  // A warp walks over all heads of its row once there are warps enough to fill the GPU; below that the heads are spread over more warps.
+  const long long walk = lq_ceil_div(p.heads, p.groups), fill = 148 * 32;
+  const long long parts = std::max(1ll, std::min(walk, fill / rows));
+  p.part_heads = (int)((walk + parts - 1) / parts) * p.groups;
+  p.parts = lq_ceil_div(p.heads, p.part_heads);
+  if (rows * p.parts > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
+  p.tasks = (int)(rows * p.parts);
   p.seq_len = seq_len; p.axes = R->axes; p.pairs = R->pairs;
   p.eps = eps; p.inv_d = 1.f / (float)head_dim;
   p.turn = R->d_turn; p.axis = R->d_axis; p.pos = pos;
@@ -351,7 +349,7 @@ extern "C" lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32
   const int rot = R->pairs == 0 ? ROT_NONE : R->halves ? ROT_HALVES : ROT_PAIRS;
   cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e =
-      in_dtype == LQ_OUT_F16 ? (out_dtype == LQ_OUT_F16 ? launch_norm<__half, __half>(p, head_dim, norm, rot, st) : launch_norm<__half, float>(p, head_dim, norm, rot, st))
-                             : (out_dtype == LQ_OUT_F16 ? launch_norm<float, __half>(p, head_dim, norm, rot, st) : launch_norm<float, float>(p, head_dim, norm, rot, st));
+      in_dtype == LQ_OUT_F16 ? (out_dtype == LQ_OUT_F16 ? launch_norm<__half, __half>(p, norm, rot, st) : launch_norm<__half, float>(p, norm, rot, st))
+                             : (out_dtype == LQ_OUT_F16 ? launch_norm<float, __half>(p, norm, rot, st) : launch_norm<float, float>(p, norm, rot, st));
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
