@@ -331,7 +331,7 @@ typedef struct {
   const void* in;                          /* device, 16-byte aligned; half or float per in_dtype                     */
   void* out;                               /* device, 16-byte aligned; half or float per out_dtype; `in` itself, with its strides and
                                               type, or memory apart from all inputs                                   */
-  int64_t in_seq, in_row, in_head;         /* strides in elements, multiples of 8                                     */
+  int64_t in_seq, in_row, in_head;         /* strides in elements, multiples of 8, below 2^31, a head's below 2^26 (the memory they span may be larger) */
   int64_t out_seq, out_row, out_head;
   const float* weight;                     /* [head_dim] device, 16-byte aligned, or NULL (ones); NULL without a norm */
   const float* bias;                       /* [head_dim] device, 16-byte aligned, or NULL (zeros); LQ_NORM_LAYER only */

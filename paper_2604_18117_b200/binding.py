@@ -299,7 +299,7 @@ def lq_rowmap_create(M_max: int, slots: int, device: int = 0):
 
 
 def lq_rowmap_set(rowmap, row_adapter_dev_ptr: int, M: int, stream: int = 0):
-    _check(lib().lq_rowmap_set(rowmap, C.c_void_p(row_adapter_dev_ptr), M, C.c_void_p(stream)), "lq_rowmap_set")
+    _check(lib().lq_rowmap_set(rowmap, row_adapter_dev_ptr, M, stream), "lq_rowmap_set")
 
 
 def lq_rowmap_free(rowmap):
@@ -308,8 +308,7 @@ def lq_rowmap_free(rowmap):
 
 def lq_adapters_forward(adapters, rowmap, X_dev_ptr: int, Y0_dev_ptr: int, Y_dev_ptr: int, dtype: int = OUT_F16, stream: int = 0):
     """Y = Y0 + each row's adapter on X; Y may be Y0 itself."""
-    _check(lib().lq_adapters_forward(adapters, rowmap, C.c_void_p(X_dev_ptr), C.c_void_p(Y0_dev_ptr), C.c_void_p(Y_dev_ptr), dtype,
-                                     C.c_void_p(stream)), "lq_adapters_forward")
+    _check(lib().lq_adapters_forward(adapters, rowmap, X_dev_ptr, Y0_dev_ptr, Y_dev_ptr, dtype, stream), "lq_adapters_forward")
 
 
 def lq_rope_config_default(dims, theta: float = 10000.0, halves: bool = False, shared: bool = False) -> LqRopeConfig:
@@ -343,9 +342,7 @@ def lq_heads(in_ptr: int, in_strides, out_ptr: int, out_strides, heads: int, wei
 
 def lq_qk_norm_rope(q: LqHeads | None, k: LqHeads | None, head_dim: int, sequences: int, seq_len: int, norm: int, eps: float, rope,
                     pos_dev_ptr: int | None, in_dtype: int = OUT_F16, out_dtype: int = OUT_F16, stream: int = 0):
-    ref = lambda h: None if h is None else C.byref(h)
-    _check(lib().lq_qk_norm_rope(ref(q), ref(k), head_dim, sequences, seq_len, norm, eps, rope, C.c_void_p(pos_dev_ptr), in_dtype, out_dtype,
-                                 C.c_void_p(stream)), "lq_qk_norm_rope")
+    _check(lib().lq_qk_norm_rope(q, k, head_dim, sequences, seq_len, norm, eps, rope, pos_dev_ptr, in_dtype, out_dtype, stream), "lq_qk_norm_rope")
 
 
 def lq_act_export(act, M: int, cfg: LqConfig, stream: int = 0) -> dict:

@@ -26,19 +26,21 @@ struct lq_rope {
 
 namespace {
 
-constexpr int MAX_D = 256, WARPS = 8;
+constexpr int MAX_D = 256, WARPS = 4, MAX_ROWS = 4;
 enum { ROT_NONE = 0, ROT_PAIRS = 1, ROT_HALVES = 2 };
 
 struct Side {
   const void* in;
   void* out;
-  long long in_seq, in_row, in_head, out_seq, out_row, out_head;
+  int in_seq, in_row, in_head, out_seq, out_row, out_head;
   const float *weight, *bias;
 };
 struct HeadsParams {
   Side side[2];
-  int tasks;                    // rows * parts: a warp's work is a row's heads of one part
-  int heads, q_heads, parts, part_heads, seq_len, lanes, groups, axes, pairs;
+  int rows, heads[2], seq_len, lanes, groups, axes, pairs;
+  int block_rows, walk, parts[2];   // rows of a block; heads a warp walks over at a time, and the parts that makes of Q's and K's
+  uint32_t by_parts, by_wide, by_groups;   // 2^32 / divisor, rounded up, of parts[0] + parts[1], of the pairs rounded up to four, of groups:
+                                // quotients of what is below 2^16 (a divisor of one is not divided by)
   float eps, inv_d;
   const uint64_t* turn;
   const uint8_t* axis;
@@ -59,23 +61,40 @@ template <bool SPLIT>
 __device__ __forceinline__ Raw<float> load_raw(const float* p, int apart) {
   return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + (SPLIT ? apart : 4))};
 }
-__device__ __forceinline__ void open8(const Raw<__half>& r, float (&x)[8]) {
-  const uint32_t w[4] = {r.a.x, r.a.y, r.b.x, r.b.y};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    x[2 * i] = f.x; x[2 * i + 1] = f.y;
-  }
+// The four pairs of a lane: first sides lo, second sides hi, two pairs to a register pair (packed arithmetic takes both at once).  NEIGHBOURS: a pair
+// is two neighbouring entries.
+struct Pairs {
+  float2 lo[2], hi[2];
+};
+template <bool NEIGHBOURS>
+__device__ __forceinline__ Pairs open8(const Raw<float>& r) {
+  if constexpr (NEIGHBOURS)
+    return {{make_float2(r.a.x, r.a.z), make_float2(r.b.x, r.b.z)}, {make_float2(r.a.y, r.a.w), make_float2(r.b.y, r.b.w)}};
+  return {{make_float2(r.a.x, r.a.y), make_float2(r.a.z, r.a.w)}, {make_float2(r.b.x, r.b.y), make_float2(r.b.z, r.b.w)}};
 }
-__device__ __forceinline__ void open8(const Raw<float>& r, float (&x)[8]) {
-  x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w; x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
+template <bool NEIGHBOURS>
+__device__ __forceinline__ Pairs open8(const Raw<__half>& r) {
+  const uint32_t w[4] = {r.a.x, r.a.y, r.b.x, r.b.y};
+  float2 f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+  return open8<NEIGHBOURS>(Raw<float>{make_float4(f[0].x, f[0].y, f[1].x, f[1].y), make_float4(f[2].x, f[2].y, f[3].x, f[3].y)});
+}
+template <bool NEIGHBOURS>
+__device__ __forceinline__ Raw<float> close8(const Pairs& x) {
+  if constexpr (NEIGHBOURS)
+    return {make_float4(x.lo[0].x, x.hi[0].x, x.lo[0].y, x.hi[0].y), make_float4(x.lo[1].x, x.hi[1].x, x.lo[1].y, x.hi[1].y)};
+  return {make_float4(x.lo[0].x, x.lo[0].y, x.lo[1].x, x.lo[1].y), make_float4(x.hi[0].x, x.hi[0].y, x.hi[1].x, x.hi[1].y)};
 }
 template <bool SPLIT>
-__device__ __forceinline__ void store8(__half* p, int apart, const float (&x)[8]) {
-  uint4 v;
-  __half2* h = reinterpret_cast<__half2*>(&v);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+__device__ __forceinline__ void store_raw(float* p, int apart, const Raw<float>& x) {
+  *reinterpret_cast<float4*>(p) = x.a;
+  *reinterpret_cast<float4*>(p + (SPLIT ? apart : 4)) = x.b;
+}
+template <bool SPLIT>
+__device__ __forceinline__ void store_raw(__half* p, int apart, const Raw<float>& x) {
+  const __half2 h[4] = {__floats2half2_rn(x.a.x, x.a.y), __floats2half2_rn(x.a.z, x.a.w), __floats2half2_rn(x.b.x, x.b.y), __floats2half2_rn(x.b.z, x.b.w)};
+  const uint4 v = *reinterpret_cast<const uint4*>(h);
   if constexpr (SPLIT) {
     *reinterpret_cast<uint2*>(p) = make_uint2(v.x, v.y);
     *reinterpret_cast<uint2*>(p + apart) = make_uint2(v.z, v.w);
@@ -83,148 +102,278 @@ __device__ __forceinline__ void store8(__half* p, int apart, const float (&x)[8]
     *reinterpret_cast<uint4*>(p) = v;
   }
 }
-template <bool SPLIT>
-__device__ __forceinline__ void store8(float* p, int apart, const float (&x)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<float4*>(p + (SPLIT ? apart : 4)) = make_float4(x[4], x[5], x[6], x[7]);
-}
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
 
+// Cosine and sine of pos * turn.  Taylor's series about the nearest quarter turn, at most pi / 4 away: the terms left out are below 2e-9 and 2e-10.
 __device__ __forceinline__ float2 cos_sin(uint64_t turn, int32_t pos) {
   const int32_t t = (int32_t)(uint32_t)((turn * (uint64_t)(int64_t)pos) >> 32);       // fraction of a turn, 2^32 = 1
-  const int32_t quarter = (int32_t)(((uint32_t)t + 0x20000000u) >> 30);                // nearest quarter turn, 0 .. 3
-  const int32_t rest = (int32_t)((uint32_t)t - ((uint32_t)quarter << 30));             // [-2^29, 2^29)
-  float s, c;
-  sincospif((float)rest * 0x1p-31f, &s, &c);
-  float2 r = (quarter & 1) ? make_float2(-s, c) : make_float2(c, s);
-  if (quarter & 2) r = make_float2(-r.x, -r.y);
-  return r;
+  const uint32_t quarter = ((uint32_t)t + 0x20000000u) >> 30;                          // nearest quarter turn, 0 .. 3
+  const int32_t rest = (int32_t)((uint32_t)t - (quarter << 30));                       // [-2^29, 2^29)
+  const float x = (float)rest * 1.46291807926715968e-9f, y = x * x;                    // 2 pi / 2^32
+  float s = fmaf(y, 2.75573192239858907e-6f, -1.98412698412698413e-4f);
+  s = fmaf(s, y, 8.33333333333333333e-3f);
+  s = fmaf(s, y, -1.66666666666666667e-1f);
+  s = fmaf(s * y, x, x);
+  float c = fmaf(y, -2.75573192239858907e-7f, 2.48015873015873016e-5f);
+  c = fmaf(c, y, -1.38888888888888889e-3f);
+  c = fmaf(c, y, 4.16666666666666667e-2f);
+  c = fmaf(c, y, -0.5f);
+  c = fmaf(c, y, 1.f);
+  const float a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;                        // one quarter on: (-s, c)
+  return make_float2((quarter + 1) & 2 ? -a : a, quarter & 2 ? -b : b);
 }
 
-// Sum over the `lanes` neighbours of a group, in every lane of it.  lanes is a power of two (then xor steps do) or not.
+// Sum over a group's L neighbouring lanes, in every lane of it.  Powers of two: xor steps.  Other L known at compile time: sums over windows of
+// 1, .., L lanes round the group, each twice the one before or one longer (L = 7: 1, 2, 3, 6, 7).  L = 0: `lanes` lanes, summed up to the group's
+// first lane and handed back.
+template <int L>
 __device__ __forceinline__ float group_sum(float a, int lanes, int at, int lane) {
-  if ((lanes & (lanes - 1)) == 0) {
-    for (int d = lanes >> 1; d > 0; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
-    return a;
+  if constexpr (L > 0 && (L & (L - 1)) == 0) {
+#pragma unroll
+    for (int d = L / 2; d > 0; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d);
+  } else if constexpr (L > 0) {
+    const float one = a;
+    int len = 1;
+#pragma unroll
+    for (int bit = L >= 16 ? 3 : L >= 8 ? 2 : L >= 4 ? 1 : 0; bit >= 0; --bit) {
+      a += __shfl_sync(0xffffffffu, a, lane + (at + len >= L ? len - L : len));
+      len *= 2;
+      if ((L >> bit) & 1) {
+        a += __shfl_sync(0xffffffffu, one, lane + (at + len >= L ? len - L : len));
+        ++len;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2)
+      if (d < lanes) {
+        const float u = __shfl_down_sync(0xffffffffu, a, d);
+        if (at + d < lanes) a += u;
+      }
+    a = __shfl_sync(0xffffffffu, a, lane - at);
   }
-  for (int d = 1; d < lanes; d *= 2) {
-    const float u = __shfl_down_sync(0xffffffffu, a, d);
-    if (at + d < lanes) a += u;
-  }
-  return __shfl_sync(0xffffffffu, a, lane - at);
+  return a;
 }
 
-// A warp takes a row and walks over its heads (or over a part of them, where rows are few): D / 8 lanes hold a head, 32 / (D / 8) heads are in
-// hand at once.  A lane's eight entries are the two sides of the same four pairs in every head, so the row's angles are formed once, in the lane
-// that needs them, and nothing passes through shared memory; the norm's sum crosses the head's lanes by shuffles.
-template <typename TIN, typename TOUT, int NORM, int ROT>
-__global__ void __launch_bounds__(32 * WARPS) lq_heads_kernel(const __grid_constant__ HeadsParams p) {
-  constexpr bool SPLIT = ROT == ROT_HALVES;
-  constexpr int U = sizeof(TIN) == 4 ? 2 : 4;             // heads of a lane whose loads are in flight together
-  const int lane = threadIdx.x & 31, V = p.lanes;
-  const int task = blockIdx.x * WARPS + (threadIdx.x >> 5);
-  const int grp = lane / V, v = lane - grp * V;
-  const bool works = grp < p.groups;
-  // pairs 4 v .. 4 v + 3: entries 8 v .. 8 v + 7, or (halves) 4 v .. 4 v + 3 and as many half of the rotated part further; what is not rotated lies
-  // behind, eight neighbours a lane
-  const bool turned = ROT != ROT_NONE && 4 * v < p.pairs;
-  const int first = SPLIT && turned ? 4 * v : 8 * v, apart = SPLIT && turned ? p.pairs : 4;
-  uint64_t turn[4];
-  int axis[4];
-  if constexpr (ROT != ROT_NONE) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = min(4 * v + j, p.pairs - 1);
-      turn[j] = p.turn[i];
-      axis[j] = p.axis[i];
-    }
-  }
+// A block takes a few rows and forms their angles together.  Its warps share out the rows' heads: one walks over the queries, or the keys, of a
+// row, or over a part of them.  L lanes hold a head, each lane C times eight entries that are the two sides of the same four pairs in every head, so
+// weights times cosines and sines stay in registers along the walk; the norm's sum crosses the head's lanes by shuffles.  What bounds it short of the
+// memory is the issue of instructions, so a lane holds as much of a head as registers allow, and where L is known (then the whole head is rotated, or
+// nothing) every address is a base and a constant.
+template <typename TIN, typename TOUT, int NORM, int ROT, int L, int C>
+__global__ void __launch_bounds__(32 * WARPS, C == 1 && sizeof(TIN) == 2 && NORM != LQ_NORM_LAYER ? 6 : C == 2 && L != 7 && sizeof(TIN) == 2 ? 5 : 4) lq_heads_kernel(const __grid_constant__ HeadsParams p) {
+  constexpr bool SPLIT = ROT == ROT_HALVES, NEIGHBOURS = ROT == ROT_PAIRS, FIXED = L > 0;
+  static_assert(FIXED || C == 1, "");
+  constexpr int DEPTH = sizeof(TIN) == 2 ? (C == 1 ? 4 : C == 2 ? 3 : 2) : (C == 1 ? 3 : C == 2 ? 2 : 1);      // heads of a lane in flight
+  constexpr int UNIT = SPLIT ? 4 : 8;                     // entries from one lane's to the next one's
+  __shared__ __align__(16) float trig[ROT == ROT_NONE ? 1 : MAX_ROWS * MAX_D];         // [rows of the block][cos, sin][pairs, a multiple of four]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lanes = FIXED ? L : p.lanes, groups = FIXED ? 32 / (FIXED ? L : 1) : p.groups;
+  int grp = 0;
+  if constexpr (FIXED) grp = lane / L;
+  else
+    for (int i = lanes; i <= lane; i += lanes) ++grp;
+  const int v = lane - grp * lanes;
+  const bool works = (FIXED && 32 % (FIXED ? L : 1) == 0) || grp < groups;
+  const int row0 = blockIdx.x * p.block_rows, wide = (p.pairs + 3) & ~3, parts = p.parts[0] + p.parts[1];
+  const int tasks = min(p.block_rows, p.rows - row0) * parts;
+  const int seq0 = row0 / p.seq_len, at0 = row0 - seq0 * p.seq_len;
+  // pairs 4 i .. 4 i + 3 of the lane's i = v, v + L, ..: entries 8 i .. 8 i + 7, or (halves) 4 i .. 4 i + 3 and as many half of the rotated part
+  // further; what is not rotated lies behind, eight neighbours at a time
+  const int turns = ROT == ROT_NONE ? 0 : FIXED ? 4 : max(0, min(4, p.pairs - 4 * v));        // pairs that are rotated
+  const int first = FIXED || turns > 0 ? UNIT * v : 8 * v, apart = !SPLIT ? 4 : FIXED ? 4 * L * C : turns > 0 ? p.pairs : 4;
   grid_launch_dependents();
   grid_dependency_wait();
-  if (task >= p.tasks) return;
-  const int row = task / p.parts, part = task - row * p.parts;
-  const int seq = row / p.seq_len, at = row - seq * p.seq_len;
-  const int h_begin = part * p.part_heads, h_end = min(p.heads, h_begin + p.part_heads);
-  float2 cs[4];
-  bool have_angles = false;
-  for (int side = 0; side < 2; ++side) {
-    const Side& s = p.side[side];
-    const int begin = max(h_begin - (side ? p.q_heads : 0), 0), end = min(h_end, side ? p.heads : p.q_heads) - (side ? p.q_heads : 0);
-    if (begin >= end) continue;
-    const TIN* in = reinterpret_cast<const TIN*>(s.in) + seq * s.in_seq + at * s.in_row + first;
-    TOUT* out = reinterpret_cast<TOUT*>(s.out) + seq * s.out_seq + at * s.out_row + first;
-    float w[8], b[8];
-    if constexpr (NORM != LQ_NORM_NONE) {
+  int task = blockIdx.y * WARPS + warp, r = 0, which = 0, begin = 0, end = 0, left = 0, in_step = 0, out_step = 0;
+  const TIN* in = nullptr;
+  TOUT* out = nullptr;
+  Raw<TIN> raw[DEPTH][C];                                 // (what is not loaded is computed with and not stored)
+  const auto open_task = [&]() {                          // where the task's heads lie; the first ones are asked for
+    r = parts == 1 ? task : (int)__umulhi(task, p.by_parts);
+    const int part = task - r * parts;
+    which = part >= p.parts[0];
+    const Side& side = p.side[which];
+    begin = (part - (which ? p.parts[0] : 0)) * p.walk;
+    end = min(p.heads[which], begin + p.walk);
+    int seq = seq0, at = at0 + r;
+    for (; at >= p.seq_len; at -= p.seq_len) ++seq;
+    in_step = groups * side.in_head; out_step = groups * side.out_head;
+    in = reinterpret_cast<const TIN*>(side.in) + ((long long)seq * side.in_seq + (long long)at * side.in_row + (long long)(begin + grp) * side.in_head + first);
+    out = reinterpret_cast<TOUT*>(side.out) + ((long long)seq * side.out_seq + (long long)at * side.out_row + (long long)(begin + grp) * side.out_head + first);
+    left = works ? end - begin - grp : 0;                 // heads that this lane has before it, in steps of `groups`
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { w[j] = 1.f; b[j] = 0.f; }
-      if (works && s.weight) open8(load_raw<SPLIT>(s.weight + first, apart), w);
-      if (NORM == LQ_NORM_LAYER && works && s.bias) open8(load_raw<SPLIT>(s.bias + first, apart), b);
+    for (int u = 0; u < DEPTH; ++u) {
+      if (left > u * groups)
+#pragma unroll
+        for (int i = 0; i < C; ++i) raw[u][i] = load_raw<SPLIT>(in + UNIT * L * i, apart);
+      in += in_step;
     }
-    for (int h0 = begin; h0 < end; h0 += U * p.groups) {
-      Raw<TIN> raw[U] = {};
+  };
+  if (task < tasks) open_task();
+  if constexpr (ROT != ROT_NONE) {
+    for (int e = threadIdx.x; e < wide * p.block_rows; e += 32 * WARPS) {
+      const int r = (int)__umulhi(e, p.by_wide), i = e - r * wide;
+      float2 cs = make_float2(1.f, 0.f);                  // (pairs behind the rotated ones stay)
+      if (i < p.pairs && row0 + r < p.rows) cs = cos_sin(p.turn[i], p.pos[(long long)(row0 + r) * p.axes + p.axis[i]]);
+      trig[2 * r * wide + i] = cs.x;
+      trig[(2 * r + 1) * wide + i] = cs.y;
+    }
+    __syncthreads();
+  }
+#pragma unroll 1
+  while (task < tasks) {
+    const Side& side = p.side[which];
+    Pairs w[C], cross[C], b[NORM == LQ_NORM_LAYER ? C : 1];       // cross: lo is hi's share in lo, hi is lo's share in hi
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = h0 + u * p.groups + grp;
-        if (works && h < end) raw[u] = load_raw<SPLIT>(in + h * s.in_head, apart);
+    for (int i = 0; i < C; ++i) {
+      w[i] = {{both(1.f), both(1.f)}, {both(1.f), both(1.f)}};
+      if constexpr (NORM != LQ_NORM_NONE)
+        if (works && side.weight) w[i] = open8<NEIGHBOURS>(load_raw<SPLIT>(side.weight + first + UNIT * L * i, apart));
+      if constexpr (NORM == LQ_NORM_LAYER) {
+        b[i] = {};
+        if (works && side.bias) b[i] = open8<NEIGHBOURS>(load_raw<SPLIT>(side.bias + first + UNIT * L * i, apart));
       }
-      if constexpr (ROT != ROT_NONE) {
-        if (!have_angles) {                               // under the first loads
+      if (ROT != ROT_NONE && turns > 0) {
+        const float* t = trig + 2 * r * wide + 4 * (v + i * L);
+        const float4 c4 = *reinterpret_cast<const float4*>(t), s4 = *reinterpret_cast<const float4*>(t + wide);
+        const float2 c[2] = {make_float2(c4.x, c4.y), make_float2(c4.z, c4.w)}, s[2] = {make_float2(s4.x, s4.y), make_float2(s4.z, s4.w)};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) cs[j] = cos_sin(turn[j], p.pos[(long long)row * p.axes + axis[j]]);
-          have_angles = true;
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (h0 + u * p.groups >= end) break;              // (the whole warp)
-        const int h = h0 + u * p.groups + grp;
-        float x[8];
-        open8(raw[u], x);
-        if constexpr (NORM != LQ_NORM_NONE) {
-          float m = 0.f, a = 0.f;
+        for (int q = 0; q < 2; ++q) {
+          const float2 neg = make_float2(-s[q].x, -s[q].y);
+          cross[i].lo[q] = __fmul2_rn(w[i].hi[q], neg);
+          cross[i].hi[q] = __fmul2_rn(w[i].lo[q], s[q]);
+          w[i].lo[q] = __fmul2_rn(w[i].lo[q], c[q]);
+          w[i].hi[q] = __fmul2_rn(w[i].hi[q], c[q]);
           if constexpr (NORM == LQ_NORM_LAYER) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m += x[j];
-            m = group_sum(m, V, v, lane) * p.inv_d;
+            const float2 l = b[i].lo[q];
+            b[i].lo[q] = __ffma2_rn(b[i].hi[q], neg, __fmul2_rn(l, c[q]));
+            b[i].hi[q] = __ffma2_rn(l, s[q], __fmul2_rn(b[i].hi[q], c[q]));
           }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            x[j] -= m;
-            a = fmaf(x[j], x[j], a);
-          }
-          a = group_sum(a, V, v, lane);
-          const float rstd = rsqrtf(fmaf(a, p.inv_d, p.eps));
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = NORM == LQ_NORM_LAYER ? fmaf(x[j] * rstd, w[j], b[j]) : x[j] * rstd * w[j];
         }
-        if (ROT != ROT_NONE && turned) {
+      }
+    }
+    int steps = groups == 1 ? end - begin : (int)__umulhi(end - begin + groups - 1, p.by_groups);
+#pragma unroll 1
+    while (steps > 0) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int lo = SPLIT ? j : 2 * j, hi = SPLIT ? j + 4 : 2 * j + 1;
-            const float a = x[lo], c = x[hi];
-            if (SPLIT || 4 * v + j < p.pairs) {           // (halves turn whole lanes)
-              x[lo] = a * cs[j].x - c * cs[j].y;
-              x[hi] = c * cs[j].x + a * cs[j].y;
+      for (int u = 0; u < DEPTH; ++u) {
+        if (u > 0 && steps <= 0) break;
+        Pairs x[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[i] = open8<NEIGHBOURS>(raw[u][i]);
+        if (left > DEPTH * groups)
+#pragma unroll
+          for (int i = 0; i < C; ++i) raw[u][i] = load_raw<SPLIT>(in + UNIT * L * i, apart);
+        float2 scale = both(1.f);
+        if constexpr (NORM == LQ_NORM_LAYER) {
+          float2 t = both(0.f);
+#pragma unroll
+          for (int i = 0; i < C; ++i) t = __fadd2_rn(t, __fadd2_rn(__fadd2_rn(x[i].lo[0], x[i].lo[1]), __fadd2_rn(x[i].hi[0], x[i].hi[1])));
+          const float2 m = both(-group_sum<L>(t.x + t.y, lanes, v, lane) * p.inv_d);
+#pragma unroll
+          for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) { x[i].lo[q] = __fadd2_rn(x[i].lo[q], m); x[i].hi[q] = __fadd2_rn(x[i].hi[q], m); }
+        }
+        if constexpr (NORM != LQ_NORM_NONE) {
+          float2 t[2] = {both(0.f), both(0.f)};
+#pragma unroll
+          for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) t[q] = __ffma2_rn(x[i].hi[q], x[i].hi[q], __ffma2_rn(x[i].lo[q], x[i].lo[q], t[q]));
+          const float2 a = __fadd2_rn(t[0], t[1]);
+          scale = both(rsqrtf(fmaf(group_sum<L>(a.x + a.y, lanes, v, lane), p.inv_d, p.eps)));
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          Pairs y;
+#pragma unroll
+          for (int q = 0; q < 2; ++q) { y.lo[q] = __fmul2_rn(x[i].lo[q], w[i].lo[q]); y.hi[q] = __fmul2_rn(x[i].hi[q], w[i].hi[q]); }
+          if constexpr (ROT != ROT_NONE && FIXED) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              y.lo[q] = __ffma2_rn(x[i].hi[q], cross[i].lo[q], y.lo[q]);
+              y.hi[q] = __ffma2_rn(x[i].lo[q], cross[i].hi[q], y.hi[q]);
+            }
+          } else if constexpr (ROT != ROT_NONE) {         // (an infinity that is not rotated stays where it is)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              if (2 * q < turns) {
+                y.lo[q].x = fmaf(x[i].hi[q].x, cross[i].lo[q].x, y.lo[q].x);
+                y.hi[q].x = fmaf(x[i].lo[q].x, cross[i].hi[q].x, y.hi[q].x);
+              }
+              if (2 * q + 1 < turns) {
+                y.lo[q].y = fmaf(x[i].hi[q].y, cross[i].lo[q].y, y.lo[q].y);
+                y.hi[q].y = fmaf(x[i].lo[q].y, cross[i].hi[q].y, y.hi[q].y);
+              }
             }
           }
+          if constexpr (NORM != LQ_NORM_NONE) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              y.lo[q] = NORM == LQ_NORM_LAYER ? __ffma2_rn(y.lo[q], scale, b[i].lo[q]) : __fmul2_rn(y.lo[q], scale);
+              y.hi[q] = NORM == LQ_NORM_LAYER ? __ffma2_rn(y.hi[q], scale, b[i].hi[q]) : __fmul2_rn(y.hi[q], scale);
+            }
+          }
+          if (left > 0) store_raw<SPLIT>(out + UNIT * L * i, apart, close8<NEIGHBOURS>(y));
         }
-        if (works && h < end) store8<SPLIT>(out + h * s.out_head, apart, x);
+        in += in_step;
+        out += out_step;
+        left -= groups;
+        --steps;
       }
     }
+    task += WARPS * gridDim.y;
+    if (task < tasks) open_task();
   }
 }
 
+template <typename TIN, typename TOUT, int NORM, int ROT, int L, int C>
+cudaError_t launch(HeadsParams& p, cudaStream_t st) {
+  p.lanes = L > 0 ? L : p.lanes;
+  p.groups = 32 / p.lanes;
+  // A warp walks over all heads of a side, or over as many as the shorter side has (at least four steps), so that warps have like work, once there
+  // are rows enough to fill the GPU (148 SMs x 24 warps); below that over fewer, down to one step.
+  const int g = p.groups, fill = 148 * 24;
+  int walk = std::max(p.heads[0], p.heads[1]);
+  if (p.heads[0] > 0 && p.heads[1] > 0) walk = std::min(walk, std::max(4 * g, std::min(p.heads[0], p.heads[1])));
+  const auto parts = [&](int w) { return (p.heads[0] + w - 1) / w + (p.heads[1] + w - 1) / w; };
+  walk = lq_round_up(walk, g);
+  while (walk > g && (long long)p.rows * parts(walk) < fill) walk -= g;
+  p.walk = walk;
+  for (int i = 0; i < 2; ++i) p.parts[i] = (p.heads[i] + walk - 1) / walk;
+  const int n = p.parts[0] + p.parts[1];
+  p.block_rows = std::max(1, std::min(MAX_ROWS, p.rows / (fill / WARPS)));
+  const int blocks_y = std::max(1, std::min(lq_ceil_div(p.block_rows * n, WARPS), fill / WARPS / lq_ceil_div(p.rows, p.block_rows)));
+  const auto reciprocal = [](int d) { return (uint32_t)(((1ull << 32) + d - 1) / d); };
+  p.by_parts = reciprocal(std::max(2, n));
+  p.by_wide = reciprocal(std::max(4, lq_round_up(p.pairs, 4)));
+  p.by_groups = reciprocal(std::max(2, g));
+  return lq_launch_grid(lq_heads_kernel<TIN, TOUT, NORM, ROT, L, C>, dim3(lq_ceil_div(p.rows, p.block_rows), blocks_y), 32 * WARPS, 1, 0, st, p);
+}
+// Under an RMS norm heads of 64, 72, 112 and 128 entries that are rotated as a whole, or not at all, have their lanes at compile time, 16 or 24 entries
+// to each; others hold eight entries a lane.
 template <typename TIN, typename TOUT, int NORM, int ROT>
-cudaError_t launch(const HeadsParams& p, cudaStream_t st) {
-  return lq_launch(lq_heads_kernel<TIN, TOUT, NORM, ROT>, (p.tasks + WARPS - 1) / WARPS, 32 * WARPS, 0, st, p);
+cudaError_t launch_lanes(HeadsParams& p, cudaStream_t st) {
+  if constexpr (NORM == LQ_NORM_RMS)
+    if (ROT == ROT_NONE || p.pairs == 4 * p.lanes) {
+      if (p.lanes == 8) return launch<TIN, TOUT, NORM, ROT, 4, 2>(p, st);
+      if (p.lanes == 9) return launch<TIN, TOUT, NORM, ROT, 3, 3>(p, st);
+      if (p.lanes == 14) return launch<TIN, TOUT, NORM, ROT, 7, 2>(p, st);
+      if (p.lanes == 16) return launch<TIN, TOUT, NORM, ROT, 8, 2>(p, st);
+    }
+  return launch<TIN, TOUT, NORM, ROT, 0, 1>(p, st);
 }
 template <typename TIN, typename TOUT, int NORM>
-cudaError_t launch_rot(const HeadsParams& p, int rot, cudaStream_t st) {
-  return rot == ROT_NONE ? launch<TIN, TOUT, NORM, ROT_NONE>(p, st) : rot == ROT_PAIRS ? launch<TIN, TOUT, NORM, ROT_PAIRS>(p, st) : launch<TIN, TOUT, NORM, ROT_HALVES>(p, st);
+cudaError_t launch_rot(HeadsParams& p, int rot, cudaStream_t st) {
+  return rot == ROT_NONE    ? launch_lanes<TIN, TOUT, NORM, ROT_NONE>(p, st)
+         : rot == ROT_PAIRS ? launch_lanes<TIN, TOUT, NORM, ROT_PAIRS>(p, st)
+                            : launch_lanes<TIN, TOUT, NORM, ROT_HALVES>(p, st);
 }
 template <typename TIN, typename TOUT>
-cudaError_t launch_norm(const HeadsParams& p, int norm, int rot, cudaStream_t st) {
-  return norm == LQ_NORM_NONE ? launch_rot<TIN, TOUT, LQ_NORM_NONE>(p, rot, st)
-         : norm == LQ_NORM_RMS ? launch_rot<TIN, TOUT, LQ_NORM_RMS>(p, rot, st) : launch_rot<TIN, TOUT, LQ_NORM_LAYER>(p, rot, st);
+cudaError_t launch_norm(HeadsParams& p, int norm, int rot, cudaStream_t st) {
+  return norm == LQ_NORM_NONE  ? launch_rot<TIN, TOUT, LQ_NORM_NONE>(p, rot, st)
+         : norm == LQ_NORM_RMS ? launch_rot<TIN, TOUT, LQ_NORM_RMS>(p, rot, st)
+                               : launch_rot<TIN, TOUT, LQ_NORM_LAYER>(p, rot, st);
 }
 
 // Strides over dimensions of one entry mean nothing; the others keep entries on 16-byte boundaries, and no two outputs on one place.
@@ -233,12 +382,15 @@ lq_status take_side(const lq_heads* h, int sequences, int seq_len, lq_norm norm,
   if (h->heads > 4096) return LQ_ERR_UNSUPPORTED;
   if ((((uintptr_t)h->in | (uintptr_t)h->out | (uintptr_t)h->weight | (uintptr_t)h->bias) & 15) != 0) return LQ_ERR_INVALID_ARG;
   if ((h->weight && norm == LQ_NORM_NONE) || (h->bias && norm != LQ_NORM_LAYER)) return LQ_ERR_INVALID_ARG;
-  *s = Side{h->in, h->out, h->in_seq, h->in_row, h->in_head, h->out_seq, h->out_row, h->out_head, h->weight, h->bias};
-  if (sequences == 1) s->in_seq = s->out_seq = 0;
-  if (seq_len == 1) s->in_row = s->out_row = 0;
-  if (h->heads == 1) s->in_head = s->out_head = 0;
-  for (long long v : {s->in_seq, s->in_row, s->in_head, s->out_seq, s->out_row, s->out_head})
+  const int64_t strides[6] = {sequences == 1 ? 0 : h->in_seq, seq_len == 1 ? 0 : h->in_row, h->heads == 1 ? 0 : h->in_head,
+                              sequences == 1 ? 0 : h->out_seq, seq_len == 1 ? 0 : h->out_row, h->heads == 1 ? 0 : h->out_head};
+  for (int64_t v : strides) {
     if (v % 8 != 0) return LQ_ERR_INVALID_ARG;
+    if (v > INT32_MAX / 32 * 32 || v < -INT32_MAX) return LQ_ERR_UNSUPPORTED;
+  }
+  for (int i : {2, 5})                                       // (a warp steps over up to 32 heads)
+    if (strides[i] > INT32_MAX / 32 || strides[i] < -(INT32_MAX / 32)) return LQ_ERR_UNSUPPORTED;
+  *s = Side{h->in, h->out, (int)strides[0], (int)strides[1], (int)strides[2], (int)strides[3], (int)strides[4], (int)strides[5], h->weight, h->bias};
   if ((sequences > 1 && s->out_seq == 0) || (seq_len > 1 && s->out_row == 0) || (h->heads > 1 && s->out_head == 0)) return LQ_ERR_INVALID_ARG;
   return LQ_OK;
 }
@@ -330,17 +482,10 @@ extern "C" lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32
   lq_status s;
   if (q && (s = take_side(q, sequences, seq_len, norm, &p.side[0])) != LQ_OK) return s;
   if (k && (s = take_side(k, sequences, seq_len, norm, &p.side[1])) != LQ_OK) return s;
-  p.q_heads = q ? q->heads : 0;
-  p.heads = p.q_heads + (k ? k->heads : 0);
+  p.heads[0] = q ? q->heads : 0;
+  p.heads[1] = k ? k->heads : 0;
+  p.rows = (int)rows;
   p.lanes = head_dim / 8;
-  p.groups = 32 / p.lanes;
-  // A warp walks over all heads of its row once there are warps enough to fill the GPU; below that the heads are spread over more warps.
-  const long long walk = lq_ceil_div(p.heads, p.groups), fill = 148 * 32;
-  const long long parts = std::max(1ll, std::min(walk, fill / rows));
-  p.part_heads = (int)((walk + parts - 1) / parts) * p.groups;
-  p.parts = lq_ceil_div(p.heads, p.part_heads);
-  if (rows * p.parts > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
-  p.tasks = (int)(rows * p.parts);
   p.seq_len = seq_len; p.axes = R->axes; p.pairs = R->pairs;
   p.eps = eps; p.inv_d = 1.f / (float)head_dim;
   p.turn = R->d_turn; p.axis = R->d_axis; p.pos = pos;

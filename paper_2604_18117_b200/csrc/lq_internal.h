@@ -231,10 +231,9 @@ extern int g_lq_store_qb;    // option "store_qb": also write the branch activat
 // quantizer -> GEMM -> next quantizer overlaps its launch gaps and tails.  All kernels here are persistent (the whole
 // grid is resident at once), so a waiting successor never holds an SM that a predecessor CTA still needs.
 template <typename... KArgs, typename... Args>
-static inline cudaError_t lq_launch_cluster(void (*kernel)(KArgs...), int grid, int block, int cluster, size_t smem, cudaStream_t st,
-                                            Args&&... args) {
+static inline cudaError_t lq_launch_grid(void (*kernel)(KArgs...), dim3 grid, int block, int cluster, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3((unsigned)grid); lc.blockDim = dim3((unsigned)block); lc.dynamicSmemBytes = smem; lc.stream = st;
+  lc.gridDim = grid; lc.blockDim = dim3((unsigned)block); lc.dynamicSmemBytes = smem; lc.stream = st;
   cudaLaunchAttribute at[2];
   int n = 0;
   if (g_lq_overlap) {
@@ -248,6 +247,10 @@ static inline cudaError_t lq_launch_cluster(void (*kernel)(KArgs...), int grid, 
   }
   lc.attrs = at; lc.numAttrs = (unsigned)n;
   return cudaLaunchKernelEx(&lc, kernel, std::forward<Args>(args)...);
+}
+template <typename... KArgs, typename... Args>
+static inline cudaError_t lq_launch_cluster(void (*kernel)(KArgs...), int grid, int block, int cluster, size_t smem, cudaStream_t st, Args&&... args) {
+  return lq_launch_grid(kernel, dim3((unsigned)grid), block, cluster, smem, st, std::forward<Args>(args)...);
 }
 template <typename... KArgs, typename... Args>
 static inline cudaError_t lq_launch(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t st, Args&&... args) {
