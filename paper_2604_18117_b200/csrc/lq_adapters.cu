@@ -2,51 +2,24 @@
 //
 // A map sorts the rows of a batch by adapter (stable) and cuts them into tiles of rows of one adapter; every projection of a step
 // uses it.
-#include <cuda_fp16.h>
 #include <math.h>
 
 #include <algorithm>
 #include <new>
 
+#include "lq_adapters.h"
 #include "lq_device.cuh"
-#include "lq_internal.h"
 
 using namespace lqdev;
 
 namespace {
 
 constexpr int MAX_SLOTS = 1023;      // bins of the sort: the slots and "none"
-constexpr int TILE_ROWS = 16;
 constexpr int CLUSTER = 8, WARPS = 8;
-
-struct Tile {
-  int adapter, begin, rows, pad;     // adapter -1: none; rows are perm[begin] .. perm[begin + rows - 1]
-};
-struct Meta {
-  int rank;                          // 0: empty slot
-  float scale;
-};
-
-}  // namespace
-
-struct lq_adapters {
-  int K, N, Npad, max_rank, rp, slots, device;  // rp: ranks are stored in rows of so many (16, or a multiple of 32); Npad: N rounded up to 32
-  __half* d_down;                    // [slots][rp][K]     column j of A as a row
-  __half* d_up;                      // [slots][Npad][rp]  column n of B as row lq_col32_slot(n)
-  Meta* d_meta;                      // [slots]
-};
-struct lq_rowmap {
-  int M_max, slots, device, M, tiles_max;
-  int* d_ntiles;
-  Tile* d_tiles;                     // [tiles_max]
-  int* d_perm;                       // [M_max]
-};
-
-namespace {
 
 // ---- the map: a stable counting sort in one block ------------------------------------------------------------------------
 // Each of the 32 warps counts the adapters of its own run of rows, then places them behind those of the warps before it.
-__global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int M, int slots, int tile_rows, int* perm, Tile* tiles, int* ntiles) {
+__global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int M, int slots, int tile_rows, int* perm, LqAdTile* tiles, int* ntiles) {
   extern __shared__ int count[];     // [32][slots + 1]
   __shared__ int scan_rows[32], scan_tiles[32];
   const int bins = slots + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -97,7 +70,7 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     int at = a - rows + (warp > 0 ? scan_rows[warp - 1] : 0);
     const int tile0 = b - nt + (warp > 0 ? scan_tiles[warp - 1] : 0);
     for (int i = 0; i < nt; ++i)
-      tiles[tile0 + i] = Tile{tid < slots ? tid : -1, at + i * tile_rows, min(tile_rows, rows - i * tile_rows), 0};
+      tiles[tile0 + i] = LqAdTile{tid < slots ? tid : -1, at + i * tile_rows, min(tile_rows, rows - i * tile_rows), 0};
     for (int w = 0; w < 32; ++w) {
       const int n = count[w * bins + tid];
       count[w * bins + tid] = at;
@@ -122,7 +95,7 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
 }
 
 // ---- a slot's new adapter in the forwards' layouts ----------------------------------------------------------------------
-__global__ void __launch_bounds__(256) lq_adapters_set_kernel(__half* down, __half* up, Meta* meta, const __half* A, const __half* B, int K, int N, int Npad,
+__global__ void __launch_bounds__(256) lq_adapters_set_kernel(__half* down, __half* up, LqAdMeta* meta, const __half* A, const __half* B, int K, int N, int Npad,
                                                               int rp, int rank, float scale) {
   grid_dependency_wait();            // (no launch_dependents: what follows sees the adapter whole)
   const long long n_down = (long long)rp * K, n_up = (long long)Npad * rp, step = (long long)gridDim.x * blockDim.x;
@@ -137,7 +110,7 @@ __global__ void __launch_bounds__(256) lq_adapters_set_kernel(__half* down, __ha
       up[e] = j < rank && n < N ? B[(long long)j * N + n] : __half(0.f);
     }
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *meta = Meta{rank, scale};
+  if (blockIdx.x == 0 && threadIdx.x == 0) *meta = LqAdMeta{rank, scale};
 }
 
 // ---- fragments ---------------------------------------------------------------------------------------------------------
@@ -150,8 +123,8 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
 // The order of a product's inner index is free as long as both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7
 // of each 32, so that a fragment of either operand is one 16-byte load from rows that run along the inner index.
 template <int RP>
-__global__ void __launch_bounds__(32 * WARPS) lq_adapters_kernel(const Tile* tiles, const int* ntiles, const int* perm, const __half* X, const void* Y0,
-                                                                 void* Y, const __half* down, const __half* up, const Meta* meta, int K, int N, int Npad,
+__global__ void __launch_bounds__(32 * WARPS) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, const int* perm, const __half* X, const void* Y0,
+                                                                 void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad,
                                                                  int out_f32) {
   constexpr int NT = RP / 8, KB = (RP + 31) / 32;
   extern __shared__ __align__(16) float smem[];
@@ -164,8 +137,8 @@ __global__ void __launch_bounds__(32 * WARPS) lq_adapters_kernel(const Tile* til
   grid_launch_dependents();
   grid_dependency_wait();
   if (ti >= *ntiles) return;                              // (the whole cluster)
-  const Tile tile = tiles[ti];
-  const Meta m = tile.adapter >= 0 ? meta[tile.adapter] : Meta{0, 0.f};
+  const LqAdTile tile = tiles[ti];
+  const LqAdMeta m = tile.adapter >= 0 ? meta[tile.adapter] : LqAdMeta{0, 0.f};
   const int unit = warp * CLUSTER + rank_in_cluster, units = WARPS * CLUSTER;
   const bool has0 = g < tile.rows, has1 = g + 8 < tile.rows;
   const long long row0 = has0 ? perm[tile.begin + g] : 0, row1 = has1 ? perm[tile.begin + g + 8] : 0;
@@ -222,10 +195,7 @@ __global__ void __launch_bounds__(32 * WARPS) lq_adapters_kernel(const Tile* til
       }
 #pragma unroll
       for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      // the row's largest magnitude comes to lie in [2^14, 2^15): no half overflows, and hi + lo keep 22 bits of it
-      int e = 0;
-      if (top > 0.f && top < INFINITY) frexpf(top, &e);
-      e = max(-100, min(100, 15 - e));
+      const int e = lq_ad_exponent(top);
       if (lane == 0) row_scale[r] = ldexpf(m.scale, -e);
 #pragma unroll
       for (int q = 0; q < KB; ++q) {
@@ -316,9 +286,8 @@ size_t forward_smem(int rp) {
 }
 template <int RP>
 cudaError_t launch_forward(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
-  const int tiles = std::min(R->M, lq_ceil_div(R->M, TILE_ROWS) + R->slots);
-  return lq_launch_cluster(lq_adapters_kernel<RP>, tiles * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st, (const Tile*)R->d_tiles, (const int*)R->d_ntiles,
-                           (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up, (const Meta*)S->d_meta, S->K,
+  return lq_launch_cluster(lq_adapters_kernel<RP>, lq_ad_tiles(R) * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st, (const LqAdTile*)R->d_tiles, (const int*)R->d_ntiles,
+                           (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up, (const LqAdMeta*)S->d_meta, S->K,
                            S->N, S->Npad, dt == LQ_OUT_F32 ? 1 : 0);
 }
 
@@ -337,14 +306,20 @@ extern "C" lq_status lq_adapters_create(int32_t K, int32_t N, int32_t max_rank, 
   S->rp = max_rank <= 16 ? 16 : lq_round_up(max_rank, 32);
   const size_t n_down = (size_t)slots * S->rp * K, n_up = (size_t)slots * S->Npad * S->rp;
   if (lq_note_cuda(cudaMalloc((void**)&S->d_down, n_down * 2)) != cudaSuccess || lq_note_cuda(cudaMalloc((void**)&S->d_up, n_up * 2)) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&S->d_meta, slots * sizeof(Meta))) != cudaSuccess) {
+      lq_note_cuda(cudaMalloc((void**)&S->d_meta, slots * sizeof(LqAdMeta))) != cudaSuccess) {
     lq_adapters_free(S);
     return LQ_ERR_ALLOC;
   }
-  // (what the factors of an empty slot hold is never read)
-  if (lq_note_cuda(cudaMemset(S->d_meta, 0, slots * sizeof(Meta))) != cudaSuccess || lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess) {
+  // (what the factors of an empty slot hold reaches no output)
+  if (lq_note_cuda(cudaMemset(S->d_meta, 0, slots * sizeof(LqAdMeta))) != cudaSuccess || lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess) {
     lq_adapters_free(S);
     return LQ_ERR_CUDA;
+  }
+  lq_status s;
+  if ((s = lq_make_tmap_bytes(&S->tmDown, S->d_down, (uint64_t)slots * S->rp, (uint64_t)K * 2, (uint32_t)S->rp)) != LQ_OK ||
+      (s = lq_make_tmap_bytes(&S->tmUp, S->d_up, (uint64_t)slots * S->Npad, (uint64_t)S->rp * 2, LQ_AD_TILE)) != LQ_OK) {
+    lq_adapters_free(S);
+    return s;
   }
   *out = S;
   return LQ_OK;
@@ -366,7 +341,7 @@ extern "C" lq_status lq_adapters_set(lq_adapters* S, int32_t slot, int32_t rank,
   LqDeviceGuard guard(S->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   if (rank == 0)                     // nothing to lay out
-    return lq_note_cuda(cudaMemsetAsync(S->d_meta + slot, 0, sizeof(Meta), (cudaStream_t)stream)) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+    return lq_note_cuda(cudaMemsetAsync(S->d_meta + slot, 0, sizeof(LqAdMeta), (cudaStream_t)stream)) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
   const int blocks = (int)std::min(((long long)S->rp * (S->K + S->Npad) + 255) / 256, 4096ll);
   const size_t at = (size_t)slot * S->rp;
   const cudaError_t e = lq_launch(lq_adapters_set_kernel, blocks, 256, 0, (cudaStream_t)stream, S->d_down + at * S->K, S->d_up + at * S->Npad, S->d_meta + slot,
@@ -384,12 +359,31 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
   lq_rowmap* R = new (std::nothrow) lq_rowmap();
   if (!R) return LQ_ERR_ALLOC;
   R->M_max = M_max; R->slots = slots; R->device = device; R->M = 0;
-  R->tiles_max = lq_ceil_div(M_max, TILE_ROWS) + slots + 1;
-  if (lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, sizeof(int))) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&R->d_tiles, (size_t)R->tiles_max * sizeof(Tile))) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&R->d_perm, (size_t)M_max * sizeof(int))) != cudaSuccess) {
+  // (a map of many rows may be set to few, in smaller tiles)
+  R->tiles_max = std::max(lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M), LQ_AD_SMALL_TILE), lq_ceil_div(M_max, LQ_AD_TILE)) + slots + 1;
+  const size_t rows = M_max > LQ_AD_SMALL_M ? (size_t)M_max + LQ_AD_TILE : 0;
+  if (lq_note_cuda(cudaDeviceGetAttribute(&R->sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, sizeof(int))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_tiles, (size_t)R->tiles_max * sizeof(LqAdTile))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_perm, (size_t)M_max * sizeof(int))) != cudaSuccess ||
+      (rows > 0 && (lq_note_cuda(cudaMalloc((void**)&R->d_T, rows * LQ_AD_TROW * 2)) != cudaSuccess ||
+                    lq_note_cuda(cudaMalloc((void**)&R->d_rscale, rows * sizeof(float))) != cudaSuccess))) {
     lq_rowmap_free(R);
     return LQ_ERR_ALLOC;
+  }
+  // (T's rows are read in whole tiles: from defined contents on)
+  lq_status s;
+  if (rows > 0 && (lq_note_cuda(cudaMemset(R->d_T, 0, rows * LQ_AD_TROW * 2)) != cudaSuccess || lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess)) {
+    lq_rowmap_free(R);
+    return LQ_ERR_CUDA;
+  }
+  if (!lq_device_status_ptr(device)) {                      // (allocated here, not under a capture)
+    lq_rowmap_free(R);
+    return LQ_ERR_CUDA;
+  }
+  if (rows > 0 && ((s = lq_make_tmap_bytes(&R->tmT, R->d_T, rows, LQ_AD_TROW * 2, LQ_AD_TILE)) != LQ_OK || (s = lq_adapters_tiles_prepare()) != LQ_OK)) {
+    lq_rowmap_free(R);
+    return s;
   }
   if (lq_note_cuda(cudaFuncSetAttribute(lq_rowmap_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * (MAX_SLOTS + 1) * 4)) != cudaSuccess ||
       lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(16))) != cudaSuccess ||
@@ -407,7 +401,7 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
 extern "C" lq_status lq_rowmap_free(lq_rowmap* R) {
   if (!R) return LQ_ERR_INVALID_ARG;
   LqDeviceGuard guard(R->device);
-  cudaFree(R->d_ntiles); cudaFree(R->d_tiles); cudaFree(R->d_perm);
+  cudaFree(R->d_ntiles); cudaFree(R->d_tiles); cudaFree(R->d_perm); cudaFree(R->d_T); cudaFree(R->d_rscale);
   delete R;
   return LQ_OK;
 }
@@ -416,10 +410,12 @@ extern "C" lq_status lq_rowmap_set(lq_rowmap* R, const int32_t* ids, int32_t M, 
   if (!R || !ids || M <= 0 || M > R->M_max || ((uintptr_t)ids & 3) != 0) return LQ_ERR_INVALID_ARG;
   LqDeviceGuard guard(R->device);
   if (!guard.ok) return LQ_ERR_CUDA;
-  const cudaError_t e = lq_launch(lq_rowmap_kernel, 1, 1024, (size_t)32 * (R->slots + 1) * 4, (cudaStream_t)stream, ids, M, R->slots, TILE_ROWS, R->d_perm,
+  const int tile_rows = M <= LQ_AD_SMALL_M ? LQ_AD_SMALL_TILE : LQ_AD_TILE;
+  const cudaError_t e = lq_launch(lq_rowmap_kernel, 1, 1024, (size_t)32 * (R->slots + 1) * 4, (cudaStream_t)stream, ids, M, R->slots, tile_rows, R->d_perm,
                                   R->d_tiles, R->d_ntiles);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
   R->M = M;
+  R->tile_rows = tile_rows;
   return LQ_OK;
 }
 
@@ -431,6 +427,7 @@ extern "C" lq_status lq_adapters_forward(const lq_adapters* S, const lq_rowmap* 
   LqDeviceGuard guard(S->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
+  if (R->tile_rows == LQ_AD_TILE) return lq_adapters_forward_tiles(S, R, X, Y0, Y, dt, st);
   const cudaError_t e = S->rp == 16   ? launch_forward<16>(S, R, X, Y0, Y, dt, st)
                         : S->rp == 32 ? launch_forward<32>(S, R, X, Y0, Y, dt, st)
                         : S->rp == 64 ? launch_forward<64>(S, R, X, Y0, Y, dt, st)

@@ -1,0 +1,473 @@
+// Low-rank adapters, the form for many rows: two kernels on tiles of 128 rows of one adapter.
+//
+//   down   T = X A of a tile, K shared by a cluster of CTAs; each row of T leaves as two halves under a power of two
+//   up     Y = Y0 + (scale / power of two) T B, tile by tile and 128 columns at a time
+//
+// Both are bound by the memory: X is read once, Y0 once, Y is written once; T is 512 bytes a row at most and stays in the L2, the factors too.
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "lq_adapters.h"
+#include "lq_device.cuh"
+
+using namespace lqdev;
+
+namespace {
+
+constexpr int BM = LQ_AD_TILE, A_STAGE = BM * 128;      // a stage: 64 halves of K
+constexpr int MAX_STAGES = 8;
+
+// four rows of a tensor, wherever they lie
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* tm, int x, const int4& rows, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ float4 ld_peer_v4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t pack_halves(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// ---- down ----------------------------------------------------------------------------------------------------------
+struct DownParams {
+  const LqAdTile* tiles;
+  const int *ntiles, *perm;
+  const LqAdMeta* meta;
+  __half* T;
+  float* rscale;
+  int32_t* status;
+  int rp, split, k_stages, ring, tmem_cols;
+};
+
+// One tile a cluster, K / (64 split) stages a CTA.  Warp 0 fetches (a tile's rows are neighbours in X where a request's rows are: one copy; else four rows
+// a copy, one copy a lane), warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial sums to shared memory and each CTA
+// adds up 128 / split rows from all of the cluster, always in the same order.
+__global__ void __launch_bounds__(128) lq_adapters_down_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmXrow,
+                                                               const __grid_constant__ CUtensorMap tmDown, const __grid_constant__ DownParams p) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t bars[2 * MAX_STAGES + 1];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int abort_flag;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int stage_bytes = A_STAGE + p.rp * 128;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int ti = blockIdx.x / p.split, part = blockIdx.x - ti * p.split;
+  auto full = [&](int s) { return smem_u32(&bars[s]); };
+  auto empty = [&](int s) { return smem_u32(&bars[MAX_STAGES + s]); };
+  const uint32_t done = smem_u32(&bars[2 * MAX_STAGES]);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    mbar_init(done, 1);
+    abort_flag = 0;
+    mbar_init_fence();
+  }
+  if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), p.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  grid_launch_dependents();
+  grid_dependency_wait();
+
+  LqAdTile tile = {-1, 0, 0, 0};
+  if (ti < *p.ntiles) tile = p.tiles[ti];
+  LqAdMeta m = {0, 0.f};
+  if (tile.adapter >= 0) m = p.meta[tile.adapter];
+  if (m.rank > 0) {                                       // (the same for the whole cluster)
+    const int k0 = part * p.k_stages / p.split, n = (part + 1) * p.k_stages / p.split - k0;
+    bool ok = true;
+    if (warp == 0) {
+      int4 rows;
+      {
+        const int* from = p.perm + tile.begin;
+        rows.x = from[min(4 * lane, tile.rows - 1)];      // (rows behind the tile's last: any, they are not stored)
+        rows.y = from[min(4 * lane + 1, tile.rows - 1)];
+        rows.z = from[min(4 * lane + 2, tile.rows - 1)];
+        rows.w = from[min(4 * lane + 3, tile.rows - 1)];
+      }
+      const int row0 = __shfl_sync(0xffffffffu, rows.x, 0), row_last = __shfl_sync(0xffffffffu, rows.w, 31);
+      const bool neighbours = row_last - row0 == tile.rows - 1;      // (perm ascends within a tile)
+      for (int it = 0; it < n; ++it) {
+        const int s = it % p.ring;
+        if (it >= p.ring && !(ok = mbar_wait_warp(empty(s), ((it / p.ring) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
+        const uint32_t a = base + s * stage_bytes;
+        if (lane == 0) mbar_expect_tx(full(s), stage_bytes);
+        __syncwarp();
+        const int x = (k0 + it) * 128;                    // bytes along K
+        if (!neighbours) tma_gather4(a + lane * 512, &tmXrow, x, rows, full(s));
+        if (lane == 0) {
+          if (neighbours) tma_load_2d(a, &tmX, x, row0, full(s));
+          tma_load_2d(a + A_STAGE, &tmDown, x, tile.adapter * p.rp, full(s));
+        }
+      }
+      if (!ok)                                            // copies in flight land before the CTA goes
+        for (int it = max(0, n - p.ring); it < n; ++it) mbar_settle(full(it % p.ring), (it / p.ring) & 1);
+    } else if (warp == 1 && lane == 0) {
+      const uint32_t idesc = IDESC_F16 | idesc_shape(p.rp);
+      for (int it = 0; it < n; ++it) {
+        const int s = it % p.ring;
+        if (!mbar_wait(full(s), (it / p.ring) & 1, &abort_flag, p.status, LQ_STAGE_MMA)) break;
+        tc_fence_after();
+        const uint64_t a = make_smem_desc(base + s * stage_bytes), b = make_smem_desc(base + s * stage_bytes + A_STAGE);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tc_mma<TC_F16>(tmem, a + 2 * k, b + 2 * k, idesc, (it | k) != 0);
+        tc_commit(empty(s));
+      }
+      tc_commit(done);
+    }
+    __syncwarp();
+    ok = mbar_wait(done, 0, &abort_flag, p.status, LQ_STAGE_DRAIN);
+    ok = __syncthreads_and(ok && !abort_flag) != 0;
+    // partial sums -> shared memory, rows 16 bytes longer than they are so that neighbouring rows lie in different banks; the ring is free: the MMAs have read it
+    const int pitch = p.rp + 4;
+    float* sums = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)));
+    if (ok) {
+      tc_fence_after();
+      const int row = warp * 32 + lane;
+      for (int c = 0; c < p.rp; c += 16) {
+        uint32_t v[16];
+        tmem_ld_32x16(tmem + ((uint32_t)(warp * 32) << 16) + c, v);
+        tmem_ld_wait();
+        float4* to = reinterpret_cast<float4*>(sums + row * pitch + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[j] = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3]));
+      }
+    }
+    if (p.split > 1) cluster_sync();
+    else __syncthreads();
+    if (ok) {
+      // eight threads to a row
+      const int rows_here = BM / p.split, j0 = threadIdx.x & 7;
+      for (int r = threadIdx.x >> 3; r < rows_here; r += 16) {
+        const int row = part * rows_here + r;
+        float4 v[4];
+        float top = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int j = j0 + 8 * q;
+          v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (4 * j < p.rp) {
+            const uint32_t at = base + (uint32_t)(row * pitch + 4 * j) * 4;
+            for (int w = 0; w < p.split; ++w) {
+              const float4 u = ld_peer_v4(p.split > 1 ? peer_smem(at, w) : at);
+              v[q].x += u.x; v[q].y += u.y; v[q].z += u.z; v[q].w += u.w;
+            }
+          }
+          top = fmaxf(fmaxf(top, fmaxf(fabsf(v[q].x), fabsf(v[q].y))), fmaxf(fabsf(v[q].z), fabsf(v[q].w)));
+        }
+#pragma unroll
+        for (int d = 1; d < 8; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        if (row < tile.rows) {
+          const int e = lq_ad_exponent(top);
+          const float f = ldexpf(1.f, e);                 // (|e| <= 100: exact)
+          __half* to = p.T + (size_t)(tile.begin + row) * LQ_AD_TROW;
+          if (j0 == 0) p.rscale[tile.begin + row] = ldexpf(m.scale, -e);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int j = j0 + 8 * q;
+            if (4 * j < p.rp) {
+              const float u[4] = {v[q].x * f, v[q].y * f, v[q].z * f, v[q].w * f};
+              float lo[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) lo[i] = u[i] - __half2float(__float2half_rn(u[i]));
+              *reinterpret_cast<uint2*>(to + 4 * j) = make_uint2(pack_halves(u[0], u[1]), pack_halves(u[2], u[3]));
+              *reinterpret_cast<uint2*>(to + LQ_AD_TROW / 2 + 4 * j) = make_uint2(pack_halves(lo[0], lo[1]), pack_halves(lo[2], lo[3]));
+            }
+          }
+        }
+      }
+    }
+    if (p.split > 1) cluster_sync();                      // the others have read this CTA's sums
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+}
+
+// ---- up ------------------------------------------------------------------------------------------------------------
+constexpr int UP_DRAIN_WARPS = 16, UP_THREADS = 32 * (2 + UP_DRAIN_WARPS), UP_COLS = 128;
+
+struct UpParams {
+  const LqAdTile* tiles;
+  const int *ntiles, *perm;
+  const LqAdMeta* meta;
+  const float* rscale;
+  const void* Y0;
+  void* Y;
+  int32_t* status;
+  int N, Npad, chunks;
+};
+
+// Persistent, one CTA an SM: the steps (tile, 128 columns) of all tiles are cut into runs of like length.  Warp 0 fetches a tile's T (both halves, into one
+// of two buffers) and each step's slab of B, warp 1 issues hi B + lo B into one of two accumulators, the drain warps hold 32 rows x 32 columns each: they
+// have asked for Y0 a step ahead, add, round and store; B's rows lie in the order that gives a lane eight neighbouring columns.
+template <bool F32, int NA>      // NA: 64-wide pieces of the rank
+__global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmUp,
+                                                                       const __grid_constant__ UpParams p) {
+  constexpr int NB = NA == 1 ? 3 : 2, PIECE = BM * 128, T_BUF = 2 * NA * PIECE, B_STAGE = NA * PIECE;
+  extern __shared__ unsigned char smem_raw[];
+  enum { TFULL = 0, TFREE = 2, BFULL = 4, BFREE = BFULL + NB, AFULL = BFREE + NB, AFREE = AFULL + 2, NBAR = AFREE + 2 };
+  __shared__ __align__(8) uint64_t bars[NBAR];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int abort_flag;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto bar = [&](int i) { return smem_u32(&bars[i]); };
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NBAR; ++i) mbar_init(bar(i), i >= AFREE ? UP_DRAIN_WARPS : 1);
+    abort_flag = 0;
+    mbar_init_fence();
+  }
+  if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), 2 * UP_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  grid_launch_dependents();
+  grid_dependency_wait();
+
+  const long long total = (long long)*p.ntiles * p.chunks;
+  const long long lo = total * blockIdx.x / gridDim.x, hi = total * (blockIdx.x + 1) / gridDim.x;
+  const int n = (int)(hi - lo), ti0 = (int)(lo / p.chunks), ch0 = (int)(lo - (long long)ti0 * p.chunks);
+  const auto rank_of = [&](const LqAdTile& t) { return t.adapter >= 0 ? p.meta[t.adapter].rank : 0; };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      bool ok = true;
+      int t_uses = 0, b_uses = 0;
+      LqAdTile tile = {};
+      int rank = 0;
+      for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
+        if (i == 0 || ch == 0) {
+          tile = p.tiles[ti];
+          rank = rank_of(tile);
+          if (rank > 0) {
+            const int buf = t_uses & 1, pieces = (rank + 63) / 64;
+            if (t_uses >= 2) ok = mbar_wait(bar(TFREE + buf), ((t_uses >> 1) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER);
+            if (ok) {
+              mbar_expect_tx(bar(TFULL + buf), 2 * pieces * PIECE);
+              for (int a = 0; a < pieces; ++a) {
+                tma_load_2d(base + buf * T_BUF + a * PIECE, &tmT, 128 * a, tile.begin, bar(TFULL + buf));
+                tma_load_2d(base + buf * T_BUF + (NA + a) * PIECE, &tmT, LQ_AD_TROW + 128 * a, tile.begin, bar(TFULL + buf));
+              }
+              ++t_uses;
+            }
+          }
+        }
+        if (rank > 0 && ok) {
+          const int s = b_uses % NB, pieces = (rank + 63) / 64;
+          if (b_uses >= NB) ok = mbar_wait(bar(BFREE + s), ((b_uses / NB) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER);
+          if (ok) {
+            mbar_expect_tx(bar(BFULL + s), pieces * PIECE);
+            for (int a = 0; a < pieces; ++a)
+              tma_load_2d(base + 2 * T_BUF + s * B_STAGE + a * PIECE, &tmUp, 128 * a, tile.adapter * p.Npad + UP_COLS * ch, bar(BFULL + s));
+            ++b_uses;
+          }
+        }
+        if (++ch == p.chunks) { ch = 0; ++ti; }
+      }
+      if (!ok) {                                          // copies in flight land before the CTA goes
+        for (int u = max(0, t_uses - 2); u < t_uses; ++u) mbar_settle(bar(TFULL + (u & 1)), (u >> 1) & 1);
+        for (int u = max(0, b_uses - NB); u < b_uses; ++u) mbar_settle(bar(BFULL + u % NB), (u / NB) & 1);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      bool ok = true;
+      int t_uses = 0, b_uses = 0, rank = 0;
+      constexpr uint32_t idesc = IDESC_F16 | idesc_shape(UP_COLS);
+      for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
+        if (i == 0 || ch == 0) {
+          rank = rank_of(p.tiles[ti]);
+          if (rank > 0) {
+            ok = mbar_wait(bar(TFULL + (t_uses & 1)), (t_uses >> 1) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
+            ++t_uses;
+          }
+        }
+        if (rank > 0 && ok) {
+          const int s = b_uses % NB, acc = b_uses & 1, buf = (t_uses - 1) & 1;
+          if (b_uses >= 2) ok = mbar_wait(bar(AFREE + acc), ((b_uses >> 1) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_MMA);
+          ok = ok && mbar_wait(bar(BFULL + s), (b_uses / NB) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
+          if (ok) {
+            tc_fence_after();
+            const int steps = (rank + 15) / 16;
+            for (int part = 0; part < 2; ++part)
+              for (int k = 0; k < steps; ++k) {
+                const uint64_t a = make_smem_desc(base + buf * T_BUF + (part * NA + (k >> 2)) * PIECE) + 2 * (k & 3);
+                const uint64_t b = make_smem_desc(base + 2 * T_BUF + s * B_STAGE + (k >> 2) * PIECE) + 2 * (k & 3);
+                tc_mma<TC_F16>(tmem + acc * UP_COLS, a, b, idesc, (part | k) != 0);
+              }
+            tc_commit(bar(BFREE + s));
+            tc_commit(bar(AFULL + acc));
+            if (i + 1 == n || ch + 1 == p.chunks) tc_commit(bar(TFREE + buf));
+            ++b_uses;
+          }
+        }
+        if (++ch == p.chunks) { ch = 0; ++ti; }
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------------- drain
+    const int quad = warp & 3, cq = (warp - 2) >> 2, g = lane >> 2, t = lane & 3;
+    const uint32_t tlane = tmem + ((uint32_t)(quad * 32) << 16) + 32 * cq;
+    constexpr int YW = F32 ? 2 : 1;                       // 16-byte words of a lane's eight columns
+    constexpr bool AHEAD = !F32;                          // (two steps of fp32 values do not fit the registers)
+    const bool in_place = p.Y0 == p.Y;
+    struct Rows {
+      int row[4];                                         // -1: none
+      float scale[4];
+      int rank;
+    };
+    const auto rows_of = [&](int ti) {
+      const LqAdTile tile = p.tiles[ti];
+      Rows r;
+      r.rank = rank_of(tile);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = quad * 32 + g + 8 * i;
+        const bool in = at < tile.rows && (r.rank > 0 || !in_place);       // a row without an adapter is left alone, or copied
+        r.row[i] = in ? p.perm[tile.begin + at] : -1;
+        r.scale[i] = in && r.rank > 0 ? p.rscale[tile.begin + at] : 0.f;
+      }
+      return r;
+    };
+    const auto ask = [&](const Rows& r, int ch, uint4 (&y)[4][YW]) {
+      const int c = ch * UP_COLS + 32 * cq + 8 * t;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r.row[i] >= 0 && c < p.N) {
+          const uint4* from = F32 ? reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(p.Y0) + (size_t)r.row[i] * p.N + c)
+                                  : reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(p.Y0) + (size_t)r.row[i] * p.N + c);
+#pragma unroll
+          for (int w = 0; w < YW; ++w) y[i][w] = from[w];
+        }
+    };
+    int uses = 0;
+    Rows r = {}, r_next = {};
+    uint4 y[4][YW], y_next[AHEAD ? 4 : 1][YW];
+    if (n > 0) {
+      r = rows_of(ti0);
+      if constexpr (AHEAD) ask(r, ch0, y);
+    }
+    bool ok = true;
+    for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
+      const int ch_next = ch + 1 == p.chunks ? 0 : ch + 1, ti_next = ti + (ch_next == 0);
+      if constexpr (AHEAD) {
+        if (i + 1 < n) {
+          if (ch_next == 0) {
+            r_next = rows_of(ti_next);
+            ask(r_next, 0, y_next);
+          } else {
+            ask(r, ch_next, y_next);
+          }
+        }
+      } else {
+        ask(r, ch, y);
+      }
+      uint32_t v[2][16];
+      if (r.rank > 0) {
+        const int acc = uses & 1;
+        ok = mbar_wait_warp(bar(AFULL + acc), (uses >> 1) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN);
+        if (!ok) break;
+        ++uses;
+        tc_fence_after();
+        tmem_ld_16x256b_x4(tlane + acc * UP_COLS, v[0]);
+        tmem_ld_16x256b_x4(tlane + (16u << 16) + acc * UP_COLS, v[1]);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(AFREE + acc));
+      }
+      const int c = ch * UP_COLS + 32 * cq + 8 * t;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (r.row[q] >= 0 && c < p.N) {
+          // fragment registers 4 j .. 4 j + 3: row g, columns 2 j, 2 j + 1 of this lane's eight, then row g + 8 the same columns
+          const int h = q >> 1, at = 2 * (q & 1);
+          if constexpr (F32) {
+            float* f = reinterpret_cast<float*>(&y[q][0]);
+            if (r.rank > 0)                               // (a row without an adapter keeps its bits)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f[j] = fmaf(r.scale[q], __uint_as_float(v[h][4 * (j >> 1) + at + (j & 1)]), f[j]);
+            uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.Y) + (size_t)r.row[q] * p.N + c);
+            to[0] = y[q][0]; to[YW - 1] = y[q][YW - 1];
+          } else {
+            __half2* f = reinterpret_cast<__half2*>(&y[q][0]);
+            if (r.rank > 0)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float2 a = __half22float2(f[j]);
+                f[j] = __floats2half2_rn(fmaf(r.scale[q], __uint_as_float(v[h][4 * j + at]), a.x), fmaf(r.scale[q], __uint_as_float(v[h][4 * j + at + 1]), a.y));
+              }
+            *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(p.Y) + (size_t)r.row[q] * p.N + c) = y[q][0];
+          }
+        }
+      if constexpr (AHEAD) {
+        if (ch_next == 0) r = r_next;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q][0] = y_next[q][0];
+      } else if (ch_next == 0 && i + 1 < n) {
+        r = rows_of(ti_next);
+      }
+      ch = ch_next; ti = ti_next;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 2 * UP_COLS);
+  }
+}
+
+constexpr int up_smem(int na) { return 1024 + 2 * (2 * na * BM * 128) + (na == 1 ? 3 : 2) * na * BM * 128; }
+constexpr int DOWN_SMEM = 110 * 1024;                     // two CTAs an SM
+
+template <bool F32, int NA>
+cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const UpParams& p, cudaStream_t st) {
+  const long long steps = (long long)lq_ad_tiles(R) * p.chunks;
+  return lq_launch(lq_adapters_up_kernel<F32, NA>, (int)std::min<long long>(steps, R->sms), UP_THREADS, up_smem(NA), st, R->tmT, S->tmUp, p);
+}
+
+}  // namespace
+
+lq_status lq_adapters_tiles_prepare() {
+  const auto room = [](auto* kernel, int bytes) { return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) == cudaSuccess; };
+  return room(lq_adapters_down_kernel, DOWN_SMEM) && room(lq_adapters_up_kernel<false, 1>, up_smem(1)) && room(lq_adapters_up_kernel<true, 1>, up_smem(1)) &&
+                 room(lq_adapters_up_kernel<false, 2>, up_smem(2)) && room(lq_adapters_up_kernel<true, 2>, up_smem(2))
+             ? LQ_OK
+             : LQ_ERR_CUDA;
+}
+
+lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
+  CUtensorMap tmX, tmXrow;
+  lq_status s;
+  if ((s = lq_make_tmap_bytes(&tmX, const_cast<void*>(X), (uint64_t)R->M, (uint64_t)S->K * 2, BM)) != LQ_OK) return s;
+  if ((s = lq_make_tmap_bytes(&tmXrow, const_cast<void*>(X), (uint64_t)R->M, (uint64_t)S->K * 2, 1)) != LQ_OK) return s;
+  int32_t* status = lq_device_status_ptr(S->device);
+  if (!status) return LQ_ERR_CUDA;
+  DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, S->rp, 1, lq_ceil_div(S->K, 64), 1, 32};
+  // K is shared by as many CTAs as fill the SMs twice over, each with at least two stages
+  const int tiles = lq_ceil_div(R->M, BM);
+  while (d.split < 8 && tiles * 2 * d.split <= 2 * R->sms && d.k_stages >= 4 * d.split) d.split *= 2;
+  const int stage = A_STAGE + S->rp * 128, most = (d.k_stages + d.split - 1) / d.split;
+  d.ring = std::min(std::min(MAX_STAGES, most), (DOWN_SMEM - 1024) / stage);
+  while (d.tmem_cols < S->rp) d.tmem_cols *= 2;
+  const int smem = 1024 + std::max(d.ring * stage, BM * (S->rp + 4) * 4);
+  cudaError_t e = lq_launch_cluster(lq_adapters_down_kernel, lq_ad_tiles(R) * d.split, 128, d.split, smem, st, tmX, tmXrow, S->tmDown, d);
+  if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
+  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y0, Y, status, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS)};
+  if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, u, st) : launch_up<true, 2>(S, R, u, st);
+  else e = S->rp <= 64 ? launch_up<false, 1>(S, R, u, st) : launch_up<false, 2>(S, R, u, st);
+  return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+}
