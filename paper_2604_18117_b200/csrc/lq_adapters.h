@@ -10,7 +10,8 @@ constexpr int LQ_AD_SMALL_M = 256, LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
 constexpr int LQ_AD_TROW = 256;        // halves of a row of the intermediate: 128 hi, 128 lo
 
 struct LqAdTile {
-  int adapter, begin, rows, pad;       // adapter -1: none; rows are perm[begin] .. perm[begin + rows - 1]
+  int adapter, begin, rows, first;     // adapter -1: none; rows are perm[begin] .. perm[begin + rows - 1]; first: perm[begin] where the
+                                       // rows are neighbours, else -1
 };
 struct LqAdMeta {
   int rank;                            // 0: empty slot

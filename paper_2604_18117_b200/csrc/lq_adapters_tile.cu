@@ -25,6 +25,10 @@ __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* tm,
                "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar)
                : "memory");
 }
+// the four rows that a lane fetches of a tile (behind the tile's last row: that one again)
+__device__ __forceinline__ int4 tile_rows4(const int* perm, int rows, int lane) {
+  return make_int4(perm[min(4 * lane, rows - 1)], perm[min(4 * lane + 1, rows - 1)], perm[min(4 * lane + 2, rows - 1)], perm[min(4 * lane + 3, rows - 1)]);
+}
 __device__ __forceinline__ float4 ld_peer_v4(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
@@ -46,8 +50,8 @@ struct DownParams {
   int rp, split, k_stages, ring, tmem_cols;
 };
 
-// One tile a cluster, K / (64 split) stages a CTA.  Warp 0 fetches (a tile's rows are neighbours in X where a request's rows are: one copy; else four rows
-// a copy, one copy a lane), warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial sums to shared memory and each CTA
+// One tile a cluster, K / (64 split) stages a CTA.  Warp 0 fetches (a whole tile of neighbouring rows in one copy, else four rows a copy, one copy a
+// lane), warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial sums to shared memory and each CTA
 // adds up 128 / split rows from all of the cluster, always in the same order.
 __global__ void __launch_bounds__(128) lq_adapters_down_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmXrow,
                                                                const __grid_constant__ CUtensorMap tmDown, const __grid_constant__ DownParams p) {
@@ -76,34 +80,31 @@ __global__ void __launch_bounds__(128) lq_adapters_down_kernel(const __grid_cons
   grid_launch_dependents();
   grid_dependency_wait();
 
-  LqAdTile tile = {-1, 0, 0, 0};
-  if (ti < *p.ntiles) tile = p.tiles[ti];
+  // (a tile behind the last one holds anything: it is asked for together with their number, which saves a trip)
+  LqAdTile tile = p.tiles[ti];
+  if (ti >= *p.ntiles) tile.adapter = -1;
   LqAdMeta m = {0, 0.f};
-  if (tile.adapter >= 0) m = p.meta[tile.adapter];
+  int4 rows = make_int4(0, 0, 0, 0);
+  if (tile.adapter >= 0) {
+    m = p.meta[tile.adapter];
+    if (warp == 0) rows = tile_rows4(p.perm + tile.begin, tile.rows, lane);
+  }
   if (m.rank > 0) {                                       // (the same for the whole cluster)
     const int k0 = part * p.k_stages / p.split, n = (part + 1) * p.k_stages / p.split - k0;
     bool ok = true;
     if (warp == 0) {
-      int4 rows;
-      {
-        const int* from = p.perm + tile.begin;
-        rows.x = from[min(4 * lane, tile.rows - 1)];      // (rows behind the tile's last: any, they are not stored)
-        rows.y = from[min(4 * lane + 1, tile.rows - 1)];
-        rows.z = from[min(4 * lane + 2, tile.rows - 1)];
-        rows.w = from[min(4 * lane + 3, tile.rows - 1)];
-      }
-      const int row0 = __shfl_sync(0xffffffffu, rows.x, 0), row_last = __shfl_sync(0xffffffffu, rows.w, 31);
-      const bool neighbours = row_last - row0 == tile.rows - 1;      // (perm ascends within a tile)
+      const bool whole = tile.first >= 0 && tile.rows == BM;
+      const uint32_t a_bytes = whole ? A_STAGE : (tile.rows + 3) / 4 * 512;
       for (int it = 0; it < n; ++it) {
         const int s = it % p.ring;
         if (it >= p.ring && !(ok = mbar_wait_warp(empty(s), ((it / p.ring) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
         const uint32_t a = base + s * stage_bytes;
-        if (lane == 0) mbar_expect_tx(full(s), stage_bytes);
+        if (lane == 0) mbar_expect_tx(full(s), a_bytes + p.rp * 128);
         __syncwarp();
         const int x = (k0 + it) * 128;                    // bytes along K
-        if (!neighbours) tma_gather4(a + lane * 512, &tmXrow, x, rows, full(s));
+        if (!whole && 4 * lane < tile.rows) tma_gather4(a + lane * 512, &tmXrow, x, rows, full(s));
         if (lane == 0) {
-          if (neighbours) tma_load_2d(a, &tmX, x, row0, full(s));
+          if (whole) tma_load_2d(a, &tmX, x, tile.first, full(s));
           tma_load_2d(a + A_STAGE, &tmDown, x, tile.adapter * p.rp, full(s));
         }
       }
@@ -195,28 +196,34 @@ __global__ void __launch_bounds__(128) lq_adapters_down_kernel(const __grid_cons
 }
 
 // ---- up ------------------------------------------------------------------------------------------------------------
-constexpr int UP_DRAIN_WARPS = 16, UP_THREADS = 32 * (2 + UP_DRAIN_WARPS), UP_COLS = 128;
+constexpr int UP_DRAIN_WARPS = 16, UP_FIRST_DRAIN = 4, UP_THREADS = 32 * (UP_FIRST_DRAIN + UP_DRAIN_WARPS), UP_COLS = 128;
+constexpr int PIECE = BM * 128, Y_SLOTS = 6;              // 128 rows x 128 bytes
+__host__ __device__ constexpr int up_t_bufs(int na) { return na == 1 ? 2 : 1; }
+__host__ __device__ constexpr int up_b_stages(int na) { return na == 1 ? 3 : 2; }
+constexpr int up_smem(int na) { return 1024 + (2 * na * up_t_bufs(na) + na * up_b_stages(na) + Y_SLOTS) * PIECE; }
 
 struct UpParams {
   const LqAdTile* tiles;
   const int *ntiles, *perm;
   const LqAdMeta* meta;
   const float* rscale;
-  const void* Y0;
   void* Y;
   int32_t* status;
-  int N, Npad, chunks;
+  int N, Npad, chunks, in_place;
 };
 
-// Persistent, one CTA an SM: the steps (tile, 128 columns) of all tiles are cut into runs of like length.  Warp 0 fetches a tile's T (both halves, into one
-// of two buffers) and each step's slab of B, warp 1 issues hi B + lo B into one of two accumulators, the drain warps hold 32 rows x 32 columns each: they
-// have asked for Y0 a step ahead, add, round and store; B's rows lie in the order that gives a lane eight neighbouring columns.
+// Persistent, one CTA an SM: the steps (tile, 128 columns) of all tiles are cut into runs of like length.  Warp 0 fetches a tile's T (both halves) and each
+// step's slab of B, warp 1 issues hi B + lo B into one of two accumulators, warp 2 fetches Y0 into a ring of 96 KB, pieces of 128 rows x 128 bytes; the
+// drain warps hold 32 rows x 32 columns each: they add, round and store.  B's rows lie in the order that gives a lane eight neighbouring columns.
+// (Y0 straight into registers a step ahead, 32 KB in flight: 30.7 us for 8192 x 3456, rank 32, against 17.3 at the measured copy rate.)
 template <bool F32, int NA>      // NA: 64-wide pieces of the rank
 __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmUp,
+                                                                       const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmYrow,
                                                                        const __grid_constant__ UpParams p) {
-  constexpr int NB = NA == 1 ? 3 : 2, PIECE = BM * 128, T_BUF = 2 * NA * PIECE, B_STAGE = NA * PIECE;
+  constexpr int NT = up_t_bufs(NA), NB = up_b_stages(NA), T_BUF = 2 * NA * PIECE, B_STAGE = NA * PIECE, B_AT = NT * T_BUF, Y_AT = B_AT + NB * B_STAGE;
+  constexpr int YP = F32 ? 4 : 2, Y_READERS = UP_DRAIN_WARPS / YP;      // pieces of a step; warps that read one
   extern __shared__ unsigned char smem_raw[];
-  enum { TFULL = 0, TFREE = 2, BFULL = 4, BFREE = BFULL + NB, AFULL = BFREE + NB, AFREE = AFULL + 2, NBAR = AFREE + 2 };
+  enum { TFULL = 0, TFREE = NT, BFULL = 2 * NT, BFREE = BFULL + NB, AFULL = BFREE + NB, YFULL = AFULL + 2, AFREE = YFULL + Y_SLOTS, YFREE = AFREE + 2, NBAR = YFREE + Y_SLOTS };
   __shared__ __align__(8) uint64_t bars[NBAR];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
@@ -224,7 +231,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
   if (threadIdx.x == 0) {
-    for (int i = 0; i < NBAR; ++i) mbar_init(bar(i), i >= AFREE ? UP_DRAIN_WARPS : 1);
+    for (int i = 0; i < NBAR; ++i) mbar_init(bar(i), i >= YFREE ? Y_READERS : i >= AFREE ? UP_DRAIN_WARPS : 1);
     abort_flag = 0;
     mbar_init_fence();
   }
@@ -236,75 +243,87 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
   grid_launch_dependents();
   grid_dependency_wait();
 
-  const long long total = (long long)*p.ntiles * p.chunks;
+  const int ntiles = *p.ntiles;
+  const long long total = (long long)ntiles * p.chunks;
   const long long lo = total * blockIdx.x / gridDim.x, hi = total * (blockIdx.x + 1) / gridDim.x;
   const int n = (int)(hi - lo), ti0 = (int)(lo / p.chunks), ch0 = (int)(lo - (long long)ti0 * p.chunks);
-  const auto rank_of = [&](const LqAdTile& t) { return t.adapter >= 0 ? p.meta[t.adapter].rank : 0; };
+  // a tile and the rank of its adapter; every role reads those of the next tile while it is busy with one
+  struct Info {
+    LqAdTile tile;
+    int rank;
+  };
+  const auto info = [&](int ti) {
+    Info f = {{-1, 0, 0, -1}, 0};
+    if (ti < ntiles) {
+      f.tile = p.tiles[ti];
+      if (f.tile.adapter >= 0) f.rank = p.meta[f.tile.adapter].rank;
+    }
+    return f;
+  };
+  bool ok = true;
 
   if (warp == 0) {
-    if (lane == 0) {
-      bool ok = true;
+    if (lane == 0 && n > 0) {
       int t_uses = 0, b_uses = 0;
-      LqAdTile tile = {};
-      int rank = 0;
+      Info f = info(ti0), next = info(ti0 + 1);
+      bool enter = true;
       for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
-        if (i == 0 || ch == 0) {
-          tile = p.tiles[ti];
-          rank = rank_of(tile);
-          if (rank > 0) {
-            const int buf = t_uses & 1, pieces = (rank + 63) / 64;
-            if (t_uses >= 2) ok = mbar_wait(bar(TFREE + buf), ((t_uses >> 1) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER);
-            if (ok) {
-              mbar_expect_tx(bar(TFULL + buf), 2 * pieces * PIECE);
-              for (int a = 0; a < pieces; ++a) {
-                tma_load_2d(base + buf * T_BUF + a * PIECE, &tmT, 128 * a, tile.begin, bar(TFULL + buf));
-                tma_load_2d(base + buf * T_BUF + (NA + a) * PIECE, &tmT, LQ_AD_TROW + 128 * a, tile.begin, bar(TFULL + buf));
-              }
-              ++t_uses;
+        const int pieces = (f.rank + 63) / 64;
+        if (enter && f.rank > 0) {
+          const int buf = t_uses % NT;
+          if (t_uses >= NT) ok = mbar_wait(bar(TFREE + buf), ((t_uses / NT) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER);
+          if (ok) {
+            mbar_expect_tx(bar(TFULL + buf), 2 * pieces * PIECE);
+            for (int a = 0; a < pieces; ++a) {
+              tma_load_2d(base + buf * T_BUF + a * PIECE, &tmT, 128 * a, f.tile.begin, bar(TFULL + buf));
+              tma_load_2d(base + buf * T_BUF + (NA + a) * PIECE, &tmT, LQ_AD_TROW + 128 * a, f.tile.begin, bar(TFULL + buf));
             }
+            ++t_uses;
           }
         }
-        if (rank > 0 && ok) {
-          const int s = b_uses % NB, pieces = (rank + 63) / 64;
+        if (f.rank > 0 && ok) {
+          const int s = b_uses % NB;
           if (b_uses >= NB) ok = mbar_wait(bar(BFREE + s), ((b_uses / NB) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER);
           if (ok) {
             mbar_expect_tx(bar(BFULL + s), pieces * PIECE);
-            for (int a = 0; a < pieces; ++a)
-              tma_load_2d(base + 2 * T_BUF + s * B_STAGE + a * PIECE, &tmUp, 128 * a, tile.adapter * p.Npad + UP_COLS * ch, bar(BFULL + s));
+            for (int a = 0; a < pieces; ++a) tma_load_2d(base + B_AT + s * B_STAGE + a * PIECE, &tmUp, 128 * a, f.tile.adapter * p.Npad + UP_COLS * ch, bar(BFULL + s));
             ++b_uses;
           }
         }
-        if (++ch == p.chunks) { ch = 0; ++ti; }
+        enter = ++ch == p.chunks;
+        if (enter) {
+          ch = 0;
+          f = next;
+          next = info(++ti + 1);
+        }
       }
       if (!ok) {                                          // copies in flight land before the CTA goes
-        for (int u = max(0, t_uses - 2); u < t_uses; ++u) mbar_settle(bar(TFULL + (u & 1)), (u >> 1) & 1);
+        for (int u = max(0, t_uses - NT); u < t_uses; ++u) mbar_settle(bar(TFULL + u % NT), (u / NT) & 1);
         for (int u = max(0, b_uses - NB); u < b_uses; ++u) mbar_settle(bar(BFULL + u % NB), (u / NB) & 1);
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      bool ok = true;
-      int t_uses = 0, b_uses = 0, rank = 0;
+    if (lane == 0 && n > 0) {
+      int t_uses = 0, b_uses = 0;
+      Info f = info(ti0), next = info(ti0 + 1);
+      bool enter = true;
       constexpr uint32_t idesc = IDESC_F16 | idesc_shape(UP_COLS);
       for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
-        if (i == 0 || ch == 0) {
-          rank = rank_of(p.tiles[ti]);
-          if (rank > 0) {
-            ok = mbar_wait(bar(TFULL + (t_uses & 1)), (t_uses >> 1) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
-            ++t_uses;
-          }
+        if (enter && f.rank > 0) {
+          ok = mbar_wait(bar(TFULL + t_uses % NT), (t_uses / NT) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
+          ++t_uses;
         }
-        if (rank > 0 && ok) {
-          const int s = b_uses % NB, acc = b_uses & 1, buf = (t_uses - 1) & 1;
+        if (f.rank > 0 && ok) {
+          const int s = b_uses % NB, acc = b_uses & 1, buf = (t_uses - 1) % NT;
           if (b_uses >= 2) ok = mbar_wait(bar(AFREE + acc), ((b_uses >> 1) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_MMA);
           ok = ok && mbar_wait(bar(BFULL + s), (b_uses / NB) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
           if (ok) {
             tc_fence_after();
-            const int steps = (rank + 15) / 16;
+            const int steps = (f.rank + 15) / 16;
             for (int part = 0; part < 2; ++part)
               for (int k = 0; k < steps; ++k) {
                 const uint64_t a = make_smem_desc(base + buf * T_BUF + (part * NA + (k >> 2)) * PIECE) + 2 * (k & 3);
-                const uint64_t b = make_smem_desc(base + 2 * T_BUF + s * B_STAGE + (k >> 2) * PIECE) + 2 * (k & 3);
+                const uint64_t b = make_smem_desc(base + B_AT + s * B_STAGE + (k >> 2) * PIECE) + 2 * (k & 3);
                 tc_mma<TC_F16>(tmem + acc * UP_COLS, a, b, idesc, (part | k) != 0);
               }
             tc_commit(bar(BFREE + s));
@@ -313,113 +332,126 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
             ++b_uses;
           }
         }
-        if (++ch == p.chunks) { ch = 0; ++ti; }
+        enter = ++ch == p.chunks;
+        if (enter) {
+          ch = 0;
+          f = next;
+          next = info(++ti + 1);
+        }
       }
     }
-  } else {
+  } else if (warp == 2) {
+    if (n > 0) {
+      int uses = 0;
+      Info f = info(ti0), next = info(ti0 + 1);
+      int4 rows = make_int4(0, 0, 0, 0);
+      bool enter = true;
+      for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
+        if (f.rank > 0 || !p.in_place) {                  // (rows without an adapter are copied, or left alone)
+          const bool whole = f.tile.first >= 0 && f.tile.rows == BM;
+          if (enter && !whole) rows = tile_rows4(p.perm + f.tile.begin, f.tile.rows, lane);
+          for (int u = 0; u < YP && ok; ++u, ++uses) {
+            const int s = uses % Y_SLOTS, x = (ch * YP + u) * 128;
+            if (uses >= Y_SLOTS && !(ok = mbar_wait_warp(bar(YFREE + s), ((uses / Y_SLOTS) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
+            if (lane == 0) mbar_expect_tx(bar(YFULL + s), whole ? PIECE : (f.tile.rows + 3) / 4 * 512);
+            __syncwarp();
+            const uint32_t to = base + Y_AT + s * PIECE;
+            if (!whole && 4 * lane < f.tile.rows) tma_gather4(to + 512 * lane, &tmYrow, x, rows, bar(YFULL + s));
+            if (whole && lane == 0) tma_load_2d(to, &tmY, x, f.tile.first, bar(YFULL + s));
+          }
+        }
+        enter = ++ch == p.chunks;
+        if (enter) {
+          ch = 0;
+          f = next;
+          next = info(++ti + 1);
+        }
+      }
+      if (!ok && lane == 0)
+        for (int u = max(0, uses - Y_SLOTS); u < uses; ++u) mbar_settle(bar(YFULL + u % Y_SLOTS), (u / Y_SLOTS) & 1);
+    }
+  } else if (warp >= UP_FIRST_DRAIN && n > 0) {
     // ---------------------------------------------------------------------- drain
-    const int quad = warp & 3, cq = (warp - 2) >> 2, g = lane >> 2, t = lane & 3;
+    const int quad = warp & 3, cq = (warp - UP_FIRST_DRAIN) >> 2, g = lane >> 2, t = lane & 3;
     const uint32_t tlane = tmem + ((uint32_t)(quad * 32) << 16) + 32 * cq;
     constexpr int YW = F32 ? 2 : 1;                       // 16-byte words of a lane's eight columns
-    constexpr bool AHEAD = !F32;                          // (two steps of fp32 values do not fit the registers)
-    const bool in_place = p.Y0 == p.Y;
+    // place of the lane's word w of row g + 8 q in a piece: its 128-byte rows are swizzled by 16 bytes
+    const int unit = F32 ? cq : cq >> 1, word = F32 ? 2 * t : 4 * (cq & 1) + t;
+    const uint32_t y_row = base + Y_AT + (uint32_t)(quad * 32 + g) * 128;
     struct Rows {
       int row[4];                                         // -1: none
       float scale[4];
       int rank;
     };
     const auto rows_of = [&](int ti) {
-      const LqAdTile tile = p.tiles[ti];
+      const Info f = info(ti);
       Rows r;
-      r.rank = rank_of(tile);
+      r.rank = f.rank;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int at = quad * 32 + g + 8 * i;
-        const bool in = at < tile.rows && (r.rank > 0 || !in_place);       // a row without an adapter is left alone, or copied
-        r.row[i] = in ? p.perm[tile.begin + at] : -1;
-        r.scale[i] = in && r.rank > 0 ? p.rscale[tile.begin + at] : 0.f;
+        const bool in = at < f.tile.rows;
+        r.row[i] = in ? p.perm[f.tile.begin + at] : -1;
+        r.scale[i] = in && f.tile.adapter >= 0 ? p.rscale[f.tile.begin + at] : 0.f;
       }
       return r;
     };
-    const auto ask = [&](const Rows& r, int ch, uint4 (&y)[4][YW]) {
-      const int c = ch * UP_COLS + 32 * cq + 8 * t;
+    int uses = 0, y_uses = unit;
+    Rows r = rows_of(ti0), r_next = {};
+    for (int i = 0, ti = ti0, ch = ch0; i < n; ++i) {
+      const bool last = ch + 1 == p.chunks;
+      if (last && i + 1 < n) r_next = rows_of(ti + 1);
+      if (r.rank > 0 || !p.in_place) {
+        const int s = y_uses % Y_SLOTS;
+        if (!mbar_wait_warp(bar(YFULL + s), (y_uses / Y_SLOTS) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN)) break;
+        uint4 y[4][YW];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (r.row[i] >= 0 && c < p.N) {
-          const uint4* from = F32 ? reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(p.Y0) + (size_t)r.row[i] * p.N + c)
-                                  : reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(p.Y0) + (size_t)r.row[i] * p.N + c);
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int w = 0; w < YW; ++w) y[i][w] = from[w];
-        }
-    };
-    int uses = 0;
-    Rows r = {}, r_next = {};
-    uint4 y[4][YW], y_next[AHEAD ? 4 : 1][YW];
-    if (n > 0) {
-      r = rows_of(ti0);
-      if constexpr (AHEAD) ask(r, ch0, y);
-    }
-    bool ok = true;
-    for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
-      const int ch_next = ch + 1 == p.chunks ? 0 : ch + 1, ti_next = ti + (ch_next == 0);
-      if constexpr (AHEAD) {
-        if (i + 1 < n) {
-          if (ch_next == 0) {
-            r_next = rows_of(ti_next);
-            ask(r_next, 0, y_next);
-          } else {
-            ask(r, ch_next, y_next);
-          }
-        }
-      } else {
-        ask(r, ch, y);
-      }
-      uint32_t v[2][16];
-      if (r.rank > 0) {
-        const int acc = uses & 1;
-        ok = mbar_wait_warp(bar(AFULL + acc), (uses >> 1) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN);
-        if (!ok) break;
-        ++uses;
-        tc_fence_after();
-        tmem_ld_16x256b_x4(tlane + acc * UP_COLS, v[0]);
-        tmem_ld_16x256b_x4(tlane + (16u << 16) + acc * UP_COLS, v[1]);
-        tmem_ld_wait();
-        tc_fence_before();
+          for (int w = 0; w < YW; ++w) y[q][w] = lds_v4(y_row + s * PIECE + q * 1024 + (((word + w) ^ g) << 4));
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(AFREE + acc));
-      }
-      const int c = ch * UP_COLS + 32 * cq + 8 * t;
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (r.row[q] >= 0 && c < p.N) {
-          // fragment registers 4 j .. 4 j + 3: row g, columns 2 j, 2 j + 1 of this lane's eight, then row g + 8 the same columns
-          const int h = q >> 1, at = 2 * (q & 1);
-          if constexpr (F32) {
-            float* f = reinterpret_cast<float*>(&y[q][0]);
-            if (r.rank > 0)                               // (a row without an adapter keeps its bits)
-#pragma unroll
-              for (int j = 0; j < 8; ++j) f[j] = fmaf(r.scale[q], __uint_as_float(v[h][4 * (j >> 1) + at + (j & 1)]), f[j]);
-            uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.Y) + (size_t)r.row[q] * p.N + c);
-            to[0] = y[q][0]; to[YW - 1] = y[q][YW - 1];
-          } else {
-            __half2* f = reinterpret_cast<__half2*>(&y[q][0]);
-            if (r.rank > 0)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float2 a = __half22float2(f[j]);
-                f[j] = __floats2half2_rn(fmaf(r.scale[q], __uint_as_float(v[h][4 * j + at]), a.x), fmaf(r.scale[q], __uint_as_float(v[h][4 * j + at + 1]), a.y));
-              }
-            *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(p.Y) + (size_t)r.row[q] * p.N + c) = y[q][0];
-          }
+        if (lane == 0) mbar_arrive(bar(YFREE + s));
+        y_uses += YP;
+        uint32_t v[2][16];
+        if (r.rank > 0) {
+          const int acc = uses & 1;
+          if (!mbar_wait_warp(bar(AFULL + acc), (uses >> 1) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN)) break;
+          ++uses;
+          tc_fence_after();
+          tmem_ld_16x256b_x4(tlane + acc * UP_COLS, v[0]);
+          tmem_ld_16x256b_x4(tlane + (16u << 16) + acc * UP_COLS, v[1]);
+          tmem_ld_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(AFREE + acc));
         }
-      if constexpr (AHEAD) {
-        if (ch_next == 0) r = r_next;
+        const int c = ch * UP_COLS + 32 * cq + 8 * t;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) y[q][0] = y_next[q][0];
-      } else if (ch_next == 0 && i + 1 < n) {
-        r = rows_of(ti_next);
+        for (int q = 0; q < 4; ++q)
+          if (r.row[q] >= 0 && c < p.N) {
+            // fragment registers 4 j .. 4 j + 3: row g, columns 2 j, 2 j + 1 of this lane's eight, then row g + 8 the same columns
+            const int h = q >> 1, at = 2 * (q & 1);
+            if constexpr (F32) {
+              float* f = reinterpret_cast<float*>(&y[q][0]);
+              if (r.rank > 0)                             // (a row without an adapter keeps its bits)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = fmaf(r.scale[q], __uint_as_float(v[h][4 * (j >> 1) + at + (j & 1)]), f[j]);
+              uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.Y) + (size_t)r.row[q] * p.N + c);
+              to[0] = y[q][0]; to[YW - 1] = y[q][YW - 1];
+            } else {
+              __half2* f = reinterpret_cast<__half2*>(&y[q][0]);
+              if (r.rank > 0)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const float2 a = __half22float2(f[j]);
+                  f[j] = __floats2half2_rn(fmaf(r.scale[q], __uint_as_float(v[h][4 * j + at]), a.x), fmaf(r.scale[q], __uint_as_float(v[h][4 * j + at + 1]), a.y));
+                }
+              *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(p.Y) + (size_t)r.row[q] * p.N + c) = y[q][0];
+            }
+          }
       }
-      ch = ch_next; ti = ti_next;
+      if (last) { r = r_next; ch = 0; ++ti; }
+      else ++ch;
     }
   }
   tc_fence_before();
@@ -430,13 +462,12 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
   }
 }
 
-constexpr int up_smem(int na) { return 1024 + 2 * (2 * na * BM * 128) + (na == 1 ? 3 : 2) * na * BM * 128; }
 constexpr int DOWN_SMEM = 110 * 1024;                     // two CTAs an SM
 
 template <bool F32, int NA>
-cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const UpParams& p, cudaStream_t st) {
+cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const CUtensorMap& tmY, const CUtensorMap& tmYrow, const UpParams& p, cudaStream_t st) {
   const long long steps = (long long)lq_ad_tiles(R) * p.chunks;
-  return lq_launch(lq_adapters_up_kernel<F32, NA>, (int)std::min<long long>(steps, R->sms), UP_THREADS, up_smem(NA), st, R->tmT, S->tmUp, p);
+  return lq_launch(lq_adapters_up_kernel<F32, NA>, (int)std::min<long long>(steps, R->sms), UP_THREADS, up_smem(NA), st, R->tmT, S->tmUp, tmY, tmYrow, p);
 }
 
 }  // namespace
@@ -450,10 +481,12 @@ lq_status lq_adapters_tiles_prepare() {
 }
 
 lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
-  CUtensorMap tmX, tmXrow;
+  CUtensorMap tmX, tmXrow, tmY, tmYrow;
+  const uint64_t M = (uint64_t)R->M, x_row = (uint64_t)S->K * 2, y_row = (uint64_t)S->N * (dt == LQ_OUT_F32 ? 4 : 2);
   lq_status s;
-  if ((s = lq_make_tmap_bytes(&tmX, const_cast<void*>(X), (uint64_t)R->M, (uint64_t)S->K * 2, BM)) != LQ_OK) return s;
-  if ((s = lq_make_tmap_bytes(&tmXrow, const_cast<void*>(X), (uint64_t)R->M, (uint64_t)S->K * 2, 1)) != LQ_OK) return s;
+  if ((s = lq_make_tmap_bytes(&tmX, const_cast<void*>(X), M, x_row, BM)) != LQ_OK || (s = lq_make_tmap_bytes(&tmXrow, const_cast<void*>(X), M, x_row, 1)) != LQ_OK ||
+      (s = lq_make_tmap_bytes(&tmY, const_cast<void*>(Y0), M, y_row, BM)) != LQ_OK || (s = lq_make_tmap_bytes(&tmYrow, const_cast<void*>(Y0), M, y_row, 1)) != LQ_OK)
+    return s;
   int32_t* status = lq_device_status_ptr(S->device);
   if (!status) return LQ_ERR_CUDA;
   DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, S->rp, 1, lq_ceil_div(S->K, 64), 1, 32};
@@ -466,8 +499,8 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
   const int smem = 1024 + std::max(d.ring * stage, BM * (S->rp + 4) * 4);
   cudaError_t e = lq_launch_cluster(lq_adapters_down_kernel, lq_ad_tiles(R) * d.split, 128, d.split, smem, st, tmX, tmXrow, S->tmDown, d);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
-  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y0, Y, status, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS)};
-  if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, u, st) : launch_up<true, 2>(S, R, u, st);
-  else e = S->rp <= 64 ? launch_up<false, 1>(S, R, u, st) : launch_up<false, 2>(S, R, u, st);
+  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y};
+  if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, tmY, tmYrow, u, st) : launch_up<true, 2>(S, R, tmY, tmYrow, u, st);
+  else e = S->rp <= 64 ? launch_up<false, 1>(S, R, tmY, tmYrow, u, st) : launch_up<false, 2>(S, R, tmY, tmYrow, u, st);
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
