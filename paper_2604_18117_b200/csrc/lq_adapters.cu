@@ -48,6 +48,7 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     if (r0 > 0) read(r0);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
+      if (r0 + 32 * u >= n) break;
       const unsigned same = __match_any_sync(0xffffffffu, bin[u]);
       if (bin[u] >= 0 && lane == __ffs(same) - 1) mine[bin[u]] += __popc(same);
       __syncwarp();
@@ -95,6 +96,7 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     if (run > 32 * AHEAD) read(r0);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
+      if (r0 + 32 * u >= n) break;
       const unsigned same = __match_any_sync(0xffffffffu, bin[u]);
       const int at = bin[u] >= 0 ? mine[bin[u]] + __popc(same & ((1u << lane) - 1)) : 0;
       __syncwarp();

@@ -39,7 +39,23 @@ __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory"); }
+// Copies 128 bytes at x of each of a tile's rows: a whole tile of neighbours in one copy, else four rows a copy (rows: a lane's).  The whole warp calls, one
+// lane issues: a copy's operands have to be uniform, and where the compiler cannot see that they are it takes the lanes one by one (455 clocks a stage of two copies for 345).
+__device__ __forceinline__ void fetch_rows(uint32_t dst, const CUtensorMap* tm, const CUtensorMap* tm_row, int x, const LqAdTile& t, bool whole, const int4& rows, uint32_t bar) {
+  if (whole) {
+    if (elect_one()) tma_load_2d(dst, tm, x, t.first, bar);
+  } else {
+    for (int i = 0; 4 * i < t.rows; ++i) {
+      const int4 r = make_int4(__shfl_sync(0xffffffffu, rows.x, i), __shfl_sync(0xffffffffu, rows.y, i), __shfl_sync(0xffffffffu, rows.z, i), __shfl_sync(0xffffffffu, rows.w, i));
+      if (elect_one()) tma_gather4(dst + i * 512, tm_row, x, r, bar);
+    }
+  }
+}
+
 // ---- down ----------------------------------------------------------------------------------------------------------
+constexpr int DOWN_WARPS = 8;
+
 struct DownParams {
   const LqAdTile* tiles;
   const int *ntiles, *perm;
@@ -47,14 +63,16 @@ struct DownParams {
   __half* T;
   float* rscale;
   int32_t* status;
-  int rp, split, k_stages, ring, tmem_cols;
+  int rp, k_stages, ring, tmem_cols;
 };
 
-// One tile a cluster, K / (64 split) stages a CTA.  Warp 0 fetches (a whole tile of neighbouring rows in one copy, else four rows a copy, one copy a
-// lane), warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial sums to shared memory and each CTA
-// adds up 128 / split rows from all of the cluster, always in the same order.
-__global__ void __launch_bounds__(128) lq_adapters_down_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmXrow,
-                                                               const __grid_constant__ CUtensorMap tmDown, const __grid_constant__ DownParams p) {
+// One tile a cluster, K / (64 SPLIT) stages a CTA.  Warp 0 fetches, warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial
+// sums to shared memory and each CTA adds up 128 / SPLIT rows from all of the cluster, always in the same order.  A short kernel is a chain of latencies:
+// nothing waits for what it does not need (an empty slot's tile is formed like another and left unread), the loads of a row's sums are all in flight
+// together.  (8192 x 1152, rank 32, us from the dependency's end: tile known 0.6, copies asked for 1.5, sums complete 6.4, in shared memory of all 7.5, T written 8.8.)
+template <int SPLIT>
+__global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmXrow,
+                                                                           const __grid_constant__ CUtensorMap tmDown, const __grid_constant__ DownParams p) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * MAX_STAGES + 1];
   __shared__ uint32_t tmem_slot;
@@ -62,7 +80,7 @@ __global__ void __launch_bounds__(128) lq_adapters_down_kernel(const __grid_cons
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int stage_bytes = A_STAGE + p.rp * 128;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int ti = blockIdx.x / p.split, part = blockIdx.x - ti * p.split;
+  const int ti = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
   auto full = [&](int s) { return smem_u32(&bars[s]); };
   auto empty = [&](int s) { return smem_u32(&bars[MAX_STAGES + s]); };
   const uint32_t done = smem_u32(&bars[2 * MAX_STAGES]);
@@ -71,121 +89,123 @@ __global__ void __launch_bounds__(128) lq_adapters_down_kernel(const __grid_cons
     mbar_init(done, 1);
     abort_flag = 0;
     mbar_init_fence();
+    prefetch_map(&tmX); prefetch_map(&tmXrow); prefetch_map(&tmDown);
   }
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), p.tmem_cols);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  grid_launch_dependents();
   grid_dependency_wait();
+  grid_launch_dependents();          // (behind the wait: the up kernel counts on what came before this one to be complete when it starts)
 
   // (a tile behind the last one holds anything: it is asked for together with their number, which saves a trip)
   LqAdTile tile = p.tiles[ti];
   if (ti >= *p.ntiles) tile.adapter = -1;
-  LqAdMeta m = {0, 0.f};
-  int4 rows = make_int4(0, 0, 0, 0);
-  if (tile.adapter >= 0) {
-    m = p.meta[tile.adapter];
-    if (warp == 0) rows = tile_rows4(p.perm + tile.begin, tile.rows, lane);
-  }
-  if (m.rank > 0) {                                       // (the same for the whole cluster)
-    const int k0 = part * p.k_stages / p.split, n = (part + 1) * p.k_stages / p.split - k0;
+  if (tile.adapter >= 0) {                                // (the same for the whole cluster)
+    const int k0 = part * p.k_stages / SPLIT, n = (part + 1) * p.k_stages / SPLIT - k0;
+    const float scale = p.meta[tile.adapter].scale;
     bool ok = true;
     if (warp == 0) {
       const bool whole = tile.first >= 0 && tile.rows == BM;
-      const uint32_t a_bytes = whole ? A_STAGE : (tile.rows + 3) / 4 * 512;
+      const uint32_t bytes = (whole ? A_STAGE : (tile.rows + 3) / 4 * 512) + p.rp * 128;
+      int4 rows = make_int4(0, 0, 0, 0);
+      if (!whole) rows = tile_rows4(p.perm + tile.begin, tile.rows, lane);
       for (int it = 0; it < n; ++it) {
         const int s = it % p.ring;
         if (it >= p.ring && !(ok = mbar_wait_warp(empty(s), ((it / p.ring) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
         const uint32_t a = base + s * stage_bytes;
-        if (lane == 0) mbar_expect_tx(full(s), a_bytes + p.rp * 128);
-        __syncwarp();
         const int x = (k0 + it) * 128;                    // bytes along K
-        if (!whole && 4 * lane < tile.rows) tma_gather4(a + lane * 512, &tmXrow, x, rows, full(s));
-        if (lane == 0) {
-          if (whole) tma_load_2d(a, &tmX, x, tile.first, full(s));
+        if (elect_one()) {
+          mbar_expect_tx(full(s), bytes);
           tma_load_2d(a + A_STAGE, &tmDown, x, tile.adapter * p.rp, full(s));
         }
+        __syncwarp();
+        fetch_rows(a, &tmX, &tmXrow, x, tile, whole, rows, full(s));
       }
       if (!ok)                                            // copies in flight land before the CTA goes
         for (int it = max(0, n - p.ring); it < n; ++it) mbar_settle(full(it % p.ring), (it / p.ring) & 1);
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
       const uint32_t idesc = IDESC_F16 | idesc_shape(p.rp);
       for (int it = 0; it < n; ++it) {
         const int s = it % p.ring;
-        if (!mbar_wait(full(s), (it / p.ring) & 1, &abort_flag, p.status, LQ_STAGE_MMA)) break;
+        if (!(ok = mbar_wait_warp(full(s), (it / p.ring) & 1, &abort_flag, p.status, LQ_STAGE_MMA))) break;
         tc_fence_after();
         const uint64_t a = make_smem_desc(base + s * stage_bytes), b = make_smem_desc(base + s * stage_bytes + A_STAGE);
+        if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tc_mma<TC_F16>(tmem, a + 2 * k, b + 2 * k, idesc, (it | k) != 0);
-        tc_commit(empty(s));
+          for (int k = 0; k < 4; ++k) tc_mma<TC_F16>(tmem, a + 2 * k, b + 2 * k, idesc, (it | k) != 0);
+          tc_commit(empty(s));
+          if (it + 1 == n) tc_commit(done);
+        }
+        __syncwarp();
       }
-      tc_commit(done);
     }
     __syncwarp();
     ok = mbar_wait(done, 0, &abort_flag, p.status, LQ_STAGE_DRAIN);
     ok = __syncthreads_and(ok && !abort_flag) != 0;
-    // partial sums -> shared memory, rows 16 bytes longer than they are so that neighbouring rows lie in different banks; the ring is free: the MMAs have read it
+    // partial sums -> shared memory, rows 16 bytes longer than they are so that neighbouring rows lie in different banks; the ring is free: the MMAs
+    // have read it
     const int pitch = p.rp + 4;
-    float* sums = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)));
     if (ok) {
       tc_fence_after();
-      const int row = warp * 32 + lane;
-      for (int c = 0; c < p.rp; c += 16) {
+      const uint32_t row = base + (uint32_t)((warp & 3) * 32 + lane) * pitch * 4;
+      for (int c = 16 * (warp >> 2); c < p.rp; c += 32) {
         uint32_t v[16];
-        tmem_ld_32x16(tmem + ((uint32_t)(warp * 32) << 16) + c, v);
+        tmem_ld_32x16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + c, v);
         tmem_ld_wait();
-        float4* to = reinterpret_cast<float4*>(sums + row * pitch + c);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) to[j] = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3]));
+        for (int j = 0; j < 4; ++j) sts_v4(row + (c + 4 * j) * 4, make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
       }
     }
-    if (p.split > 1) cluster_sync();
+    if constexpr (SPLIT > 1) cluster_sync();
     else __syncthreads();
-    if (ok) {
-      // eight threads to a row
-      const int rows_here = BM / p.split, j0 = threadIdx.x & 7;
-      for (int r = threadIdx.x >> 3; r < rows_here; r += 16) {
-        const int row = part * rows_here + r;
-        float4 v[4];
-        float top = 0.f;
+    // eight threads to a row, a float4 in 32 columns each
+    constexpr int ROWS = BM / SPLIT, AT_ONCE = 4 * DOWN_WARPS;
+    const int j0 = threadIdx.x & 7;
+#pragma unroll 1
+    for (int r = threadIdx.x >> 3; ok && r < ROWS; r += AT_ONCE) {
+      const int row = part * ROWS + r;
+      float4 v[4];
+      float top = 0.f;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int j = j0 + 8 * q;
-          v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (4 * j < p.rp) {
-            const uint32_t at = base + (uint32_t)(row * pitch + 4 * j) * 4;
-            for (int w = 0; w < p.split; ++w) {
-              const float4 u = ld_peer_v4(p.split > 1 ? peer_smem(at, w) : at);
-              v[q].x += u.x; v[q].y += u.y; v[q].z += u.z; v[q].w += u.w;
-            }
-          }
-          top = fmaxf(fmaxf(top, fmaxf(fabsf(v[q].x), fabsf(v[q].y))), fmaxf(fabsf(v[q].z), fabsf(v[q].w)));
-        }
+      for (int q = 0; q < 4; ++q) {
+        v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (4 * j0 + 32 * q < p.rp) {
+          const uint32_t at = base + (uint32_t)(row * pitch + 4 * j0 + 32 * q) * 4;
+          if constexpr (SPLIT == 1) {
+            const uint4 u = lds_v4(at);
+            v[q] = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+          } else {
+            float4 u[SPLIT];
 #pragma unroll
-        for (int d = 1; d < 8; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        if (row < tile.rows) {
-          const int e = lq_ad_exponent(top);
-          const float f = ldexpf(1.f, e);                 // (|e| <= 100: exact)
-          __half* to = p.T + (size_t)(tile.begin + row) * LQ_AD_TROW;
-          if (j0 == 0) p.rscale[tile.begin + row] = ldexpf(m.scale, -e);
+            for (int w = 0; w < SPLIT; ++w) u[w] = ld_peer_v4(peer_smem(at, w));
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int j = j0 + 8 * q;
-            if (4 * j < p.rp) {
-              const float u[4] = {v[q].x * f, v[q].y * f, v[q].z * f, v[q].w * f};
-              float lo[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) lo[i] = u[i] - __half2float(__float2half_rn(u[i]));
-              *reinterpret_cast<uint2*>(to + 4 * j) = make_uint2(pack_halves(u[0], u[1]), pack_halves(u[2], u[3]));
-              *reinterpret_cast<uint2*>(to + LQ_AD_TROW / 2 + 4 * j) = make_uint2(pack_halves(lo[0], lo[1]), pack_halves(lo[2], lo[3]));
-            }
+            for (int w = 0; w < SPLIT; ++w) { v[q].x += u[w].x; v[q].y += u[w].y; v[q].z += u[w].z; v[q].w += u[w].w; }
           }
         }
+        top = fmaxf(fmaxf(top, fmaxf(fabsf(v[q].x), fabsf(v[q].y))), fmaxf(fabsf(v[q].z), fabsf(v[q].w)));
+      }
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      if (row < tile.rows) {
+        const int e = lq_ad_exponent(top);
+        const float f = __int_as_float((127 + e) << 23);  // 2^e, |e| <= 100
+        __half* to = p.T + (size_t)(tile.begin + row) * LQ_AD_TROW + 4 * j0;
+        if (j0 == 0) p.rscale[tile.begin + row] = ldexpf(scale, -e);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (4 * j0 + 32 * q < p.rp) {
+            const float u[4] = {v[q].x * f, v[q].y * f, v[q].z * f, v[q].w * f};
+            float lo[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lo[i] = u[i] - __half2float(__float2half_rn(u[i]));
+            *reinterpret_cast<uint2*>(to + 32 * q) = make_uint2(pack_halves(u[0], u[1]), pack_halves(u[2], u[3]));
+            *reinterpret_cast<uint2*>(to + LQ_AD_TROW / 2 + 32 * q) = make_uint2(pack_halves(lo[0], lo[1]), pack_halves(lo[2], lo[3]));
+          }
       }
     }
-    if (p.split > 1) cluster_sync();                      // the others have read this CTA's sums
+    if constexpr (SPLIT > 1) cluster_sync();              // the others have read this CTA's sums
   }
   tc_fence_before();
   __syncthreads();
@@ -234,6 +254,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
     for (int i = 0; i < NBAR; ++i) mbar_init(bar(i), i >= YFREE ? Y_READERS : i >= AFREE ? UP_DRAIN_WARPS : 1);
     abort_flag = 0;
     mbar_init_fence();
+    prefetch_map(&tmT); prefetch_map(&tmUp); prefetch_map(&tmY); prefetch_map(&tmYrow);
   }
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), 2 * UP_COLS);
   tc_fence_before();
@@ -241,7 +262,9 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   grid_launch_dependents();
-  grid_dependency_wait();
+  // The down kernel lets this one start when all that came before has completed: the map, the factors and Y0 are there.  Only T and its rows' scales
+  // are waited for (and every CTA waits, so that who waits for this kernel has waited for that one).
+  if (warp == 3) grid_dependency_wait();
 
   const int ntiles = *p.ntiles;
   const long long total = (long long)ntiles * p.chunks;
@@ -263,32 +286,35 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
   bool ok = true;
 
   if (warp == 0) {
-    if (lane == 0 && n > 0) {
+    if (n > 0) {
       int t_uses = 0, b_uses = 0;
       Info f = info(ti0), next = info(ti0 + 1);
       bool enter = true;
       for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
         const int pieces = (f.rank + 63) / 64;
+        if (f.rank > 0) {
+          const int s = b_uses % NB;
+          if (b_uses >= NB && !(ok = mbar_wait_warp(bar(BFREE + s), ((b_uses / NB) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
+          if (elect_one()) {
+            mbar_expect_tx(bar(BFULL + s), pieces * PIECE);
+            for (int a = 0; a < pieces; ++a) tma_load_2d(base + B_AT + s * B_STAGE + a * PIECE, &tmUp, 128 * a, f.tile.adapter * p.Npad + UP_COLS * ch, bar(BFULL + s));
+          }
+          __syncwarp();
+          ++b_uses;
+        }
         if (enter && f.rank > 0) {
           const int buf = t_uses % NT;
-          if (t_uses >= NT) ok = mbar_wait(bar(TFREE + buf), ((t_uses / NT) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER);
-          if (ok) {
+          if (t_uses == 0) grid_dependency_wait();
+          if (t_uses >= NT && !(ok = mbar_wait_warp(bar(TFREE + buf), ((t_uses / NT) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
+          if (elect_one()) {
             mbar_expect_tx(bar(TFULL + buf), 2 * pieces * PIECE);
             for (int a = 0; a < pieces; ++a) {
               tma_load_2d(base + buf * T_BUF + a * PIECE, &tmT, 128 * a, f.tile.begin, bar(TFULL + buf));
               tma_load_2d(base + buf * T_BUF + (NA + a) * PIECE, &tmT, LQ_AD_TROW + 128 * a, f.tile.begin, bar(TFULL + buf));
             }
-            ++t_uses;
           }
-        }
-        if (f.rank > 0 && ok) {
-          const int s = b_uses % NB;
-          if (b_uses >= NB) ok = mbar_wait(bar(BFREE + s), ((b_uses / NB) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER);
-          if (ok) {
-            mbar_expect_tx(bar(BFULL + s), pieces * PIECE);
-            for (int a = 0; a < pieces; ++a) tma_load_2d(base + B_AT + s * B_STAGE + a * PIECE, &tmUp, 128 * a, f.tile.adapter * p.Npad + UP_COLS * ch, bar(BFULL + s));
-            ++b_uses;
-          }
+          __syncwarp();
+          ++t_uses;
         }
         enter = ++ch == p.chunks;
         if (enter) {
@@ -297,40 +323,42 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
           next = info(++ti + 1);
         }
       }
-      if (!ok) {                                          // copies in flight land before the CTA goes
+      if (!ok && lane == 0) {                             // copies in flight land before the CTA goes
         for (int u = max(0, t_uses - NT); u < t_uses; ++u) mbar_settle(bar(TFULL + u % NT), (u / NT) & 1);
         for (int u = max(0, b_uses - NB); u < b_uses; ++u) mbar_settle(bar(BFULL + u % NB), (u / NB) & 1);
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && n > 0) {
+    if (n > 0) {
       int t_uses = 0, b_uses = 0;
       Info f = info(ti0), next = info(ti0 + 1);
       bool enter = true;
       constexpr uint32_t idesc = IDESC_F16 | idesc_shape(UP_COLS);
       for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
         if (enter && f.rank > 0) {
-          ok = mbar_wait(bar(TFULL + t_uses % NT), (t_uses / NT) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
+          ok = mbar_wait_warp(bar(TFULL + t_uses % NT), (t_uses / NT) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
           ++t_uses;
         }
         if (f.rank > 0 && ok) {
           const int s = b_uses % NB, acc = b_uses & 1, buf = (t_uses - 1) % NT;
-          if (b_uses >= 2) ok = mbar_wait(bar(AFREE + acc), ((b_uses >> 1) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_MMA);
-          ok = ok && mbar_wait(bar(BFULL + s), (b_uses / NB) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
-          if (ok) {
-            tc_fence_after();
-            const int steps = (f.rank + 15) / 16;
-            for (int part = 0; part < 2; ++part)
-              for (int k = 0; k < steps; ++k) {
-                const uint64_t a = make_smem_desc(base + buf * T_BUF + (part * NA + (k >> 2)) * PIECE) + 2 * (k & 3);
-                const uint64_t b = make_smem_desc(base + B_AT + s * B_STAGE + (k >> 2) * PIECE) + 2 * (k & 3);
-                tc_mma<TC_F16>(tmem + acc * UP_COLS, a, b, idesc, (part | k) != 0);
-              }
+          if (b_uses >= 2) ok = mbar_wait_warp(bar(AFREE + acc), ((b_uses >> 1) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_MMA);
+          ok = ok && mbar_wait_warp(bar(BFULL + s), (b_uses / NB) & 1, &abort_flag, p.status, LQ_STAGE_MMA);
+          if (!ok) break;
+          tc_fence_after();
+          const int steps = (f.rank + 15) / 16;
+          const uint64_t hi = make_smem_desc(base + buf * T_BUF), lo = make_smem_desc(base + buf * T_BUF + NA * PIECE), slab = make_smem_desc(base + B_AT + s * B_STAGE);
+          if (elect_one()) {
+            for (int k = 0; k < steps; ++k) {             // (64 of the rank are a piece)
+              const uint32_t at = (uint32_t)((k >> 2) * (PIECE >> 4) + 2 * (k & 3));
+              tc_mma<TC_F16>(tmem + acc * UP_COLS, hi + at, slab + at, idesc, k != 0);
+              tc_mma<TC_F16>(tmem + acc * UP_COLS, lo + at, slab + at, idesc, 1);
+            }
             tc_commit(bar(BFREE + s));
             tc_commit(bar(AFULL + acc));
             if (i + 1 == n || ch + 1 == p.chunks) tc_commit(bar(TFREE + buf));
-            ++b_uses;
           }
+          __syncwarp();
+          ++b_uses;
         }
         enter = ++ch == p.chunks;
         if (enter) {
@@ -353,11 +381,9 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
           for (int u = 0; u < YP && ok; ++u, ++uses) {
             const int s = uses % Y_SLOTS, x = (ch * YP + u) * 128;
             if (uses >= Y_SLOTS && !(ok = mbar_wait_warp(bar(YFREE + s), ((uses / Y_SLOTS) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
-            if (lane == 0) mbar_expect_tx(bar(YFULL + s), whole ? PIECE : (f.tile.rows + 3) / 4 * 512);
+            if (elect_one()) mbar_expect_tx(bar(YFULL + s), whole ? PIECE : (f.tile.rows + 3) / 4 * 512);
             __syncwarp();
-            const uint32_t to = base + Y_AT + s * PIECE;
-            if (!whole && 4 * lane < f.tile.rows) tma_gather4(to + 512 * lane, &tmYrow, x, rows, bar(YFULL + s));
-            if (whole && lane == 0) tma_load_2d(to, &tmY, x, f.tile.first, bar(YFULL + s));
+            fetch_rows(base + Y_AT + s * PIECE, &tmY, &tmYrow, x, f.tile, whole, rows, bar(YFULL + s));
           }
         }
         enter = ++ch == p.chunks;
@@ -381,12 +407,16 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
     struct Rows {
       int row[4];                                         // -1: none
       float scale[4];
-      int rank;
+      int rank, rows;
     };
+    bool waited = false;
     const auto rows_of = [&](int ti) {
       const Info f = info(ti);
+      if (!waited) grid_dependency_wait();
+      waited = true;
       Rows r;
       r.rank = f.rank;
+      r.rows = f.tile.rows;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int at = quad * 32 + g + 8 * i;
@@ -404,51 +434,60 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
       if (r.rank > 0 || !p.in_place) {
         const int s = y_uses % Y_SLOTS;
         if (!mbar_wait_warp(bar(YFULL + s), (y_uses / Y_SLOTS) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN)) break;
-        uint4 y[4][YW];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int w = 0; w < YW; ++w) y[q][w] = lds_v4(y_row + s * PIECE + q * 1024 + (((word + w) ^ g) << 4));
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(YFREE + s));
-        y_uses += YP;
-        uint32_t v[2][16];
+        const int acc = uses & 1;
         if (r.rank > 0) {
-          const int acc = uses & 1;
           if (!mbar_wait_warp(bar(AFULL + acc), (uses >> 1) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN)) break;
           ++uses;
           tc_fence_after();
-          tmem_ld_16x256b_x4(tlane + acc * UP_COLS, v[0]);
-          tmem_ld_16x256b_x4(tlane + (16u << 16) + acc * UP_COLS, v[1]);
-          tmem_ld_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(AFREE + acc));
         }
         const int c = ch * UP_COLS + 32 * cq + 8 * t;
+        // rows g, g + 8, then rows g + 16, g + 24 of the quarter, where the tile has some: fragment registers 4 j .. 4 j + 3 hold row g, columns 2 j, 2 j + 1 of
+        // this lane's eight, then row g + 8 the same columns
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (r.row[q] >= 0 && c < p.N) {
-            // fragment registers 4 j .. 4 j + 3: row g, columns 2 j, 2 j + 1 of this lane's eight, then row g + 8 the same columns
-            const int h = q >> 1, at = 2 * (q & 1);
-            if constexpr (F32) {
-              float* f = reinterpret_cast<float*>(&y[q][0]);
-              if (r.rank > 0)                             // (a row without an adapter keeps its bits)
+        for (int h = 0; h < 2; ++h) {
+          const bool any = 32 * quad + 16 * h < r.rows;
+          uint32_t v[16];
+          uint4 y[2][YW];
+          if (any) {
+            if (r.rank > 0) tmem_ld_16x256b_x4(tlane + ((uint32_t)(16 * h) << 16) + acc * UP_COLS, v);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = fmaf(r.scale[q], __uint_as_float(v[h][4 * (j >> 1) + at + (j & 1)]), f[j]);
-              uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.Y) + (size_t)r.row[q] * p.N + c);
-              to[0] = y[q][0]; to[YW - 1] = y[q][YW - 1];
-            } else {
-              __half2* f = reinterpret_cast<__half2*>(&y[q][0]);
-              if (r.rank > 0)
+            for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  const float2 a = __half22float2(f[j]);
-                  f[j] = __floats2half2_rn(fmaf(r.scale[q], __uint_as_float(v[h][4 * j + at]), a.x), fmaf(r.scale[q], __uint_as_float(v[h][4 * j + at + 1]), a.y));
-                }
-              *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(p.Y) + (size_t)r.row[q] * p.N + c) = y[q][0];
+              for (int w = 0; w < YW; ++w) y[q][w] = lds_v4(y_row + s * PIECE + (2 * h + q) * 1024 + (((word + w) ^ g) << 4));
+            if (r.rank > 0) tmem_ld_wait();
+          }
+          if (h == 1) {                                   // all of this warp's is in registers
+            if (r.rank > 0) tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+              mbar_arrive(bar(YFREE + s));
+              if (r.rank > 0) mbar_arrive(bar(AFREE + acc));
             }
           }
+          if (any)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+              if (r.row[2 * h + q] >= 0 && c < p.N) {
+                const float2 by = make_float2(r.scale[2 * h + q], r.scale[2 * h + q]);
+                const size_t to = (size_t)(unsigned)r.row[2 * h + q] * (unsigned)p.N + c;
+                const auto d = [&](int j) { return make_float2(__uint_as_float(v[4 * j + 2 * q]), __uint_as_float(v[4 * j + 2 * q + 1])); };     // columns 2 j, 2 j + 1
+                if constexpr (F32) {
+                  float2* f = reinterpret_cast<float2*>(&y[q][0]);
+                  if (r.rank > 0)                         // (a row without an adapter keeps its bits)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = __ffma2_rn(by, d(j), f[j]);
+                  uint4* at = reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.Y) + to);
+                  at[0] = y[q][0]; at[YW - 1] = y[q][YW - 1];
+                } else {
+                  __half2* f = reinterpret_cast<__half2*>(&y[q][0]);
+                  if (r.rank > 0)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = __float22half2_rn(__ffma2_rn(by, d(j), __half22float2(f[j])));
+                  *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(p.Y) + to) = y[q][0];
+                }
+              }
+        }
+        y_uses += YP;
       }
       if (last) { r = r_next; ch = 0; ++ti; }
       else ++ch;
@@ -464,6 +503,15 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
 
 constexpr int DOWN_SMEM = 110 * 1024;                     // two CTAs an SM
 
+template <int SPLIT>
+cudaError_t launch_down(const lq_adapters* S, const lq_rowmap* R, const CUtensorMap& tmX, const CUtensorMap& tmXrow, DownParams& d, cudaStream_t st) {
+  const int stage = A_STAGE + S->rp * 128, most = (d.k_stages + SPLIT - 1) / SPLIT;
+  d.ring = std::min(std::min(MAX_STAGES, most), (DOWN_SMEM - 1024) / stage);
+  while (d.tmem_cols < S->rp) d.tmem_cols *= 2;
+  const int smem = 1024 + std::max(d.ring * stage, BM * (S->rp + 4) * 4);
+  return lq_launch_cluster(lq_adapters_down_kernel<SPLIT>, lq_ad_tiles(R) * SPLIT, 32 * DOWN_WARPS, SPLIT, smem, st, tmX, tmXrow, S->tmDown, d);
+}
+
 template <bool F32, int NA>
 cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const CUtensorMap& tmY, const CUtensorMap& tmYrow, const UpParams& p, cudaStream_t st) {
   const long long steps = (long long)lq_ad_tiles(R) * p.chunks;
@@ -474,7 +522,8 @@ cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const CUtensorMa
 
 lq_status lq_adapters_tiles_prepare() {
   const auto room = [](auto* kernel, int bytes) { return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) == cudaSuccess; };
-  return room(lq_adapters_down_kernel, DOWN_SMEM) && room(lq_adapters_up_kernel<false, 1>, up_smem(1)) && room(lq_adapters_up_kernel<true, 1>, up_smem(1)) &&
+  return room(lq_adapters_down_kernel<1>, DOWN_SMEM) && room(lq_adapters_down_kernel<2>, DOWN_SMEM) && room(lq_adapters_down_kernel<4>, DOWN_SMEM) &&
+                 room(lq_adapters_down_kernel<8>, DOWN_SMEM) && room(lq_adapters_up_kernel<false, 1>, up_smem(1)) && room(lq_adapters_up_kernel<true, 1>, up_smem(1)) &&
                  room(lq_adapters_up_kernel<false, 2>, up_smem(2)) && room(lq_adapters_up_kernel<true, 2>, up_smem(2))
              ? LQ_OK
              : LQ_ERR_CUDA;
@@ -489,15 +538,15 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
     return s;
   int32_t* status = lq_device_status_ptr(S->device);
   if (!status) return LQ_ERR_CUDA;
-  DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, S->rp, 1, lq_ceil_div(S->K, 64), 1, 32};
+  DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, S->rp, lq_ceil_div(S->K, 64), 1, 32};
   // K is shared by as many CTAs as fill the SMs twice over, each with at least two stages
   const int tiles = lq_ceil_div(R->M, BM);
-  while (d.split < 8 && tiles * 2 * d.split <= 2 * R->sms && d.k_stages >= 4 * d.split) d.split *= 2;
-  const int stage = A_STAGE + S->rp * 128, most = (d.k_stages + d.split - 1) / d.split;
-  d.ring = std::min(std::min(MAX_STAGES, most), (DOWN_SMEM - 1024) / stage);
-  while (d.tmem_cols < S->rp) d.tmem_cols *= 2;
-  const int smem = 1024 + std::max(d.ring * stage, BM * (S->rp + 4) * 4);
-  cudaError_t e = lq_launch_cluster(lq_adapters_down_kernel, lq_ad_tiles(R) * d.split, 128, d.split, smem, st, tmX, tmXrow, S->tmDown, d);
+  int split = 1;
+  while (split < 8 && tiles * 2 * split <= 2 * R->sms && d.k_stages >= 4 * split) split *= 2;
+  cudaError_t e = split == 1   ? launch_down<1>(S, R, tmX, tmXrow, d, st)
+                  : split == 2 ? launch_down<2>(S, R, tmX, tmXrow, d, st)
+                  : split == 4 ? launch_down<4>(S, R, tmX, tmXrow, d, st)
+                               : launch_down<8>(S, R, tmX, tmXrow, d, st);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
   const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y};
   if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, tmY, tmYrow, u, st) : launch_up<true, 2>(S, R, tmY, tmYrow, u, st);
