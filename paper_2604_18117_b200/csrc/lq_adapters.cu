@@ -20,15 +20,16 @@ constexpr int CLUSTER = 8, WARPS = 8;
 // ---- the map: a stable counting sort in one block ------------------------------------------------------------------------
 // Each of the 32 warps counts the adapters of its own run of rows, then places them behind those of the warps before it.  Eight loads of a warp are in
 // flight together, and a run of up to 256 rows is read once: what this costs is latency (us, M = 8192, three adapters: 11.3 one load after the other).
-__global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int M, int slots, int tile_rows, int* perm, LqAdTile* tiles, int* ntiles) {
+__global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int M, int slots, int* perm, LqAdTile* tiles, LqAdTile* small, int* ntiles) {
   extern __shared__ int count[];     // [32][slots + 1]
   __shared__ int scan_rows[32], scan_tiles[32];
   constexpr int AHEAD = 8;
   const int bins = slots + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  for (int i = tid; i < 32 * bins; i += 1024) count[i] = 0;
+  const int run = ((M + 31) / 32 + 31) & ~31;                  // rows a warp: whole loads
+  const int warps = (M + run - 1) / run;                       // that have any
+  for (int i = tid; i < warps * bins; i += 1024) count[i] = 0;
   grid_launch_dependents();
   grid_dependency_wait();
-  const int run = ((M + 31) / 32 + 31) & ~31;                  // rows a warp: whole loads
   const long long first = (long long)warp * run;
   const int n = (int)max(0ll, min((long long)run, M - first)); // this warp's rows
   int* mine = count + warp * bins;
@@ -55,12 +56,11 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     }
   }
   __syncthreads();
-  // thread b: rows and tiles of bin b, and where they begin
-  int rows = 0, nt = 0;
-  if (tid < bins) {
-    for (int w = 0; w < 32; ++w) rows += count[w * bins + tid];
-    nt = (rows + tile_rows - 1) / tile_rows;
-  }
+  // thread b: rows and tiles of bin b, and where they begin.  Tiles of 128 rows count from bit 12 on, tiles of 16, of which there are fewer than 4096, below
+  int rows = 0;
+  if (tid < bins)
+    for (int w = 0; w < warps; ++w) rows += count[w * bins + tid];
+  const int large = (rows + LQ_AD_TILE - 1) / LQ_AD_TILE, little = M <= LQ_AD_SMALL_M_NARROW ? (rows + LQ_AD_SMALL_TILE - 1) / LQ_AD_SMALL_TILE : 0, nt = large << 12 | little;
   int a = rows, b = nt;
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
@@ -79,13 +79,14 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     scan_rows[lane] = u; scan_tiles[lane] = v;
   }
   __syncthreads();
-  if (tid == 0) *ntiles = scan_tiles[31];
+  if (tid == 0) { ntiles[0] = scan_tiles[31] >> 12; ntiles[1] = scan_tiles[31] & 0xFFF; }
   if (tid < bins) {
     int at = a - rows + (warp > 0 ? scan_rows[warp - 1] : 0);
     const int tile0 = b - nt + (warp > 0 ? scan_tiles[warp - 1] : 0);
-    for (int i = 0; i < nt; ++i)
-      tiles[tile0 + i] = LqAdTile{tid < slots ? tid : -1, at + i * tile_rows, min(tile_rows, rows - i * tile_rows), -1};
-    for (int w = 0; w < 32; ++w) {
+    const int adapter = tid < slots ? tid : -1;
+    for (int i = 0; i < large; ++i) tiles[(tile0 >> 12) + i] = LqAdTile{adapter, at + i * LQ_AD_TILE, min(LQ_AD_TILE, rows - i * LQ_AD_TILE), -1};
+    for (int i = 0; i < little; ++i) small[(tile0 & 0xFFF) + i] = LqAdTile{adapter, at + i * LQ_AD_SMALL_TILE, min(LQ_AD_SMALL_TILE, rows - i * LQ_AD_SMALL_TILE), -1};
+    for (int w = 0; w < warps; ++w) {
       const int c = count[w * bins + tid];
       count[w * bins + tid] = at;
       at += c;
@@ -107,10 +108,10 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
       __syncwarp();
     }
   }
-  // tiles whose rows are neighbours (perm ascends within a tile): the form for many rows asks
-  if (tile_rows < LQ_AD_TILE) return;
+  // large tiles whose rows are neighbours (perm ascends within a tile)
+  if (M <= LQ_AD_SMALL_M) return;
   __syncthreads();
-  for (int i = tid; i < scan_tiles[31]; i += 1024) {
+  for (int i = tid; i < scan_tiles[31] >> 12; i += 1024) {
     const LqAdTile t = tiles[i];
     const int r = perm[t.begin];
     if (perm[t.begin + t.rows - 1] - r == t.rows - 1) tiles[i].first = r;
@@ -146,7 +147,7 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
 // The order of a product's inner index is free as long as both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7
 // of each 32, so that a fragment of either operand is one 16-byte load from rows that run along the inner index.
 template <int RP>
-__global__ void __launch_bounds__(32 * WARPS) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, const int* perm, const __half* X, const void* Y0,
+__global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, const int* perm, const __half* X, const void* Y0,
                                                                  void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad,
                                                                  int out_f32) {
   constexpr int NT = RP / 8, KB = (RP + 31) / 32;
@@ -159,8 +160,9 @@ __global__ void __launch_bounds__(32 * WARPS) lq_adapters_kernel(const LqAdTile*
   const int rank_in_cluster = blockIdx.x % CLUSTER, ti = blockIdx.x / CLUSTER;
   grid_launch_dependents();
   grid_dependency_wait();
-  if (ti >= *ntiles) return;                              // (the whole cluster)
+  // (a tile behind the last one holds anything: it is asked for together with their number, which saves a trip)
   const LqAdTile tile = tiles[ti];
+  if (ti >= *ntiles) return;                              // (the whole cluster)
   const LqAdMeta m = tile.adapter >= 0 ? meta[tile.adapter] : LqAdMeta{0, 0.f};
   const int unit = warp * CLUSTER + rank_in_cluster, units = WARPS * CLUSTER;
   const bool has0 = g < tile.rows, has1 = g + 8 < tile.rows;
@@ -309,7 +311,8 @@ size_t forward_smem(int rp) {
 }
 template <int RP>
 cudaError_t launch_forward(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
-  return lq_launch_cluster(lq_adapters_kernel<RP>, lq_ad_tiles(R) * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st, (const LqAdTile*)R->d_tiles, (const int*)R->d_ntiles,
+  return lq_launch_cluster(lq_adapters_kernel<RP>, lq_ad_tiles(R->M, R->slots, LQ_AD_SMALL_TILE) * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st,
+                           (const LqAdTile*)R->d_small, (const int*)R->d_ntiles + 1,
                            (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up, (const LqAdMeta*)S->d_meta, S->K,
                            S->N, S->Npad, dt == LQ_OUT_F32 ? 1 : 0);
 }
@@ -382,12 +385,12 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
   lq_rowmap* R = new (std::nothrow) lq_rowmap();
   if (!R) return LQ_ERR_ALLOC;
   R->M_max = M_max; R->slots = slots; R->device = device; R->M = 0;
-  // (a map of many rows may be set to few, in smaller tiles)
-  R->tiles_max = std::max(lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M), LQ_AD_SMALL_TILE), lq_ceil_div(M_max, LQ_AD_TILE)) + slots + 1;
   const size_t rows = M_max > LQ_AD_SMALL_M ? (size_t)M_max + LQ_AD_TILE : 0;
+  const size_t large = (size_t)lq_ceil_div(M_max, LQ_AD_TILE) + slots + 1, little = (size_t)lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M_NARROW), LQ_AD_SMALL_TILE) + slots + 1;
   if (lq_note_cuda(cudaDeviceGetAttribute(&R->sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, sizeof(int))) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&R->d_tiles, (size_t)R->tiles_max * sizeof(LqAdTile))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, 2 * sizeof(int))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_tiles, large * sizeof(LqAdTile))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_small, little * sizeof(LqAdTile))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_perm, (size_t)M_max * sizeof(int))) != cudaSuccess ||
       (rows > 0 && (lq_note_cuda(cudaMalloc((void**)&R->d_T, rows * LQ_AD_TROW * 2)) != cudaSuccess ||
                     lq_note_cuda(cudaMalloc((void**)&R->d_rscale, rows * sizeof(float))) != cudaSuccess))) {
@@ -424,7 +427,7 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
 extern "C" lq_status lq_rowmap_free(lq_rowmap* R) {
   if (!R) return LQ_ERR_INVALID_ARG;
   LqDeviceGuard guard(R->device);
-  cudaFree(R->d_ntiles); cudaFree(R->d_tiles); cudaFree(R->d_perm); cudaFree(R->d_T); cudaFree(R->d_rscale);
+  cudaFree(R->d_ntiles); cudaFree(R->d_tiles); cudaFree(R->d_small); cudaFree(R->d_perm); cudaFree(R->d_T); cudaFree(R->d_rscale);
   delete R;
   return LQ_OK;
 }
@@ -433,12 +436,9 @@ extern "C" lq_status lq_rowmap_set(lq_rowmap* R, const int32_t* ids, int32_t M, 
   if (!R || !ids || M <= 0 || M > R->M_max || ((uintptr_t)ids & 3) != 0) return LQ_ERR_INVALID_ARG;
   LqDeviceGuard guard(R->device);
   if (!guard.ok) return LQ_ERR_CUDA;
-  const int tile_rows = M <= LQ_AD_SMALL_M ? LQ_AD_SMALL_TILE : LQ_AD_TILE;
-  const cudaError_t e = lq_launch(lq_rowmap_kernel, 1, 1024, (size_t)32 * (R->slots + 1) * 4, (cudaStream_t)stream, ids, M, R->slots, tile_rows, R->d_perm,
-                                  R->d_tiles, R->d_ntiles);
+  const cudaError_t e = lq_launch(lq_rowmap_kernel, 1, 1024, (size_t)32 * (R->slots + 1) * 4, (cudaStream_t)stream, ids, M, R->slots, R->d_perm, R->d_tiles, R->d_small, R->d_ntiles);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
   R->M = M;
-  R->tile_rows = tile_rows;
   return LQ_OK;
 }
 
@@ -450,7 +450,7 @@ extern "C" lq_status lq_adapters_forward(const lq_adapters* S, const lq_rowmap* 
   LqDeviceGuard guard(S->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
-  if (R->tile_rows == LQ_AD_TILE) return lq_adapters_forward_tiles(S, R, X, Y0, Y, dt, st);
+  if (!lq_ad_small_form(R->M, S->rp)) return lq_adapters_forward_tiles(S, R, X, Y0, Y, dt, st);
   const cudaError_t e = S->rp == 16   ? launch_forward<16>(S, R, X, Y0, Y, dt, st)
                         : S->rp == 32 ? launch_forward<32>(S, R, X, Y0, Y, dt, st)
                         : S->rp == 64 ? launch_forward<64>(S, R, X, Y0, Y, dt, st)

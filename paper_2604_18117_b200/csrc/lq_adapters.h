@@ -5,8 +5,11 @@
 
 #include "lq_internal.h"
 
-// A map's rows are cut into tiles of rows of one adapter: 16 rows for the form that serves few rows, 128 for the one that serves many.
-constexpr int LQ_AD_SMALL_M = 256, LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
+// Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows, and one on tiles of 128 rows.  us with the map, eight adapters, six
+// requests, K x N and rank, small / large form: 1152 x 3456, 32: 600 rows 15.6 / 20.8, 2048 rows 29.0 / 26.7, 3000 rows 43.7 / 34.5; 1152 x 1152, 16: 2048 rows
+// 17.5 / 20.6; 5600 x 2240, 128: 300 rows 29.5 / 24.9, 600 rows 51.4 / 31.2; 512 x 8192, 64: 300 rows 21.2 / 18.4.
+constexpr int LQ_AD_SMALL_M = 256, LQ_AD_SMALL_M_NARROW = 2048, LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
+static inline bool lq_ad_small_form(int M, int rp) { return M <= (rp <= 32 ? LQ_AD_SMALL_M_NARROW : LQ_AD_SMALL_M); }
 constexpr int LQ_AD_TROW = 256;        // halves of a row of the intermediate: 128 hi, 128 lo
 
 struct LqAdTile {
@@ -26,9 +29,9 @@ struct lq_adapters {
   CUtensorMap tmDown, tmUp;            // boxes of [rp] and [128] rows x 128 bytes, 128-byte swizzle
 };
 struct lq_rowmap {
-  int M_max, slots, device, M, tile_rows, tiles_max, sms;
-  int* d_ntiles;
-  LqAdTile* d_tiles;                   // [tiles_max]
+  int M_max, slots, device, M, sms;
+  int* d_ntiles;                       // [2]: tiles of 128 rows, of 16
+  LqAdTile *d_tiles, *d_small;         // (tiles of 16 rows only up to LQ_AD_SMALL_M_NARROW rows)
   int* d_perm;                         // [M_max]
   __half* d_T;                         // [M_max + 128][LQ_AD_TROW], in the order of perm (only with M_max > LQ_AD_SMALL_M)
   float* d_rscale;                     // [M_max + 128] what a row of T times B is multiplied with
@@ -36,7 +39,7 @@ struct lq_rowmap {
 };
 
 // most tiles that M rows can make
-static inline int lq_ad_tiles(const lq_rowmap* R) { return R->M < lq_ceil_div(R->M, R->tile_rows) + R->slots ? R->M : lq_ceil_div(R->M, R->tile_rows) + R->slots; }
+static inline int lq_ad_tiles(int M, int slots, int rows) { return M < lq_ceil_div(M, rows) + slots ? M : lq_ceil_div(M, rows) + slots; }
 
 lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st);
 lq_status lq_adapters_tiles_prepare();   // once for each device that a map is made on, with that device current

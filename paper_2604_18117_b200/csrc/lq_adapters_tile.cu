@@ -509,12 +509,12 @@ cudaError_t launch_down(const lq_adapters* S, const lq_rowmap* R, const CUtensor
   d.ring = std::min(std::min(MAX_STAGES, most), (DOWN_SMEM - 1024) / stage);
   while (d.tmem_cols < S->rp) d.tmem_cols *= 2;
   const int smem = 1024 + std::max(d.ring * stage, BM * (S->rp + 4) * 4);
-  return lq_launch_cluster(lq_adapters_down_kernel<SPLIT>, lq_ad_tiles(R) * SPLIT, 32 * DOWN_WARPS, SPLIT, smem, st, tmX, tmXrow, S->tmDown, d);
+  return lq_launch_cluster(lq_adapters_down_kernel<SPLIT>, lq_ad_tiles(R->M, R->slots, BM) * SPLIT, 32 * DOWN_WARPS, SPLIT, smem, st, tmX, tmXrow, S->tmDown, d);
 }
 
 template <bool F32, int NA>
 cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const CUtensorMap& tmY, const CUtensorMap& tmYrow, const UpParams& p, cudaStream_t st) {
-  const long long steps = (long long)lq_ad_tiles(R) * p.chunks;
+  const long long steps = (long long)lq_ad_tiles(R->M, R->slots, BM) * p.chunks;
   return lq_launch(lq_adapters_up_kernel<F32, NA>, (int)std::min<long long>(steps, R->sms), UP_THREADS, up_smem(NA), st, R->tmT, S->tmUp, tmY, tmYrow, p);
 }
 
