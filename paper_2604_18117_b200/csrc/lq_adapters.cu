@@ -56,10 +56,11 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     }
   }
   __syncthreads();
-  // thread b: rows and tiles of bin b, and where they begin.  Tiles of 128 rows count from bit 12 on, tiles of 16, of which there are fewer than 4096, below
+  // thread b: rows and tiles of bin b, and where they begin.  Tiles of 128 rows count from bit 12 on, tiles of 16, of which there are fewer than 4096, below it
   int rows = 0;
   if (tid < bins)
-    for (int w = 0; w < warps; ++w) rows += count[w * bins + tid];
+#pragma unroll
+    for (int w = 0; w < 32; ++w) rows += w < warps ? count[w * bins + tid] : 0;
   const int large = (rows + LQ_AD_TILE - 1) / LQ_AD_TILE, little = M <= LQ_AD_SMALL_M_NARROW ? (rows + LQ_AD_SMALL_TILE - 1) / LQ_AD_SMALL_TILE : 0, nt = large << 12 | little;
   int a = rows, b = nt;
 #pragma unroll
@@ -86,10 +87,13 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     const int adapter = tid < slots ? tid : -1;
     for (int i = 0; i < large; ++i) tiles[(tile0 >> 12) + i] = LqAdTile{adapter, at + i * LQ_AD_TILE, min(LQ_AD_TILE, rows - i * LQ_AD_TILE), -1};
     for (int i = 0; i < little; ++i) small[(tile0 & 0xFFF) + i] = LqAdTile{adapter, at + i * LQ_AD_SMALL_TILE, min(LQ_AD_SMALL_TILE, rows - i * LQ_AD_SMALL_TILE), -1};
-    for (int w = 0; w < warps; ++w) {
-      const int c = count[w * bins + tid];
-      count[w * bins + tid] = at;
-      at += c;
+    int c[32];
+#pragma unroll
+    for (int w = 0; w < 32; ++w) c[w] = w < warps ? count[w * bins + tid] : 0;
+#pragma unroll
+    for (int w = 0; w < 32; ++w) {
+      if (w < warps) count[w * bins + tid] = at;
+      at += c[w];
     }
   }
   __syncthreads();

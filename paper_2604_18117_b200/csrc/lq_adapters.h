@@ -6,9 +6,10 @@
 #include "lq_internal.h"
 
 // Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows, and one on tiles of 128 rows.  us with the map, eight adapters, six
-// requests, K x N and rank, small / large form: 1152 x 3456, 32: 600 rows 15.6 / 20.8, 2048 rows 29.0 / 26.7, 3000 rows 43.7 / 34.5; 1152 x 1152, 16: 2048 rows
-// 17.5 / 20.6; 5600 x 2240, 128: 300 rows 29.5 / 24.9, 600 rows 51.4 / 31.2; 512 x 8192, 64: 300 rows 21.2 / 18.4.
-constexpr int LQ_AD_SMALL_M = 256, LQ_AD_SMALL_M_NARROW = 2048, LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
+// requests of neighbouring rows, K x N and rank, small / large form: 1152 x 3456, 32: 600 rows 15.6 / 17, 1400 rows 25.1 / 21, 3000 rows 43.7 / 23.8; 1152 x 1152,
+// 16: 600 rows 10.6 / 14; 5600 x 2240, 128: 300 rows 29.5 / 20.5, 600 rows 51.4 / 20.7; 512 x 8192, 64: 300 rows 21.2 / 15.7.  Rows in any order, which the large
+// form fetches four at a time: 1160 x 2312, 24, fp32, 1365 rows 23.0 / 36.9.
+constexpr int LQ_AD_SMALL_M = 256, LQ_AD_SMALL_M_NARROW = 1536, LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
 static inline bool lq_ad_small_form(int M, int rp) { return M <= (rp <= 32 ? LQ_AD_SMALL_M_NARROW : LQ_AD_SMALL_M); }
 constexpr int LQ_AD_TROW = 256;        // halves of a row of the intermediate: 128 hi, 128 lo
 

@@ -39,18 +39,30 @@ __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory"); }
-// Copies 128 bytes at x of each of a tile's rows: a whole tile of neighbours in one copy, else four rows a copy (rows: a lane's).  The whole warp calls, one
-// lane issues: a copy's operands have to be uniform, and where the compiler cannot see that they are it takes the lanes one by one (455 clocks a stage of two copies for 345).
-__device__ __forceinline__ void fetch_rows(uint32_t dst, const CUtensorMap* tm, const CUtensorMap* tm_row, int x, const LqAdTile& t, bool whole, const int4& rows, uint32_t bar) {
-  if (whole) {
-    if (elect_one()) tma_load_2d(dst, tm, x, t.first, bar);
-  } else {
+// Copies 128 bytes at x of each of a tile's rows.  Neighbours: in one copy of 128 rows, or, where the tile is half of that or less, in copies of 32 (rows behind the
+// tile's last come along and are not looked at); others: four a copy (rows: a lane's).  The whole warp calls, one lane issues: a copy's operands have to be
+// uniform, and where the compiler cannot see that they are it takes the lanes one by one (455 clocks a stage of two copies for 345).
+struct RowMaps {
+  CUtensorMap whole, part, row;        // boxes of 128, 32 and one row x 128 bytes
+};
+__device__ __forceinline__ uint32_t fetch_bytes(const LqAdTile& t) {
+  return t.first < 0 ? (t.rows + 3) / 4 * 512 : 2 * t.rows > BM ? A_STAGE : (t.rows + 31) / 32 * 4096;
+}
+__device__ __forceinline__ void fetch_rows(uint32_t dst, const RowMaps& tm, int x, const LqAdTile& t, const int4& rows, uint32_t bar) {
+  if (t.first < 0) {
     for (int i = 0; 4 * i < t.rows; ++i) {
       const int4 r = make_int4(__shfl_sync(0xffffffffu, rows.x, i), __shfl_sync(0xffffffffu, rows.y, i), __shfl_sync(0xffffffffu, rows.z, i), __shfl_sync(0xffffffffu, rows.w, i));
-      if (elect_one()) tma_gather4(dst + i * 512, tm_row, x, r, bar);
+      if (elect_one()) tma_gather4(dst + i * 512, &tm.row, x, r, bar);
     }
+  } else if (2 * t.rows > BM) {
+    if (elect_one()) tma_load_2d(dst, &tm.whole, x, t.first, bar);
+  } else if (elect_one()) {
+    for (int i = 0; 32 * i < t.rows; ++i) tma_load_2d(dst + i * 4096, &tm.part, x, t.first + 32 * i, bar);
   }
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory"); }
+__device__ __forceinline__ void prefetch_maps(const RowMaps& tm) {
+  prefetch_map(&tm.whole); prefetch_map(&tm.part); prefetch_map(&tm.row);
 }
 
 // ---- down ----------------------------------------------------------------------------------------------------------
@@ -71,8 +83,8 @@ struct DownParams {
 // nothing waits for what it does not need (an empty slot's tile is formed like another and left unread), the loads of a row's sums are all in flight
 // together.  (8192 x 1152, rank 32, us from the dependency's end: tile known 0.6, copies asked for 1.5, sums complete 6.4, in shared memory of all 7.5, T written 8.8.)
 template <int SPLIT>
-__global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmXrow,
-                                                                           const __grid_constant__ CUtensorMap tmDown, const __grid_constant__ DownParams p) {
+__global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const __grid_constant__ RowMaps tmX, const __grid_constant__ CUtensorMap tmDown,
+                                                                           const __grid_constant__ DownParams p) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * MAX_STAGES + 1];
   __shared__ uint32_t tmem_slot;
@@ -89,7 +101,7 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
     mbar_init(done, 1);
     abort_flag = 0;
     mbar_init_fence();
-    prefetch_map(&tmX); prefetch_map(&tmXrow); prefetch_map(&tmDown);
+    prefetch_maps(tmX); prefetch_map(&tmDown);
   }
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), p.tmem_cols);
   tc_fence_before();
@@ -107,10 +119,9 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
     const float scale = p.meta[tile.adapter].scale;
     bool ok = true;
     if (warp == 0) {
-      const bool whole = tile.first >= 0 && tile.rows == BM;
-      const uint32_t bytes = (whole ? A_STAGE : (tile.rows + 3) / 4 * 512) + p.rp * 128;
+      const uint32_t bytes = fetch_bytes(tile) + p.rp * 128;
       int4 rows = make_int4(0, 0, 0, 0);
-      if (!whole) rows = tile_rows4(p.perm + tile.begin, tile.rows, lane);
+      if (tile.first < 0) rows = tile_rows4(p.perm + tile.begin, tile.rows, lane);
       for (int it = 0; it < n; ++it) {
         const int s = it % p.ring;
         if (it >= p.ring && !(ok = mbar_wait_warp(empty(s), ((it / p.ring) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
@@ -121,7 +132,7 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
           tma_load_2d(a + A_STAGE, &tmDown, x, tile.adapter * p.rp, full(s));
         }
         __syncwarp();
-        fetch_rows(a, &tmX, &tmXrow, x, tile, whole, rows, full(s));
+        fetch_rows(a, tmX, x, tile, rows, full(s));
       }
       if (!ok)                                            // copies in flight land before the CTA goes
         for (int it = max(0, n - p.ring); it < n; ++it) mbar_settle(full(it % p.ring), (it / p.ring) & 1);
@@ -238,7 +249,7 @@ struct UpParams {
 // (Y0 straight into registers a step ahead, 32 KB in flight: 30.7 us for 8192 x 3456, rank 32, against 17.3 at the measured copy rate.)
 template <bool F32, int NA>      // NA: 64-wide pieces of the rank
 __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmUp,
-                                                                       const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmYrow,
+                                                                       const __grid_constant__ RowMaps tmY,
                                                                        const __grid_constant__ UpParams p) {
   constexpr int NT = up_t_bufs(NA), NB = up_b_stages(NA), T_BUF = 2 * NA * PIECE, B_STAGE = NA * PIECE, B_AT = NT * T_BUF, Y_AT = B_AT + NB * B_STAGE;
   constexpr int YP = F32 ? 4 : 2, Y_READERS = UP_DRAIN_WARPS / YP;      // pieces of a step; warps that read one
@@ -254,7 +265,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
     for (int i = 0; i < NBAR; ++i) mbar_init(bar(i), i >= YFREE ? Y_READERS : i >= AFREE ? UP_DRAIN_WARPS : 1);
     abort_flag = 0;
     mbar_init_fence();
-    prefetch_map(&tmT); prefetch_map(&tmUp); prefetch_map(&tmY); prefetch_map(&tmYrow);
+    prefetch_map(&tmT); prefetch_map(&tmUp); prefetch_maps(tmY);
   }
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), 2 * UP_COLS);
   tc_fence_before();
@@ -376,14 +387,13 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
       bool enter = true;
       for (int i = 0, ti = ti0, ch = ch0; i < n && ok; ++i) {
         if (f.rank > 0 || !p.in_place) {                  // (rows without an adapter are copied, or left alone)
-          const bool whole = f.tile.first >= 0 && f.tile.rows == BM;
-          if (enter && !whole) rows = tile_rows4(p.perm + f.tile.begin, f.tile.rows, lane);
+          if (enter && f.tile.first < 0) rows = tile_rows4(p.perm + f.tile.begin, f.tile.rows, lane);
           for (int u = 0; u < YP && ok; ++u, ++uses) {
             const int s = uses % Y_SLOTS, x = (ch * YP + u) * 128;
             if (uses >= Y_SLOTS && !(ok = mbar_wait_warp(bar(YFREE + s), ((uses / Y_SLOTS) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
-            if (elect_one()) mbar_expect_tx(bar(YFULL + s), whole ? PIECE : (f.tile.rows + 3) / 4 * 512);
+            if (elect_one()) mbar_expect_tx(bar(YFULL + s), fetch_bytes(f.tile));
             __syncwarp();
-            fetch_rows(base + Y_AT + s * PIECE, &tmY, &tmYrow, x, f.tile, whole, rows, bar(YFULL + s));
+            fetch_rows(base + Y_AT + s * PIECE, tmY, x, f.tile, rows, bar(YFULL + s));
           }
         }
         enter = ++ch == p.chunks;
@@ -504,18 +514,18 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
 constexpr int DOWN_SMEM = 110 * 1024;                     // two CTAs an SM
 
 template <int SPLIT>
-cudaError_t launch_down(const lq_adapters* S, const lq_rowmap* R, const CUtensorMap& tmX, const CUtensorMap& tmXrow, DownParams& d, cudaStream_t st) {
+cudaError_t launch_down(const lq_adapters* S, const lq_rowmap* R, const RowMaps& tmX, DownParams& d, cudaStream_t st) {
   const int stage = A_STAGE + S->rp * 128, most = (d.k_stages + SPLIT - 1) / SPLIT;
   d.ring = std::min(std::min(MAX_STAGES, most), (DOWN_SMEM - 1024) / stage);
   while (d.tmem_cols < S->rp) d.tmem_cols *= 2;
   const int smem = 1024 + std::max(d.ring * stage, BM * (S->rp + 4) * 4);
-  return lq_launch_cluster(lq_adapters_down_kernel<SPLIT>, lq_ad_tiles(R->M, R->slots, BM) * SPLIT, 32 * DOWN_WARPS, SPLIT, smem, st, tmX, tmXrow, S->tmDown, d);
+  return lq_launch_cluster(lq_adapters_down_kernel<SPLIT>, lq_ad_tiles(R->M, R->slots, BM) * SPLIT, 32 * DOWN_WARPS, SPLIT, smem, st, tmX, S->tmDown, d);
 }
 
 template <bool F32, int NA>
-cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const CUtensorMap& tmY, const CUtensorMap& tmYrow, const UpParams& p, cudaStream_t st) {
+cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const RowMaps& tmY, const UpParams& p, cudaStream_t st) {
   const long long steps = (long long)lq_ad_tiles(R->M, R->slots, BM) * p.chunks;
-  return lq_launch(lq_adapters_up_kernel<F32, NA>, (int)std::min<long long>(steps, R->sms), UP_THREADS, up_smem(NA), st, R->tmT, S->tmUp, tmY, tmYrow, p);
+  return lq_launch(lq_adapters_up_kernel<F32, NA>, (int)std::min<long long>(steps, R->sms), UP_THREADS, up_smem(NA), st, R->tmT, S->tmUp, tmY, p);
 }
 
 }  // namespace
@@ -530,12 +540,15 @@ lq_status lq_adapters_tiles_prepare() {
 }
 
 lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
-  CUtensorMap tmX, tmXrow, tmY, tmYrow;
-  const uint64_t M = (uint64_t)R->M, x_row = (uint64_t)S->K * 2, y_row = (uint64_t)S->N * (dt == LQ_OUT_F32 ? 4 : 2);
+  RowMaps tmX, tmY;
+  const auto rows_of = [R](RowMaps* tm, const void* base, uint64_t bytes) {
+    lq_status s;
+    if ((s = lq_make_tmap_bytes(&tm->whole, const_cast<void*>(base), (uint64_t)R->M, bytes, BM)) != LQ_OK) return s;
+    if ((s = lq_make_tmap_bytes(&tm->part, const_cast<void*>(base), (uint64_t)R->M, bytes, 32)) != LQ_OK) return s;
+    return lq_make_tmap_bytes(&tm->row, const_cast<void*>(base), (uint64_t)R->M, bytes, 1);
+  };
   lq_status s;
-  if ((s = lq_make_tmap_bytes(&tmX, const_cast<void*>(X), M, x_row, BM)) != LQ_OK || (s = lq_make_tmap_bytes(&tmXrow, const_cast<void*>(X), M, x_row, 1)) != LQ_OK ||
-      (s = lq_make_tmap_bytes(&tmY, const_cast<void*>(Y0), M, y_row, BM)) != LQ_OK || (s = lq_make_tmap_bytes(&tmYrow, const_cast<void*>(Y0), M, y_row, 1)) != LQ_OK)
-    return s;
+  if ((s = rows_of(&tmX, X, (uint64_t)S->K * 2)) != LQ_OK || (s = rows_of(&tmY, Y0, (uint64_t)S->N * (dt == LQ_OUT_F32 ? 4 : 2))) != LQ_OK) return s;
   int32_t* status = lq_device_status_ptr(S->device);
   if (!status) return LQ_ERR_CUDA;
   DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, S->rp, lq_ceil_div(S->K, 64), 1, 32};
@@ -543,13 +556,13 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
   const int tiles = lq_ceil_div(R->M, BM);
   int split = 1;
   while (split < 8 && tiles * 2 * split <= 2 * R->sms && d.k_stages >= 4 * split) split *= 2;
-  cudaError_t e = split == 1   ? launch_down<1>(S, R, tmX, tmXrow, d, st)
-                  : split == 2 ? launch_down<2>(S, R, tmX, tmXrow, d, st)
-                  : split == 4 ? launch_down<4>(S, R, tmX, tmXrow, d, st)
-                               : launch_down<8>(S, R, tmX, tmXrow, d, st);
+  cudaError_t e = split == 1   ? launch_down<1>(S, R, tmX, d, st)
+                  : split == 2 ? launch_down<2>(S, R, tmX, d, st)
+                  : split == 4 ? launch_down<4>(S, R, tmX, d, st)
+                               : launch_down<8>(S, R, tmX, d, st);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
   const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y};
-  if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, tmY, tmYrow, u, st) : launch_up<true, 2>(S, R, tmY, tmYrow, u, st);
-  else e = S->rp <= 64 ? launch_up<false, 1>(S, R, tmY, tmYrow, u, st) : launch_up<false, 2>(S, R, tmY, tmYrow, u, st);
+  if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, tmY, u, st) : launch_up<true, 2>(S, R, tmY, u, st);
+  else e = S->rp <= 64 ? launch_up<false, 1>(S, R, tmY, u, st) : launch_up<false, 2>(S, R, tmY, u, st);
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
