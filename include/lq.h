@@ -349,6 +349,27 @@ typedef struct {
 lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32_t head_dim, int32_t sequences, int32_t seq_len, lq_norm norm, float eps,
                           const lq_rope* rope, const int32_t* pos_dev, lq_out_dtype in_dtype, lq_out_dtype out_dtype, void* cuda_stream);
 
+/* The queries, keys and values of an attention block in one call, four kernels on the stream: lq_quantize_act and lq_linear_forward of a
+ * layer whose N output columns are q_heads heads of queries, kv_heads of keys and kv_heads of values; the rows' adapters added to all of them;
+ * norm and rotation of the queries and keys, in place.  Equal to the bit to those calls one by one. */
+typedef struct {
+  int32_t head_dim, q_heads, kv_heads;     /* (q_heads + 2 kv_heads) head_dim = N                              */
+  int32_t sequences;                       /* M = sequences * rows of each                                     */
+  int32_t norm;                            /* an lq_norm                                                       */
+  float eps;
+  const float *q_weight, *k_weight;        /* as lq_heads.weight and .bias                                     */
+  const float *q_bias, *k_bias;
+  const lq_rope* rope;                     /* a table of no axes: no rotation                                  */
+  const int32_t* pos_dev;                  /* [M][axes]                                                        */
+} lq_qkv;
+
+/*   act, X_f16_dev, M   as for lq_quantize_act
+ *   set, map            the rows' adapters of this projection (set's K and N the layer's, map's rows M), or both NULL
+ *   Y_dev               [M][N] row-major half or float per `dtype`, device, 16-byte aligned
+ * Nothing is launched if an argument is refused.  Asynchronous on `cuda_stream`. */
+lq_status lq_qkv_forward(const lq_layer* layer, lq_act* act, const void* X_f16_dev, int32_t M, const lq_adapters* set, const lq_rowmap* map,
+                         const lq_qkv* qkv, void* Y_dev, lq_out_dtype dtype, void* cuda_stream);
+
 /* Decode the activation record of the last lq_quantize_act into plain host arrays (for
  * parity checks); NULL skips a part.  qx int8 [M][K], sx half bits [M][G] (MXINT4: the block
  * exponents e as int16 [M][G], since 2^e may lie below the fp16 range), qb int8 [M][K],

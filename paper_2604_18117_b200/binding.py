@@ -42,6 +42,12 @@ class LqHeads(C.Structure):
                 ("heads", C.c_int32)]
 
 
+class LqQkv(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("sequences", C.c_int32), ("norm", C.c_int32),
+                ("eps", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("q_bias", C.c_void_p), ("k_bias", C.c_void_p),
+                ("rope", C.c_void_p), ("pos_dev", C.c_void_p)]
+
+
 class LqError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -79,6 +85,7 @@ _SIGNATURES = {
     "lq_rope_free": [C.c_void_p],
     "lq_qk_norm_rope": [C.POINTER(LqHeads), C.POINTER(LqHeads), C.c_int32, C.c_int32, C.c_int32, C.c_int, C.c_float, C.c_void_p,
                         C.c_void_p, C.c_int, C.c_int, C.c_void_p],
+    "lq_qkv_forward": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(LqQkv), C.c_void_p, C.c_int, C.c_void_p],
     "lq_act_export": [C.c_void_p] * 8,
     "lq_get_device_status": [C.c_int, C.POINTER(C.c_int32), C.POINTER(C.c_int32)],
     "lq_set_option": [C.c_char_p, C.c_int32],
@@ -343,6 +350,16 @@ def lq_heads(in_ptr: int, in_strides, out_ptr: int, out_strides, heads: int, wei
 def lq_qk_norm_rope(q: LqHeads | None, k: LqHeads | None, head_dim: int, sequences: int, seq_len: int, norm: int, eps: float, rope,
                     pos_dev_ptr: int | None, in_dtype: int = OUT_F16, out_dtype: int = OUT_F16, stream: int = 0):
     _check(lib().lq_qk_norm_rope(q, k, head_dim, sequences, seq_len, norm, eps, rope, pos_dev_ptr, in_dtype, out_dtype, stream), "lq_qk_norm_rope")
+
+
+def lq_qkv(head_dim: int, q_heads: int, kv_heads: int, sequences: int, norm: int, eps: float, rope, pos_dev_ptr: int | None = None,
+           q_weight_ptr: int | None = None, k_weight_ptr: int | None = None, q_bias_ptr: int | None = None, k_bias_ptr: int | None = None) -> LqQkv:
+    return LqQkv(head_dim, q_heads, kv_heads, sequences, norm, eps, q_weight_ptr, k_weight_ptr, q_bias_ptr, k_bias_ptr, rope, pos_dev_ptr)
+
+
+def lq_qkv_forward(layer, act, X_dev_ptr: int, M: int, adapters, rowmap, qkv: LqQkv, Y_dev_ptr: int, dtype: int = OUT_F16, stream: int = 0):
+    """Quantizer, GEMM, the rows' adapters (both handles, or None), norm and rotation of queries and keys: Y [M, N]."""
+    _check(lib().lq_qkv_forward(layer, act, X_dev_ptr, M, adapters, rowmap, qkv, Y_dev_ptr, dtype, stream), "lq_qkv_forward")
 
 
 def lq_act_export(act, M: int, cfg: LqConfig, stream: int = 0) -> dict:

@@ -8,6 +8,7 @@
 #include <mutex>
 #include <new>
 
+#include "lq_adapters.h"
 #include "lq_host_chunks.h"
 #include "lq_internal.h"
 
@@ -740,6 +741,32 @@ extern "C" lq_status lq_linear_forward(const lq_layer* L, const lq_act* A, void*
   if (dt != LQ_OUT_F16 && dt != LQ_OUT_F32) return LQ_ERR_INVALID_ARG;
   if (((uintptr_t)Y & 15) != 0) return LQ_ERR_INVALID_ARG;
   return L->mx ? lq_launch_gemm_mx(L, A, Y, dt, (cudaStream_t)stream) : lq_launch_gemm(L, A, Y, dt, (cudaStream_t)stream);
+}
+
+extern "C" lq_status lq_qkv_forward(const lq_layer* L, lq_act* A, const void* X, int32_t M, const lq_adapters* S, const lq_rowmap* R, const lq_qkv* c, void* Y,
+                                    lq_out_dtype dt, void* stream) {
+  // all checks first, so that a refused call has changed nothing
+  if (!L || !A || !X || !c || !Y || !act_matches(L, A)) return LQ_ERR_INVALID_ARG;
+  if (M <= 0 || M > A->M_max || (dt != LQ_OUT_F16 && dt != LQ_OUT_F32)) return LQ_ERR_INVALID_ARG;
+  if ((((uintptr_t)X | (uintptr_t)Y) & 15) != 0) return LQ_ERR_INVALID_ARG;
+  if (c->head_dim <= 0 || c->q_heads <= 0 || c->kv_heads <= 0 || c->sequences <= 0 || M % c->sequences != 0) return LQ_ERR_INVALID_ARG;
+  if (((long long)c->q_heads + 2ll * c->kv_heads) * c->head_dim != L->N) return LQ_ERR_INVALID_ARG;
+  if ((S == nullptr) != (R == nullptr)) return LQ_ERR_INVALID_ARG;
+  if (S && (S->K != L->K || S->N != L->N || S->device != L->device || R->device != L->device || R->M != M || R->slots > S->slots)) return LQ_ERR_INVALID_ARG;
+  const int D = c->head_dim, rows = M / c->sequences;
+  const size_t esz = dt == LQ_OUT_F32 ? 4 : 2;
+  void* Yk = (uint8_t*)Y + (size_t)c->q_heads * D * esz;
+  const int64_t seq = (int64_t)rows * L->N;
+  const lq_heads q = {Y, Y, seq, L->N, D, seq, L->N, D, c->q_weight, c->q_bias, c->q_heads};
+  const lq_heads k = {Yk, Yk, seq, L->N, D, seq, L->N, D, c->k_weight, c->k_bias, c->kv_heads};
+  const auto heads = [&](bool launch) {
+    return lq_heads_run(&q, &k, D, c->sequences, rows, (lq_norm)c->norm, c->eps, c->rope, c->pos_dev, dt, dt, L->device, launch, (cudaStream_t)stream);
+  };
+  lq_status s;
+  if ((s = heads(false)) != LQ_OK) return s;
+  if ((s = lq_quantize_act(L, X, M, A, stream)) != LQ_OK || (s = lq_linear_forward(L, A, Y, dt, stream)) != LQ_OK) return s;
+  if (S && (s = lq_adapters_forward(S, R, X, Y, Y, dt, stream)) != LQ_OK) return s;
+  return heads(true);
 }
 
 static lq_status forward_host(const lq_layer* L, lq_act* A, const void* Xh, int32_t M, void* Yh, lq_out_dtype dt, void* stream,

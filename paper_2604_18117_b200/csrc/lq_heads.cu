@@ -467,8 +467,8 @@ extern "C" lq_status lq_rope_free(lq_rope* R) {
   return LQ_OK;
 }
 
-extern "C" lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32_t head_dim, int32_t sequences, int32_t seq_len, lq_norm norm,
-                                     float eps, const lq_rope* R, const int32_t* pos, lq_out_dtype in_dtype, lq_out_dtype out_dtype, void* stream) {
+lq_status lq_heads_run(const lq_heads* q, const lq_heads* k, int32_t head_dim, int32_t sequences, int32_t seq_len, lq_norm norm, float eps, const lq_rope* R,
+                       const int32_t* pos, lq_out_dtype in_dtype, lq_out_dtype out_dtype, int device, bool launch, cudaStream_t st) {
   if (!R || (!q && !k) || sequences < 1 || seq_len < 1 || head_dim < 1) return LQ_ERR_INVALID_ARG;
   if (norm != LQ_NORM_NONE && norm != LQ_NORM_RMS && norm != LQ_NORM_LAYER) return LQ_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || !isfinite(eps)) return LQ_ERR_INVALID_ARG;
@@ -489,12 +489,18 @@ extern "C" lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32
   p.seq_len = seq_len; p.axes = R->axes; p.pairs = R->pairs;
   p.eps = eps; p.inv_d = 1.f / (float)head_dim;
   p.turn = R->d_turn; p.axis = R->d_axis; p.pos = pos;
+  if (device >= 0 && device != R->device) return LQ_ERR_INVALID_ARG;
+  if (!launch) return LQ_OK;
   LqDeviceGuard guard(R->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   const int rot = R->pairs == 0 ? ROT_NONE : R->halves ? ROT_HALVES : ROT_PAIRS;
-  cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e =
       in_dtype == LQ_OUT_F16 ? (out_dtype == LQ_OUT_F16 ? launch_norm<__half, __half>(p, norm, rot, st) : launch_norm<__half, float>(p, norm, rot, st))
                              : (out_dtype == LQ_OUT_F16 ? launch_norm<float, __half>(p, norm, rot, st) : launch_norm<float, float>(p, norm, rot, st));
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+}
+
+extern "C" lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32_t head_dim, int32_t sequences, int32_t seq_len, lq_norm norm,
+                                     float eps, const lq_rope* R, const int32_t* pos, lq_out_dtype in_dtype, lq_out_dtype out_dtype, void* stream) {
+  return lq_heads_run(q, k, head_dim, sequences, seq_len, norm, eps, R, pos, in_dtype, out_dtype, -1, true, (cudaStream_t)stream);
 }

@@ -96,6 +96,10 @@ def inputs(rng, M, K, N, f32):
     (2500, 96, 72, [32] * 40, 0, False),
     (4096, 2240, 256, [128, 64], 4, True),
     (5000, 136, 344, [16, 1], 7, False),
+    (700, 576, 520, [64, 48, 20, 64], 20, False),          # many-row form: neighbours of less than half a tile
+    (261, 1152, 200, [96, 128, 70], 0, True),              # rows of three adapters in any order
+    (900, 64, 8, [128] * 30, 60, False),                   # tiles of few rows, one step each
+    (40000, 72, 136, [40, 40], 3, False),                  # several tiles to a CTA, runs that end inside them
 ])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_rows_against_64_bits(M, K, N, ranks, runs, f32, in_place):
@@ -171,6 +175,32 @@ def test_a_slot_is_replaced_and_emptied_in_stream_order():
     S.ranks[0] = 0
     last = forward(S, ids, X, Y0, True, slots=5)
     assert np.array_equal(last[ids != 1], Y0[ids != 1]) and np.array_equal(last[ids == 1], again[ids == 1])
+    S.free()
+
+
+@pytest.mark.parametrize("M", [150, 1500, 3000])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_empty_slots_are_no_adapters(M, in_place):
+    """Slots that hold nothing, between others: their rows keep Y0, also where whole tiles are theirs."""
+    rng = np.random.default_rng(M)
+    S = Set(rng, 200, 264, 64, [40, 64], slots=6)
+    X, Y0 = inputs(rng, M, 200, 264, False)
+    ids = (np.arange(M) * 11 // M) % 6
+    Y = forward(S, ids, X, Y0, False, in_place, slots=6)
+    ref, bound = reference(S, X, Y0, ids, False)
+    assert np.array_equal(Y[ids >= 2], Y0[ids >= 2]) and (np.abs(Y - ref) <= bound).all()
+    S.free()
+
+
+def test_the_most_slots_and_rows_of_each():
+    rng = np.random.default_rng(21)
+    S = Set(rng, 64, 40, 8, [8] * 5, slots=1023)
+    for M in (1023, 5000):
+        X, Y0 = inputs(rng, M, 64, 40, True)
+        ids = rng.permutation(np.arange(M) % 1023)         # a row or a few for every slot, five of which hold something
+        Y = forward(S, ids, X, Y0, True, slots=1023)
+        ref, bound = reference(S, X, Y0, ids, True)
+        assert np.array_equal(Y[ids >= 5], Y0[ids >= 5]) and (np.abs(Y - ref) <= bound).all()
     S.free()
 
 

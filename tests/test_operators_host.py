@@ -31,6 +31,7 @@ def test_null_handles():
     assert L.lq_adapters_set(None, 0, 1, None, None, 1.0, None) == 1 and L.lq_rowmap_set(None, None, 1, None) == 1
     assert L.lq_adapters_forward(None, None, None, None, None, 0, None) == 1
     assert L.lq_qk_norm_rope(None, None, 64, 1, 1, 1, 1e-6, None, None, 0, 0, None) == 1
+    assert L.lq_qkv_forward(None, None, None, 1, None, None, None, None, 0, None) == 1
     assert L.lq_rope_config_default(None, 0, None) == 1 and L.lq_rope_create(None, None, None, 0, None) == 1
 
 
@@ -55,3 +56,4 @@ def test_rotation_tables():
 def test_layouts_of_the_structures():
     """The binding's structures have the header's sizes (four bytes before theta, and at the end of the heads)."""
     assert C.sizeof(B.LqHeads) == 2 * 8 + 6 * 8 + 2 * 8 + 8 and C.sizeof(B.LqRopeConfig) == 7 * 4 + 4 + 8
+    assert C.sizeof(B.LqQkv) == 6 * 4 + 6 * 8
