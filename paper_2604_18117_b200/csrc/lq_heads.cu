@@ -26,7 +26,7 @@ struct lq_rope {
 
 namespace {
 
-constexpr int MAX_D = 256, WARPS = 4, MAX_ROWS = 4;
+constexpr int MAX_D = 256, WARPS = 4, MAX_ROWS = 2;
 enum { ROT_NONE = 0, ROT_PAIRS = 1, ROT_HALVES = 2 };
 
 struct Side {
@@ -124,7 +124,7 @@ __device__ __forceinline__ float2 cos_sin(uint64_t turn, int32_t pos) {
 }
 
 // Sum over a group's L neighbouring lanes, in every lane of it.  Powers of two: xor steps.  Other L known at compile time: sums over windows of
-// 1, .., L lanes round the group, each twice the one before or one longer (L = 7: 1, 2, 3, 6, 7).  L = 0: `lanes` lanes, summed up to the group's
+// 1, .., L lanes round the group, each twice the one before or one longer (L = 9: 1, 2, 4, 8, 9).  L = 0: `lanes` lanes, summed up to the group's
 // first lane and handed back.
 template <int L>
 __device__ __forceinline__ float group_sum(float a, int lanes, int at, int lane) {
@@ -158,13 +158,16 @@ __device__ __forceinline__ float group_sum(float a, int lanes, int at, int lane)
 // A block takes a few rows and forms their angles together.  Its warps share out the rows' heads: one walks over the queries, or the keys, of a
 // row, or over a part of them.  L lanes hold a head, each lane C times eight entries that are the two sides of the same four pairs in every head, so
 // weights times cosines and sines stay in registers along the walk; the norm's sum crosses the head's lanes by shuffles.  What bounds it short of the
-// memory is the issue of instructions, so a lane holds as much of a head as registers allow, and where L is known (then the whole head is rotated, or
-// nothing) every address is a base and a constant.
+// memory is the issue of instructions (32 heads of 72: 1924 a row at first, 64-bit address arithmetic and moves most of them) and warps enough to cover their
+// latency: where L is known (then the whole head is rotated, or nothing) every address is a base and a constant; a lane holds 16 entries of heads of 64 and 128,
+// but of 72 only 8 (24, for three lanes a head, take 128 registers: 24.7 us for 18.9); blocks are small, so that few warps wait for the angles of others.
+// B200, us and share of the measured copy rate of its bytes: 32760 rows, 40 heads of 128, fp16 110.6, 0.93; 8192 rows, 32 heads of 72, fp16 18.9, 0.61;
+// 4100 rows, 32 heads of 128, fp32, no norm 24.6, 0.83; one row 2.0.
 template <typename TIN, typename TOUT, int NORM, int ROT, int L, int C>
-__global__ void __launch_bounds__(32 * WARPS, C == 1 && sizeof(TIN) == 2 && NORM != LQ_NORM_LAYER ? 6 : C == 2 && L != 7 && sizeof(TIN) == 2 ? 5 : 4) lq_heads_kernel(const __grid_constant__ HeadsParams p) {
+__global__ void __launch_bounds__(32 * WARPS, C == 1 && sizeof(TIN) == 2 && NORM != LQ_NORM_LAYER ? 7 : C == 2 && sizeof(TIN) == 2 ? 5 : 4) lq_heads_kernel(const __grid_constant__ HeadsParams p) {
   constexpr bool SPLIT = ROT == ROT_HALVES, NEIGHBOURS = ROT == ROT_PAIRS, FIXED = L > 0;
   static_assert(FIXED || C == 1, "");
-  constexpr int DEPTH = sizeof(TIN) == 2 ? (C == 1 ? 4 : C == 2 ? 3 : 2) : (C == 1 ? 3 : C == 2 ? 2 : 1);      // heads of a lane in flight
+  constexpr int DEPTH = sizeof(TIN) == 2 ? 3 : C == 1 ? 3 : 2;      // heads of a lane in flight
   constexpr int UNIT = SPLIT ? 4 : 8;                     // entries from one lane's to the next one's
   __shared__ __align__(16) float trig[ROT == ROT_NONE ? 1 : MAX_ROWS * MAX_D];         // [rows of the block][cos, sin][pairs, a multiple of four]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lanes = FIXED ? L : p.lanes, groups = FIXED ? 32 / (FIXED ? L : 1) : p.groups;
@@ -350,15 +353,15 @@ cudaError_t launch(HeadsParams& p, cudaStream_t st) {
   p.by_groups = reciprocal(std::max(2, g));
   return lq_launch_grid(lq_heads_kernel<TIN, TOUT, NORM, ROT, L, C>, dim3(lq_ceil_div(p.rows, p.block_rows), blocks_y), 32 * WARPS, 1, 0, st, p);
 }
-// Under an RMS norm heads of 64, 72, 112 and 128 entries that are rotated as a whole, or not at all, have their lanes at compile time, 16 or 24 entries
-// to each; others hold eight entries a lane.
+// Under an RMS norm heads of 64, 72, 112 and 128 entries that are rotated as a whole, or not at all, have their lanes at compile time, 16 entries to each where
+// lanes are a power of two; others hold eight entries a lane.  (8192 rows, 32 heads of 72: 26 us by the general form.)
 template <typename TIN, typename TOUT, int NORM, int ROT>
 cudaError_t launch_lanes(HeadsParams& p, cudaStream_t st) {
   if constexpr (NORM == LQ_NORM_RMS)
     if (ROT == ROT_NONE || p.pairs == 4 * p.lanes) {
       if (p.lanes == 8) return launch<TIN, TOUT, NORM, ROT, 4, 2>(p, st);
-      if (p.lanes == 9) return launch<TIN, TOUT, NORM, ROT, 3, 3>(p, st);
-      if (p.lanes == 14) return launch<TIN, TOUT, NORM, ROT, 7, 2>(p, st);
+      if (p.lanes == 9) return launch<TIN, TOUT, NORM, ROT, 9, 1>(p, st);
+      if (p.lanes == 14) return launch<TIN, TOUT, NORM, ROT, 14, 1>(p, st);
       if (p.lanes == 16) return launch<TIN, TOUT, NORM, ROT, 8, 2>(p, st);
     }
   return launch<TIN, TOUT, NORM, ROT, 0, 1>(p, st);
