@@ -15,7 +15,7 @@ using namespace lqdev;
 namespace {
 
 constexpr int MAX_SLOTS = 1023;      // bins of the sort: the slots and "none"
-constexpr int CLUSTER = 8, WARPS = 8;
+constexpr int WARPS = 8;
 
 // ---- the map: a stable counting sort in one block ------------------------------------------------------------------------
 // Each of the 32 warps counts the adapters of its own run of rows, then places them behind those of the warps before it.  Eight loads of a warp are in
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
   if (tid < bins)
 #pragma unroll
     for (int w = 0; w < 32; ++w) rows += w < warps ? count[w * bins + tid] : 0;
-  const int large = (rows + LQ_AD_TILE - 1) / LQ_AD_TILE, little = M <= LQ_AD_SMALL_M_NARROW ? (rows + LQ_AD_SMALL_TILE - 1) / LQ_AD_SMALL_TILE : 0, nt = large << 12 | little;
+  const int large = (rows + LQ_AD_TILE - 1) / LQ_AD_TILE, little = M <= LQ_AD_SMALL_M ? (rows + LQ_AD_SMALL_TILE - 1) / LQ_AD_SMALL_TILE : 0, nt = large << 12 | little;
   int a = rows, b = nt;
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     }
   }
   // large tiles whose rows are neighbours (perm ascends within a tile)
-  if (M <= LQ_AD_SMALL_M) return;
+  if (M <= LQ_AD_SMALL_M_128) return;
   __syncthreads();
   for (int i = tid; i < scan_tiles[31] >> 12; i += 1024) {
     const LqAdTile t = tiles[i];
@@ -150,7 +150,7 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
 
 // The order of a product's inner index is free as long as both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7
 // of each 32, so that a fragment of either operand is one 16-byte load from rows that run along the inner index.
-template <int RP>
+template <int RP, int CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, const int* perm, const __half* X, const void* Y0,
                                                                  void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad,
                                                                  int out_f32) {
@@ -313,12 +313,18 @@ size_t forward_smem(int rp) {
   const int kb = (rp + 31) / 32;
   return (size_t)(WARPS + 1) * 16 * rp * 4 + 2 * 16 * kb * 32 * 2 + 16 * 4;
 }
+template <int RP, int CLUSTER>
+cudaError_t launch_cluster(const lq_adapters* S, const lq_rowmap* R, int tiles, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
+  return lq_launch_cluster(lq_adapters_kernel<RP, CLUSTER>, tiles * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st, (const LqAdTile*)R->d_small,
+                           (const int*)R->d_ntiles + 1, (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up,
+                           (const LqAdMeta*)S->d_meta, S->K, S->N, S->Npad, dt == LQ_OUT_F32 ? 1 : 0);
+}
 template <int RP>
 cudaError_t launch_forward(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
-  return lq_launch_cluster(lq_adapters_kernel<RP>, lq_ad_tiles(R->M, R->slots, LQ_AD_SMALL_TILE) * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st,
-                           (const LqAdTile*)R->d_small, (const int*)R->d_ntiles + 1,
-                           (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up, (const LqAdMeta*)S->d_meta, S->K,
-                           S->N, S->Npad, dt == LQ_OUT_F32 ? 1 : 0);
+  // Eight CTAs a tile while all of them are resident at once, else four (us with the map, eight / four: 1400 rows, 1152 x 3456, rank 32 25.8 / 20.9; 64 rows with an
+  // adapter each, 512 x 8192, rank 64 43.4 / 32.3; one row, 1152 x 3456, rank 32 9.2 / 11.2; two were never better).
+  const int tiles = lq_ad_tiles(R->M, R->slots, LQ_AD_SMALL_TILE), resident = (RP <= 32 ? 4 : RP <= 64 ? 3 : 2) * R->sms;
+  return 8 * tiles <= resident ? launch_cluster<RP, 8>(S, R, tiles, X, Y0, Y, dt, st) : launch_cluster<RP, 4>(S, R, tiles, X, Y0, Y, dt, st);
 }
 
 }  // namespace
@@ -389,8 +395,8 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
   lq_rowmap* R = new (std::nothrow) lq_rowmap();
   if (!R) return LQ_ERR_ALLOC;
   R->M_max = M_max; R->slots = slots; R->device = device; R->M = 0;
-  const size_t rows = M_max > LQ_AD_SMALL_M ? (size_t)M_max + LQ_AD_TILE : 0;
-  const size_t large = (size_t)lq_ceil_div(M_max, LQ_AD_TILE) + slots + 1, little = (size_t)lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M_NARROW), LQ_AD_SMALL_TILE) + slots + 1;
+  const size_t rows = M_max > LQ_AD_SMALL_M_128 ? (size_t)M_max + LQ_AD_TILE : 0;
+  const size_t large = (size_t)lq_ceil_div(M_max, LQ_AD_TILE) + slots + 1, little = (size_t)lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M), LQ_AD_SMALL_TILE) + slots + 1;
   if (lq_note_cuda(cudaDeviceGetAttribute(&R->sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, 2 * sizeof(int))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_tiles, large * sizeof(LqAdTile))) != cudaSuccess ||
@@ -415,12 +421,15 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
     lq_rowmap_free(R);
     return s;
   }
+  const auto room = [](auto* kernel, int rp) {
+    return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(rp))) == cudaSuccess;
+  };
   if (lq_note_cuda(cudaFuncSetAttribute(lq_rowmap_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * (MAX_SLOTS + 1) * 4)) != cudaSuccess ||
-      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(16))) != cudaSuccess ||
-      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(32))) != cudaSuccess ||
-      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(64))) != cudaSuccess ||
-      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<96>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(96))) != cudaSuccess ||
-      lq_note_cuda(cudaFuncSetAttribute(lq_adapters_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(128))) != cudaSuccess) {
+      !room(lq_adapters_kernel<16, 8>, 16) || !room(lq_adapters_kernel<16, 4>, 16) ||
+      !room(lq_adapters_kernel<32, 8>, 32) || !room(lq_adapters_kernel<32, 4>, 32) ||
+      !room(lq_adapters_kernel<64, 8>, 64) || !room(lq_adapters_kernel<64, 4>, 64) ||
+      !room(lq_adapters_kernel<96, 8>, 96) || !room(lq_adapters_kernel<96, 4>, 96) ||
+      !room(lq_adapters_kernel<128, 8>, 128) || !room(lq_adapters_kernel<128, 4>, 128)) {
     lq_rowmap_free(R);
     return LQ_ERR_CUDA;
   }

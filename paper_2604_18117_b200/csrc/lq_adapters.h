@@ -5,12 +5,13 @@
 
 #include "lq_internal.h"
 
-// Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows, and one on tiles of 128 rows.  us with the map, eight adapters, six
-// requests of neighbouring rows, K x N and rank, small / large form: 1152 x 3456, 32: 600 rows 15.6 / 17, 1400 rows 25.1 / 21, 3000 rows 43.7 / 23.8; 1152 x 1152,
-// 16: 600 rows 10.6 / 14; 5600 x 2240, 128: 300 rows 29.5 / 20.5, 600 rows 51.4 / 20.7; 512 x 8192, 64: 300 rows 21.2 / 15.7.  Rows in any order, which the large
-// form fetches four at a time: 1160 x 2312, 24, fp32, 1365 rows 23.0 / 36.9.
-constexpr int LQ_AD_SMALL_M = 256, LQ_AD_SMALL_M_NARROW = 1536, LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
-static inline bool lq_ad_small_form(int M, int rp) { return M <= (rp <= 32 ? LQ_AD_SMALL_M_NARROW : LQ_AD_SMALL_M); }
+// Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows, and one on tiles of 128 rows.  us with the map, K x N and rank, small /
+// large form.  Six requests of neighbouring rows: 1152 x 3456, 32: 600 rows 15.4 / 17, 1400 rows 20.9 / 21, 2048 rows 28.8 / 19.3; 512 x 8192, 64: 250 rows
+// 19.8 / 15.7; 5600 x 2240, 128: 250 rows 29.2 / 20.2.  Rows in any order, which the large form fetches four at a time: 1160 x 2312, 24, fp32, 1365 rows 20.2 / 36.9.
+// Rows with an adapter each: 512 x 8192, 64: 32 rows 22.0 / 23.8, 64 rows 32.4 / 36.4; 5600 x 2240, 128: 12 rows 27.1 / 22.4, 32 rows 49.5 / 30.7.
+constexpr int LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
+constexpr int LQ_AD_SMALL_M = 1536, LQ_AD_SMALL_M_64 = 128, LQ_AD_SMALL_M_128 = 16;      // most rows of the small form, for stored ranks up to 32, 64, 128
+static inline bool lq_ad_small_form(int M, int rp) { return M <= (rp <= 32 ? LQ_AD_SMALL_M : rp <= 64 ? LQ_AD_SMALL_M_64 : LQ_AD_SMALL_M_128); }
 constexpr int LQ_AD_TROW = 256;        // halves of a row of the intermediate: 128 hi, 128 lo
 
 struct LqAdTile {
@@ -32,9 +33,9 @@ struct lq_adapters {
 struct lq_rowmap {
   int M_max, slots, device, M, sms;
   int* d_ntiles;                       // [2]: tiles of 128 rows, of 16
-  LqAdTile *d_tiles, *d_small;         // (tiles of 16 rows only up to LQ_AD_SMALL_M_NARROW rows)
+  LqAdTile *d_tiles, *d_small;         // (tiles of 16 rows only up to LQ_AD_SMALL_M rows)
   int* d_perm;                         // [M_max]
-  __half* d_T;                         // [M_max + 128][LQ_AD_TROW], in the order of perm (only with M_max > LQ_AD_SMALL_M)
+  __half* d_T;                         // [M_max + 128][LQ_AD_TROW], in the order of perm (only where M_max can have the large form)
   float* d_rscale;                     // [M_max + 128] what a row of T times B is multiplied with
   CUtensorMap tmT;
 };
