@@ -1,7 +1,11 @@
 // Low-rank adapters of many requests beside a shared projection:  Y[m] = Y0[m] + scale_a (X[m] A_a) B_a,  a = the adapter of row m.
 //
 // A map sorts the rows of a batch by adapter (stable) and cuts them into tiles of rows of one adapter; every projection of a step
-// uses it.
+// uses it.  This file has the map, the set of adapters, and the forward for few rows; lq_adapters_tile.cu has the one for many.
+//
+// T = X A is summed in fp32 and enters the second product as two halves, hi + lo, under a power of two of its row: 22 bits of the row's largest entry, at
+// the price of a second MMA for each 16 of the rank, which no form is bound by.  (One half would round T to 11 bits, as much as an fp16 output is
+// rounded, and too much for an fp32 one.)
 #include <math.h>
 
 #include <algorithm>
@@ -16,22 +20,24 @@ namespace {
 
 constexpr int MAX_SLOTS = 1023;      // bins of the sort: the slots and "none"
 constexpr int WARPS = 8;
+constexpr int ROWMAP_SINGLE = 4096;  // most rows that one block sorts; more: eight blocks (us: 2048 rows 4.2 / 5.5, 8192 rows 6.6 / 5.7, 32768 rows 18.4 / 7.1)
 
-// ---- the map: a stable counting sort in one block ------------------------------------------------------------------------
-// Each of the 32 warps counts the adapters of its own run of rows, then places them behind those of the warps before it.  Eight loads of a warp are in
-// flight together, and a run of up to 256 rows is read once: what this costs is latency (us, M = 8192, three adapters: 11.3 one load after the other).
+// ---- the map: a stable counting sort by one block, or by a cluster of them -----------------------------------------------
+// Each warp counts the adapters of its own run of rows, then places them behind those of the warps before it.  What this costs is latency: up to eight loads of a
+// warp are in flight together, a run of up to 256 rows is read once, and many rows are shared by eight blocks.
+template <int BLOCKS>
 __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int M, int slots, int* perm, LqAdTile* tiles, LqAdTile* small, int* ntiles) {
   extern __shared__ int count[];     // [32][slots + 1]
-  __shared__ int scan_rows[32], scan_tiles[32];
+  __shared__ int scan_rows[32], scan_tiles[32], total[MAX_SLOTS + 1];
   constexpr int AHEAD = 8;
-  const int bins = slots + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int run = ((M + 31) / 32 + 31) & ~31;                  // rows a warp: whole loads
-  const int warps = (M + run - 1) / run;                       // that have any
+  const int bins = slots + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, block = BLOCKS > 1 ? blockIdx.x : 0;
+  const int run = ((M + 32 * BLOCKS - 1) / (32 * BLOCKS) + 31) & ~31;    // rows a warp: whole loads
+  const long long first = (long long)(block * 32 + warp) * run;
+  const int n = (int)max(0ll, min((long long)run, M - first)); // this warp's rows
+  const int warps = (int)max(0ll, min(32ll, (M - (long long)block * 32 * run + run - 1) / run));     // of this block that have any
   for (int i = tid; i < warps * bins; i += 1024) count[i] = 0;
   grid_launch_dependents();
   grid_dependency_wait();
-  const long long first = (long long)warp * run;
-  const int n = (int)max(0ll, min((long long)run, M - first)); // this warp's rows
   int* mine = count + warp * bins;
   int bin[AHEAD];                                              // of the rows in hand; -1: no row
   const auto read = [&](int r0) {
@@ -57,10 +63,25 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
   }
   __syncthreads();
   // thread b: rows and tiles of bin b, and where they begin.  Tiles of 128 rows count from bit 12 on, tiles of 16, of which there are fewer than 4096, below it
-  int rows = 0;
+  int rows = 0, before = 0;
   if (tid < bins)
 #pragma unroll
     for (int w = 0; w < 32; ++w) rows += w < warps ? count[w * bins + tid] : 0;
+  if constexpr (BLOCKS > 1) {
+    if (tid < bins) total[tid] = rows;
+    cluster_sync();
+    rows = 0;
+    if (tid < bins) {
+      int u[BLOCKS];
+#pragma unroll
+      for (int c = 0; c < BLOCKS; ++c) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(u[c]) : "r"(peer_smem(smem_u32(total + tid), c)) : "memory");
+#pragma unroll
+      for (int c = 0; c < BLOCKS; ++c) {
+        before += c < block ? u[c] : 0;
+        rows += u[c];
+      }
+    }
+  }
   const int large = (rows + LQ_AD_TILE - 1) / LQ_AD_TILE, little = M <= LQ_AD_SMALL_M ? (rows + LQ_AD_SMALL_TILE - 1) / LQ_AD_SMALL_TILE : 0, nt = large << 12 | little;
   int a = rows, b = nt;
 #pragma unroll
@@ -80,14 +101,14 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     scan_rows[lane] = u; scan_tiles[lane] = v;
   }
   __syncthreads();
-  if (tid == 0) { ntiles[0] = scan_tiles[31] >> 12; ntiles[1] = scan_tiles[31] & 0xFFF; }
+  if (tid == 0 && block == 0) { ntiles[0] = scan_tiles[31] >> 12; ntiles[1] = scan_tiles[31] & 0xFFF; }
   if (tid < bins) {
-    int at = a - rows + (warp > 0 ? scan_rows[warp - 1] : 0);
-    const int tile0 = b - nt + (warp > 0 ? scan_tiles[warp - 1] : 0);
-    const int adapter = tid < slots ? tid : -1;
-    for (int i = 0; i < large; ++i) tiles[(tile0 >> 12) + i] = LqAdTile{adapter, at + i * LQ_AD_TILE, min(LQ_AD_TILE, rows - i * LQ_AD_TILE), -1};
-    for (int i = 0; i < little; ++i) small[(tile0 & 0xFFF) + i] = LqAdTile{adapter, at + i * LQ_AD_SMALL_TILE, min(LQ_AD_SMALL_TILE, rows - i * LQ_AD_SMALL_TILE), -1};
-    int c[32];
+    const int at0 = a - rows + (warp > 0 ? scan_rows[warp - 1] : 0);
+    const int tile0 = b - nt + (warp > 0 ? scan_tiles[warp - 1] : 0), adapter = tid < slots ? tid : -1;
+    for (int i = block; i < large; i += BLOCKS) tiles[(tile0 >> 12) + i] = LqAdTile{adapter, at0 + i * LQ_AD_TILE, min(LQ_AD_TILE, rows - i * LQ_AD_TILE), -1};
+    for (int i = block; i < little; i += BLOCKS)
+      small[(tile0 & 0xFFF) + i] = LqAdTile{adapter, at0 + i * LQ_AD_SMALL_TILE, min(LQ_AD_SMALL_TILE, rows - i * LQ_AD_SMALL_TILE), -1};
+    int c[32], at = at0 + before;
 #pragma unroll
     for (int w = 0; w < 32; ++w) c[w] = w < warps ? count[w * bins + tid] : 0;
 #pragma unroll
@@ -113,9 +134,13 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     }
   }
   // large tiles whose rows are neighbours (perm ascends within a tile)
-  if (M <= LQ_AD_SMALL_M_128) return;
-  __syncthreads();
-  for (int i = tid; i < scan_tiles[31] >> 12; i += 1024) {
+  if constexpr (BLOCKS > 1) {
+    cluster_sync();                                            // (and the others have read this block's totals)
+  } else {
+    if (M <= LQ_AD_SMALL_M_128) return;
+    __syncthreads();
+  }
+  for (int i = block * 1024 + tid; i < scan_tiles[31] >> 12; i += 1024 * BLOCKS) {
     const LqAdTile t = tiles[i];
     const int r = perm[t.begin];
     if (perm[t.begin + t.rows - 1] - r == t.rows - 1) tiles[i].first = r;
@@ -148,8 +173,12 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The order of a product's inner index is free as long as both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7
-// of each 32, so that a fragment of either operand is one 16-byte load from rows that run along the inner index.
+// The forward for few rows: a cluster of CTAs has 16 rows of one adapter, shares out K for the first product, joins the sums through distributed shared memory
+// (each CTA all of them, always in the same order) and shares out the columns for the second.  A chain of latencies: one launch, and operands straight from
+// global memory into the fragments of mma.sync (tiles of 16 rows would leave tcgen05's 128 empty).  The order of a product's inner index is free as long as
+// both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7 of each 32, so that a fragment of either operand is one 16-byte load from
+// rows that run along the inner index.  us with the map: one row, 1152 x 1152, rank 16 7.3; 64 rows with an adapter each, 1152 x 4608, rank 32 15.4 (25 MB of factors:
+// 3.8 at the measured copy rate); of these 3.4 are the map.  (The next columns' B loaded ahead: registers spill, 22.7 for 15.0.)
 template <int RP, int CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, const int* perm, const __half* X, const void* Y0,
                                                                  void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad,
@@ -424,7 +453,8 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
   const auto room = [](auto* kernel, int rp) {
     return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(rp))) == cudaSuccess;
   };
-  if (lq_note_cuda(cudaFuncSetAttribute(lq_rowmap_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * (MAX_SLOTS + 1) * 4)) != cudaSuccess ||
+  if (lq_note_cuda(cudaFuncSetAttribute(lq_rowmap_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * (MAX_SLOTS + 1) * 4)) != cudaSuccess ||
+      lq_note_cuda(cudaFuncSetAttribute(lq_rowmap_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * (MAX_SLOTS + 1) * 4)) != cudaSuccess ||
       !room(lq_adapters_kernel<16, 8>, 16) || !room(lq_adapters_kernel<16, 4>, 16) ||
       !room(lq_adapters_kernel<32, 8>, 32) || !room(lq_adapters_kernel<32, 4>, 32) ||
       !room(lq_adapters_kernel<64, 8>, 64) || !room(lq_adapters_kernel<64, 4>, 64) ||
@@ -449,7 +479,11 @@ extern "C" lq_status lq_rowmap_set(lq_rowmap* R, const int32_t* ids, int32_t M, 
   if (!R || !ids || M <= 0 || M > R->M_max || ((uintptr_t)ids & 3) != 0) return LQ_ERR_INVALID_ARG;
   LqDeviceGuard guard(R->device);
   if (!guard.ok) return LQ_ERR_CUDA;
-  const cudaError_t e = lq_launch(lq_rowmap_kernel, 1, 1024, (size_t)32 * (R->slots + 1) * 4, (cudaStream_t)stream, ids, M, R->slots, R->d_perm, R->d_tiles, R->d_small, R->d_ntiles);
+  const size_t smem = (size_t)32 * (R->slots + 1) * 4;
+  const auto launch = [&](auto* kernel, int blocks) {
+    return lq_launch_cluster(kernel, blocks, 1024, blocks, smem, (cudaStream_t)stream, ids, M, R->slots, R->d_perm, R->d_tiles, R->d_small, R->d_ntiles);
+  };
+  const cudaError_t e = M > ROWMAP_SINGLE ? launch(lq_rowmap_kernel<8>, 8) : launch(lq_rowmap_kernel<1>, 1);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
   R->M = M;
   return LQ_OK;
