@@ -272,13 +272,14 @@ lq_status lq_adapters_set(lq_adapters* set, int32_t slot, int32_t rank, const vo
                           void* cuda_stream);
 
 /* A map of up to M_max rows to the slots 0 .. slots - 1 (1 <= slots <= 1023, M_max <= 2^24), with the workspace of the forwards
- * that use it (synchronous). */
+ * that use it (synchronous): 4 bytes a row, and 516 more where M_max > 16. */
 lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, lq_rowmap** out);
 lq_status lq_rowmap_free(lq_rowmap* map);
 
 /* Sorts the rows by adapter (stable; on the device, so a captured graph sorts anew on each replay what the array then holds).
  *   row_adapter_dev  [M] int32, device: the slot of each row; anything outside 0 .. slots - 1 means none
- *   M                1 <= M <= M_max; the rows of every forward until the next call
+ *   M                1 <= M <= M_max; the rows of every forward until the next call.  A replayed graph that sorts leaves its own rows in the map: a forward
+ *                    of another M behind it needs a call before it (without one it writes nothing, and lq_get_device_status says INVALID_ARG)
  * Asynchronous on `cuda_stream`. */
 lq_status lq_rowmap_set(lq_rowmap* map, const int32_t* row_adapter_dev, int32_t M, void* cuda_stream);
 
@@ -287,7 +288,7 @@ lq_status lq_rowmap_set(lq_rowmap* map, const int32_t* row_adapter_dev, int32_t 
  *   X_f16_dev  [M][K] row-major half, device, 16-byte aligned, finite
  *   Y0_dev     [M][N] row-major half or float per `dtype`, device, 16-byte aligned: the projection's output
  *   Y_dev      the same shape and type: Y0_dev itself (rows without an adapter are then left alone) or memory apart from it
- *              and from X
+ *              (INVALID_ARG where they overlap otherwise), and apart from X
  * The map's slots must not be more than the set's, and map and set must be on one device.  No sum depends on the order of execution, so
  * equal calls give equal bits; a row may differ by rounding between calls of other M or other maps.
  * Calls that use one map, lq_rowmap_set among them, share its workspace: they must not overlap on the GPU (one stream, or events;
@@ -330,9 +331,9 @@ lq_status lq_rope_free(lq_rope* rope);
 typedef struct {
   const void* in;                          /* device, 16-byte aligned; half or float per in_dtype                     */
   void* out;                               /* device, 16-byte aligned; half or float per out_dtype; `in` itself, with its strides and
-                                              type, or memory apart from all inputs                                   */
+                                              type (INVALID_ARG otherwise), or memory apart from all inputs           */
   int64_t in_seq, in_row, in_head;         /* strides in elements, multiples of 8, below 2^31, a head's below 2^26 (the memory they span may be larger) */
-  int64_t out_seq, out_row, out_head;
+  int64_t out_seq, out_row, out_head;      /* no two outputs on one place; may be negative, like those of `in`        */
   const float* weight;                     /* [head_dim] device, 16-byte aligned, or NULL (ones); NULL without a norm */
   const float* bias;                       /* [head_dim] device, 16-byte aligned, or NULL (zeros); LQ_NORM_LAYER only */
   int32_t heads;                           /* 1 .. 4096                                                               */
@@ -381,7 +382,7 @@ lq_status lq_qkv_forward(const lq_layer* layer, lq_act* act, const void* X_f16_d
 lq_status lq_act_export(const lq_act* act, int8_t* qx, uint16_t* sx, int8_t* qb, float* sXb,
                         void* tq, float* sT, void* cuda_stream);
 
-/* Status word the kernels write when a bounded wait expires: code is an lq_status
+/* Status word the kernels write when a bounded wait expires (or a map holds other rows than its forward's): code is an lq_status
  * (LQ_OK if none), stage identifies the waiting role.  Reading clears it.  Synchronises
  * the device. */
 lq_status lq_get_device_status(int device, int32_t* code, int32_t* stage);

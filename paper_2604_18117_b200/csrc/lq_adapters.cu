@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     scan_rows[lane] = u; scan_tiles[lane] = v;
   }
   __syncthreads();
-  if (tid == 0 && block == 0) { ntiles[0] = scan_tiles[31] >> 12; ntiles[1] = scan_tiles[31] & 0xFFF; }
+  if (tid == 0 && block == 0) *reinterpret_cast<int4*>(ntiles) = make_int4(scan_tiles[31] >> 12, scan_tiles[31] & 0xFFF, M, 0);
   if (tid < bins) {
     const int at0 = a - rows + (warp > 0 ? scan_rows[warp - 1] : 0);
     const int tile0 = b - nt + (warp > 0 ? scan_tiles[warp - 1] : 0), adapter = tid < slots ? tid : -1;
@@ -180,7 +180,7 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
 // rows that run along the inner index.  us with the map: one row, 1152 x 1152, rank 16 7.3; 64 rows with an adapter each, 1152 x 4608, rank 32 15.4 (25 MB of factors:
 // 3.8 at the measured copy rate); of these 3.4 are the map.  (The next columns' B loaded ahead: registers spill, 22.7 for 15.0.)
 template <int RP, int CLUSTER>
-__global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, const int* perm, const __half* X, const void* Y0,
+__global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, int M, int32_t* status, const int* perm, const __half* X, const void* Y0,
                                                                  void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad,
                                                                  int out_f32) {
   constexpr int NT = RP / 8, KB = (RP + 31) / 32;
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) l
   grid_dependency_wait();
   // (a tile behind the last one holds anything: it is asked for together with their number, which saves a trip)
   const LqAdTile tile = tiles[ti];
-  if (ti >= *ntiles) return;                              // (the whole cluster)
+  if (ti >= lq_ad_tiles_of<true>(ntiles, M, status)) return;            // (the whole cluster)
   const LqAdMeta m = tile.adapter >= 0 ? meta[tile.adapter] : LqAdMeta{0, 0.f};
   const int unit = warp * CLUSTER + rank_in_cluster, units = WARPS * CLUSTER;
   const bool has0 = g < tile.rows, has1 = g + 8 < tile.rows;
@@ -345,7 +345,7 @@ size_t forward_smem(int rp) {
 template <int RP, int CLUSTER>
 cudaError_t launch_cluster(const lq_adapters* S, const lq_rowmap* R, int tiles, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
   return lq_launch_cluster(lq_adapters_kernel<RP, CLUSTER>, tiles * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st, (const LqAdTile*)R->d_small,
-                           (const int*)R->d_ntiles + 1, (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up,
+                           (const int*)R->d_ntiles, R->M, lq_device_status_ptr(R->device), (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up,
                            (const LqAdMeta*)S->d_meta, S->K, S->N, S->Npad, dt == LQ_OUT_F32 ? 1 : 0);
 }
 template <int RP>
@@ -427,7 +427,7 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
   const size_t rows = M_max > LQ_AD_SMALL_M_128 ? (size_t)M_max + LQ_AD_TILE : 0;
   const size_t large = (size_t)lq_ceil_div(M_max, LQ_AD_TILE) + slots + 1, little = (size_t)lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M), LQ_AD_SMALL_TILE) + slots + 1;
   if (lq_note_cuda(cudaDeviceGetAttribute(&R->sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, 2 * sizeof(int))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, sizeof(int4))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_tiles, large * sizeof(LqAdTile))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_small, little * sizeof(LqAdTile))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_perm, (size_t)M_max * sizeof(int))) != cudaSuccess ||
@@ -436,9 +436,10 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
     lq_rowmap_free(R);
     return LQ_ERR_ALLOC;
   }
-  // (T's rows are read in whole tiles: from defined contents on)
+  // (no rows yet; T's rows are read in whole tiles: from defined contents on)
   lq_status s;
-  if (rows > 0 && (lq_note_cuda(cudaMemset(R->d_T, 0, rows * LQ_AD_TROW * 2)) != cudaSuccess || lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess)) {
+  if (lq_note_cuda(cudaMemset(R->d_ntiles, 0, sizeof(int4))) != cudaSuccess ||
+      (rows > 0 && lq_note_cuda(cudaMemset(R->d_T, 0, rows * LQ_AD_TROW * 2)) != cudaSuccess) || lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess) {
     lq_rowmap_free(R);
     return LQ_ERR_CUDA;
   }
@@ -494,6 +495,8 @@ extern "C" lq_status lq_adapters_forward(const lq_adapters* S, const lq_rowmap* 
   if (S->device != R->device || R->slots > S->slots || R->M <= 0) return LQ_ERR_INVALID_ARG;
   if (dt != LQ_OUT_F16 && dt != LQ_OUT_F32) return LQ_ERR_INVALID_ARG;
   if ((((uintptr_t)X | (uintptr_t)Y0 | (uintptr_t)Y) & 15) != 0) return LQ_ERR_INVALID_ARG;
+  const size_t y_bytes = (size_t)R->M * S->N * (dt == LQ_OUT_F32 ? 4 : 2);
+  if ((Y0 != Y && lq_overlap(Y0, y_bytes, Y, y_bytes)) || lq_overlap(X, (size_t)R->M * S->K * 2, Y, y_bytes)) return LQ_ERR_INVALID_ARG;
   LqDeviceGuard guard(S->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;

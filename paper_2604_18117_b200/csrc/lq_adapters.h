@@ -32,7 +32,7 @@ struct lq_adapters {
 };
 struct lq_rowmap {
   int M_max, slots, device, M, sms;
-  int* d_ntiles;                       // [2]: tiles of 128 rows, of 16
+  int* d_ntiles;                       // [4]: tiles of 128 rows, of 16, rows that were sorted, 0
   LqAdTile *d_tiles, *d_small;         // (tiles of 16 rows only up to LQ_AD_SMALL_M rows)
   int* d_perm;                         // [M_max]
   __half* d_T;                         // [M_max + 128][LQ_AD_TROW], in the order of perm (only where M_max can have the large form)
@@ -47,6 +47,16 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
 lq_status lq_adapters_tiles_prepare();   // once for each device that a map is made on, with that device current
 
 #ifdef __CUDACC__
+// The tiles (of 128 rows, or of 16) of a forward of M rows.  None where the map holds other rows by now, so that no row behind the forward's is touched: a graph that
+// sorts was replayed between, or was captured and not yet replayed.  A forward that finds that says so in the status word.
+template <bool SMALL>
+__device__ __forceinline__ int lq_ad_tiles_of(const int* d_ntiles, int M, int32_t* status) {
+  const int4 n = *reinterpret_cast<const int4*>(d_ntiles);
+  if (n.z == M) return SMALL ? n.y : n.x;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && atomicCAS(status, 0, (int)LQ_ERR_INVALID_ARG) == 0) status[1] = LQ_STAGE_NONE;
+  return 0;
+}
+
 // The power of two that brings a row's largest magnitude to [2^14, 2^15): no half overflows, and hi + lo keep 22 bits of it.
 __device__ __forceinline__ int lq_ad_exponent(float top) {
   int e = 0;

@@ -75,7 +75,7 @@ struct DownParams {
   __half* T;
   float* rscale;
   int32_t* status;
-  int rp, k_stages, ring, tmem_cols;
+  int rp, k_stages, ring, tmem_cols, M;
 };
 
 // One tile a cluster, K / (64 SPLIT) stages a CTA.  Warp 0 fetches, warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
 
   // (a tile behind the last one holds anything: it is asked for together with their number, which saves a trip)
   LqAdTile tile = p.tiles[ti];
-  if (ti >= *p.ntiles) tile.adapter = -1;
+  if (ti >= lq_ad_tiles_of<false>(p.ntiles, p.M, p.status)) tile.adapter = -1;
   if (tile.adapter >= 0) {                                // (the same for the whole cluster)
     const int k0 = part * p.k_stages / SPLIT, n = (part + 1) * p.k_stages / SPLIT - k0;
     const float scale = p.meta[tile.adapter].scale;
@@ -240,7 +240,7 @@ struct UpParams {
   const float* rscale;
   void* Y;
   int32_t* status;
-  int N, Npad, chunks, in_place;
+  int N, Npad, chunks, in_place, M;
 };
 
 // Persistent, one CTA an SM: the steps (tile, 128 columns) of all tiles are cut into runs of like length.  Warp 0 fetches a tile's T (both halves) and each
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
   // are waited for (and every CTA waits, so that who waits for this kernel has waited for that one).
   if (warp == 3) grid_dependency_wait();
 
-  const int ntiles = *p.ntiles;
+  const int ntiles = lq_ad_tiles_of<false>(p.ntiles, p.M, p.status);
   const long long total = (long long)ntiles * p.chunks;
   const long long lo = total * blockIdx.x / gridDim.x, hi = total * (blockIdx.x + 1) / gridDim.x;
   const int n = (int)(hi - lo), ti0 = (int)(lo / p.chunks), ch0 = (int)(lo - (long long)ti0 * p.chunks);
@@ -551,7 +551,7 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
   if ((s = rows_of(&tmX, X, (uint64_t)S->K * 2)) != LQ_OK || (s = rows_of(&tmY, Y0, (uint64_t)S->N * (dt == LQ_OUT_F32 ? 4 : 2))) != LQ_OK) return s;
   int32_t* status = lq_device_status_ptr(S->device);
   if (!status) return LQ_ERR_CUDA;
-  DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, S->rp, lq_ceil_div(S->K, 64), 1, 32};
+  DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, S->rp, lq_ceil_div(S->K, 64), 1, 32, R->M};
   // K is shared by as many CTAs as fill the SMs twice over, each with at least two stages
   const int tiles = lq_ceil_div(R->M, BM);
   int split = 1;
@@ -561,7 +561,7 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
                   : split == 4 ? launch_down<4>(S, R, tmX, d, st)
                                : launch_down<8>(S, R, tmX, d, st);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
-  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y};
+  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y, R->M};
   if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, tmY, u, st) : launch_up<true, 2>(S, R, tmY, u, st);
   else e = S->rp <= 64 ? launch_up<false, 1>(S, R, tmY, u, st) : launch_up<false, 2>(S, R, tmY, u, st);
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;

@@ -755,6 +755,7 @@ extern "C" lq_status lq_qkv_forward(const lq_layer* L, lq_act* A, const void* X,
   if (S && (S->K != L->K || S->N != L->N || S->device != L->device || R->device != L->device || R->M != M || R->slots > S->slots)) return LQ_ERR_INVALID_ARG;
   const int D = c->head_dim, rows = M / c->sequences;
   const size_t esz = dt == LQ_OUT_F32 ? 4 : 2;
+  if (S && lq_overlap(X, (size_t)M * L->K * 2, Y, (size_t)M * L->N * esz)) return LQ_ERR_INVALID_ARG;      // X is read again behind the GEMM
   void* Yk = (uint8_t*)Y + (size_t)c->q_heads * D * esz;
   const int64_t seq = (int64_t)rows * L->N;
   const lq_heads q = {Y, Y, seq, L->N, D, seq, L->N, D, c->q_weight, c->q_bias, c->q_heads};

@@ -341,8 +341,13 @@ cudaError_t launch(HeadsParams& p, cudaStream_t st) {
   if (p.heads[0] > 0 && p.heads[1] > 0) walk = std::min(walk, std::max(4 * g, std::min(p.heads[0], p.heads[1])));
   const auto parts = [&](int w) { return (p.heads[0] + w - 1) / w + (p.heads[1] + w - 1) / w; };
   walk = lq_round_up(walk, g);
-  while (walk > g && (long long)p.rows * parts(walk) < fill) walk -= g;
-  p.walk = walk;
+  int low = 1, high = walk / g;                           // the longest walk, in steps, that fills, or one
+  while (low < high) {
+    const int mid = (low + high + 1) / 2;
+    if ((long long)p.rows * parts(mid * g) < fill) high = mid - 1;
+    else low = mid;
+  }
+  p.walk = walk = low * g;
   for (int i = 0; i < 2; ++i) p.parts[i] = (p.heads[i] + walk - 1) / walk;
   const int n = p.parts[0] + p.parts[1];
   p.block_rows = std::max(1, std::min(MAX_ROWS, p.rows / (fill / WARPS)));
@@ -380,7 +385,7 @@ cudaError_t launch_norm(HeadsParams& p, int norm, int rot, cudaStream_t st) {
 }
 
 // Strides over dimensions of one entry mean nothing; the others keep entries on 16-byte boundaries, and no two outputs on one place.
-lq_status take_side(const lq_heads* h, int sequences, int seq_len, lq_norm norm, Side* s) {
+lq_status take_side(const lq_heads* h, int head_dim, int sequences, int seq_len, lq_norm norm, bool same_type, Side* s) {
   if (!h->in || !h->out || h->heads < 1) return LQ_ERR_INVALID_ARG;
   if (h->heads > 4096) return LQ_ERR_UNSUPPORTED;
   if ((((uintptr_t)h->in | (uintptr_t)h->out | (uintptr_t)h->weight | (uintptr_t)h->bias) & 15) != 0) return LQ_ERR_INVALID_ARG;
@@ -394,7 +399,10 @@ lq_status take_side(const lq_heads* h, int sequences, int seq_len, lq_norm norm,
   for (int i : {2, 5})                                       // (a warp steps over up to 32 heads)
     if (strides[i] > INT32_MAX / 32 || strides[i] < -(INT32_MAX / 32)) return LQ_ERR_UNSUPPORTED;
   *s = Side{h->in, h->out, (int)strides[0], (int)strides[1], (int)strides[2], (int)strides[3], (int)strides[4], (int)strides[5], h->weight, h->bias};
-  if ((sequences > 1 && s->out_seq == 0) || (seq_len > 1 && s->out_row == 0) || (h->heads > 1 && s->out_head == 0)) return LQ_ERR_INVALID_ARG;
+  const int64_t counts[3] = {sequences, seq_len, h->heads};
+  for (int i = 0; i < 3; ++i)
+    if (counts[i] > 1 && strides[3 + i] < head_dim && strides[3 + i] > -head_dim) return LQ_ERR_INVALID_ARG;
+  if (h->in == h->out && (!same_type || strides[0] != strides[3] || strides[1] != strides[4] || strides[2] != strides[5])) return LQ_ERR_INVALID_ARG;
   return LQ_OK;
 }
 
@@ -483,8 +491,10 @@ lq_status lq_heads_run(const lq_heads* q, const lq_heads* k, int32_t head_dim, i
   if (rows > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
   HeadsParams p = {};
   lq_status s;
-  if (q && (s = take_side(q, sequences, seq_len, norm, &p.side[0])) != LQ_OK) return s;
-  if (k && (s = take_side(k, sequences, seq_len, norm, &p.side[1])) != LQ_OK) return s;
+  const lq_heads* both[2] = {q, k};
+  for (int i = 0; i < 2; ++i)
+    if (both[i] && (s = take_side(both[i], head_dim, sequences, seq_len, norm, in_dtype == out_dtype, &p.side[i])) != LQ_OK) return s;
+  if (q && k && q->out == k->out) return LQ_ERR_INVALID_ARG;
   p.heads[0] = q ? q->heads : 0;
   p.heads[1] = k ? k->heads : 0;
   p.rows = (int)rows;

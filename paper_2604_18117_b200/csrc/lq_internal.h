@@ -173,6 +173,11 @@ struct LqDeviceGuard {
   LqDeviceGuard& operator=(const LqDeviceGuard&) = delete;
 };
 
+// whether two ranges of memory share a byte
+static inline bool lq_overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
 // device status word (one per device, allocated on first use): {code, stage}
 int32_t* lq_device_status_ptr(int device);
 

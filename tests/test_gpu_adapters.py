@@ -309,3 +309,100 @@ def test_refusals():
     for r in (m, big):
         B.lq_rowmap_free(r)
     S.free()
+
+
+@pytest.mark.parametrize("M,other", [(40, 100), (2000, 2500)])
+def test_a_map_that_a_replayed_graph_has_set_is_not_another_forwards(M, other):
+    """The rows of a map are those of the call that ran last on the device; a forward of another number writes nothing and says so."""
+    import torch
+    rng = np.random.default_rng(7)
+    K, N = 64, 64
+    S = Set(rng, K, N, 16, [16, 8])
+    m = B.lq_rowmap_create(other, 2, 0)
+    ids = torch.arange(other, dtype=torch.int32, device="cuda") % 2
+    X, Y0 = inputs(rng, other, K, N, False)
+    x, y0, y = torch.from_numpy(X).cuda(), torch.from_numpy(Y0).cuda(), torch.full((other, N), 5.0, dtype=torch.float16, device="cuda")
+    side = torch.cuda.Stream()
+    forward_ = lambda: B.lq_adapters_forward(S.h, m, x.data_ptr(), y0.data_ptr(), y.data_ptr(), B.OUT_F16, side.cuda_stream)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):             # captured, not run: the map has no rows yet
+        B.lq_rowmap_set(m, ids.data_ptr(), other, torch.cuda.current_stream().cuda_stream)
+    for replay in (False, True):
+        if replay:
+            B.lq_rowmap_set(m, ids.data_ptr(), M, side.cuda_stream)
+            side.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+        forward_()
+        torch.cuda.synchronize()
+        assert (y == 5).all() and B.lq_get_device_status(0)[0] == 1 and B.lq_get_device_status(0)[0] == 0
+    B.lq_rowmap_set(m, ids.data_ptr(), M, side.cuda_stream)
+    forward_()
+    torch.cuda.synchronize()
+    ref, bound = reference(S, X[:M], Y0[:M], np.arange(M) % 2, False)
+    assert (np.abs(y.cpu().numpy()[:M] - ref) <= bound).all() and (y[M:] == 5).all() and B.lq_get_device_status(0)[0] == 0
+    del graph
+    B.lq_rowmap_free(m)
+    S.free()
+
+
+def test_outputs_that_share_memory_with_inputs_are_refused():
+    import torch
+    S = Set(np.random.default_rng(8), 64, 64, 8, [8])
+    m = B.lq_rowmap_create(32, 1, 0)
+    B.lq_rowmap_set(m, torch.zeros(32, dtype=torch.int32, device="cuda").data_ptr(), 32, 0)
+    torch.cuda.synchronize()
+    t = torch.zeros(3 * 32 * 64, dtype=torch.float16, device="cuda")
+    at = lambda row: t.data_ptr() + row * 128
+    st = torch.cuda.current_stream().cuda_stream
+    for x, y0, y in ((0, 32, 33), (0, 33, 32), (0, 32, 63), (0, 32, 0), (0, 64, 31), (32, 64, 1)):
+        with pytest.raises(B.LqError) as e:
+            B.lq_adapters_forward(S.h, m, at(x), at(y0), at(y), B.OUT_F16, st)
+        assert e.value.code == 1, (x, y0, y)
+    B.lq_adapters_forward(S.h, m, at(0), at(32), at(64), B.OUT_F16, st)
+    B.lq_adapters_forward(S.h, m, at(0), at(32), at(32), B.OUT_F16, st)
+    B.lq_adapters_forward(S.h, m, at(0), at(0), at(32), B.OUT_F16, st)
+    torch.cuda.synchronize()
+    B.lq_rowmap_free(m)
+    S.free()
+
+
+@pytest.mark.parametrize("rank,max_rank", [(8, 8), (30, 128)])
+def test_outputs_behind_four_billion_elements(rank, max_rank):
+    """Rows whose elements lie behind 2^32 of them, neighbours and scattered, in place."""
+    import torch
+    rng = np.random.default_rng(9)
+    K, N, M = 8, 8192, (1 << 19) + 777
+    S = Set(rng, K, N, max_rank, [rank, rank])
+    X = rng.standard_normal((M, K)).astype(np.float16)
+    for scattered in (False, True):
+        ids = np.arange(M) % 3 if scattered else np.arange(M) // 200000
+        look = np.r_[0:5, 199998:200003, 400000 - 3:400003, (1 << 19) - 4:(1 << 19) + 4, M - 300:M]
+        y = torch.empty(M, N, dtype=torch.float16, device="cuda").fill_(0.5)
+        x, i = torch.from_numpy(X).cuda(), torch.from_numpy(ids.astype(np.int32)).cuda()
+        m = B.lq_rowmap_create(M, 2, 0)
+        st = torch.cuda.current_stream().cuda_stream
+        B.lq_rowmap_set(m, i.data_ptr(), M, st)
+        B.lq_adapters_forward(S.h, m, x.data_ptr(), y.data_ptr(), y.data_ptr(), B.OUT_F16, st)
+        torch.cuda.synchronize()
+        ref, bound = reference(S, X[look], np.full((look.size, N), 0.5, np.float16), ids[look], False)
+        got = y[torch.from_numpy(look).cuda()].cpu().numpy()
+        assert (np.abs(got - ref) <= bound).all()
+        assert bool((y[i == 2] == 0.5).all()) and bool((y[i < 2] != 0.5).any(1).all())
+        del y
+        B.lq_rowmap_free(m)
+    assert B.lq_get_device_status(0)[0] == 0
+    S.free()
+
+
+def test_a_thousand_slots_of_which_few_are_used():
+    rng = np.random.default_rng(10)
+    S = Set(rng, 128, 136, 16, [16, 8, 5], slots=1023)
+    for M in (1, 130, 1537, 9000):
+        X, Y0 = inputs(rng, M, 128, 136, False)
+        ids = rng.integers(-1, 3, M)
+        Y = forward(S, ids, X, Y0, False, slots=1023)
+        ref, bound = reference(S, X, Y0, ids, False)
+        assert (np.abs(Y - ref) <= bound).all(), M
+    S.free()

@@ -236,3 +236,56 @@ def test_refusals():
     torch.cuda.synchronize()
     B.lq_rope_free(rope)
     B.lq_rope_free(none)
+
+
+def test_outputs_on_one_place_and_other_ways_in_place_are_refused():
+    import torch
+    x = torch.zeros(1 << 14, dtype=torch.float16, device="cuda")
+    P = x.data_ptr()
+    none = B.lq_rope_create(B.lq_rope_config_default([]), 0)
+
+    def code(q, k=None, fin=0, fout=0, Bn=2):
+        try:
+            B.lq_qk_norm_rope(B.lq_heads(*q), B.lq_heads(*k) if k else None, 64, Bn, 4, B.NORM_RMS, 1e-6, none, None, fin, fout, 0)
+        except B.LqError as e:
+            return e.code
+        return 0
+
+    good, far = (512, 128, 64), P + 16384
+    assert code((P, good, far, good, 2)) == 0 and code((P, good, P, good, 2)) == 0 and code((P, good, far, (64, 256, 128), 2), Bn=1) == 0
+    for bad in ((512, 128, 56), (512, 128, -56), (512, 56, 128), (56, 128, 64)):
+        assert code((P, good, far, bad, 2)) == 1, bad
+    assert code((P, good, P, (512, 128, 72), 2)) == 1 and code((P, good, P, good, 2), fout=1) == 1 and code((P, good, P, good, 2), fin=1) == 1
+    assert code((P, good, far, good, 1), (P + 128, good, far, good, 1)) == 1
+    torch.cuda.synchronize()
+    B.lq_rope_free(none)
+
+
+@pytest.mark.parametrize("norm", ["none", "rms"])
+def test_strides_backwards_and_far_apart(norm):
+    """Rows in the opposite order, heads too, and sequences of outputs 2^30 elements and more apart."""
+    import torch
+    rng = np.random.default_rng(11)
+    Bn, S, h, D = 4, 5, 3, 64
+    x = rng.standard_normal((Bn, S, h, D)).astype(np.float16)
+    pos = rng.integers(0, 1000, (Bn, S, 1)).astype(np.int32)
+    axis, freq = frequencies([D], 10000.0, False)
+    rope = B.lq_rope_create(B.lq_rope_config_default([D]), 0)
+    xd, pd = torch.from_numpy(x).cuda(), torch.from_numpy(pos).cuda()
+    apart = 1 << 30
+    out = torch.empty(3 * apart + S * h * D, dtype=torch.float16, device="cuda")
+    last = (S - 1) * h * D + (h - 1) * D                   # the place of the first row's first head
+    side = B.lq_heads(xd.data_ptr(), (S * h * D, h * D, D), out.data_ptr() + 2 * last, (apart, -h * D, -D), h)
+    B.lq_qk_norm_rope(side, None, D, Bn, S, NORMS[norm], 1e-6, rope, pd.data_ptr(), B.OUT_F16, B.OUT_F16, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    ref, bound = reference(x, None, None, norm, 1e-6, axis, freq, False, pos, False)
+    for b in range(Bn):
+        got = out[b * apart:b * apart + S * h * D].view(S, h, D).flip(0, 1).float().cpu().numpy()
+        assert (np.abs(got - ref[b]) <= bound[b]).all(), b
+    B.lq_rope_free(rope)
+
+
+def test_the_most_heads_of_the_longest():
+    for norm in ("rms", "layer"):
+        Case(1, 1, 4095, 7, 256, norm, (256,)).run()
+        Case(1, 3, 1, 4096, 8, norm, (8,), halves=True).run()

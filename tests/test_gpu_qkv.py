@@ -198,3 +198,18 @@ def test_refusals():
     torch.cuda.synchronize()
     assert B.lq_get_device_status(0)[0] == 0
     b.free()
+
+
+def test_inputs_that_share_memory_with_outputs_under_adapters():
+    import torch
+    b = Block(64, 2, False)
+    B.lq_rowmap_set(b.map, b.i.data_ptr(), 64, 0)
+    torch.cuda.synchronize()
+    b.y[0].fill_(3.0)
+    c = B.lq_qkv(b.D, b.hq, b.hk, b.seqs, B.NORM_RMS, 1e-6, b.rope, b.p.data_ptr())
+    with pytest.raises(B.LqError) as e:
+        B.lq_qkv_forward(b.h, b.act, b.y[0].data_ptr(), 64, b.set, b.map, c, b.y[0].data_ptr(), b.code, 0)
+    assert e.value.code == 1
+    torch.cuda.synchronize()
+    assert (b.y[0] == 3).all()
+    b.free()
