@@ -78,7 +78,7 @@ struct DownParams {
   int rp, k_stages, ring, tmem_cols, M;
 };
 
-// One tile a cluster, K / (64 SPLIT) stages a CTA.  Warp 0 fetches, warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial
+// One tile of a cluster at a time, K / (64 SPLIT) stages a CTA.  Warp 0 fetches, warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial
 // sums to shared memory and each CTA adds up 128 / SPLIT rows from all of the cluster, always in the same order.  A short kernel is a chain of latencies:
 // nothing waits for what it does not need (an empty slot's tile is formed like another and left unread), the loads of a row's sums are all in flight
 // together.  (8192 x 1152, rank 32, us from the dependency's end: tile known 0.6, copies asked for 1.5, sums complete 6.4, in shared memory of all 7.5, T written 8.8.)
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int stage_bytes = A_STAGE + p.rp * 128;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int ti = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
+  const int part = blockIdx.x % SPLIT, clusters = gridDim.x / SPLIT;
   auto full = [&](int s) { return smem_u32(&bars[s]); };
   auto empty = [&](int s) { return smem_u32(&bars[MAX_STAGES + s]); };
   const uint32_t done = smem_u32(&bars[2 * MAX_STAGES]);
@@ -112,21 +112,26 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
   grid_launch_dependents();          // (behind the wait: the up kernel counts on what came before this one to be complete when it starts)
 
   // (a tile behind the last one holds anything: it is asked for together with their number, which saves a trip)
-  LqAdTile tile = p.tiles[ti];
-  if (ti >= lq_ad_tiles_of<false>(p.ntiles, p.M, p.status)) tile.adapter = -1;
-  if (tile.adapter >= 0) {                                // (the same for the whole cluster)
-    const int k0 = part * p.k_stages / SPLIT, n = (part + 1) * p.k_stages / SPLIT - k0;
+  LqAdTile tile = p.tiles[blockIdx.x / SPLIT];
+  const int ntiles = lq_ad_tiles_of<false>(p.ntiles, p.M, p.status);
+  const int k0 = part * p.k_stages / SPLIT, n = (part + 1) * p.k_stages / SPLIT - k0;
+  bool ok = true;                                         // (a CTA that has given up still meets the others at their barriers)
+  int used = 0;                                           // stages of the tiles before
+#pragma unroll 1
+  for (int ti = blockIdx.x / SPLIT, turn = 0; ti < ntiles; ti += clusters) {
+    if (ti >= clusters) tile = p.tiles[ti];
+    if (tile.adapter < 0) continue;                       // (the same for the whole cluster)
     const float scale = p.meta[tile.adapter].scale;
-    bool ok = true;
-    if (warp == 0) {
+    if (warp == 0 && ok) {
       const uint32_t bytes = fetch_bytes(tile) + p.rp * 128;
       int4 rows = make_int4(0, 0, 0, 0);
       if (tile.first < 0) rows = tile_rows4(p.perm + tile.begin, tile.rows, lane);
-      for (int it = 0; it < n; ++it) {
+      int it = used;
+      for (; it < used + n; ++it) {
         const int s = it % p.ring;
         if (it >= p.ring && !(ok = mbar_wait_warp(empty(s), ((it / p.ring) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
         const uint32_t a = base + s * stage_bytes;
-        const int x = (k0 + it) * 128;                    // bytes along K
+        const int x = (k0 + it - used) * 128;             // bytes along K
         if (elect_one()) {
           mbar_expect_tx(full(s), bytes);
           tma_load_2d(a + A_STAGE, &tmDown, x, tile.adapter * p.rp, full(s));
@@ -135,26 +140,28 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
         fetch_rows(a, tmX, x, tile, rows, full(s));
       }
       if (!ok)                                            // copies in flight land before the CTA goes
-        for (int it = max(0, n - p.ring); it < n; ++it) mbar_settle(full(it % p.ring), (it / p.ring) & 1);
-    } else if (warp == 1) {
+        for (int i = max(0, it - p.ring); i < it; ++i) mbar_settle(full(i % p.ring), (i / p.ring) & 1);
+    } else if (warp == 1 && ok) {
       const uint32_t idesc = IDESC_F16 | idesc_shape(p.rp);
-      for (int it = 0; it < n; ++it) {
+      for (int it = used; it < used + n; ++it) {
         const int s = it % p.ring;
         if (!(ok = mbar_wait_warp(full(s), (it / p.ring) & 1, &abort_flag, p.status, LQ_STAGE_MMA))) break;
         tc_fence_after();
         const uint64_t a = make_smem_desc(base + s * stage_bytes), b = make_smem_desc(base + s * stage_bytes + A_STAGE);
         if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) tc_mma<TC_F16>(tmem, a + 2 * k, b + 2 * k, idesc, (it | k) != 0);
+          for (int k = 0; k < 4; ++k) tc_mma<TC_F16>(tmem, a + 2 * k, b + 2 * k, idesc, it > used || k != 0);
           tc_commit(empty(s));
-          if (it + 1 == n) tc_commit(done);
+          if (it + 1 == used + n) tc_commit(done);
         }
         __syncwarp();
       }
     }
     __syncwarp();
-    ok = mbar_wait(done, 0, &abort_flag, p.status, LQ_STAGE_DRAIN);
+    if (ok) ok = mbar_wait(done, turn, &abort_flag, p.status, LQ_STAGE_DRAIN);
     ok = __syncthreads_and(ok && !abort_flag) != 0;
+    used += n;
+    turn ^= 1;
     // partial sums -> shared memory, rows 16 bytes longer than they are so that neighbouring rows lie in different banks; the ring is free: the MMAs
     // have read it
     const int pitch = p.rp + 4;
@@ -216,7 +223,14 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
           }
       }
     }
-    if constexpr (SPLIT > 1) cluster_sync();              // the others have read this CTA's sums
+    // the others have read this CTA's sums; what follows may write over them, copies too
+    if (ti + clusters < ntiles) {
+      fence_proxy_async();
+      tc_fence_before();
+      if constexpr (SPLIT == 1) __syncthreads();
+    }
+    if constexpr (SPLIT > 1) cluster_sync();
+    tc_fence_after();
   }
   tc_fence_before();
   __syncthreads();
@@ -519,7 +533,10 @@ cudaError_t launch_down(const lq_adapters* S, const lq_rowmap* R, const RowMaps&
   d.ring = std::min(std::min(MAX_STAGES, most), (DOWN_SMEM - 1024) / stage);
   while (d.tmem_cols < S->rp) d.tmem_cols *= 2;
   const int smem = 1024 + std::max(d.ring * stage, BM * (S->rp + 4) * 4);
-  return lq_launch_cluster(lq_adapters_down_kernel<SPLIT>, lq_ad_tiles(R->M, R->slots, BM) * SPLIT, 32 * DOWN_WARPS, SPLIT, smem, st, tmX, S->tmDown, d);
+  // no more clusters than are resident: with many slots most tiles that there might be are not there (8192 x 1152 x 3456, rank 32, 1023 slots of which eight are used,
+  // us with the map: 61.1 by a cluster for each, 40.4 so)
+  const int tiles = std::min(lq_ad_tiles(R->M, R->slots, BM), std::max(1, 2 * R->sms / SPLIT));
+  return lq_launch_cluster(lq_adapters_down_kernel<SPLIT>, tiles * SPLIT, 32 * DOWN_WARPS, SPLIT, smem, st, tmX, S->tmDown, d);
 }
 
 template <bool F32, int NA>

@@ -406,3 +406,17 @@ def test_a_thousand_slots_of_which_few_are_used():
         ref, bound = reference(S, X, Y0, ids, False)
         assert (np.abs(Y - ref) <= bound).all(), M
     S.free()
+
+
+@pytest.mark.parametrize("M,K,max_rank,used", [(1600, 2048, 16, 300), (1700, 1160, 128, 200), (700, 320, 64, 400), (5000, 640, 40, 600)])
+@pytest.mark.parametrize("none", [False, True])
+def test_more_tiles_than_are_at_work_at_once(M, K, max_rank, used, none):
+    rng = np.random.default_rng(M)
+    N = 72
+    S = Set(rng, K, N, max_rank, [int(r) for r in rng.integers(0, max_rank + 1, used)], slots=used)
+    X, Y0 = inputs(rng, M, K, N, True)
+    ids = rng.integers(-1 if none else 0, used, M)
+    Y = forward(S, ids, X, Y0, True)
+    ref, bound = reference(S, X, Y0, ids, True)
+    assert (np.abs(Y - ref) <= bound).all()
+    S.free()
