@@ -173,16 +173,26 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+template <int BYTES, bool L1 = false>     // L1: a copy takes half of a 32-byte sector and another one the rest (1365 rows, 1160 x 2312, fp32: 20.7 us, without 22.7)
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
+  if constexpr (BYTES == 16 && L1) asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// bytes of a warp's places for what is fetched ahead
+__host__ __device__ constexpr int adapters_stage(int rp, bool f32) { return ((rp <= 32 ? 4 : 0) + (f32 ? 4 : 2)) * 512; }
+
 // The forward for few rows: a cluster of CTAs has 16 rows of one adapter, shares out K for the first product, joins the sums through distributed shared memory
 // (each CTA all of them, always in the same order) and shares out the columns for the second.  A chain of latencies: one launch, and operands straight from
 // global memory into the fragments of mma.sync (tiles of 16 rows would leave tcgen05's 128 empty).  The order of a product's inner index is free as long as
 // both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7 of each 32, so that a fragment of either operand is one 16-byte load from
-// rows that run along the inner index.  us with the map: one row, 1152 x 1152, rank 16 7.3; 64 rows with an adapter each, 1152 x 4608, rank 32 15.4 (25 MB of factors:
-// 3.8 at the measured copy rate); of these 3.4 are the map.  (The next columns' B loaded ahead: registers spill, 22.7 for 15.0.)
-template <int RP, int CLUSTER>
+// rows that run along the inner index.  us with the map: one row, 1152 x 1152, rank 16 7.2; 64 rows with an adapter each, 1152 x 4608, rank 32 14.8 (25 MB of factors:
+// 3.8 at the measured copy rate); of these 3.4 are the map.  The first columns' B and Y0 are on their way during the first product, through shared memory (asked for
+// where they are used 15.3; ahead through registers, which spill, 22.7).
+template <int RP, int CLUSTER, bool F32>
 __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, int M, int32_t* status, const int* perm, const __half* X, const void* Y0,
-                                                                 void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad,
-                                                                 int out_f32) {
+                                                                 void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad) {
   constexpr int NT = RP / 8, KB = (RP + 31) / 32;
   extern __shared__ __align__(16) float smem[];
   float* red = smem;                                      // [WARPS][16][RP]
@@ -201,6 +211,31 @@ __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) l
   const bool has0 = g < tile.rows, has1 = g + 8 < tile.rows;
   const long long row0 = has0 ? perm[tile.begin + g] : 0, row1 = has1 ? perm[tile.begin + g + 8] : 0;
   if (m.rank == 0 && Y == Y0) return;
+  // What the lane adds to and, of narrow factors, its B, for the first columns and then, ahead of the stores, for the next ones, without registers: through places
+  // of shared memory that no other lane looks at.
+  constexpr int YW = F32 ? 2 : 1;                         // 16-byte words of eight columns
+  constexpr bool STAGE_B = RP <= 32;
+  const uint32_t stage = smem_u32(row_scale + 16) + warp * adapters_stage(RP, F32) + lane * 16;
+  const __half* Bu = up + (long long)max(tile.adapter, 0) * Npad * RP;
+  const auto fetch = [&](int cg) {
+    if (cg * 32 >= N) return;
+    if (STAGE_B && m.rank > 0)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const __half* src = Bu + (long long)(32 * cg + 8 * j + g) * RP;
+        if constexpr (RP == 16) cp_async<8>(stage + (2 * YW + j) * 512, src + 4 * t);        // half a block: four neighbours a lane
+        else cp_async<16>(stage + (2 * YW + j) * 512, src + 8 * t);
+      }
+    const int n = 32 * cg + 8 * t;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (n < N && (h ? has1 : has0)) {
+        const unsigned char* src = reinterpret_cast<const unsigned char*>(Y0) + ((h ? row1 : row0) * N + n) * (F32 ? 4 : 2);
+#pragma unroll
+        for (int w = 0; w < YW; ++w) cp_async<16, F32>(stage + (YW * h + w) * 512, src + 16 * w);
+      }
+  };
+  fetch(unit);
 
   float c[NT][4];
   if (m.rank > 0) {
@@ -267,11 +302,12 @@ __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) l
     __syncthreads();
   }
   const float s0 = m.rank > 0 ? row_scale[g] : 0.f, s1 = m.rank > 0 ? row_scale[g + 8] : 0.f;
-  const __half* Bu = up + (long long)max(tile.adapter, 0) * Npad * RP;
   for (int cg = unit; cg * 32 < N; cg += units) {
     float d[4][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
+    const int n = 32 * cg + 8 * t;                        // this lane's eight columns
+    cp_async_wait();
     if (m.rank > 0) {
 #pragma unroll
       for (int q = 0; q < KB; ++q)
@@ -279,13 +315,8 @@ __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) l
           uint4 b[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const __half* src = Bu + (long long)(32 * cg + 8 * j + g) * RP + 32 * q;
-            if constexpr (RP == 16) {                     // half a block: four neighbours a lane
-              const uint2 v = *reinterpret_cast<const uint2*>(src + 4 * t);
-              b[j] = make_uint4(v.x, v.y, 0, 0);
-            } else {
-              b[j] = *reinterpret_cast<const uint4*>(src + 8 * t);
-            }
+            if constexpr (STAGE_B) b[j] = lds_v4(stage + (2 * YW + j) * 512);
+            else b[j] = *reinterpret_cast<const uint4*>(Bu + (long long)(32 * cg + 8 * j + g) * RP + 32 * q + 8 * t);
           }
 #pragma unroll
           for (int part_of = 0; part_of < 2; ++part_of) {
@@ -306,47 +337,48 @@ __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) l
           }
         }
     }
-    const int n = 32 * cg + 8 * t;                        // this lane's eight columns
-    if (n < N)
+    uint4 y[2][YW];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (h ? has1 : has0) {
-          const long long at = (h ? row1 : row0) * N + n;
-          const float s = h ? s1 : s0;
-          if (out_f32) {
-            const float4* y0 = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(Y0) + at);
-            float4 a = y0[0], b = y0[1];
-            if (m.rank > 0) {                             // (a row without an adapter keeps its bits)
-              a.x = fmaf(s, d[0][2 * h], a.x); a.y = fmaf(s, d[0][2 * h + 1], a.y); a.z = fmaf(s, d[1][2 * h], a.z); a.w = fmaf(s, d[1][2 * h + 1], a.w);
-              b.x = fmaf(s, d[2][2 * h], b.x); b.y = fmaf(s, d[2][2 * h + 1], b.y); b.z = fmaf(s, d[3][2 * h], b.z); b.w = fmaf(s, d[3][2 * h + 1], b.w);
-            }
-            float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(Y) + at);
-            o[0] = a; o[1] = b;
-          } else {
-            uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(Y0) + at);
-            __half2* w = reinterpret_cast<__half2*>(&v);
-            if (m.rank > 0)
+    for (int h = 0; h < 2; ++h) {
+      const float s = h ? s1 : s0;
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float2 f = __half22float2(w[j]);
-                w[j] = __floats2half2_rn(fmaf(s, d[j][2 * h], f.x), fmaf(s, d[j][2 * h + 1], f.y));
-              }
-            *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(Y) + at) = v;
+      for (int w = 0; w < YW; ++w) y[h][w] = lds_v4(stage + (YW * h + w) * 512);
+      if (m.rank > 0) {                                   // (a row without an adapter keeps its bits)
+        if constexpr (F32) {
+          float* f = reinterpret_cast<float*>(&y[h][0]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = fmaf(s, d[j / 2][2 * h + j % 2], f[j]);
+        } else {
+          __half2* w = reinterpret_cast<__half2*>(&y[h][0]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 f = __half22float2(w[j]);
+            w[j] = __floats2half2_rn(fmaf(s, d[j][2 * h], f.x), fmaf(s, d[j][2 * h + 1], f.y));
           }
         }
+      }
+    }
+    fetch(cg + units);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (n < N && (h ? has1 : has0)) {
+        uint4* to = reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(Y) + ((h ? row1 : row0) * N + n) * (F32 ? 4 : 2));
+#pragma unroll
+        for (int w = 0; w < YW; ++w) to[w] = y[h][w];
+      }
   }
   if (m.rank > 0) cluster_wait();                         // the others have read this CTA's share
 }
 
-size_t forward_smem(int rp) {
+size_t forward_smem(int rp, bool f32) {
   const int kb = (rp + 31) / 32;
-  return (size_t)(WARPS + 1) * 16 * rp * 4 + 2 * 16 * kb * 32 * 2 + 16 * 4;
+  return (size_t)(WARPS + 1) * 16 * rp * 4 + 2 * 16 * kb * 32 * 2 + 16 * 4 + (size_t)WARPS * adapters_stage(rp, f32);
 }
 template <int RP, int CLUSTER>
 cudaError_t launch_cluster(const lq_adapters* S, const lq_rowmap* R, int tiles, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
-  return lq_launch_cluster(lq_adapters_kernel<RP, CLUSTER>, tiles * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP), st, (const LqAdTile*)R->d_small,
+  return lq_launch_cluster(dt == LQ_OUT_F32 ? lq_adapters_kernel<RP, CLUSTER, true> : lq_adapters_kernel<RP, CLUSTER, false>, tiles * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP, dt == LQ_OUT_F32), st, (const LqAdTile*)R->d_small,
                            (const int*)R->d_ntiles, R->M, lq_device_status_ptr(R->device), (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up,
-                           (const LqAdMeta*)S->d_meta, S->K, S->N, S->Npad, dt == LQ_OUT_F32 ? 1 : 0);
+                           (const LqAdMeta*)S->d_meta, S->K, S->N, S->Npad);
 }
 template <int RP>
 cudaError_t launch_forward(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
@@ -354,6 +386,11 @@ cudaError_t launch_forward(const lq_adapters* S, const lq_rowmap* R, const void*
   // adapter each, 512 x 8192, rank 64 43.4 / 32.3; one row, 1152 x 3456, rank 32 9.2 / 11.2; two were never better).
   const int tiles = lq_ad_tiles(R->M, R->slots, LQ_AD_SMALL_TILE), resident = (RP <= 32 ? 4 : RP <= 64 ? 3 : 2) * R->sms;
   return 8 * tiles <= resident ? launch_cluster<RP, 8>(S, R, tiles, X, Y0, Y, dt, st) : launch_cluster<RP, 4>(S, R, tiles, X, Y0, Y, dt, st);
+}
+template <int RP, typename Room>
+bool room_of_rank(const Room& room) {
+  return room(lq_adapters_kernel<RP, 8, false>, forward_smem(RP, false)) && room(lq_adapters_kernel<RP, 8, true>, forward_smem(RP, true)) &&
+         room(lq_adapters_kernel<RP, 4, false>, forward_smem(RP, false)) && room(lq_adapters_kernel<RP, 4, true>, forward_smem(RP, true));
 }
 
 }  // namespace
@@ -451,16 +488,11 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
     lq_rowmap_free(R);
     return s;
   }
-  const auto room = [](auto* kernel, int rp) {
-    return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)forward_smem(rp))) == cudaSuccess;
+  const auto room = [](auto* kernel, size_t bytes) {
+    return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes)) == cudaSuccess;
   };
-  if (lq_note_cuda(cudaFuncSetAttribute(lq_rowmap_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * (MAX_SLOTS + 1) * 4)) != cudaSuccess ||
-      lq_note_cuda(cudaFuncSetAttribute(lq_rowmap_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * (MAX_SLOTS + 1) * 4)) != cudaSuccess ||
-      !room(lq_adapters_kernel<16, 8>, 16) || !room(lq_adapters_kernel<16, 4>, 16) ||
-      !room(lq_adapters_kernel<32, 8>, 32) || !room(lq_adapters_kernel<32, 4>, 32) ||
-      !room(lq_adapters_kernel<64, 8>, 64) || !room(lq_adapters_kernel<64, 4>, 64) ||
-      !room(lq_adapters_kernel<96, 8>, 96) || !room(lq_adapters_kernel<96, 4>, 96) ||
-      !room(lq_adapters_kernel<128, 8>, 128) || !room(lq_adapters_kernel<128, 4>, 128)) {
+  if (!room(lq_rowmap_kernel<1>, 32 * (MAX_SLOTS + 1) * 4) || !room(lq_rowmap_kernel<8>, 32 * (MAX_SLOTS + 1) * 4) || !room_of_rank<16>(room) ||
+      !room_of_rank<32>(room) || !room_of_rank<64>(room) || !room_of_rank<96>(room) || !room_of_rank<128>(room)) {
     lq_rowmap_free(R);
     return LQ_ERR_CUDA;
   }

@@ -6,7 +6,7 @@
 #include "lq_internal.h"
 
 // Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows, and one on tiles of 128 rows.  us with the map, K x N and rank, small /
-// large form.  Six requests of neighbouring rows: 1152 x 3456, 32: 600 rows 15.4 / 17, 1400 rows 20.9 / 21, 2048 rows 28.8 / 19.3; 512 x 8192, 64: 250 rows
+// large form.  Six requests of neighbouring rows: 1152 x 3456, 32: 600 rows 15.4 / 17, 1400 rows 18.4 / 21, 2048 rows 28.8 / 19.3; 512 x 8192, 64: 250 rows
 // 19.8 / 15.7; 5600 x 2240, 128: 250 rows 29.2 / 20.2.  Rows in any order, which the large form fetches four at a time: 1160 x 2312, 24, fp32, 1365 rows 20.2 / 36.9.
 // Rows with an adapter each: 512 x 8192, 64: 32 rows 22.0 / 23.8, 64 rows 32.4 / 36.4; 5600 x 2240, 128: 12 rows 27.1 / 22.4, 32 rows 49.5 / 30.7.
 constexpr int LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
