@@ -187,7 +187,7 @@ __host__ __device__ constexpr int adapters_stage(int rp, bool f32) { return ((rp
 // (each CTA all of them, always in the same order) and shares out the columns for the second.  A chain of latencies: one launch, and operands straight from
 // global memory into the fragments of mma.sync (tiles of 16 rows would leave tcgen05's 128 empty).  The order of a product's inner index is free as long as
 // both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7 of each 32, so that a fragment of either operand is one 16-byte load from
-// rows that run along the inner index.  us with the map: one row, 1152 x 1152, rank 16 7.2; 64 rows with an adapter each, 1152 x 4608, rank 32 14.8 (25 MB of factors:
+// rows that run along the inner index.  us with the map: one row, 1152 x 1152, rank 16 7.3; 64 rows with an adapter each, 1152 x 4608, rank 32 15.0 (25 MB of factors:
 // 3.8 at the measured copy rate); of these 3.4 are the map.  The first columns' B and Y0 are on their way during the first product, through shared memory (asked for
 // where they are used 15.3; ahead through registers, which spill, 22.7).
 template <int RP, int CLUSTER, bool F32>
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) l
   const bool has0 = g < tile.rows, has1 = g + 8 < tile.rows;
   const long long row0 = has0 ? perm[tile.begin + g] : 0, row1 = has1 ? perm[tile.begin + g + 8] : 0;
   if (m.rank == 0 && Y == Y0) return;
-  // What the lane adds to and, of narrow factors, its B, for the first columns and then, ahead of the stores, for the next ones, without registers: through places
+  // What the lane adds to and, of narrow factors, its B, for the first columns and then for the next ones, without registers: through places
   // of shared memory that no other lane looks at.
   constexpr int YW = F32 ? 2 : 1;                         // 16-byte words of eight columns
   constexpr bool STAGE_B = RP <= 32;
@@ -358,7 +358,6 @@ __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) l
         }
       }
     }
-    fetch(cg + units);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
       if (n < N && (h ? has1 : has0)) {
@@ -366,6 +365,7 @@ __global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) l
 #pragma unroll
         for (int w = 0; w < YW; ++w) to[w] = y[h][w];
       }
+    fetch(cg + units);                                    // (behind the stores: what is here has been read by then)
   }
   if (m.rank > 0) cluster_wait();                         // the others have read this CTA's share
 }

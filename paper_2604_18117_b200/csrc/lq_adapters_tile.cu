@@ -266,7 +266,11 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
                                                                        const __grid_constant__ RowMaps tmY,
                                                                        const __grid_constant__ UpParams p) {
   constexpr int NT = up_t_bufs(NA), NB = up_b_stages(NA), T_BUF = 2 * NA * PIECE, B_STAGE = NA * PIECE, B_AT = NT * T_BUF, Y_AT = B_AT + NB * B_STAGE;
-  constexpr int YP = F32 ? 4 : 2, Y_READERS = UP_DRAIN_WARPS / YP;      // pieces of a step; warps that read one
+  // Pieces of a step, and warps that wait for one and give it back.  A wait tells a phase from the next one, not from the one after that, so who waits on a place of
+  // the ring has to wait for each of its turns.  With two pieces a step the six places are always read by the same warps.  With four a place's turns would
+  // alternate between two groups of them: every warp waits for all pieces and gives all back.
+  constexpr int YP = F32 ? 4 : 2, Y_READERS = F32 ? UP_DRAIN_WARPS : UP_DRAIN_WARPS / YP;
+  static_assert(F32 || Y_SLOTS % YP == 0, "");
   extern __shared__ unsigned char smem_raw[];
   enum { TFULL = 0, TFREE = NT, BFULL = 2 * NT, BFREE = BFULL + NB, AFULL = BFREE + NB, YFULL = AFULL + 2, AFREE = YFULL + Y_SLOTS, YFREE = AFREE + 2, NBAR = YFREE + Y_SLOTS };
   __shared__ __align__(8) uint64_t bars[NBAR];
@@ -450,14 +454,19 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
       }
       return r;
     };
-    int uses = 0, y_uses = unit;
+    int uses = 0, y_uses = 0;
     Rows r = rows_of(ti0), r_next = {};
     for (int i = 0, ti = ti0, ch = ch0; i < n; ++i) {
       const bool last = ch + 1 == p.chunks;
       if (last && i + 1 < n) r_next = rows_of(ti + 1);
       if (r.rank > 0 || !p.in_place) {
-        const int s = y_uses % Y_SLOTS;
-        if (!mbar_wait_warp(bar(YFULL + s), (y_uses / Y_SLOTS) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN)) break;
+        const int s = (y_uses + unit) % Y_SLOTS;
+        bool landed = true;
+        for (int u = F32 ? 0 : unit; landed && u < (F32 ? YP : unit + 1); ++u) {
+          const int use = y_uses + u;
+          landed = mbar_wait_warp(bar(YFULL + use % Y_SLOTS), (use / Y_SLOTS) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN);
+        }
+        if (!landed) break;
         const int acc = uses & 1;
         if (r.rank > 0) {
           if (!mbar_wait_warp(bar(AFULL + acc), (uses >> 1) & 1, &abort_flag, p.status, LQ_STAGE_DRAIN)) break;
@@ -480,13 +489,10 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
               for (int w = 0; w < YW; ++w) y[q][w] = lds_v4(y_row + s * PIECE + (2 * h + q) * 1024 + (((word + w) ^ g) << 4));
             if (r.rank > 0) tmem_ld_wait();
           }
-          if (h == 1) {                                   // all of this warp's is in registers
-            if (r.rank > 0) tc_fence_before();
+          if (h == 1 && r.rank > 0) {                     // the accumulator is in registers
+            tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-              mbar_arrive(bar(YFREE + s));
-              if (r.rank > 0) mbar_arrive(bar(AFREE + acc));
-            }
+            if (lane == 0) mbar_arrive(bar(AFREE + acc));
           }
           if (any)
 #pragma unroll
@@ -511,6 +517,9 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
                 }
               }
         }
+        // (behind the stores, which have to wait for the words that they store: right behind its loads the arrival, and the next copy with it, can overtake them)
+        __syncwarp();
+        if (lane < (F32 ? YP : 1)) mbar_arrive(bar(YFREE + (F32 ? (y_uses + lane) % Y_SLOTS : s)));
         y_uses += YP;
       }
       if (last) { r = r_next; ch = 0; ++ti; }
