@@ -260,7 +260,8 @@ struct UpParams {
 // Persistent, one CTA an SM: the steps (tile, 128 columns) of all tiles are cut into runs of like length.  Warp 0 fetches a tile's T (both halves) and each
 // step's slab of B, warp 1 issues hi B + lo B into one of two accumulators, warp 2 fetches Y0 into a ring of 96 KB, pieces of 128 rows x 128 bytes; the
 // drain warps hold 32 rows x 32 columns each: they add, round and store.  B's rows lie in the order that gives a lane eight neighbouring columns.
-// (Y0 straight into registers a step ahead, 32 KB in flight: 30.7 us for 8192 x 3456, rank 32, against 17.3 at the measured copy rate.)
+// 8192 x 3456, rank 32: 20 us from the down kernel's end on, 17.3 at the measured copy rate (Y0 straight into registers a step ahead, 32 KB in flight: 30.7).
+// Both kernels and the map, us: 8192 rows 1152 x 3456, rank 32 37; 32768 rows 5600 x 2240, rank 128 139 (103 at the copy rate).
 template <bool F32, int NA>      // NA: 64-wide pieces of the rank
 __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmUp,
                                                                        const __grid_constant__ RowMaps tmY,

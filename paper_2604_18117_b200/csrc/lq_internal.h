@@ -236,8 +236,9 @@ extern int g_lq_store_qb;    // option "store_qb": also write the branch activat
 // stream is still draining its last tiles; every kernel of this library executes griddepcontrol.wait after that set-up,
 // before it reads what an earlier kernel may write or writes global memory (weights, which no kernel writes, and the quantizer's
 // prefetch of X to the L2 come before it), and griddepcontrol.launch_dependents after the set-up, so that the chain
-// quantizer -> GEMM -> next quantizer overlaps its launch gaps and tails.  All kernels here are persistent (the whole
-// grid is resident at once), so a waiting successor never holds an SM that a predecessor CTA still needs.
+// quantizer -> GEMM -> next quantizer overlaps its launch gaps and tails.  The layer's kernels are persistent (the whole grid
+// is resident at once), and a dependent of the others starts only when their last CTA has, so a waiting successor never holds an SM that a predecessor
+// CTA still needs.
 template <typename... KArgs, typename... Args>
 static inline cudaError_t lq_launch_grid(void (*kernel)(KArgs...), dim3 grid, int block, int cluster, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t lc = {};
