@@ -272,7 +272,7 @@ lq_status lq_adapters_set(lq_adapters* set, int32_t slot, int32_t rank, const vo
                           void* cuda_stream);
 
 /* A map of up to M_max rows to the slots 0 .. slots - 1 (1 <= slots <= 1023, M_max <= 2^24), with the workspace of the forwards
- * that use it (synchronous): 4 bytes a row, and 516 more where M_max > 16. */
+ * that use it (synchronous): 520 bytes a row. */
 lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, lq_rowmap** out);
 lq_status lq_rowmap_free(lq_rowmap* map);
 

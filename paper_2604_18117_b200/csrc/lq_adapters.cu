@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
   if constexpr (BLOCKS > 1) {
     cluster_sync();                                            // (and the others have read this block's totals)
   } else {
-    if (M <= LQ_AD_SMALL_M_128) return;
+    if (M <= LQ_AD_ANY_M) return;
     __syncthreads();
   }
   for (int i = block * 1024 + tid; i < scan_tiles[31] >> 12; i += 1024 * BLOCKS) {
@@ -191,7 +191,7 @@ __host__ __device__ constexpr int adapters_stage(int rp, bool f32) { return ((rp
 // 3.8 at the measured copy rate); of these 3.4 are the map.  The first columns' B and Y0 are on their way during the first product, through shared memory (asked for
 // where they are used 15.3; ahead through registers, which spill, 22.7).
 template <int RP, int CLUSTER, bool F32>
-__global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : RP <= 64 ? 3 : 2) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, int M, int32_t* status, const int* perm, const __half* X, const void* Y0,
+__global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : 3) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, int M, int32_t* status, const int* perm, const __half* X, const void* Y0,
                                                                  void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad) {
   constexpr int NT = RP / 8, KB = (RP + 31) / 32;
   extern __shared__ __align__(16) float smem[];
@@ -384,7 +384,7 @@ template <int RP>
 cudaError_t launch_forward(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
   // Eight CTAs a tile while all of them are resident at once, else four (us with the map, eight / four: 1400 rows, 1152 x 3456, rank 32 25.8 / 20.9; 64 rows with an
   // adapter each, 512 x 8192, rank 64 43.4 / 32.3; one row, 1152 x 3456, rank 32 9.2 / 11.2; two were never better).
-  const int tiles = lq_ad_tiles(R->M, R->slots, LQ_AD_SMALL_TILE), resident = (RP <= 32 ? 4 : RP <= 64 ? 3 : 2) * R->sms;
+  const int tiles = lq_ad_tiles(R->M, R->slots, LQ_AD_SMALL_TILE), resident = (RP <= 32 ? 4 : 3) * R->sms;
   return 8 * tiles <= resident ? launch_cluster<RP, 8>(S, R, tiles, X, Y0, Y, dt, st) : launch_cluster<RP, 4>(S, R, tiles, X, Y0, Y, dt, st);
 }
 template <int RP, typename Room>
@@ -461,22 +461,21 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
   lq_rowmap* R = new (std::nothrow) lq_rowmap();
   if (!R) return LQ_ERR_ALLOC;
   R->M_max = M_max; R->slots = slots; R->device = device; R->M = 0;
-  const size_t rows = M_max > LQ_AD_SMALL_M_128 ? (size_t)M_max + LQ_AD_TILE : 0;
+  const size_t rows = (size_t)M_max + LQ_AD_TILE;
   const size_t large = (size_t)lq_ceil_div(M_max, LQ_AD_TILE) + slots + 1, little = (size_t)lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M), LQ_AD_SMALL_TILE) + slots + 1;
   if (lq_note_cuda(cudaDeviceGetAttribute(&R->sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, sizeof(int4))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_tiles, large * sizeof(LqAdTile))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_small, little * sizeof(LqAdTile))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_perm, (size_t)M_max * sizeof(int))) != cudaSuccess ||
-      (rows > 0 && (lq_note_cuda(cudaMalloc((void**)&R->d_T, rows * LQ_AD_TROW * 2)) != cudaSuccess ||
-                    lq_note_cuda(cudaMalloc((void**)&R->d_rscale, rows * sizeof(float))) != cudaSuccess))) {
+      lq_note_cuda(cudaMalloc((void**)&R->d_T, rows * LQ_AD_TROW * 2)) != cudaSuccess || lq_note_cuda(cudaMalloc((void**)&R->d_rscale, rows * sizeof(float))) != cudaSuccess) {
     lq_rowmap_free(R);
     return LQ_ERR_ALLOC;
   }
   // (no rows yet; T's rows are read in whole tiles: from defined contents on)
   lq_status s;
-  if (lq_note_cuda(cudaMemset(R->d_ntiles, 0, sizeof(int4))) != cudaSuccess ||
-      (rows > 0 && lq_note_cuda(cudaMemset(R->d_T, 0, rows * LQ_AD_TROW * 2)) != cudaSuccess) || lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess) {
+  if (lq_note_cuda(cudaMemset(R->d_ntiles, 0, sizeof(int4))) != cudaSuccess || lq_note_cuda(cudaMemset(R->d_T, 0, rows * LQ_AD_TROW * 2)) != cudaSuccess ||
+      lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess) {
     lq_rowmap_free(R);
     return LQ_ERR_CUDA;
   }
@@ -484,7 +483,7 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
     lq_rowmap_free(R);
     return LQ_ERR_CUDA;
   }
-  if (rows > 0 && ((s = lq_make_tmap_bytes(&R->tmT, R->d_T, rows, LQ_AD_TROW * 2, LQ_AD_TILE)) != LQ_OK || (s = lq_adapters_tiles_prepare()) != LQ_OK)) {
+  if ((s = lq_make_tmap_bytes(&R->tmT, R->d_T, rows, LQ_AD_TROW * 2, LQ_AD_TILE)) != LQ_OK || (s = lq_adapters_tiles_prepare()) != LQ_OK) {
     lq_rowmap_free(R);
     return s;
   }
@@ -492,7 +491,7 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
     return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes)) == cudaSuccess;
   };
   if (!room(lq_rowmap_kernel<1>, 32 * (MAX_SLOTS + 1) * 4) || !room(lq_rowmap_kernel<8>, 32 * (MAX_SLOTS + 1) * 4) || !room_of_rank<16>(room) ||
-      !room_of_rank<32>(room) || !room_of_rank<64>(room) || !room_of_rank<96>(room) || !room_of_rank<128>(room)) {
+      !room_of_rank<32>(room) || !room_of_rank<64>(room)) {
     lq_rowmap_free(R);
     return LQ_ERR_CUDA;
   }
@@ -535,8 +534,6 @@ extern "C" lq_status lq_adapters_forward(const lq_adapters* S, const lq_rowmap* 
   if (!lq_ad_small_form(R->M, S->rp)) return lq_adapters_forward_tiles(S, R, X, Y0, Y, dt, st);
   const cudaError_t e = S->rp == 16   ? launch_forward<16>(S, R, X, Y0, Y, dt, st)
                         : S->rp == 32 ? launch_forward<32>(S, R, X, Y0, Y, dt, st)
-                        : S->rp == 64 ? launch_forward<64>(S, R, X, Y0, Y, dt, st)
-                        : S->rp == 96 ? launch_forward<96>(S, R, X, Y0, Y, dt, st)
-                                      : launch_forward<128>(S, R, X, Y0, Y, dt, st);
+                                      : launch_forward<64>(S, R, X, Y0, Y, dt, st);
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }

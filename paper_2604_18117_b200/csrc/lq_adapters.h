@@ -5,13 +5,15 @@
 
 #include "lq_internal.h"
 
-// Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows, and one on tiles of 128 rows.  us with the map, K x N and rank, small /
-// large form.  Six requests of neighbouring rows: 1152 x 3456, 32: 600 rows 15.4 / 17, 1400 rows 18.4 / 21, 2048 rows 28.8 / 19.3; 512 x 8192, 64: 250 rows
-// 19.8 / 15.7; 5600 x 2240, 128: 250 rows 29.2 / 20.2.  Rows in any order, which the large form fetches four at a time: 1160 x 2312, 24, fp32, 1365 rows 20.2 / 36.9.
-// Rows with an adapter each: 512 x 8192, 64: 32 rows 22.0 / 23.8, 64 rows 32.4 / 36.4; 5600 x 2240, 128: 12 rows 27.1 / 22.4, 32 rows 49.5 / 30.7.
+// Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows of narrow factors, and one on tiles of 128 rows.  us with the map, K x N
+// and rank, small / large form.  Six requests of neighbouring rows: 1152 x 3456, 32: 600 rows 14.1 / 15.5, 1400 rows 18.2 / 17.7, 2048 rows 19.0 / 19.6; 512 x 8192,
+// 64: 90 rows 14.3 / 15.2, 250 rows 20.7 / 15.9.  Rows in any order, which the large form fetches four at a time: 1160 x 2312, 24, 1365 rows 16.8 / 23.9 (fp32 21.2 /
+// 31.9).  Rows with an adapter each: 512 x 8192, 64: 64 rows 27.8 / 34.8.  Ranks above 64 (the small form is not built for them): 5600 x 2240, 128: one row 23.9 / 17.2,
+// 12 rows 26.8 / 22.3; 512 x 8192, 128: one row 20.0 / 12.7; 1152 x 1152, 96: one row 12.4 / 13.2.
 constexpr int LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
-constexpr int LQ_AD_SMALL_M = 1536, LQ_AD_SMALL_M_64 = 128, LQ_AD_SMALL_M_128 = 16;      // most rows of the small form, for stored ranks up to 32, 64, 128
-static inline bool lq_ad_small_form(int M, int rp) { return M <= (rp <= 32 ? LQ_AD_SMALL_M : rp <= 64 ? LQ_AD_SMALL_M_64 : LQ_AD_SMALL_M_128); }
+constexpr int LQ_AD_SMALL_M = 1536, LQ_AD_SMALL_M_64 = 128;      // most rows of the small form, for stored ranks up to 32, 64
+static inline bool lq_ad_small_form(int M, int rp) { return rp <= 32 ? M <= LQ_AD_SMALL_M : rp <= 64 && M <= LQ_AD_SMALL_M_64; }
+constexpr int LQ_AD_ANY_M = 16;        // maps of so few rows do not look for neighbours: at most four copies bring a tile's rows
 constexpr int LQ_AD_TROW = 256;        // halves of a row of the intermediate: 128 hi, 128 lo
 
 struct LqAdTile {
@@ -35,7 +37,7 @@ struct lq_rowmap {
   int* d_ntiles;                       // [4]: tiles of 128 rows, of 16, rows that were sorted, 0
   LqAdTile *d_tiles, *d_small;         // (tiles of 16 rows only up to LQ_AD_SMALL_M rows)
   int* d_perm;                         // [M_max]
-  __half* d_T;                         // [M_max + 128][LQ_AD_TROW], in the order of perm (only where M_max can have the large form)
+  __half* d_T;                         // [M_max + 128][LQ_AD_TROW], in the order of perm
   float* d_rscale;                     // [M_max + 128] what a row of T times B is multiplied with
   CUtensorMap tmT;
 };

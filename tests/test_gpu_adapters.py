@@ -449,3 +449,19 @@ def test_pass_after_pass_gives_the_same_bits(M, K, N, rank, f32):
     assert (np.abs(first.cpu().numpy()[look] - ref) <= bound).all()
     B.lq_rowmap_free(m)
     S.free()
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("rank", [65, 96, 128])
+def test_few_rows_of_wide_factors(rank, f32):
+    """From one row on these have tiles of 128 rows, up to 16 rows fetched four at a time."""
+    rng = np.random.default_rng(rank)
+    for K, N in ((8, 8), (200, 136), (2048, 320)):
+        S = Set(rng, K, N, rank, [rank, 1, 0, rank // 2])
+        for M in (1, 2, 4, 5, 15, 16, 17, 33, 129):
+            X, Y0 = inputs(rng, M, K, N, f32)
+            for ids in (np.zeros(M, int), rng.integers(-1, 5, M), np.full(M, 2), np.arange(M) * 3 // M):
+                Y = forward(S, ids, X, Y0, f32, in_place=bool(M & 1))
+                ref, bound = reference(S, X, Y0, ids, f32)
+                assert (np.abs(Y - ref) <= bound).all(), (K, M)
+        S.free()
