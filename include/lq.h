@@ -333,7 +333,8 @@ typedef struct {
   void* out;                               /* device, 16-byte aligned; half or float per out_dtype; `in` itself, with its strides and
                                               type (INVALID_ARG otherwise), or memory apart from all inputs           */
   int64_t in_seq, in_row, in_head;         /* strides in elements, multiples of 8, below 2^31, a head's below 2^26 (the memory they span may be larger) */
-  int64_t out_seq, out_row, out_head;      /* no two outputs on one place; may be negative, like those of `in`        */
+  int64_t out_seq, out_row, out_head;      /* no two outputs of the call on one place, none on an input (INVALID_ARG; UNSUPPORTED where dimensions run
+                                              through one another too often to tell); may be negative, like those of `in` */
   const float* weight;                     /* [head_dim] device, 16-byte aligned, or NULL (ones); NULL without a norm */
   const float* bias;                       /* [head_dim] device, 16-byte aligned, or NULL (zeros); LQ_NORM_LAYER only */
   int32_t heads;                           /* 1 .. 4096                                                               */

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "lq_device.cuh"
+#include "lq_heads_places.h"
 #include "lq_internal.h"
 
 using namespace lqdev;
@@ -384,8 +385,8 @@ cudaError_t launch_norm(HeadsParams& p, int norm, int rot, cudaStream_t st) {
                                : launch_rot<TIN, TOUT, LQ_NORM_LAYER>(p, rot, st);
 }
 
-// Strides over dimensions of one entry mean nothing; the others keep entries on 16-byte boundaries, and no two outputs on one place.
-lq_status take_side(const lq_heads* h, int head_dim, int sequences, int seq_len, lq_norm norm, bool same_type, Side* s) {
+// Strides over dimensions of one entry mean nothing; the others keep entries on 16-byte boundaries.
+lq_status take_side(const lq_heads* h, int sequences, int seq_len, lq_norm norm, bool same_type, Side* s) {
   if (!h->in || !h->out || h->heads < 1) return LQ_ERR_INVALID_ARG;
   if (h->heads > 4096) return LQ_ERR_UNSUPPORTED;
   if ((((uintptr_t)h->in | (uintptr_t)h->out | (uintptr_t)h->weight | (uintptr_t)h->bias) & 15) != 0) return LQ_ERR_INVALID_ARG;
@@ -399,11 +400,35 @@ lq_status take_side(const lq_heads* h, int head_dim, int sequences, int seq_len,
   for (int i : {2, 5})                                       // (a warp steps over up to 32 heads)
     if (strides[i] > INT32_MAX / 32 || strides[i] < -(INT32_MAX / 32)) return LQ_ERR_UNSUPPORTED;
   *s = Side{h->in, h->out, (int)strides[0], (int)strides[1], (int)strides[2], (int)strides[3], (int)strides[4], (int)strides[5], h->weight, h->bias};
-  const int64_t counts[3] = {sequences, seq_len, h->heads};
-  for (int i = 0; i < 3; ++i)
-    if (counts[i] > 1 && strides[3 + i] < head_dim && strides[3 + i] > -head_dim) return LQ_ERR_INVALID_ARG;
   if (h->in == h->out && (!same_type || strides[0] != strides[3] || strides[1] != strides[4] || strides[2] != strides[5])) return LQ_ERR_INVALID_ARG;
   return LQ_OK;
+}
+
+// No two outputs on one place, and none on an input, but for a side that is worked on in place (in == out: the same strides and type by now).
+lq_status check_places(const HeadsParams& p, int head_dim, int sequences, lq_out_dtype in_dtype, lq_out_dtype out_dtype) {
+  const auto runs = [&](const void* at, int seq, int row, int head, int heads, lq_out_dtype dt) {
+    const int64_t esz = dt == LQ_OUT_F32 ? 4 : 2;
+    return LqRuns{(uintptr_t)at, {seq * esz, row * esz, head * esz}, {sequences, p.seq_len, heads}, head_dim * esz};
+  };
+  const auto line = [](const void* at, int64_t bytes) { return LqRuns{(uintptr_t)at, {0, 0, 0}, {1, 1, 1}, bytes}; };
+  LqRuns out[2], in[9];                                      // in: of both sides, their weights and biases, the positions
+  int n_out = 0, n_in = 0;
+  for (int i = 0; i < 2; ++i) {
+    if (p.heads[i] == 0) continue;
+    const Side& s = p.side[i];
+    out[n_out++] = runs(s.out, s.out_seq, s.out_row, s.out_head, p.heads[i], out_dtype);
+    if (s.in != s.out) in[n_in++] = runs(s.in, s.in_seq, s.in_row, s.in_head, p.heads[i], in_dtype);
+    if (s.weight) in[n_in++] = line(s.weight, head_dim * 4);
+    if (s.bias) in[n_in++] = line(s.bias, head_dim * 4);
+  }
+  if (p.pairs > 0) in[n_in++] = line(p.pos, (int64_t)p.rows * p.axes * 4);
+  const auto status = [](LqPlaces c) { return c == LQ_APART ? LQ_OK : c == LQ_SHARED ? LQ_ERR_INVALID_ARG : LQ_ERR_UNSUPPORTED; };
+  lq_status s = n_out > 1 ? status(lq_runs_meet(out[0], out[1])) : LQ_OK;
+  for (int i = 0; i < n_out && s == LQ_OK; ++i) {
+    s = status(lq_runs_collide(out[i]));
+    for (int j = 0; j < n_in && s == LQ_OK; ++j) s = status(lq_runs_meet(out[i], in[j]));
+  }
+  return s;
 }
 
 }  // namespace
@@ -493,8 +518,7 @@ lq_status lq_heads_run(const lq_heads* q, const lq_heads* k, int32_t head_dim, i
   lq_status s;
   const lq_heads* both[2] = {q, k};
   for (int i = 0; i < 2; ++i)
-    if (both[i] && (s = take_side(both[i], head_dim, sequences, seq_len, norm, in_dtype == out_dtype, &p.side[i])) != LQ_OK) return s;
-  if (q && k && q->out == k->out) return LQ_ERR_INVALID_ARG;
+    if (both[i] && (s = take_side(both[i], sequences, seq_len, norm, in_dtype == out_dtype, &p.side[i])) != LQ_OK) return s;
   p.heads[0] = q ? q->heads : 0;
   p.heads[1] = k ? k->heads : 0;
   p.rows = (int)rows;
@@ -503,7 +527,7 @@ lq_status lq_heads_run(const lq_heads* q, const lq_heads* k, int32_t head_dim, i
   p.eps = eps; p.inv_d = 1.f / (float)head_dim;
   p.turn = R->d_turn; p.axis = R->d_axis; p.pos = pos;
   if (device >= 0 && device != R->device) return LQ_ERR_INVALID_ARG;
-  if (!launch) return LQ_OK;
+  if ((s = check_places(p, head_dim, sequences, in_dtype, out_dtype)) != LQ_OK || !launch) return s;
   LqDeviceGuard guard(R->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   const int rot = R->pairs == 0 ? ROT_NONE : R->halves ? ROT_HALVES : ROT_PAIRS;

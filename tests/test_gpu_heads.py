@@ -261,6 +261,50 @@ def test_outputs_on_one_place_and_other_ways_in_place_are_refused():
     B.lq_rope_free(none)
 
 
+def test_every_output_has_a_place_of_its_own_apart_from_the_inputs():
+    """Dimensions that run through one another, a side's output on the other's input, on its own input shifted, on weights or positions: refused,
+    and nothing is written.  The same without a shared place: taken."""
+    import torch
+    x = torch.zeros(1 << 15, dtype=torch.float16, device="cuda")
+    x[:] = torch.arange(1 << 15, device="cuda") % 100
+    before = x.clone()
+    P, far = x.data_ptr(), x.data_ptr() + 32768
+    rope = B.lq_rope_create(B.lq_rope_config_default([64]), 0)
+    pos = torch.zeros(8, dtype=torch.int32, device="cuda").data_ptr()
+
+    def code(q, k=None, Bn=2, at=pos, fin=0, fout=0):
+        try:
+            B.lq_qk_norm_rope(B.lq_heads(*q), B.lq_heads(*k) if k else None, 64, Bn, 4, B.NORM_RMS, 1e-6, rope, at, fin, fout, 0)
+        except B.LqError as e:
+            return e.code
+        return 0
+
+    s = (512, 128, 64)
+    for bad in ((512, 64, 64), (512, 128, 128), (128, 128, 64), (256, 128, 64), (512, 128, -128), (512, 128, 256)):
+        assert code((P, s, far, bad, 2)) == 1, bad
+    for q, k in (((P, s, far, s, 2), (P + 2048, s, P, s, 2)),                    # keys onto what queries are read from
+                 ((P, s, P + 2048, s, 2), (P + 2048, s, far, s, 2)),             # queries onto what keys are read from
+                 ((P, s, far, s, 2), (P + 2048, s, far + 128, s, 2)),            # the keys' first head on the queries' second
+                 ((P, s, far, (512, 128, 64), 1), (P + 2048, s, far + 64, s, 1)),
+                 ((P, s, P, s, 2), (P + 128, s, P + 128, s, 1))):                # in place, and one head of both sides
+        assert code(q, k) == 1, (q, k)
+    assert code((P, s, P + 128, s, 1)) == 0 and code((P, s, P + 16, s, 1)) == 1 and code((P, s, P + 128, s, 2)) == 1
+    assert code((P, s, far, s, 2, far + 1024)) == 1 and code((P, s, far, s, 2), at=far + 4) == 1
+    assert code((P, s, far, s, 2), fout=1) == 0 and code((P, s, far - 3072, s, 2), fout=1) == 0 and code((P, s, P + 1024, s, 2), fout=1) == 1
+    torch.cuda.synchronize()
+    x.copy_(before)
+    torch.cuda.synchronize()
+    for q, k in (((P, s, far, s, 2), (P + 2048, s, P, s, 2)), ((P, s, P, s, 2), (P + 128, s, P + 128, s, 1))):
+        assert code(q, k) == 1
+    torch.cuda.synchronize()
+    assert torch.equal(x, before)
+    assert code((P, s, P, s, 1), (P + 128, s, P + 128, s, 1)) == 0               # in place, side by side in a row
+    assert code((P, s, far, (1024, 256, 128), 2), (P + 2048, s, far + 128, (1024, 256, 128), 2)) == 0      # a query beside its key
+    assert code((P, s, far, (0, 512, 384), 2), Bn=1) == 0                        # woven, every place once
+    torch.cuda.synchronize()
+    B.lq_rope_free(rope)
+
+
 @pytest.mark.parametrize("norm", ["none", "rms"])
 def test_strides_backwards_and_far_apart(norm):
     """Rows in the opposite order, heads too, and sequences of outputs 2^30 elements and more apart."""
