@@ -367,7 +367,8 @@ typedef struct {
 
 /*   act, X_f16_dev, M   as for lq_quantize_act
  *   set, map            the rows' adapters of this projection (set's K and N the layer's, map's rows M), or both NULL
- *   Y_dev               [M][N] row-major half or float per `dtype`, device, 16-byte aligned
+ *   Y_dev               [M][N] row-major half or float per `dtype`, device, 16-byte aligned, apart from weights, biases and positions
+ *                       and, with adapters, from X (INVALID_ARG)
  * Nothing is launched if an argument is refused.  Asynchronous on `cuda_stream`. */
 lq_status lq_qkv_forward(const lq_layer* layer, lq_act* act, const void* X_f16_dev, int32_t M, const lq_adapters* set, const lq_rowmap* map,
                          const lq_qkv* qkv, void* Y_dev, lq_out_dtype dtype, void* cuda_stream);

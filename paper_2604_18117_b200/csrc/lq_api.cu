@@ -765,6 +765,10 @@ extern "C" lq_status lq_qkv_forward(const lq_layer* L, lq_act* A, const void* X,
   };
   lq_status s;
   if ((s = heads(false)) != LQ_OK) return s;
+  // (those checks know the queries' and keys' places; the GEMM writes the values' too, before weights and positions are read)
+  for (const float* v : {c->q_weight, c->k_weight, c->q_bias, c->k_bias})
+    if (v && lq_overlap(v, (size_t)D * 4, Y, (size_t)M * L->N * esz)) return LQ_ERR_INVALID_ARG;
+  if (c->rope->pairs > 0 && lq_overlap(c->pos_dev, (size_t)M * c->rope->axes * 4, Y, (size_t)M * L->N * esz)) return LQ_ERR_INVALID_ARG;
   if ((s = lq_quantize_act(L, X, M, A, stream)) != LQ_OK || (s = lq_linear_forward(L, A, Y, dt, stream)) != LQ_OK) return s;
   if (S && (s = lq_adapters_forward(S, R, X, Y, Y, dt, stream)) != LQ_OK) return s;
   return heads(true);

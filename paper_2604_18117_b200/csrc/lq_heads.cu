@@ -19,12 +19,6 @@
 
 using namespace lqdev;
 
-struct lq_rope {
-  int axes, pairs, halves, device;
-  uint64_t* d_turn;   // [pairs] fraction of a turn a position, 2^64 = 1
-  uint8_t* d_axis;    // [pairs]
-};
-
 namespace {
 
 constexpr int MAX_D = 256, WARPS = 4, MAX_ROWS = 2;

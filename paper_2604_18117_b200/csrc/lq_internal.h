@@ -188,6 +188,11 @@ lq_status lq_gemm_prepare(int device);
 lq_status lq_launch_gemm_mx(const lq_layer* L, const lq_act* A, void* Y, lq_out_dtype dt, cudaStream_t st);
 lq_status lq_gemm_mx_prepare(int device);
 lq_status lq_launch_wait_probe(int device, cudaStream_t st);   // bounded-wait self-test kernel
+struct lq_rope {
+  int axes, pairs, halves, device;
+  uint64_t* d_turn;   // [pairs] fraction of a turn a position, 2^64 = 1
+  uint8_t* d_axis;    // [pairs]
+};
 // lq_qk_norm_rope on `device` (-1: the table's, whichever); launch = false: its checks alone
 lq_status lq_heads_run(const lq_heads* q, const lq_heads* k, int32_t head_dim, int32_t sequences, int32_t seq_len, lq_norm norm, float eps, const lq_rope* R,
                        const int32_t* pos, lq_out_dtype in_dtype, lq_out_dtype out_dtype, int device, bool launch, cudaStream_t st);

@@ -213,3 +213,32 @@ def test_inputs_that_share_memory_with_outputs_under_adapters():
     torch.cuda.synchronize()
     assert (b.y[0] == 3).all()
     b.free()
+
+
+@pytest.mark.parametrize("adapters", [True, False])
+def test_weights_and_positions_among_the_values_are_refused(adapters):
+    """The GEMM writes the values' columns too, before the heads read their weights and the rows' positions."""
+    import torch
+    b = Block(64, 2, False)
+    B.lq_rowmap_set(b.map, b.i.data_ptr(), 64, 0)
+    torch.cuda.synchronize()
+    b.y[0].fill_(3.0)
+    Y, v = b.y[0].data_ptr(), 2 * (b.hq + b.hk) * b.D      # the first row's values, 576 bytes of them
+    end = Y + 2 * b.M * b.N
+
+    def code(p=b.p.data_ptr(), q_weight=None, k_weight=None, norm=B.NORM_RMS, q_bias=None, k_bias=None):
+        c = B.lq_qkv(b.D, b.hq, b.hk, b.seqs, norm, 1e-6, b.rope, p, q_weight, k_weight, q_bias, k_bias)
+        try:
+            B.lq_qkv_forward(b.h, b.act, b.x.data_ptr(), 64, b.set if adapters else None, b.map if adapters else None, c, Y, b.code, 0)
+        except B.LqError as e:
+            return e.code
+        return 0
+
+    assert code(p=Y + v) == 1 and code(p=end - 4) == 1 and code(p=Y - 64 * 2 * 4 + 4) == 1
+    assert code(q_weight=Y + v) == 1 and code(k_weight=Y + v) == 1 and code(k_weight=end - 16) == 1
+    assert code(norm=B.NORM_LAYER, q_bias=Y + v) == 1 and code(norm=B.NORM_LAYER, k_bias=Y + v) == 1
+    torch.cuda.synchronize()
+    assert (b.y[0] == 3).all()                             # a refused call has launched nothing
+    assert code() == 0
+    torch.cuda.synchronize()
+    b.free()
