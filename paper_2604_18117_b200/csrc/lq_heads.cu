@@ -16,6 +16,7 @@
 #include "lq_device.cuh"
 #include "lq_heads_places.h"
 #include "lq_internal.h"
+#include "lq_turns.h"
 
 using namespace lqdev;
 
@@ -454,14 +455,11 @@ extern "C" lq_status lq_rope_create(const lq_rope_config* cfg, const double* fre
     for (int a = 0; a < cfg->axes; ++a)
       for (int j = 0; j < cfg->dims[a] / 2; ++j, ++i) {
         if (axis && (axis[i] < 0 || axis[i] >= cfg->axes)) return LQ_ERR_INVALID_ARG;
-        if (freq && !isfinite(freq[i])) return LQ_ERR_NUMERIC;
         const long double f = freq ? (long double)freq[i]
                                    : powl((long double)cfg->theta, -2.0L * (cfg->shared ? i : j) / (cfg->shared ? rot : cfg->dims[a]));
-        long double t = f / (2.0L * acosl(-1.0L));
-        if (!isfinite(t)) return LQ_ERR_NUMERIC;
-        t -= floorl(t);                                      // [0, 1]: 1 itself wraps to 0 below
-        const long double scaled = roundl(ldexpl(t, 64));
-        turn.push_back(scaled >= 0x1p64L ? 0 : (uint64_t)scaled);
+        if (!isfinite(f)) return LQ_ERR_NUMERIC;
+        if (fabsl(f) >= 0x1p64L) return LQ_ERR_UNSUPPORTED;
+        turn.push_back(lq_turn_fraction(f));
         which.push_back((uint8_t)(axis ? axis[i] : a));
       }
   } catch (const std::bad_alloc&) { return LQ_ERR_ALLOC; }

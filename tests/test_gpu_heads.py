@@ -163,6 +163,33 @@ def test_frequencies_and_axes_of_the_caller():
     Case(1, 50, 2, 2, 64, "none", (64, 0, 0), freq=freq, axis=rng.integers(0, 3, 32), fin="f32", fout="f32").run()
 
 
+def test_fast_frequencies_at_far_positions():
+    """Many turns a position, up to 2^31 positions away, against angles from whole numbers of 400 bits: the fraction of a turn that is kept is
+    right whatever the whole turns before it."""
+    import torch
+    from fractions import Fraction
+    from tests.test_turns_host import pi
+    freq = np.array([100.0, -12345.678, 1e6, 3.7e9, -2.0 ** 40 - 0.5, 1e15 + 0.125, 2.0 ** 63, 6.0])
+    pos = np.array([1, -1, 12345, 10 ** 8 + 1, 2 ** 31 - 1, -2 ** 31, -2 ** 31 + 1], np.int32)
+    two_pi = 2 * pi()
+    t = np.array([[float((int(p) * Fraction(float(f)) / two_pi % 1 + Fraction(1, 2)) % 1 - Fraction(1, 2)) for f in freq] for p in pos]) * 2 * np.pi
+    S, D = pos.size, 16
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((S, 1, D)).astype(np.float32)
+    rope = B.lq_rope_create(B.lq_rope_config_default([D]), 0, freq)
+    xd, pd, out = torch.from_numpy(x).cuda(), torch.from_numpy(pos).cuda(), torch.zeros(S, 1, D, device="cuda")
+    side = B.lq_heads(xd.data_ptr(), (S * D, D, D), out.data_ptr(), (S * D, D, D), 1)
+    B.lq_qk_norm_rope(side, None, D, 1, S, B.NORM_NONE, 0.0, rope, pd.data_ptr(), B.OUT_F32, B.OUT_F32, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    B.lq_rope_free(rope)
+    u, v = x[:, 0, 0::2].astype(np.float64), x[:, 0, 1::2].astype(np.float64)
+    y = out.cpu().numpy()[:, 0].astype(np.float64)
+    # cosine and sine within 4 * 2^-24 of theirs, two products and a sum, a rounding: as in reference()
+    bound = 10 * 2.0 ** -24 * (np.abs(u) + np.abs(v))
+    assert (np.abs(y[:, 0::2] - (u * np.cos(t) - v * np.sin(t))) <= bound).all()
+    assert (np.abs(y[:, 1::2] - (v * np.cos(t) + u * np.sin(t))) <= bound).all()
+
+
 def test_zero_heads_and_large_values():
     """A head of zeros stays zero; fp32 entries whose squares are large or tiny."""
     import torch
