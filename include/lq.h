@@ -320,10 +320,13 @@ typedef struct lq_rope lq_rope;    /* opaque: axis and frequency of each pair, o
 /* Fill *cfg: `axes` axes of dims[0 .. axes - 1] entries (host), neighbouring pairs, frequencies of each axis its own, theta 10000. */
 lq_status lq_rope_config_default(lq_rope_config* cfg, int32_t axes, const int32_t* dims);
 
-/* A table of rotations (synchronous).  freq_host: NULL (frequencies as the configuration says) or rot_dim / 2 finite doubles below 2^64
- * in magnitude (as must be the configuration's; UNSUPPORTED), radians a position, pair by pair: scaled or interpolated frequencies.  axis_host: NULL or rot_dim / 2 axes, pair by pair (the configuration's
- * dims then only give rot_dim).  Frequencies are kept as 64-bit fractions of a turn and multiplied by the position in integers, so an angle is
- * right to 1e-9 radians at any position. */
+/* A table of rotations (synchronous).
+ *   freq_host  NULL (frequencies as the configuration says) or rot_dim / 2 finite doubles, radians a position, pair by pair: scaled or
+ *              interpolated frequencies.  Below 2^64 in magnitude, as must be the configuration's (UNSUPPORTED)
+ *   axis_host  NULL or rot_dim / 2 axes, pair by pair (the configuration's dims then only give rot_dim)
+ * Frequencies are kept as 64-bit fractions of a turn and multiplied by the position in integers: modulo a turn an angle is within 1.5e-9
+ * radians of frequency times position at any position (theta below 1: times the frequency).  What is left of it beside the nearest quarter
+ * turn becomes a float, within 1.4e-7 radians; cosine and sine are within 4 * 2^-24. */
 lq_status lq_rope_create(const lq_rope_config* cfg, const double* freq_host, const int32_t* axis_host, int device, lq_rope** out);
 lq_status lq_rope_free(lq_rope* rope);
 

@@ -4,8 +4,9 @@
 //   (u, v) -> (u cos t - v sin t, v cos t + u sin t),   t = pos[axis of the pair] * frequency of the pair
 //
 // Angles.  A frequency is kept as a 64-bit fraction of a turn, F = 2^64 frac(f / 2 pi); pos * F modulo 2^64 is the exact fraction of a
-// turn that the rounded F gives at an int32 position, so that an angle is off by 2^31 * 2^-65 turns (4e-10 radians) at most.  The nearest
-// quarter turn is taken off in integers and only the rest, at most an eighth of a turn, becomes a float.
+// turn that the rounded F gives at an int32 position: off by 2^31 * 2^-65 turns (4e-10 radians) at most.  It is rounded to 32 bits (7e-10
+// radians), the nearest quarter turn is taken off in integers and only the rest, at most an eighth of a turn, becomes a float: three
+// roundings of 2^-24 of it, 1.4e-7 radians at an eighth of a turn.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -102,7 +103,7 @@ __device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
 
 // Cosine and sine of pos * turn.  Taylor's series about the nearest quarter turn, at most pi / 4 away: the terms left out are below 2e-9 and 2e-10.
 __device__ __forceinline__ float2 cos_sin(uint64_t turn, int32_t pos) {
-  const int32_t t = (int32_t)(uint32_t)((turn * (uint64_t)(int64_t)pos) >> 32);       // fraction of a turn, 2^32 = 1
+  const int32_t t = (int32_t)(uint32_t)((turn * (uint64_t)(int64_t)pos + 0x80000000u) >> 32);       // fraction of a turn, 2^32 = 1
   const uint32_t quarter = ((uint32_t)t + 0x20000000u) >> 30;                          // nearest quarter turn, 0 .. 3
   const int32_t rest = (int32_t)((uint32_t)t - (quarter << 30));                       // [-2^29, 2^29)
   const float x = (float)rest * 1.46291807926715968e-9f, y = x * x;                    // 2 pi / 2^32
