@@ -348,12 +348,13 @@ cudaError_t launch(HeadsParams& p, cudaStream_t st) {
   for (int i = 0; i < 2; ++i) p.parts[i] = (p.heads[i] + walk - 1) / walk;
   const int n = p.parts[0] + p.parts[1];
   p.block_rows = std::max(1, std::min(MAX_ROWS, p.rows / (fill / WARPS)));
-  const int blocks_y = std::max(1, std::min(lq_ceil_div(p.block_rows * n, WARPS), fill / WARPS / lq_ceil_div(p.rows, p.block_rows)));
+  const int blocks = 1 + (p.rows - 1) / p.block_rows;     // (up to 2^31 - 1 rows: no sum beyond them)
+  const int blocks_y = std::max(1, std::min(lq_ceil_div(p.block_rows * n, WARPS), fill / WARPS / blocks));
   const auto reciprocal = [](int d) { return (uint32_t)(((1ull << 32) + d - 1) / d); };
   p.by_parts = reciprocal(std::max(2, n));
   p.by_wide = reciprocal(std::max(4, lq_round_up(p.pairs, 4)));
   p.by_groups = reciprocal(std::max(2, g));
-  return lq_launch_grid(lq_heads_kernel<TIN, TOUT, NORM, ROT, L, C>, dim3(lq_ceil_div(p.rows, p.block_rows), blocks_y), 32 * WARPS, 1, 0, st, p);
+  return lq_launch_grid(lq_heads_kernel<TIN, TOUT, NORM, ROT, L, C>, dim3(blocks, blocks_y), 32 * WARPS, 1, 0, st, p);
 }
 // Under an RMS norm heads of 64, 72, 112 and 128 entries that are rotated as a whole, or not at all, have their lanes at compile time, 16 entries to each where
 // lanes are a power of two; others hold eight entries a lane.  (8192 rows, 32 heads of 72: 26 us by the general form.)

@@ -387,3 +387,29 @@ def test_the_most_heads_of_the_longest():
     for norm in ("rms", "layer"):
         Case(1, 1, 4095, 7, 256, norm, (256,)).run()
         Case(1, 3, 1, 4096, 8, norm, (8,), halves=True).run()
+
+
+def test_the_most_rows():
+    """2^31 - 1 rows of one head of eight entries, in place."""
+    import torch
+    n, D = 2 ** 31 - 1, 8
+    if torch.cuda.mem_get_info()[0] < 44e9:
+        pytest.skip("the rows alone are 34 GB")
+    x = torch.full((n, D), 3.0, dtype=torch.float16, device="cuda")
+    look = torch.tensor([0, 1, 2, n // 2, n - 3, n - 2, n - 1], device="cuda")
+    rng = np.random.default_rng(0)
+    rows = rng.standard_normal((look.numel(), D)).astype(np.float16)
+    x[look] = torch.from_numpy(rows).cuda()
+    rope = B.lq_rope_create(B.lq_rope_config_default([]), 0)
+    side = B.lq_heads(x.data_ptr(), (0, D, 0), x.data_ptr(), (0, D, 0), 1)
+    B.lq_qk_norm_rope(side, None, D, 1, n, B.NORM_RMS, 0.0, rope, None, B.OUT_F16, B.OUT_F16, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    B.lq_rope_free(rope)
+    ref, bound = reference(rows[None, :, None], None, None, "rms", 0.0, np.zeros(0, int), np.zeros(0), False, None, False)
+    assert (np.abs(x[look].float().cpu().numpy() - ref[0, :, 0]) <= bound[0, :, 0]).all()
+    x[look] = 1.0                                          # the others: 3 / sqrt(9) within a rounding
+    for part in x.view(-1).split(1 << 28):
+        lo, hi = torch.aminmax(part)
+        assert abs(float(lo) - 1) <= 2.0 ** -11 and abs(float(hi) - 1) <= 2.0 ** -11
+    del x, part
+    torch.cuda.empty_cache()
