@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "lq_device.cuh"
+#include "lq_heads_cut.h"
 #include "lq_heads_places.h"
 #include "lq_internal.h"
 #include "lq_turns.h"
@@ -23,7 +24,7 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int MAX_D = 256, WARPS = 4, MAX_ROWS = 2;
+constexpr int MAX_D = 256, WARPS = LQ_HEADS_WARPS, MAX_ROWS = LQ_HEADS_ROWS;
 enum { ROT_NONE = 0, ROT_PAIRS = 1, ROT_HALVES = 2 };
 
 struct Side {
@@ -328,58 +329,44 @@ __global__ void __launch_bounds__(32 * WARPS, C == 1 && sizeof(TIN) == 2 && NORM
 }
 
 template <typename TIN, typename TOUT, int NORM, int ROT, int L, int C>
-cudaError_t launch(HeadsParams& p, cudaStream_t st) {
+cudaError_t launch(HeadsParams& p, int sms, cudaStream_t st) {
   p.lanes = L > 0 ? L : p.lanes;
   p.groups = 32 / p.lanes;
-  // A warp walks over all heads of a side, or over as many as the shorter side has (at least four steps), so that warps have like work, once there
-  // are rows enough to fill the GPU (148 SMs x 24 warps); below that over fewer, down to one step.
-  const int g = p.groups, fill = 148 * 24;
-  int walk = std::max(p.heads[0], p.heads[1]);
-  if (p.heads[0] > 0 && p.heads[1] > 0) walk = std::min(walk, std::max(4 * g, std::min(p.heads[0], p.heads[1])));
-  const auto parts = [&](int w) { return (p.heads[0] + w - 1) / w + (p.heads[1] + w - 1) / w; };
-  walk = lq_round_up(walk, g);
-  int low = 1, high = walk / g;                           // the longest walk, in steps, that fills, or one
-  while (low < high) {
-    const int mid = (low + high + 1) / 2;
-    if ((long long)p.rows * parts(mid * g) < fill) high = mid - 1;
-    else low = mid;
-  }
-  p.walk = walk = low * g;
-  for (int i = 0; i < 2; ++i) p.parts[i] = (p.heads[i] + walk - 1) / walk;
-  const int n = p.parts[0] + p.parts[1];
-  p.block_rows = std::max(1, std::min(MAX_ROWS, p.rows / (fill / WARPS)));
-  const int blocks = 1 + (p.rows - 1) / p.block_rows;     // (up to 2^31 - 1 rows: no sum beyond them)
-  const int blocks_y = std::max(1, std::min(lq_ceil_div(p.block_rows * n, WARPS), fill / WARPS / blocks));
+  const int g = p.groups;
+  const LqHeadsCut c = lq_heads_cut(p.rows, p.heads[0], p.heads[1], g, sms);
+  p.walk = c.walk;
+  p.block_rows = c.block_rows;
+  for (int i = 0; i < 2; ++i) p.parts[i] = c.parts[i];
   const auto reciprocal = [](int d) { return (uint32_t)(((1ull << 32) + d - 1) / d); };
-  p.by_parts = reciprocal(std::max(2, n));
+  p.by_parts = reciprocal(std::max(2, c.parts[0] + c.parts[1]));
   p.by_wide = reciprocal(std::max(4, lq_round_up(p.pairs, 4)));
   p.by_groups = reciprocal(std::max(2, g));
-  return lq_launch_grid(lq_heads_kernel<TIN, TOUT, NORM, ROT, L, C>, dim3(blocks, blocks_y), 32 * WARPS, 1, 0, st, p);
+  return lq_launch_grid(lq_heads_kernel<TIN, TOUT, NORM, ROT, L, C>, dim3(c.blocks, c.blocks_y), 32 * WARPS, 1, 0, st, p);
 }
 // Under an RMS norm heads of 64, 72, 112 and 128 entries that are rotated as a whole, or not at all, have their lanes at compile time, 16 entries to each where
 // lanes are a power of two; others hold eight entries a lane.  (8192 rows, 32 heads of 72: 26 us by the general form.)
 template <typename TIN, typename TOUT, int NORM, int ROT>
-cudaError_t launch_lanes(HeadsParams& p, cudaStream_t st) {
+cudaError_t launch_lanes(HeadsParams& p, int sms, cudaStream_t st) {
   if constexpr (NORM == LQ_NORM_RMS)
     if (ROT == ROT_NONE || p.pairs == 4 * p.lanes) {
-      if (p.lanes == 8) return launch<TIN, TOUT, NORM, ROT, 4, 2>(p, st);
-      if (p.lanes == 9) return launch<TIN, TOUT, NORM, ROT, 9, 1>(p, st);
-      if (p.lanes == 14) return launch<TIN, TOUT, NORM, ROT, 14, 1>(p, st);
-      if (p.lanes == 16) return launch<TIN, TOUT, NORM, ROT, 8, 2>(p, st);
+      if (p.lanes == 8) return launch<TIN, TOUT, NORM, ROT, 4, 2>(p, sms, st);
+      if (p.lanes == 9) return launch<TIN, TOUT, NORM, ROT, 9, 1>(p, sms, st);
+      if (p.lanes == 14) return launch<TIN, TOUT, NORM, ROT, 14, 1>(p, sms, st);
+      if (p.lanes == 16) return launch<TIN, TOUT, NORM, ROT, 8, 2>(p, sms, st);
     }
-  return launch<TIN, TOUT, NORM, ROT, 0, 1>(p, st);
+  return launch<TIN, TOUT, NORM, ROT, 0, 1>(p, sms, st);
 }
 template <typename TIN, typename TOUT, int NORM>
-cudaError_t launch_rot(HeadsParams& p, int rot, cudaStream_t st) {
-  return rot == ROT_NONE    ? launch_lanes<TIN, TOUT, NORM, ROT_NONE>(p, st)
-         : rot == ROT_PAIRS ? launch_lanes<TIN, TOUT, NORM, ROT_PAIRS>(p, st)
-                            : launch_lanes<TIN, TOUT, NORM, ROT_HALVES>(p, st);
+cudaError_t launch_rot(HeadsParams& p, int rot, int sms, cudaStream_t st) {
+  return rot == ROT_NONE    ? launch_lanes<TIN, TOUT, NORM, ROT_NONE>(p, sms, st)
+         : rot == ROT_PAIRS ? launch_lanes<TIN, TOUT, NORM, ROT_PAIRS>(p, sms, st)
+                            : launch_lanes<TIN, TOUT, NORM, ROT_HALVES>(p, sms, st);
 }
 template <typename TIN, typename TOUT>
-cudaError_t launch_norm(HeadsParams& p, int norm, int rot, cudaStream_t st) {
-  return norm == LQ_NORM_NONE  ? launch_rot<TIN, TOUT, LQ_NORM_NONE>(p, rot, st)
-         : norm == LQ_NORM_RMS ? launch_rot<TIN, TOUT, LQ_NORM_RMS>(p, rot, st)
-                               : launch_rot<TIN, TOUT, LQ_NORM_LAYER>(p, rot, st);
+cudaError_t launch_norm(HeadsParams& p, int norm, int rot, int sms, cudaStream_t st) {
+  return norm == LQ_NORM_NONE  ? launch_rot<TIN, TOUT, LQ_NORM_NONE>(p, rot, sms, st)
+         : norm == LQ_NORM_RMS ? launch_rot<TIN, TOUT, LQ_NORM_RMS>(p, rot, sms, st)
+                               : launch_rot<TIN, TOUT, LQ_NORM_LAYER>(p, rot, sms, st);
 }
 
 // Strides over dimensions of one entry mean nothing; the others keep entries on 16-byte boundaries.
@@ -469,8 +456,12 @@ extern "C" lq_status lq_rope_create(const lq_rope_config* cfg, const double* fre
   if (lq_note_cuda(cudaGetDeviceCount(&ndev)) != cudaSuccess || device < 0 || device >= ndev) return LQ_ERR_CUDA;
   LqDeviceGuard guard(device);
   if (!guard.ok) return LQ_ERR_CUDA;
-  lq_rope* R = new (std::nothrow) lq_rope{cfg->axes, rot / 2, cfg->halves, device, nullptr, nullptr};
+  lq_rope* R = new (std::nothrow) lq_rope{cfg->axes, rot / 2, cfg->halves, device, 0, nullptr, nullptr};
   if (!R) return LQ_ERR_ALLOC;
+  if (lq_note_cuda(cudaDeviceGetAttribute(&R->sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) {
+    lq_rope_free(R);
+    return LQ_ERR_CUDA;
+  }
   if (rot > 0) {
     const size_t n = turn.size();
     if (lq_note_cuda(cudaMalloc((void**)&R->d_turn, n * sizeof(uint64_t))) != cudaSuccess ||
@@ -524,10 +515,11 @@ lq_status lq_heads_run(const lq_heads* q, const lq_heads* k, int32_t head_dim, i
   if ((s = check_places(p, head_dim, sequences, in_dtype, out_dtype)) != LQ_OK || !launch) return s;
   LqDeviceGuard guard(R->device);
   if (!guard.ok) return LQ_ERR_CUDA;
-  const int rot = R->pairs == 0 ? ROT_NONE : R->halves ? ROT_HALVES : ROT_PAIRS;
+  const int rot = R->pairs == 0 ? ROT_NONE : R->halves ? ROT_HALVES : ROT_PAIRS, sms = R->sms;
+  const bool f32_out = out_dtype == LQ_OUT_F32;
   const cudaError_t e =
-      in_dtype == LQ_OUT_F16 ? (out_dtype == LQ_OUT_F16 ? launch_norm<__half, __half>(p, norm, rot, st) : launch_norm<__half, float>(p, norm, rot, st))
-                             : (out_dtype == LQ_OUT_F16 ? launch_norm<float, __half>(p, norm, rot, st) : launch_norm<float, float>(p, norm, rot, st));
+      in_dtype == LQ_OUT_F16 ? (f32_out ? launch_norm<__half, float>(p, norm, rot, sms, st) : launch_norm<__half, __half>(p, norm, rot, sms, st))
+                             : (f32_out ? launch_norm<float, float>(p, norm, rot, sms, st) : launch_norm<float, __half>(p, norm, rot, sms, st));
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
 

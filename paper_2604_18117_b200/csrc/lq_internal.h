@@ -189,7 +189,7 @@ lq_status lq_launch_gemm_mx(const lq_layer* L, const lq_act* A, void* Y, lq_out_
 lq_status lq_gemm_mx_prepare(int device);
 lq_status lq_launch_wait_probe(int device, cudaStream_t st);   // bounded-wait self-test kernel
 struct lq_rope {
-  int axes, pairs, halves, device;
+  int axes, pairs, halves, device, sms;
   uint64_t* d_turn;   // [pairs] fraction of a turn a position, 2^64 = 1
   uint8_t* d_axis;    // [pairs]
 };
