@@ -265,7 +265,8 @@ lq_status lq_adapters_free(lq_adapters* set);
 
 /* Puts an adapter into a slot, or another one in its place; rank 0 empties the slot (A and B are then ignored).
  *   A_f16_dev  [K][rank] row-major half bits, device        B_f16_dev  [rank][N] row-major half bits, device
- *   scale      finite; applied to the product in fp32
+ *   scale      finite, below 2^96 in magnitude (UNSUPPORTED); applied to the product in fp32.  Where the scale times the largest entry of a
+ *              row's X A is below 2^-111, what is added loses bits
  * The set keeps its own copy.  Asynchronous on `cuda_stream`: forwards queued there earlier use what was there before,
  * later ones the new adapter; forwards on other streams must be ordered by the caller.  May be captured. */
 lq_status lq_adapters_set(lq_adapters* set, int32_t slot, int32_t rank, const void* A_f16_dev, const void* B_f16_dev, float scale,

@@ -440,6 +440,9 @@ extern "C" lq_status lq_adapters_set(lq_adapters* S, int32_t slot, int32_t rank,
   if (rank > S->max_rank) return LQ_ERR_UNSUPPORTED;
   if (rank > 0 && (!A || !B || (((uintptr_t)A | (uintptr_t)B) & 1) != 0)) return LQ_ERR_INVALID_ARG;
   if (!isfinite(scale)) return LQ_ERR_NUMERIC;
+  // A row's sums are below 2^46 (8192 products of halves), so their power of two is 2^-31 at least and scale / that a float; a larger scale
+  // would be an infinity, and nothing times it no number.
+  if (rank > 0 && fabsf(scale) >= 0x1p96f) return LQ_ERR_UNSUPPORTED;
   LqDeviceGuard guard(S->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   if (rank == 0)                     // nothing to lay out

@@ -465,3 +465,31 @@ def test_few_rows_of_wide_factors(rank, f32):
                 ref, bound = reference(S, X, Y0, ids, f32)
                 assert (np.abs(Y - ref) <= bound).all(), (K, M)
         S.free()
+
+
+@pytest.mark.parametrize("M", [20, 1600])
+@pytest.mark.parametrize("max_rank", [16, 128])
+def test_the_largest_scale_and_sums(M, max_rank):
+    """The largest sums of X A that halves make, under the largest scale: right where the result is a float, Y0 where B is zero.  Scales above
+    are refused."""
+    rng = np.random.default_rng(13)
+    K, N = 8192, 40
+    top = float(np.nextafter(np.float32(2.0 ** 96), np.float32(0)))
+    S = Set(rng, K, N, max_rank, [8], scales=[top])
+    A, Bf = np.full((K, 8), 65504, np.float16), np.zeros((8, N), np.float16)
+    Bf[0, 8:16], Bf[0, 16:24] = 2.0 ** -24, -2.0 ** -24
+    S.put(0, A, Bf, top, 0)
+    X = np.where(np.arange(M)[:, None] % 2 == 0, 65504, rng.integers(0, 2, (M, K))).astype(np.float16)
+    Y0 = rng.standard_normal((M, N)).astype(np.float32)
+    Y = forward(S, np.zeros(M, int), X, Y0, True)
+    ref, bound = reference(S, X, Y0, np.zeros(M, int), True)
+    assert np.array_equal(Y[:, :8], Y0[:, :8]) and np.array_equal(Y[:, 24:], Y0[:, 24:])
+    assert np.abs(ref).max() > 2.0 ** 116 and (np.abs(Y - ref) <= bound).all()
+    for scale in (2.0 ** 96, -2.0 ** 96, 3e38):
+        with pytest.raises(B.LqError) as e:
+            S.put(0, A, Bf, scale, 0)
+        assert e.value.code == 2
+    B.lq_adapters_set(S.h, 0, 0, None, None, 3e38, 0)       # an empty slot has none
+    S.ranks[0] = 0
+    assert np.array_equal(forward(S, np.zeros(M, int), X, Y0, True), Y0)
+    S.free()
