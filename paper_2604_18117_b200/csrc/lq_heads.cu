@@ -496,7 +496,7 @@ lq_status lq_heads_run(const lq_heads* q, const lq_heads* k, int32_t head_dim, i
   for (lq_out_dtype d : {in_dtype, out_dtype})
     if (d != LQ_OUT_F16 && d != LQ_OUT_F32) return LQ_ERR_INVALID_ARG;
   if (head_dim % 8 != 0 || head_dim > MAX_D) return LQ_ERR_UNSUPPORTED;
-  if (2 * R->pairs > head_dim || (R->pairs > 0 && !pos) || ((uintptr_t)pos & 3) != 0) return LQ_ERR_INVALID_ARG;
+  if (2 * R->pairs > head_dim || (R->pairs > 0 && (!pos || ((uintptr_t)pos & 3) != 0))) return LQ_ERR_INVALID_ARG;
   const long long rows = (long long)sequences * seq_len;
   if (rows > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
   HeadsParams p = {};

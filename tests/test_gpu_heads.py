@@ -383,6 +383,19 @@ def test_strides_backwards_and_far_apart(norm):
     B.lq_rope_free(rope)
 
 
+def test_positions_are_ignored_without_axes():
+    import torch
+    x = torch.ones(4 * 64, dtype=torch.float16, device="cuda")
+    side = B.lq_heads(x.data_ptr(), (0, 64, 0), x.data_ptr(), (0, 64, 0), 1)
+    for dims in ([], [0, 0]):
+        rope = B.lq_rope_create(B.lq_rope_config_default(dims), 0)
+        for pos in (None, 1, x.data_ptr() + 2):
+            B.lq_qk_norm_rope(side, None, 64, 1, 4, B.NORM_RMS, 0.0, rope, pos, B.OUT_F16, B.OUT_F16, 0)
+        torch.cuda.synchronize()
+        B.lq_rope_free(rope)
+    assert (x == 1).all()
+
+
 def test_the_most_heads_of_the_longest():
     for norm in ("rms", "layer"):
         Case(1, 1, 4095, 7, 256, norm, (256,)).run()
