@@ -379,7 +379,7 @@ lq_status take_side(const lq_heads* h, int sequences, int seq_len, lq_norm norm,
                               sequences == 1 ? 0 : h->out_seq, seq_len == 1 ? 0 : h->out_row, h->heads == 1 ? 0 : h->out_head};
   for (int64_t v : strides) {
     if (v % 8 != 0) return LQ_ERR_INVALID_ARG;
-    if (v > INT32_MAX / 32 * 32 || v < -INT32_MAX) return LQ_ERR_UNSUPPORTED;
+    if (v > INT32_MAX || v < -INT32_MAX) return LQ_ERR_UNSUPPORTED;
   }
   for (int i : {2, 5})                                       // (a warp steps over up to 32 heads)
     if (strides[i] > INT32_MAX / 32 || strides[i] < -(INT32_MAX / 32)) return LQ_ERR_UNSUPPORTED;

@@ -396,6 +396,37 @@ def test_positions_are_ignored_without_axes():
     assert (x == 1).all()
 
 
+@pytest.mark.parametrize("sequences", [1, 2])
+def test_the_longest_strides(sequences):
+    """The largest multiple of eight below 2^31, of rows and of sequences; the next one is refused."""
+    import torch
+    rng = np.random.default_rng(2)
+    D, apart = 8, 2 ** 31 - 8
+    x, y = (torch.empty(apart + D, dtype=torch.float16, device="cuda") for _ in range(2))
+    rows = rng.standard_normal((2, D)).astype(np.float16)
+    x[:D], x[apart:] = torch.from_numpy(rows[0]).cuda(), torch.from_numpy(rows[1]).cuda()
+    rope = B.lq_rope_create(B.lq_rope_config_default([]), 0)
+    S = 2 // sequences
+
+    def call(step, back=1):
+        at = [t.data_ptr() + (2 * apart if back < 0 else 0) for t in (x, y)]
+        strides = (back * step, back * step, 0)
+        side = B.lq_heads(at[0], strides, at[1], strides, 1)
+        B.lq_qk_norm_rope(side, None, D, sequences, S, B.NORM_RMS, 1e-6, rope, None, B.OUT_F16, B.OUT_F16, torch.cuda.current_stream().cuda_stream)
+
+    ref, bound = reference(rows[:, None, None], None, None, "rms", 1e-6, np.zeros(0, int), np.zeros(0), False, None, False)
+    for back in (1, -1):
+        y[:D] = y[apart:] = 9
+        call(apart, back)
+        torch.cuda.synchronize()
+        got = torch.stack([y[:D], y[apart:]]).float().cpu().numpy()
+        assert (np.abs(got - ref[:, 0, 0]) <= bound[:, 0, 0]).all(), back
+        with pytest.raises(B.LqError) as e:
+            call(apart + 8, back)
+        assert e.value.code == 2
+    B.lq_rope_free(rope)
+
+
 def test_the_most_heads_of_the_longest():
     for norm in ("rms", "layer"):
         Case(1, 1, 4095, 7, 256, norm, (256,)).run()
