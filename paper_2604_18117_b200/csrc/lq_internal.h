@@ -238,12 +238,17 @@ extern int g_lq_store_qb;    // option "store_qb": also write the branch activat
 #ifdef __CUDACC__
 // Launches `kernel` on `st`.  With the "overlap" option the launch carries programmatic stream serialization: the
 // kernel's CTAs may become resident and run their set-up (barriers, tensor memory) while the previous kernel on the
-// stream is still draining its last tiles; every kernel of this library executes griddepcontrol.wait after that set-up,
+// stream is still draining its last tiles.  Every kernel of this library executes griddepcontrol.wait after that set-up,
 // before it reads what an earlier kernel may write or writes global memory (weights, which no kernel writes, and the quantizer's
 // prefetch of X to the L2 come before it), and griddepcontrol.launch_dependents after the set-up, so that the chain
-// quantizer -> GEMM -> next quantizer overlaps its launch gaps and tails.  The layer's kernels are persistent (the whole grid
-// is resident at once), and a dependent of the others starts only when their last CTA has, so a waiting successor never holds an SM that a predecessor
-// CTA still needs.
+// quantizer -> GEMM -> next quantizer overlaps its launch gaps and tails.  Three kernels differ:
+//   lq_adapters_set_kernel   lets no dependent start early: what follows sees the adapter whole
+//   lq_adapters_down_kernel  lets its dependent, the up kernel, start behind its own wait
+//   lq_adapters_up_kernel    reads the map, the factors and Y0 before its wait, T and its rows' scales behind it
+// A kernel may read early only what was complete before the kernel right before it, and only because that one lets it start behind a wait
+// of its own: were the down kernel's launch_dependents moved up to its set-up, as elsewhere, the up kernel would read an old map and an old Y0.
+// The layer's kernels are persistent (the whole grid is resident at once), and a dependent of the others starts only when their last CTA
+// has, so a waiting successor never holds an SM that a predecessor CTA still needs.
 template <typename... KArgs, typename... Args>
 static inline cudaError_t lq_launch_grid(void (*kernel)(KArgs...), dim3 grid, int block, int cluster, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t lc = {};

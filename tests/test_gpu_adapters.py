@@ -493,3 +493,89 @@ def test_the_largest_scale_and_sums(M, max_rank):
     S.ranks[0] = 0
     assert np.array_equal(forward(S, np.zeros(M, int), X, Y0, True), Y0)
     S.free()
+
+
+@pytest.mark.parametrize("M,K,N,rank,f32", [(1600, 64, 512, 32, False), (2100, 72, 640, 128, True), (4096, 512, 2304, 128, False), (8192, 1152, 1152, 32, True),
+                                            (700, 256, 512, 24, False)])
+def test_many_rows_follow_what_changes_from_pass_to_pass(M, K, N, rank, f32):
+    """Map, factors, X and Y0 are other ones in each pass, written by the kernels right before, of which each lets the next one start early; nothing
+    waits on the host.  Queued, captured and replayed the bits are those of calls that wait for each other."""
+    import torch
+    rng = np.random.default_rng(M + rank)
+    passes, slots, dt = 5, 6, torch.float32 if f32 else torch.float16
+    S = Set(rng, K, N, rank, [rank] * slots)
+    m = B.lq_rowmap_create(M, slots, 0)
+    none = B.lq_rope_create(B.lq_rope_config_default([]), 0)
+    code = B.OUT_F32 if f32 else B.OUT_F16
+    ids = torch.empty(passes, M, dtype=torch.int32, device="cuda")
+    x = torch.empty(passes, M, K, dtype=torch.float16, device="cuda")
+    src = torch.empty(passes, M, N, dtype=dt, device="cuda")
+    y0, y = torch.empty(M, N, dtype=dt, device="cuda"), torch.empty(passes, M, N, dtype=dt, device="cuda")
+    A = [torch.from_numpy((rng.standard_normal((K, rank)) / np.sqrt(K)).astype(np.float16)).cuda() for _ in range(passes)]
+    Bf = [torch.from_numpy((rng.standard_normal((rank, N)) * 0.3).astype(np.float16)).cuda() for _ in range(passes)]
+
+    def fill(seed):
+        r = np.random.default_rng(seed)
+        for k in range(passes):                            # neighbours in one pass, scattered in the next
+            i = np.arange(M) * 7 // M - 1 if k % 2 else r.integers(-1, slots, M)
+            ids[k].copy_(torch.from_numpy(((i + seed) % (slots + 1) - 1).astype(np.int32)))
+            x[k].copy_(torch.from_numpy(r.standard_normal((M, K)).astype(np.float16)))
+            src[k].copy_(torch.from_numpy(r.standard_normal((M, N)).astype(np.float16)).to(dt))
+        y.fill_(7)
+        torch.cuda.synchronize()
+
+    first = [(torch.from_numpy(a).cuda(), torch.from_numpy(b).cuda()) for a, b in zip(S.A, S.B)]
+
+    def run(st, wait):
+        # (every run begins with the first factors in all slots)
+        calls = [lambda s=s, a=a, b=b: B.lq_adapters_set(S.h, s, rank, a.data_ptr(), b.data_ptr(), S.scales[s], st) for s, (a, b) in enumerate(first)]
+        for k in range(passes):
+            heads = lambda k=k: B.lq_qk_norm_rope(B.lq_heads(src[k].data_ptr(), (0, N, 64), y0.data_ptr(), (0, N, 64), N // 64), None, 64, 1, M, B.NORM_RMS,
+                                                  1e-6, none, None, code, code, st)
+            sort = lambda k=k: B.lq_rowmap_set(m, ids[k].data_ptr(), M, st)
+            put = lambda k=k: B.lq_adapters_set(S.h, k % slots, rank, A[k].data_ptr(), Bf[k].data_ptr(), 1.0 - k, st)
+            calls += [(heads, sort, put), (sort, put, heads), (put, heads, sort)][k % 3]
+            calls.append(lambda k=k: B.lq_adapters_forward(S.h, m, x[k].data_ptr(), y0.data_ptr(), y[k].data_ptr(), code, st))
+            calls.append(lambda k=k: B.lq_adapters_forward(S.h, m, x[k].data_ptr(), y[k].data_ptr(), y[k].data_ptr(), code, st))
+        for c in calls:
+            c()
+            if wait:
+                torch.cuda.synchronize()
+
+    side = torch.cuda.Stream()
+    graph = None
+    for seed in range(3):
+        fill(seed)
+        run(side.cuda_stream, True)
+        want = y.clone()
+        for turn in range(6):
+            y.fill_(7)
+            torch.cuda.synchronize()
+            run(side.cuda_stream, False)
+            torch.cuda.synchronize()
+            assert torch.equal(y, want), (seed, turn)
+        if graph is None:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                run(torch.cuda.current_stream().cuda_stream, False)
+        for turn in range(6):
+            y.fill_(7)
+            torch.cuda.synchronize()
+            graph.replay()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(y, want), (seed, turn, "replayed")
+    # the last pass against the formula, twice the adapters on its Y0
+    look = rng.permutation(M)[:300]
+    k = passes - 1
+    for j in range(passes):
+        S.A[j], S.B[j], S.scales[j] = A[j].cpu().numpy(), Bf[j].cpu().numpy(), 1.0 - j
+    X, i, Y0 = x[k].cpu().numpy()[look], ids[k].cpu().numpy()[look], y0.cpu().numpy()[look]
+    once, bound = reference(S, X, Y0, i, f32)
+    ref, more = reference(S, X, once, i, f32)
+    assert (np.abs(y[k].cpu().numpy()[look] - ref) <= bound + more).all()
+    assert B.lq_get_device_status(0)[0] == 0
+    del graph
+    B.lq_rowmap_free(m)
+    B.lq_rope_free(none)
+    S.free()
