@@ -34,7 +34,7 @@ struct lq_adapters {
 };
 struct lq_rowmap {
   int M_max, slots, device, M, sms;
-  int* d_ntiles;                       // [4]: tiles of 128 rows, of 16, rows that were sorted, 0
+  int* d_ntiles;                       // [4]: tiles of 128 rows, of 16, rows that were sorted, 1 from a down kernel's wait to its up kernel's end
   LqAdTile *d_tiles, *d_small;         // (tiles of 16 rows only up to LQ_AD_SMALL_M rows)
   int* d_perm;                         // [M_max]
   __half* d_T;                         // [M_max + 128][LQ_AD_TROW], in the order of perm

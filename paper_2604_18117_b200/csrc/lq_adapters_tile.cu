@@ -34,6 +34,12 @@ __device__ __forceinline__ float4 ld_peer_v4(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
+__device__ __forceinline__ void st_release(int* p, int v) { asm volatile("st.release.gpu.global.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory"); }
+__device__ __forceinline__ int ld_acquire(const int* p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -75,6 +81,7 @@ struct DownParams {
   __half* T;
   float* rscale;
   int32_t* status;
+  int* ready;
   int rp, k_stages, ring, tmem_cols, M;
 };
 
@@ -109,7 +116,10 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   grid_dependency_wait();
-  grid_launch_dependents();          // (behind the wait: the up kernel counts on what came before this one to be complete when it starts)
+  // All that came before is complete: the up kernel may read it as soon as it starts.  (A word, and not the start alone, tells it so: where
+  // another thread has put a kernel on the stream between the two, that one's start lets the up kernel start.)
+  if (blockIdx.x == 0 && threadIdx.x == 96) st_release(p.ready, 1);
+  grid_launch_dependents();
 
   // (a tile behind the last one holds anything: it is asked for together with their number, which saves a trip)
   LqAdTile tile = p.tiles[blockIdx.x / SPLIT];
@@ -254,6 +264,7 @@ struct UpParams {
   const float* rscale;
   void* Y;
   int32_t* status;
+  int* ready;
   int N, Npad, chunks, in_place, M;
 };
 
@@ -277,6 +288,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
   __shared__ __align__(8) uint64_t bars[NBAR];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
+  __shared__ int early;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
@@ -287,14 +299,15 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
     prefetch_map(&tmT); prefetch_map(&tmUp); prefetch_maps(tmY);
   }
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), 2 * UP_COLS);
+  if (threadIdx.x == 96) early = ld_acquire(p.ready);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   grid_launch_dependents();
-  // The down kernel lets this one start when all that came before has completed: the map, the factors and Y0 are there.  Only T and its rows' scales
-  // are waited for (and every CTA waits, so that who waits for this kernel has waited for that one).
-  if (warp == 3) grid_dependency_wait();
+  // Where the down kernel has said that all that came before it has completed, the map, the factors and Y0 are there, and only T and its rows' scales
+  // are waited for (and every CTA waits, so that who waits for this kernel has waited for that one).  Else everything is.
+  if (warp == 3 || !early) grid_dependency_wait();
 
   const int ntiles = lq_ad_tiles_of<false>(p.ntiles, p.M, p.status);
   const long long total = (long long)ntiles * p.chunks;
@@ -533,6 +546,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
     tc_fence_after();
     tmem_dealloc(tmem, 2 * UP_COLS);
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.ready = 0;  // (a CTA that starts later than this waits, for nothing any more)
 }
 
 constexpr int DOWN_SMEM = 110 * 1024;                     // two CTAs an SM
@@ -578,7 +592,7 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
   if ((s = rows_of(&tmX, X, (uint64_t)S->K * 2)) != LQ_OK || (s = rows_of(&tmY, Y0, (uint64_t)S->N * (dt == LQ_OUT_F32 ? 4 : 2))) != LQ_OK) return s;
   int32_t* status = lq_device_status_ptr(S->device);
   if (!status) return LQ_ERR_CUDA;
-  DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, S->rp, lq_ceil_div(S->K, 64), 1, 32, R->M};
+  DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, R->d_ntiles + 3, S->rp, lq_ceil_div(S->K, 64), 1, 32, R->M};
   // K is shared by as many CTAs as fill the SMs twice over, each with at least two stages (us with the map by 1, 2, 4 and 8 of them, 5600 x 2240, rank 128: 4096 rows
   // 60.2, 44.6, 38.9, 38.0; 8192 rows 70.0, 57.4, 53.9, 63.2; 16384 rows 88.4, 82.8, 91.6, 132; 32768 rows 142, 150, 203, 289)
   const int tiles = lq_ceil_div(R->M, BM);
@@ -589,7 +603,7 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
                   : split == 4 ? launch_down<4>(S, R, tmX, d, st)
                                : launch_down<8>(S, R, tmX, d, st);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
-  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y, R->M};
+  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, R->d_ntiles + 3, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y, R->M};
   if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, tmY, u, st) : launch_up<true, 2>(S, R, tmY, u, st);
   else e = S->rp <= 64 ? launch_up<false, 1>(S, R, tmY, u, st) : launch_up<false, 2>(S, R, tmY, u, st);
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;

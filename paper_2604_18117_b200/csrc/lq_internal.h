@@ -243,10 +243,11 @@ extern int g_lq_store_qb;    // option "store_qb": also write the branch activat
 // prefetch of X to the L2 come before it), and griddepcontrol.launch_dependents after the set-up, so that the chain
 // quantizer -> GEMM -> next quantizer overlaps its launch gaps and tails.  Three kernels differ:
 //   lq_adapters_set_kernel   lets no dependent start early: what follows sees the adapter whole
-//   lq_adapters_down_kernel  lets its dependent, the up kernel, start behind its own wait
-//   lq_adapters_up_kernel    reads the map, the factors and Y0 before its wait, T and its rows' scales behind it
-// A kernel may read early only what was complete before the kernel right before it, and only because that one lets it start behind a wait
-// of its own: were the down kernel's launch_dependents moved up to its set-up, as elsewhere, the up kernel would read an old map and an old Y0.
+//   lq_adapters_down_kernel  lets its dependent start behind its own wait, and first sets a word of the map's (release, device scope)
+//   lq_adapters_up_kernel    reads the map, the factors and Y0 before its wait if it finds that word set (acquire), T and its rows'
+//                            scales behind it; its last act is to clear the word
+// A kernel may read early only what it knows to be complete.  That it has started tells nothing: calls of distinct handles may come from
+// distinct threads to one stream, and the kernel right before it, which lets it start, need not be the one that its caller launched last.
 // The layer's kernels are persistent (the whole grid is resident at once), and a dependent of the others starts only when their last CTA
 // has, so a waiting successor never holds an SM that a predecessor CTA still needs.
 template <typename... KArgs, typename... Args>

@@ -579,3 +579,62 @@ def test_many_rows_follow_what_changes_from_pass_to_pass(M, K, N, rank, f32):
     B.lq_rowmap_free(m)
     B.lq_rope_free(none)
     S.free()
+
+
+@pytest.mark.parametrize("K,N,rank,f32", [(64, 512, 32, False), (640, 1152, 128, True)])
+def test_two_threads_on_one_stream(K, N, rank, f32):
+    """Two threads, each with maps and buffers of its own, one set, one stream: a launch of the other may come between any two of a call's.  The map
+    changes from call to call, and between maps of one thread the rows' number too."""
+    import threading
+    import torch
+    rng = np.random.default_rng(14)
+    dt, code, passes = torch.float32 if f32 else torch.float16, B.OUT_F32 if f32 else B.OUT_F16, 12
+    S = Set(rng, K, N, rank, [rank] * 4)
+    none = B.lq_rope_create(B.lq_rope_config_default([]), 0)
+    side = torch.cuda.Stream()
+
+    class Work:
+        def __init__(self, seed, sizes):
+            r = torch.Generator(device="cuda").manual_seed(seed)
+            M = max(sizes)
+            self.sizes = [sizes[k % len(sizes)] for k in range(passes)]
+            self.map = B.lq_rowmap_create(M, 4, 0)
+            self.ids = torch.randint(-1, 4, (passes, M), generator=r, device="cuda", dtype=torch.int32)
+            self.ids[1::2] = self.ids[1::2].sort(dim=1).values
+            self.x = torch.randn(passes, M, K, generator=r, device="cuda").half()
+            self.src = torch.randn(passes, M, N, generator=r, device="cuda").to(dt)
+            self.y = torch.full((passes, M, N), 7.0, dtype=dt, device="cuda")
+
+        def run(self, wait=False):
+            st = side.cuda_stream
+            for k, M in enumerate(self.sizes):
+                y = self.y[k].data_ptr()
+                B.lq_rowmap_set(self.map, self.ids[k].data_ptr(), M, st)
+                B.lq_qk_norm_rope(B.lq_heads(self.src[k].data_ptr(), (0, N, 64), y, (0, N, 64), N // 64), None, 64, 1, M, B.NORM_RMS, 1e-6, none, None,
+                                  code, code, st)
+                B.lq_adapters_forward(S.h, self.map, self.x[k].data_ptr(), y, y, code, st)
+                if wait:
+                    torch.cuda.synchronize()
+
+    work = [Work(1, (1800, 2500)), Work(2, (3000, 1700, 1600))]
+    torch.cuda.synchronize()
+    want = []
+    for w in work:
+        w.run(wait=True)
+        want.append(w.y.clone())
+    for turn in range(25):
+        for w in work:
+            w.y.fill_(7)
+        torch.cuda.synchronize()
+        threads = [threading.Thread(target=w.run) for w in work]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        torch.cuda.synchronize()
+        assert all(torch.equal(w.y, v) for w, v in zip(work, want)), turn
+    assert B.lq_get_device_status(0)[0] == 0
+    for w in work:
+        B.lq_rowmap_free(w.map)
+    B.lq_rope_free(none)
+    S.free()
