@@ -137,6 +137,29 @@ def test_rows_heads_and_types(fin, fout, Bn, S, hq, hk, D, halves):
     Case(Bn, S, hq, hk, D, "rms", (D - 8,), halves=halves, fin=fin, fout=fout, bhsd=S % 2 == 1).run()
 
 
+# Heads of 64, 72, 112 and 128 entries, turned as a whole or not at all, have instances of their own under an RMS norm; the others have the
+# general one.  Rows enough for two a block (1776 and more on 148 SMs, the last block with one), heads enough for a warp to take more steps
+# than it has loads in flight (three: eight, three, two, four heads a step, and one or more of the general form).
+LONG = {64: 40, 72: 16, 112: 10, 128: 20, 80: 13, 96: 15, 160: 7, 256: 5}
+
+
+@pytest.mark.parametrize("fin,fout", [("f16", "f16"), ("f16", "f32"), ("f32", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("turned", ["none", "pairs", "halves"])
+@pytest.mark.parametrize("D", [64, 72, 112, 128])
+def test_long_walks_of_the_instances_by_size(D, turned, fin, fout):
+    dims = () if turned == "none" else (D - 24, 24) if turned == "pairs" else (D,)
+    Case(1, 1777, LONG[D], LONG[D], D, "rms", dims, halves=turned == "halves", fin=fin, fout=fout).run()
+    Case(3, 7, LONG[D], 3, D, "rms", dims, halves=turned == "halves", fin=fin, fout=fout, bhsd=True, weight=False).run()
+
+
+@pytest.mark.parametrize("fin,fout", [("f16", "f16"), ("f16", "f32"), ("f32", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("D,dims,norm", [(64, (64,), "layer"), (72, (40,), "rms"), (80, (80,), "rms"), (96, (64,), "layer"), (128, (128,), "none"),
+                                         (160, (160,), "none"), (256, (), "layer"), (112, (112,), "layer")])
+def test_long_walks_of_the_general_instance(D, dims, norm, fin, fout):
+    Case(1, 1777, LONG[D], LONG[D], D, norm, dims, halves=D % 64 == 0, fin=fin, fout=fout).run()
+    Case(2, 889, LONG[D] + 5, LONG[D], D, norm, dims, halves=D % 64 == 0, fin=fin, fout=fout, in_place=fin == fout).run()
+
+
 @pytest.mark.parametrize("fin", ["f16", "f32"])
 @pytest.mark.parametrize("halves", [False, True])
 def test_in_place(fin, halves):

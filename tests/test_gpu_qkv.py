@@ -242,3 +242,52 @@ def test_weights_and_positions_among_the_values_are_refused(adapters):
     assert code() == 0
     torch.cuda.synchronize()
     b.free()
+
+
+def _within(b, got):
+    ref, tol = b.formula(), 4e-5 if b.f32 else 4 * 2.0 ** -11          # as in the first test above
+    scale = np.abs(ref.reshape(b.M, -1, b.D)).max(-1, keepdims=True)
+    return (np.abs(got.astype(np.float64) - ref).reshape(b.M, -1, b.D) / scale).max() <= tol
+
+
+@pytest.mark.parametrize("M,sequences,f32", [(60, 60, False), (130, 2, True), (1900, 1, False)])
+def test_without_adapters_against_the_formula(M, sequences, f32):
+    import torch
+    b = Block(M, sequences, f32)
+    b.one_call(b.y[0], torch.cuda.current_stream().cuda_stream, adapters=False)
+    torch.cuda.synchronize()
+    b.ids[:] = -1
+    assert _within(b, b.y[0].cpu().numpy())
+    b.free()
+
+
+def test_one_layer_set_and_table_on_two_streams():
+    """What a server has once for all its streams: layer, adapters and rotation.  Maps, activations and outputs are each stream's own; one stream has
+    few rows, the other many."""
+    import torch
+    one, two = Block(300, 2, True, seed=1), Block(2050, 1, True, seed=2)
+    for f, h in ((B.lq_act_free, two.act), (B.lq_layer_free, two.h), (B.lq_adapters_free, two.set), (B.lq_rope_free, two.rope)):
+        f(h)
+    two.layer, two.h, two.set, two.rope, two.A, two.Bf = one.layer, one.h, one.set, one.rope, one.A, one.Bf
+    two.act = B.lq_act_create(two.h, two.M, 0)
+    two.qkv = B.lq_qkv(two.D, two.hq, two.hk, two.seqs, B.NORM_RMS, 1e-6, two.rope, two.p.data_ptr(), two.wd[0].data_ptr(), two.wd[1].data_ptr())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for b in (one, two):
+        b.one_by_one(b.y[1], torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for turn in range(10):
+        for b in (one, two):
+            b.y[0].fill_(7)
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for b, s in zip((one, two), streams):
+                b.one_call(b.y[0], s.cuda_stream)
+        torch.cuda.synchronize()
+        for b in (one, two):
+            assert torch.equal(b.y[0], b.y[1]), turn
+    for b in (one, two):
+        assert _within(b, b.y[0].cpu().numpy())
+    B.lq_act_free(two.act)
+    B.lq_rowmap_free(two.map)
+    one.free()
