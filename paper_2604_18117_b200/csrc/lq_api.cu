@@ -25,7 +25,10 @@ int g_lq_overlap = 1;
 static thread_local cudaError_t t_last_cuda_error = cudaSuccess;
 
 cudaError_t lq_note_cuda(cudaError_t e) {
-  if (e != cudaSuccess) t_last_cuda_error = e;
+  if (e != cudaSuccess) {
+    t_last_cuda_error = e;
+    cudaGetLastError();            // (else a later call, whose launch succeeds, would find this failure and take it for its own)
+  }
   return e;
 }
 
@@ -409,7 +412,7 @@ int32_t* lq_device_status_ptr(int device) {
     cudaGetDevice(&prev);
     if (cudaSetDevice(device) != cudaSuccess) return nullptr;
     int32_t* p = nullptr;
-    if (cudaMalloc(&p, 2 * sizeof(int32_t)) != cudaSuccess) { cudaSetDevice(prev); return nullptr; }
+    if (lq_note_cuda(cudaMalloc(&p, 2 * sizeof(int32_t))) != cudaSuccess) { cudaSetDevice(prev); return nullptr; }
     cudaMemset(p, 0, 2 * sizeof(int32_t));
     g_status[device] = p;
     cudaSetDevice(prev);
@@ -452,7 +455,7 @@ static void layer_free_device(lq_layer* L) {
 
 template <typename T>
 static lq_status upload(T** dptr, const std::vector<T>& h) {
-  if (cudaMalloc((void**)dptr, h.size() * sizeof(T)) != cudaSuccess) return LQ_ERR_ALLOC;
+  if (lq_note_cuda(cudaMalloc((void**)dptr, h.size() * sizeof(T))) != cudaSuccess) return LQ_ERR_ALLOC;
   CUDA_OK(cudaMemcpy(*dptr, h.data(), h.size() * sizeof(T), cudaMemcpyHostToDevice));
   return LQ_OK;
 }
@@ -678,14 +681,14 @@ extern "C" lq_status lq_act_create(const lq_layer* L, int32_t M_max, int device,
   A->device = device; A->main_kind = L->main_kind; A->M = 0;
   if (cudaSetDevice(device) != cudaSuccess) { delete A; return LQ_ERR_CUDA; }
   const size_t Mp = A->Mpad, Kp = A->Kpad, Kx = (size_t)A->planes * Kp;   // Kx: bytes per row of the main codes
-  bool ok = cudaMalloc((void**)&A->d_qx8, Mp * Kx) == cudaSuccess &&
-            cudaMalloc((void**)&A->d_sx, (size_t)A->Gpad * Mp * sizeof(float)) == cudaSuccess &&
-            cudaMalloc((void**)&A->d_qb, Mp * Kp) == cudaSuccess &&
-            cudaMalloc((void**)&A->d_sXb, Mp * sizeof(float)) == cudaSuccess &&
-            cudaMalloc((void**)&A->d_tq, Mp * A->tq_stride) == cudaSuccess &&
-            cudaMalloc((void**)&A->d_sT, Mp * sizeof(float)) == cudaSuccess &&
-            (!A->mx || cudaMalloc((void**)&A->d_sfa, (Mp / 128) * (Kx / 128) * 512) == cudaSuccess) &&
-            (!(A->mxfp || A->a8) || cudaMalloc((void**)&A->d_sft, (Mp / 128) * 512 * (A->tq_stride / LQ_RCONT)) == cudaSuccess);
+  bool ok = lq_note_cuda(cudaMalloc((void**)&A->d_qx8, Mp * Kx)) == cudaSuccess &&
+            lq_note_cuda(cudaMalloc((void**)&A->d_sx, (size_t)A->Gpad * Mp * sizeof(float))) == cudaSuccess &&
+            lq_note_cuda(cudaMalloc((void**)&A->d_qb, Mp * Kp)) == cudaSuccess &&
+            lq_note_cuda(cudaMalloc((void**)&A->d_sXb, Mp * sizeof(float))) == cudaSuccess &&
+            lq_note_cuda(cudaMalloc((void**)&A->d_tq, Mp * A->tq_stride)) == cudaSuccess &&
+            lq_note_cuda(cudaMalloc((void**)&A->d_sT, Mp * sizeof(float))) == cudaSuccess &&
+            (!A->mx || lq_note_cuda(cudaMalloc((void**)&A->d_sfa, (Mp / 128) * (Kx / 128) * 512)) == cudaSuccess) &&
+            (!(A->mxfp || A->a8) || lq_note_cuda(cudaMalloc((void**)&A->d_sft, (Mp / 128) * 512 * (A->tq_stride / LQ_RCONT))) == cudaSuccess);
   if (!ok) { lq_act_free(A); return LQ_ERR_ALLOC; }
   // padding rows/columns are read by the GEMM's tiles: start from defined contents
   cudaMemset(A->d_qx8, 0, Mp * Kx);
@@ -782,12 +785,12 @@ static lq_status forward_host(const lq_layer* L, lq_act* A, const void* Xh, int3
   if (dt != LQ_OUT_F16 && dt != LQ_OUT_F32) return LQ_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   CUDA_OK(cudaSetDevice(A->device));
-  if (!A->d_Xstage && cudaMalloc(&A->d_Xstage, (size_t)A->M_max * A->K * 2) != cudaSuccess) return LQ_ERR_ALLOC;
+  if (!A->d_Xstage && lq_note_cuda(cudaMalloc(&A->d_Xstage, (size_t)A->M_max * A->K * 2)) != cudaSuccess) return LQ_ERR_ALLOC;
   // sized once, for the wider output type: it is never freed or re-allocated while an earlier call's copies
   // may still be queued
   const size_t ybytes = (size_t)A->M_max * A->N * 4;
   if (!A->d_Ystage) {
-    if (cudaMalloc(&A->d_Ystage, ybytes) != cudaSuccess) return LQ_ERR_ALLOC;
+    if (lq_note_cuda(cudaMalloc(&A->d_Ystage, ybytes)) != cudaSuccess) return LQ_ERR_ALLOC;
     A->ystage_bytes = ybytes;
   }
   // Rows are independent, so the call is pipelined over row chunks: while chunk c is computed on the caller's

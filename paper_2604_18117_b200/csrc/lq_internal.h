@@ -157,7 +157,8 @@ struct lq_act {
   int block0;                  // a view's first row / 128 (tmA and tmT begin there, tmSfa and tmSft at the record's first row)
 };
 
-// remembers the last failing CUDA runtime code (per host thread) for lq_last_cuda_error(); returns its argument
+// remembers the last failing CUDA runtime code (per host thread) for lq_last_cuda_error(), and takes it off the runtime's own record;
+// returns its argument
 cudaError_t lq_note_cuda(cudaError_t e);
 
 // Makes `device` the calling thread's current one and puts the one before back at the end of the scope.

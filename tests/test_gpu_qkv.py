@@ -291,3 +291,19 @@ def test_one_layer_set_and_table_on_two_streams():
     B.lq_act_free(two.act)
     B.lq_rowmap_free(two.map)
     one.free()
+
+
+def test_a_refused_allocation_is_not_a_later_calls_error():
+    """A set, or a record, that no GPU has room for is refused; the calls behind it are what they were."""
+    import torch
+    b = Block(64, 2, False)
+    st = torch.cuda.current_stream().cuda_stream
+    b.one_by_one(b.y[1], st)
+    for create in (lambda: B.lq_adapters_create(8192, 1 << 20, 128, 1023, 0), lambda: B.lq_act_create(b.h, 1 << 30, 0)):
+        with pytest.raises(B.LqError) as e:
+            create()
+        assert e.value.code == 3
+        b.one_call(b.y[0], st)
+        torch.cuda.synchronize()
+        assert torch.equal(b.y[0], b.y[1])
+    b.free()
