@@ -279,13 +279,15 @@ lq_status lq_rowmap_free(lq_rowmap* map);
 
 /* Sorts the rows by adapter (stable; on the device, so a captured graph sorts anew on each replay what the array then holds).
  *   row_adapter_dev  [M] int32, device: the slot of each row; anything outside 0 .. slots - 1 means none
- *   M                1 <= M <= M_max; the rows of every forward until the next call.  A replayed graph that sorts leaves its own rows in the map: a forward
- *                    of another M behind it needs a call before it (without one it writes nothing, and lq_get_device_status says INVALID_ARG)
+ *   M                1 <= M <= M_max; the rows of every forward until the next call.  A replayed graph that sorts leaves its own rows in the
+ *                    map: a forward of another M behind it needs a call before it (without one it writes nothing, and lq_get_device_status
+ *                    says INVALID_ARG)
  * Asynchronous on `cuda_stream`. */
 lq_status lq_rowmap_set(lq_rowmap* map, const int32_t* row_adapter_dev, int32_t M, void* cuda_stream);
 
 /* Y = Y0 + the rows' adapters.  Products and sums in fp32; the rank-r intermediate travels as two halves under a power-of-two
- * scale of its row (22 bits); rounded once to `dtype`.
+ * scale of its row (22 bits of the row's largest entry); rounded once to `dtype`.  Beside an fp32 Y0 the result can be some four times
+ * farther from the exact one than fp32 products and sums throughout (relative errors of 1e-7 to 4e-7), or nearer.
  *   X_f16_dev  [M][K] row-major half, device, 16-byte aligned, finite
  *   Y0_dev     [M][N] row-major half or float per `dtype`, device, 16-byte aligned: the projection's output
  *   Y_dev      the same shape and type: Y0_dev itself (rows without an adapter are then left alone) or memory apart from it
@@ -336,9 +338,11 @@ typedef struct {
   const void* in;                          /* device, 16-byte aligned; half or float per in_dtype                     */
   void* out;                               /* device, 16-byte aligned; half or float per out_dtype; `in` itself, with its strides and
                                               type (INVALID_ARG otherwise), or memory apart from all inputs           */
-  int64_t in_seq, in_row, in_head;         /* strides in elements, multiples of 8, below 2^31, a head's below 2^26 (the memory they span may be larger) */
-  int64_t out_seq, out_row, out_head;      /* no two outputs of the call on one place, none on an input (INVALID_ARG; UNSUPPORTED where dimensions run
-                                              through one another too often to tell); may be negative, like those of `in` */
+  int64_t in_seq, in_row, in_head;         /* strides in elements, multiples of 8, below 2^31, a head's below 2^26 (the memory they span
+                                              may be larger)                                                          */
+  int64_t out_seq, out_row, out_head;      /* no two outputs of the call on one place, none on an input (INVALID_ARG;
+                                              UNSUPPORTED where dimensions run through one another too often to tell);
+                                              may be negative, like those of `in`                                     */
   const float* weight;                     /* [head_dim] device, 16-byte aligned, or NULL (ones); NULL without a norm */
   const float* bias;                       /* [head_dim] device, 16-byte aligned, or NULL (zeros); LQ_NORM_LAYER only */
   int32_t heads;                           /* 1 .. 4096                                                               */

@@ -3,9 +3,9 @@
 // A map sorts the rows of a batch by adapter (stable) and cuts them into tiles of rows of one adapter; every projection of a step
 // uses it.  This file has the map, the set of adapters, and the forward for few rows; lq_adapters_tile.cu has the one for many.
 //
-// T = X A is summed in fp32 and enters the second product as two halves, hi + lo, under a power of two of its row: 22 bits of the row's largest entry, at
-// the price of a second MMA for each 16 of the rank, which no form is bound by.  (One half would round T to 11 bits, as much as an fp16 output is
-// rounded, and too much for an fp32 one.)
+// T = X A is summed in fp32 and enters the second product as two halves, hi + lo, under a power of two of its row: 22 bits of the row's
+// largest entry, at the price of a second MMA for each 16 of the rank, which no form is bound by.  (One half would round T to 11 bits, as
+// much as an fp16 output is rounded, and too much for an fp32 one.)
 #include <math.h>
 
 #include <algorithm>
@@ -20,13 +20,16 @@ namespace {
 
 constexpr int MAX_SLOTS = 1023;      // bins of the sort: the slots and "none"
 constexpr int WARPS = 8;
-constexpr int ROWMAP_SINGLE = 4096;  // most rows that one block sorts; more: eight blocks (us: 2048 rows 4.2 / 5.5, 8192 rows 6.6 / 5.7, 32768 rows 18.4 / 7.1)
+// most rows that one block sorts; more: eight blocks (us: 2048 rows 4.2 / 5.5, 8192 rows 6.6 / 5.7, 32768 rows 18.4 / 7.1)
+constexpr int ROWMAP_SINGLE = 4096;
 
 // ---- the map: a stable counting sort by one block, or by a cluster of them -----------------------------------------------
-// Each warp counts the adapters of its own run of rows, then places them behind those of the warps before it.  What this costs is latency: up to eight loads of a
-// warp are in flight together, a run of up to 256 rows is read once, and many rows are shared by eight blocks.
+// Each warp counts the adapters of its own run of rows, then places them behind those of the warps before it.  What this costs is latency:
+// up to eight loads of a warp are in flight together, a run of up to 256 rows is read once, and many rows are shared by eight blocks.  (64
+// registers are all that 1024 threads can have; the form of eight blocks spills 52 bytes.)
 template <int BLOCKS>
-__global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int M, int slots, int* perm, LqAdTile* tiles, LqAdTile* small, int* ntiles) {
+__global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int M, int slots, int* perm, LqAdTile* tiles, LqAdTile* small,
+                                                         int* ntiles) {
   extern __shared__ int count[];     // [32][slots + 1]
   __shared__ int scan_rows[32], scan_tiles[32], total[MAX_SLOTS + 1];
   constexpr int AHEAD = 8;
@@ -62,7 +65,8 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     }
   }
   __syncthreads();
-  // thread b: rows and tiles of bin b, and where they begin.  Tiles of 128 rows count from bit 12 on, tiles of 16, of which there are fewer than 4096, below it
+  // thread b: rows and tiles of bin b, and where they begin.  Tiles of 128 rows count from bit 12 on, tiles of 16, of which there are fewer
+  // than 4096, below it
   int rows = 0, before = 0;
   if (tid < bins)
 #pragma unroll
@@ -74,7 +78,8 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
     if (tid < bins) {
       int u[BLOCKS];
 #pragma unroll
-      for (int c = 0; c < BLOCKS; ++c) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(u[c]) : "r"(peer_smem(smem_u32(total + tid), c)) : "memory");
+      for (int c = 0; c < BLOCKS; ++c)
+        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(u[c]) : "r"(peer_smem(smem_u32(total + tid), c)) : "memory");
 #pragma unroll
       for (int c = 0; c < BLOCKS; ++c) {
         before += c < block ? u[c] : 0;
@@ -82,7 +87,8 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
       }
     }
   }
-  const int large = (rows + LQ_AD_TILE - 1) / LQ_AD_TILE, little = M <= LQ_AD_SMALL_M ? (rows + LQ_AD_SMALL_TILE - 1) / LQ_AD_SMALL_TILE : 0, nt = large << 12 | little;
+  const int large = (rows + LQ_AD_TILE - 1) / LQ_AD_TILE, little = M <= LQ_AD_SMALL_M ? (rows + LQ_AD_SMALL_TILE - 1) / LQ_AD_SMALL_TILE : 0;
+  const int nt = large << 12 | little;
   int a = rows, b = nt;
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
@@ -105,7 +111,8 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
   if (tid < bins) {
     const int at0 = a - rows + (warp > 0 ? scan_rows[warp - 1] : 0);
     const int tile0 = b - nt + (warp > 0 ? scan_tiles[warp - 1] : 0), adapter = tid < slots ? tid : -1;
-    for (int i = block; i < large; i += BLOCKS) tiles[(tile0 >> 12) + i] = LqAdTile{adapter, at0 + i * LQ_AD_TILE, min(LQ_AD_TILE, rows - i * LQ_AD_TILE), -1};
+    for (int i = block; i < large; i += BLOCKS)
+      tiles[(tile0 >> 12) + i] = LqAdTile{adapter, at0 + i * LQ_AD_TILE, min(LQ_AD_TILE, rows - i * LQ_AD_TILE), -1};
     for (int i = block; i < little; i += BLOCKS)
       small[(tile0 & 0xFFF) + i] = LqAdTile{adapter, at0 + i * LQ_AD_SMALL_TILE, min(LQ_AD_SMALL_TILE, rows - i * LQ_AD_SMALL_TILE), -1};
     int c[32], at = at0 + before;
@@ -148,8 +155,8 @@ __global__ void __launch_bounds__(1024) lq_rowmap_kernel(const int32_t* ids, int
 }
 
 // ---- a slot's new adapter in the forwards' layouts ----------------------------------------------------------------------
-__global__ void __launch_bounds__(256) lq_adapters_set_kernel(__half* down, __half* up, LqAdMeta* meta, const __half* A, const __half* B, int K, int N, int Npad,
-                                                              int rp, int rank, float scale) {
+__global__ void __launch_bounds__(256) lq_adapters_set_kernel(__half* down, __half* up, LqAdMeta* meta, const __half* A, const __half* B, int K,
+                                                              int N, int Npad, int rp, int rank, float scale) {
   grid_dependency_wait();            // (no launch_dependents: what follows sees the adapter whole)
   const long long n_down = (long long)rp * K, n_up = (long long)Npad * rp, step = (long long)gridDim.x * blockDim.x;
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n_down + n_up; i += step) {
@@ -173,7 +180,8 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int BYTES, bool L1 = false>     // L1: a copy takes half of a 32-byte sector and another one the rest (1365 rows, 1160 x 2312, fp32: 20.7 us, without 22.7)
+// L1: a copy takes half of a 32-byte sector and another one the rest (1365 rows, 1160 x 2312, fp32: 20.7 us, without 22.7)
+template <int BYTES, bool L1 = false>
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
   if constexpr (BYTES == 16 && L1) asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
   else if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -183,16 +191,18 @@ __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_al
 // bytes of a warp's places for what is fetched ahead
 __host__ __device__ constexpr int adapters_stage(int rp, bool f32) { return ((rp <= 32 ? 4 : 0) + (f32 ? 4 : 2)) * 512; }
 
-// The forward for few rows: a cluster of CTAs has 16 rows of one adapter, shares out K for the first product, joins the sums through distributed shared memory
-// (each CTA all of them, always in the same order) and shares out the columns for the second.  A chain of latencies: one launch, and operands straight from
-// global memory into the fragments of mma.sync (tiles of 16 rows would leave tcgen05's 128 empty).  The order of a product's inner index is free as long as
-// both operands have the same: lane (g, t) takes the eight neighbours 8 t .. 8 t + 7 of each 32, so that a fragment of either operand is one 16-byte load from
-// rows that run along the inner index.  us with the map: one row, 1152 x 1152, rank 16 7.3; 64 rows with an adapter each, 1152 x 4608, rank 32 15.0 (25 MB of factors:
-// 3.8 at the measured copy rate); of these 3.4 are the map.  The first columns' B and Y0 are on their way during the first product, through shared memory (asked for
+// The forward for few rows: a cluster of CTAs has 16 rows of one adapter, shares out K for the first product, joins the sums through
+// distributed shared memory (each CTA all of them, always in the same order) and shares out the columns for the second.  A chain of
+// latencies: one launch, and operands straight from global memory into the fragments of mma.sync (tiles of 16 rows would leave tcgen05's 128
+// empty).  The order of a product's inner index is free as long as both operands have the same: lane (g, t) takes the eight neighbours 8 t ..
+// 8 t + 7 of each 32, so that a fragment of either operand is one 16-byte load from rows that run along the inner index.  us with the map:
+// one row, 1152 x 1152, rank 16 7.3; 64 rows with an adapter each, 1152 x 4608, rank 32 15.0 (25 MB of factors: 3.8 at the measured copy
+// rate); of these 3.4 are the map.  The first columns' B and Y0 are on their way during the first product, through shared memory (asked for
 // where they are used 15.3; ahead through registers, which spill, 22.7).
 template <int RP, int CLUSTER, bool F32>
-__global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : 3) lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, int M, int32_t* status, const int* perm, const __half* X, const void* Y0,
-                                                                 void* Y, const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad) {
+__global__ void __launch_bounds__(32 * WARPS, RP <= 32 ? 4 : 3)
+    lq_adapters_kernel(const LqAdTile* tiles, const int* ntiles, int M, int32_t* status, const int* perm, const __half* X, const void* Y0, void* Y,
+                       const __half* down, const __half* up, const LqAdMeta* meta, int K, int N, int Npad) {
   constexpr int NT = RP / 8, KB = (RP + 31) / 32;
   extern __shared__ __align__(16) float smem[];
   float* red = smem;                                      // [WARPS][16][RP]
@@ -376,14 +386,16 @@ size_t forward_smem(int rp, bool f32) {
 }
 template <int RP, int CLUSTER>
 cudaError_t launch_cluster(const lq_adapters* S, const lq_rowmap* R, int tiles, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
-  return lq_launch_cluster(dt == LQ_OUT_F32 ? lq_adapters_kernel<RP, CLUSTER, true> : lq_adapters_kernel<RP, CLUSTER, false>, tiles * CLUSTER, 32 * WARPS, CLUSTER, forward_smem(RP, dt == LQ_OUT_F32), st, (const LqAdTile*)R->d_small,
-                           (const int*)R->d_ntiles, R->M, lq_device_status_ptr(R->device), (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up,
-                           (const LqAdMeta*)S->d_meta, S->K, S->N, S->Npad);
+  const bool f32 = dt == LQ_OUT_F32;
+  return lq_launch_cluster(f32 ? lq_adapters_kernel<RP, CLUSTER, true> : lq_adapters_kernel<RP, CLUSTER, false>, tiles * CLUSTER, 32 * WARPS, CLUSTER,
+                           forward_smem(RP, f32), st, (const LqAdTile*)R->d_small, (const int*)R->d_ntiles, R->M, lq_device_status_ptr(R->device),
+                           (const int*)R->d_perm, (const __half*)X, Y0, Y, (const __half*)S->d_down, (const __half*)S->d_up, (const LqAdMeta*)S->d_meta,
+                           S->K, S->N, S->Npad);
 }
 template <int RP>
 cudaError_t launch_forward(const lq_adapters* S, const lq_rowmap* R, const void* X, const void* Y0, void* Y, lq_out_dtype dt, cudaStream_t st) {
-  // Eight CTAs a tile while all of them are resident at once, else four (us with the map, eight / four: 1400 rows, 1152 x 3456, rank 32 25.8 / 20.9; 64 rows with an
-  // adapter each, 512 x 8192, rank 64 43.4 / 32.3; one row, 1152 x 3456, rank 32 9.2 / 11.2; two were never better).
+  // Eight CTAs a tile while all of them are resident at once, else four (us with the map, eight / four: 1400 rows, 1152 x 3456, rank 32 25.8
+  // / 20.9; 64 rows with an adapter each, 512 x 8192, rank 64 43.4 / 32.3; one row, 1152 x 3456, rank 32 9.2 / 11.2; two were never better).
   const int tiles = lq_ad_tiles(R->M, R->slots, LQ_AD_SMALL_TILE), resident = (RP <= 32 ? 4 : 3) * R->sms;
   return 8 * tiles <= resident ? launch_cluster<RP, 8>(S, R, tiles, X, Y0, Y, dt, st) : launch_cluster<RP, 4>(S, R, tiles, X, Y0, Y, dt, st);
 }
@@ -449,8 +461,8 @@ extern "C" lq_status lq_adapters_set(lq_adapters* S, int32_t slot, int32_t rank,
     return lq_note_cuda(cudaMemsetAsync(S->d_meta + slot, 0, sizeof(LqAdMeta), (cudaStream_t)stream)) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
   const int blocks = (int)std::min(((long long)S->rp * (S->K + S->Npad) + 255) / 256, 4096ll);
   const size_t at = (size_t)slot * S->rp;
-  const cudaError_t e = lq_launch(lq_adapters_set_kernel, blocks, 256, 0, (cudaStream_t)stream, S->d_down + at * S->K, S->d_up + at * S->Npad, S->d_meta + slot,
-                                  (const __half*)A, (const __half*)B, S->K, S->N, S->Npad, S->rp, rank, scale);
+  const cudaError_t e = lq_launch(lq_adapters_set_kernel, blocks, 256, 0, (cudaStream_t)stream, S->d_down + at * S->K, S->d_up + at * S->Npad,
+                                  S->d_meta + slot, (const __half*)A, (const __half*)B, S->K, S->N, S->Npad, S->rp, rank, scale);
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
 
@@ -465,13 +477,15 @@ extern "C" lq_status lq_rowmap_create(int32_t M_max, int32_t slots, int device, 
   if (!R) return LQ_ERR_ALLOC;
   R->M_max = M_max; R->slots = slots; R->device = device; R->M = 0;
   const size_t rows = (size_t)M_max + LQ_AD_TILE;
-  const size_t large = (size_t)lq_ceil_div(M_max, LQ_AD_TILE) + slots + 1, little = (size_t)lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M), LQ_AD_SMALL_TILE) + slots + 1;
+  const size_t large = (size_t)lq_ceil_div(M_max, LQ_AD_TILE) + slots + 1;
+  const size_t little = (size_t)lq_ceil_div(std::min(M_max, LQ_AD_SMALL_M), LQ_AD_SMALL_TILE) + slots + 1;
   if (lq_note_cuda(cudaDeviceGetAttribute(&R->sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_ntiles, sizeof(int4))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_tiles, large * sizeof(LqAdTile))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_small, little * sizeof(LqAdTile))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&R->d_perm, (size_t)M_max * sizeof(int))) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&R->d_T, rows * LQ_AD_TROW * 2)) != cudaSuccess || lq_note_cuda(cudaMalloc((void**)&R->d_rscale, rows * sizeof(float))) != cudaSuccess) {
+      lq_note_cuda(cudaMalloc((void**)&R->d_T, rows * LQ_AD_TROW * 2)) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&R->d_rscale, rows * sizeof(float))) != cudaSuccess) {
     lq_rowmap_free(R);
     return LQ_ERR_ALLOC;
   }

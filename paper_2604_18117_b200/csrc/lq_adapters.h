@@ -5,11 +5,13 @@
 
 #include "lq_internal.h"
 
-// Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows of narrow factors, and one on tiles of 128 rows.  us with the map, K x N
-// and rank, small / large form.  Six requests of neighbouring rows: 1152 x 3456, 32: 600 rows 14.1 / 15.5, 1400 rows 18.2 / 17.7, 2048 rows 19.0 / 19.6; 512 x 8192,
-// 64: 90 rows 14.3 / 15.2, 250 rows 20.7 / 15.9.  Rows in any order, which the large form fetches four at a time: 1160 x 2312, 24, 1365 rows 16.8 / 23.9 (fp32 21.2 /
-// 31.9).  Rows with an adapter each: 512 x 8192, 64: 64 rows 27.8 / 34.8.  Ranks above 64 (the small form is not built for them): 5600 x 2240, 128: one row 23.9 / 17.2,
-// 12 rows 26.8 / 22.3; 512 x 8192, 128: one row 20.0 / 12.7; 1152 x 1152, 96: one row 12.4 / 13.2.
+// Two forms of the forward: one of clusters on tiles of 16 rows of one adapter, for few rows of narrow factors, and one on tiles of 128 rows.
+// us with the map, K x N and rank, small / large form.  Six requests of neighbouring rows: 1152 x 3456, 32: 600 rows 14.1 / 15.5, 1400 rows
+// 18.2 / 17.7, 2048 rows 19.0 / 19.6; 512 x 8192, 64: 90 rows 14.3 / 15.2, 250 rows 20.7 / 15.9.  Rows in any order, which the large form
+// fetches four at a time: 1160 x 2312, 24, 1365 rows 16.8 / 23.9 (fp32 21.2 / 31.9); so such rows take a step up at the cut, which goes by their
+// number alone (1536 and 1537 rows 17.6 and 24.6, fp32 22.0 and 33.0; neighbours 16.9 and 17.8, 21.3 and 21.5).  Rows with an adapter each:
+// 512 x 8192, 64: 64 rows 27.8 / 34.8.  Ranks above 64 (the small form is not built for them): 5600 x 2240, 128: one row 23.9 / 17.2, 12 rows
+// 26.8 / 22.3; 512 x 8192, 128: one row 20.0 / 12.7; 1152 x 1152, 96: one row 12.4 / 13.2, the one where the small form was ahead.
 constexpr int LQ_AD_SMALL_TILE = 16, LQ_AD_TILE = 128;
 constexpr int LQ_AD_SMALL_M = 1536, LQ_AD_SMALL_M_64 = 128;      // most rows of the small form, for stored ranks up to 32, 64
 static inline bool lq_ad_small_form(int M, int rp) { return rp <= 32 ? M <= LQ_AD_SMALL_M : rp <= 64 && M <= LQ_AD_SMALL_M_64; }
@@ -49,8 +51,9 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
 lq_status lq_adapters_tiles_prepare();   // once for each device that a map is made on, with that device current
 
 #ifdef __CUDACC__
-// The tiles (of 128 rows, or of 16) of a forward of M rows.  None where the map holds other rows by now, so that no row behind the forward's is touched: a graph that
-// sorts was replayed between, or was captured and not yet replayed.  A forward that finds that says so in the status word.
+// The tiles (of 128 rows, or of 16) of a forward of M rows.  None where the map holds other rows by now, so that no row behind the forward's
+// is touched: a graph that sorts was replayed between, or was captured and not yet replayed.  A forward that finds that says so in the status
+// word.
 template <bool SMALL>
 __device__ __forceinline__ int lq_ad_tiles_of(const int* d_ntiles, int M, int32_t* status) {
   const int4 n = *reinterpret_cast<const int4*>(d_ntiles);

@@ -3,7 +3,9 @@
 //   down   T = X A of a tile, K shared by a cluster of CTAs; each row of T leaves as two halves under a power of two
 //   up     Y = Y0 + (scale / power of two) T B, tile by tile and 128 columns at a time
 //
-// Both are bound by the memory: X is read once, Y0 once, Y is written once; T is 512 bytes a row at most and stays in the L2, the factors too.
+// X is read once, Y0 once, Y is written once; T is 512 bytes a row at most and stays in the L2, the factors too.  Once under way the up kernel
+// runs at the memory's rate and the down kernel at 4 to 5 TB/s; of 8192 rows (13 to 31 us each, the memory busy 18 to 44 % of it) each spends 4 to
+// 5 us in starting and ending.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -45,9 +47,10 @@ __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Copies 128 bytes at x of each of a tile's rows.  Neighbours: in one copy of 128 rows, or, where the tile is half of that or less, in copies of 32 (rows behind the
-// tile's last come along and are not looked at); others: four a copy (rows: a lane's).  The whole warp calls, one lane issues: a copy's operands have to be
-// uniform, and where the compiler cannot see that they are it takes the lanes one by one (455 clocks a stage of two copies for 345).
+// Copies 128 bytes at x of each of a tile's rows.  Neighbours: in one copy of 128 rows, or, where the tile is half of that or less, in copies
+// of 32 (rows behind the tile's last come along and are not looked at); others: four a copy (rows: a lane's).  The whole warp calls, one lane
+// issues: a copy's operands have to be uniform, and where the compiler cannot see that they are it takes the lanes one by one (455 clocks a
+// stage of two copies for 345).
 struct RowMaps {
   CUtensorMap whole, part, row;        // boxes of 128, 32 and one row x 128 bytes
 };
@@ -57,7 +60,8 @@ __device__ __forceinline__ uint32_t fetch_bytes(const LqAdTile& t) {
 __device__ __forceinline__ void fetch_rows(uint32_t dst, const RowMaps& tm, int x, const LqAdTile& t, const int4& rows, uint32_t bar) {
   if (t.first < 0) {
     for (int i = 0; 4 * i < t.rows; ++i) {
-      const int4 r = make_int4(__shfl_sync(0xffffffffu, rows.x, i), __shfl_sync(0xffffffffu, rows.y, i), __shfl_sync(0xffffffffu, rows.z, i), __shfl_sync(0xffffffffu, rows.w, i));
+      const int4 r = make_int4(__shfl_sync(0xffffffffu, rows.x, i), __shfl_sync(0xffffffffu, rows.y, i), __shfl_sync(0xffffffffu, rows.z, i),
+                               __shfl_sync(0xffffffffu, rows.w, i));
       if (elect_one()) tma_gather4(dst + i * 512, &tm.row, x, r, bar);
     }
   } else if (2 * t.rows > BM) {
@@ -66,7 +70,9 @@ __device__ __forceinline__ void fetch_rows(uint32_t dst, const RowMaps& tm, int 
     for (int i = 0; 32 * i < t.rows; ++i) tma_load_2d(dst + i * 4096, &tm.part, x, t.first + 32 * i, bar);
   }
 }
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
+}
 __device__ __forceinline__ void prefetch_maps(const RowMaps& tm) {
   prefetch_map(&tm.whole); prefetch_map(&tm.part); prefetch_map(&tm.row);
 }
@@ -85,10 +91,11 @@ struct DownParams {
   int rp, k_stages, ring, tmem_cols, M;
 };
 
-// One tile of a cluster at a time, K / (64 SPLIT) stages a CTA.  Warp 0 fetches, warp 1 issues the MMAs into 128 x rp of tensor memory; then all warps bring the partial
-// sums to shared memory and each CTA adds up 128 / SPLIT rows from all of the cluster, always in the same order.  A short kernel is a chain of latencies:
-// nothing waits for what it does not need (an empty slot's tile is formed like another and left unread), the loads of a row's sums are all in flight
-// together.  (8192 x 1152, rank 32, us from the dependency's end: tile known 0.6, copies asked for 1.5, sums complete 6.4, in shared memory of all 7.5, T written 8.8.)
+// One tile of a cluster at a time, K / (64 SPLIT) stages a CTA.  Warp 0 fetches, warp 1 issues the MMAs into 128 x rp of tensor memory; then
+// all warps bring the partial sums to shared memory and each CTA adds up 128 / SPLIT rows from all of the cluster, always in the same order.
+// A short kernel is a chain of latencies: nothing waits for what it does not need (an empty slot's tile is formed like another and left
+// unread), the loads of a row's sums are all in flight together.  (8192 x 1152, rank 32, us from the dependency's end: tile known 0.6, copies
+// asked for 1.5, sums complete 6.4, in shared memory of all 7.5, T written 8.8.)
 template <int SPLIT>
 __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const __grid_constant__ RowMaps tmX, const __grid_constant__ CUtensorMap tmDown,
                                                                            const __grid_constant__ DownParams p) {
@@ -172,8 +179,8 @@ __global__ void __launch_bounds__(32 * DOWN_WARPS) lq_adapters_down_kernel(const
     ok = __syncthreads_and(ok && !abort_flag) != 0;
     used += n;
     turn ^= 1;
-    // partial sums -> shared memory, rows 16 bytes longer than they are so that neighbouring rows lie in different banks; the ring is free: the MMAs
-    // have read it
+    // partial sums -> shared memory, rows 16 bytes longer than they are so that neighbouring rows lie in different banks; the ring is free:
+    // the MMAs have read it
     const int pitch = p.rp + 4;
     if (ok) {
       tc_fence_after();
@@ -268,23 +275,26 @@ struct UpParams {
   int N, Npad, chunks, in_place, M;
 };
 
-// Persistent, one CTA an SM: the steps (tile, 128 columns) of all tiles are cut into runs of like length.  Warp 0 fetches a tile's T (both halves) and each
-// step's slab of B, warp 1 issues hi B + lo B into one of two accumulators, warp 2 fetches Y0 into a ring of 96 KB, pieces of 128 rows x 128 bytes; the
-// drain warps hold 32 rows x 32 columns each: they add, round and store.  B's rows lie in the order that gives a lane eight neighbouring columns.
-// 8192 x 3456, rank 32: 20 us from the down kernel's end on, 17.3 at the measured copy rate (Y0 straight into registers a step ahead, 32 KB in flight: 30.7).
-// Both kernels and the map, us: 8192 rows 1152 x 3456, rank 32 37; 32768 rows 5600 x 2240, rank 128 139 (103 at the copy rate).
+// Persistent, one CTA an SM: the steps (tile, 128 columns) of all tiles are cut into runs of like length.  Warp 0 fetches a tile's T (both
+// halves) and each step's slab of B, warp 1 issues hi B + lo B into one of two accumulators, warp 2 fetches Y0 into a ring of 96 KB, pieces
+// of 128 rows x 128 bytes; the drain warps hold 32 rows x 32 columns each: they add, round and store.  B's rows lie in the order that gives a
+// lane eight neighbouring columns.
+// 8192 x 3456, rank 32: 20 us from the down kernel's end on, 17.3 at the measured copy rate (Y0 straight into registers a step ahead, 32 KB in
+// flight: 30.7).  Both kernels and the map, us in a graph of ten passes: 8192 rows 1152 x 3456, rank 32 37; 32768 rows 5600 x 2240, rank 128 140 to 142
+// (103 at the copy rate), in long runs 155 to 168.
 template <bool F32, int NA>      // NA: 64-wide pieces of the rank
 __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmUp,
                                                                        const __grid_constant__ RowMaps tmY,
                                                                        const __grid_constant__ UpParams p) {
   constexpr int NT = up_t_bufs(NA), NB = up_b_stages(NA), T_BUF = 2 * NA * PIECE, B_STAGE = NA * PIECE, B_AT = NT * T_BUF, Y_AT = B_AT + NB * B_STAGE;
-  // Pieces of a step, and warps that wait for one and give it back.  A wait tells a phase from the next one, not from the one after that, so who waits on a place of
-  // the ring has to wait for each of its turns.  With two pieces a step the six places are always read by the same warps.  With four a place's turns would
-  // alternate between two groups of them: every warp waits for all pieces and gives all back.
+  // Pieces of a step, and warps that wait for one and give it back.  A wait tells a phase from the next one, not from the one after that, so
+  // who waits on a place of the ring has to wait for each of its turns.  With two pieces a step the six places are always read by the same
+  // warps.  With four a place's turns would alternate between two groups of them: every warp waits for all pieces and gives all back.
   constexpr int YP = F32 ? 4 : 2, Y_READERS = F32 ? UP_DRAIN_WARPS : UP_DRAIN_WARPS / YP;
   static_assert(F32 || Y_SLOTS % YP == 0, "");
   extern __shared__ unsigned char smem_raw[];
-  enum { TFULL = 0, TFREE = NT, BFULL = 2 * NT, BFREE = BFULL + NB, AFULL = BFREE + NB, YFULL = AFULL + 2, AFREE = YFULL + Y_SLOTS, YFREE = AFREE + 2, NBAR = YFREE + Y_SLOTS };
+  enum { TFULL = 0, TFREE = NT, BFULL = 2 * NT, BFREE = BFULL + NB, AFULL = BFREE + NB, YFULL = AFULL + 2, AFREE = YFULL + Y_SLOTS };
+  enum { YFREE = AFREE + 2, NBAR = YFREE + Y_SLOTS };
   __shared__ __align__(8) uint64_t bars[NBAR];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
@@ -305,8 +315,8 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   grid_launch_dependents();
-  // Where the down kernel has said that all that came before it has completed, the map, the factors and Y0 are there, and only T and its rows' scales
-  // are waited for (and every CTA waits, so that who waits for this kernel has waited for that one).  Else everything is.
+  // Where the down kernel has said that all that came before it has completed, the map, the factors and Y0 are there, and only T and its
+  // rows' scales are waited for (and every CTA waits, so that who waits for this kernel has waited for that one).  Else everything is.
   if (warp == 3 || !early) grid_dependency_wait();
 
   const int ntiles = lq_ad_tiles_of<false>(p.ntiles, p.M, p.status);
@@ -340,7 +350,8 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
           if (b_uses >= NB && !(ok = mbar_wait_warp(bar(BFREE + s), ((b_uses / NB) & 1) ^ 1, &abort_flag, p.status, LQ_STAGE_PRODUCER))) break;
           if (elect_one()) {
             mbar_expect_tx(bar(BFULL + s), pieces * PIECE);
-            for (int a = 0; a < pieces; ++a) tma_load_2d(base + B_AT + s * B_STAGE + a * PIECE, &tmUp, 128 * a, f.tile.adapter * p.Npad + UP_COLS * ch, bar(BFULL + s));
+            for (int a = 0; a < pieces; ++a)
+              tma_load_2d(base + B_AT + s * B_STAGE + a * PIECE, &tmUp, 128 * a, f.tile.adapter * p.Npad + UP_COLS * ch, bar(BFULL + s));
           }
           __syncwarp();
           ++b_uses;
@@ -389,7 +400,8 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
           if (!ok) break;
           tc_fence_after();
           const int steps = (f.rank + 15) / 16;
-          const uint64_t hi = make_smem_desc(base + buf * T_BUF), lo = make_smem_desc(base + buf * T_BUF + NA * PIECE), slab = make_smem_desc(base + B_AT + s * B_STAGE);
+          const uint64_t hi = make_smem_desc(base + buf * T_BUF), lo = make_smem_desc(base + buf * T_BUF + NA * PIECE);
+          const uint64_t slab = make_smem_desc(base + B_AT + s * B_STAGE);
           if (elect_one()) {
             for (int k = 0; k < steps; ++k) {             // (64 of the rank are a piece)
               const uint32_t at = (uint32_t)((k >> 2) * (PIECE >> 4) + 2 * (k & 3));
@@ -488,8 +500,8 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
           tc_fence_after();
         }
         const int c = ch * UP_COLS + 32 * cq + 8 * t;
-        // rows g, g + 8, then rows g + 16, g + 24 of the quarter, where the tile has some: fragment registers 4 j .. 4 j + 3 hold row g, columns 2 j, 2 j + 1 of
-        // this lane's eight, then row g + 8 the same columns
+        // rows g, g + 8, then rows g + 16, g + 24 of the quarter, where the tile has some: fragment registers 4 j .. 4 j + 3 hold row g,
+        // columns 2 j, 2 j + 1 of this lane's eight, then row g + 8 the same columns
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const bool any = 32 * quad + 16 * h < r.rows;
@@ -514,7 +526,9 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
               if (r.row[2 * h + q] >= 0 && c < p.N) {
                 const float2 by = make_float2(r.scale[2 * h + q], r.scale[2 * h + q]);
                 const size_t to = (size_t)(unsigned)r.row[2 * h + q] * (unsigned)p.N + c;
-                const auto d = [&](int j) { return make_float2(__uint_as_float(v[4 * j + 2 * q]), __uint_as_float(v[4 * j + 2 * q + 1])); };     // columns 2 j, 2 j + 1
+                const auto d = [&](int j) {               // columns 2 j, 2 j + 1
+                  return make_float2(__uint_as_float(v[4 * j + 2 * q]), __uint_as_float(v[4 * j + 2 * q + 1]));
+                };
                 if constexpr (F32) {
                   float2* f = reinterpret_cast<float2*>(&y[q][0]);
                   if (r.rank > 0)                         // (a row without an adapter keeps its bits)
@@ -531,7 +545,8 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lq_adapters_up_kernel(const __g
                 }
               }
         }
-        // (behind the stores, which have to wait for the words that they store: right behind its loads the arrival, and the next copy with it, can overtake them)
+        // (behind the stores, which have to wait for the words that they store: right behind its loads the arrival, and the next copy with
+        // it, can overtake them)
         __syncwarp();
         if (lane < (F32 ? YP : 1)) mbar_arrive(bar(YFREE + (F32 ? (y_uses + lane) % Y_SLOTS : s)));
         y_uses += YP;
@@ -557,8 +572,8 @@ cudaError_t launch_down(const lq_adapters* S, const lq_rowmap* R, const RowMaps&
   d.ring = std::min(std::min(MAX_STAGES, most), (DOWN_SMEM - 1024) / stage);
   while (d.tmem_cols < S->rp) d.tmem_cols *= 2;
   const int smem = 1024 + std::max(d.ring * stage, BM * (S->rp + 4) * 4);
-  // no more clusters than are resident: with many slots most tiles that there might be are not there (8192 x 1152 x 3456, rank 32, 1023 slots of which eight are used,
-  // us with the map: 61.1 by a cluster for each, 40.4 so)
+  // no more clusters than are resident: with many slots most tiles that there might be are not there (8192 x 1152 x 3456, rank 32, 1023 slots
+  // of which eight are used, us with the map: 61.1 by a cluster for each, 40.4 so)
   const int tiles = std::min(lq_ad_tiles(R->M, R->slots, BM), std::max(1, 2 * R->sms / SPLIT));
   return lq_launch_cluster(lq_adapters_down_kernel<SPLIT>, tiles * SPLIT, 32 * DOWN_WARPS, SPLIT, smem, st, tmX, S->tmDown, d);
 }
@@ -572,9 +587,12 @@ cudaError_t launch_up(const lq_adapters* S, const lq_rowmap* R, const RowMaps& t
 }  // namespace
 
 lq_status lq_adapters_tiles_prepare() {
-  const auto room = [](auto* kernel, int bytes) { return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) == cudaSuccess; };
-  return room(lq_adapters_down_kernel<1>, DOWN_SMEM) && room(lq_adapters_down_kernel<2>, DOWN_SMEM) && room(lq_adapters_down_kernel<4>, DOWN_SMEM) &&
-                 room(lq_adapters_down_kernel<8>, DOWN_SMEM) && room(lq_adapters_up_kernel<false, 1>, up_smem(1)) && room(lq_adapters_up_kernel<true, 1>, up_smem(1)) &&
+  const auto room = [](auto* kernel, int bytes) {
+    return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) == cudaSuccess;
+  };
+  return room(lq_adapters_down_kernel<1>, DOWN_SMEM) && room(lq_adapters_down_kernel<2>, DOWN_SMEM) &&
+                 room(lq_adapters_down_kernel<4>, DOWN_SMEM) && room(lq_adapters_down_kernel<8>, DOWN_SMEM) &&
+                 room(lq_adapters_up_kernel<false, 1>, up_smem(1)) && room(lq_adapters_up_kernel<true, 1>, up_smem(1)) &&
                  room(lq_adapters_up_kernel<false, 2>, up_smem(2)) && room(lq_adapters_up_kernel<true, 2>, up_smem(2))
              ? LQ_OK
              : LQ_ERR_CUDA;
@@ -593,8 +611,9 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
   int32_t* status = lq_device_status_ptr(S->device);
   if (!status) return LQ_ERR_CUDA;
   DownParams d = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_T, R->d_rscale, status, R->d_ntiles + 3, S->rp, lq_ceil_div(S->K, 64), 1, 32, R->M};
-  // K is shared by as many CTAs as fill the SMs twice over, each with at least two stages (us with the map by 1, 2, 4 and 8 of them, 5600 x 2240, rank 128: 4096 rows
-  // 60.2, 44.6, 38.9, 38.0; 8192 rows 70.0, 57.4, 53.9, 63.2; 16384 rows 88.4, 82.8, 91.6, 132; 32768 rows 142, 150, 203, 289)
+  // K is shared by as many CTAs as fill the SMs twice over, each with at least two stages (us with the map by 1, 2, 4 and 8 of them, 5600 x
+  // 2240, rank 128: 4096 rows 60.2, 44.6, 38.9, 38.0; 8192 rows 70.0, 57.4, 53.9, 63.2; 16384 rows 88.4, 82.8, 91.6, 132; 32768 rows 142,
+  // 150, 203, 289)
   const int tiles = lq_ceil_div(R->M, BM);
   int split = 1;
   while (split < 8 && tiles * 2 * split <= 2 * R->sms && d.k_stages >= 4 * split) split *= 2;
@@ -603,7 +622,8 @@ lq_status lq_adapters_forward_tiles(const lq_adapters* S, const lq_rowmap* R, co
                   : split == 4 ? launch_down<4>(S, R, tmX, d, st)
                                : launch_down<8>(S, R, tmX, d, st);
   if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
-  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, R->d_ntiles + 3, S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y, R->M};
+  const UpParams u = {R->d_tiles, R->d_ntiles, R->d_perm, S->d_meta, R->d_rscale, Y, status, R->d_ntiles + 3,
+                      S->N, S->Npad, lq_ceil_div(S->N, UP_COLS), Y0 == Y, R->M};
   if (dt == LQ_OUT_F32) e = S->rp <= 64 ? launch_up<true, 1>(S, R, tmY, u, st) : launch_up<true, 2>(S, R, tmY, u, st);
   else e = S->rp <= 64 ? launch_up<false, 1>(S, R, tmY, u, st) : launch_up<false, 2>(S, R, tmY, u, st);
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;

@@ -59,8 +59,8 @@ template <bool SPLIT>
 __device__ __forceinline__ Raw<float> load_raw(const float* p, int apart) {
   return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + (SPLIT ? apart : 4))};
 }
-// The four pairs of a lane: first sides lo, second sides hi, two pairs to a register pair (packed arithmetic takes both at once).  NEIGHBOURS: a pair
-// is two neighbouring entries.
+// The four pairs of a lane: first sides lo, second sides hi, two pairs to a register pair (packed arithmetic takes both at once).
+// NEIGHBOURS: a pair is two neighbouring entries.
 struct Pairs {
   float2 lo[2], hi[2];
 };
@@ -153,16 +153,19 @@ __device__ __forceinline__ float group_sum(float a, int lanes, int at, int lane)
   return a;
 }
 
-// A block takes a few rows and forms their angles together.  Its warps share out the rows' heads: one walks over the queries, or the keys, of a
-// row, or over a part of them.  L lanes hold a head, each lane C times eight entries that are the two sides of the same four pairs in every head, so
-// weights times cosines and sines stay in registers along the walk; the norm's sum crosses the head's lanes by shuffles.  What bounds it short of the
-// memory is the issue of instructions (32 heads of 72: 1924 a row at first, 64-bit address arithmetic and moves most of them) and warps enough to cover their
-// latency: where L is known (then the whole head is rotated, or nothing) every address is a base and a constant; a lane holds 16 entries of heads of 64 and 128,
-// but of 72 only 8 (24, for three lanes a head, take 128 registers: 24.7 us for 18.9); blocks are small, so that few warps wait for the angles of others.
-// B200, us and share of the measured copy rate of its bytes: 32760 rows, 40 heads of 128, fp16 110.6, 0.93; 8192 rows, 32 heads of 72, fp16 18.9, 0.61;
-// 4100 rows, 32 heads of 128, fp32, no norm 24.6, 0.83; one row 2.0.
+// A block takes a few rows and forms their angles together.  Its warps share out the rows' heads: one walks over the queries, or the keys, of
+// a row, or over a part of them.  L lanes hold a head, each lane C times eight entries that are the two sides of the same four pairs in every
+// head, so weights times cosines and sines stay in registers along the walk; the norm's sum crosses the head's lanes by shuffles.  What
+// bounds it short of the memory is the issue of instructions (32 heads of 72: 1924 a row at first, 64-bit address arithmetic and moves most
+// of them) and warps enough to cover their latency: where L is known (then the whole head is rotated, or nothing) every address is a base and
+// a constant; a lane holds 16 entries of heads of 64 and 128, but of 72 only 8 (24, for three lanes a head, take 128 registers: 24.7 us for
+// 18.9); blocks are small, so that few warps wait for the angles of others.  (The bounds of 72 and 96 registers cost up to 20 bytes of spills in
+// the fp16 instances.)
+// B200, us in a graph of ten passes and share of the measured copy rate of its bytes: 32760 rows, 40 heads of 128, fp16 110.6, 0.93 (in long runs
+// 116 to 118, 0.87); 8192 rows, 32 heads of 72, fp16 19.0, 0.61; 4100 rows, 32 heads of 128, fp32, no norm 24.7, 0.83; one row 2.1.
 template <typename TIN, typename TOUT, int NORM, int ROT, int L, int C>
-__global__ void __launch_bounds__(32 * WARPS, C == 1 && sizeof(TIN) == 2 && NORM != LQ_NORM_LAYER ? 7 : C == 2 && sizeof(TIN) == 2 ? 5 : 4) lq_heads_kernel(const __grid_constant__ HeadsParams p) {
+__global__ void __launch_bounds__(32 * WARPS, C == 1 && sizeof(TIN) == 2 && NORM != LQ_NORM_LAYER ? 7 : C == 2 && sizeof(TIN) == 2 ? 5 : 4)
+    lq_heads_kernel(const __grid_constant__ HeadsParams p) {
   constexpr bool SPLIT = ROT == ROT_HALVES, NEIGHBOURS = ROT == ROT_PAIRS, FIXED = L > 0;
   static_assert(FIXED || C == 1, "");
   constexpr int DEPTH = sizeof(TIN) == 2 ? 3 : C == 1 ? 3 : 2;      // heads of a lane in flight
@@ -198,8 +201,10 @@ __global__ void __launch_bounds__(32 * WARPS, C == 1 && sizeof(TIN) == 2 && NORM
     int seq = seq0, at = at0 + r;
     for (; at >= p.seq_len; at -= p.seq_len) ++seq;
     in_step = groups * side.in_head; out_step = groups * side.out_head;
-    in = reinterpret_cast<const TIN*>(side.in) + ((long long)seq * side.in_seq + (long long)at * side.in_row + (long long)(begin + grp) * side.in_head + first);
-    out = reinterpret_cast<TOUT*>(side.out) + ((long long)seq * side.out_seq + (long long)at * side.out_row + (long long)(begin + grp) * side.out_head + first);
+    in = reinterpret_cast<const TIN*>(side.in) +
+         ((long long)seq * side.in_seq + (long long)at * side.in_row + (long long)(begin + grp) * side.in_head + first);
+    out = reinterpret_cast<TOUT*>(side.out) +
+          ((long long)seq * side.out_seq + (long long)at * side.out_row + (long long)(begin + grp) * side.out_head + first);
     left = works ? end - begin - grp : 0;                 // heads that this lane has before it, in steps of `groups`
 #pragma unroll
     for (int u = 0; u < DEPTH; ++u) {
@@ -343,8 +348,10 @@ cudaError_t launch(HeadsParams& p, int sms, cudaStream_t st) {
   p.by_groups = reciprocal(std::max(2, g));
   return lq_launch_grid(lq_heads_kernel<TIN, TOUT, NORM, ROT, L, C>, dim3(c.blocks, c.blocks_y), 32 * WARPS, 1, 0, st, p);
 }
-// Under an RMS norm heads of 64, 72, 112 and 128 entries that are rotated as a whole, or not at all, have their lanes at compile time, 16 entries to each where
-// lanes are a power of two; others hold eight entries a lane.  (8192 rows, 32 heads of 72: 26 us by the general form.)
+// Under an RMS norm heads of 64, 72, 112 and 128 entries that are rotated as a whole, or not at all, have their lanes at compile time, 16
+// entries to each where lanes are a power of two; others hold eight entries a lane.  us of 8192 rows of 32 heads by these and by the general
+// form: fp16, rotated 64 16.5 / 18.6, 72 18.8 / 24.3, 112 25.0 / 29.8, 128 25.5 / 30.1; fp16, not rotated 13.9 / 14.9, 16.8 / 19.2, 22.4 / 24.6,
+// 22.9 / 25.3; fp32, rotated 25.3 / 29.6, 34.6 / 39.1, 46.9 / 50.9, 42.5 / 52.5; of 64 rows 2.3 to 2.5 / 2.5 to 2.8.
 template <typename TIN, typename TOUT, int NORM, int ROT>
 cudaError_t launch_lanes(HeadsParams& p, int sms, cudaStream_t st) {
   if constexpr (NORM == LQ_NORM_RMS)

@@ -45,7 +45,8 @@ struct LqPlaceSearch {
     if (c + rest_hi[i] < low || c + rest_lo[i] > high) return LQ_APART;
     if (i == n) return LQ_SHARED;
     const Term& t = term[i];
-    const int64_t first = std::max(t.lo, -floor_div(c + rest_hi[i + 1] - low, t.step)), last = std::min(t.hi, floor_div(high - c - rest_lo[i + 1], t.step));
+    const int64_t first = std::max(t.lo, -floor_div(c + rest_hi[i + 1] - low, t.step));
+    const int64_t last = std::min(t.hi, floor_div(high - c - rest_lo[i + 1], t.step));
     for (int64_t x = first; x <= last; ++x) {
       if (++nodes > MAX_NODES) return LQ_ENTANGLED;
       const LqPlaces p = look(c + t.step * x, i + 1);
