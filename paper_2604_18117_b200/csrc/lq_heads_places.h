@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <numeric>
 
 // counts[0] x counts[1] x counts[2] runs of `bytes` bytes, steps[i] bytes apart
 struct LqRuns {
@@ -16,13 +17,14 @@ enum LqPlaces { LQ_APART = 0, LQ_SHARED = 1, LQ_ENTANGLED = 2 };      // entangl
 
 // Whether c + the sum of step[i] x[i], lo[i] <= x[i] <= hi[i], falls into [low, high] for some whole x.  Steps in falling order of
 // magnitude: what the later ones reach leaves an x few values where layouts are nested (about 0.1 us for an output inside a
-// projection's rows); the bound only meets layouts whose dimensions run through one another many times.
+// projection's rows).  Where it has many, what their steps have in common may settle it; the bound only meets layouts whose dimensions run
+// through one another many times.
 struct LqPlaceSearch {
   static constexpr int MAX_TERMS = 6, MAX_NODES = 1 << 16;
   struct Term {
     int64_t step, lo, hi;
   } term[MAX_TERMS];
-  int64_t rest_lo[MAX_TERMS + 1], rest_hi[MAX_TERMS + 1], low, high;
+  int64_t rest_lo[MAX_TERMS + 1], rest_hi[MAX_TERMS + 1], common[MAX_TERMS + 1], low, high;
   int n = 0, nodes = 0;
 
   void add(int64_t step, int64_t lo, int64_t hi) {
@@ -34,10 +36,11 @@ struct LqPlaceSearch {
   LqPlaces run(int64_t c, int64_t from, int64_t to) {
     low = from; high = to;
     std::sort(term, term + n, [](const Term& a, const Term& b) { return a.step > b.step; });
-    rest_lo[n] = rest_hi[n] = 0;
+    rest_lo[n] = rest_hi[n] = common[n] = 0;
     for (int i = n - 1; i >= 0; --i) {
       rest_lo[i] = rest_lo[i + 1] + term[i].step * term[i].lo;
       rest_hi[i] = rest_hi[i + 1] + term[i].step * term[i].hi;
+      common[i] = std::gcd(common[i + 1], term[i].step);
     }
     return look(c, 0);
   }
@@ -47,6 +50,8 @@ struct LqPlaceSearch {
     const Term& t = term[i];
     const int64_t first = std::max(t.lo, -floor_div(c + rest_hi[i + 1] - low, t.step));
     const int64_t last = std::min(t.hi, floor_div(high - c - rest_lo[i + 1], t.step));
+    // c and a multiple of the common divisor
+    if (last - first > 3 && floor_div(high - c, common[i]) < -floor_div(c - low, common[i])) return LQ_APART;
     for (int64_t x = first; x <= last; ++x) {
       if (++nodes > MAX_NODES) return LQ_ENTANGLED;
       const LqPlaces p = look(c + t.step * x, i + 1);

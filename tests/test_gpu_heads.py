@@ -367,7 +367,7 @@ def test_every_output_has_a_place_of_its_own_apart_from_the_inputs():
         assert code(q, k) == 1, (q, k)
     assert code((P, s, P + 128, s, 1)) == 0 and code((P, s, P + 16, s, 1)) == 1 and code((P, s, P + 128, s, 2)) == 1
     assert code((P, s, far, s, 2, far + 1024)) == 1 and code((P, s, far, s, 2), at=far + 4) == 1
-    assert code((P, s, far, s, 2), fout=1) == 0 and code((P, s, far - 3072, s, 2), fout=1) == 0 and code((P, s, P + 1024, s, 2), fout=1) == 1
+    assert code((P, s, far, s, 2), fout=1) == 0 and code((P, s, far - 2560, s, 2), fout=1) == 0 and code((P, s, P + 1024, s, 2), fout=1) == 1
     torch.cuda.synchronize()
     x.copy_(before)
     torch.cuda.synchronize()

@@ -88,6 +88,17 @@ def test_outputs_of_two_dimensions_on_one_place(lib):
     assert collide(runs(0, (0, 1 << 33, 16), (1, (1 << 31) - 1, 2), 16)) == SHARED         # no memory is as large
 
 
+def test_what_cannot_be_told_in_few_steps_is_said_to_be_so(lib):
+    """Each side's rows hit the other's steps at a different place each time, all of them just beside its heads: apart, but found so only by looking
+    at half a million places."""
+    _, meet = lib
+    a = runs(0, (0, 1 << 20, 0), (1, 1 << 20, 1), 16)
+    b = runs(1 << 19, (0, (1 << 20) + 32, 0), (1, 1 << 14, 1), 16)             # 2^19 + 32 i over i < 2^14: behind a head's end, before the next one's
+    assert meet(a, b) == APART
+    c = runs(1 << 19, (0, (1 << 20) + 1, 0), (1, (1 << 19) - 16, 1), 16)
+    assert meet(a, c) == ENTANGLED
+
+
 def test_the_longest_rows_take_few_steps(lib):
     collide, meet = lib
     n = (1 << 31) - 1
@@ -97,5 +108,7 @@ def test_the_longest_rows_take_few_steps(lib):
     # two combs whose teeth fall beside one another, in step and out of step
     comb = runs(1 << 20, (0, 64, 0), (1, n // 4, 1), 16)
     assert meet(comb, runs((1 << 20) + 32, (0, 64, 0), (1, n // 4, 1), 16)) == APART
-    assert meet(comb, runs((1 << 20) + 32, (0, 128, 0), (1, n // 8, 1), 16)) in (APART, ENTANGLED)
+    assert meet(comb, runs((1 << 20) + 32, (0, 128, 0), (1, n // 8, 1), 16)) == APART
+    assert meet(comb, runs((1 << 20) + 32, (0, 192, 64), (1, n // 16, 3), 16)) == APART
+    assert meet(comb, runs((1 << 20) + 48, (0, 192, 64), (1, n // 16, 3), 17)) == SHARED
     assert meet(comb, runs((1 << 20) + 32, (0, 80, 0), (1, n // 8, 1), 16)) == SHARED
