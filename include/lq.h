@@ -359,9 +359,9 @@ typedef struct {
 lq_status lq_qk_norm_rope(const lq_heads* q, const lq_heads* k, int32_t head_dim, int32_t sequences, int32_t seq_len, lq_norm norm, float eps,
                           const lq_rope* rope, const int32_t* pos_dev, lq_out_dtype in_dtype, lq_out_dtype out_dtype, void* cuda_stream);
 
-/* The queries, keys and values of an attention block in one call, four kernels on the stream: lq_quantize_act and lq_linear_forward of a
- * layer whose N output columns are q_heads heads of queries, kv_heads of keys and kv_heads of values; the rows' adapters added to all of them;
- * norm and rotation of the queries and keys, in place.  Equal to the bit to those calls one by one. */
+/* The queries, keys and values of an attention block in one call, three to five kernels on the stream: lq_quantize_act and
+ * lq_linear_forward of a layer whose N output columns are q_heads heads of queries, kv_heads of keys and kv_heads of values; the rows'
+ * adapters, if any, added to all of them; norm and rotation of the queries and keys, in place.  Equal to the bit to those calls one by one. */
 typedef struct {
   int32_t head_dim, q_heads, kv_heads;     /* (q_heads + 2 kv_heads) head_dim = N                              */
   int32_t sequences;                       /* M = sequences * rows of each                                     */
