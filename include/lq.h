@@ -381,6 +381,109 @@ typedef struct {
 lq_status lq_qkv_forward(const lq_layer* layer, lq_act* act, const void* X_f16_dev, int32_t M, const lq_adapters* set, const lq_rowmap* map,
                          const lq_qkv* qkv, void* Y_dev, lq_out_dtype dtype, void* cuda_stream);
 
+/* ---- a cache of keys and values in 8 bits, and attention over it --------------------------------------------------
+ * (Outside the paper's layer: what an attention block does with the rows that lq_qkv_forward has written.)
+ *
+ * Tokens are kept in pages of page_tokens, pages in any order; every 32 tokens of a head share one step 2^e for their keys and one
+ * for their values, e the smallest integer in [-20, 9] with 127 * 2^e >= the largest magnitude written, and are stored as
+ * rint(x / 2^e) in [-127, 127].  (What is beyond 127 * 2^9 = 65024 becomes that.)  Tokens that come to 32 which hold some already may
+ * need a larger e': the codes c that are there become rint(c / 2^(e' - e)).  Every value c 2^e is a half.                          */
+#define LQ_KV_BLOCK 32
+#define LQ_KV_MAX_SEQUENCES 65535
+typedef struct lq_kvcache lq_kvcache;
+
+/* A cache of `layers` layers of `pages` pages each on one device (allocates layers * pages * page_tokens / 32 * kv_heads * (64 Dp + 32) bytes,
+ * Dp = head_dim rounded up to 64, 80, 96, 112, 128, 192 or 256, and the attention's workspace; synchronous).  page_tokens a multiple of 32
+ * up to 65536, kv_heads <= 4096, head_dim a multiple of 8 up to 256; anything else is UNSUPPORTED.  Holds zeros at first. */
+lq_status lq_kvcache_create(int32_t layers, int32_t pages, int32_t page_tokens, int32_t kv_heads, int32_t head_dim, int device, lq_kvcache** out);
+lq_status lq_kvcache_free(lq_kvcache* cache);
+
+/* The sequences of a step, the same for every layer.  The arrays are device memory and are read when the kernels run, so a captured graph
+ * goes by what they then hold.  A sequence that does not fit them (a length below 0, above its pages' or, where that matters, below its rows;
+ * a page outside the cache) makes the kernels leave its tokens, or those of that page, out; lq_get_device_status then says INVALID_ARG. */
+typedef struct {
+  int32_t sequences;                       /* 1 .. LQ_KV_MAX_SEQUENCES                                                */
+  int32_t rows;                            /* rows of the call's tensors, >= 0                                        */
+  const int32_t* row_start;                /* [sequences + 1], not falling: sequence s has rows row_start[s] .. row_start[s + 1] - 1, its
+                                              newest tokens in order (none is fine); rows behind row_start[sequences] are no sequence's
+                                              and are left alone.  NULL: rows / sequences rows each                   */
+  const int32_t* length;                   /* [sequences] tokens of each sequence, those of this step among them      */
+  const int32_t* pages;                    /* [sequences][page_stride] pages of each sequence, from its first token on */
+  int32_t page_stride;                     /* >= 1                                                                    */
+} lq_kvbatch;
+
+/* Keys and values as rows, or as an output.  Entry d of head h of row i lies at i * row + h * head + d elements (an output's of token i
+ * of sequence s: s * seq more).  Pointers 16-byte aligned; strides multiples of 8, of less than 2^40 in magnitude. */
+typedef struct {
+  void *k, *v;                             /* device; half or float                                                   */
+  int64_t k_seq, k_row, k_head;            /* (seq: of outputs alone)                                                 */
+  int64_t v_seq, v_row, v_head;
+} lq_kvrows;
+
+/* Writes the batch's rows, finite keys and values, as each sequence's last tokens: tokens length - n .. length - 1 of one with n rows
+ * (length >= n).  A token that is the first of its 32 begins them anew.  Pages that are written belong to one sequence of the batch.
+ * Asynchronous on `cuda_stream`. */
+lq_status lq_kvcache_append(lq_kvcache* cache, int32_t layer, const lq_kvbatch* batch, const lq_kvrows* rows, lq_out_dtype dtype, void* cuda_stream);
+
+/* Reads tokens begin .. length - 1 of each sequence, at most max_tokens of them, into rows 0, 1, .. of its part of the output; what lies
+ * behind stays.  Values are exact in either type.  (Uses the batch's sequences, lengths and pages alone.)
+ *   begin_dev  [sequences] int32, device, >= 0; NULL: from the first token on
+ *   rows       k or v may be NULL (not wanted); no two entries on one place (INVALID_ARG; UNSUPPORTED where dimensions run through one
+ *              another too often to tell)
+ * Asynchronous on `cuda_stream`. */
+lq_status lq_kvcache_read(const lq_kvcache* cache, int32_t layer, const lq_kvbatch* batch, const int32_t* begin_dev, int32_t max_tokens,
+                          const lq_kvrows* rows, lq_out_dtype dtype, void* cuda_stream);
+
+typedef struct {
+  const void* q;                           /* device, half, 16-byte aligned, finite: entry d of head h of row i at i * q_row + h * q_head + d */
+  void* out;                               /* the same, of what the row's head attends to; apart from q, no two entries on one place
+                                              (INVALID_ARG; UNSUPPORTED where it cannot be told)                      */
+  int64_t q_row, q_head;                   /* strides in elements, multiples of 8, below 2^40 in magnitude            */
+  int64_t out_row, out_head;
+  int32_t q_heads;                         /* a multiple of the cache's heads, up to 4096: heads h * q_heads / kv_heads and on share head h   */
+  int32_t causal;                          /* 1: row i of a sequence's n is token p = length - n + i (length >= n) and sees tokens 0 .. p;
+                                              0: every row sees the whole sequence, of any length (0: the output is zeros) */
+  int32_t window;                          /* with causal: > 0: of those the last `window` ones, p among them, and    */
+  int32_t sinks;                           /* the sequence's first `sinks` (only with a window)                       */
+  float scale;                             /* of the products, e.g. 1 / sqrt(head_dim); below 2^64 in magnitude       */
+} lq_attn;
+
+/* Attention of the batch's rows over what the cache holds: out = sum_j w_j v_j / sum_j w_j, w_j = exp(scale q . k_j), j over the tokens that
+ * the row sees.  Products on the tensor cores from halves, sums in fp32; weights are rounded to halves beside the values.  One token a
+ * sequence, a few, whole prompts, or all of these in one batch.  No sum depends on the order of execution: equal calls give equal bits; a
+ * row may differ by rounding between calls of other batches.
+ * rows * q_heads / kv_heads <= 2^30, rows * q_heads <= 2^34.  Attention calls of one cache, of any of its layers, share its workspace: they
+ * must not overlap on the GPU (one stream, or events; graphs that were captured with one cache must not run side by side).
+ * Asynchronous on `cuda_stream`. */
+lq_status lq_cache_attention(const lq_kvcache* cache, int32_t layer, const lq_kvbatch* batch, const lq_attn* attn, void* cuda_stream);
+
+/* ---- the residual stream between two blocks: gate, sum and norms in one pass ---------------------------------------
+ * (Outside the paper's layer: what lies between a block's last projection and the next one's lq_quantize_act.)
+ *
+ *     x' = x + factor * gate * N1(y),     h = (N2(x') * weight + bias) * (1 + scale) + shift                              */
+typedef struct {
+  const void* x;                           /* [rows][features], device: the stream                                    */
+  const void* y;                           /* the block's output, or NULL: x' = x                                     */
+  void* x_out;                             /* x', or NULL (not wanted); may be x itself, with its stride              */
+  void* h;                                 /* the normed rows, or NULL; may be y itself, with its stride and type     */
+  int64_t x_row, y_row, x_out_row, h_row;  /* strides of rows in elements, multiples of 8                             */
+  const float* after_weight;               /* [features] of N1, or NULL (ones); NULL without that norm                */
+  const float* weight;                     /* [features] of N2, or NULL (ones); NULL without that norm                */
+  const float* bias;                       /* [features] or NULL; LQ_NORM_LAYER only                                  */
+  const void *gate, *scale, *shift;        /* [features] for each sequence, mod_seq elements apart (a multiple of 8; 0: one for all), of
+                                              mod_dtype; NULL: gate 1, scale 0, shift 0                               */
+  int64_t mod_seq;
+  int32_t rows, features, sequences;       /* rows = sequences * rows of each; features a multiple of 8 up to 8192    */
+  int32_t after, norm;                     /* lq_norm of N1 and N2                                                    */
+  int32_t x_dtype, y_dtype, h_dtype, mod_dtype;    /* lq_out_dtype; x_out's is x_dtype                                */
+  float factor, eps;
+  int32_t device;
+} lq_residual;
+
+/* All pointers 16-byte aligned; outputs on no input but in place as said (INVALID_ARG).  In fp32; h is made of x' before it is rounded.
+ * Runs on r->device.  Asynchronous on `cuda_stream`. */
+lq_status lq_residual_norm(const lq_residual* r, void* cuda_stream);
+
 /* Decode the activation record of the last lq_quantize_act into plain host arrays (for
  * parity checks); NULL skips a part.  qx int8 [M][K], sx half bits [M][G] (MXINT4: the block
  * exponents e as int16 [M][G], since 2^e may lie below the fp16 range), qb int8 [M][K],

@@ -48,6 +48,31 @@ class LqQkv(C.Structure):
                 ("rope", C.c_void_p), ("pos_dev", C.c_void_p)]
 
 
+class LqKvBatch(C.Structure):
+    _fields_ = [("sequences", C.c_int32), ("rows", C.c_int32), ("row_start", C.c_void_p), ("length", C.c_void_p), ("pages", C.c_void_p),
+                ("page_stride", C.c_int32)]
+
+
+class LqKvRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_seq", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+                ("v_seq", C.c_int64), ("v_row", C.c_int64), ("v_head", C.c_int64)]
+
+
+class LqAttn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64), ("out_row", C.c_int64),
+                ("out_head", C.c_int64), ("q_heads", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class LqResidual(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("x_out", C.c_void_p), ("h", C.c_void_p), ("x_row", C.c_int64), ("y_row", C.c_int64),
+                ("x_out_row", C.c_int64), ("h_row", C.c_int64), ("after_weight", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p),
+                ("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("mod_seq", C.c_int64), ("rows", C.c_int32),
+                ("features", C.c_int32), ("sequences", C.c_int32), ("after", C.c_int32), ("norm", C.c_int32), ("x_dtype", C.c_int32),
+                ("y_dtype", C.c_int32), ("h_dtype", C.c_int32), ("mod_dtype", C.c_int32), ("factor", C.c_float), ("eps", C.c_float),
+                ("device", C.c_int32)]
+
+
 class LqError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -86,6 +111,12 @@ _SIGNATURES = {
     "lq_qk_norm_rope": [C.POINTER(LqHeads), C.POINTER(LqHeads), C.c_int32, C.c_int32, C.c_int32, C.c_int, C.c_float, C.c_void_p,
                         C.c_void_p, C.c_int, C.c_int, C.c_void_p],
     "lq_qkv_forward": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(LqQkv), C.c_void_p, C.c_int, C.c_void_p],
+    "lq_kvcache_create": [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int, C.POINTER(C.c_void_p)],
+    "lq_kvcache_free": [C.c_void_p],
+    "lq_kvcache_append": [C.c_void_p, C.c_int32, C.POINTER(LqKvBatch), C.POINTER(LqKvRows), C.c_int, C.c_void_p],
+    "lq_kvcache_read": [C.c_void_p, C.c_int32, C.POINTER(LqKvBatch), C.c_void_p, C.c_int32, C.POINTER(LqKvRows), C.c_int, C.c_void_p],
+    "lq_cache_attention": [C.c_void_p, C.c_int32, C.POINTER(LqKvBatch), C.POINTER(LqAttn), C.c_void_p],
+    "lq_residual_norm": [C.POINTER(LqResidual), C.c_void_p],
     "lq_act_export": [C.c_void_p] * 8,
     "lq_get_device_status": [C.c_int, C.POINTER(C.c_int32), C.POINTER(C.c_int32)],
     "lq_set_option": [C.c_char_p, C.c_int32],
@@ -360,6 +391,61 @@ def lq_qkv(head_dim: int, q_heads: int, kv_heads: int, sequences: int, norm: int
 def lq_qkv_forward(layer, act, X_dev_ptr: int, M: int, adapters, rowmap, qkv: LqQkv, Y_dev_ptr: int, dtype: int = OUT_F16, stream: int = 0):
     """Quantizer, GEMM, the rows' adapters (both handles, or None), norm and rotation of queries and keys: Y [M, N]."""
     _check(lib().lq_qkv_forward(layer, act, X_dev_ptr, M, adapters, rowmap, qkv, Y_dev_ptr, dtype, stream), "lq_qkv_forward")
+
+
+def lq_kvcache_create(layers: int, pages: int, page_tokens: int, kv_heads: int, head_dim: int, device: int = 0):
+    h = C.c_void_p()
+    _check(lib().lq_kvcache_create(layers, pages, page_tokens, kv_heads, head_dim, device, C.byref(h)), "lq_kvcache_create")
+    return h
+
+
+def lq_kvcache_free(cache):
+    _check(lib().lq_kvcache_free(cache), "lq_kvcache_free")
+
+
+def lq_kvbatch(sequences: int, rows: int, length_ptr: int, pages_ptr: int, page_stride: int, row_start_ptr: int | None = None) -> LqKvBatch:
+    """The sequences of a step: int32 arrays on the device; without row_start every sequence has rows / sequences rows."""
+    return LqKvBatch(sequences, rows, row_start_ptr, length_ptr, pages_ptr, page_stride)
+
+
+def lq_kvrows(k_ptr: int | None, k_strides, v_ptr: int | None, v_strides) -> LqKvRows:
+    """Keys and values; strides of sequence (outputs alone), row and head in elements."""
+    return LqKvRows(k_ptr, v_ptr, *k_strides, *v_strides)
+
+
+def lq_kvcache_append(cache, layer: int, batch: LqKvBatch, rows: LqKvRows, dtype: int = OUT_F16, stream: int = 0):
+    """Quantises the batch's rows into the cache as each sequence's last tokens."""
+    _check(lib().lq_kvcache_append(cache, layer, batch, rows, dtype, stream), "lq_kvcache_append")
+
+
+def lq_kvcache_read(cache, layer: int, batch: LqKvBatch, begin_dev_ptr: int | None, max_tokens: int, rows: LqKvRows, dtype: int = OUT_F16, stream: int = 0):
+    """Tokens from begin (None: the first) to each sequence's length, at most max_tokens, as values."""
+    _check(lib().lq_kvcache_read(cache, layer, batch, begin_dev_ptr, max_tokens, rows, dtype, stream), "lq_kvcache_read")
+
+
+def lq_attn(q_ptr: int, q_strides, out_ptr: int, out_strides, q_heads: int, scale: float, causal: bool = True, window: int = 0, sinks: int = 0) -> LqAttn:
+    """Queries and output of an attention call; strides of row and head in elements."""
+    return LqAttn(q_ptr, out_ptr, *q_strides, *out_strides, q_heads, int(causal), window, sinks, scale)
+
+
+def lq_cache_attention(cache, layer: int, batch: LqKvBatch, attn: LqAttn, stream: int = 0):
+    _check(lib().lq_cache_attention(cache, layer, batch, attn, stream), "lq_cache_attention")
+
+
+def lq_residual(rows: int, features: int, x_ptr: int, x_out_ptr: int | None, h_ptr: int | None, y_ptr: int | None = None, sequences: int = 1,
+                after: int = NORM_NONE, after_weight_ptr: int | None = None, factor: float = 1.0, gate_ptr: int | None = None,
+                norm: int = NORM_NONE, weight_ptr: int | None = None, bias_ptr: int | None = None, scale_ptr: int | None = None,
+                shift_ptr: int | None = None, mod_seq: int = 0, eps: float = 1e-6, x_dtype: int = OUT_F16, y_dtype: int = OUT_F16,
+                h_dtype: int = OUT_F16, mod_dtype: int = OUT_F16, strides=None, device: int = 0) -> LqResidual:
+    """strides: of the rows of x, y, x_out and h in elements (None: rows follow each other)."""
+    st = strides or (features,) * 4
+    return LqResidual(x_ptr, y_ptr, x_out_ptr, h_ptr, *st, after_weight_ptr, weight_ptr, bias_ptr, gate_ptr, scale_ptr, shift_ptr, mod_seq, rows,
+                      features, sequences, after, norm, x_dtype, y_dtype, h_dtype, mod_dtype, factor, eps, device)
+
+
+def lq_residual_norm(residual: LqResidual, stream: int = 0):
+    """x' = x + factor * gate * N1(y) and h = (N2(x') * weight + bias) * (1 + scale) + shift."""
+    _check(lib().lq_residual_norm(residual, stream), "lq_residual_norm")
 
 
 def lq_act_export(act, M: int, cfg: LqConfig, stream: int = 0) -> dict:

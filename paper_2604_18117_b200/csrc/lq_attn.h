@@ -1,0 +1,66 @@
+// Attention over the cache: what its two forms share (lq_attn.cu, lq_attn_tile.cu).
+#pragma once
+
+#include "lq_kvcache.h"
+
+struct LqAttnParams {
+  LqBatch b;
+  const uint8_t* records;
+  const __half* q;
+  __half* out;
+  long long q_row, q_head, out_row, out_head;
+  int D, Dp, group;                      // query heads of a head of keys and values
+  int causal, window, sinks;
+  float scale;                           // of the products of queries and stored keys, times log2 e
+  float* part;
+  int* count;
+  int few, many;                         // sequences whose rows * group are in [few, many) are this launch's
+  int32_t* status;
+};
+
+// Sequences of up to so many rows (new tokens x query heads of a group) are the form for few rows'
+constexpr int LQ_ATTN_FEW = 64;
+
+lq_status lq_attn_tile_launch(const lq_kvcache* C, const LqAttnParams& p, cudaStream_t st);
+
+#ifdef __CUDACC__
+// Tokens that any of the rows at places lo .. hi of a sequence may see, as blocks of 32: the first `sink` ones and those from `from` to `to` - 1;
+// the b-th of them, and how many.
+struct LqSeen {
+  int sink, from, to;
+  __device__ __forceinline__ int count() const { return sink + to - from; }
+  __device__ __forceinline__ int block(int b) const { return b < sink ? b : b - sink + from; }
+};
+__device__ __forceinline__ LqSeen lq_seen(const LqAttnParams& p, int lo, int hi, int len) {
+  LqSeen s{0, 0, (len + LQ_KV_BLOCK - 1) / LQ_KV_BLOCK};
+  if (p.causal) {
+    s.to = hi / LQ_KV_BLOCK + 1;
+    if (p.window > 0 && lo >= p.window) {
+      s.from = (lo - p.window + 1) / LQ_KV_BLOCK;
+      s.sink = min(s.from, (min(p.sinks, len) + LQ_KV_BLOCK - 1) / LQ_KV_BLOCK);
+    }
+  }
+  return s;
+}
+// whether the row at place `at` sees token t
+__device__ __forceinline__ bool lq_sees(const LqAttnParams& p, int at, int t, int len) {
+  if (!p.causal) return t < len;
+  return t <= at && (p.window == 0 || t > at - p.window || t < p.sinks);
+}
+// whether all rows at places lo .. hi see all tokens t0 .. t1
+__device__ __forceinline__ bool lq_all_seen(const LqAttnParams& p, int lo, int hi, int t0, int t1, int len) {
+  if (!p.causal) return t1 < len;
+  return t1 <= lo && (p.window == 0 || t0 > hi - p.window || t1 < p.sinks);
+}
+// whether this launch takes a sequence, and whether it can be taken at all
+__device__ __forceinline__ bool lq_attn_takes(const LqAttnParams& p, const LqSeq& q, bool tell) {
+  if (q.n == 0) return false;
+  const long long rows = (long long)q.n * p.group;
+  if (rows < p.few || rows >= p.many) return false;
+  if (!lq_seq_fits(p.b, q) || (p.causal && q.len < q.n)) {
+    if (tell) lq_kv_refuse(p.status);
+    return false;
+  }
+  return true;
+}
+#endif

@@ -1,0 +1,98 @@
+// The cache of keys and values: its handle, how it lies in memory, and how a step's sequences are found in it (lq_kvcache.cu, lq_attn.cu,
+// lq_attn_tile.cu).
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "lq_internal.h"
+
+// A record holds 32 tokens of one head: their keys, their values, and a tail of 32 bytes that begins with the exponents of both.  Codes are
+// kept as bytes u = c + 128, in the order in which a warp of the attention kernels reads them as operands of m16n8k16 products, 16 bytes a
+// lane (c8 = lane / 4, t = lane % 4) for every 16 entries of the head:
+//   keys    word i = 2 s + h: token 16 s + 4 (c8 / 2) + 2 h + c8 % 2, bytes: entries 4 t .. 4 t + 3 of the 16 (column c8 of the products' tile i)
+//   values  word 2 s + i: entry 2 c8 + i of the 16, bytes: tokens 16 s + 4 t .. 4 t + 3
+// so that every load is one of 16 bytes a lane, neighbours across lanes, and no byte has to change lanes.
+// Records follow each other by layer, page, block of the page and head.
+constexpr int LQ_KV_TAIL = 32, LQ_KV_E_MIN = -20, LQ_KV_E_MAX = 9;
+static inline __host__ __device__ int lq_kv_side_bytes(int Dp) { return LQ_KV_BLOCK * Dp; }
+static inline __host__ __device__ int lq_kv_record_bytes(int Dp) { return 2 * lq_kv_side_bytes(Dp) + LQ_KV_TAIL; }
+
+// heads are stored padded to the next of these
+constexpr int LQ_KV_DIMS[] = {64, 80, 96, 112, 128, 192, 256};
+static inline int lq_kv_padded(int D) {
+  for (int d : LQ_KV_DIMS)
+    if (D <= d) return d;
+  return 0;
+}
+
+constexpr int LQ_ATTN_ROWS = 16;         // rows (new tokens x query heads of a group) of a tile of the form for few rows
+struct lq_kvcache {
+  int layers, pages, page_tokens, heads, D, Dp, device, sms;
+  uint8_t* d_records;
+  // workspace of the attention: for each block of its grid two partial results of a tile of rows, and a count of those that have arrived
+  float* d_part;                         // [2 * sms][LQ_ATTN_ROWS][Dp + 2]
+  int* d_count;                          // [sms]
+};
+
+// A step's sequences, as kernels take them
+struct LqBatch {
+  const int32_t *row_start, *length, *pages;
+  int sequences, rows, each;             // each: rows of every sequence where row_start is NULL
+  int page_stride, page_count, page_blocks, heads;
+  long long record;                      // bytes
+};
+
+// checks a caller's batch against a cache; LQ_OK fills *out
+lq_status lq_take_batch(const lq_kvcache* C, int32_t layer, const lq_kvbatch* b, LqBatch* out);
+static inline uint8_t* lq_kv_layer(const lq_kvcache* C, int layer) {
+  return C->d_records + (size_t)layer * C->pages * (C->page_tokens / LQ_KV_BLOCK) * C->heads * lq_kv_record_bytes(C->Dp);
+}
+lq_status lq_attn_prepare(const lq_kvcache* C);        // once for each cache, with its device current
+lq_status lq_attn_tile_prepare(const lq_kvcache* C);
+
+#ifdef __CUDACC__
+// Rows of a sequence and its tokens.  What the arrays hold is the caller's: rows are kept within the call's, so that nothing outside its
+// tensors is touched.
+struct LqSeq {
+  int row, n, len;                       // first row, rows, tokens with them
+};
+__device__ __forceinline__ LqSeq lq_seq(const LqBatch& b, int s) {
+  LqSeq q;
+  if (b.row_start) {
+    q.row = max(0, min(b.row_start[s], b.rows));
+    q.n = max(0, min(b.row_start[s + 1], b.rows) - q.row);
+  } else {
+    q.row = s * b.each;
+    q.n = b.each;
+  }
+  q.len = b.length[s];
+  return q;
+}
+// Whether a sequence's length fits its row of pages.  A kernel that meets another says so in the status word and leaves the sequence out.
+__device__ __forceinline__ bool lq_seq_fits(const LqBatch& b, const LqSeq& q) {
+  return q.len >= 0 && ((long long)q.len + LQ_KV_BLOCK - 1) / LQ_KV_BLOCK <= (long long)b.page_stride * b.page_blocks;
+}
+__device__ __forceinline__ void lq_kv_refuse(int32_t* status) {
+  if (atomicCAS(status, 0, (int)LQ_ERR_INVALID_ARG) == 0) status[1] = LQ_STAGE_NONE;
+}
+// index of a block's first record (of head 0), or -1: the page is none of the cache's
+__device__ __forceinline__ long long lq_kv_at(const LqBatch& b, int s, int block) {
+  const int slot = block / b.page_blocks, page = b.pages[(long long)s * b.page_stride + slot];
+  if (page < 0 || page >= b.page_count) return -1;
+  return ((long long)page * b.page_blocks + (block - slot * b.page_blocks)) * b.heads;
+}
+// Two codes of a word (SEL: 0x4140 the lower two, 0x4342 the upper two) as halves, each times 2^(e - 4): a byte u under the upper byte `high` of a
+// half is (1024 + u) 2^(e - 4), and what `less` takes off leaves u - 128 = c of that, all of it exact for e in [-20, 9].
+__device__ __forceinline__ uint32_t lq_kv_high(int e) { return 0x01010101u * (uint32_t)(0x64 + 4 * (e - 4)); }
+__device__ __forceinline__ __half2 lq_kv_less(uint32_t high) {          // 1152 2^(e - 4) = 1024 2^(e - 4) + 128 2^(e - 4)
+  const uint32_t h = ((high & 0xFF) << 8) | 0x80;
+  const uint32_t w = h | (h << 16);
+  return *reinterpret_cast<const __half2*>(&w);
+}
+template <uint32_t SEL>
+__device__ __forceinline__ uint32_t lq_kv_open(uint32_t word, uint32_t high, __half2 less) {
+  const uint32_t w = __byte_perm(word, high, SEL);
+  const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&w), less);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+#endif
