@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblq.so")
-SOURCES = ["lq_api.cu", "lq_quant.cu", "lq_gemm.cu", "lq_gemm_mx.cu", "lq_noalloc.cu", "lq_adapters.cu", "lq_adapters_tile.cu", "lq_heads.cu", "lq_kvcache.cu", "lq_attn.cu",
+SOURCES = ["lq_api.cu", "lq_quant.cu", "lq_gemm.cu", "lq_gemm_mx.cu", "lq_noalloc.cu", "lq_adapters.cu", "lq_adapters_tile.cu", "lq_heads.cu", "lq_kvcache.cu", "lq_attn.cu", "lq_attn_tile.cu",
            "lq_residual.cu", "lq_calibrate.cpp"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

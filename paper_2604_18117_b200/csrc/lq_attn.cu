@@ -405,7 +405,8 @@ cudaError_t launch_few(const lq_kvcache* C, const LqAttnParams& p, cudaStream_t 
 lq_status lq_attn_prepare(const lq_kvcache* C) {
   const bool ok = C->Dp == 64 ? room<4, 8, 4>() : C->Dp == 80 ? room<5, 8, 3>() : C->Dp == 96 ? room<6, 8, 2>() : C->Dp == 112 ? room<7, 8, 2>()
                   : C->Dp == 128 ? room<8, 8, 2>() : C->Dp == 192 ? room<12, 4, 3>() : room<16, 4, 2>();
-  return ok ? LQ_OK : LQ_ERR_CUDA;
+  if (!ok) return LQ_ERR_CUDA;
+  return C->Dp <= 128 ? lq_attn_tile_prepare(C) : LQ_OK;
 }
 
 extern "C" lq_status lq_cache_attention(const lq_kvcache* C, int32_t layer, const lq_kvbatch* batch, const lq_attn* a, void* stream) {
@@ -440,6 +441,19 @@ extern "C" lq_status lq_cache_attention(const lq_kvcache* C, int32_t layer, cons
   p.scale = a->scale * 16.f * 1.44269504088896341f;        // (keys are opened as 2^-4 of themselves)
   p.part = C->d_part; p.count = C->d_count;
   p.status = lq_device_status_ptr(C->device);
-  p.few = 1; p.many = 0x7fffffff;
-  return lq_note_cuda(launch_few(C, p, (cudaStream_t)stream)) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+  // Which form a sequence's rows are the kernels tell by themselves where sequences have different numbers of them; a form that no sequence can be is
+  // not launched.
+  const bool tiles = C->Dp <= 128;
+  const long long most = p.b.row_start ? (long long)p.b.rows * p.group : (long long)p.b.each * p.group, least = p.b.row_start ? 1 : most;
+  if (!tiles || least <= LQ_ATTN_FEW) {
+    p.few = 1;
+    p.many = tiles ? LQ_ATTN_FEW + 1 : 0x7fffffff;
+    if (lq_note_cuda(launch_few(C, p, (cudaStream_t)stream)) != cudaSuccess) return LQ_ERR_CUDA;
+  }
+  if (tiles && most > LQ_ATTN_FEW) {
+    p.few = LQ_ATTN_FEW + 1;
+    p.many = 0x7fffffff;
+    return lq_attn_tile_launch(C, p, (cudaStream_t)stream);
+  }
+  return LQ_OK;
 }

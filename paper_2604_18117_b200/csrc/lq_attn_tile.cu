@@ -1,0 +1,473 @@
+// Attention over the cache, the form for many rows of heads of up to 128 entries: tiles of 256 rows (new tokens x query heads of a group) on
+// tcgen05.
+//
+//   S = Q K^T,   P = 2^(S c - m c),   O += P V,   l += P 1        over 128 tokens (four records) at a time, m a maximum of the row so far
+//
+// What bounds it is the tensor cores and what feeds them.  Four warps open the records to halves in shared memory (two buffers of K and V, in
+// the core matrices of K-major operands; with the pads below no two lanes of a store meet in a bank); one thread issues the products; two
+// groups of four warps have 128 rows each, a row a thread, and take turns with the tensor cores: while one forms P of its rows, the products
+// of the other run.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
+// there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are up to 2^8,
+// which halves and sums hold as well, and the last division takes care of it.
+#include <math.h>
+
+#include "lq_attn.h"
+#include "lq_device.cuh"
+
+using namespace lqdev;
+
+namespace {
+
+constexpr int TILE = 128, KV = 128, SOFT_WARPS = 8, OPEN_WARPS = 4, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 32 * (MMA_WARP + 1);
+constexpr int TMEM_COLS = 512;
+constexpr uint32_t COL_S = 0, COL_O = 256;                 // of the first 128 rows; the other's are 128 columns on
+constexpr float GROWTH = 8.f;
+
+// Core matrices (8 rows x 16 bytes) lie [16-byte column][row]: a column of K or Q has 128 rows, of V (whose rows are the head's entries) Dp.
+// Lanes c8 / 2, t of a store of K are 2 columns and rows 0, 1, 4, 5 of 16 bytes: with columns 32 bytes beyond a multiple of 128 apart they take all
+// banks once; of V 2 columns and every second row: 16 bytes.
+constexpr int Q_LBO = 128 * 16, K_LBO = KV * 16 + 32;
+__host__ __device__ constexpr int v_lbo(int Dp) { return Dp * 16 + 16; }
+__host__ __device__ constexpr int k_bytes(int Dp) { return (Dp / 8 * K_LBO + 127) / 128 * 128; }
+__host__ __device__ constexpr int v_bytes(int Dp) { return (KV / 8 * v_lbo(Dp) + 127) / 128 * 128; }
+__host__ __device__ constexpr int q_bytes(int Dp) { return Dp / 8 * Q_LBO; }
+
+struct Control {
+  uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint32_t tmem;
+  alignas(4) uint8_t missing[4][4];                 // of the last tiles: whether record i is no page's
+  int abort_flag;
+  int place[2];
+  int prefix[THREADS + 1];
+};
+
+__device__ __forceinline__ void tmem_ld_32(uint32_t taddr, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
+        "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]),
+        "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]),
+      "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// the same product with A in tensor memory: row r in lane r, two halves a column
+__device__ __forceinline__ void tc_mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void sts_v2(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
+
+// What a block works on.
+struct Task {
+  LqSeq q;
+  LqSeen seen;
+  int s, head, row0, rows, tiles;        // rows: of up to 256; tiles: of 128 tokens
+};
+
+template <int NK>
+__global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_constant__ LqAttnParams p) {
+  constexpr int DP = 16 * NK, V_LBO = v_lbo(DP);
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t* sq = smem;                                      // [2]
+  uint8_t* sk = sq + 2 * q_bytes(DP);                      // [2]
+  uint8_t* sv = sk + 2 * k_bytes(DP);                      // [2]
+  Control& c = *reinterpret_cast<Control*>(sv + 2 * v_bytes(DP));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&c.q_full[i]), 4);
+      mbar_init(smem_u32(&c.k_full[i]), OPEN_WARPS);
+      mbar_init(smem_u32(&c.v_full[i]), OPEN_WARPS);
+      mbar_init(smem_u32(&c.k_empty[i]), 1);
+      mbar_init(smem_u32(&c.v_empty[i]), 1);
+      mbar_init(smem_u32(&c.s_full[i]), 1);
+      mbar_init(smem_u32(&c.p_full[i]), 4);
+      mbar_init(smem_u32(&c.o_full[i]), 1);
+    }
+    c.abort_flag = 0;
+    mbar_init_fence();
+  }
+  if (warp == MMA_WARP) tmem_alloc(smem_u32(&c.tmem), TMEM_COLS);
+  __syncthreads();                                         // (a kernel that starts early finds this block's tensor memory taken)
+  grid_launch_dependents();
+  grid_dependency_wait();
+
+  // the block's sequence and tile of rows: blocks of a tile's heads follow each other, a sequence's last tiles (which see most) come first
+  Task k = {};
+  k.head = blockIdx.x % p.b.heads;
+  const int unit = blockIdx.x / p.b.heads;
+  if (!p.b.row_start) {
+    const int each = (int)(((long long)p.b.each * p.group + 2 * TILE - 1) / (2 * TILE)), back = unit / p.b.sequences;
+    k.s = unit - back * p.b.sequences;
+    k.row0 = (each - 1 - back) * 2 * TILE;
+    k.q = lq_seq(p.b, k.s);
+    if (!lq_attn_takes(p, k.q, blockIdx.x < p.b.heads * p.b.sequences)) k.s = -1;
+  } else {
+    const int chunk = (p.b.sequences + THREADS - 1) / THREADS;
+    int sum = 0;
+    for (int s = tid * chunk; s < min(p.b.sequences, (tid + 1) * chunk); ++s) {
+      const LqSeq q = lq_seq(p.b, s);
+      if (lq_attn_takes(p, q, blockIdx.x == 0)) sum += (int)(((long long)q.n * p.group + 2 * TILE - 1) / (2 * TILE));
+    }
+    int up = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int v = __shfl_up_sync(0xffffffffu, up, d);
+      if (lane >= d) up += v;
+    }
+    if (lane == 31) c.prefix[warp] = up;
+    if (tid == 0) c.place[0] = -1;
+    __syncthreads();
+    int base = up - sum;
+    for (int i = 0; i < warp; ++i) base += c.prefix[i];
+    if (unit >= base && unit < base + sum)                 // in this thread's sequences
+      for (int s = tid * chunk; s < min(p.b.sequences, (tid + 1) * chunk); ++s) {
+        const LqSeq q = lq_seq(p.b, s);
+        if (!lq_attn_takes(p, q, false)) continue;
+        const int tiles = (int)(((long long)q.n * p.group + 2 * TILE - 1) / (2 * TILE));
+        if (unit < base + tiles) {
+          c.place[0] = s;
+          c.place[1] = (tiles - 1 - (unit - base)) * 2 * TILE;
+          break;
+        }
+        base += tiles;
+      }
+    __syncthreads();
+    k.s = c.place[0];
+    k.row0 = c.place[1];
+    if (k.s >= 0) k.q = lq_seq(p.b, k.s);
+  }
+  const uint32_t tmem = *const_cast<volatile uint32_t*>(&c.tmem);
+  const int base = k.q.len - k.q.n;
+  if (k.s >= 0) {
+    k.rows = min(2 * TILE, k.q.n * p.group - k.row0);
+    k.seen = lq_seen(p, base + k.row0 / p.group, base + (k.row0 + k.rows - 1) / p.group, k.q.len);
+    k.tiles = (k.seen.count() + 3) / 4;
+  } else {
+    k.rows = 0; k.tiles = 0;
+  }
+  const int halves = k.rows > TILE ? 2 : 1;
+  bool good = true;
+  const auto wait = [&](uint64_t& bar, int phase, int role) {
+    if (good) good = mbar_wait_warp(smem_u32(&bar), phase & 1, &c.abort_flag, p.status, role);
+    return good;
+  };
+
+  if (warp < SOFT_WARPS) {
+    const int half = warp / 4, row = (warp & 3) * 32 + lane;
+    if (half < halves && k.rows > 0) {
+      const int r = k.row0 + half * TILE + row, all_rows = k.q.n * p.group;
+      const bool real = r < all_rows;
+      const int tok = min(r, all_rows - 1) / p.group, at = base + tok;
+      const long long qh = k.head * p.group + (min(r, all_rows - 1) - tok * p.group);
+      const int r_lo = k.row0 + half * TILE + (warp & 3) * 32;
+      const int lo = base + min(r_lo, all_rows - 1) / p.group, hi = base + min(r_lo + 31, all_rows - 1) / p.group;
+      // the row of Q, with the sign of the scale; 16-byte columns, a row's neighbours beside it
+      {
+        const uint4* from = reinterpret_cast<const uint4*>(p.q + (k.q.row + tok) * p.q_row + qh * p.q_head);
+        const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
+        const uint32_t to = smem_u32(sq + half * q_bytes(DP)) + row * 16;
+#pragma unroll
+        for (int g = 0; g < DP / 8; ++g) {
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (real && 8 * g < p.D) {
+            v = from[g];
+            v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
+          }
+          sts_v4(to + g * Q_LBO, v);
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&c.q_full[half]));
+      }
+      const float scale = fabsf(p.scale);
+      const uint32_t lanes = (uint32_t)(warp & 3) << 21, ts = tmem + lanes + COL_S + half * 128, to = tmem + lanes + COL_O + half * 128;
+      float m = -INFINITY, l = 0.f;                        // m: what the weights are below, times scale
+      for (int j = 0; j < k.tiles; ++j) {
+        if (!wait(c.s_full[half], j, LQ_STAGE_DRAIN)) break;
+        tc_fence_after();
+        const uint32_t missing = *reinterpret_cast<volatile uint32_t*>(c.missing[j & 3]);
+        // what of the tile's four blocks the warp's rows see: all, some, nothing
+        int first[4], kind[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int b = 4 * j + i;
+          first[i] = k.seen.block(b) * LQ_KV_BLOCK;
+          kind[i] = b >= k.seen.count() || (missing >> (8 * i) & 1) ? 2 : lq_all_seen(p, lo, hi, first[i], first[i] + LQ_KV_BLOCK - 1, k.q.len) ? 0 : 1;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t v[32];
+          if (kind[i] == 2) continue;
+          tmem_ld_32(ts + 32 * i, v);
+          tmem_ld_wait();
+          if (kind[i] == 0) {
+            float a = -INFINITY, b = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 32; x += 4) {
+              a = fmaxf(fmaxf(a, __uint_as_float(v[x])), __uint_as_float(v[x + 1]));
+              b = fmaxf(fmaxf(b, __uint_as_float(v[x + 2])), __uint_as_float(v[x + 3]));
+            }
+            top = fmaxf(top, fmaxf(a, b));
+          } else {
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (lq_sees(p, at, first[i] + x, k.q.len)) top = fmaxf(top, __uint_as_float(v[x]));
+          }
+        }
+        top *= scale;                                      // (-inf times a scale of zero is no number, and counts as nothing seen)
+        if (!(top > -INFINITY)) top = -INFINITY;
+        const bool grow = top > m + GROWTH || (m == -INFINITY && top > -INFINITY);
+        if (__any_sync(0xffffffffu, grow)) {
+          // (a row that has seen nothing yet has sums of zero; its factor is one)
+          const float by = grow && m > -INFINITY ? ex2(m - top) : 1.f;
+          if (grow) { l *= by; m = top; }
+          if (j > 0 && __any_sync(0xffffffffu, by != 1.f))
+#pragma unroll 1
+            for (int x = 0; x < DP; x += 16) {
+              uint32_t v[16];
+              tmem_ld_32x16(to + x, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int y = 0; y < 16; ++y) v[y] = __float_as_uint(__uint_as_float(v[y]) * by);
+              tmem_st_16(to + x, v);
+            }
+        }
+        const float ref = m > -INFINITY ? -m : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t v[32], w[16];
+          if (kind[i] == 2) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) w[x] = 0;
+          } else {
+            tmem_ld_32(ts + 32 * i, v);
+            tmem_ld_wait();
+            float a = 0.f, b = 0.f;
+#pragma unroll
+            for (int x = 0; x < 32; x += 2) {
+              float e0 = ex2(fmaf(__uint_as_float(v[x]), scale, ref)), e1 = ex2(fmaf(__uint_as_float(v[x + 1]), scale, ref));
+              if (kind[i] == 1) {
+                e0 = lq_sees(p, at, first[i] + x, k.q.len) ? e0 : 0.f;
+                e1 = lq_sees(p, at, first[i] + x + 1, k.q.len) ? e1 : 0.f;
+              }
+              a += e0; b += e1;
+              w[x / 2] = pack(e0, e1);
+            }
+            l += a + b;
+          }
+          tmem_st_16(ts + 16 * i, w);                      // (over columns of S that have been read)
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&c.p_full[half]));
+      }
+      // values were opened as 2^-4 of themselves
+      const float by = l > 0.f ? 16.f / l : 0.f;
+      __half* out = p.out + (k.q.row + tok) * p.out_row + qh * p.out_head;
+      if (k.tiles > 0 && wait(c.o_full[half], 0, LQ_STAGE_DRAIN)) tc_fence_after();
+      if (good)
+#pragma unroll 1
+        for (int x = 0; x < DP; x += 16) {
+          uint32_t v[16] = {};
+          if (k.tiles > 0) {
+            tmem_ld_32x16(to + x, v);
+            tmem_ld_wait();
+          }
+          uint32_t w[8];
+#pragma unroll
+          for (int y = 0; y < 8; ++y) w[y] = pack(__uint_as_float(v[2 * y]) * by, __uint_as_float(v[2 * y + 1]) * by);
+          if (real && x < p.D) *reinterpret_cast<uint4*>(out + x) = make_uint4(w[0], w[1], w[2], w[3]);
+          if (real && x + 8 < p.D) *reinterpret_cast<uint4*>(out + x + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+      tc_fence_before();
+    }
+  } else if (warp < MMA_WARP) {
+    // Warp w opens record w of every tile.  A record's codes are asked for as soon as those of the one before have been opened.
+    const int w = warp - SOFT_WARPS, c8 = lane >> 2, t = lane & 3, count = k.tiles > 0 ? k.seen.count() : 0;
+    uint4 kr[NK], vr[NK];
+    uint32_t tail = 0, tail_next = 0;
+    long long at = -1, at_next = -1;
+    const uint8_t* rec = nullptr;
+    const auto find = [&](int j) -> long long {            // the record of tile j, -1: behind the last or no page's
+      const int b = 4 * j + w;
+      if (j >= k.tiles || b >= count) return -1;
+      const long long x = lq_kv_at(p.b, k.s, k.seen.block(b));
+      if (x < 0 && lane == 0) lq_kv_refuse(p.status);
+      return x;
+    };
+    const auto of = [&](long long x) { return p.records + (x + k.head) * p.b.record; };
+    at = find(0);
+    if (at >= 0) {
+      rec = of(at);
+#pragma unroll
+      for (int g = 0; g < NK; ++g) kr[g] = reinterpret_cast<const uint4*>(rec)[32 * g + lane];
+#pragma unroll
+      for (int g = 0; g < NK; ++g) vr[g] = reinterpret_cast<const uint4*>(rec)[32 * (NK + g) + lane];
+      tail = *reinterpret_cast<const uint32_t*>(rec + 64 * DP);
+    }
+    const int token = 32 * w + 4 * (c8 >> 1) + (c8 & 1);
+    const uint32_t kto = smem_u32(sk) + (t >> 1) * K_LBO + token * 16 + (t & 1) * 8;
+    const uint32_t vto = smem_u32(sv) + (4 * w + (t >> 1)) * V_LBO + 2 * c8 * 16 + (t & 1) * 8;
+    for (int j = 0; j < k.tiles; ++j) {
+      const int st = j & 1;
+      at_next = find(j + 1);
+      const uint8_t* next = at_next >= 0 ? of(at_next) : nullptr;
+      if (j >= 2 && !wait(c.k_empty[st], (j >> 1) - 1, LQ_STAGE_PRODUCER)) break;
+      {
+        const uint32_t high = lq_kv_high((int8_t)(tail & 0xFF)), to = kto + st * k_bytes(DP);
+        const __half2 less = lq_kv_less(high);
+        if (lane == 0) c.missing[j & 3][w] = at < 0;
+#pragma unroll
+        for (int g = 0; g < NK; ++g) {
+          const uint32_t u[4] = {kr[g].x, kr[g].y, kr[g].z, kr[g].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t a = to + 2 * g * K_LBO + (16 * (i >> 1) + 2 * (i & 1)) * 16;
+            if (at >= 0) sts_v2(a, lq_kv_open<0x4140>(u[i], high, less), lq_kv_open<0x4342>(u[i], high, less));
+            else sts_v2(a, 0, 0);
+          }
+          if (next) kr[g] = reinterpret_cast<const uint4*>(next)[32 * g + lane];
+        }
+        if (next) tail_next = *reinterpret_cast<const uint32_t*>(next + 64 * DP);
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&c.k_full[st]));
+      if (j >= 2 && !wait(c.v_empty[st], (j >> 1) - 1, LQ_STAGE_PRODUCER)) break;
+      {
+        const uint32_t high = lq_kv_high((int8_t)(tail >> 8 & 0xFF)), to = vto + st * v_bytes(DP);
+        const __half2 less = lq_kv_less(high);
+#pragma unroll
+        for (int g = 0; g < NK; ++g) {
+          const uint32_t u[4] = {vr[g].x, vr[g].y, vr[g].z, vr[g].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t a = to + (i >> 1) * 2 * V_LBO + (16 * g + (i & 1)) * 16;
+            if (at >= 0) sts_v2(a, lq_kv_open<0x4140>(u[i], high, less), lq_kv_open<0x4342>(u[i], high, less));
+            else sts_v2(a, 0, 0);
+          }
+          if (next) vr[g] = reinterpret_cast<const uint4*>(next)[32 * (NK + g) + lane];
+        }
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&c.v_full[st]));
+      at = at_next;
+      tail = tail_next;
+    }
+  } else if (k.tiles > 0) {
+    const uint32_t idesc_s = IDESC_F16 | idesc_shape(KV), idesc_o = IDESC_F16 | idesc_shape(DP);
+    const auto product_s = [&](int half, int st) {         // by one thread
+      const uint32_t a = smem_u32(sq + half * q_bytes(DP)), b = smem_u32(sk + st * k_bytes(DP));
+#pragma unroll
+      for (int x = 0; x < NK; ++x)
+        tc_mma<TC_F16>(tmem + COL_S + half * 128, make_smem_desc_plain(a + 2 * x * Q_LBO, Q_LBO, 128), make_smem_desc_plain(b + 2 * x * K_LBO, K_LBO, 128), idesc_s,
+                       x > 0);
+    };
+    const auto product_o = [&](int half, int st, bool add) {
+      const uint32_t b = smem_u32(sv + st * v_bytes(DP));
+#pragma unroll
+      for (int x = 0; x < KV / 16; ++x)
+        tc_mma_ta(tmem + COL_O + half * 128, tmem + COL_S + half * 128 + 8 * x, make_smem_desc_plain(b + 2 * x * V_LBO, V_LBO, 128), idesc_o, add || x > 0);
+    };
+    wait(c.k_full[0], 0, LQ_STAGE_MMA);
+    for (int half = 0; half < halves; ++half) {
+      if (!wait(c.q_full[half], 0, LQ_STAGE_MMA)) break;
+      tc_fence_after();
+      if (elect_one()) {
+        product_s(half, 0);
+        tc_commit(smem_u32(&c.s_full[half]));
+        if (half == halves - 1) tc_commit(smem_u32(&c.k_empty[0]));
+      }
+      __syncwarp();
+    }
+    for (int j = 0; j < k.tiles && good; ++j) {
+      const int st = j & 1, next = st ^ 1;
+      const bool last = j == k.tiles - 1;
+      for (int half = 0; half < halves; ++half) {
+        if (half == 0 && !wait(c.v_full[st], j >> 1, LQ_STAGE_MMA)) break;
+        if (!wait(c.p_full[half], j, LQ_STAGE_MMA)) break;
+        if (half == 0 && !last && !wait(c.k_full[next], (j + 1) >> 1, LQ_STAGE_MMA)) break;
+        tc_fence_after();
+        if (elect_one()) {
+          product_o(half, st, j > 0);
+          if (half == halves - 1) tc_commit(smem_u32(&c.v_empty[st]));
+          if (last) {
+            tc_commit(smem_u32(&c.o_full[half]));
+          } else {
+            product_s(half, next);
+            tc_commit(smem_u32(&c.s_full[half]));
+            if (half == halves - 1) tc_commit(smem_u32(&c.k_empty[next]));
+          }
+        }
+        __syncwarp();
+      }
+    }
+    if (!good) {                                           // a wait gave up: what has been issued gets a bounded time to end
+      if (elect_one()) tc_commit(smem_u32(&c.q_full[0]));
+      __syncwarp();
+      mbar_settle(smem_u32(&c.o_full[0]), 0);
+    }
+  }
+  __syncthreads();
+  if (warp == MMA_WARP) {
+    tc_fence_after();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+size_t tile_smem(int Dp) { return 2 * (size_t)(q_bytes(Dp) + k_bytes(Dp) + v_bytes(Dp)) + sizeof(Control); }
+
+template <typename F>
+auto with_size(int Dp, const F& f) {
+  switch (Dp) {
+    case 64: return f(lq_attn_tile_kernel<4>);
+    case 80: return f(lq_attn_tile_kernel<5>);
+    case 96: return f(lq_attn_tile_kernel<6>);
+    case 112: return f(lq_attn_tile_kernel<7>);
+    default: return f(lq_attn_tile_kernel<8>);
+  }
+}
+
+}  // namespace
+
+lq_status lq_attn_tile_prepare(const lq_kvcache* C) {
+  return with_size(C->Dp, [&](auto* kernel) {
+           return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tile_smem(C->Dp)));
+         }) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+}
+
+lq_status lq_attn_tile_launch(const lq_kvcache* C, const LqAttnParams& p, cudaStream_t st) {
+  // tiles of 256 rows: exactly so many where all sequences have as many rows; else at most one of each sequence is not full
+  const long long units = p.b.row_start ? (long long)p.b.rows * p.group / (2 * TILE) + p.b.sequences
+                                        : p.b.sequences * (((long long)p.b.each * p.group + 2 * TILE - 1) / (2 * TILE));
+  if (units * C->heads > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
+  const cudaError_t e = with_size(C->Dp, [&](auto* kernel) { return lq_launch(kernel, (int)(units * C->heads), THREADS, tile_smem(C->Dp), st, p); });
+  return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+}
