@@ -61,7 +61,7 @@ __device__ __forceinline__ void seek(const LqAttnParams& p, Place& at, long long
 
 template <int NK, int WARPS, int STAGES>
 struct Shared {
-  static constexpr int DP = 16 * NK, REC = 2 * LQ_KV_BLOCK * DP + LQ_KV_TAIL, PITCH = DP + 4;
+  static constexpr int DP = 16 * NK, REC = LQ_KV_HEAD + 2 * LQ_KV_BLOCK * DP, PITCH = DP + 4;
   alignas(16) uint8_t ring[WARPS][STAGES][REC];
   alignas(16) float sums[WARPS][ROWS][PITCH];
   float top[WARPS][ROWS], total[WARPS][ROWS];
@@ -206,9 +206,9 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
       ++taken;
       const uint8_t* rec = sm.ring[warp][st];
       const int i = (int)(f - tile_begin);
-      const uint4* ku = reinterpret_cast<const uint4*>(rec) + lane;
+      const uint4* ku = reinterpret_cast<const uint4*>(rec + LQ_KV_HEAD) + lane;
       const uint4* vu = ku + 2 * DP;
-      const uint32_t tail = *reinterpret_cast<const uint32_t*>(rec + REC - LQ_KV_TAIL);
+      const uint32_t tail = *reinterpret_cast<const uint32_t*>(rec);
       const bool empty = sm.empty[warp][st] != 0;
       const int token0 = here.seen.block(i) * LQ_KV_BLOCK;
       if (!empty) {
@@ -232,13 +232,13 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
             for (int j = 0; j < 4; ++j) mma_f16(s[j], a, lq_kv_open<0x4140>(ww[j], high, less), lq_kv_open<0x4342>(ww[j], high, less));
           }
         }
-        // tile j = 2 u + v, column 2 t + b: token 16 u + 4 t + 2 v + b
+        // tile j, column 2 t + b
         const bool all = lq_all_seen(p, first_at, last_at, token0, token0 + LQ_KV_BLOCK - 1, here.q.len);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
-            const int token = token0 + 16 * (j >> 1) + 4 * t + 2 * (j & 1) + b;
+            const int token = token0 + lq_kv_token(2 * t + b, j);
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
               float& x = s[j][2 * r + b];
@@ -278,17 +278,19 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
         }
         const uint32_t high = lq_kv_high((int8_t)(tail >> 8 & 0xFF));
         const __half2 less = lq_kv_less(high);
+        // tile 2 s, columns 2 t and 2 t + 1: tokens 0 and 2 of the lane's four; tile 2 s + 1: tokens 1 and 3
         const uint32_t a0[4] = {w[0][0], w[0][1], w[1][0], w[1][1]}, a1[4] = {w[2][0], w[2][1], w[3][0], w[3][1]};
 #pragma unroll
         for (int g = 0; g < NK; ++g) {
           const uint4 v = vu[32 * g];
-          mma_f16(o[g][0], a0, lq_kv_open<0x4140>(v.x, high, less), lq_kv_open<0x4342>(v.x, high, less));
-          mma_f16(o[g][1], a0, lq_kv_open<0x4140>(v.y, high, less), lq_kv_open<0x4342>(v.y, high, less));
-          mma_f16(o[g][0], a1, lq_kv_open<0x4140>(v.z, high, less), lq_kv_open<0x4342>(v.z, high, less));
-          mma_f16(o[g][1], a1, lq_kv_open<0x4140>(v.w, high, less), lq_kv_open<0x4342>(v.w, high, less));
+          mma_f16(o[g][0], a0, lq_kv_open<0x4240>(v.x, high, less), lq_kv_open<0x4341>(v.x, high, less));
+          mma_f16(o[g][1], a0, lq_kv_open<0x4240>(v.y, high, less), lq_kv_open<0x4341>(v.y, high, less));
+          mma_f16(o[g][0], a1, lq_kv_open<0x4240>(v.z, high, less), lq_kv_open<0x4341>(v.z, high, less));
+          mma_f16(o[g][1], a1, lq_kv_open<0x4240>(v.w, high, less), lq_kv_open<0x4341>(v.w, high, less));
         }
       }
-      __syncwarp();                                        // the stage is read
+      fence_proxy_async();                                 // the stage is read by all lanes before a copy into it is asked for
+      __syncwarp();
       issue();
     }
     // the warps' results of the tile

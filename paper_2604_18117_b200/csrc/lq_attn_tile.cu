@@ -18,27 +18,27 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int TILE = 128, KV = 128, SOFT_WARPS = 8, OPEN_WARPS = 4, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 32 * (MMA_WARP + 1);
+constexpr int TILE = 128, KV = 128, SOFT_WARPS = 8, OPEN_WARPS = 4, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 512;
+constexpr int SOFT_REGS = 176, LEAN_REGS = 80;             // of a thread: 8 * 176 + 8 * 80 = 16 * 128, as the block is launched
 constexpr int TMEM_COLS = 512;
 constexpr uint32_t COL_S = 0, COL_O = 256;                 // of the first 128 rows; the other's are 128 columns on
 constexpr float GROWTH = 8.f;
 
-// Core matrices (8 rows x 16 bytes) lie [16-byte column][row]: a column of K or Q has 128 rows, of V (whose rows are the head's entries) Dp.
-// Lanes c8 / 2, t of a store of K are 2 columns and rows 0, 1, 4, 5 of 16 bytes: with columns 32 bytes beyond a multiple of 128 apart they take all
-// banks once; of V 2 columns and every second row: 16 bytes.
-constexpr int Q_LBO = 128 * 16, K_LBO = KV * 16 + 32;
-__host__ __device__ constexpr int v_lbo(int Dp) { return Dp * 16 + 16; }
-__host__ __device__ constexpr int k_bytes(int Dp) { return (Dp / 8 * K_LBO + 127) / 128 * 128; }
-__host__ __device__ constexpr int v_bytes(int Dp) { return (KV / 8 * v_lbo(Dp) + 127) / 128 * 128; }
-__host__ __device__ constexpr int q_bytes(int Dp) { return Dp / 8 * Q_LBO; }
+// Operands are K-major rows of 128 bytes (64 halves), 128-byte swizzle; a wider K has panel after panel.  Q and K: rows are rows and tokens, 64
+// entries a panel; V: rows are the head's entries, 64 tokens a panel.
+__host__ __device__ constexpr int q_bytes(int Dp) { return (Dp + 63) / 64 * TILE * 128; }
+__host__ __device__ constexpr int k_bytes(int Dp) { return (Dp + 63) / 64 * KV * 128; }
+__host__ __device__ constexpr int v_bytes(int Dp) { return KV / 64 * Dp * 128; }
+// one record of every opening warp: head and keys, and values
+__host__ __device__ constexpr int raw_bytes(int Dp) { return LQ_KV_HEAD + 2 * LQ_KV_BLOCK * Dp; }
 
 struct Control {
-  uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t raw_k[OPEN_WARPS], raw_v[OPEN_WARPS], q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
   uint32_t tmem;
   alignas(4) uint8_t missing[4][4];                 // of the last tiles: whether record i is no page's
   int abort_flag;
   int place[2];
-  int prefix[THREADS + 1];
+  int prefix[THREADS / 32];
 };
 
 __device__ __forceinline__ void tmem_ld_32(uint32_t taddr, uint32_t (&v)[32]) {
@@ -87,14 +87,33 @@ struct Task {
   int s, head, row0, rows, tiles;        // rows: of up to 256; tiles: of 128 tokens
 };
 
+// Which of the 32 tokens from `first` on the row at place `at` sees, and whether all rows at places lo .. hi see all of the four blocks from the
+// b-th on.
+__device__ __forceinline__ uint32_t below(int n) { return (uint32_t)((1ull << max(0, min(32, n))) - 1); }
+__device__ __forceinline__ uint32_t seen_of(const LqAttnParams& p, int at, int first, int len) {
+  const int end = p.causal ? at + 1 : len;
+  uint32_t m = below(end - first);
+  if (p.window > 0) m &= ~below(at - p.window + 1 - first) | below(p.sinks - first);
+  return m;
+}
+__device__ __forceinline__ bool seen_whole(const LqAttnParams& p, const Task& k, int lo, int hi, int b) {
+  bool all = true;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int first = k.seen.block(b + i) * LQ_KV_BLOCK;
+    all = all && lq_all_seen(p, lo, hi, first, first + LQ_KV_BLOCK - 1, k.q.len);
+  }
+  return all;
+}
 template <int NK>
 __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_constant__ LqAttnParams p) {
-  constexpr int DP = 16 * NK, V_LBO = v_lbo(DP);
+  constexpr int DP = 16 * NK;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* sq = smem;                                      // [2]
   uint8_t* sk = sq + 2 * q_bytes(DP);                      // [2]
   uint8_t* sv = sk + 2 * k_bytes(DP);                      // [2]
-  Control& c = *reinterpret_cast<Control*>(sv + 2 * v_bytes(DP));
+  uint8_t* raw = sv + 2 * v_bytes(DP);                     // [OPEN_WARPS]
+  Control& c = *reinterpret_cast<Control*>(raw + OPEN_WARPS * raw_bytes(DP));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -106,6 +125,10 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
       mbar_init(smem_u32(&c.s_full[i]), 1);
       mbar_init(smem_u32(&c.p_full[i]), 4);
       mbar_init(smem_u32(&c.o_full[i]), 1);
+    }
+    for (int i = 0; i < OPEN_WARPS; ++i) {
+      mbar_init(smem_u32(&c.raw_k[i]), 1);
+      mbar_init(smem_u32(&c.raw_v[i]), 1);
     }
     c.abort_flag = 0;
     mbar_init_fence();
@@ -172,11 +195,13 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
   const int halves = k.rows > TILE ? 2 : 1;
   bool good = true;
   const auto wait = [&](uint64_t& bar, int phase, int role) {
-    if (good) good = mbar_wait_warp(smem_u32(&bar), phase & 1, &c.abort_flag, p.status, role);
+    // (without a call: the warps' registers are not those that the block was launched with)
+    if (good) good = __all_sync(0xffffffffu, mbar_wait_inline(smem_u32(&bar), phase & 1, &c.abort_flag, p.status, role));
     return good;
   };
 
   if (warp < SOFT_WARPS) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
     const int half = warp / 4, row = (warp & 3) * 32 + lane;
     if (half < halves && k.rows > 0) {
       const int r = k.row0 + half * TILE + row, all_rows = k.q.n * p.group;
@@ -189,7 +214,7 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
       {
         const uint4* from = reinterpret_cast<const uint4*>(p.q + (k.q.row + tok) * p.q_row + qh * p.q_head);
         const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
-        const uint32_t to = smem_u32(sq + half * q_bytes(DP)) + row * 16;
+        const uint32_t to = smem_u32(sq + half * q_bytes(DP)) + row * 128;
 #pragma unroll
         for (int g = 0; g < DP / 8; ++g) {
           uint4 v = make_uint4(0, 0, 0, 0);
@@ -197,50 +222,51 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
             v = from[g];
             v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
           }
-          sts_v4(to + g * Q_LBO, v);
+          sts_v4(to + g / 8 * TILE * 128 + (((g & 7) ^ (row & 7)) * 16), v);
         }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&c.q_full[half]));
       }
-      const float scale = fabsf(p.scale);
+      const float scale = fmaxf(fabsf(p.scale), 1e-30f);   // (a scale of zero: all weights are one, and what is covered stays -inf)
       const uint32_t lanes = (uint32_t)(warp & 3) << 21, ts = tmem + lanes + COL_S + half * 128, to = tmem + lanes + COL_O + half * 128;
       float m = -INFINITY, l = 0.f;                        // m: what the weights are below, times scale
       for (int j = 0; j < k.tiles; ++j) {
         if (!wait(c.s_full[half], j, LQ_STAGE_DRAIN)) break;
         tc_fence_after();
         const uint32_t missing = *reinterpret_cast<volatile uint32_t*>(c.missing[j & 3]);
-        // what of the tile's four blocks the warp's rows see: all, some, nothing
-        int first[4], kind[4];
+        // which tokens of the tile's four blocks the row sees; most tiles are seen by all rows as a whole
+        const bool whole = missing == 0 && 4 * j + 3 < k.seen.count() && seen_whole(p, k, lo, hi, 4 * j);
+        if (!whole) {                                      // (S is written anew with what no row sees at -inf)
+#pragma unroll 1
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t mask = 4 * j + i < k.seen.count() && !(missing >> (8 * i) & 1) ? seen_of(p, at, k.seen.block(4 * j + i) * LQ_KV_BLOCK, k.q.len) : 0;
+#pragma unroll 1
+            for (int x = 0; x < 32; x += 16) {
+              uint32_t u[16];
+              tmem_ld_32x16(ts + 32 * i + x, u);
+              tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int b = 4 * j + i;
-          first[i] = k.seen.block(b) * LQ_KV_BLOCK;
-          kind[i] = b >= k.seen.count() || (missing >> (8 * i) & 1) ? 2 : lq_all_seen(p, lo, hi, first[i], first[i] + LQ_KV_BLOCK - 1, k.q.len) ? 0 : 1;
-        }
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t v[32];
-          if (kind[i] == 2) continue;
-          tmem_ld_32(ts + 32 * i, v);
-          tmem_ld_wait();
-          if (kind[i] == 0) {
-            float a = -INFINITY, b = -INFINITY;
-#pragma unroll
-            for (int x = 0; x < 32; x += 4) {
-              a = fmaxf(fmaxf(a, __uint_as_float(v[x])), __uint_as_float(v[x + 1]));
-              b = fmaxf(fmaxf(b, __uint_as_float(v[x + 2])), __uint_as_float(v[x + 3]));
+              for (int y = 0; y < 16; ++y)
+                if (!(mask >> (x + y) & 1)) u[y] = 0xff800000u;
+              tmem_st_16(ts + 32 * i + x, u);
             }
-            top = fmaxf(top, fmaxf(a, b));
-          } else {
-#pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (lq_sees(p, at, first[i] + x, k.q.len)) top = fmaxf(top, __uint_as_float(v[x]));
           }
+          tmem_st_wait();
         }
-        top *= scale;                                      // (-inf times a scale of zero is no number, and counts as nothing seen)
-        if (!(top > -INFINITY)) top = -INFINITY;
+        uint32_t v[4][32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld_32(ts + 32 * i, v[i]);
+        tmem_ld_wait();
+        float tops[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          tops[i] = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < 32; x += 2) tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(v[i][x])), __uint_as_float(v[i][x + 1]));
+        }
+        float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        top *= scale;
         const bool grow = top > m + GROWTH || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, grow)) {
           // (a row that has seen nothing yet has sums of zero; its factor is one)
@@ -258,30 +284,21 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
             }
         }
         const float ref = m > -INFINITY ? -m : 0.f;
+        const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(ref, ref);
+        float2 sum[2] = {make_float2(l, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          uint32_t v[32], w[16];
-          if (kind[i] == 2) {
+          uint32_t w[16];
 #pragma unroll
-            for (int x = 0; x < 16; ++x) w[x] = 0;
-          } else {
-            tmem_ld_32(ts + 32 * i, v);
-            tmem_ld_wait();
-            float a = 0.f, b = 0.f;
-#pragma unroll
-            for (int x = 0; x < 32; x += 2) {
-              float e0 = ex2(fmaf(__uint_as_float(v[x]), scale, ref)), e1 = ex2(fmaf(__uint_as_float(v[x + 1]), scale, ref));
-              if (kind[i] == 1) {
-                e0 = lq_sees(p, at, first[i] + x, k.q.len) ? e0 : 0.f;
-                e1 = lq_sees(p, at, first[i] + x + 1, k.q.len) ? e1 : 0.f;
-              }
-              a += e0; b += e1;
-              w[x / 2] = pack(e0, e1);
-            }
-            l += a + b;
+          for (int x = 0; x < 32; x += 2) {
+            float2 e = __ffma2_rn(make_float2(__uint_as_float(v[i][x]), __uint_as_float(v[i][x + 1])), scale2, ref2);
+            e.x = ex2(e.x); e.y = ex2(e.y);
+            sum[x / 2 & 1] = __fadd2_rn(sum[x / 2 & 1], e);
+            w[x / 2] = pack(e.x, e.y);
           }
-          tmem_st_16(ts + 16 * i, w);                      // (over columns of S that have been read)
+          tmem_st_16(ts + 16 * i, w);                      // (over columns of S, which has been read)
         }
+        l = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -308,93 +325,134 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
       tc_fence_before();
     }
   } else if (warp < MMA_WARP) {
-    // Warp w opens record w of every tile.  A record's codes are asked for as soon as those of the one before have been opened.
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LEAN_REGS));
+    // Warp w opens record w of every tile.  Its keys (with the record's head) and its values are copied to the warp's own place in shared memory;
+    // the next record's are asked for as soon as these are in registers.
     const int w = warp - SOFT_WARPS, c8 = lane >> 2, t = lane & 3, count = k.tiles > 0 ? k.seen.count() : 0;
-    uint4 kr[NK], vr[NK];
-    uint32_t tail = 0, tail_next = 0;
-    long long at = -1, at_next = -1;
-    const uint8_t* rec = nullptr;
-    const auto find = [&](int j) -> long long {            // the record of tile j, -1: behind the last or no page's
+    uint8_t* place = raw + w * raw_bytes(DP);
+    const uint32_t bar_k = smem_u32(&c.raw_k[w]), bar_v = smem_u32(&c.raw_v[w]);
+    const auto find = [&](int j) -> const uint8_t* {       // the record of tile j, null: behind the last or no page's
       const int b = 4 * j + w;
-      if (j >= k.tiles || b >= count) return -1;
+      if (j >= k.tiles || b >= count) return nullptr;
       const long long x = lq_kv_at(p.b, k.s, k.seen.block(b));
       if (x < 0 && lane == 0) lq_kv_refuse(p.status);
-      return x;
+      return x < 0 ? nullptr : p.records + (x + k.head) * p.b.record;
     };
-    const auto of = [&](long long x) { return p.records + (x + k.head) * p.b.record; };
-    at = find(0);
-    if (at >= 0) {
-      rec = of(at);
+    const auto fetch_k = [&](const uint8_t* rec) {
+      if (rec && lane == 0) {
+        mbar_expect_tx(bar_k, LQ_KV_HEAD + LQ_KV_BLOCK * DP);
+        bulk_load(smem_u32(place), rec, LQ_KV_HEAD + LQ_KV_BLOCK * DP, bar_k);
+      }
+    };
+    const auto fetch_v = [&](const uint8_t* rec) {
+      if (rec && lane == 0) {
+        mbar_expect_tx(bar_v, LQ_KV_BLOCK * DP);
+        bulk_load(smem_u32(place) + LQ_KV_HEAD + LQ_KV_BLOCK * DP, rec + LQ_KV_HEAD + LQ_KV_BLOCK * DP, LQ_KV_BLOCK * DP, bar_v);
+      }
+    };
+    const uint8_t *now = find(0), *next = find(1);
+    fetch_k(now);
+    fetch_v(now);
+    int asked_k = now ? 1 : 0, asked_v = asked_k, had = 0;  // copies asked for, records that have been opened
+    // Keys: rows are tokens; the lane's word i is 8 bytes of row 32 w + lq_kv_token(c8, i).  Values: rows are entries, words 2 s + i are 8 bytes of row
+    // 16 g + 2 c8 + i.  In a half of the warp's lanes these 8 bytes take all banks once.
+    uint32_t kto[4], vto[2][2];
 #pragma unroll
-      for (int g = 0; g < NK; ++g) kr[g] = reinterpret_cast<const uint4*>(rec)[32 * g + lane];
+    for (int i = 0; i < 4; ++i) kto[i] = smem_u32(sk) + (32 * w + lq_kv_token(c8, i)) * 128 + (t & 1) * 8;
 #pragma unroll
-      for (int g = 0; g < NK; ++g) vr[g] = reinterpret_cast<const uint4*>(rec)[32 * (NK + g) + lane];
-      tail = *reinterpret_cast<const uint32_t*>(rec + 64 * DP);
-    }
-    const int token = 32 * w + 4 * (c8 >> 1) + (c8 & 1);
-    const uint32_t kto = smem_u32(sk) + (t >> 1) * K_LBO + token * 16 + (t & 1) * 8;
-    const uint32_t vto = smem_u32(sv) + (4 * w + (t >> 1)) * V_LBO + 2 * c8 * 16 + (t & 1) * 8;
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int chunk = (4 * w + 2 * s + (t >> 1)) & 7, r = 2 * c8 + i;
+        vto[s][i] = smem_u32(sv) + w / 2 * DP * 128 + r * 128 + ((chunk ^ (r & 7)) * 16) + (t & 1) * 8;
+      }
+    const int kx = 2 * (c8 & 1) + 4 * (c8 >> 1 & 1);       // (token & 7 but for its lowest bit, i & 1)
     for (int j = 0; j < k.tiles; ++j) {
       const int st = j & 1;
-      at_next = find(j + 1);
-      const uint8_t* next = at_next >= 0 ? of(at_next) : nullptr;
+      const uint8_t* after = find(j + 2);
+      uint32_t head = 0;
+      uint4 u[NK];
+      if (now && good) {
+        if (!wait(c.raw_k[w], had, LQ_STAGE_PRODUCER)) break;
+        head = *reinterpret_cast<const volatile uint32_t*>(place);
+#pragma unroll
+        for (int g = 0; g < NK; ++g) u[g] = lds_v4(smem_u32(place) + LQ_KV_HEAD + 512 * g + 16 * lane);
+      }
+      fence_proxy_async();                                 // (a copy into the place of the keys comes behind the loads of all lanes; without this it
+      __syncwarp();                                        // has overtaken some)
+      fetch_k(next);
+      asked_k += next ? 1 : 0;
       if (j >= 2 && !wait(c.k_empty[st], (j >> 1) - 1, LQ_STAGE_PRODUCER)) break;
       {
-        const uint32_t high = lq_kv_high((int8_t)(tail & 0xFF)), to = kto + st * k_bytes(DP);
+        const uint32_t high = lq_kv_high((int8_t)(head & 0xFF));
         const __half2 less = lq_kv_less(high);
-        if (lane == 0) c.missing[j & 3][w] = at < 0;
+        if (lane == 0) c.missing[j & 3][w] = !now;
 #pragma unroll
         for (int g = 0; g < NK; ++g) {
-          const uint32_t u[4] = {kr[g].x, kr[g].y, kr[g].z, kr[g].w};
+          const uint32_t ww[4] = {u[g].x, u[g].y, u[g].z, u[g].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t a = to + 2 * g * K_LBO + (16 * (i >> 1) + 2 * (i & 1)) * 16;
-            if (at >= 0) sts_v2(a, lq_kv_open<0x4140>(u[i], high, less), lq_kv_open<0x4342>(u[i], high, less));
+            const uint32_t a = kto[i] + st * k_bytes(DP) + g / 4 * KV * 128 + ((((2 * g & 7) + (t >> 1)) ^ (kx + (i & 1))) * 16);
+            if (now) sts_v2(a, lq_kv_open<0x4140>(ww[i], high, less), lq_kv_open<0x4342>(ww[i], high, less));
             else sts_v2(a, 0, 0);
           }
-          if (next) kr[g] = reinterpret_cast<const uint4*>(next)[32 * g + lane];
         }
-        if (next) tail_next = *reinterpret_cast<const uint32_t*>(next + 64 * DP);
       }
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&c.k_full[st]));
+      if (now) {
+        if (!wait(c.raw_v[w], had, LQ_STAGE_PRODUCER)) break;
+#pragma unroll
+        for (int g = 0; g < NK; ++g) u[g] = lds_v4(smem_u32(place) + LQ_KV_HEAD + LQ_KV_BLOCK * DP + 512 * g + 16 * lane);
+        ++had;
+      }
+      fence_proxy_async();
+      __syncwarp();
+      fetch_v(next);
+      asked_v += next ? 1 : 0;
       if (j >= 2 && !wait(c.v_empty[st], (j >> 1) - 1, LQ_STAGE_PRODUCER)) break;
       {
-        const uint32_t high = lq_kv_high((int8_t)(tail >> 8 & 0xFF)), to = vto + st * v_bytes(DP);
+        const uint32_t high = lq_kv_high((int8_t)(head >> 8 & 0xFF));
         const __half2 less = lq_kv_less(high);
 #pragma unroll
         for (int g = 0; g < NK; ++g) {
-          const uint32_t u[4] = {vr[g].x, vr[g].y, vr[g].z, vr[g].w};
+          const uint32_t ww[4] = {u[g].x, u[g].y, u[g].z, u[g].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t a = to + (i >> 1) * 2 * V_LBO + (16 * g + (i & 1)) * 16;
-            if (at >= 0) sts_v2(a, lq_kv_open<0x4140>(u[i], high, less), lq_kv_open<0x4342>(u[i], high, less));
+            const uint32_t a = vto[i >> 1][i & 1] + st * v_bytes(DP) + g * 2048;
+            if (now) sts_v2(a, lq_kv_open<0x4140>(ww[i], high, less), lq_kv_open<0x4342>(ww[i], high, less));
             else sts_v2(a, 0, 0);
           }
-          if (next) vr[g] = reinterpret_cast<const uint4*>(next)[32 * (NK + g) + lane];
         }
       }
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&c.v_full[st]));
-      at = at_next;
-      tail = tail_next;
+      now = next;
+      next = after;
     }
-  } else if (k.tiles > 0) {
+    if (!good) {                                           // a wait gave up: what is in flight lands before the block leaves
+      if (asked_k > had) mbar_settle(bar_k, (asked_k - 1) & 1);
+      if (asked_v > had) mbar_settle(bar_v, (asked_v - 1) & 1);
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LEAN_REGS));
+  }
+  if (warp == MMA_WARP && k.tiles > 0) {
     const uint32_t idesc_s = IDESC_F16 | idesc_shape(KV), idesc_o = IDESC_F16 | idesc_shape(DP);
     const auto product_s = [&](int half, int st) {         // by one thread
       const uint32_t a = smem_u32(sq + half * q_bytes(DP)), b = smem_u32(sk + st * k_bytes(DP));
 #pragma unroll
       for (int x = 0; x < NK; ++x)
-        tc_mma<TC_F16>(tmem + COL_S + half * 128, make_smem_desc_plain(a + 2 * x * Q_LBO, Q_LBO, 128), make_smem_desc_plain(b + 2 * x * K_LBO, K_LBO, 128), idesc_s,
+        tc_mma<TC_F16>(tmem + COL_S + half * 128, make_smem_desc(a + x / 4 * TILE * 128 + x % 4 * 32), make_smem_desc(b + x / 4 * KV * 128 + x % 4 * 32), idesc_s,
                        x > 0);
     };
     const auto product_o = [&](int half, int st, bool add) {
       const uint32_t b = smem_u32(sv + st * v_bytes(DP));
 #pragma unroll
       for (int x = 0; x < KV / 16; ++x)
-        tc_mma_ta(tmem + COL_O + half * 128, tmem + COL_S + half * 128 + 8 * x, make_smem_desc_plain(b + 2 * x * V_LBO, V_LBO, 128), idesc_o, add || x > 0);
+        tc_mma_ta(tmem + COL_O + half * 128, tmem + COL_S + half * 128 + 8 * x, make_smem_desc(b + x / 4 * DP * 128 + x % 4 * 32), idesc_o, add || x > 0);
     };
     wait(c.k_full[0], 0, LQ_STAGE_MMA);
     for (int half = 0; half < halves; ++half) {
@@ -442,7 +500,7 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
   }
 }
 
-size_t tile_smem(int Dp) { return 2 * (size_t)(q_bytes(Dp) + k_bytes(Dp) + v_bytes(Dp)) + sizeof(Control); }
+size_t tile_smem(int Dp) { return 2 * (size_t)(q_bytes(Dp) + k_bytes(Dp) + v_bytes(Dp)) + OPEN_WARPS * raw_bytes(Dp) + sizeof(Control); }
 
 template <typename F>
 auto with_size(int Dp, const F& f) {

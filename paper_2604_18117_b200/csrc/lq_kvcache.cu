@@ -89,16 +89,16 @@ __device__ void write_block(uint8_t* record, const T* in, long long row, int t0,
   }
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-  int8_t* exps = reinterpret_cast<int8_t*>(record + 2 * lq_kv_side_bytes(Dp)) + (KEYS ? 0 : 1);
+  int8_t* exps = reinterpret_cast<int8_t*>(record) + (KEYS ? 0 : 1);
   const int need = exponent_of(top), was = t0 > 0 ? max(LQ_KV_E_MIN, min(LQ_KV_E_MAX, (int)*exps)) : LQ_KV_E_MIN, e = max(need, was);
   const bool grows = t0 > 0 && e > was;
   const float inv = pow2(-e), less = pow2(was - e);
   __syncwarp();
   if (lane == 0) *exps = (int8_t)e;
-  uint8_t* side = record + (KEYS ? 0 : lq_kv_side_bytes(Dp));
+  uint8_t* side = record + LQ_KV_HEAD + (KEYS ? 0 : lq_kv_side_bytes(Dp));
   const int c8 = lane >> 2, t = lane & 3;
   // Bit i: the lane's unit has token i of the block.  Units without a token to write are left alone.
-  const uint32_t mine = KEYS ? 0x00050005u << (4 * (c8 / 2) + c8 % 2) : 0x000F000Fu << (4 * t);
+  const uint32_t mine = KEYS ? 0x00030003u << (2 * c8) : 0x000F000Fu << (4 * t);
   const uint32_t below1 = t1 == 32 ? 0xffffffffu : (1u << t1) - 1, fresh = below1 & ~((1u << t0) - 1);
   if (!(mine & (grows ? below1 : fresh))) return;
   const bool keeps = t0 > 0 && (mine & ((1u << t0) - 1)) != 0;
@@ -117,7 +117,7 @@ __device__ void write_block(uint8_t* record, const T* in, long long row, int t0,
       const int d = 16 * g + 4 * t;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int token = 16 * (i >> 1) + 4 * (c8 >> 1) + 2 * (i & 1) + (c8 & 1);
+        const int token = lq_kv_token(c8, i);
         if (token < t0 || token >= t1) continue;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
         if (d < D) x = load4(in + (token - t0) * row + d);
@@ -232,9 +232,9 @@ __global__ void __launch_bounds__(32 * WARPS) lq_kv_read_kernel(const __grid_con
     return;
   }
   const uint8_t* record = p.records + (at + head) * p.b.record;
-  const int e = reinterpret_cast<const int8_t*>(record + 2 * lq_kv_side_bytes(p.Dp))[side];
+  const int e = reinterpret_cast<const int8_t*>(record)[side];
   const float step = pow2(e);
-  const uint4* units = reinterpret_cast<const uint4*>(record + (side ? lq_kv_side_bytes(p.Dp) : 0)) + lane;
+  const uint4* units = reinterpret_cast<const uint4*>(record + LQ_KV_HEAD + (side ? lq_kv_side_bytes(p.Dp) : 0)) + lane;
   const int c8 = lane >> 2, t = lane & 3, first = (int)(block * LQ_KV_BLOCK);
   T* out = reinterpret_cast<T*>(side ? p.v : p.k) + s * p.seq[side] + head * p.head[side] + ((long long)first - begin) * p.row[side];
   for (int g = 0; 16 * g < p.D; ++g) {
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(32 * WARPS) lq_kv_read_kernel(const __grid_con
       const int d = 16 * g + 4 * t;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int token = 16 * (j >> 1) + 4 * (c8 >> 1) + 2 * (j & 1) + (c8 & 1);
+        const int token = lq_kv_token(c8, j);
         if (d < p.D && first + token >= begin && first + token < end)
           store4(out + token * p.row[side] + d, make_float4(value_of(w[j], 0, step), value_of(w[j], 1, step), value_of(w[j], 2, step), value_of(w[j], 3, step)));
       }
@@ -313,7 +313,7 @@ extern "C" lq_status lq_kvcache_create(int32_t layers, int32_t pages, int32_t pa
   }
   // All zeros (code 0, exponent 0): what no token has been written to is multiplied with zero weights, and has to be a number.
   if (lq_note_cuda(cudaMemset(C->d_records, 0x80, n * rec)) != cudaSuccess ||
-      lq_note_cuda(cudaMemset2D(C->d_records + rec - LQ_KV_TAIL, rec, 0, LQ_KV_TAIL, n)) != cudaSuccess ||
+      lq_note_cuda(cudaMemset2D(C->d_records, rec, 0, LQ_KV_HEAD, n)) != cudaSuccess ||
       lq_note_cuda(cudaMemset(C->d_count, 0, C->sms * sizeof(int))) != cudaSuccess || lq_note_cuda(cudaDeviceSynchronize()) != cudaSuccess ||
       !lq_device_status_ptr(device)) {                       // (allocated here, not under a capture)
     lq_kvcache_free(C);

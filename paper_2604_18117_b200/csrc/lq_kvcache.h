@@ -6,16 +6,17 @@
 
 #include "lq_internal.h"
 
-// A record holds 32 tokens of one head: their keys, their values, and a tail of 32 bytes that begins with the exponents of both.  Codes are
-// kept as bytes u = c + 128, in the order in which a warp of the attention kernels reads them as operands of m16n8k16 products, 16 bytes a
-// lane (c8 = lane / 4, t = lane % 4) for every 16 entries of the head:
-//   keys    word i = 2 s + h: token 16 s + 4 (c8 / 2) + 2 h + c8 % 2, bytes: entries 4 t .. 4 t + 3 of the 16 (column c8 of the products' tile i)
+// A record holds 32 tokens of one head: 32 bytes that begin with the exponents of keys and values, the keys, the values.  Codes are kept as
+// bytes u = c + 128, in the order in which a warp of the attention kernels reads them as operands of m16n8k16 products, 16 bytes a lane
+// (c8 = lane / 4, t = lane % 4) for every 16 entries of the head:
+//   keys    word i = 2 s + h: token lq_kv_token(c8, i), bytes: entries 4 t .. 4 t + 3 of the 16 (column c8 of the products' tile i)
 //   values  word 2 s + i: entry 2 c8 + i of the 16, bytes: tokens 16 s + 4 t .. 4 t + 3
-// so that every load is one of 16 bytes a lane, neighbours across lanes, and no byte has to change lanes.
-// Records follow each other by layer, page, block of the page and head.
-constexpr int LQ_KV_TAIL = 32, LQ_KV_E_MIN = -20, LQ_KV_E_MAX = 9;
+// so that every load is one of 16 bytes a lane, neighbours across lanes, no byte has to change lanes, and stores of opened codes to swizzled
+// rows of 128 bytes meet in no bank.  Records follow each other by layer, page, block of the page and head.
+constexpr int LQ_KV_HEAD = 32, LQ_KV_E_MIN = -20, LQ_KV_E_MAX = 9;
 static inline __host__ __device__ int lq_kv_side_bytes(int Dp) { return LQ_KV_BLOCK * Dp; }
-static inline __host__ __device__ int lq_kv_record_bytes(int Dp) { return 2 * lq_kv_side_bytes(Dp) + LQ_KV_TAIL; }
+static inline __host__ __device__ int lq_kv_record_bytes(int Dp) { return LQ_KV_HEAD + 2 * lq_kv_side_bytes(Dp); }
+static inline __host__ __device__ int lq_kv_token(int c8, int i) { return 16 * (i >> 1) + 4 * (c8 >> 1) + 2 * (c8 & 1) + (i & 1); }
 
 // heads are stored padded to the next of these
 constexpr int LQ_KV_DIMS[] = {64, 80, 96, 112, 128, 192, 256};
@@ -81,7 +82,7 @@ __device__ __forceinline__ long long lq_kv_at(const LqBatch& b, int s, int block
   if (page < 0 || page >= b.page_count) return -1;
   return ((long long)page * b.page_blocks + (block - slot * b.page_blocks)) * b.heads;
 }
-// Two codes of a word (SEL: 0x4140 the lower two, 0x4342 the upper two) as halves, each times 2^(e - 4): a byte u under the upper byte `high` of a
+// Two codes of a word (SEL: 0x4140 the lower two, 0x4342 the upper two, 0x4240 and 0x4341 every second one) as halves, each times 2^(e - 4): a byte u under the upper byte `high` of a
 // half is (1024 + u) 2^(e - 4), and what `less` takes off leaves u - 128 = c of that, all of it exact for e in [-20, 9].
 __device__ __forceinline__ uint32_t lq_kv_high(int e) { return 0x01010101u * (uint32_t)(0x64 + 4 * (e - 4)); }
 __device__ __forceinline__ __half2 lq_kv_less(uint32_t high) {          // 1152 2^(e - 4) = 1024 2^(e - 4) + 128 2^(e - 4)

@@ -310,6 +310,22 @@ def test_many_sequences(sequences):
     c.close()
 
 
+@pytest.mark.parametrize("D,hq,hk", [(128, 4, 1), (80, 2, 2), (64, 8, 1)])
+def test_equal_calls_give_equal_bits(D, hq, hk):
+    """Prompts, again and again: operands are whole when they are read, whatever the order in which copies and warps come."""
+    import torch
+    c = filled(D, hk, [513, 300, 100], 64)
+    ns = [200, 300, 1]
+    q = torch.randn(sum(ns), hq, D, dtype=torch.float16, device="cuda")
+    out = torch.empty(2, sum(ns), hq, D, dtype=torch.float16, device="cuda")
+    b = c.batch(ns, c.len)
+    for i in range(300):
+        a = B.lq_attn(q.data_ptr(), q.stride()[:2], out[min(i, 1)].data_ptr(), out.stride()[1:3], hq, 0.1)
+        B.lq_cache_attention(c.h, 0, b, a, torch.cuda.current_stream().cuda_stream)
+        assert i == 0 or torch.equal(out[0], out[1]), i
+    c.close()
+
+
 def test_heavy_rows_and_large_products():
     """One token takes all the weight (a difference of exponents beyond fp32's range); values of very different size."""
     c = Cache(64, 1, [200], 32)
