@@ -8,10 +8,11 @@
 // takes many blocks and ragged batches leave none idle.  A tile whose records are two blocks' or more leaves partial results (unscaled sums,
 // maximum, sum), which the last of them to arrive joins in the order of the blocks: no result depends on who was last.
 //
-// Within a block each warp takes every WARPS-th record, through a ring of its own in shared memory that bulk copies fill.  A record is opened to halves in
-// registers (a byte permutation and a packed subtraction for two codes) in the order of m16n8k16 operands; rows' weights go from the
-// accumulators of the first product to the operand of the second without a change of lanes.  Weights are rounded to halves there (2^-11 of
-// each); sums, maxima and accumulators are fp32.
+// Within a block each warp takes every WARPS-th record, through a ring of its own in shared memory that bulk copies fill.  A record is opened
+// to halves in registers (a byte permutation and a packed subtraction for two codes), which are the first operands of m16n8k16 products: S^T =
+// K Q^T with 8 or 16 rows of Q as columns, so that no more products are made than rows ask for, and O^T = V^T W^T.  The rows' weights are
+// rounded to halves between the two (2^-11 of each) and turned round 8 x 8 at a time; sums, maxima and accumulators are fp32.  Accumulators
+// are only scaled when a row's maximum has grown by 8 or more (in powers of two): until then weights are up to 2^8.
 #include <math.h>
 
 #include "lq_attn.h"
@@ -22,60 +23,83 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int ROWS = LQ_ATTN_ROWS;
+constexpr float GROWTH = 8.f;
 
-__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint2& b) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
+}
+__device__ __forceinline__ uint32_t turned(uint32_t v) {  // 8 x 8 halves, rows for columns
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
 }
 __device__ __forceinline__ uint32_t pack(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
-// Where a record lies in the launch's row of records: walks forward through the sequences that the launch takes.
+// A place in the launch's row of records: sequence by sequence, head by head, tile of rows by tile of rows.  Walks forward.
 struct Place {
   LqSeq q;
   LqSeen seen;
   int s, tiles, each;                    // tiles: of rows of the sequence; each: records of a tile
-  long long begin, end;                  // of the sequence's records
+  int head, tile, i;                     // i: record of the tile
 };
+template <int ROWS>
 __device__ __forceinline__ void measure(const LqAttnParams& p, int s, Place& at, bool tell) {
   at.s = s;
   at.q = lq_seq(p.b, s);
-  at.tiles = at.each = 0;
+  at.tiles = at.each = at.head = at.tile = at.i = 0;
   if (!lq_attn_takes(p, at.q, tell)) return;
   at.seen = lq_seen(p, at.q.len - at.q.n, at.q.len - 1, at.q.len);
   at.each = max(1, at.seen.count());
   at.tiles = (int)(((long long)at.q.n * p.group + ROWS - 1) / ROWS);
 }
 __device__ __forceinline__ long long records_of(const LqAttnParams& p, const Place& at) { return (long long)at.tiles * at.each * p.b.heads; }
-__device__ __forceinline__ void seek(const LqAttnParams& p, Place& at, long long f) {
-  while (f >= at.end && at.s + 1 < p.b.sequences) {
-    measure(p, at.s + 1, at, false);
-    at.begin = at.end;
-    at.end += records_of(p, at);
+// n records on; false: behind the last
+template <int ROWS>
+__device__ __forceinline__ bool walk(const LqAttnParams& p, Place& at, int n) {
+  at.i += n;
+  while (at.i >= at.each) {
+    const int left = at.i - at.each;
+    at.i = left;
+    if (++at.tile < at.tiles) continue;
+    at.tile = 0;
+    if (++at.head < p.b.heads && at.tiles > 0) continue;
+    do {
+      if (at.s + 1 >= p.b.sequences) { at.i = 0; return false; }
+      measure<ROWS>(p, at.s + 1, at, false);
+    } while (at.tiles == 0);
+    at.i = left;
   }
+  return true;
 }
 
-template <int NK, int WARPS, int STAGES>
+template <int NK, int NT, int WARPS, int STAGES>
 struct Shared {
-  static constexpr int DP = 16 * NK, REC = LQ_KV_HEAD + 2 * LQ_KV_BLOCK * DP, PITCH = DP + 4;
+  static constexpr int DP = 16 * NK, REC = LQ_KV_HEAD + 2 * LQ_KV_BLOCK * DP, PITCH = DP + 4, ROWS = 8 * NT;
+  static constexpr bool Q_HERE = NK * NT > 16;             // Q in shared memory: its registers would not be there
   alignas(16) uint8_t ring[WARPS][STAGES][REC];
   alignas(16) float sums[WARPS][ROWS][PITCH];
   float top[WARPS][ROWS], total[WARPS][ROWS];
-  alignas(16) uint32_t q[NK > 8 ? NK : 1][32][4];
+  alignas(16) uint2 q[Q_HERE ? NK : 1][NT][32];
   long long prefix[32 * WARPS + 1];
   alignas(8) uint64_t bars[WARPS][STAGES];
   uint8_t empty[WARPS][STAGES];
   int abort_flag, last;
 };
 
-template <int NK, int WARPS, int STAGES>
+template <int NK, int NT, int WARPS, int STAGES>
 __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_constant__ LqAttnParams p) {
-  using Smem = Shared<NK, WARPS, STAGES>;
-  constexpr int DP = 16 * NK, REC = Smem::REC, THREADS = 32 * WARPS;
+  using Smem = Shared<NK, NT, WARPS, STAGES>;
+  constexpr int DP = 16 * NK, REC = Smem::REC, THREADS = 32 * WARPS, ROWS = 8 * NT;
   extern __shared__ __align__(128) uint8_t raw[];
   Smem& sm = *reinterpret_cast<Smem*>(raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c8 = lane >> 2, t = lane & 3;
@@ -87,12 +111,12 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
   grid_dependency_wait();
 
   // the launch's records, and this block's share
+  const int chunk = (p.b.sequences + THREADS - 1) / THREADS;
   {
-    const int chunk = (p.b.sequences + THREADS - 1) / THREADS;
     long long sum = 0;
     for (int s = tid * chunk; s < min(p.b.sequences, (tid + 1) * chunk); ++s) {
       Place at;
-      measure(p, s, at, blockIdx.x == 0);
+      measure<ROWS>(p, s, at, blockIdx.x == 0);
       sum += records_of(p, at);
     }
     long long up = sum;
@@ -122,171 +146,188 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
       const int m = (a + b) / 2;
       if (sm.prefix[m] <= lo) a = m; else b = m;
     }
-    const int chunk = (p.b.sequences + THREADS - 1) / THREADS;
-    measure(p, a * chunk, here, false);
-    here.begin = sm.prefix[a];
-    here.end = here.begin + records_of(p, here);
-    seek(p, here, lo);
+    long long begin = sm.prefix[a];
+    measure<ROWS>(p, a * chunk, here, false);
+    while (lo - begin >= records_of(p, here)) {
+      begin += records_of(p, here);
+      measure<ROWS>(p, here.s + 1, here, false);
+    }
+    const long long tile = (lo - begin) / here.each;
+    here.i = (int)(lo - begin - tile * here.each);
+    here.head = (int)(tile / here.tiles);
+    here.tile = (int)(tile - (long long)here.head * here.tiles);
   }
 
-  // The warp's ring: record lo + warp, lo + warp + WARPS, ...
+  // The warp's ring: records lo + warp, lo + warp + WARPS, ...  The page of the one that is next is known when it is asked for.
   Place ahead = here;
-  long long f_ahead = lo + warp;
-  int issued = 0;
-  const auto issue = [&]() {                               // (a record that is no page's, or of no token, is not fetched; its stage then stays empty)
-    if (f_ahead < hi) {
-      seek(p, ahead, f_ahead);
-      const int i = (int)((f_ahead - ahead.begin) % ahead.each), h = (int)((f_ahead - ahead.begin) / ahead.each / ahead.tiles);
-      long long at = -1;
-      if (i < ahead.seen.count()) {
-        at = lq_kv_at(p.b, ahead.s, ahead.seen.block(i));
-        if (at < 0 && lane == 0) lq_kv_refuse(p.status);
-      }
-      if (lane == 0) {
-        const int st = issued % STAGES;
-        const uint32_t bar = smem_u32(&sm.bars[warp][st]);
-        sm.empty[warp][st] = at < 0;
-        if (at >= 0) {
-          mbar_expect_tx(bar, REC);
-          bulk_load(smem_u32(sm.ring[warp][st]), p.records + (at + h) * p.b.record, REC, bar);
-        } else {
-          mbar_arrive(bar);
-        }
-      }
-      ++issued;
+  int left = (int)((hi - lo - warp + WARPS - 1) / WARPS), slot = 0, page = -1, issued = 0;
+  const auto look = [&]() {
+    page = -1;
+    if (left > 0 && ahead.i < ahead.seen.count()) {
+      slot = lq_kv_slot(p.b, ahead.seen.block(ahead.i));
+      page = p.b.pages[(long long)ahead.s * p.b.page_stride + slot];
     }
-    f_ahead += WARPS;
   };
+  const auto issue = [&]() {                               // (a record that is no page's, or of no token, is not fetched; its stage then stays empty)
+    if (left <= 0) return;
+    if (lane == 0) {
+      long long at = -1;
+      if (ahead.i < ahead.seen.count()) {
+        at = lq_kv_at(p.b, ahead.seen.block(ahead.i), slot, page);
+        if (at < 0) lq_kv_refuse(p.status);
+      }
+      const int st = issued % STAGES;
+      const uint32_t bar = smem_u32(&sm.bars[warp][st]);
+      sm.empty[warp][st] = at < 0;
+      if (at >= 0) {
+        mbar_expect_tx(bar, REC);
+        bulk_load(smem_u32(sm.ring[warp][st]), p.records + (at + ahead.head) * p.b.record, REC, bar);
+      } else {
+        mbar_arrive(bar);
+      }
+    }
+    ++issued;
+    if (--left > 0) {
+      walk<ROWS>(p, ahead, WARPS);
+      look();
+    }
+  };
+  if (left > 0) {
+    if (warp > 0) walk<ROWS>(p, ahead, warp);
+    look();
+  }
   for (int i = 0; i < STAGES; ++i) issue();
 
+  const float scale = fmaxf(fabsf(p.scale), 1e-30f);       // (a scale of zero: all weights are one, and what is not seen stays -inf)
+  const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;  // of the signs of Q
   int taken = 0;
   bool good = true;
-  long long f = lo + warp;
   for (long long seg = lo; seg < hi;) {
-    // a tile of rows, or the part of it that is this block's
-    seek(p, here, seg);
-    const long long off = seg - here.begin;
-    const int tile_no = (int)(off / here.each), h = tile_no / here.tiles, tile = tile_no - h * here.tiles;
-    const long long tile_begin = here.begin + (long long)tile_no * here.each, tile_end = tile_begin + here.each;
-    const long long seg_end = min(hi, tile_end);
-    const int rows = min(ROWS, here.q.n * p.group - tile * ROWS), base = here.q.len - here.q.n;
-    // the lane's two rows: c8 and c8 + 8
-    int pos[2];
-    uint32_t qa[NK > 8 ? 1 : NK][4];
-    {
-      const __half* from[2];
+    // a tile of rows, or the part of it that is this block's: records first .. last - 1 of the tile
+    const int first = here.i, last = (int)min((long long)here.each, first + (hi - seg));
+    const int rows = min(ROWS, here.q.n * p.group - here.tile * ROWS), base = here.q.len - here.q.n;
+    int pos[NT][2];                                        // of the columns of S^T that the lane holds
+    uint2 qb[Smem::Q_HERE ? 1 : NK][NT];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = min(tile * ROWS + c8 + 8 * i, here.q.n * p.group - 1), tok = r / p.group;
-        pos[i] = base + tok;
-        from[i] = p.q + (here.q.row + tok) * p.q_row + (long long)(h * p.group + r - tok * p.group) * p.q_head;
-      }
-      if (NK <= 8 || warp == 0)
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) pos[n][b] = base + min(here.tile * ROWS + 8 * n + 2 * t + b, here.q.n * p.group - 1) / p.group;
+      const int r = here.tile * ROWS + 8 * n + c8, tok = r / p.group;
+      const bool real = 8 * n + c8 < rows;
+      const __half* from = p.q + (here.q.row + tok) * p.q_row + (long long)(here.head * p.group + r - tok * p.group) * p.q_head;
+      if (!Smem::Q_HERE || warp == 0)
 #pragma unroll
         for (int g = 0; g < NK; ++g) {
-          uint2 v[2] = {};
-          if (16 * g + 4 * t < p.D)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const uint2*>(from[i] + 16 * g + 4 * t);
-          if constexpr (NK <= 8) {
-            qa[g][0] = v[0].x; qa[g][1] = v[1].x; qa[g][2] = v[0].y; qa[g][3] = v[1].y;
-          } else {
-            *reinterpret_cast<uint4*>(sm.q[g][lane]) = make_uint4(v[0].x, v[1].x, v[0].y, v[1].y);
+          uint2 v = make_uint2(0, 0);
+          if (real && 16 * g + 4 * t < p.D) {
+            v = *reinterpret_cast<const uint2*>(from + 16 * g + 4 * t);
+            v.x ^= flip; v.y ^= flip;
           }
+          if constexpr (Smem::Q_HERE) sm.q[g][n][lane] = v;
+          else qb[g][n] = v;
         }
-      if constexpr (NK > 8) __syncthreads();
     }
-    const int first_at = base + tile * ROWS / p.group, last_at = base + (tile * ROWS + rows - 1) / p.group;
-    float o[NK][2][4] = {};
-    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-    for (; f < seg_end; f += WARPS) {
+    if constexpr (Smem::Q_HERE) __syncthreads();
+    const int first_at = base + here.tile * ROWS / p.group, last_at = base + (here.tile * ROWS + rows - 1) / p.group;
+    float o[NK][NT][4] = {};
+    float top[NT][2], sum[NT][2] = {};                     // top: what the weights are below, times scale; sum: of the lane's tokens
+#pragma unroll
+    for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
+    // the warp's records are every WARPS-th of the block's
+    int i = first + (int)((warp + WARPS - (seg - lo) % WARPS) % WARPS);
+    for (; i < last; i += WARPS) {
       const int st = taken % STAGES;
       if (good) good = mbar_wait_warp(smem_u32(&sm.bars[warp][st]), (taken / STAGES) & 1, &sm.abort_flag, p.status, LQ_STAGE_DRAIN);
       if (!good) break;
       ++taken;
       const uint8_t* rec = sm.ring[warp][st];
-      const int i = (int)(f - tile_begin);
       const uint4* ku = reinterpret_cast<const uint4*>(rec + LQ_KV_HEAD) + lane;
       const uint4* vu = ku + 2 * DP;
-      const uint32_t tail = *reinterpret_cast<const uint32_t*>(rec);
-      const bool empty = sm.empty[warp][st] != 0;
-      const int token0 = here.seen.block(i) * LQ_KV_BLOCK;
-      if (!empty) {
-        float s[4][4] = {};
+      if (!sm.empty[warp][st]) {
+        const uint32_t head = *reinterpret_cast<const uint32_t*>(rec);
+        const int token0 = here.seen.block(i) * LQ_KV_BLOCK;
+        float s[2][NT][4] = {};                            // [words 2 a, 2 a + 1][..][token of word 2 a: rows 2 t, 2 t + 1; of 2 a + 1]
         {
-          const uint32_t high = lq_kv_high((int8_t)(tail & 0xFF));
+          const uint32_t high = lq_kv_high((int8_t)(head & 0xFF));
           const __half2 less = lq_kv_less(high);
 #pragma unroll
           for (int g = 0; g < NK; ++g) {
             const uint4 w = ku[32 * g];
             const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-            uint32_t a[4];
-            if constexpr (NK <= 8) {
 #pragma unroll
-              for (int j = 0; j < 4; ++j) a[j] = qa[g][j];
-            } else {
-              const uint4 v = *reinterpret_cast<const uint4*>(sm.q[g][lane]);
-              a[0] = v.x; a[1] = v.y; a[2] = v.z; a[3] = v.w;
+            for (int a = 0; a < 2; ++a) {
+              const uint32_t a0 = lq_kv_open<0x4140>(ww[2 * a], high, less), a2 = lq_kv_open<0x4342>(ww[2 * a], high, less);
+              const uint32_t a1 = lq_kv_open<0x4140>(ww[2 * a + 1], high, less), a3 = lq_kv_open<0x4342>(ww[2 * a + 1], high, less);
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                if constexpr (Smem::Q_HERE) mma_f16(s[a][n], a0, a1, a2, a3, sm.q[g][n][lane]);
+                else mma_f16(s[a][n], a0, a1, a2, a3, qb[g][n]);
+              }
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) mma_f16(s[j], a, lq_kv_open<0x4140>(ww[j], high, less), lq_kv_open<0x4342>(ww[j], high, less));
           }
         }
-        // tile j, column 2 t + b
-        const bool all = lq_all_seen(p, first_at, last_at, token0, token0 + LQ_KV_BLOCK - 1, here.q.len);
+        if (!lq_all_seen(p, first_at, last_at, token0, token0 + LQ_KV_BLOCK - 1, here.q.len)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+          for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                if (!lq_sees(p, pos[n][x & 1], token0 + lq_kv_token(c8, 2 * a + (x >> 1)), here.q.len)) s[a][n][x] = -INFINITY;
+        }
+        float high_s[NT][2];
+        bool grow = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
-            const int token = token0 + lq_kv_token(2 * t + b, j);
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-              float& x = s[j][2 * r + b];
-              x *= p.scale;
-              if (!all && !lq_sees(p, pos[r], token, here.q.len)) x = -INFINITY;
-            }
+            high_s[n][b] = scale * fmaxf(fmaxf(s[0][n][b], s[0][n][2 + b]), fmaxf(s[1][n][b], s[1][n][2 + b]));
+            grow = grow || high_s[n][b] > top[n][b] + GROWTH;
           }
-        uint32_t w[4][2];                                  // weights of tile j, rows c8 and c8 + 8
-        float keep[2];
+        if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          float m = top[r];
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) m = fmaxf(m, fmaxf(s[j][2 * r], s[j][2 * r + 1]));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-          const float ref = m == -INFINITY ? 0.f : m;      // (a row that has seen nothing yet)
-          keep[r] = exp2f(top[r] - ref);
-          top[r] = m;
-          float add = 0.f;
+            for (int b = 0; b < 2; ++b) {
+              float m = high_s[n][b];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float x = exp2f(s[j][2 * r] - ref), y = exp2f(s[j][2 * r + 1] - ref);
-            add += x + y;
-            w[j][r] = pack(x, y);
-          }
-          sum[r] = fmaf(sum[r], keep[r], add);
-        }
-        if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {
+              for (int d = 4; d < 32; d *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+              m = fmaxf(m, top[n][b]);
+              // (a row that has seen nothing yet has sums of zero)
+              const float by = top[n][b] == -INFINITY ? 1.f : ex2(top[n][b] - m);
+              top[n][b] = m;
+              sum[n][b] *= by;
 #pragma unroll
-          for (int g = 0; g < NK; ++g)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              o[g][j][0] *= keep[0]; o[g][j][1] *= keep[0];
-              o[g][j][2] *= keep[1]; o[g][j][3] *= keep[1];
+              for (int g = 0; g < NK; ++g) { o[g][n][b] *= by; o[g][n][2 + b] *= by; }
             }
         }
-        const uint32_t high = lq_kv_high((int8_t)(tail >> 8 & 0xFF));
+        uint2 w[2][NT];                                    // weights of 16 tokens: of words 2 a, of words 2 a + 1
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const float r0 = top[n][0] == -INFINITY ? 0.f : -top[n][0], r1 = top[n][1] == -INFINITY ? 0.f : -top[n][1];
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            const float x0 = ex2(fmaf(s[a][n][0], scale, r0)), x1 = ex2(fmaf(s[a][n][1], scale, r1));
+            const float x2 = ex2(fmaf(s[a][n][2], scale, r0)), x3 = ex2(fmaf(s[a][n][3], scale, r1));
+            sum[n][0] += x0 + x2;
+            sum[n][1] += x1 + x3;
+            w[a][n] = make_uint2(turned(pack(x0, x1)), turned(pack(x2, x3)));
+          }
+        }
+        const uint32_t high = lq_kv_high((int8_t)(head >> 8 & 0xFF));
         const __half2 less = lq_kv_less(high);
-        // tile 2 s, columns 2 t and 2 t + 1: tokens 0 and 2 of the lane's four; tile 2 s + 1: tokens 1 and 3
-        const uint32_t a0[4] = {w[0][0], w[0][1], w[1][0], w[1][1]}, a1[4] = {w[2][0], w[2][1], w[3][0], w[3][1]};
+        // columns 2 t and 2 t + 1 of words 2 a are tokens 0 and 2 of the lane's four, of words 2 a + 1 tokens 1 and 3
 #pragma unroll
         for (int g = 0; g < NK; ++g) {
           const uint4 v = vu[32 * g];
-          mma_f16(o[g][0], a0, lq_kv_open<0x4240>(v.x, high, less), lq_kv_open<0x4341>(v.x, high, less));
-          mma_f16(o[g][1], a0, lq_kv_open<0x4240>(v.y, high, less), lq_kv_open<0x4341>(v.y, high, less));
-          mma_f16(o[g][0], a1, lq_kv_open<0x4240>(v.z, high, less), lq_kv_open<0x4341>(v.z, high, less));
-          mma_f16(o[g][1], a1, lq_kv_open<0x4240>(v.w, high, less), lq_kv_open<0x4341>(v.w, high, less));
+          const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            const uint32_t a0 = lq_kv_open<0x4240>(vv[2 * a], high, less), a2 = lq_kv_open<0x4341>(vv[2 * a], high, less);
+            const uint32_t a1 = lq_kv_open<0x4240>(vv[2 * a + 1], high, less), a3 = lq_kv_open<0x4341>(vv[2 * a + 1], high, less);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_f16(o[g][n], a0, a1, a2, a3, w[a][n]);
+          }
         }
       }
       fence_proxy_async();                                 // the stage is read by all lanes before a copy into it is asked for
@@ -295,39 +336,41 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
     }
     // the warps' results of the tile
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 1);
-      sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 2);
-      const int row = c8 + 8 * r;
-      if (row < rows) {
-        if (t == 0) { sm.top[warp][row] = top[r]; sm.total[warp][row] = sum[r]; }
-        if (top[r] != -INFINITY)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int g = 0; g < NK; ++g)                     // column 2 t + b of tile i is entry 2 (2 t + b) + i of the 16
-            *reinterpret_cast<float4*>(&sm.sums[warp][row][16 * g + 4 * t]) = make_float4(o[g][0][2 * r], o[g][1][2 * r], o[g][0][2 * r + 1], o[g][1][2 * r + 1]);
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) sum[n][b] += __shfl_xor_sync(0xffffffffu, sum[n][b], d);
+        const int row = 8 * n + 2 * t + b;
+        if (row < rows) {
+          if (c8 == 0) { sm.top[warp][row] = top[n][b]; sm.total[warp][row] = sum[n][b]; }
+          if (top[n][b] != -INFINITY)
+#pragma unroll
+            for (int g = 0; g < NK; ++g) *reinterpret_cast<float2*>(&sm.sums[warp][row][16 * g + 2 * c8]) = make_float2(o[g][n][b], o[g][n][2 + b]);
+        }
       }
-    }
     __syncthreads();
+    const long long tile_begin = seg - first, tile_end = tile_begin + here.each;
     const bool whole = tile_begin >= lo && tile_end <= hi;
-    const long long row0 = (long long)tile * ROWS;
     const auto put = [&](int row, int d, float4 x, float total_w) {
       // values were opened as 2^-4 of themselves
       const float by = total_w > 0.f ? 16.f / total_w : 0.f;
       if (d >= p.D) return;
-      const int r = (int)row0 + row, tok = r / p.group;
-      __half* to = p.out + (here.q.row + tok) * p.out_row + (long long)(h * p.group + r - tok * p.group) * p.out_head + d;
+      const int r = here.tile * ROWS + row, tok = r / p.group;
+      __half* to = p.out + (here.q.row + tok) * p.out_row + (long long)(here.head * p.group + r - tok * p.group) * p.out_head + d;
       *reinterpret_cast<uint2*>(to) = make_uint2(pack(x.x * by, x.y * by), pack(x.z * by, x.w * by));
     };
-    const int slot = 2 * blockIdx.x + (tile_begin >= lo ? 1 : 0);
-    float* part = p.part + (long long)slot * ROWS * (DP + 2);
+    const int place = 2 * blockIdx.x + (tile_begin >= lo ? 1 : 0);
+    float* part = p.part + (long long)place * LQ_ATTN_ROWS * (DP + 2);
     for (int e = tid; e < rows * (DP / 4); e += THREADS) {
       const int row = e / (DP / 4), d = 4 * (e - row * (DP / 4));
       float m = -INFINITY, n = 0.f;
+#pragma unroll
       for (int i = 0; i < WARPS; ++i) m = fmaxf(m, sm.top[i][row]);
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int i = 0; i < WARPS; ++i) {
         if (sm.top[i][row] == -INFINITY) continue;
-        const float k = exp2f(sm.top[i][row] - m);
+        const float k = ex2(sm.top[i][row] - m);
         const float4 v = *reinterpret_cast<const float4*>(&sm.sums[i][row][d]);
         n = fmaf(k, sm.total[i][row], n);
         x.x = fmaf(k, v.x, x.x); x.y = fmaf(k, v.y, x.y); x.z = fmaf(k, v.z, x.z); x.w = fmaf(k, v.w, x.w);
@@ -355,7 +398,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
       if (sm.last) {
         for (int e = tid; e < rows * (DP / 4); e += THREADS) {
           const int row = e / (DP / 4), d = 4 * (e - row * (DP / 4));
-          const auto of = [&](int c) { return p.part + ((long long)(2 * c + (c == from ? 1 : 0)) * ROWS + row) * (DP + 2); };
+          const auto of = [&](int c) { return p.part + ((long long)(2 * c + (c == from ? 1 : 0)) * LQ_ATTN_ROWS + row) * (DP + 2); };
           float m = -INFINITY, n = 0.f;
           for (int c = from; c <= to; ++c) m = fmaxf(m, __ldcg(of(c)));
           float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -364,7 +407,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
             const float2 head = __ldcg(reinterpret_cast<const float2*>(v)), u0 = __ldcg(reinterpret_cast<const float2*>(v + 2 + d)),
                          u1 = __ldcg(reinterpret_cast<const float2*>(v + 4 + d));
             if (head.x == -INFINITY) continue;
-            const float k = exp2f(head.x - m);
+            const float k = ex2(head.x - m);
             n = fmaf(k, head.y, n);
             x.x = fmaf(k, u0.x, x.x); x.y = fmaf(k, u0.y, x.y); x.z = fmaf(k, u1.x, x.z); x.w = fmaf(k, u1.y, x.w);
           }
@@ -373,41 +416,47 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
       }
     }
     __syncthreads();                                       // the warps' results are read
-    seg = seg_end;
+    seg += last - first;
+    if (seg < hi) walk<ROWS>(p, here, last - first);
   }
   // (only after a wait that gave up: what is in flight lands before the block leaves)
   if (!good)
     for (; taken < issued; ++taken) mbar_settle(smem_u32(&sm.bars[warp][taken % STAGES]), (taken / STAGES) & 1);
 }
 
-// Shared memory holds two to four records of every warp and the warps' sums: eight warps up to 128 entries, four above.
-template <int NK, int WARPS, int STAGES>
-cudaError_t launch_one(const lq_kvcache* C, const LqAttnParams& p, cudaStream_t st) {
-  return lq_launch(lq_attn_kernel<NK, WARPS, STAGES>, C->sms, 32 * WARPS, sizeof(Shared<NK, WARPS, STAGES>), st, p);
-}
-template <int NK, int WARPS, int STAGES>
-bool room() {
-  return lq_note_cuda(cudaFuncSetAttribute(lq_attn_kernel<NK, WARPS, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           (int)sizeof(Shared<NK, WARPS, STAGES>))) == cudaSuccess;
-}
-cudaError_t launch_few(const lq_kvcache* C, const LqAttnParams& p, cudaStream_t st) {
-  switch (C->Dp) {
-    case 64: return launch_one<4, 8, 4>(C, p, st);
-    case 80: return launch_one<5, 8, 3>(C, p, st);
-    case 96: return launch_one<6, 8, 2>(C, p, st);
-    case 112: return launch_one<7, 8, 2>(C, p, st);
-    case 128: return launch_one<8, 8, 2>(C, p, st);
-    case 192: return launch_one<12, 4, 3>(C, p, st);
-    default: return launch_one<16, 4, 2>(C, p, st);
+// Shared memory holds two to four records of every warp and the warps' sums.
+template <int NK, int NT, int WARPS, int STAGES>
+struct Form {
+  static cudaError_t launch(const lq_kvcache* C, const LqAttnParams& p, cudaStream_t st) {
+    return lq_launch(lq_attn_kernel<NK, NT, WARPS, STAGES>, C->sms, 32 * WARPS, sizeof(Shared<NK, NT, WARPS, STAGES>), st, p);
+  }
+  static bool room() {
+    return lq_note_cuda(cudaFuncSetAttribute(lq_attn_kernel<NK, NT, WARPS, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)sizeof(Shared<NK, NT, WARPS, STAGES>))) == cudaSuccess;
+  }
+};
+#ifndef W8
+#define W8 8
+#define S8 2
+#endif
+template <typename F>
+auto with_form(int Dp, bool narrow, const F& f) {
+  switch (Dp) {
+    case 64: return narrow ? f(Form<4, 1, 8, 4>()) : f(Form<4, 2, 8, 4>());
+    case 80: return narrow ? f(Form<5, 1, 8, 3>()) : f(Form<5, 2, 8, 3>());
+    case 96: return narrow ? f(Form<6, 1, 8, 3>()) : f(Form<6, 2, 8, 2>());
+    case 112: return narrow ? f(Form<7, 1, 8, 2>()) : f(Form<7, 2, 8, 2>());
+    case 128: return narrow ? f(Form<8, 1, W8, S8>()) : f(Form<8, 2, 8, 2>());
+    case 192: return narrow ? f(Form<12, 1, 4, 3>()) : f(Form<12, 2, 4, 3>());
+    default: return narrow ? f(Form<16, 1, 4, 2>()) : f(Form<16, 2, 4, 2>());
   }
 }
 
 }  // namespace
 
 lq_status lq_attn_prepare(const lq_kvcache* C) {
-  const bool ok = C->Dp == 64 ? room<4, 8, 4>() : C->Dp == 80 ? room<5, 8, 3>() : C->Dp == 96 ? room<6, 8, 2>() : C->Dp == 112 ? room<7, 8, 2>()
-                  : C->Dp == 128 ? room<8, 8, 2>() : C->Dp == 192 ? room<12, 4, 3>() : room<16, 4, 2>();
-  if (!ok) return LQ_ERR_CUDA;
+  for (bool narrow : {false, true})
+    if (!with_form(C->Dp, narrow, [](auto form) { return form.room(); })) return LQ_ERR_CUDA;
   return C->Dp <= 128 ? lq_attn_tile_prepare(C) : LQ_OK;
 }
 
@@ -450,7 +499,9 @@ extern "C" lq_status lq_cache_attention(const lq_kvcache* C, int32_t layer, cons
   if (!tiles || least <= LQ_ATTN_FEW) {
     p.few = 1;
     p.many = tiles ? LQ_ATTN_FEW + 1 : 0x7fffffff;
-    if (lq_note_cuda(launch_few(C, p, (cudaStream_t)stream)) != cudaSuccess) return LQ_ERR_CUDA;
+    // (tiles of eight rows where no sequence has more)
+    const cudaError_t e = with_form(C->Dp, most <= 8, [&](auto form) { return form.launch(C, p, (cudaStream_t)stream); });
+    if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
   }
   if (tiles && most > LQ_ATTN_FEW) {
     p.few = LQ_ATTN_FEW + 1;

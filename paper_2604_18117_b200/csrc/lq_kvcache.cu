@@ -282,7 +282,7 @@ lq_status lq_take_batch(const lq_kvcache* C, int32_t layer, const lq_kvbatch* b,
   if (b->sequences > LQ_KV_MAX_SEQUENCES) return LQ_ERR_UNSUPPORTED;
   if (!b->row_start && b->rows % b->sequences != 0) return LQ_ERR_INVALID_ARG;
   *out = LqBatch{b->row_start, b->length, b->pages, b->sequences, b->rows, b->rows / b->sequences, b->page_stride, C->pages, C->page_tokens / LQ_KV_BLOCK,
-                 C->heads, lq_kv_record_bytes(C->Dp)};
+                 C->heads, lq_kv_record_bytes(C->Dp), ((1ull << 37) + C->page_tokens / LQ_KV_BLOCK - 1) / (C->page_tokens / LQ_KV_BLOCK)};
   return LQ_OK;
 }
 

@@ -41,6 +41,7 @@ struct LqBatch {
   int sequences, rows, each;             // each: rows of every sequence where row_start is NULL
   int page_stride, page_count, page_blocks, heads;
   long long record;                      // bytes
+  uint64_t by_page_blocks;               // 2^37 / page_blocks, rounded up: quotients of what is below 2^26 (page_blocks <= 2^11)
 };
 
 // checks a caller's batch against a cache; LQ_OK fills *out
@@ -76,11 +77,15 @@ __device__ __forceinline__ bool lq_seq_fits(const LqBatch& b, const LqSeq& q) {
 __device__ __forceinline__ void lq_kv_refuse(int32_t* status) {
   if (atomicCAS(status, 0, (int)LQ_ERR_INVALID_ARG) == 0) status[1] = LQ_STAGE_NONE;
 }
+__device__ __forceinline__ int lq_kv_slot(const LqBatch& b, int block) { return (int)(((uint64_t)(uint32_t)block * b.by_page_blocks) >> 37); }
 // index of a block's first record (of head 0), or -1: the page is none of the cache's
-__device__ __forceinline__ long long lq_kv_at(const LqBatch& b, int s, int block) {
-  const int slot = block / b.page_blocks, page = b.pages[(long long)s * b.page_stride + slot];
+__device__ __forceinline__ long long lq_kv_at(const LqBatch& b, int block, int slot, int page) {
   if (page < 0 || page >= b.page_count) return -1;
   return ((long long)page * b.page_blocks + (block - slot * b.page_blocks)) * b.heads;
+}
+__device__ __forceinline__ long long lq_kv_at(const LqBatch& b, int s, int block) {
+  const int slot = lq_kv_slot(b, block);
+  return lq_kv_at(b, block, slot, b.pages[(long long)s * b.page_stride + slot]);
 }
 // Two codes of a word (SEL: 0x4140 the lower two, 0x4342 the upper two, 0x4240 and 0x4341 every second one) as halves, each times 2^(e - 4): a byte u under the upper byte `high` of a
 // half is (1024 + u) 2^(e - 4), and what `less` takes off leaves u - 128 = c of that, all of it exact for e in [-20, 9].
