@@ -6,7 +6,8 @@
 // What bounds it is the memory: a code is read once for all query heads of its group.  The records of all (sequence, head, tile of 16 rows)
 // that a launch has lie in a row, tile after tile, and are shared out evenly, neighbouring ones to a block of the grid, so a long sequence
 // takes many blocks and ragged batches leave none idle.  A tile whose records are two blocks' or more leaves partial results (unscaled sums,
-// maximum, sum), which the last of them to arrive joins in the order of the blocks: no result depends on who was last.
+// maximum, sum), which the last of them to arrive joins in the order of the blocks: no result depends on who was last.  That costs some 2 us, as
+// much as a few records a warp, so a tile of few records is one block's as a whole.
 //
 // Within a block each warp takes every WARPS-th record, through a ring of its own in shared memory that bulk copies fill.  A record is opened
 // to halves in registers (a byte permutation and a packed subtraction for two codes), which are the first operands of m16n8k16 products: S^T =
@@ -16,6 +17,7 @@
 #include <math.h>
 
 #include "lq_attn.h"
+#include "lq_attn_places.h"
 #include "lq_device.cuh"
 #include "lq_heads_places.h"
 
@@ -24,6 +26,7 @@ using namespace lqdev;
 namespace {
 
 constexpr float GROWTH = 8.f;
+constexpr int SHORT = 4;                 // records a warp of a tile that is not shared out
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint2& b) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -45,41 +48,21 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// A place in the launch's row of records: sequence by sequence, head by head, tile of rows by tile of rows.  Walks forward.
-struct Place {
-  LqSeq q;
+struct Seq {
+  LqSeq rows;
   LqSeen seen;
-  int s, tiles, each;                    // tiles: of rows of the sequence; each: records of a tile
-  int head, tile, i;                     // i: record of the tile
 };
+using Place = LqAttnPlace<Seq>;
 template <int ROWS>
-__device__ __forceinline__ void measure(const LqAttnParams& p, int s, Place& at, bool tell) {
+__device__ __forceinline__ Place measure(const LqAttnParams& p, int s, bool tell) {
+  Place at = {};
   at.s = s;
-  at.q = lq_seq(p.b, s);
-  at.tiles = at.each = at.head = at.tile = at.i = 0;
-  if (!lq_attn_takes(p, at.q, tell)) return;
-  at.seen = lq_seen(p, at.q.len - at.q.n, at.q.len - 1, at.q.len);
-  at.each = max(1, at.seen.count());
-  at.tiles = (int)(((long long)at.q.n * p.group + ROWS - 1) / ROWS);
-}
-__device__ __forceinline__ long long records_of(const LqAttnParams& p, const Place& at) { return (long long)at.tiles * at.each * p.b.heads; }
-// n records on; false: behind the last
-template <int ROWS>
-__device__ __forceinline__ bool walk(const LqAttnParams& p, Place& at, int n) {
-  at.i += n;
-  while (at.i >= at.each) {
-    const int left = at.i - at.each;
-    at.i = left;
-    if (++at.tile < at.tiles) continue;
-    at.tile = 0;
-    if (++at.head < p.b.heads && at.tiles > 0) continue;
-    do {
-      if (at.s + 1 >= p.b.sequences) { at.i = 0; return false; }
-      measure<ROWS>(p, at.s + 1, at, false);
-    } while (at.tiles == 0);
-    at.i = left;
-  }
-  return true;
+  const LqSeq q = at.q.rows = lq_seq(p.b, s);
+  if (!lq_attn_takes(p, q, tell)) return at;
+  at.q.seen = lq_seen(p, q.len - q.n, q.len - 1, q.len);
+  at.each = max(1, at.q.seen.count());
+  at.tiles = (int)(((long long)q.n * p.group + ROWS - 1) / ROWS);
+  return at;
 }
 
 template <int NK, int NT, int WARPS, int STAGES>
@@ -90,10 +73,11 @@ struct Shared {
   alignas(16) float sums[WARPS][ROWS][PITCH];
   float top[WARPS][ROWS], total[WARPS][ROWS];
   alignas(16) uint2 q[Q_HERE ? NK : 1][NT][32];
-  long long prefix[32 * WARPS + 1];
+  long long prefix[WARPS], edge[2];
+  Place found;
   alignas(8) uint64_t bars[WARPS][STAGES];
   uint8_t empty[WARPS][STAGES];
-  int abort_flag, last;
+  int abort_flag, last, from, parts;
 };
 
 template <int NK, int NT, int WARPS, int STAGES>
@@ -109,15 +93,19 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
   mbar_init_fence();
   grid_launch_dependents();
   grid_dependency_wait();
+  long long share;
+  const auto sequence = [&](int s) { return measure<ROWS>(p, s, false); };
 
-  // the launch's records, and this block's share
-  const int chunk = (p.b.sequences + THREADS - 1) / THREADS;
+  // The launch's records, and this block's share of them: from edge[0] on, a place that is found, to before edge[1].  The thread that has an
+  // edge among its sequences' records looks it up.
   {
+    const int chunk = (p.b.sequences + THREADS - 1) / THREADS, first = tid * chunk, behind = min(p.b.sequences, first + chunk);
+    Place mine = {};                                       // the thread's first sequence
     long long sum = 0;
-    for (int s = tid * chunk; s < min(p.b.sequences, (tid + 1) * chunk); ++s) {
-      Place at;
-      measure<ROWS>(p, s, at, blockIdx.x == 0);
-      sum += records_of(p, at);
+    for (int s = first; s < behind; ++s) {
+      const Place at = measure<ROWS>(p, s, blockIdx.x == 0);
+      if (s == first) mine = at;
+      sum += lq_attn_records(at, p.b.heads);
     }
     long long up = sum;
 #pragma unroll
@@ -127,44 +115,63 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
     }
     if (lane == 31) sm.prefix[warp] = up;
     __syncthreads();
-    long long base = 0;
-    for (int i = 0; i < warp; ++i) base += sm.prefix[i];
+    long long begin = up - sum, total = 0;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+      if (i < warp) begin += sm.prefix[i];
+      total += sm.prefix[i];
+    }
+    share = max((long long)WARPS, lq_quotient(total + gridDim.x - 1, gridDim.x));       // at least a record for each warp
+    if (tid == 0) { sm.edge[0] = sm.edge[1] = total; }
     __syncthreads();
-    sm.prefix[tid + 1] = base + up;
-    if (tid == 0) sm.prefix[0] = 0;
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+      const long long edge = (blockIdx.x + i) * share;
+      if (edge < begin || edge >= begin + sum) continue;
+      Place at = mine;
+      const long long there = lq_attn_edge(at, begin, edge, p.b.heads, SHORT * WARPS, sequence);
+      sm.edge[i] = there;
+      if (i == 0) {
+        if (there < total) lq_attn_walk(at, 0, p.b.heads, p.b.sequences, sequence);
+        sm.found = at;
+      }
+    }
     __syncthreads();
   }
-  const long long total = sm.prefix[THREADS];
-  // at least a record for each warp
-  const long long share = max((long long)WARPS, (total + gridDim.x - 1) / gridDim.x);
-  const long long lo = blockIdx.x * share, hi = min(total, lo + share);
+  const long long lo = sm.edge[0], hi = sm.edge[1];
   if (lo >= hi) return;
-  Place here;
-  {
-    int a = 0, b = THREADS;                                // the last chunk that begins at or before lo
-    while (b - a > 1) {
-      const int m = (a + b) / 2;
-      if (sm.prefix[m] <= lo) a = m; else b = m;
+  Place here = sm.found;
+
+  const float scale = fmaxf(fabsf(p.scale), 1e-30f);       // (a scale of zero: all weights are one, and what is not seen stays -inf)
+  uint2 qb[Smem::Q_HERE ? 1 : NK][NT];
+  const auto load_q = [&](const Place& at) {
+    const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;              // of the signs of Q
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int r = at.tile * ROWS + 8 * n + c8, tok = r / p.group;
+      const bool real = r < at.q.rows.n * p.group;
+      const __half* from = p.q + (at.q.rows.row + tok) * p.q_row + (long long)(at.head * p.group + r - tok * p.group) * p.q_head + 4 * t;
+#pragma unroll
+      for (int g = 0; g < NK; ++g) {
+        uint2 v = make_uint2(0, 0);
+        if (real && 16 * g + 4 * t < p.D) {
+          v = *reinterpret_cast<const uint2*>(from + 16 * g);
+          v.x ^= flip; v.y ^= flip;
+        }
+        if constexpr (Smem::Q_HERE) sm.q[g][n][lane] = v;
+        else qb[g][n] = v;
+      }
     }
-    long long begin = sm.prefix[a];
-    measure<ROWS>(p, a * chunk, here, false);
-    while (lo - begin >= records_of(p, here)) {
-      begin += records_of(p, here);
-      measure<ROWS>(p, here.s + 1, here, false);
-    }
-    const long long tile = (lo - begin) / here.each;
-    here.i = (int)(lo - begin - tile * here.each);
-    here.head = (int)(tile / here.tiles);
-    here.tile = (int)(tile - (long long)here.head * here.tiles);
-  }
+  };
+  if constexpr (!Smem::Q_HERE) load_q(here);               // (here and below: asked for ahead of the wait for something else)
 
   // The warp's ring: records lo + warp, lo + warp + WARPS, ...  The page of the one that is next is known when it is asked for.
   Place ahead = here;
   int left = (int)((hi - lo - warp + WARPS - 1) / WARPS), slot = 0, page = -1, issued = 0;
   const auto look = [&]() {
     page = -1;
-    if (left > 0 && ahead.i < ahead.seen.count()) {
-      slot = lq_kv_slot(p.b, ahead.seen.block(ahead.i));
+    if (left > 0 && ahead.i < ahead.q.seen.count()) {
+      slot = lq_kv_slot(p.b, ahead.q.seen.block(ahead.i));
       page = p.b.pages[(long long)ahead.s * p.b.page_stride + slot];
     }
   };
@@ -172,8 +179,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
     if (left <= 0) return;
     if (lane == 0) {
       long long at = -1;
-      if (ahead.i < ahead.seen.count()) {
-        at = lq_kv_at(p.b, ahead.seen.block(ahead.i), slot, page);
+      if (ahead.i < ahead.q.seen.count()) {
+        at = lq_kv_at(p.b, ahead.q.seen.block(ahead.i), slot, page);
         if (at < 0) lq_kv_refuse(p.status);
       }
       const int st = issued % STAGES;
@@ -188,46 +195,31 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
     }
     ++issued;
     if (--left > 0) {
-      walk<ROWS>(p, ahead, WARPS);
+      if (!lq_attn_walk(ahead, WARPS, p.b.heads, p.b.sequences, sequence)) left = 0;
       look();
     }
   };
   if (left > 0) {
-    if (warp > 0) walk<ROWS>(p, ahead, warp);
+    if (!lq_attn_walk(ahead, warp, p.b.heads, p.b.sequences, sequence)) left = 0;
     look();
   }
   for (int i = 0; i < STAGES; ++i) issue();
 
-  const float scale = fmaxf(fabsf(p.scale), 1e-30f);       // (a scale of zero: all weights are one, and what is not seen stays -inf)
-  const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;  // of the signs of Q
   int taken = 0;
   bool good = true;
   for (long long seg = lo; seg < hi;) {
     // a tile of rows, or the part of it that is this block's: records first .. last - 1 of the tile
     const int first = here.i, last = (int)min((long long)here.each, first + (hi - seg));
-    const int rows = min(ROWS, here.q.n * p.group - here.tile * ROWS), base = here.q.len - here.q.n;
+    const int rows = min(ROWS, here.q.rows.n * p.group - here.tile * ROWS), base = here.q.rows.len - here.q.rows.n;
     int pos[NT][2];                                        // of the columns of S^T that the lane holds
-    uint2 qb[Smem::Q_HERE ? 1 : NK][NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) pos[n][b] = base + min(here.tile * ROWS + 8 * n + 2 * t + b, here.q.n * p.group - 1) / p.group;
-      const int r = here.tile * ROWS + 8 * n + c8, tok = r / p.group;
-      const bool real = 8 * n + c8 < rows;
-      const __half* from = p.q + (here.q.row + tok) * p.q_row + (long long)(here.head * p.group + r - tok * p.group) * p.q_head;
-      if (!Smem::Q_HERE || warp == 0)
-#pragma unroll
-        for (int g = 0; g < NK; ++g) {
-          uint2 v = make_uint2(0, 0);
-          if (real && 16 * g + 4 * t < p.D) {
-            v = *reinterpret_cast<const uint2*>(from + 16 * g + 4 * t);
-            v.x ^= flip; v.y ^= flip;
-          }
-          if constexpr (Smem::Q_HERE) sm.q[g][n][lane] = v;
-          else qb[g][n] = v;
-        }
+      for (int b = 0; b < 2; ++b) pos[n][b] = base + min(here.tile * ROWS + 8 * n + 2 * t + b, here.q.rows.n * p.group - 1) / p.group;
+    if constexpr (Smem::Q_HERE) {
+      if (warp == 0) load_q(here);
+      __syncthreads();
     }
-    if constexpr (Smem::Q_HERE) __syncthreads();
     const int first_at = base + here.tile * ROWS / p.group, last_at = base + (here.tile * ROWS + rows - 1) / p.group;
     float o[NK][NT][4] = {};
     float top[NT][2], sum[NT][2] = {};                     // top: what the weights are below, times scale; sum: of the lane's tokens
@@ -245,7 +237,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
       const uint4* vu = ku + 2 * DP;
       if (!sm.empty[warp][st]) {
         const uint32_t head = *reinterpret_cast<const uint32_t*>(rec);
-        const int token0 = here.seen.block(i) * LQ_KV_BLOCK;
+        const int token0 = here.q.seen.block(i) * LQ_KV_BLOCK;
         float s[2][NT][4] = {};                            // [words 2 a, 2 a + 1][..][token of word 2 a: rows 2 t, 2 t + 1; of 2 a + 1]
         {
           const uint32_t high = lq_kv_high((int8_t)(head & 0xFF));
@@ -266,14 +258,14 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
             }
           }
         }
-        if (!lq_all_seen(p, first_at, last_at, token0, token0 + LQ_KV_BLOCK - 1, here.q.len)) {
+        if (!lq_all_seen(p, first_at, last_at, token0, token0 + LQ_KV_BLOCK - 1, here.q.rows.len)) {
 #pragma unroll
           for (int a = 0; a < 2; ++a)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
               for (int x = 0; x < 4; ++x)
-                if (!lq_sees(p, pos[n][x & 1], token0 + lq_kv_token(c8, 2 * a + (x >> 1)), here.q.len)) s[a][n][x] = -INFINITY;
+                if (!lq_sees(p, pos[n][x & 1], token0 + lq_kv_token(c8, 2 * a + (x >> 1)), here.q.rows.len)) s[a][n][x] = -INFINITY;
         }
         float high_s[NT][2];
         bool grow = false;
@@ -334,6 +326,12 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
       __syncwarp();
       issue();
     }
+    const Place was = here;
+    const long long next = seg + (last - first);
+    if (next < hi) {
+      if (!lq_attn_walk(here, last - first, p.b.heads, p.b.sequences, sequence)) break;
+      if constexpr (!Smem::Q_HERE) load_q(here);
+    }
     // the warps' results of the tile
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -350,27 +348,28 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
         }
       }
     __syncthreads();
-    const long long tile_begin = seg - first, tile_end = tile_begin + here.each;
-    const bool whole = tile_begin >= lo && tile_end <= hi;
+    const long long tile_begin = seg - first;
+    const bool whole = first == 0 && last == was.each;
     const auto put = [&](int row, int d, float4 x, float total_w) {
       // values were opened as 2^-4 of themselves
       const float by = total_w > 0.f ? 16.f / total_w : 0.f;
       if (d >= p.D) return;
-      const int r = here.tile * ROWS + row, tok = r / p.group;
-      __half* to = p.out + (here.q.row + tok) * p.out_row + (long long)(here.head * p.group + r - tok * p.group) * p.out_head + d;
+      const int r = was.tile * ROWS + row, tok = r / p.group;
+      __half* to = p.out + (was.q.rows.row + tok) * p.out_row + (long long)(was.head * p.group + r - tok * p.group) * p.out_head + d;
       *reinterpret_cast<uint2*>(to) = make_uint2(pack(x.x * by, x.y * by), pack(x.z * by, x.w * by));
     };
-    const int place = 2 * blockIdx.x + (tile_begin >= lo ? 1 : 0);
-    float* part = p.part + (long long)place * LQ_ATTN_ROWS * (DP + 2);
+    float* part = p.part + (2ll * blockIdx.x + (first == 0 ? 1 : 0)) * LQ_ATTN_ROWS * (DP + 4);
     for (int e = tid; e < rows * (DP / 4); e += THREADS) {
       const int row = e / (DP / 4), d = 4 * (e - row * (DP / 4));
       float m = -INFINITY, n = 0.f;
+      float tops[WARPS];
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) m = fmaxf(m, sm.top[i][row]);
+      for (int i = 0; i < WARPS; ++i) m = fmaxf(m, tops[i] = sm.top[i][row]);
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
       for (int i = 0; i < WARPS; ++i) {
-        if (sm.top[i][row] == -INFINITY) continue;
-        const float k = ex2(sm.top[i][row] - m);
+        if (tops[i] == -INFINITY) continue;
+        const float k = ex2(tops[i] - m);
         const float4 v = *reinterpret_cast<const float4*>(&sm.sums[i][row][d]);
         n = fmaf(k, sm.total[i][row], n);
         x.x = fmaf(k, v.x, x.x); x.y = fmaf(k, v.y, x.y); x.z = fmaf(k, v.z, x.z); x.w = fmaf(k, v.w, x.w);
@@ -378,46 +377,57 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
       if (whole) {
         put(row, d, x, n);
       } else {
-        float* to = part + row * (DP + 2) + 2;
-        *reinterpret_cast<float2*>(to + d) = make_float2(x.x, x.y);
-        *reinterpret_cast<float2*>(to + d + 2) = make_float2(x.z, x.w);
-        if (d == 0) { to[-2] = m; to[-1] = n; }
+        float* to = part + row * (DP + 4);
+        *reinterpret_cast<float4*>(to + 4 + d) = x;
+        if (d == 0) *reinterpret_cast<float2*>(to) = make_float2(m, n);
       }
     }
     if (!whole) {
-      const int from = (int)(tile_begin / share), to = (int)((tile_end - 1) / share);
       __threadfence();
       __syncthreads();
       if (tid == 0) {
-        const int before = atomicAdd(&p.count[from], 1);
-        sm.last = before == to - from;
+        const int from = (int)lq_quotient(tile_begin, share), to = (int)lq_quotient(tile_begin + was.each - 1, share);
+        sm.from = from;
+        sm.parts = to - from + 1;
+        sm.last = atomicAdd(&p.count[from], 1) == to - from;
         if (sm.last) p.count[from] = 0;                    // (nobody else comes)
         __threadfence();
       }
       __syncthreads();
       if (sm.last) {
+        const int from = sm.from, parts = sm.parts;
         for (int e = tid; e < rows * (DP / 4); e += THREADS) {
           const int row = e / (DP / 4), d = 4 * (e - row * (DP / 4));
-          const auto of = [&](int c) { return p.part + ((long long)(2 * c + (c == from ? 1 : 0)) * LQ_ATTN_ROWS + row) * (DP + 2); };
           float m = -INFINITY, n = 0.f;
-          for (int c = from; c <= to; ++c) m = fmaxf(m, __ldcg(of(c)));
           float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int c = from; c <= to; ++c) {
-            const float* v = of(c);
-            const float2 head = __ldcg(reinterpret_cast<const float2*>(v)), u0 = __ldcg(reinterpret_cast<const float2*>(v + 2 + d)),
-                         u1 = __ldcg(reinterpret_cast<const float2*>(v + 4 + d));
-            if (head.x == -INFINITY) continue;
-            const float k = ex2(head.x - m);
-            n = fmaf(k, head.y, n);
-            x.x = fmaf(k, u0.x, x.x); x.y = fmaf(k, u0.y, x.y); x.z = fmaf(k, u1.x, x.z); x.w = fmaf(k, u1.y, x.w);
+          for (int c = 0; c < parts; c += 4) {             // four at a time are on their way
+            float2 head[4];
+            float4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float* at = p.part + ((2ll * (from + min(c + i, parts - 1)) + (c + i == 0 ? 1 : 0)) * LQ_ATTN_ROWS + row) * (DP + 4);
+              head[i] = __ldcg(reinterpret_cast<const float2*>(at));
+              v[i] = __ldcg(reinterpret_cast<const float4*>(at + 4 + d));
+              if (c + i >= parts) head[i].x = -INFINITY;
+            }
+            const float top = fmaxf(m, fmaxf(fmaxf(head[0].x, head[1].x), fmaxf(head[2].x, head[3].x)));
+            const float by = m == -INFINITY ? 0.f : ex2(m - top);
+            n *= by; x.x *= by; x.y *= by; x.z *= by; x.w *= by;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (head[i].x == -INFINITY) continue;
+              const float k = ex2(head[i].x - top);
+              n = fmaf(k, head[i].y, n);
+              x.x = fmaf(k, v[i].x, x.x); x.y = fmaf(k, v[i].y, x.y); x.z = fmaf(k, v[i].z, x.z); x.w = fmaf(k, v[i].w, x.w);
+            }
+            m = top;
           }
           put(row, d, x, n);
         }
       }
     }
     __syncthreads();                                       // the warps' results are read
-    seg += last - first;
-    if (seg < hi) walk<ROWS>(p, here, last - first);
+    seg = next;
   }
   // (only after a wait that gave up: what is in flight lands before the block leaves)
   if (!good)

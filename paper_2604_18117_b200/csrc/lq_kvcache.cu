@@ -306,7 +306,7 @@ extern "C" lq_status lq_kvcache_create(int32_t layers, int32_t pages, int32_t pa
     return LQ_ERR_CUDA;
   }
   if (lq_note_cuda(cudaMalloc((void**)&C->d_records, n * rec)) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&C->d_part, (size_t)2 * C->sms * LQ_ATTN_ROWS * (Dp + 2) * sizeof(float))) != cudaSuccess ||
+      lq_note_cuda(cudaMalloc((void**)&C->d_part, (size_t)2 * C->sms * LQ_ATTN_ROWS * (Dp + 4) * sizeof(float))) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&C->d_count, C->sms * sizeof(int))) != cudaSuccess) {
     lq_kvcache_free(C);
     return LQ_ERR_ALLOC;

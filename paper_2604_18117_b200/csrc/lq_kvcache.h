@@ -31,7 +31,7 @@ struct lq_kvcache {
   int layers, pages, page_tokens, heads, D, Dp, device, sms;
   uint8_t* d_records;
   // workspace of the attention: for each block of its grid two partial results of a tile of rows, and a count of those that have arrived
-  float* d_part;                         // [2 * sms][LQ_ATTN_ROWS][Dp + 2]
+  float* d_part;                         // [2 * sms][LQ_ATTN_ROWS][Dp + 4]: maximum, sum, -, -, sums
   int* d_count;                          // [sms]
 };
 
