@@ -18,35 +18,18 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int WARPS = 4;
+constexpr int THREADS = 128;             // two warps for the keys of a block of tokens, two for its values
 
 struct RowsParams {
   LqBatch b;
   uint8_t* records;
   void *k, *v;
   long long seq[2], row[2], head[2];     // strides in elements
-  int D, Dp, tile;                       // tile: rows that a warp looks through
+  int D, Dp, tile;                       // append: tile: rows that a thread block looks through
   const int32_t* begin;
   int most, blocks;                      // read: most tokens of a sequence, blocks that they can touch
   int32_t* status;
 };
-
-template <typename T>
-__device__ __forceinline__ float4 load4(const T* p);
-template <>
-__device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <>
-__device__ __forceinline__ float4 load4<__half>(const __half* p) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&v.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
-  return make_float4(a.x, a.y, b.x, b.y);
-}
-template <typename T>
-__device__ __forceinline__ float2 load2(const T* p);
-template <>
-__device__ __forceinline__ float2 load2<float>(const float* p) { return *reinterpret_cast<const float2*>(p); }
-template <>
-__device__ __forceinline__ float2 load2<__half>(const __half* p) { return __half22float2(*reinterpret_cast<const __half2*>(p)); }
 
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
 // smallest e in range with 127 * 2^e >= top
@@ -56,11 +39,61 @@ __device__ __forceinline__ int exponent_of(float top) {
   const int x = (int)(bits >> 23) - 127, e = x - 6 + ((bits & 0x7FFFFF) > (63u << 17));
   return max(LQ_KV_E_MIN, min(LQ_KV_E_MAX, e));
 }
-__device__ __forceinline__ uint32_t code_of(float x, float inv) {         // byte c + 128
-  return (uint32_t)(__float2int_rn(fminf(fmaxf(x * inv, -127.f), 127.f)) + 128);
-}
 // rint(c / 2^k) of a byte c + 128
 __device__ __forceinline__ uint32_t shrink(uint32_t u, float inv) { return (uint32_t)(__float2int_rn((float)((int)u - 128) * inv) + 128); }
+
+// Eight neighbouring entries of a token, as they lie in memory: their largest magnitude, and their codes as bytes c + 128, four to a word.
+// FMA with a constant whose last place is one rounds to whole numbers, to even in the middle, and leaves the byte as the lowest of the sum.
+template <typename T> struct Raw8;
+template <> struct Raw8<__half> {
+  uint4 v;
+  __device__ __forceinline__ static Raw8 load(const __half* p) { return {*reinterpret_cast<const uint4*>(p)}; }
+  __device__ __forceinline__ static Raw8 zero() { return {make_uint4(0, 0, 0, 0)}; }
+  __device__ __forceinline__ float top(float m) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    __half2 a = __habs2(*reinterpret_cast<const __half2*>(&w[0]));
+#pragma unroll
+    for (int i = 1; i < 4; ++i) a = __hmax2(a, __habs2(*reinterpret_cast<const __half2*>(&w[i])));
+    return fmaxf(m, __half2float(__hmax(__low2half(a), __high2half(a))));
+  }
+  __device__ __forceinline__ uint2 codes(int e) const {
+    // 2^-e is a half down to e = -15; below that in two steps, both exact
+    const __half2 first = __float2half2_rn(e < -15 ? 32.f : 1.f), rest = __float2half2_rn(pow2(e < -15 ? -e - 5 : -e)), place = __float2half2_rn(1664.f);
+    const __half2 most = __float2half2_rn(65024.f), least = __float2half2_rn(-65024.f);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __half2 x = *reinterpret_cast<const __half2*>(&w[i]);
+      if (e == LQ_KV_E_MAX) x = __hmax2(least, __hmin2(most, x));
+      x = __hfma2(__hmul2(x, first), rest, place);
+      c[i] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+    return make_uint2(__byte_perm(c[0], c[1], 0x6420), __byte_perm(c[2], c[3], 0x6420));
+  }
+};
+template <> struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ static Raw8 load(const float* p) { return {reinterpret_cast<const float4*>(p)[0], reinterpret_cast<const float4*>(p)[1]}; }
+  __device__ __forceinline__ static Raw8 zero() { return {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}; }
+  __device__ __forceinline__ float top(float m) const {
+    m = fmaxf(fmaxf(m, fmaxf(fabsf(a.x), fabsf(a.y))), fmaxf(fabsf(a.z), fabsf(a.w)));
+    return fmaxf(fmaxf(m, fmaxf(fabsf(b.x), fabsf(b.y))), fmaxf(fabsf(b.z), fabsf(b.w)));
+  }
+  __device__ __forceinline__ uint2 codes(int e) const {
+    const float inv = pow2(-e), place = 12582912.f + 128.f;
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float y = x[i];
+      if (e == LQ_KV_E_MAX) y = fminf(fmaxf(y, -65024.f), 65024.f);
+      c[i] = __float_as_uint(fmaf(y, inv, place));
+    }
+    return make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
+  }
+};
 
 // The sequence that row r belongs to: the last one that begins at or before it and has rows, found by the warp together.
 __device__ __forceinline__ int sequence_of(const LqBatch& b, int r, int lane) {
@@ -76,86 +109,154 @@ __device__ __forceinline__ int sequence_of(const LqBatch& b, int r, int lane) {
   return lo;
 }
 
-// One block, keys or values, one warp: tokens t0 .. t1 - 1 of it are new, rows of `in` from that of t0 on; those before t0 are there already.
+// A side of a record in shared memory, between rows and the order that it is kept in.  A thread turns units of four neighbouring tokens (a
+// quad, of eight) times eight neighbouring entries (a chunk), so that rows are read and written 16 bytes a lane, whole rows by neighbouring
+// lanes, and the record eight bytes at a time.  Lanes: bit 0 the upper half of a quad's number, the others the chunk; the warp the rest of the
+// quad's number.  Records' 16-byte pieces change places within groups of eight, so that these eight bytes meet in no bank.
+template <bool KEYS>
+__device__ __forceinline__ int piece(int n) {
+  const int g = n >> 5;
+  return n ^ (KEYS ? (g & 1) | (g & 2) << 1 : (g & 3) | (n >> 2 & 4));
+}
+struct Unit {
+  int upper, quad, chunk;                // the quad is 4 * upper + quad
+  __device__ __forceinline__ int token(int x) const { return 16 * upper + 4 * quad + x; }
+  // the i-th eight bytes: keys: entries 4 (i / 2) .. of the chunk, tokens 2 (i % 2), 2 (i % 2) + 1; values: entries 2 i, 2 i + 1, all tokens
+  template <bool KEYS>
+  __device__ __forceinline__ int at(int i) const {
+    const int n = KEYS ? (chunk >> 1) * 32 + (2 * quad + (i & 1)) * 4 + (chunk & 1) * 2 + (i >> 1) : (chunk >> 1) * 32 + ((chunk & 1) * 4 + i) * 4 + quad;
+    return piece<KEYS>(n) * 16 + upper * 8;
+  }
+};
+// keys' and values' warps meet, each in code of their own
+__device__ __forceinline__ void meet() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+__device__ __forceinline__ uint2 lds_v2(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts_v2(uint32_t a, const uint2& v) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(v.x), "r"(v.y) : "memory"); }
+
+// One block, keys or values, that has no tokens yet, two warps: tokens 0 .. n - 1 are rows of `in`, the others zeros.
+template <typename T, bool KEYS, int CHUNKS>
+__device__ __forceinline__ void fill_block(uint8_t* record, const T* in, long long row, int n, int D, int Dp, uint32_t image, float* tops) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 1, groups = (D + 15) / 16;
+  Raw8<T> raw[CHUNKS][2][4];
+  float top = 0.f;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const Unit u{lane & 1, 2 * q + warp, (lane >> 1) + 16 * c};
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        raw[c][q][x] = Raw8<T>::zero();
+        if (8 * u.chunk < D && u.token(x) < n) raw[c][q][x] = Raw8<T>::load(in + u.token(x) * row + 8 * u.chunk);
+      }
+    }
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) top = raw[c][q][x].top(top);
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  if (lane == 0) tops[threadIdx.x >> 5] = top;
+  meet();
+  const int e = exponent_of(fmaxf(tops[KEYS ? 0 : 2], tops[KEYS ? 1 : 3]));
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const Unit u{lane & 1, 2 * q + warp, (lane >> 1) + 16 * c};
+      if (u.chunk >= 2 * groups) continue;
+      uint2 w[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[x] = raw[c][q][x].codes(e);
+      if constexpr (KEYS) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sts_v2(image + u.at<true>(i), make_uint2(w[2 * i].x, w[2 * i + 1].x));
+          sts_v2(image + u.at<true>(2 + i), make_uint2(w[2 * i].y, w[2 * i + 1].y));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {                      // four tokens' bytes of four entries, rows for columns
+          const uint32_t t0 = i ? w[0].y : w[0].x, t1 = i ? w[1].y : w[1].x, t2 = i ? w[2].y : w[2].x, t3 = i ? w[3].y : w[3].x;
+          const uint32_t a = __byte_perm(t0, t1, 0x5140), b = __byte_perm(t2, t3, 0x5140), c2 = __byte_perm(t0, t1, 0x7362), d2 = __byte_perm(t2, t3, 0x7362);
+          sts_v2(image + u.at<false>(2 * i), make_uint2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632)));
+          sts_v2(image + u.at<false>(2 * i + 1), make_uint2(__byte_perm(c2, d2, 0x5410), __byte_perm(c2, d2, 0x7632)));
+        }
+      }
+    }
+  meet();
+  uint4* to = reinterpret_cast<uint4*>(record + LQ_KV_HEAD + (KEYS ? 0 : lq_kv_side_bytes(Dp)));
+  for (int i = threadIdx.x & 63; i < 32 * groups; i += 64) to[i] = lds_v4(image + piece<KEYS>(i) * 16);
+  if ((threadIdx.x & 63) == 0) reinterpret_cast<int8_t*>(record)[KEYS ? 0 : 1] = (int8_t)e;
+}
+
+// One block, keys or values, one warp: tokens t0 .. t1 - 1 of it are new, rows of `in` from that of t0 on; those before t0 (there are some) are there
+// already.
 template <typename T, bool KEYS>
-__device__ void write_block(uint8_t* record, const T* in, long long row, int t0, int t1, int D, int Dp, int lane) {
-  const int chunks = D / 8, n = t1 - t0;
+__device__ __forceinline__ void add_to_block(uint8_t* record, const T* in, long long row, int t0, int t1, int D, int Dp) {
+  const int lane = threadIdx.x & 31, chunks = D / 8, n = t1 - t0;
+  int8_t* exps = reinterpret_cast<int8_t*>(record) + (KEYS ? 0 : 1);
+  const int was = max(LQ_KV_E_MIN, min(LQ_KV_E_MAX, (int)*reinterpret_cast<volatile int8_t*>(exps)));
   float top = 0.f;
   for (int i = lane; i < n * chunks; i += 32) {
     const int r = i / chunks, c = i - r * chunks;
-    const T* p = in + r * row + 8 * c;
-    const float4 a = load4(p), b = load4(p + 4);
-    top = fmaxf(top, fmaxf(fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(a.z), fabsf(a.w))), fmaxf(fmaxf(fabsf(b.x), fabsf(b.y)), fmaxf(fabsf(b.z), fabsf(b.w)))));
+    top = Raw8<T>::load(in + r * row + 8 * c).top(top);
   }
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-  int8_t* exps = reinterpret_cast<int8_t*>(record) + (KEYS ? 0 : 1);
-  const int need = exponent_of(top), was = t0 > 0 ? max(LQ_KV_E_MIN, min(LQ_KV_E_MAX, (int)*exps)) : LQ_KV_E_MIN, e = max(need, was);
-  const bool grows = t0 > 0 && e > was;
-  const float inv = pow2(-e), less = pow2(was - e);
-  __syncwarp();
-  if (lane == 0) *exps = (int8_t)e;
+  const int e = max(exponent_of(top), was);
   uint8_t* side = record + LQ_KV_HEAD + (KEYS ? 0 : lq_kv_side_bytes(Dp));
-  const int c8 = lane >> 2, t = lane & 3;
-  // Bit i: the lane's unit has token i of the block.  Units without a token to write are left alone.
-  const uint32_t mine = KEYS ? 0x00030003u << (2 * c8) : 0x000F000Fu << (4 * t);
-  const uint32_t below1 = t1 == 32 ? 0xffffffffu : (1u << t1) - 1, fresh = below1 & ~((1u << t0) - 1);
-  if (!(mine & (grows ? below1 : fresh))) return;
-  const bool keeps = t0 > 0 && (mine & ((1u << t0) - 1)) != 0;
-  for (int g = 0; g < Dp / 16; ++g) {
-    uint4* at = reinterpret_cast<uint4*>(side + 512 * g + 16 * lane);
-    uint32_t w[4] = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-    if (keeps) {
+  if (e > was) {                                           // what is there is rounded to the larger step
+    const float less = pow2(was - e);
+    const int c8 = lane >> 2, t = lane & 3;
+    for (int g = 0; 16 * g < D; ++g) {
+      uint4* at = reinterpret_cast<uint4*>(side + 512 * g + 16 * lane);
       const uint4 v = *at;
-      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-      if (grows)                         // (what lies behind the old tokens is written below, or is no token's)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          w[i] = shrink(w[i] & 0xFF, less) | shrink((w[i] >> 8) & 0xFF, less) << 8 | shrink((w[i] >> 16) & 0xFF, less) << 16 | shrink(w[i] >> 24, less) << 24;
-    }
-    if constexpr (KEYS) {
-      const int d = 16 * g + 4 * t;
+      uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int token = lq_kv_token(c8, i);
-        if (token < t0 || token >= t1) continue;
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (d < D) x = load4(in + (token - t0) * row + d);
-        w[i] = code_of(x.x, inv) | code_of(x.y, inv) << 8 | code_of(x.z, inv) << 16 | code_of(x.w, inv) << 24;
+        if (KEYS ? lq_kv_token(c8, i) >= t0 : 16 * (i >> 1) + 4 * t >= t0) continue;
+        w[i] = shrink(w[i] & 0xFF, less) | shrink((w[i] >> 8) & 0xFF, less) << 8 | shrink((w[i] >> 16) & 0xFF, less) << 16 | shrink(w[i] >> 24, less) << 24;
       }
-    } else {
-      const int d = 16 * g + 2 * c8;
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token = 16 * s + 4 * t + i;
-          if (token < t0 || token >= t1) continue;
-          float2 x = make_float2(0.f, 0.f);
-          if (d < D) x = load2(in + (token - t0) * row + d);
-          w[2 * s] = (w[2 * s] & ~(0xFFu << (8 * i))) | code_of(x.x, inv) << (8 * i);
-          w[2 * s + 1] = (w[2 * s + 1] & ~(0xFFu << (8 * i))) | code_of(x.y, inv) << (8 * i);
-        }
+      *at = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    *at = make_uint4(w[0], w[1], w[2], w[3]);
+    if (lane == 0) *exps = (int8_t)e;
+    __syncwarp();
+  }
+  for (int i = lane; i < n * chunks; i += 32) {            // (bytes of other tokens in the same words stay)
+    const int r = i / chunks, c = i - r * chunks, token = t0 + r, quad = token >> 2 & 3, s = token >> 4;
+    const uint2 w = Raw8<T>::load(in + r * row + 8 * c).codes(e);
+    if constexpr (KEYS) {
+      const int column = 2 * quad + (token >> 1 & 1), word = 2 * s + (token & 1);
+      uint32_t* at = reinterpret_cast<uint32_t*>(side + 512 * (c >> 1) + (column * 4 + (c & 1) * 2) * 16 + word * 4);
+      at[0] = w.x;
+      at[4] = w.y;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        side[512 * (c >> 1) + (((c & 1) * 4 + (k >> 1)) * 4 + quad) * 16 + s * 8 + (k & 1) * 4 + (token & 3)] = (uint8_t)((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
+    }
   }
 }
 
-// A warp takes a head's keys or values in the blocks that begin within its tile of rows: with a sequence's first new row, or with a token
-// that is the first of its block.
-template <typename T>
-__global__ void __launch_bounds__(32 * WARPS) lq_kv_append_kernel(const __grid_constant__ RowsParams p) {
-  const int lane = threadIdx.x & 31;
-  const long long task = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
+// A thread block takes a head in the blocks of tokens that begin within its tile of rows: with a sequence's first new row, or with a token that
+// is the first of its block.
+template <typename T, int CHUNKS>
+__global__ void __launch_bounds__(THREADS) lq_kv_append_kernel(const __grid_constant__ RowsParams p) {
+  __shared__ __align__(16) uint8_t images[2][16 * CHUNKS * 256];
+  __shared__ float tops[THREADS / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, side = warp >> 1;
   grid_launch_dependents();
   grid_dependency_wait();
-  const int side = (int)(task & 1);
-  const long long rest = task >> 1;
-  const int head = (int)(rest % p.b.heads);
-  const long long first = rest / p.b.heads * p.tile;
-  if (first >= p.b.rows) return;
-  int r = (int)first;
-  const int end = (int)min((long long)p.b.rows, first + p.tile);
+  const int head = blockIdx.x % p.b.heads;
+  int r = (int)(blockIdx.x / p.b.heads) * p.tile;
+  const int end = min(p.b.rows - r, p.tile) + r;
   const T* in = reinterpret_cast<const T*>(side ? p.v : p.k) + head * p.head[side];
   int s = sequence_of(p.b, r, lane);
   while (r < end && s < p.b.sequences) {
@@ -166,61 +267,100 @@ __global__ void __launch_bounds__(32 * WARPS) lq_kv_append_kernel(const __grid_c
       continue;
     }
     if (!lq_seq_fits(p.b, q) || q.len < q.n) {
-      if (lane == 0) lq_kv_refuse(p.status);
+      if (threadIdx.x == 0) lq_kv_refuse(p.status);
       r = q.row + q.n;
       continue;
     }
     const int at = q.len - q.n + (r - q.row), t0 = at % LQ_KV_BLOCK, t1 = min(LQ_KV_BLOCK, t0 + q.row + q.n - r);
     if (r == q.row || t0 == 0) {
-      const long long record = lq_kv_at(p.b, s, at / LQ_KV_BLOCK);
-      if (record < 0) {
-        if (lane == 0) lq_kv_refuse(p.status);
+      const long long found = lq_kv_at(p.b, s, at / LQ_KV_BLOCK);
+      if (found < 0) {
+        if (threadIdx.x == 0) lq_kv_refuse(p.status);
       } else {
-        uint8_t* to = p.records + (record + head) * p.b.record;
-        if (side) write_block<T, false>(to, in + r * p.row[side], p.row[side], t0, t1, p.D, p.Dp, lane);
-        else write_block<T, true>(to, in + r * p.row[side], p.row[side], t0, t1, p.D, p.Dp, lane);
+        uint8_t* record = p.records + (found + head) * p.b.record;
+        const T* rows = in + r * p.row[side];
+        if (t0 > 0) {
+          if (warp == 0) add_to_block<T, true>(record, rows, p.row[0], t0, t1, p.D, p.Dp);
+          else if (warp == 2) add_to_block<T, false>(record, rows, p.row[1], t0, t1, p.D, p.Dp);
+        } else {
+          __syncthreads();                                 // (the images of the block before are read)
+          if (side == 0) fill_block<T, true, CHUNKS>(record, rows, p.row[0], t1, p.D, p.Dp, smem_u32(images[0]), tops);
+          else fill_block<T, false, CHUNKS>(record, rows, p.row[1], t1, p.D, p.Dp, smem_u32(images[1]), tops);
+        }
       }
     }
     r += t1 - t0;
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, float4 x);
-template <>
-__device__ __forceinline__ void store4<float>(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
-template <>
-__device__ __forceinline__ void store4<__half>(__half* p, float4 x) {
-  const __half2 a = __floats2half2_rn(x.x, x.y), b = __floats2half2_rn(x.z, x.w);
-  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+// Four neighbouring values, as halves times 16 (they were opened as 2^-4 of themselves)
+__device__ __forceinline__ uint32_t whole(uint32_t v) {
+  const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&v), __float2half2_rn(16.f));
+  return *reinterpret_cast<const uint32_t*>(&x);
 }
-template <typename T>
-__device__ __forceinline__ void store2(T* p, float x, float y);
-template <>
-__device__ __forceinline__ void store2<float>(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
-template <>
-__device__ __forceinline__ void store2<__half>(__half* p, float x, float y) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(x, y); }
+__device__ __forceinline__ void store8(__half* p, const uint32_t (&w)[4]) { *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+__device__ __forceinline__ void store8(float* p, const uint32_t (&w)[4]) {
+  float2 f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+  reinterpret_cast<float4*>(p)[0] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+  reinterpret_cast<float4*>(p)[1] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
+}
+template <typename T, bool KEYS, int CHUNKS>
+__device__ __forceinline__ void open_block(const uint8_t* record, T* out, long long row, int from, int to, int D, int Dp, uint32_t image) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 1, groups = (D + 15) / 16;
+  const uint4* units = reinterpret_cast<const uint4*>(record + LQ_KV_HEAD + (KEYS ? 0 : lq_kv_side_bytes(Dp)));
+  const uint32_t high = lq_kv_high(reinterpret_cast<const int8_t*>(record)[KEYS ? 0 : 1]);
+  const __half2 less = lq_kv_less(high);
+#pragma unroll
+  for (int i = 0; i < 4 * CHUNKS; ++i) {
+    const int n = (threadIdx.x & 63) + 64 * i;
+    if (n < 32 * groups) sts_v4(image + piece<KEYS>(n) * 16, units[n]);
+  }
+  meet();
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const Unit u{lane & 1, 2 * q + warp, (lane >> 1) + 16 * c};
+      if (8 * u.chunk >= D) continue;
+      uint32_t w[4][4];                                    // [token][pair of entries]
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 v = lds_v2(image + u.at<KEYS>(i));
+        if constexpr (KEYS) {
+          const int x = 2 * (i & 1), d = 2 * (i >> 1);
+          w[x][d] = lq_kv_open<0x4140>(v.x, high, less); w[x][d + 1] = lq_kv_open<0x4342>(v.x, high, less);
+          w[x + 1][d] = lq_kv_open<0x4140>(v.y, high, less); w[x + 1][d + 1] = lq_kv_open<0x4342>(v.y, high, less);
+        } else {
+          const uint32_t a = __byte_perm(v.x, v.y, 0x5140), b = __byte_perm(v.x, v.y, 0x7362);
+          w[0][i] = lq_kv_open<0x4140>(a, high, less); w[1][i] = lq_kv_open<0x4342>(a, high, less);
+          w[2][i] = lq_kv_open<0x4140>(b, high, less); w[3][i] = lq_kv_open<0x4342>(b, high, less);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[x][i] = whole(w[x][i]);
+        const int token = u.token(x);
+        if (token >= from && token < to) store8(out + token * row + 8 * u.chunk, w[x]);
+      }
+    }
+}
 
-__device__ __forceinline__ float value_of(uint32_t w, int i, float step) { return (float)((int)((w >> (8 * i)) & 0xFF) - 128) * step; }
-
-// A warp takes a head's keys or values of one block.
-template <typename T>
-__global__ void __launch_bounds__(32 * WARPS) lq_kv_read_kernel(const __grid_constant__ RowsParams p) {
-  const int lane = threadIdx.x & 31;
-  const long long task = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
+// A thread block takes a head in one block of tokens.
+template <typename T, int CHUNKS>
+__global__ void __launch_bounds__(THREADS) lq_kv_read_kernel(const __grid_constant__ RowsParams p) {
+  __shared__ __align__(16) uint8_t images[2][16 * CHUNKS * 256];
+  const int side = threadIdx.x >> 6, head = blockIdx.x % p.b.heads;
   grid_launch_dependents();
   grid_dependency_wait();
-  const int side = (int)(task & 1);
-  long long rest = task >> 1;
-  const int head = (int)(rest % p.b.heads);
-  rest /= p.b.heads;
-  const int s = (int)(rest / p.blocks), i = (int)(rest % p.blocks);
-  if (s >= p.b.sequences || (side ? p.v : p.k) == nullptr) return;
+  const int rest = blockIdx.x / p.b.heads, s = rest / p.blocks, i = rest - s * p.blocks;
   LqSeq q;
   q.len = p.b.length[s];
   const int begin = p.begin ? p.begin[s] : 0;
   if (!lq_seq_fits(p.b, q) || begin < 0) {
-    if (lane == 0) lq_kv_refuse(p.status);
+    if (threadIdx.x == 0) lq_kv_refuse(p.status);
     return;
   }
   const long long block = (long long)begin / LQ_KV_BLOCK + i;
@@ -228,36 +368,14 @@ __global__ void __launch_bounds__(32 * WARPS) lq_kv_read_kernel(const __grid_con
   if (block * LQ_KV_BLOCK >= end) return;
   const long long at = lq_kv_at(p.b, s, (int)block);
   if (at < 0) {
-    if (lane == 0) lq_kv_refuse(p.status);
+    if (threadIdx.x == 0) lq_kv_refuse(p.status);
     return;
   }
   const uint8_t* record = p.records + (at + head) * p.b.record;
-  const int e = reinterpret_cast<const int8_t*>(record)[side];
-  const float step = pow2(e);
-  const uint4* units = reinterpret_cast<const uint4*>(record + LQ_KV_HEAD + (side ? lq_kv_side_bytes(p.Dp) : 0)) + lane;
-  const int c8 = lane >> 2, t = lane & 3, first = (int)(block * LQ_KV_BLOCK);
+  const int first = (int)(block * LQ_KV_BLOCK), from = max(0, begin - first), to = min(LQ_KV_BLOCK, end - first);
   T* out = reinterpret_cast<T*>(side ? p.v : p.k) + s * p.seq[side] + head * p.head[side] + ((long long)first - begin) * p.row[side];
-  for (int g = 0; 16 * g < p.D; ++g) {
-    const uint4 v = units[32 * g];
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    if (side == 0) {
-      const int d = 16 * g + 4 * t;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int token = lq_kv_token(c8, j);
-        if (d < p.D && first + token >= begin && first + token < end)
-          store4(out + token * p.row[side] + d, make_float4(value_of(w[j], 0, step), value_of(w[j], 1, step), value_of(w[j], 2, step), value_of(w[j], 3, step)));
-      }
-    } else {
-      const int d = 16 * g + 2 * c8;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int token = 16 * (j >> 2) + 4 * t + (j & 3), half = 2 * (j >> 2);
-        if (d < p.D && first + token >= begin && first + token < end)
-          store2(out + token * p.row[side] + d, value_of(w[half], j & 3, step), value_of(w[half + 1], j & 3, step));
-      }
-    }
-  }
+  if (side == 0) open_block<T, true, CHUNKS>(record, out, p.row[0], p.k ? from : LQ_KV_BLOCK, to, p.D, p.Dp, smem_u32(images[0]));
+  else open_block<T, false, CHUNKS>(record, out, p.row[1], p.v ? from : LQ_KV_BLOCK, to, p.D, p.Dp, smem_u32(images[1]));
 }
 
 // Strides of one side's rows: multiples of 8 elements, so that every head begins on a 16-byte boundary.
@@ -348,14 +466,14 @@ extern "C" lq_status lq_kvcache_append(lq_kvcache* C, int32_t layer, const lq_kv
   p.records = lq_kv_layer(C, layer);
   p.D = C->D; p.Dp = C->Dp;
   p.status = lq_device_status_ptr(C->device);
-  // Rows a warp looks through: 32, as many as a block has, once that gives every SM 32 warps; with fewer rows fewer, so that blocks of
-  // different sequences are not one warp's.
-  const long long tasks = 2ll * C->heads * p.b.rows;
-  p.tile = (int)std::max(1ll, std::min(32ll, tasks / (32ll * C->sms)));
-  const long long blocks = (2ll * C->heads * lq_ceil_div(p.b.rows, p.tile) + WARPS - 1) / WARPS;
+  // Rows a thread block looks through: 32, as many as a block of tokens has, once that gives every SM eight; with fewer rows fewer, so that
+  // single tokens of different sequences are not one's.
+  p.tile = (int)std::max(1ll, std::min(32ll, (long long)C->heads * p.b.rows / (8ll * C->sms)));
+  const long long blocks = (long long)C->heads * lq_ceil_div(p.b.rows, p.tile);
   if (blocks > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
-  const cudaError_t e = dt == LQ_OUT_F16 ? lq_launch(lq_kv_append_kernel<__half>, (int)blocks, 32 * WARPS, 0, (cudaStream_t)stream, p)
-                                         : lq_launch(lq_kv_append_kernel<float>, (int)blocks, 32 * WARPS, 0, (cudaStream_t)stream, p);
+  const auto launch = [&](auto* kernel) { return lq_launch(kernel, (int)blocks, THREADS, 0, (cudaStream_t)stream, p); };
+  const cudaError_t e = dt == LQ_OUT_F16 ? (C->D <= 128 ? launch(lq_kv_append_kernel<__half, 1>) : launch(lq_kv_append_kernel<__half, 2>))
+                                         : (C->D <= 128 ? launch(lq_kv_append_kernel<float, 1>) : launch(lq_kv_append_kernel<float, 2>));
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
 
@@ -387,9 +505,10 @@ extern "C" lq_status lq_kvcache_read(const lq_kvcache* C, int32_t layer, const l
   p.records = lq_kv_layer(C, layer);
   p.D = C->D; p.Dp = C->Dp;
   p.status = lq_device_status_ptr(C->device);
-  const long long blocks = (2ll * C->heads * p.b.sequences * p.blocks + WARPS - 1) / WARPS;
+  const long long blocks = (long long)C->heads * p.b.sequences * p.blocks;
   if (blocks > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
-  const cudaError_t e = dt == LQ_OUT_F16 ? lq_launch(lq_kv_read_kernel<__half>, (int)blocks, 32 * WARPS, 0, (cudaStream_t)stream, p)
-                                         : lq_launch(lq_kv_read_kernel<float>, (int)blocks, 32 * WARPS, 0, (cudaStream_t)stream, p);
+  const auto launch = [&](auto* kernel) { return lq_launch(kernel, (int)blocks, THREADS, 0, (cudaStream_t)stream, p); };
+  const cudaError_t e = dt == LQ_OUT_F16 ? (C->D <= 128 ? launch(lq_kv_read_kernel<__half, 1>) : launch(lq_kv_read_kernel<__half, 2>))
+                                         : (C->D <= 128 ? launch(lq_kv_read_kernel<float, 1>) : launch(lq_kv_read_kernel<float, 2>));
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
