@@ -3,8 +3,9 @@
 //   x' = x + factor * gate * N1(y),   h = (N2(x') * w + b) * (1 + scale) + shift
 //
 // N: none, RMS or LayerNorm of a row; gate, scale and shift are a sequence's.  Reads x and y once and writes x' and h once; the memory
-// bounds it.  A row is held in registers by one to eight warps, eight neighbouring entries a lane at a time, so that variances are sums
-// about the mean that is known; h is made of x' before that is rounded to its type.
+// bounds it.  A row is held in registers by one, two or four warps, up to nine times eight neighbouring entries a lane, all asked for at once and
+// kept as they lie in memory until they are used: with few warps of many loads each no row waits for another's, and most sums stay within
+// a warp.  Variances are sums about the mean that is known; h is made of x' before that is rounded to its type.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -18,7 +19,7 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr int THREADS = 128, WARPS = THREADS / 32;
 
 struct ResidualParams {
   const void *x, *y;
@@ -26,29 +27,39 @@ struct ResidualParams {
   long long x_row, y_row, x_out_row, h_row, mod_seq;
   const float *after_weight, *weight, *bias;
   const void *gate, *scale, *shift;
-  int rows, features, seq_rows, after, norm, y_f32, h_f32, mod_f32, wide;      // wide: warps of a row
+  int rows, features, seq_rows, after, norm, h_f32, mod_f32, wide;     // wide: warps of a row
   float factor, eps, inv;
 };
 
 struct Eight {
   float v[8];
 };
-__device__ __forceinline__ Eight open(const uint4& r) {
-  Eight e;
-  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+template <bool F32> struct Raw;
+template <> struct Raw<false> {
+  uint4 a;
+  __device__ __forceinline__ static Raw load(const void* p, long long at) { return {*reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(p) + at)}; }
+  __device__ __forceinline__ static Raw zero() { return {make_uint4(0, 0, 0, 0)}; }
+  __device__ __forceinline__ Eight open() const {
+    Eight e;
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    e.v[2 * i] = f.x; e.v[2 * i + 1] = f.y;
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      e.v[2 * i] = f.x; e.v[2 * i + 1] = f.y;
+    }
+    return e;
   }
-  return e;
-}
-__device__ __forceinline__ Eight load8(const void* p, long long at, bool f32) {
-  if (!f32) return open(*reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(p) + at));
-  const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + at);
-  const float4 a = q[0], b = q[1];
-  return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-}
+};
+template <> struct Raw<true> {
+  float4 a, b;
+  __device__ __forceinline__ static Raw load(const void* p, long long at) {
+    const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + at);
+    return {q[0], q[1]};
+  }
+  __device__ __forceinline__ static Raw zero() { return {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}; }
+  __device__ __forceinline__ Eight open() const { return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}}; }
+};
+__device__ __forceinline__ Eight load8(const void* p, long long at, bool f32) { return f32 ? Raw<true>::load(p, at).open() : Raw<false>::load(p, at).open(); }
 __device__ __forceinline__ void store8(void* p, long long at, bool f32, const Eight& e) {
   if (f32) {
     float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + at);
@@ -82,35 +93,38 @@ __device__ __forceinline__ float row_sum(float a, int wide, float (&part)[2][WAR
   return a;
 }
 
-template <int N>
-__device__ __forceinline__ void normed(Eight (&v)[N], const bool (&live)[N], int kind, const ResidualParams& p, float (&part)[2][WARPS], int& turn) {
+// Mean and 1 / deviation of a row (0 and 1 without a norm): (v - mean) * rstd.  get(j): the j-th eight entries, zeros where the lane has none.
+struct Moments {
+  float mean, rstd;
+};
+template <int N, typename Get>
+__device__ __forceinline__ Moments moments(const Get& get, const bool (&live)[N], int kind, const ResidualParams& p, float (&part)[2][WARPS], int& turn) {
+  Moments m{0.f, 1.f};
   if (kind == LQ_NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+    for (int j = 0; j < N; ++j) {
+      const Eight e = get(j);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += v[j].v[i];
-    const float m = row_sum(s, p.wide, part, turn) * p.inv;
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j].v[i] = live[j] ? v[j].v[i] - m : 0.f;
+      for (int i = 0; i < 8; ++i) s += e.v[i];
+    }
+    m.mean = row_sum(s, p.wide, part, turn) * p.inv;
   }
   if (kind != LQ_NORM_NONE) {
     float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+    for (int j = 0; j < N; ++j) {
+      const Eight e = get(j);
+      const float off = live[j] ? m.mean : 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s = fmaf(v[j].v[i], v[j].v[i], s);
-    const float r = rsqrtf(fmaf(row_sum(s, p.wide, part, turn), p.inv, p.eps));
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j].v[i] *= r;
+      for (int i = 0; i < 8; ++i) s = fmaf(e.v[i] - off, e.v[i] - off, s);
+    }
+    m.rstd = rsqrtf(fmaf(row_sum(s, p.wide, part, turn), p.inv, p.eps));
   }
+  return m;
 }
 
-template <bool F32, int N>
+template <bool XF32, bool YF32, int N>
 __global__ void __launch_bounds__(THREADS) lq_residual_kernel(const __grid_constant__ ResidualParams p) {
   __shared__ float part[2][WARPS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = WARPS / p.wide, first = (warp % p.wide) * 32 + lane;
@@ -122,80 +136,87 @@ __global__ void __launch_bounds__(THREADS) lq_residual_kernel(const __grid_const
     const long long row = (long long)g * per + warp / p.wide;
     const bool real = row < p.rows;
     bool live[N];
-    Eight x[N], y[N];
-    long long at[N];
+    Raw<XF32> rx[N];
+    Raw<YF32> ry[N];
+    const auto at = [&](int j) { return 8 * (first + 32 * p.wide * j); };
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      at[j] = 8ll * (first + 32 * p.wide * j);
-      live[j] = real && at[j] < p.features;
-      x[j] = y[j] = Eight{};
+      live[j] = real && at(j) < p.features;
+      rx[j] = Raw<XF32>::zero();
+      ry[j] = Raw<YF32>::zero();
       if (live[j]) {
-        x[j] = load8(p.x, row * p.x_row + at[j], F32);
-        if (p.y) y[j] = load8(p.y, row * p.y_row + at[j], p.y_f32);
+        rx[j] = Raw<XF32>::load(p.x, row * p.x_row + at(j));
+        if (p.y) ry[j] = Raw<YF32>::load(p.y, row * p.y_row + at(j));
       }
     }
     const long long mod = real ? row / p.seq_rows * p.mod_seq : 0;
-    if (p.y) {
-      normed(y, live, p.after, p, part, turn);
+    Eight x[N];
+    const Moments my = p.y ? moments<N>([&](int j) { return ry[j].open(); }, live, p.after, p, part, turn) : Moments{0.f, 1.f};
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (!live[j]) continue;
+    for (int j = 0; j < N; ++j) {
+      x[j] = rx[j].open();
+      if (!live[j]) continue;
+      if (p.y) {
+        Eight y = ry[j].open();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y.v[i] = (y.v[i] - my.mean) * my.rstd;
         if (p.after_weight) {
-          const Eight w = load8(p.after_weight, at[j], true);
+          const Eight w = load8(p.after_weight, at(j), true);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[j].v[i] *= w.v[i];
+          for (int i = 0; i < 8; ++i) y.v[i] *= w.v[i];
         }
         if (p.gate) {
-          const Eight w = load8(p.gate, mod + at[j], p.mod_f32);
+          const Eight w = load8(p.gate, mod + at(j), p.mod_f32);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[j].v[i] *= w.v[i];
+          for (int i = 0; i < 8; ++i) y.v[i] *= w.v[i];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[j].v[i] = fmaf(p.factor, y[j].v[i], x[j].v[i]);
+        for (int i = 0; i < 8; ++i) x[j].v[i] = fmaf(p.factor, y.v[i], x[j].v[i]);
       }
+      if (p.x_out) store8(p.x_out, row * p.x_out_row + at(j), XF32, x[j]);
     }
-    if (p.x_out)
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (live[j]) store8(p.x_out, row * p.x_out_row + at[j], F32, x[j]);
     if (!p.h) continue;
-    normed(x, live, p.norm, p, part, turn);
+    const Moments mx = moments<N>([&](int j) { return x[j]; }, live, p.norm, p, part, turn);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       if (!live[j]) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[j].v[i] = (x[j].v[i] - mx.mean) * mx.rstd;
       if (p.weight) {
-        const Eight w = load8(p.weight, at[j], true);
+        const Eight w = load8(p.weight, at(j), true);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[j].v[i] *= w.v[i];
       }
       if (p.bias) {
-        const Eight w = load8(p.bias, at[j], true);
+        const Eight w = load8(p.bias, at(j), true);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[j].v[i] += w.v[i];
       }
       if (p.scale) {
-        const Eight w = load8(p.scale, mod + at[j], p.mod_f32);
+        const Eight w = load8(p.scale, mod + at(j), p.mod_f32);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[j].v[i] = fmaf(x[j].v[i], w.v[i], x[j].v[i]);
       }
       if (p.shift) {
-        const Eight w = load8(p.shift, mod + at[j], p.mod_f32);
+        const Eight w = load8(p.shift, mod + at(j), p.mod_f32);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[j].v[i] += w.v[i];
       }
-      store8(p.h, row * p.h_row + at[j], p.h_f32, x[j]);
+      store8(p.h, row * p.h_row + at(j), p.h_f32, x[j]);
     }
   }
 }
 
-template <bool F32>
+// eights a lane holds: these, and what lies between takes the next
+template <bool XF32, bool YF32>
 cudaError_t launch_held(const ResidualParams& p, int held, int blocks, cudaStream_t st) {
-  switch (held) {
-    case 1: return lq_launch(lq_residual_kernel<F32, 1>, blocks, THREADS, 0, st, p);
-    case 2: return lq_launch(lq_residual_kernel<F32, 2>, blocks, THREADS, 0, st, p);
-    case 3: return lq_launch(lq_residual_kernel<F32, 3>, blocks, THREADS, 0, st, p);
-    default: return lq_launch(lq_residual_kernel<F32, 4>, blocks, THREADS, 0, st, p);
-  }
+  const auto launch = [&](auto* kernel) { return lq_launch(kernel, blocks, THREADS, 0, st, p); };
+  return held == 1   ? launch(lq_residual_kernel<XF32, YF32, 1>)
+         : held == 2 ? launch(lq_residual_kernel<XF32, YF32, 2>)
+         : held == 3 ? launch(lq_residual_kernel<XF32, YF32, 3>)
+         : held <= 5 ? launch(lq_residual_kernel<XF32, YF32, 5>)
+         : held <= 7 ? launch(lq_residual_kernel<XF32, YF32, 7>)
+                     : launch(lq_residual_kernel<XF32, YF32, 9>);
 }
 
 }  // namespace
@@ -255,18 +276,21 @@ extern "C" lq_status lq_residual_norm(const lq_residual* r, void* stream) {
   if (s == LQ_OK && n_out == 2) s = status(lq_runs_meet(out[0], out[1]));
   if (s != LQ_OK) return s;
   ResidualParams p = {r->x, r->y, r->x_out, r->h, r->x_row, r->y_row, r->x_out_row, r->h_row, r->sequences == 1 ? 0 : r->mod_seq, r->after_weight, r->weight,
-                      r->bias, r->gate, r->scale, r->shift, r->rows, r->features, r->rows / r->sequences, r->after, r->norm, r->y_dtype == LQ_OUT_F32,
+                      r->bias, r->gate, r->scale, r->shift, r->rows, r->features, r->rows / r->sequences, r->after, r->norm,
                       r->h_dtype == LQ_OUT_F32, r->mod_dtype == LQ_OUT_F32, 1, r->factor, r->eps, 1.f / (float)r->features};
   int ndev = 0;
   if (lq_note_cuda(cudaGetDeviceCount(&ndev)) != cudaSuccess || r->device < 0 || r->device >= ndev) return LQ_ERR_CUDA;
   LqDeviceGuard guard(r->device);
   if (!guard.ok) return LQ_ERR_CUDA;
-  // the fewest warps that hold a row with four times eight entries a lane
+  int sms = 0;
+  if (lq_note_cuda(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, r->device)) != cudaSuccess) return LQ_ERR_CUDA;
+  // The fewest warps that hold a row; with rows too few to give every SM eight warps more of them, for then a row's own time is what counts.
   const int chunks = r->features / 8;
-  while (32 * p.wide * 4 < chunks) p.wide *= 2;
-  const int held = lq_ceil_div(chunks, 32 * p.wide), groups = lq_ceil_div(r->rows, WARPS / p.wide);
-  const bool f32 = r->x_dtype == LQ_OUT_F32;
-  const int blocks = std::min(groups, 148 * 16);
-  const cudaError_t e = f32 ? launch_held<true>(p, held, blocks, (cudaStream_t)stream) : launch_held<false>(p, held, blocks, (cudaStream_t)stream);
+  while (32 * p.wide * 9 < chunks || (p.wide < WARPS && 32 * p.wide < chunks && (long long)r->rows * p.wide < 8ll * sms)) p.wide *= 2;
+  const int held = lq_ceil_div(chunks, 32 * p.wide), groups = lq_ceil_div(r->rows, WARPS / p.wide), blocks = std::min(groups, sms * 32);
+  const bool xf = r->x_dtype == LQ_OUT_F32, yf = r->y && r->y_dtype == LQ_OUT_F32;
+  cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = xf ? (yf ? launch_held<true, true>(p, held, blocks, st) : launch_held<true, false>(p, held, blocks, st))
+                           : (yf ? launch_held<false, true>(p, held, blocks, st) : launch_held<false, false>(p, held, blocks, st));
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
