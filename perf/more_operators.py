@@ -438,7 +438,7 @@ def _own_norm(L, s, stream):
     ptr = lambda t: None if t is None else t.data_ptr()                                      # noqa: E731
     mod = [None] * 3 if s["mod"] is None else [s["mod"][:, i].data_ptr() for i in range(3)]
     r = L.lq_residual(case["M"], case["C"], s["x"].data_ptr(), s["x_out"].data_ptr(), s["h"].data_ptr(), y_ptr=s["y"].data_ptr(),
-                      sequences=case["B"], after=kind[case["after"]], after_weight_ptr=ptr(s["w_after"]), factor=s["factor"],
+                      sequences=case["B"], after=kind[case["after"]], after_weight_ptr=None if case["after"] == "none" else ptr(s["w_after"]), factor=s["factor"],
                       gate_ptr=mod[2], norm=kind[case["norm"]], weight_ptr=ptr(s["w"]), shift_ptr=mod[0], scale_ptr=mod[1],
                       mod_seq=6 * case["C"], eps=_EPS, x_dtype=code[case["fx"]], y_dtype=code[case["fy"]], h_dtype=code[case["fh"]],
                       mod_dtype=L.OUT_F16)
