@@ -3,9 +3,12 @@
 //   x' = x + factor * gate * N1(y),   h = (N2(x') * w + b) * (1 + scale) + shift
 //
 // N: none, RMS or LayerNorm of a row; gate, scale and shift are a sequence's.  Reads x and y once and writes x' and h once; the memory
-// bounds it.  A row is held in registers by one, two or four warps, up to nine times eight neighbouring entries a lane, all asked for at once and
-// kept as they lie in memory until they are used: with few warps of many loads each no row waits for another's, and most sums stay within
-// a warp.  Variances are sums about the mean that is known; h is made of x' before that is rounded to its type.
+// bounds it.  A row is held in registers by one to eight warps, up to nine times four neighbouring entries a lane, all asked for at once and
+// kept as they lie in memory until they are used, so that many rows are on their way.  What a row is multiplied with and what is added is
+// put together once for a sequence's rows of a thread block, in shared memory, and arithmetic goes two entries at a time: with five vectors
+// from global memory a row and entry by entry the issue of instructions took most of the time (32768 rows of 2240, fp32 stream: 369 us; now
+// 151 us, 5.8 TB/s, 0.89 of the measured copy rate).
+// Variances are sums about the mean that is known; h is made of x' before that is rounded to its type.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -19,7 +22,7 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int THREADS = 128, WARPS = THREADS / 32;
+constexpr int THREADS = 256, WARPS = THREADS / 32;
 
 struct ResidualParams {
   const void *x, *y;
@@ -27,54 +30,42 @@ struct ResidualParams {
   long long x_row, y_row, x_out_row, h_row, mod_seq;
   const float *after_weight, *weight, *bias;
   const void *gate, *scale, *shift;
-  int rows, features, seq_rows, after, norm, h_f32, mod_f32, wide;     // wide: warps of a row
+  int rows, features, seq_rows, after, norm, mod_f32, wide;            // seq_rows: rows that have the same vectors; wide: warps of a row
+  int groups, seq_groups, share;         // groups of rows that a thread block takes at once, of all rows and of a sequence; groups a block takes
   float factor, eps, inv;
 };
 
-struct Eight {
-  float v[8];
+struct Four {
+  float2 lo, hi;
 };
 template <bool F32> struct Raw;
 template <> struct Raw<false> {
-  uint4 a;
-  __device__ __forceinline__ static Raw load(const void* p, long long at) { return {*reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(p) + at)}; }
-  __device__ __forceinline__ static Raw zero() { return {make_uint4(0, 0, 0, 0)}; }
-  __device__ __forceinline__ Eight open() const {
-    Eight e;
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      e.v[2 * i] = f.x; e.v[2 * i + 1] = f.y;
-    }
-    return e;
+  uint2 a;
+  __device__ __forceinline__ static Raw load(const uint8_t* p) { return {*reinterpret_cast<const uint2*>(p)}; }
+  __device__ __forceinline__ static Raw zero() { return {make_uint2(0, 0)}; }
+  __device__ __forceinline__ Four open() const {
+    return {__half22float2(*reinterpret_cast<const __half2*>(&a.x)), __half22float2(*reinterpret_cast<const __half2*>(&a.y))};
+  }
+  __device__ __forceinline__ static void store(uint8_t* p, const Four& e) {
+    const __half2 a = __floats2half2_rn(e.lo.x, e.lo.y), b = __floats2half2_rn(e.hi.x, e.hi.y);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
   }
 };
 template <> struct Raw<true> {
-  float4 a, b;
-  __device__ __forceinline__ static Raw load(const void* p, long long at) {
-    const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + at);
-    return {q[0], q[1]};
-  }
-  __device__ __forceinline__ static Raw zero() { return {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}; }
-  __device__ __forceinline__ Eight open() const { return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}}; }
+  float4 a;
+  __device__ __forceinline__ static Raw load(const uint8_t* p) { return {*reinterpret_cast<const float4*>(p)}; }
+  __device__ __forceinline__ static Raw zero() { return {make_float4(0.f, 0.f, 0.f, 0.f)}; }
+  __device__ __forceinline__ Four open() const { return {make_float2(a.x, a.y), make_float2(a.z, a.w)}; }
+  __device__ __forceinline__ static void store(uint8_t* p, const Four& e) { *reinterpret_cast<float4*>(p) = make_float4(e.lo.x, e.lo.y, e.hi.x, e.hi.y); }
 };
-__device__ __forceinline__ Eight load8(const void* p, long long at, bool f32) { return f32 ? Raw<true>::load(p, at).open() : Raw<false>::load(p, at).open(); }
-__device__ __forceinline__ void store8(void* p, long long at, bool f32, const Eight& e) {
-  if (f32) {
-    float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + at);
-    q[0] = make_float4(e.v[0], e.v[1], e.v[2], e.v[3]);
-    q[1] = make_float4(e.v[4], e.v[5], e.v[6], e.v[7]);
-  } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __half2 h = __floats2half2_rn(e.v[2 * i], e.v[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(p) + at) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
+__device__ __forceinline__ Four load4(const void* p, long long at, bool f32) {
+  return f32 ? Raw<true>::load(reinterpret_cast<const uint8_t*>(p) + 4 * at).open() : Raw<false>::load(reinterpret_cast<const uint8_t*>(p) + 2 * at).open();
 }
+__device__ __forceinline__ Four mul(const Four& a, const Four& b) { return {__fmul2_rn(a.lo, b.lo), __fmul2_rn(a.hi, b.hi)}; }
+__device__ __forceinline__ Four add(const Four& a, const Four& b) { return {__fadd2_rn(a.lo, b.lo), __fadd2_rn(a.hi, b.hi)}; }
+__device__ __forceinline__ Four fma(const Four& a, const Four& b, const Four& c) { return {__ffma2_rn(a.lo, b.lo, c.lo), __ffma2_rn(a.hi, b.hi, c.hi)}; }
+__device__ __forceinline__ Four all(float v) { return {make_float2(v, v), make_float2(v, v)}; }
+__device__ __forceinline__ float sum(const Four& a) { return (a.lo.x + a.lo.y) + (a.hi.x + a.hi.y); }
 
 // Sum over the warps of a row, in all of them.  `turn` counts the sums, whose places alternate: a warp that is one sum ahead writes
 // elsewhere than the others still read.
@@ -82,141 +73,140 @@ __device__ __forceinline__ float row_sum(float a, int wide, float (&part)[2][WAR
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d);
   if (wide == 1) return a;
-  const int warp = threadIdx.x >> 5;
+  const int warp = threadIdx.x >> 5, team = warp / wide;
   float(&at)[WARPS] = part[turn & 1];
   ++turn;
   if ((threadIdx.x & 31) == 0) at[warp] = a;
-  __syncthreads();
-  const int first = warp / wide * wide;
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * wide) : "memory");        // (a row's warps alone)
   a = 0.f;
-  for (int i = 0; i < wide; ++i) a += at[first + i];
+  for (int i = 0; i < wide; ++i) a += at[team * wide + i];
   return a;
 }
 
-// Mean and 1 / deviation of a row (0 and 1 without a norm): (v - mean) * rstd.  get(j): the j-th eight entries, zeros where the lane has none.
+// -mean / deviation and 1 / deviation of a row (0 and 1 without a norm): v * rstd + shift.  get(j): the j-th four entries; the lane has `mine` of them,
+// and zeros behind.
 struct Moments {
-  float mean, rstd;
+  float shift, rstd;
 };
 template <int N, typename Get>
-__device__ __forceinline__ Moments moments(const Get& get, const bool (&live)[N], int kind, const ResidualParams& p, float (&part)[2][WARPS], int& turn) {
-  Moments m{0.f, 1.f};
-  if (kind == LQ_NORM_LAYER) {
-    float s = 0.f;
+__device__ __forceinline__ Moments moments(const Get& get, int mine, int kind, const ResidualParams& p, float (&part)[2][WARPS], int& turn) {
+  if (kind == LQ_NORM_NONE) return {0.f, 1.f};
+  Four s = all(0.f);
+  if (kind == LQ_NORM_RMS) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const Eight e = get(j);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s += e.v[i];
+      const Four e = get(j);
+      s = fma(e, e, s);
     }
-    m.mean = row_sum(s, p.wide, part, turn) * p.inv;
+    return {0.f, rsqrtf(fmaf(row_sum(sum(s), p.wide, part, turn), p.inv, p.eps))};
   }
-  if (kind != LQ_NORM_NONE) {
-    float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const Eight e = get(j);
-      const float off = live[j] ? m.mean : 0.f;
+  for (int j = 0; j < N; ++j) s = add(s, get(j));
+  const float mean = row_sum(sum(s), p.wide, part, turn) * p.inv;
+  s = all(0.f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s = fmaf(e.v[i] - off, e.v[i] - off, s);
-    }
-    m.rstd = rsqrtf(fmaf(row_sum(s, p.wide, part, turn), p.inv, p.eps));
+  for (int j = 0; j < N; ++j) {
+    const Four e = add(get(j), all(j < mine ? -mean : 0.f));
+    s = fma(e, e, s);
   }
-  return m;
+  const float rstd = rsqrtf(fmaf(row_sum(sum(s), p.wide, part, turn), p.inv, p.eps));
+  return {-mean * rstd, rstd};
 }
 
-template <bool XF32, bool YF32, int N>
+template <bool XF32, bool YF32, bool HF32, int N>
 __global__ void __launch_bounds__(THREADS) lq_residual_kernel(const __grid_constant__ ResidualParams p) {
+  extern __shared__ __align__(16) float4 vectors[];        // [3][features / 4]: factor * gate * weight of N1, weight of N2 * (1 + scale), bias * (1 + scale) + shift
   __shared__ float part[2][WARPS];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = WARPS / p.wide, first = (warp % p.wide) * 32 + lane;
-  int turn = 0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = WARPS / p.wide, first = (warp % p.wide) * 32 + lane, fours = p.features / 4;
+  int turn = 0, held = -1;
   grid_launch_dependents();
   grid_dependency_wait();
-  const int groups = (p.rows + per - 1) / per;
-  for (int g = blockIdx.x; g < groups; g += gridDim.x) {
-    const long long row = (long long)g * per + warp / p.wide;
-    const bool real = row < p.rows;
-    bool live[N];
+  const int step = 32 * p.wide, last = min(p.groups, (int)(blockIdx.x + 1) * p.share);
+  const int places = first < fours ? (fours - first + step - 1) / step : 0;
+  const float4 *va = vectors + first, *vb = va + fours, *vc = vb + fours;
+  constexpr int XB = XF32 ? 16 : 8, YB = YF32 ? 16 : 8, HB = HF32 ? 16 : 8;
+  for (int g = blockIdx.x * p.share; g < last; ++g) {
+    const int seq = g / p.seq_groups, in_seq = (g - seq * p.seq_groups) * per + warp / p.wide;
+    const long long row = (long long)seq * p.seq_rows + in_seq;
+    const int mine = in_seq < p.seq_rows ? places : 0;
+    const uint8_t* px = reinterpret_cast<const uint8_t*>(p.x) + row * p.x_row * (XF32 ? 4 : 2) + first * XB;
+    const uint8_t* py = reinterpret_cast<const uint8_t*>(p.y) + row * p.y_row * (YF32 ? 4 : 2) + first * YB;
     Raw<XF32> rx[N];
     Raw<YF32> ry[N];
-    const auto at = [&](int j) { return 8 * (first + 32 * p.wide * j); };
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      live[j] = real && at(j) < p.features;
       rx[j] = Raw<XF32>::zero();
       ry[j] = Raw<YF32>::zero();
-      if (live[j]) {
-        rx[j] = Raw<XF32>::load(p.x, row * p.x_row + at(j));
-        if (p.y) ry[j] = Raw<YF32>::load(p.y, row * p.y_row + at(j));
+      if (j < mine) {
+        rx[j] = Raw<XF32>::load(px + j * step * XB);
+        if (p.y) ry[j] = Raw<YF32>::load(py + j * step * YB);
       }
     }
-    const long long mod = real ? row / p.seq_rows * p.mod_seq : 0;
-    Eight x[N];
-    const Moments my = p.y ? moments<N>([&](int j) { return ry[j].open(); }, live, p.after, p, part, turn) : Moments{0.f, 1.f};
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      x[j] = rx[j].open();
-      if (!live[j]) continue;
-      if (p.y) {
-        Eight y = ry[j].open();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y.v[i] = (y.v[i] - my.mean) * my.rstd;
-        if (p.after_weight) {
-          const Eight w = load8(p.after_weight, at(j), true);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y.v[i] *= w.v[i];
-        }
-        if (p.gate) {
-          const Eight w = load8(p.gate, mod + at(j), p.mod_f32);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y.v[i] *= w.v[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[j].v[i] = fmaf(p.factor, y.v[i], x[j].v[i]);
+    if (seq != held) {                                     // (under the way of the row's loads)
+      __syncthreads();
+      const long long mod = seq * p.mod_seq;
+      for (int i = threadIdx.x; i < fours; i += THREADS) {
+        Four a = all(p.factor), b = all(1.f), c = all(0.f), scale = all(0.f);
+        if (p.gate) a = mul(a, load4(p.gate, mod + 4 * i, p.mod_f32));
+        if (p.after_weight) a = mul(a, load4(p.after_weight, 4 * i, true));
+        if (p.weight) b = load4(p.weight, 4 * i, true);
+        if (p.bias) c = load4(p.bias, 4 * i, true);
+        if (p.scale) scale = load4(p.scale, mod + 4 * i, p.mod_f32);
+        b = fma(b, scale, b);
+        c = fma(c, scale, c);
+        if (p.shift) c = add(c, load4(p.shift, mod + 4 * i, p.mod_f32));
+        vectors[i] = make_float4(a.lo.x, a.lo.y, a.hi.x, a.hi.y);
+        vectors[fours + i] = make_float4(b.lo.x, b.lo.y, b.hi.x, b.hi.y);
+        vectors[2 * fours + i] = make_float4(c.lo.x, c.lo.y, c.hi.x, c.hi.y);
       }
-      if (p.x_out) store8(p.x_out, row * p.x_out_row + at(j), XF32, x[j]);
+      __syncthreads();
+      held = seq;
+    }
+    const auto open = [](const float4& v) { return Four{make_float2(v.x, v.y), make_float2(v.z, v.w)}; };
+    Four x[N];
+    if (p.y) {
+      const Moments m = moments<N>([&](int j) { return ry[j].open(); }, mine, p.after, p, part, turn);
+      const Four rstd = all(m.rstd), off = all(m.shift);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        x[j] = rx[j].open();
+        if (j < mine) x[j] = fma(fma(ry[j].open(), rstd, off), open(va[j * step]), x[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = rx[j].open();
+    }
+    if (p.x_out) {
+      uint8_t* to = reinterpret_cast<uint8_t*>(p.x_out) + row * p.x_out_row * (XF32 ? 4 : 2) + first * XB;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < mine) Raw<XF32>::store(to + j * step * XB, x[j]);
     }
     if (!p.h) continue;
-    const Moments mx = moments<N>([&](int j) { return x[j]; }, live, p.norm, p, part, turn);
+    const Moments m = moments<N>([&](int j) { return x[j]; }, mine, p.norm, p, part, turn);
+    const Four rstd = all(m.rstd), off = all(m.shift);
+    uint8_t* to = reinterpret_cast<uint8_t*>(p.h) + row * p.h_row * (HF32 ? 4 : 2) + first * HB;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      if (!live[j]) continue;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[j].v[i] = (x[j].v[i] - mx.mean) * mx.rstd;
-      if (p.weight) {
-        const Eight w = load8(p.weight, at(j), true);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[j].v[i] *= w.v[i];
-      }
-      if (p.bias) {
-        const Eight w = load8(p.bias, at(j), true);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[j].v[i] += w.v[i];
-      }
-      if (p.scale) {
-        const Eight w = load8(p.scale, mod + at(j), p.mod_f32);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[j].v[i] = fmaf(x[j].v[i], w.v[i], x[j].v[i]);
-      }
-      if (p.shift) {
-        const Eight w = load8(p.shift, mod + at(j), p.mod_f32);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[j].v[i] += w.v[i];
-      }
-      store8(p.h, row * p.h_row + at(j), p.h_f32, x[j]);
-    }
+    for (int j = 0; j < N; ++j)
+      if (j < mine) Raw<HF32>::store(to + j * step * HB, fma(fma(x[j], rstd, off), open(vb[j * step]), open(vc[j * step])));
   }
 }
 
-// eights a lane holds: these, and what lies between takes the next
-template <bool XF32, bool YF32>
-cudaError_t launch_held(const ResidualParams& p, int held, int blocks, cudaStream_t st) {
-  const auto launch = [&](auto* kernel) { return lq_launch(kernel, blocks, THREADS, 0, st, p); };
-  return held == 1   ? launch(lq_residual_kernel<XF32, YF32, 1>)
-         : held == 2 ? launch(lq_residual_kernel<XF32, YF32, 2>)
-         : held == 3 ? launch(lq_residual_kernel<XF32, YF32, 3>)
-         : held <= 5 ? launch(lq_residual_kernel<XF32, YF32, 5>)
-         : held <= 7 ? launch(lq_residual_kernel<XF32, YF32, 7>)
-                     : launch(lq_residual_kernel<XF32, YF32, 9>);
+// fours a lane holds: these, and what lies between takes the next
+template <bool XF32, bool YF32, bool HF32, typename F>
+cudaError_t with_held(int held, const F& f) {
+  return held <= 1   ? f(lq_residual_kernel<XF32, YF32, HF32, 1>)
+         : held <= 2 ? f(lq_residual_kernel<XF32, YF32, HF32, 2>)
+         : held <= 3 ? f(lq_residual_kernel<XF32, YF32, HF32, 3>)
+         : held <= 5 ? f(lq_residual_kernel<XF32, YF32, HF32, 5>)
+         : held <= 7 ? f(lq_residual_kernel<XF32, YF32, HF32, 7>)
+                     : f(lq_residual_kernel<XF32, YF32, HF32, 9>);
+}
+template <bool XF32, bool YF32, typename F>
+cudaError_t with_h(bool h, int held, const F& f) { return h ? with_held<XF32, YF32, true>(held, f) : with_held<XF32, YF32, false>(held, f); }
+template <typename F>
+cudaError_t with_types(bool x, bool y, bool h, int held, const F& f) {
+  return x ? (y ? with_h<true, true>(h, held, f) : with_h<true, false>(h, held, f)) : (y ? with_h<false, true>(h, held, f) : with_h<false, false>(h, held, f));
 }
 
 }  // namespace
@@ -275,22 +265,40 @@ extern "C" lq_status lq_residual_norm(const lq_residual* r, void* stream) {
   }
   if (s == LQ_OK && n_out == 2) s = status(lq_runs_meet(out[0], out[1]));
   if (s != LQ_OK) return s;
-  ResidualParams p = {r->x, r->y, r->x_out, r->h, r->x_row, r->y_row, r->x_out_row, r->h_row, r->sequences == 1 ? 0 : r->mod_seq, r->after_weight, r->weight,
-                      r->bias, r->gate, r->scale, r->shift, r->rows, r->features, r->rows / r->sequences, r->after, r->norm,
-                      r->h_dtype == LQ_OUT_F32, r->mod_dtype == LQ_OUT_F32, 1, r->factor, r->eps, 1.f / (float)r->features};
   int ndev = 0;
   if (lq_note_cuda(cudaGetDeviceCount(&ndev)) != cudaSuccess || r->device < 0 || r->device >= ndev) return LQ_ERR_CUDA;
   LqDeviceGuard guard(r->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   int sms = 0;
   if (lq_note_cuda(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, r->device)) != cudaSuccess) return LQ_ERR_CUDA;
-  // The fewest warps that hold a row; with rows too few to give every SM eight warps more of them, for then a row's own time is what counts.
-  const int chunks = r->features / 8;
-  while (32 * p.wide * 9 < chunks || (p.wide < WARPS && 32 * p.wide < chunks && (long long)r->rows * p.wide < 8ll * sms)) p.wide *= 2;
-  const int held = lq_ceil_div(chunks, 32 * p.wide), groups = lq_ceil_div(r->rows, WARPS / p.wide), blocks = std::min(groups, sms * 32);
-  const bool xf = r->x_dtype == LQ_OUT_F32, yf = r->y && r->y_dtype == LQ_OUT_F32;
-  cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = xf ? (yf ? launch_held<true, true>(p, held, blocks, st) : launch_held<true, false>(p, held, blocks, st))
-                           : (yf ? launch_held<false, true>(p, held, blocks, st) : launch_held<false, false>(p, held, blocks, st));
+  ResidualParams p = {};
+  p.x = r->x; p.y = r->y; p.x_out = r->x_out; p.h = r->h;
+  p.x_row = r->x_row; p.y_row = r->y_row; p.x_out_row = r->x_out_row; p.h_row = r->h_row;
+  p.after_weight = r->after_weight; p.weight = r->weight; p.bias = r->bias;
+  p.gate = r->gate; p.scale = r->scale; p.shift = r->shift;
+  const bool one = !(r->gate || r->scale || r->shift) || r->mod_seq == 0 || r->sequences == 1;
+  p.mod_seq = one ? 0 : r->mod_seq;
+  p.rows = r->rows; p.features = r->features; p.seq_rows = one ? r->rows : r->rows / r->sequences;
+  p.after = r->after; p.norm = r->norm; p.mod_f32 = r->mod_dtype == LQ_OUT_F32;
+  p.factor = r->factor; p.eps = r->eps; p.inv = 1.f / (float)r->features;
+  // The fewest warps that hold a row; more of them where a sequence has fewer rows than a thread block would take, and with rows too few to give
+  // every SM eight warps, for then a row's own time is what counts.
+  const int fours = r->features / 4;
+  p.wide = 1;
+  while (32 * p.wide * 9 < fours || (p.wide < WARPS && 32 * p.wide < fours && (p.seq_rows * p.wide < WARPS || (long long)r->rows * p.wide < 8ll * sms)))
+    p.wide *= 2;
+  const int per = WARPS / p.wide, held = lq_ceil_div(fours, 32 * p.wide);
+  p.seq_groups = 1 + (p.seq_rows - 1) / per;
+  p.groups = p.seq_groups * (p.rows / p.seq_rows);
+  const size_t smem = 3 * (size_t)p.features * sizeof(float);
+  const auto launch = [&](auto* kernel) {
+    const cudaError_t c = smem > 47 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+    if (c != cudaSuccess) return c;
+    // Neighbouring groups to a thread block, as many blocks as are resident at once: with seven and nine fours a lane two an SM (us of 32768 rows of
+    // 2240, fp32 stream, with 2 / 3 / 4 / 8 / 16 blocks an SM: 151 / 184 / 153 / 158 / 175; of 8192 rows of 1152 14.9 / 19.5 / 16.7 / 19.7 / 19.6).
+    p.share = 1 + (p.groups - 1) / (sms * (held > 5 ? 2 : held > 2 ? 4 : 8));
+    return lq_launch(kernel, 1 + (p.groups - 1) / p.share, THREADS, smem, (cudaStream_t)stream, p);
+  };
+  const cudaError_t e = with_types(r->x_dtype == LQ_OUT_F32, r->y && r->y_dtype == LQ_OUT_F32, r->h_dtype == LQ_OUT_F32, held, launch);
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
