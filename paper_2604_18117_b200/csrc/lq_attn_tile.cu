@@ -3,10 +3,10 @@
 //
 //   S = Q K^T,   P = 2^(S c - m c),   O += P V,   l += P 1        over 128 tokens (four records) at a time, m a maximum of the row so far
 //
-// What bounds it is the tensor cores and what feeds them.  Four warps open the records to halves in shared memory (two buffers of K and V, in
+// What bounds it is the tensor cores and what feeds them.  Seven warps open the records to halves in shared memory (two buffers of K and V, in
 // the core matrices of K-major operands; with the pads below no two lanes of a store meet in a bank); one thread issues the products; two
-// groups of four warps have 128 rows each, a row a thread, and take turns with the tensor cores: while one forms P of its rows, the products
-// of the other run.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
+// groups of eight warps have 128 rows each, a row two threads, and take turns with the tensor cores: while one forms P of its rows, the products
+// of the other run; O's product begins with the half of P that is there.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
 // there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are up to 2^8,
 // which halves and sums hold as well, and the last division takes care of it.
 #include <math.h>
@@ -18,8 +18,11 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int TILE = 128, KV = 128, SOFT_WARPS = 8, OPEN_WARPS = 4, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 512;
-constexpr int SOFT_REGS = 176, LEAN_REGS = 80;             // of a thread: 8 * 176 + 8 * 80 = 16 * 128, as the block is launched
+constexpr int TILE = 128, KV = 128, SOFT_WARPS = 16, OPEN_WARPS = 7, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 32 * (MMA_WARP + 1);
+// Registers of a thread: as the block is launched (the kernel's bound, and what ptxas reports), and of the first kind and the openers after setmaxnreg,
+// which takes from what the block was launched with and would wait for ever for more.
+constexpr int LAUNCH_REGS = 80, SOFT_REGS = 88, LEAN_REGS = 64;
+static_assert(SOFT_WARPS * SOFT_REGS + (OPEN_WARPS + 1) * LEAN_REGS <= THREADS / 32 * LAUNCH_REGS && THREADS % 128 == 0 && THREADS * LAUNCH_REGS <= 65536, "");
 constexpr int TMEM_COLS = 512;
 constexpr uint32_t COL_S = 0, COL_O = 256;                 // of the first 128 rows; the other's are 128 columns on
 constexpr float GROWTH = 8.f;
@@ -29,16 +32,25 @@ constexpr float GROWTH = 8.f;
 __host__ __device__ constexpr int q_bytes(int Dp) { return (Dp + 63) / 64 * TILE * 128; }
 __host__ __device__ constexpr int k_bytes(int Dp) { return (Dp + 63) / 64 * KV * 128; }
 __host__ __device__ constexpr int v_bytes(int Dp) { return KV / 64 * Dp * 128; }
-// one record of every opening warp: head and keys, and values
-__host__ __device__ constexpr int raw_bytes(int Dp) { return LQ_KV_HEAD + 2 * LQ_KV_BLOCK * Dp; }
+// the keys or the values of a record, behind its head, for every opening warp
+__host__ __device__ constexpr int raw_bytes(int Dp) { return LQ_KV_HEAD + LQ_KV_BLOCK * Dp; }
+
+// What a block works on.
+struct Task {
+  LqSeq q;
+  LqSeen seen;
+  int s, head, row0, rows, tiles;        // rows: of up to 256; tiles: of 128 tokens
+};
 
 struct Control {
-  uint64_t raw_k[OPEN_WARPS], raw_v[OPEN_WARPS], q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t raw[OPEN_WARPS], q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2][2], o_full[2];
   uint32_t tmem;
   alignas(4) uint8_t missing[4][4];                 // of the last tiles: whether record i is no page's
   int abort_flag;
   int place[2];
+  Task task;
   int prefix[THREADS / 32];
+  float tops[2][2][TILE];                // [half of the block's rows][half of the tokens][row]: what two warps of the same rows tell each other
 };
 
 __device__ __forceinline__ void tmem_ld_32(uint32_t taddr, uint32_t (&v)[32]) {
@@ -80,15 +92,7 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 }
 __device__ __forceinline__ void sts_v2(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
 
-// What a block works on.
-struct Task {
-  LqSeq q;
-  LqSeen seen;
-  int s, head, row0, rows, tiles;        // rows: of up to 256; tiles: of 128 tokens
-};
-
-// Which of the 32 tokens from `first` on the row at place `at` sees, and whether all rows at places lo .. hi see all of the four blocks from the
-// b-th on.
+// Which of the 32 tokens from `first` on the row at place `at` sees.
 __device__ __forceinline__ uint32_t below(int n) { return (uint32_t)((1ull << max(0, min(32, n))) - 1); }
 __device__ __forceinline__ uint32_t seen_of(const LqAttnParams& p, int at, int first, int len) {
   const int end = p.causal ? at + 1 : len;
@@ -96,17 +100,17 @@ __device__ __forceinline__ uint32_t seen_of(const LqAttnParams& p, int at, int f
   if (p.window > 0) m &= ~below(at - p.window + 1 - first) | below(p.sinks - first);
   return m;
 }
-__device__ __forceinline__ bool seen_whole(const LqAttnParams& p, const Task& k, int lo, int hi, int b) {
-  bool all = true;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int first = k.seen.block(b + i) * LQ_KV_BLOCK;
-    all = all && lq_all_seen(p, lo, hi, first, first + LQ_KV_BLOCK - 1, k.q.len);
-  }
-  return all;
+// Of a tile's list of blocks the run that rows at places lo .. hi see as a whole (but for blocks of first tokens, which count as seen in part).
+__device__ __forceinline__ int2 seen_whole(const LqAttnParams& p, const LqSeen& seen, int lo, int hi, int len) {
+  if (!p.causal) return make_int2(0, len / LQ_KV_BLOCK);
+  const int behind = (lo + 1) / LQ_KV_BLOCK - seen.from + seen.sink;
+  if (p.window == 0) return make_int2(0, behind);
+  const int first = max(0, hi - p.window + 1 + LQ_KV_BLOCK - 1) / LQ_KV_BLOCK;
+  return make_int2(max(seen.sink, first - seen.from + seen.sink), behind);
 }
+
 template <int NK>
-__global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_constant__ LqAttnParams p) {
+__global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_constant__ LqAttnParams p) {
   constexpr int DP = 16 * NK;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* sq = smem;                                      // [2]
@@ -117,19 +121,17 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&c.q_full[i]), 4);
-      mbar_init(smem_u32(&c.k_full[i]), OPEN_WARPS);
-      mbar_init(smem_u32(&c.v_full[i]), OPEN_WARPS);
+      mbar_init(smem_u32(&c.q_full[i]), 8);
+      mbar_init(smem_u32(&c.k_full[i]), 4);
+      mbar_init(smem_u32(&c.v_full[i]), 4);
       mbar_init(smem_u32(&c.k_empty[i]), 1);
       mbar_init(smem_u32(&c.v_empty[i]), 1);
       mbar_init(smem_u32(&c.s_full[i]), 1);
-      mbar_init(smem_u32(&c.p_full[i]), 4);
+      mbar_init(smem_u32(&c.p_full[i][0]), 8);
+      mbar_init(smem_u32(&c.p_full[i][1]), 8);
       mbar_init(smem_u32(&c.o_full[i]), 1);
     }
-    for (int i = 0; i < OPEN_WARPS; ++i) {
-      mbar_init(smem_u32(&c.raw_k[i]), 1);
-      mbar_init(smem_u32(&c.raw_v[i]), 1);
-    }
+    for (int i = 0; i < OPEN_WARPS; ++i) mbar_init(smem_u32(&c.raw[i]), 1);
     c.abort_flag = 0;
     mbar_init_fence();
   }
@@ -192,7 +194,9 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
   } else {
     k.rows = 0; k.tiles = 0;
   }
-  const int halves = k.rows > TILE ? 2 : 1;
+  const int halves = k.rows > TILE ? 2 : 1, tiles = k.tiles;
+  if (tid == 0) c.task = k;                                // (for code that has no registers for it)
+  __syncthreads();
   bool good = true;
   const auto wait = [&](uint64_t& bar, int phase, int role) {
     // (without a call: the warps' registers are not those that the block was launched with)
@@ -202,21 +206,35 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
 
   if (warp < SOFT_WARPS) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
-    const int half = warp / 4, row = (warp & 3) * 32 + lane;
+    // Two warps for the same 32 rows: one has the first 64 tokens of a tile, the other the rest; of O's columns half each.
+    const int half = warp / 8, part = warp / 4 & 1, row = (warp & 3) * 32 + lane;
     if (half < halves && k.rows > 0) {
-      const int r = k.row0 + half * TILE + row, all_rows = k.q.n * p.group;
-      const bool real = r < all_rows;
-      const int tok = min(r, all_rows - 1) / p.group, at = base + tok;
-      const long long qh = k.head * p.group + (min(r, all_rows - 1) - tok * p.group);
-      const int r_lo = k.row0 + half * TILE + (warp & 3) * 32;
-      const int lo = base + min(r_lo, all_rows - 1) / p.group, hi = base + min(r_lo + 31, all_rows - 1) / p.group;
-      // the row of Q, with the sign of the scale; 16-byte columns, a row's neighbours beside it
+      const volatile Task& task = c.task;
+      const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + half * 4 + (warp & 3)) : "memory"); };
+      // the row: of the sequence's rows, behind which the last one stands in
+      const auto row_of = [&](int i, int& tok) {
+        const int r = min(task.row0 + half * TILE + i, task.q.n * p.group - 1);
+        tok = r / p.group;
+        return task.head * p.group + (r - tok * p.group);  // the query head
+      };
+      int2 whole;
       {
-        const uint4* from = reinterpret_cast<const uint4*>(p.q + (k.q.row + tok) * p.q_row + qh * p.q_head);
+        int lo, hi;
+        row_of((warp & 3) * 32, lo);
+        row_of((warp & 3) * 32 + 31, hi);
+        whole = seen_whole(p, k.seen, base + lo, base + hi, k.q.len);
+      }
+      // the row of Q, with the sign of the scale: every other 16 bytes by either warp
+      {
+        int tok;
+        const long long head = row_of(row, tok);
+        const bool real = k.row0 + half * TILE + row < k.q.n * p.group;
+        const uint4* from = reinterpret_cast<const uint4*>(p.q + (k.q.row + tok) * p.q_row + head * p.q_head);
         const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
         const uint32_t to = smem_u32(sq + half * q_bytes(DP)) + row * 128;
 #pragma unroll
-        for (int g = 0; g < DP / 8; ++g) {
+        for (int x = 0; x < DP / 16; ++x) {
+          const int g = 2 * x + part;
           uint4 v = make_uint4(0, 0, 0, 0);
           if (real && 8 * g < p.D) {
             v = from[g];
@@ -229,44 +247,53 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
         if (lane == 0) mbar_arrive(smem_u32(&c.q_full[half]));
       }
       const float scale = fmaxf(fabsf(p.scale), 1e-30f);   // (a scale of zero: all weights are one, and what is covered stays -inf)
-      const uint32_t lanes = (uint32_t)(warp & 3) << 21, ts = tmem + lanes + COL_S + half * 128, to = tmem + lanes + COL_O + half * 128;
-      float m = -INFINITY, l = 0.f;                        // m: what the weights are below, times scale
-      for (int j = 0; j < k.tiles; ++j) {
-        if (!wait(c.s_full[half], j, LQ_STAGE_DRAIN)) break;
+      const uint32_t ts = tmem + ((uint32_t)(warp & 3) << 21) + COL_S + half * 128, to = ts + COL_O - COL_S;
+      float m = -INFINITY, l = 0.f;                        // m: what the weights are below, times scale; l: of the warp's tokens
+      for (int j = 0; j < tiles; ++j) {
+        if (!wait(c.s_full[half], j, LQ_STAGE_DRAIN)) {    // (given up: the other warp of the rows meets this one all the same)
+          meet();
+          continue;
+        }
         tc_fence_after();
-        const uint32_t missing = *reinterpret_cast<volatile uint32_t*>(c.missing[j & 3]);
-        // which tokens of the tile's four blocks the row sees; most tiles are seen by all rows as a whole
-        const bool whole = missing == 0 && 4 * j + 3 < k.seen.count() && seen_whole(p, k, lo, hi, 4 * j);
-        if (!whole) {                                      // (S is written anew with what no row sees at -inf)
+        const uint32_t ss = ts + 64 * part;
+        const uint32_t missing = *reinterpret_cast<volatile uint32_t*>(c.missing[j & 3]) >> (16 * part);
+        // (most tiles are seen by all rows as a whole)
+        if ((missing & 0xFFFF) != 0 || 4 * j + 2 * part < whole.x || 4 * j + 2 * part + 1 >= whole.y) {       // S is written anew with what no row sees at -inf
+          int tok;
+          row_of(row, tok);
+          const LqSeen seen{task.seen.sink, task.seen.from, task.seen.to};
+          const int len = task.q.len, at = len - task.q.n + tok;
 #pragma unroll 1
           for (int i = 0; i < 4; ++i) {
-            const uint32_t mask = 4 * j + i < k.seen.count() && !(missing >> (8 * i) & 1) ? seen_of(p, at, k.seen.block(4 * j + i) * LQ_KV_BLOCK, k.q.len) : 0;
-#pragma unroll 1
-            for (int x = 0; x < 32; x += 16) {
-              uint32_t u[16];
-              tmem_ld_32x16(ts + 32 * i + x, u);
-              tmem_ld_wait();
+            const int b = 4 * j + 2 * part + (i >> 1);
+            const uint32_t mask = (b < seen.count() && !(missing >> (8 * (i >> 1)) & 1) ? seen_of(p, at, seen.block(b) * LQ_KV_BLOCK, len) : 0) >> (16 * (i & 1));
+            uint32_t u[16];
+            tmem_ld_32x16(ss + 16 * i, u);
+            tmem_ld_wait();
 #pragma unroll
-              for (int y = 0; y < 16; ++y)
-                if (!(mask >> (x + y) & 1)) u[y] = 0xff800000u;
-              tmem_st_16(ts + 32 * i + x, u);
-            }
+            for (int y = 0; y < 16; ++y)
+              if (!(mask >> y & 1)) u[y] = 0xff800000u;
+            tmem_st_16(ss + 16 * i, u);
           }
           tmem_st_wait();
         }
-        uint32_t v[4][32];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld_32(ts + 32 * i, v[i]);
+        uint32_t v[2][32];
+        tmem_ld_32(ss, v[0]);
+        tmem_ld_32(ss + 32, v[1]);
         tmem_ld_wait();
-        float tops[4];
+        float top = -INFINITY;
+        {
+          float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          tops[i] = -INFINITY;
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int x = 0; x < 32; x += 2) tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(v[i][x])), __uint_as_float(v[i][x + 1]));
+            for (int x = 0; x < 32; x += 2) t[x / 2 & 3] = fmaxf(fmaxf(t[x / 2 & 3], __uint_as_float(v[i][x])), __uint_as_float(v[i][x + 1]));
+          top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
         }
-        float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-        top *= scale;
+        // (behind the meeting both have read S, and P may take its place; the next S comes when both have written P, and so read this)
+        c.tops[half][part][row] = top;
+        meet();
+        top = scale * fmaxf(top, c.tops[half][part ^ 1][row]);
         const bool grow = top > m + GROWTH || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, grow)) {
           // (a row that has seen nothing yet has sums of zero; its factor is one)
@@ -274,20 +301,20 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
           if (grow) { l *= by; m = top; }
           if (j > 0 && __any_sync(0xffffffffu, by != 1.f))
 #pragma unroll 1
-            for (int x = 0; x < DP; x += 16) {
-              uint32_t v[16];
-              tmem_ld_32x16(to + x, v);
+            for (int x = 16 * part; x < DP; x += 32) {
+              uint32_t u[16];
+              tmem_ld_32x16(to + x, u);
               tmem_ld_wait();
 #pragma unroll
-              for (int y = 0; y < 16; ++y) v[y] = __float_as_uint(__uint_as_float(v[y]) * by);
-              tmem_st_16(to + x, v);
+              for (int y = 0; y < 16; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * by);
+              tmem_st_16(to + x, u);
             }
         }
         const float ref = m > -INFINITY ? -m : 0.f;
         const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(ref, ref);
         float2 sum[2] = {make_float2(l, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2; ++i) {
           uint32_t w[16];
 #pragma unroll
           for (int x = 0; x < 32; x += 2) {
@@ -296,23 +323,30 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
             sum[x / 2 & 1] = __fadd2_rn(sum[x / 2 & 1], e);
             w[x / 2] = pack(e.x, e.y);
           }
-          tmem_st_16(ts + 16 * i, w);                      // (over columns of S, which has been read)
+          tmem_st_16(ts + 32 * part + 16 * i, w);          // (over columns of S, which has been read)
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&c.p_full[half][i]));
         }
         l = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&c.p_full[half]));
       }
+      meet();
+      c.tops[half][part][row] = l;
+      meet();
+      l += c.tops[half][part ^ 1][row];
       // values were opened as 2^-4 of themselves
       const float by = l > 0.f ? 16.f / l : 0.f;
-      __half* out = p.out + (k.q.row + tok) * p.out_row + qh * p.out_head;
-      if (k.tiles > 0 && wait(c.o_full[half], 0, LQ_STAGE_DRAIN)) tc_fence_after();
+      int tok;
+      const long long head = row_of(row, tok);
+      const bool real = task.row0 + half * TILE + row < task.q.n * p.group;
+      __half* out = p.out + (task.q.row + tok) * p.out_row + head * p.out_head;
+      if (tiles > 0 && wait(c.o_full[half], 0, LQ_STAGE_DRAIN)) tc_fence_after();
       if (good)
 #pragma unroll 1
-        for (int x = 0; x < DP; x += 16) {
+        for (int x = 16 * part; x < DP; x += 32) {
           uint32_t v[16] = {};
-          if (k.tiles > 0) {
+          if (tiles > 0) {
             tmem_ld_32x16(to + x, v);
             tmem_ld_wait();
           }
@@ -324,173 +358,156 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
         }
       tc_fence_before();
     }
-  } else if (warp < MMA_WARP) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LEAN_REGS));
-    // Warp w opens record w of every tile.  Its keys (with the record's head) and its values are copied to the warp's own place in shared memory;
-    // the next record's are asked for as soon as these are in registers.
-    const int w = warp - SOFT_WARPS, c8 = lane >> 2, t = lane & 3, count = k.tiles > 0 ? k.seen.count() : 0;
-    uint8_t* place = raw + w * raw_bytes(DP);
-    const uint32_t bar_k = smem_u32(&c.raw_k[w]), bar_v = smem_u32(&c.raw_v[w]);
-    const auto find = [&](int j) -> const uint8_t* {       // the record of tile j, null: behind the last or no page's
-      const int b = 4 * j + w;
-      if (j >= k.tiles || b >= count) return nullptr;
-      const long long x = lq_kv_at(p.b, k.s, k.seen.block(b));
-      if (x < 0 && lane == 0) lq_kv_refuse(p.status);
-      return x < 0 ? nullptr : p.records + (x + k.head) * p.b.record;
-    };
-    const auto fetch_k = [&](const uint8_t* rec) {
-      if (rec && lane == 0) {
-        mbar_expect_tx(bar_k, LQ_KV_HEAD + LQ_KV_BLOCK * DP);
-        bulk_load(smem_u32(place), rec, LQ_KV_HEAD + LQ_KV_BLOCK * DP, bar_k);
-      }
-    };
-    const auto fetch_v = [&](const uint8_t* rec) {
-      if (rec && lane == 0) {
-        mbar_expect_tx(bar_v, LQ_KV_BLOCK * DP);
-        bulk_load(smem_u32(place) + LQ_KV_HEAD + LQ_KV_BLOCK * DP, rec + LQ_KV_HEAD + LQ_KV_BLOCK * DP, LQ_KV_BLOCK * DP, bar_v);
-      }
-    };
-    const uint8_t *now = find(0), *next = find(1);
-    fetch_k(now);
-    fetch_v(now);
-    int asked_k = now ? 1 : 0, asked_v = asked_k, had = 0;  // copies asked for, records that have been opened
-    // Keys: rows are tokens; the lane's word i is 8 bytes of row 32 w + lq_kv_token(c8, i).  Values: rows are entries, words 2 s + i are 8 bytes of row
-    // 16 g + 2 c8 + i.  In a half of the warp's lanes these 8 bytes take all banks once.
-    uint32_t kto[4], vto[2][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) kto[i] = smem_u32(sk) + (32 * w + lq_kv_token(c8, i)) * 128 + (t & 1) * 8;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int chunk = (4 * w + 2 * s + (t >> 1)) & 7, r = 2 * c8 + i;
-        vto[s][i] = smem_u32(sv) + w / 2 * DP * 128 + r * 128 + ((chunk ^ (r & 7)) * 16) + (t & 1) * 8;
-      }
-    const int kx = 2 * (c8 & 1) + 4 * (c8 >> 1 & 1);       // (token & 7 but for its lowest bit, i & 1)
-    for (int j = 0; j < k.tiles; ++j) {
-      const int st = j & 1;
-      const uint8_t* after = find(j + 2);
-      uint32_t head = 0;
-      uint4 u[NK];
-      if (now && good) {
-        if (!wait(c.raw_k[w], had, LQ_STAGE_PRODUCER)) break;
-        head = *reinterpret_cast<const volatile uint32_t*>(place);
-#pragma unroll
-        for (int g = 0; g < NK; ++g) u[g] = lds_v4(smem_u32(place) + LQ_KV_HEAD + 512 * g + 16 * lane);
-      }
-      fence_proxy_async();                                 // (a copy into the place of the keys comes behind the loads of all lanes; without this it
-      __syncwarp();                                        // has overtaken some)
-      fetch_k(next);
-      asked_k += next ? 1 : 0;
-      if (j >= 2 && !wait(c.k_empty[st], (j >> 1) - 1, LQ_STAGE_PRODUCER)) break;
-      {
-        const uint32_t high = lq_kv_high((int8_t)(head & 0xFF));
-        const __half2 less = lq_kv_less(high);
-        if (lane == 0) c.missing[j & 3][w] = !now;
-#pragma unroll
-        for (int g = 0; g < NK; ++g) {
-          const uint32_t ww[4] = {u[g].x, u[g].y, u[g].z, u[g].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t a = kto[i] + st * k_bytes(DP) + g / 4 * KV * 128 + ((((2 * g & 7) + (t >> 1)) ^ (kx + (i & 1))) * 16);
-            if (now) sts_v2(a, lq_kv_open<0x4140>(ww[i], high, less), lq_kv_open<0x4342>(ww[i], high, less));
-            else sts_v2(a, 0, 0);
-          }
-        }
-      }
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&c.k_full[st]));
-      if (now) {
-        if (!wait(c.raw_v[w], had, LQ_STAGE_PRODUCER)) break;
-#pragma unroll
-        for (int g = 0; g < NK; ++g) u[g] = lds_v4(smem_u32(place) + LQ_KV_HEAD + LQ_KV_BLOCK * DP + 512 * g + 16 * lane);
-        ++had;
-      }
-      fence_proxy_async();
-      __syncwarp();
-      fetch_v(next);
-      asked_v += next ? 1 : 0;
-      if (j >= 2 && !wait(c.v_empty[st], (j >> 1) - 1, LQ_STAGE_PRODUCER)) break;
-      {
-        const uint32_t high = lq_kv_high((int8_t)(head >> 8 & 0xFF));
-        const __half2 less = lq_kv_less(high);
-#pragma unroll
-        for (int g = 0; g < NK; ++g) {
-          const uint32_t ww[4] = {u[g].x, u[g].y, u[g].z, u[g].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t a = vto[i >> 1][i & 1] + st * v_bytes(DP) + g * 2048;
-            if (now) sts_v2(a, lq_kv_open<0x4140>(ww[i], high, less), lq_kv_open<0x4342>(ww[i], high, less));
-            else sts_v2(a, 0, 0);
-          }
-        }
-      }
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&c.v_full[st]));
-      now = next;
-      next = after;
-    }
-    if (!good) {                                           // a wait gave up: what is in flight lands before the block leaves
-      if (asked_k > had) mbar_settle(bar_k, (asked_k - 1) & 1);
-      if (asked_v > had) mbar_settle(bar_v, (asked_v - 1) & 1);
-    }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(LEAN_REGS));
-  }
-  if (warp == MMA_WARP && k.tiles > 0) {
-    const uint32_t idesc_s = IDESC_F16 | idesc_shape(KV), idesc_o = IDESC_F16 | idesc_shape(DP);
-    const auto product_s = [&](int half, int st) {         // by one thread
-      const uint32_t a = smem_u32(sq + half * q_bytes(DP)), b = smem_u32(sk + st * k_bytes(DP));
+    if (warp < MMA_WARP) {
+      // A tile's eight jobs, the keys of its four records and then the values, go round the seven warps.  What a job opens, with the record's head,
+      // is copied to the warp's own place in shared memory; that of its next job is asked for as soon as this has been loaded.
+      const int ow = warp - SOFT_WARPS, c8 = lane >> 2, t = lane & 3, count = tiles > 0 ? k.seen.count() : 0;
+      const uint32_t place = smem_u32(raw + ow * raw_bytes(DP)), bar = smem_u32(&c.raw[ow]);
+      const auto find = [&](int n) -> const uint8_t* {       // the record of job n, null: behind the last or no page's
+        const int b = 4 * (n >> 3) + (n & 3);
+        if (n >= 8 * tiles || b >= count) return nullptr;
+        const long long x = lq_kv_at(p.b, k.s, k.seen.block(b));
+        if (x < 0 && lane == 0) lq_kv_refuse(p.status);
+        return x < 0 ? nullptr : p.records + (x + k.head) * p.b.record;
+      };
+      const auto fetch = [&](int n, const uint8_t* rec) {
+        if (rec && lane == 0) {
+          mbar_expect_tx(bar, LQ_KV_HEAD + LQ_KV_BLOCK * DP);
+          if ((n & 4) == 0) {
+            bulk_load(place, rec, LQ_KV_HEAD + LQ_KV_BLOCK * DP, bar);
+          } else {
+            bulk_load(place, rec, LQ_KV_HEAD, bar);
+            bulk_load(place + LQ_KV_HEAD, rec + LQ_KV_HEAD + LQ_KV_BLOCK * DP, LQ_KV_BLOCK * DP, bar);
+          }
+        }
+      };
+      const uint8_t *now = find(ow), *next = find(ow + OPEN_WARPS);
+      fetch(ow, now);
+      int asked = now ? 1 : 0, had = 0;                      // copies that were asked for, that have come
+      for (int n = ow; n < 8 * tiles; n += OPEN_WARPS) {
+        const int j = n >> 3, st = j & 1, side = n >> 2 & 1, w = n & 3;
+        const uint8_t* after = find(n + 2 * OPEN_WARPS);
+        // Where the lane's words go in the stage, 8 bytes each; in a half of the warp's lanes these take all banks once.  Keys: rows are tokens, word i
+        // is part of row 32 w + lq_kv_token(c8, i).  Values: rows are entries, words 2 s + i are part of row 16 g + 2 c8 + i.
+        uint32_t to[4];
+        if (side == 0) {
 #pragma unroll
-      for (int x = 0; x < NK; ++x)
-        tc_mma<TC_F16>(tmem + COL_S + half * 128, make_smem_desc(a + x / 4 * TILE * 128 + x % 4 * 32), make_smem_desc(b + x / 4 * KV * 128 + x % 4 * 32), idesc_s,
-                       x > 0);
-    };
-    const auto product_o = [&](int half, int st, bool add) {
-      const uint32_t b = smem_u32(sv + st * v_bytes(DP));
+          for (int i = 0; i < 4; ++i) to[i] = smem_u32(sk) + st * k_bytes(DP) + (32 * w + lq_kv_token(c8, i)) * 128 + (t & 1) * 8;
+        } else {
 #pragma unroll
-      for (int x = 0; x < KV / 16; ++x)
-        tc_mma_ta(tmem + COL_O + half * 128, tmem + COL_S + half * 128 + 8 * x, make_smem_desc(b + x / 4 * DP * 128 + x % 4 * 32), idesc_o, add || x > 0);
-    };
-    wait(c.k_full[0], 0, LQ_STAGE_MMA);
-    for (int half = 0; half < halves; ++half) {
-      if (!wait(c.q_full[half], 0, LQ_STAGE_MMA)) break;
-      tc_fence_after();
-      if (elect_one()) {
-        product_s(half, 0);
-        tc_commit(smem_u32(&c.s_full[half]));
-        if (half == halves - 1) tc_commit(smem_u32(&c.k_empty[0]));
+          for (int i = 0; i < 4; ++i) {
+            const int chunk = (4 * w + 2 * (i >> 1) + (t >> 1)) & 7, r = 2 * c8 + (i & 1);
+            to[i] = smem_u32(sv) + st * v_bytes(DP) + w / 2 * DP * 128 + r * 128 + ((chunk ^ (r & 7)) * 16) + (t & 1) * 8;
+          }
+        }
+        uint32_t head = 0;
+        if (now) {
+          if (!wait(c.raw[ow], had, LQ_STAGE_PRODUCER)) break;
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(head) : "r"(place) : "memory");
+          ++had;
+        }
+        if (j >= 2 && !wait(side == 0 ? c.k_empty[st] : c.v_empty[st], (j >> 1) - 1, LQ_STAGE_PRODUCER)) break;
+        if (side == 0 && lane == 0) c.missing[j & 3][w] = !now;
+        const uint32_t high = lq_kv_high((int8_t)(head >> (8 * side) & 0xFF));
+        const __half2 less = lq_kv_less(high);
+        constexpr int BATCH = (NK + 1) / 2;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          uint4 u[BATCH];
+          if (now)
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x)
+              if (b * BATCH + x < NK) u[x] = lds_v4(place + LQ_KV_HEAD + 512 * (b * BATCH + x) + 16 * lane);
+          if (b == 1) {
+            fence_proxy_async();                             // (a copy into the place comes behind the loads of all lanes; without this it has
+            __syncwarp();                                    // overtaken some)
+            fetch(n + OPEN_WARPS, next);
+            asked += next ? 1 : 0;
+          }
+#pragma unroll
+          for (int x = 0; x < BATCH; ++x) {
+            const int g = b * BATCH + x;
+            if (g >= NK) continue;
+            const uint32_t ww[4] = {u[x].x, u[x].y, u[x].z, u[x].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int row = lq_kv_token(c8, i) & 7;        // (32 w is a multiple of eight)
+              const uint32_t a = to[i] + (side == 0 ? g / 4 * KV * 128 + ((((2 * g & 7) + (t >> 1)) ^ row) * 16) : g * 2048);
+              if (now) sts_v2(a, lq_kv_open<0x4140>(ww[i], high, less), lq_kv_open<0x4342>(ww[i], high, less));
+              else sts_v2(a, 0, 0);
+            }
+          }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(side == 0 ? &c.k_full[st] : &c.v_full[st]));
+        now = next;
+        next = after;
       }
-      __syncwarp();
-    }
-    for (int j = 0; j < k.tiles && good; ++j) {
-      const int st = j & 1, next = st ^ 1;
-      const bool last = j == k.tiles - 1;
+      // (a wait gave up: what is in flight lands before the block leaves)
+      if (!good && asked > had) mbar_settle(bar, (asked - 1) & 1);
+    } else if (tiles > 0) {
+      const uint32_t idesc_s = IDESC_F16 | idesc_shape(KV), idesc_o = IDESC_F16 | idesc_shape(DP);
+      const auto product_s = [&](int half, int st) {         // by one thread
+        const uint32_t a = smem_u32(sq + half * q_bytes(DP)), b = smem_u32(sk + st * k_bytes(DP));
+#pragma unroll
+        for (int x = 0; x < NK; ++x)
+          tc_mma<TC_F16>(tmem + COL_S + half * 128, make_smem_desc(a + x / 4 * TILE * 128 + x % 4 * 32), make_smem_desc(b + x / 4 * KV * 128 + x % 4 * 32), idesc_s,
+                         x > 0);
+      };
+      // tokens 32 piece .. 32 piece + 31 and 64 more: those of which either warp of a row's has written its first or second half
+      const auto product_o = [&](int half, int st, int piece, bool add) {
+        const uint32_t b = smem_u32(sv + st * v_bytes(DP));
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int x = 2 * piece + (y & 1) + 4 * (y >> 1);
+          tc_mma_ta(tmem + COL_O + half * 128, tmem + COL_S + half * 128 + 8 * x, make_smem_desc(b + x / 4 * DP * 128 + x % 4 * 32), idesc_o, add || y > 0);
+        }
+      };
+      wait(c.k_full[0], 0, LQ_STAGE_MMA);
       for (int half = 0; half < halves; ++half) {
-        if (half == 0 && !wait(c.v_full[st], j >> 1, LQ_STAGE_MMA)) break;
-        if (!wait(c.p_full[half], j, LQ_STAGE_MMA)) break;
-        if (half == 0 && !last && !wait(c.k_full[next], (j + 1) >> 1, LQ_STAGE_MMA)) break;
+        if (!wait(c.q_full[half], 0, LQ_STAGE_MMA)) break;
         tc_fence_after();
         if (elect_one()) {
-          product_o(half, st, j > 0);
-          if (half == halves - 1) tc_commit(smem_u32(&c.v_empty[st]));
-          if (last) {
-            tc_commit(smem_u32(&c.o_full[half]));
-          } else {
-            product_s(half, next);
-            tc_commit(smem_u32(&c.s_full[half]));
-            if (half == halves - 1) tc_commit(smem_u32(&c.k_empty[next]));
-          }
+          product_s(half, 0);
+          tc_commit(smem_u32(&c.s_full[half]));
+          if (half == halves - 1) tc_commit(smem_u32(&c.k_empty[0]));
         }
         __syncwarp();
       }
-    }
-    if (!good) {                                           // a wait gave up: what has been issued gets a bounded time to end
-      if (elect_one()) tc_commit(smem_u32(&c.q_full[0]));
-      __syncwarp();
-      mbar_settle(smem_u32(&c.o_full[0]), 0);
+      for (int j = 0; j < k.tiles && good; ++j) {
+        const int st = j & 1, next = st ^ 1;
+        const bool last = j == k.tiles - 1;
+        for (int half = 0; half < halves; ++half) {
+          if (half == 0 && !wait(c.v_full[st], j >> 1, LQ_STAGE_MMA)) break;
+          if (half == 0 && !last && !wait(c.k_full[next], (j + 1) >> 1, LQ_STAGE_MMA)) break;
+          if (!wait(c.p_full[half][0], j, LQ_STAGE_MMA)) break;
+          tc_fence_after();
+          if (elect_one()) product_o(half, st, 0, j > 0);
+          __syncwarp();
+          if (!wait(c.p_full[half][1], j, LQ_STAGE_MMA)) break;
+          tc_fence_after();
+          if (elect_one()) {
+            product_o(half, st, 1, true);
+            if (half == halves - 1) tc_commit(smem_u32(&c.v_empty[st]));
+            if (last) {
+              tc_commit(smem_u32(&c.o_full[half]));
+            } else {
+              product_s(half, next);
+              tc_commit(smem_u32(&c.s_full[half]));
+              if (half == halves - 1) tc_commit(smem_u32(&c.k_empty[next]));
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if (!good) {                                           // a wait gave up: what has been issued gets a bounded time to end
+        if (elect_one()) tc_commit(smem_u32(&c.q_full[0]));
+        __syncwarp();
+        mbar_settle(smem_u32(&c.o_full[0]), 0);
+      }
     }
   }
   __syncthreads();
@@ -500,7 +517,9 @@ __global__ void __launch_bounds__(THREADS, 1) lq_attn_tile_kernel(const __grid_c
   }
 }
 
-size_t tile_smem(int Dp) { return 2 * (size_t)(q_bytes(Dp) + k_bytes(Dp) + v_bytes(Dp)) + OPEN_WARPS * raw_bytes(Dp) + sizeof(Control); }
+constexpr size_t tile_smem(int Dp) { return 2 * (size_t)(q_bytes(Dp) + k_bytes(Dp) + v_bytes(Dp)) + OPEN_WARPS * raw_bytes(Dp) + sizeof(Control); }
+
+static_assert(tile_smem(128) <= 232448, "");
 
 template <typename F>
 auto with_size(int Dp, const F& f) {
