@@ -90,7 +90,100 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+// waits until all lanes have the value
+__device__ __forceinline__ void arrived(uint32_t v) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b32 r;\n\tsetp.ne.u32 p, %0, 0;\n\tvote.sync.ballot.b32 r, p, 0xffffffff;\n\t}" ::"r"(v) : "memory");
+}
 __device__ __forceinline__ void sts_v2(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
+
+// A record's keys as rows of 64 entries a panel, its 32 tokens from `to` on.  The lane's word i is 8 bytes of row lq_kv_token(c8, i); in a half of the
+// warp's lanes these 8 bytes take all banks once.  then(): all lanes' loads have come (a copy that was asked for without that has overtaken some
+// of them; a proxy fence there waits for the stores as well).
+template <int NK, typename Then>
+__device__ __forceinline__ void open_keys(uint32_t from, uint32_t to, uint32_t head, int lane, const Then& then) {
+  constexpr int BATCH = (NK + 1) / 2;
+  const int c8 = lane >> 2, t = lane & 3;
+  const uint32_t high = lq_kv_high((int8_t)(head & 0xFF));
+  const __half2 less = lq_kv_less(high);
+  uint32_t at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = lq_kv_token(c8, i);
+    at[i] = to + row * 128 + (((t >> 1) ^ (row & 7)) * 16) + (t & 1) * 8;
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    uint4 u[BATCH];
+    uint32_t any = 0;
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x)
+      if (b * BATCH + x < NK) u[x] = lds_v4(from + 512 * (b * BATCH + x) + 16 * lane);
+    if (b == 1) {
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x)
+        if (b * BATCH + x < NK) any |= u[x].w;
+      arrived(any);
+      then();
+    }
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) {
+      const int g = b * BATCH + x;
+      if (g >= NK) continue;
+      const uint32_t ww[4] = {u[x].x, u[x].y, u[x].z, u[x].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sts_v2((at[i] ^ (32 * (g & 3))) + g / 4 * KV * 128, lq_kv_open<0x4140>(ww[i], high, less), lq_kv_open<0x4342>(ww[i], high, less));
+    }
+  }
+}
+// Its values: rows are entries, 64 tokens a panel, of which the record has the lower or upper half.  Words 2 s + i are 8 bytes of row 16 g + 2 c8 + i.
+template <int NK, typename Then>
+__device__ __forceinline__ void open_values(uint32_t from, uint32_t to, uint32_t exponent, int upper, int lane, const Then& then) {
+  constexpr int BATCH = (NK + 1) / 2;
+  const int c8 = lane >> 2, t = lane & 3;
+  const uint32_t high = lq_kv_high((int8_t)(exponent & 0xFF));
+  const __half2 less = lq_kv_less(high);
+  uint32_t at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int chunk = 4 * upper + 2 * (i >> 1) + (t >> 1), row = 2 * c8 + (i & 1);
+    at[i] = to + row * 128 + ((chunk ^ (row & 7)) * 16) + (t & 1) * 8;
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    uint4 u[BATCH];
+    uint32_t any = 0;
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x)
+      if (b * BATCH + x < NK) u[x] = lds_v4(from + 512 * (b * BATCH + x) + 16 * lane);
+    if (b == 1) {
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x)
+        if (b * BATCH + x < NK) any |= u[x].w;
+      arrived(any);
+      then();
+    }
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) {
+      const int g = b * BATCH + x;
+      if (g >= NK) continue;
+      const uint32_t ww[4] = {u[x].x, u[x].y, u[x].z, u[x].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sts_v2(at[i] + g * 2048, lq_kv_open<0x4140>(ww[i], high, less), lq_kv_open<0x4342>(ww[i], high, less));
+    }
+  }
+}
+// zeros in place of record w
+__device__ __forceinline__ void zero_rows(uint32_t stage, int w, int side, int Dp, int lane) {
+  if (side == 0) {
+    for (int i = lane; i < (Dp + 63) / 64 * 256; i += 32) sts_v4(stage + i / 256 * KV * 128 + 32 * w * 128 + i % 256 * 16, make_uint4(0, 0, 0, 0));
+  } else {
+    for (int i = lane; i < Dp * 4; i += 32) {              // four of a row's eight 16-byte pieces
+      const int row = i / 4, chunk = 4 * (w & 1) + i % 4;
+      sts_v4(stage + w / 2 * Dp * 128 + row * 128 + ((chunk ^ (row & 7)) * 16), make_uint4(0, 0, 0, 0));
+    }
+  }
+}
 
 // Which of the 32 tokens from `first` on the row at place `at` sees.
 __device__ __forceinline__ uint32_t below(int n) { return (uint32_t)((1ull << max(0, min(32, n))) - 1); }
@@ -257,30 +350,25 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         tc_fence_after();
         const uint32_t ss = ts + 64 * part;
         const uint32_t missing = *reinterpret_cast<volatile uint32_t*>(c.missing[j & 3]) >> (16 * part);
-        // (most tiles are seen by all rows as a whole)
-        if ((missing & 0xFFFF) != 0 || 4 * j + 2 * part < whole.x || 4 * j + 2 * part + 1 >= whole.y) {       // S is written anew with what no row sees at -inf
-          int tok;
-          row_of(row, tok);
-          const LqSeen seen{task.seen.sink, task.seen.from, task.seen.to};
-          const int len = task.q.len, at = len - task.q.n + tok;
-#pragma unroll 1
-          for (int i = 0; i < 4; ++i) {
-            const int b = 4 * j + 2 * part + (i >> 1);
-            const uint32_t mask = (b < seen.count() && !(missing >> (8 * (i >> 1)) & 1) ? seen_of(p, at, seen.block(b) * LQ_KV_BLOCK, len) : 0) >> (16 * (i & 1));
-            uint32_t u[16];
-            tmem_ld_32x16(ss + 16 * i, u);
-            tmem_ld_wait();
-#pragma unroll
-            for (int y = 0; y < 16; ++y)
-              if (!(mask >> y & 1)) u[y] = 0xff800000u;
-            tmem_st_16(ss + 16 * i, u);
-          }
-          tmem_st_wait();
-        }
         uint32_t v[2][32];
         tmem_ld_32(ss, v[0]);
         tmem_ld_32(ss + 32, v[1]);
         tmem_ld_wait();
+        // (most tiles are seen by all rows as a whole)
+        if ((missing & 0xFFFF) != 0 || 4 * j + 2 * part < whole.x || 4 * j + 2 * part + 1 >= whole.y) {
+          int tok;
+          row_of(row, tok);
+          const LqSeen seen{task.seen.sink, task.seen.from, task.seen.to};
+          const int len = task.q.len, at = len - task.q.n + tok;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int b = 4 * j + 2 * part + i;
+            const uint32_t mask = b < seen.count() && !(missing >> (8 * i) & 1) ? seen_of(p, at, seen.block(b) * LQ_KV_BLOCK, len) : 0;
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (!(mask >> x & 1)) v[i][x] = 0xff800000u; // -inf
+          }
+        }
         float top = -INFINITY;
         {
           float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -363,12 +451,19 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
     if (warp < MMA_WARP) {
       // A tile's eight jobs, the keys of its four records and then the values, go round the seven warps.  What a job opens, with the record's head,
       // is copied to the warp's own place in shared memory; that of its next job is asked for as soon as this has been loaded.
-      const int ow = warp - SOFT_WARPS, c8 = lane >> 2, t = lane & 3, count = tiles > 0 ? k.seen.count() : 0;
+      const int ow = warp - SOFT_WARPS, count = tiles > 0 ? k.seen.count() : 0;
       const uint32_t place = smem_u32(raw + ow * raw_bytes(DP)), bar = smem_u32(&c.raw[ow]);
-      const auto find = [&](int n) -> const uint8_t* {       // the record of job n, null: behind the last or no page's
+      // the record of job n, null: behind the last or no page's.  Its page is asked for a job before.
+      int page = -1;
+      const auto ask = [&](int n) {
+        const int b = 4 * (n >> 3) + (n & 3);
+        if (n < 8 * tiles && b < count) page = p.b.pages[(long long)k.s * p.b.page_stride + lq_kv_slot(p.b, k.seen.block(b))];
+      };
+      const auto find = [&](int n) -> const uint8_t* {
         const int b = 4 * (n >> 3) + (n & 3);
         if (n >= 8 * tiles || b >= count) return nullptr;
-        const long long x = lq_kv_at(p.b, k.s, k.seen.block(b));
+        const int block = k.seen.block(b);
+        const long long x = lq_kv_at(p.b, block, lq_kv_slot(p.b, block), page);
         if (x < 0 && lane == 0) lq_kv_refuse(p.status);
         return x < 0 ? nullptr : p.records + (x + k.head) * p.b.record;
       };
@@ -383,25 +478,15 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
           }
         }
       };
-      const uint8_t *now = find(ow), *next = find(ow + OPEN_WARPS);
+      ask(ow);
+      const uint8_t* now = find(ow);
       fetch(ow, now);
+      ask(ow + OPEN_WARPS);
       int asked = now ? 1 : 0, had = 0;                      // copies that were asked for, that have come
       for (int n = ow; n < 8 * tiles; n += OPEN_WARPS) {
         const int j = n >> 3, st = j & 1, side = n >> 2 & 1, w = n & 3;
-        const uint8_t* after = find(n + 2 * OPEN_WARPS);
-        // Where the lane's words go in the stage, 8 bytes each; in a half of the warp's lanes these take all banks once.  Keys: rows are tokens, word i
-        // is part of row 32 w + lq_kv_token(c8, i).  Values: rows are entries, words 2 s + i are part of row 16 g + 2 c8 + i.
-        uint32_t to[4];
-        if (side == 0) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) to[i] = smem_u32(sk) + st * k_bytes(DP) + (32 * w + lq_kv_token(c8, i)) * 128 + (t & 1) * 8;
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int chunk = (4 * w + 2 * (i >> 1) + (t >> 1)) & 7, r = 2 * c8 + (i & 1);
-            to[i] = smem_u32(sv) + st * v_bytes(DP) + w / 2 * DP * 128 + r * 128 + ((chunk ^ (r & 7)) * 16) + (t & 1) * 8;
-          }
-        }
+        const uint8_t* next = find(n + OPEN_WARPS);
+        ask(n + 2 * OPEN_WARPS);
         uint32_t head = 0;
         if (now) {
           if (!wait(c.raw[ow], had, LQ_STAGE_PRODUCER)) break;
@@ -410,41 +495,22 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         }
         if (j >= 2 && !wait(side == 0 ? c.k_empty[st] : c.v_empty[st], (j >> 1) - 1, LQ_STAGE_PRODUCER)) break;
         if (side == 0 && lane == 0) c.missing[j & 3][w] = !now;
-        const uint32_t high = lq_kv_high((int8_t)(head >> (8 * side) & 0xFF));
-        const __half2 less = lq_kv_less(high);
-        constexpr int BATCH = (NK + 1) / 2;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          uint4 u[BATCH];
-          if (now)
-#pragma unroll
-            for (int x = 0; x < BATCH; ++x)
-              if (b * BATCH + x < NK) u[x] = lds_v4(place + LQ_KV_HEAD + 512 * (b * BATCH + x) + 16 * lane);
-          if (b == 1) {
-            fence_proxy_async();                             // (a copy into the place comes behind the loads of all lanes; without this it has
-            __syncwarp();                                    // overtaken some)
-            fetch(n + OPEN_WARPS, next);
-            asked += next ? 1 : 0;
-          }
-#pragma unroll
-          for (int x = 0; x < BATCH; ++x) {
-            const int g = b * BATCH + x;
-            if (g >= NK) continue;
-            const uint32_t ww[4] = {u[x].x, u[x].y, u[x].z, u[x].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int row = lq_kv_token(c8, i) & 7;        // (32 w is a multiple of eight)
-              const uint32_t a = to[i] + (side == 0 ? g / 4 * KV * 128 + ((((2 * g & 7) + (t >> 1)) ^ row) * 16) : g * 2048);
-              if (now) sts_v2(a, lq_kv_open<0x4140>(ww[i], high, less), lq_kv_open<0x4342>(ww[i], high, less));
-              else sts_v2(a, 0, 0);
-            }
-          }
+        const auto then = [&]() {                            // what the warp's place held is in registers
+          fetch(n + OPEN_WARPS, next);
+          asked += next ? 1 : 0;
+        };
+        if (!now) {
+          then();
+          zero_rows(smem_u32(side == 0 ? sk : sv) + st * (side == 0 ? k_bytes(DP) : v_bytes(DP)), w, side, DP, lane);
+        } else if (side == 0) {
+          open_keys<NK>(place + LQ_KV_HEAD, smem_u32(sk) + st * k_bytes(DP) + 32 * w * 128, head, lane, then);
+        } else {
+          open_values<NK>(place + LQ_KV_HEAD, smem_u32(sv) + st * v_bytes(DP) + w / 2 * DP * 128, head >> 8, w & 1, lane, then);
         }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(side == 0 ? &c.k_full[st] : &c.v_full[st]));
         now = next;
-        next = after;
       }
       // (a wait gave up: what is in flight lands before the block leaves)
       if (!good && asked > had) mbar_settle(bar, (asked - 1) & 1);
