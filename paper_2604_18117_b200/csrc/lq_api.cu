@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 #include <new>
 
@@ -418,6 +419,19 @@ int32_t* lq_device_status_ptr(int device) {
     cudaSetDevice(prev);
   }
   return g_status[device];
+}
+
+int lq_device_sms(int device) {
+  static std::atomic<int> known[64];
+  if (device < 0 || device >= 64) return 0;
+  int n = known[device].load(std::memory_order_relaxed);
+  if (n == 0) {
+    int count = 0;
+    if (lq_note_cuda(cudaGetDeviceCount(&count)) != cudaSuccess || device >= count ||
+        lq_note_cuda(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return 0;
+    known[device].store(n, std::memory_order_relaxed);
+  }
+  return n;
 }
 
 extern "C" lq_status lq_get_device_status(int device, int32_t* code, int32_t* stage) {

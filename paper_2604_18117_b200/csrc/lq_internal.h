@@ -181,6 +181,8 @@ static inline bool lq_overlap(const void* a, size_t na, const void* b, size_t nb
 
 // device status word (one per device, allocated on first use): {code, stage}
 int32_t* lq_device_status_ptr(int device);
+// multiprocessors of a device (asked for once); 0: there is none of that number
+int lq_device_sms(int device);
 
 // kernels' host launchers (defined in lq_quant.cu / lq_gemm.cu)
 lq_status lq_launch_quantize(const lq_layer* L, const void* X, int M, lq_act* A, cudaStream_t st);

@@ -265,12 +265,10 @@ extern "C" lq_status lq_residual_norm(const lq_residual* r, void* stream) {
   }
   if (s == LQ_OK && n_out == 2) s = status(lq_runs_meet(out[0], out[1]));
   if (s != LQ_OK) return s;
-  int ndev = 0;
-  if (lq_note_cuda(cudaGetDeviceCount(&ndev)) != cudaSuccess || r->device < 0 || r->device >= ndev) return LQ_ERR_CUDA;
+  const int sms = lq_device_sms(r->device);
+  if (sms == 0) return LQ_ERR_CUDA;
   LqDeviceGuard guard(r->device);
   if (!guard.ok) return LQ_ERR_CUDA;
-  int sms = 0;
-  if (lq_note_cuda(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, r->device)) != cudaSuccess) return LQ_ERR_CUDA;
   ResidualParams p = {};
   p.x = r->x; p.y = r->y; p.x_out = r->x_out; p.h = r->h;
   p.x_row = r->x_row; p.y_row = r->y_row; p.x_out_row = r->x_out_row; p.h_row = r->h_row;
