@@ -501,6 +501,7 @@ extern "C" lq_status lq_cache_attention(const lq_kvcache* C, int32_t layer, cons
   p.causal = a->causal; p.window = a->window; p.sinks = a->sinks;
   p.scale = a->scale * 16.f * 1.44269504088896341f;        // (keys are opened as 2^-4 of themselves)
   p.part = C->d_part; p.count = C->d_count;
+  p.tile_part = C->d_tile_part; p.tile_meta = C->d_tile_meta;
   p.status = lq_device_status_ptr(C->device);
   // Which form a sequence's rows are the kernels tell by themselves where sequences have different numbers of them; a form that no sequence can be is
   // not launched.

@@ -15,13 +15,16 @@ struct LqAttnParams {
   float* part;
   int* count;
   int few, many;                         // sequences whose rows * group are in [few, many) are this launch's
+  int splits;                            // form for many rows: thread blocks that share out a tile's tokens
+  float* tile_part;                      // [sms][Dp + 2][256]: what each of them leaves: sums by entry, maxima, sums of weights
+  int4* tile_meta;                       // [sms]: of a tile: parts that it has, first row in the call, its place in the sequence's rows, how many
   int32_t* status;
 };
 
 // Sequences of up to so many rows (new tokens x query heads of a group) are the form for few rows'
 constexpr int LQ_ATTN_FEW = 64;
 
-lq_status lq_attn_tile_launch(const lq_kvcache* C, const LqAttnParams& p, cudaStream_t st);
+lq_status lq_attn_tile_launch(const lq_kvcache* C, LqAttnParams p, cudaStream_t st);
 
 #ifdef __CUDACC__
 // Tokens that any of the rows at places lo .. hi of a sequence may see, as blocks of 32: the first `sink` ones and those from `from` to `to` - 1;

@@ -5,11 +5,13 @@
 //
 // What bounds it is the tensor cores and what feeds them.  Seven warps open the records to halves in shared memory (two buffers of K and V, in
 // the core matrices of K-major operands; with the pads below no two lanes of a store meet in a bank); one thread issues the products; two
-// groups of eight warps have 128 rows each, a row two threads, and take turns with the tensor cores: while one forms P of its rows, the products
-// of the other run; O's product begins with the half of P that is there.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
+// groups of four warps have 128 rows each, a row a thread, and take turns with the tensor cores: while one forms P of its rows, the products
+// of the other run, and O's product follows P 32 tokens at a time.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
 // there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are up to 2^8,
 // which halves and sums hold as well, and the last division takes care of it.
 #include <math.h>
+
+#include <algorithm>
 
 #include "lq_attn.h"
 #include "lq_device.cuh"
@@ -18,14 +20,15 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int TILE = 128, KV = 128, SOFT_WARPS = 16, OPEN_WARPS = 7, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 32 * (MMA_WARP + 1);
-// Registers of a thread: as the block is launched (the kernel's bound, and what ptxas reports), and of the first kind and the openers after setmaxnreg,
+constexpr int TILE = 128, KV = 128, SOFT_WARPS = 8, OPEN_WARPS = 7, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 32 * (MMA_WARP + 1);
+// Registers of a thread: as the block is launched (the kernel's bound, and what ptxas reports), and of the first kind and the others after setmaxnreg,
 // which takes from what the block was launched with and would wait for ever for more.
-constexpr int LAUNCH_REGS = 80, SOFT_REGS = 88, LEAN_REGS = 64;
+constexpr int LAUNCH_REGS = 128, SOFT_REGS = 176, LEAN_REGS = 80;
 static_assert(SOFT_WARPS * SOFT_REGS + (OPEN_WARPS + 1) * LEAN_REGS <= THREADS / 32 * LAUNCH_REGS && THREADS % 128 == 0 && THREADS * LAUNCH_REGS <= 65536, "");
 constexpr int TMEM_COLS = 512;
 constexpr uint32_t COL_S = 0, COL_O = 256;                 // of the first 128 rows; the other's are 128 columns on
 constexpr float GROWTH = 8.f;
+constexpr int MIN_TILES = 4;             // of 128 tokens a thread block takes at least where a tile of rows is shared out
 
 // Operands are K-major rows of 128 bytes (64 halves), 128-byte swizzle; a wider K has panel after panel.  Q and K: rows are rows and tokens, 64
 // entries a panel; V: rows are the head's entries, 64 tokens a panel.
@@ -39,18 +42,18 @@ __host__ __device__ constexpr int raw_bytes(int Dp) { return LQ_KV_HEAD + LQ_KV_
 struct Task {
   LqSeq q;
   LqSeen seen;
-  int s, head, row0, rows, tiles;        // rows: of up to 256; tiles: of 128 tokens
+  int s, head, row0, rows;               // rows: of up to 256
+  int first, tiles, parts;               // tiles of 128 tokens: from the first-th of the rows' on so many; parts: thread blocks that have some
 };
 
 struct Control {
-  uint64_t raw[OPEN_WARPS], q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2][2], o_full[2];
+  uint64_t raw[OPEN_WARPS], q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2][4], o_full[2];
   uint32_t tmem;
   alignas(4) uint8_t missing[4][4];                 // of the last tiles: whether record i is no page's
   int abort_flag;
   int place[2];
   Task task;
   int prefix[THREADS / 32];
-  float tops[2][2][TILE];                // [half of the block's rows][half of the tokens][row]: what two warps of the same rows tell each other
 };
 
 __device__ __forceinline__ void tmem_ld_32(uint32_t taddr, uint32_t (&v)[32]) {
@@ -63,6 +66,14 @@ __device__ __forceinline__ void tmem_ld_32(uint32_t taddr, uint32_t (&v)[32]) {
         "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
       : "r"(taddr)
       : "memory");
+}
+// what has been loaded is used behind this place alone
+__device__ __forceinline__ void settled(uint32_t (&v)[32]) {
+  asm volatile(""
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]),
+                 "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]),
+                 "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]));
 }
 __device__ __forceinline__ void tmem_st_16(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile(
@@ -214,14 +225,13 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&c.q_full[i]), 8);
+      mbar_init(smem_u32(&c.q_full[i]), 4);
       mbar_init(smem_u32(&c.k_full[i]), 4);
       mbar_init(smem_u32(&c.v_full[i]), 4);
       mbar_init(smem_u32(&c.k_empty[i]), 1);
       mbar_init(smem_u32(&c.v_empty[i]), 1);
       mbar_init(smem_u32(&c.s_full[i]), 1);
-      mbar_init(smem_u32(&c.p_full[i][0]), 8);
-      mbar_init(smem_u32(&c.p_full[i][1]), 8);
+      for (int x = 0; x < 4; ++x) mbar_init(smem_u32(&c.p_full[i][x]), 4);
       mbar_init(smem_u32(&c.o_full[i]), 1);
     }
     for (int i = 0; i < OPEN_WARPS; ++i) mbar_init(smem_u32(&c.raw[i]), 1);
@@ -235,14 +245,15 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
 
   // the block's sequence and tile of rows: blocks of a tile's heads follow each other, a sequence's last tiles (which see most) come first
   Task k = {};
-  k.head = blockIdx.x % p.b.heads;
-  const int unit = blockIdx.x / p.b.heads;
+  const int part = blockIdx.x % p.splits, place = blockIdx.x / p.splits;
+  k.head = place % p.b.heads;
+  const int unit = place / p.b.heads;
   if (!p.b.row_start) {
     const int each = (int)(((long long)p.b.each * p.group + 2 * TILE - 1) / (2 * TILE)), back = unit / p.b.sequences;
     k.s = unit - back * p.b.sequences;
     k.row0 = (each - 1 - back) * 2 * TILE;
     k.q = lq_seq(p.b, k.s);
-    if (!lq_attn_takes(p, k.q, blockIdx.x < p.b.heads * p.b.sequences)) k.s = -1;
+    if (!lq_attn_takes(p, k.q, place < p.b.heads * p.b.sequences)) k.s = -1;
   } else {
     const int chunk = (p.b.sequences + THREADS - 1) / THREADS;
     int sum = 0;
@@ -283,10 +294,13 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
   if (k.s >= 0) {
     k.rows = min(2 * TILE, k.q.n * p.group - k.row0);
     k.seen = lq_seen(p, base + k.row0 / p.group, base + (k.row0 + k.rows - 1) / p.group, k.q.len);
-    k.tiles = (k.seen.count() + 3) / 4;
-  } else {
-    k.rows = 0; k.tiles = 0;
+    const int all = (k.seen.count() + 3) / 4, each = max(MIN_TILES, (all + p.splits - 1) / p.splits);
+    k.parts = max(1, (all + each - 1) / each);
+    k.first = part * each;
+    k.tiles = max(0, min(each, all - k.first));
+    if (part >= k.parts) k.rows = 0;                       // (nothing is left for this block)
   }
+  if (p.splits > 1 && part == 0 && tid == 0) p.tile_meta[place] = make_int4(k.parts, k.q.row, k.row0, k.rows);
   const int halves = k.rows > TILE ? 2 : 1, tiles = k.tiles;
   if (tid == 0) c.task = k;                                // (for code that has no registers for it)
   __syncthreads();
@@ -299,11 +313,9 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
 
   if (warp < SOFT_WARPS) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
-    // Two warps for the same 32 rows: one has the first 64 tokens of a tile, the other the rest; of O's columns half each.
-    const int half = warp / 8, part = warp / 4 & 1, row = (warp & 3) * 32 + lane;
+    const int half = warp / 4, row = (warp & 3) * 32 + lane;
     if (half < halves && k.rows > 0) {
       const volatile Task& task = c.task;
-      const auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + half * 4 + (warp & 3)) : "memory"); };
       // the row: of the sequence's rows, behind which the last one stands in
       const auto row_of = [&](int i, int& tok) {
         const int r = min(task.row0 + half * TILE + i, task.q.n * p.group - 1);
@@ -316,8 +328,9 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         row_of((warp & 3) * 32, lo);
         row_of((warp & 3) * 32 + 31, hi);
         whole = seen_whole(p, k.seen, base + lo, base + hi, k.q.len);
+        whole.x -= 4 * k.first; whole.y -= 4 * k.first;    // of the block's tiles
       }
-      // the row of Q, with the sign of the scale: every other 16 bytes by either warp
+      // the row of Q, with the sign of the scale
       {
         int tok;
         const long long head = row_of(row, tok);
@@ -326,8 +339,7 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
         const uint32_t to = smem_u32(sq + half * q_bytes(DP)) + row * 128;
 #pragma unroll
-        for (int x = 0; x < DP / 16; ++x) {
-          const int g = 2 * x + part;
+        for (int g = 0; g < DP / 8; ++g) {
           uint4 v = make_uint4(0, 0, 0, 0);
           if (real && 8 * g < p.D) {
             v = from[g];
@@ -341,47 +353,58 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
       }
       const float scale = fmaxf(fabsf(p.scale), 1e-30f);   // (a scale of zero: all weights are one, and what is covered stays -inf)
       const uint32_t ts = tmem + ((uint32_t)(warp & 3) << 21) + COL_S + half * 128, to = ts + COL_O - COL_S;
-      float m = -INFINITY, l = 0.f;                        // m: what the weights are below, times scale; l: of the warp's tokens
+      float m = -INFINITY, l = 0.f;                        // m: what the weights are below, times scale
       for (int j = 0; j < tiles; ++j) {
-        if (!wait(c.s_full[half], j, LQ_STAGE_DRAIN)) {    // (given up: the other warp of the rows meets this one all the same)
-          meet();
-          continue;
-        }
+        if (!wait(c.s_full[half], j, LQ_STAGE_DRAIN)) break;
         tc_fence_after();
-        const uint32_t ss = ts + 64 * part;
-        const uint32_t missing = *reinterpret_cast<volatile uint32_t*>(c.missing[j & 3]) >> (16 * part);
-        uint32_t v[2][32];
-        tmem_ld_32(ss, v[0]);
-        tmem_ld_32(ss + 32, v[1]);
+        const uint32_t missing = *reinterpret_cast<volatile uint32_t*>(c.missing[j & 3]);
+        uint32_t v[4][32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld_32(ts + 32 * i, v[i]);
         tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) settled(v[i]);
+        // Of 32 tokens the weights, as they go to tensor memory, and their sum
+        const float2 scale2 = make_float2(scale, scale);
+        uint32_t w[16];
+        float2 sum[2];
+        const auto weigh = [&](const uint32_t (&v)[32]) {
+          const float ref = m > -INFINITY ? -m : 0.f;
+          const float2 ref2 = make_float2(ref, ref);
+          sum[0] = sum[1] = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int x = 0; x < 32; x += 2) {
+            float2 e = __ffma2_rn(make_float2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), scale2, ref2);
+            e.x = ex2(e.x); e.y = ex2(e.y);
+            sum[x / 2 & 1] = __fadd2_rn(sum[x / 2 & 1], e);
+            w[x / 2] = pack(e.x, e.y);
+          }
+        };
         // (most tiles are seen by all rows as a whole)
-        if ((missing & 0xFFFF) != 0 || 4 * j + 2 * part < whole.x || 4 * j + 2 * part + 1 >= whole.y) {
+        const bool covered = missing != 0 || 4 * j < whole.x || 4 * j + 3 >= whole.y;
+        if (covered) {
           int tok;
           row_of(row, tok);
           const LqSeen seen{task.seen.sink, task.seen.from, task.seen.to};
           const int len = task.q.len, at = len - task.q.n + tok;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int b = 4 * j + 2 * part + i;
+          for (int i = 0; i < 4; ++i) {
+            const int b = 4 * (task.first + j) + i;
             const uint32_t mask = b < seen.count() && !(missing >> (8 * i) & 1) ? seen_of(p, at, seen.block(b) * LQ_KV_BLOCK, len) : 0;
 #pragma unroll
             for (int x = 0; x < 32; ++x)
               if (!(mask >> x & 1)) v[i][x] = 0xff800000u; // -inf
           }
         }
-        float top = -INFINITY;
+        float top;
         {
           float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int x = 0; x < 32; x += 2) t[x / 2 & 3] = fmaxf(fmaxf(t[x / 2 & 3], __uint_as_float(v[i][x])), __uint_as_float(v[i][x + 1]));
-          top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+          top = scale * fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
         }
-        // (behind the meeting both have read S, and P may take its place; the next S comes when both have written P, and so read this)
-        c.tops[half][part][row] = top;
-        meet();
-        top = scale * fmaxf(top, c.tops[half][part ^ 1][row]);
         const bool grow = top > m + GROWTH || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, grow)) {
           // (a row that has seen nothing yet has sums of zero; its factor is one)
@@ -389,7 +412,7 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
           if (grow) { l *= by; m = top; }
           if (j > 0 && __any_sync(0xffffffffu, by != 1.f))
 #pragma unroll 1
-            for (int x = 16 * part; x < DP; x += 32) {
+            for (int x = 0; x < DP; x += 16) {
               uint32_t u[16];
               tmem_ld_32x16(to + x, u);
               tmem_ld_wait();
@@ -398,52 +421,53 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
               tmem_st_16(to + x, u);
             }
         }
-        const float ref = m > -INFINITY ? -m : 0.f;
-        const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(ref, ref);
-        float2 sum[2] = {make_float2(l, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t w[16];
-#pragma unroll
-          for (int x = 0; x < 32; x += 2) {
-            float2 e = __ffma2_rn(make_float2(__uint_as_float(v[i][x]), __uint_as_float(v[i][x + 1])), scale2, ref2);
-            e.x = ex2(e.x); e.y = ex2(e.y);
-            sum[x / 2 & 1] = __fadd2_rn(sum[x / 2 & 1], e);
-            w[x / 2] = pack(e.x, e.y);
-          }
-          tmem_st_16(ts + 32 * part + 16 * i, w);          // (over columns of S, which has been read)
+        for (int i = 0; i < 4; ++i) {
+          weigh(v[i]);
+          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          tmem_st_16(ts + 16 * i, w);                      // (over columns of S, which has been read)
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&c.p_full[half][i]));
         }
-        l = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
-      meet();
-      c.tops[half][part][row] = l;
-      meet();
-      l += c.tops[half][part ^ 1][row];
-      // values were opened as 2^-4 of themselves
-      const float by = l > 0.f ? 16.f / l : 0.f;
-      int tok;
-      const long long head = row_of(row, tok);
-      const bool real = task.row0 + half * TILE + row < task.q.n * p.group;
-      __half* out = p.out + (task.q.row + tok) * p.out_row + head * p.out_head;
       if (tiles > 0 && wait(c.o_full[half], 0, LQ_STAGE_DRAIN)) tc_fence_after();
-      if (good)
+      if (task.parts > 1) {                                // for lq_attn_join_kernel
+        float* out = p.tile_part + (long long)blockIdx.x * (DP + 2) * (2 * TILE) + half * TILE + row;
+        if (good)
 #pragma unroll 1
-        for (int x = 16 * part; x < DP; x += 32) {
-          uint32_t v[16] = {};
-          if (tiles > 0) {
+          for (int x = 0; x < DP; x += 16) {
+            uint32_t v[16];
             tmem_ld_32x16(to + x, v);
             tmem_ld_wait();
-          }
-          uint32_t w[8];
 #pragma unroll
-          for (int y = 0; y < 8; ++y) w[y] = pack(__uint_as_float(v[2 * y]) * by, __uint_as_float(v[2 * y + 1]) * by);
-          if (real && x < p.D) *reinterpret_cast<uint4*>(out + x) = make_uint4(w[0], w[1], w[2], w[3]);
-          if (real && x + 8 < p.D) *reinterpret_cast<uint4*>(out + x + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-        }
+            for (int y = 0; y < 16; ++y) out[(x + y) * (2 * TILE)] = __uint_as_float(v[y]);
+          }
+        out[DP * (2 * TILE)] = m;
+        out[(DP + 1) * (2 * TILE)] = l;
+      } else {
+        // values were opened as 2^-4 of themselves
+        const float by = l > 0.f ? 16.f / l : 0.f;
+        int tok;
+        const long long head = row_of(row, tok);
+        const bool real = task.row0 + half * TILE + row < task.q.n * p.group;
+        __half* out = p.out + (task.q.row + tok) * p.out_row + head * p.out_head;
+        if (good)
+#pragma unroll 1
+          for (int x = 0; x < DP; x += 16) {
+            uint32_t v[16] = {};
+            if (tiles > 0) {
+              tmem_ld_32x16(to + x, v);
+              tmem_ld_wait();
+            }
+            uint32_t w[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) w[y] = pack(__uint_as_float(v[2 * y]) * by, __uint_as_float(v[2 * y + 1]) * by);
+            if (real && x < p.D) *reinterpret_cast<uint4*>(out + x) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (real && x + 8 < p.D) *reinterpret_cast<uint4*>(out + x + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+          }
+      }
       tc_fence_before();
     }
   } else {
@@ -456,11 +480,11 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
       // the record of job n, null: behind the last or no page's.  Its page is asked for a job before.
       int page = -1;
       const auto ask = [&](int n) {
-        const int b = 4 * (n >> 3) + (n & 3);
+        const int b = 4 * (k.first + (n >> 3)) + (n & 3);
         if (n < 8 * tiles && b < count) page = p.b.pages[(long long)k.s * p.b.page_stride + lq_kv_slot(p.b, k.seen.block(b))];
       };
       const auto find = [&](int n) -> const uint8_t* {
-        const int b = 4 * (n >> 3) + (n & 3);
+        const int b = 4 * (k.first + (n >> 3)) + (n & 3);
         if (n >= 8 * tiles || b >= count) return nullptr;
         const int block = k.seen.block(b);
         const long long x = lq_kv_at(p.b, block, lq_kv_slot(p.b, block), page);
@@ -523,12 +547,11 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
           tc_mma<TC_F16>(tmem + COL_S + half * 128, make_smem_desc(a + x / 4 * TILE * 128 + x % 4 * 32), make_smem_desc(b + x / 4 * KV * 128 + x % 4 * 32), idesc_s,
                          x > 0);
       };
-      // tokens 32 piece .. 32 piece + 31 and 64 more: those of which either warp of a row's has written its first or second half
-      const auto product_o = [&](int half, int st, int piece, bool add) {
+      const auto product_o = [&](int half, int st, int piece, bool add) {          // 32 tokens
         const uint32_t b = smem_u32(sv + st * v_bytes(DP));
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const int x = 2 * piece + (y & 1) + 4 * (y >> 1);
+        for (int y = 0; y < 2; ++y) {
+          const int x = 2 * piece + y;
           tc_mma_ta(tmem + COL_O + half * 128, tmem + COL_S + half * 128 + 8 * x, make_smem_desc(b + x / 4 * DP * 128 + x % 4 * 32), idesc_o, add || y > 0);
         }
       };
@@ -549,14 +572,17 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         for (int half = 0; half < halves; ++half) {
           if (half == 0 && !wait(c.v_full[st], j >> 1, LQ_STAGE_MMA)) break;
           if (half == 0 && !last && !wait(c.k_full[next], (j + 1) >> 1, LQ_STAGE_MMA)) break;
-          if (!wait(c.p_full[half][0], j, LQ_STAGE_MMA)) break;
-          tc_fence_after();
-          if (elect_one()) product_o(half, st, 0, j > 0);
-          __syncwarp();
-          if (!wait(c.p_full[half][1], j, LQ_STAGE_MMA)) break;
+#pragma unroll
+          for (int x = 0; x < 3; ++x) {
+            if (!wait(c.p_full[half][x], j, LQ_STAGE_MMA)) break;
+            tc_fence_after();
+            if (elect_one()) product_o(half, st, x, j > 0 || x > 0);
+            __syncwarp();
+          }
+          if (!wait(c.p_full[half][3], j, LQ_STAGE_MMA)) break;
           tc_fence_after();
           if (elect_one()) {
-            product_o(half, st, 1, true);
+            product_o(half, st, 3, true);
             if (half == halves - 1) tc_commit(smem_u32(&c.v_empty[st]));
             if (last) {
               tc_commit(smem_u32(&c.o_full[half]));
@@ -583,6 +609,43 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
   }
 }
 
+// Joins the parts of tiles that were shared out: 32 rows a thread block, a row a lane, entries by warps, every load a line of 128 bytes.
+constexpr int JOIN_WARPS = 8, JOIN_ROWS = 32;
+template <int NK>
+__global__ void __launch_bounds__(32 * JOIN_WARPS) lq_attn_join_kernel(const __grid_constant__ LqAttnParams p) {
+  constexpr int DP = 16 * NK, STEP = 2 * TILE;
+  const int warp = threadIdx.x >> 5, row = blockIdx.y * JOIN_ROWS + (threadIdx.x & 31);
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int4 meta = p.tile_meta[blockIdx.x];
+  const int parts = meta.x;
+  if (parts < 2 || row >= meta.w) return;
+  const float* from = p.tile_part + (long long)blockIdx.x * p.splits * (DP + 2) * STEP + row;
+  constexpr long long PART = (DP + 2) * STEP;
+  float m = -INFINITY, l = 0.f;
+  for (int i = 0; i < parts; ++i) m = fmaxf(m, from[i * PART + DP * STEP]);
+  const float ref = m > -INFINITY ? m : 0.f;
+  float2 o[NK];
+#pragma unroll
+  for (int g = 0; g < NK; ++g) o[g] = make_float2(0.f, 0.f);
+  for (int i = 0; i < parts; ++i) {
+    const float* at = from + i * PART;
+    const float by = ex2(at[DP * STEP] - ref);
+    l = fmaf(by, at[(DP + 1) * STEP], l);
+#pragma unroll
+    for (int g = 0; g < NK; ++g) {                         // entries 16 g + 2 warp and the next
+      o[g].x = fmaf(by, at[(16 * g + 2 * warp) * STEP], o[g].x);
+      o[g].y = fmaf(by, at[(16 * g + 2 * warp + 1) * STEP], o[g].y);
+    }
+  }
+  const float by = l > 0.f ? 16.f / l : 0.f;
+  const int place = blockIdx.x % p.b.heads, r = meta.z + row, tok = r / p.group;
+  __half* out = p.out + (meta.y + tok) * p.out_row + (long long)(place * p.group + r - tok * p.group) * p.out_head;
+#pragma unroll
+  for (int g = 0; g < NK; ++g)
+    if (16 * g + 2 * warp < p.D) *reinterpret_cast<uint32_t*>(out + 16 * g + 2 * warp) = pack(o[g].x * by, o[g].y * by);
+}
+
 constexpr size_t tile_smem(int Dp) { return 2 * (size_t)(q_bytes(Dp) + k_bytes(Dp) + v_bytes(Dp)) + OPEN_WARPS * raw_bytes(Dp) + sizeof(Control); }
 
 static_assert(tile_smem(128) <= 232448, "");
@@ -590,27 +653,33 @@ static_assert(tile_smem(128) <= 232448, "");
 template <typename F>
 auto with_size(int Dp, const F& f) {
   switch (Dp) {
-    case 64: return f(lq_attn_tile_kernel<4>);
-    case 80: return f(lq_attn_tile_kernel<5>);
-    case 96: return f(lq_attn_tile_kernel<6>);
-    case 112: return f(lq_attn_tile_kernel<7>);
-    default: return f(lq_attn_tile_kernel<8>);
+    case 64: return f(lq_attn_tile_kernel<4>, lq_attn_join_kernel<4>);
+    case 80: return f(lq_attn_tile_kernel<5>, lq_attn_join_kernel<5>);
+    case 96: return f(lq_attn_tile_kernel<6>, lq_attn_join_kernel<6>);
+    case 112: return f(lq_attn_tile_kernel<7>, lq_attn_join_kernel<7>);
+    default: return f(lq_attn_tile_kernel<8>, lq_attn_join_kernel<8>);
   }
 }
 
 }  // namespace
 
 lq_status lq_attn_tile_prepare(const lq_kvcache* C) {
-  return with_size(C->Dp, [&](auto* kernel) {
+  return with_size(C->Dp, [&](auto* kernel, auto*) {
            return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tile_smem(C->Dp)));
          }) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
 
-lq_status lq_attn_tile_launch(const lq_kvcache* C, const LqAttnParams& p, cudaStream_t st) {
+lq_status lq_attn_tile_launch(const lq_kvcache* C, LqAttnParams p, cudaStream_t st) {
   // tiles of 256 rows: exactly so many where all sequences have as many rows; else at most one of each sequence is not full
-  const long long units = p.b.row_start ? (long long)p.b.rows * p.group / (2 * TILE) + p.b.sequences
-                                        : p.b.sequences * (((long long)p.b.each * p.group + 2 * TILE - 1) / (2 * TILE));
-  if (units * C->heads > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
-  const cudaError_t e = with_size(C->Dp, [&](auto* kernel) { return lq_launch(kernel, (int)(units * C->heads), THREADS, tile_smem(C->Dp), st, p); });
+  const long long units = (p.b.row_start ? (long long)p.b.rows * p.group / (2 * TILE) + p.b.sequences
+                                         : p.b.sequences * (((long long)p.b.each * p.group + 2 * TILE - 1) / (2 * TILE))) * C->heads;
+  if (units > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
+  // where they leave SMs idle, as many thread blocks to a tile as there is room for
+  p.splits = (int)std::max(1ll, C->sms / units);
+  const cudaError_t e = with_size(C->Dp, [&](auto* kernel, auto* join) {
+    const cudaError_t first = lq_launch(kernel, (int)units * p.splits, THREADS, tile_smem(C->Dp), st, p);
+    if (first != cudaSuccess || p.splits == 1) return first;
+    return lq_launch_grid(join, dim3((unsigned)units, 2 * TILE / JOIN_ROWS), 32 * JOIN_WARPS, 1, 0, st, p);
+  });
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }

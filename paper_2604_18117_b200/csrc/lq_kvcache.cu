@@ -425,7 +425,9 @@ extern "C" lq_status lq_kvcache_create(int32_t layers, int32_t pages, int32_t pa
   }
   if (lq_note_cuda(cudaMalloc((void**)&C->d_records, n * rec)) != cudaSuccess ||
       lq_note_cuda(cudaMalloc((void**)&C->d_part, (size_t)2 * C->sms * LQ_ATTN_ROWS * (Dp + 4) * sizeof(float))) != cudaSuccess ||
-      lq_note_cuda(cudaMalloc((void**)&C->d_count, C->sms * sizeof(int))) != cudaSuccess) {
+      lq_note_cuda(cudaMalloc((void**)&C->d_count, C->sms * sizeof(int))) != cudaSuccess ||
+      (Dp <= 128 && (lq_note_cuda(cudaMalloc((void**)&C->d_tile_part, (size_t)C->sms * 256 * (Dp + 2) * sizeof(float))) != cudaSuccess ||
+                     lq_note_cuda(cudaMalloc((void**)&C->d_tile_meta, C->sms * sizeof(int4))) != cudaSuccess))) {
     lq_kvcache_free(C);
     return LQ_ERR_ALLOC;
   }
@@ -449,7 +451,7 @@ extern "C" lq_status lq_kvcache_create(int32_t layers, int32_t pages, int32_t pa
 extern "C" lq_status lq_kvcache_free(lq_kvcache* C) {
   if (!C) return LQ_ERR_INVALID_ARG;
   LqDeviceGuard guard(C->device);
-  cudaFree(C->d_records); cudaFree(C->d_part); cudaFree(C->d_count);
+  cudaFree(C->d_records); cudaFree(C->d_part); cudaFree(C->d_count); cudaFree(C->d_tile_part); cudaFree(C->d_tile_meta);
   delete C;
   return LQ_OK;
 }

@@ -33,6 +33,8 @@ struct lq_kvcache {
   // workspace of the attention: for each block of its grid two partial results of a tile of rows, and a count of those that have arrived
   float* d_part;                         // [2 * sms][LQ_ATTN_ROWS][Dp + 4]: maximum, sum, -, -, sums
   int* d_count;                          // [sms]
+  float* d_tile_part;                    // the same for tiles of 256 rows (Dp <= 128)
+  int4* d_tile_meta;
 };
 
 // A step's sequences, as kernels take them

@@ -301,6 +301,19 @@ def test_every_token_sees_every_other(D, hq, hk):
     c.close()
 
 
+@pytest.mark.parametrize("D,hq,hk,window,sinks", [(128, 8, 2, 0, 0), (72, 2, 2, 0, 0), (64, 8, 1, 1500, 40), (96, 3, 1, 700, 0), (112, 6, 2, 0, 0)])
+def test_few_tiles_of_rows_over_a_long_cache(D, hq, hk, window, sinks):
+    """Tiles of rows that many thread blocks share; one sequence of one length, ragged ones, some with rows of the other form, all and causal."""
+    lens = [4500, 90, 2500]
+    c = filled(D, hk, lens, 64)
+    for ns in ([70, 0, 0], [100, 90, 300], [3, 1, 200]):
+        run_attention(c, ns, lens, hq, True, window, sinks, behind=2)
+        if not window:
+            run_attention(c, ns, lens, hq, False)
+    run_attention(c, [90, 90, 90], lens, hq, True, window, sinks, uniform=True)
+    c.close()
+
+
 @pytest.mark.parametrize("sequences", [300, 1000])
 def test_many_sequences(sequences):
     lens = [1 + (37 * i) % 90 for i in range(sequences)]
