@@ -506,16 +506,17 @@ extern "C" lq_status lq_cache_attention(const lq_kvcache* C, int32_t layer, cons
   // Which form a sequence's rows are the kernels tell by themselves where sequences have different numbers of them; a form that no sequence can be is
   // not launched.
   const bool tiles = C->Dp <= 128;
+  const int few = lq_attn_few(p.b.sequences, C->heads, C->sms);
   const long long most = p.b.row_start ? (long long)p.b.rows * p.group : (long long)p.b.each * p.group, least = p.b.row_start ? 1 : most;
-  if (!tiles || least <= LQ_ATTN_FEW) {
+  if (!tiles || least <= few) {
     p.few = 1;
-    p.many = tiles ? LQ_ATTN_FEW + 1 : 0x7fffffff;
+    p.many = tiles ? few + 1 : 0x7fffffff;
     // (tiles of eight rows where no sequence has more)
     const cudaError_t e = with_form(C->Dp, most <= 8, [&](auto form) { return form.launch(C, p, (cudaStream_t)stream); });
     if (lq_note_cuda(e) != cudaSuccess) return LQ_ERR_CUDA;
   }
-  if (tiles && most > LQ_ATTN_FEW) {
-    p.few = LQ_ATTN_FEW + 1;
+  if (tiles && most > few) {
+    p.few = few + 1;
     p.many = 0x7fffffff;
     return lq_attn_tile_launch(C, p, (cudaStream_t)stream);
   }

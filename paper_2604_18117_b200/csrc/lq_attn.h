@@ -21,8 +21,11 @@ struct LqAttnParams {
   int32_t* status;
 };
 
-// Sequences of up to so many rows (new tokens x query heads of a group) are the form for few rows'
-constexpr int LQ_ATTN_FEW = 64;
+// Sequences of up to so many rows (new tokens x query heads of a group) are the form for few rows', which reads the cache once for every 16 of them but
+// shares it out evenly over the SMs.  us of one sequence of 8192 tokens, 8 heads of 128, few / many: 36 rows 24.2 / 35.7, 64 rows 26.8 / 37.4, 128
+// rows 36.4 / 43.4, 256 rows 56.9 / 49.0.  Sixteen sequences of 2000 tokens, which fill the SMs with tiles: 20 rows 39.0 / 38.3, 32 rows 40.1 / 38.3, 64 rows
+// 67.7 / 38.7, 128 rows 119.5 / 39.7; eight of 20000, a query head to a head: 20 rows 118 / 171.
+static inline int lq_attn_few(int sequences, int heads, int sms) { return 2ll * sequences * heads < sms ? 128 : 32; }
 
 lq_status lq_attn_tile_launch(const lq_kvcache* C, LqAttnParams p, cudaStream_t st);
 
