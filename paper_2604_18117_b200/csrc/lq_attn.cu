@@ -42,6 +42,11 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ int add_acq_rel(int* p, int v) {
+  int before;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(before) : "l"(p), "r"(v) : "memory");
+  return before;
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -73,11 +78,11 @@ struct Shared {
   alignas(16) float sums[WARPS][ROWS][PITCH];
   float top[WARPS][ROWS], total[WARPS][ROWS];
   alignas(16) uint2 q[Q_HERE ? NK : 1][NT][32];
-  long long prefix[WARPS], edge[2];
+  long long prefix[WARPS], tiles[WARPS], edge[2];
   Place found;
   alignas(8) uint64_t bars[WARPS][STAGES];
   uint8_t empty[WARPS][STAGES];
-  int abort_flag, last, from, parts;
+  int abort_flag, last, part, parts;
 };
 
 template <int NK, int NT, int WARPS, int STAGES>
@@ -93,47 +98,68 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
   mbar_init_fence();
   grid_launch_dependents();
   grid_dependency_wait();
-  long long share;
   const auto sequence = [&](int s) { return measure<ROWS>(p, s, false); };
 
-  // The launch's records, and this block's share of them: from edge[0] on, a place that is found, to before edge[1].  The thread that has an
-  // edge among its sequences' records looks it up.
+  // The launch's records, and this block's share of them: from edge[0] on, a place that is found, to before edge[1].  The thread among whose
+  // sequences an edge is looks it up.
+  LqAttnCut cut;
   {
     const int chunk = (p.b.sequences + THREADS - 1) / THREADS, first = tid * chunk, behind = min(p.b.sequences, first + chunk);
     Place mine = {};                                       // the thread's first sequence
-    long long sum = 0;
+    long long records = 0, tiles = 0;
     for (int s = first; s < behind; ++s) {
       const Place at = measure<ROWS>(p, s, blockIdx.x == 0);
       if (s == first) mine = at;
-      sum += lq_attn_records(at, p.b.heads);
+      records += lq_attn_records(at, p.b.heads);
+      tiles += (long long)at.tiles * p.b.heads;
     }
-    long long up = sum;
+    long long all = records;
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) {
+      all += __shfl_xor_sync(0xffffffffu, all, d);
+      tiles += __shfl_xor_sync(0xffffffffu, tiles, d);
+    }
+    if (lane == 0) { sm.prefix[warp] = all; sm.tiles[warp] = tiles; }
+    __syncthreads();
+    all = tiles = 0;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) { all += sm.prefix[i]; tiles += sm.tiles[i]; }
+    cut = lq_attn_cut(all, tiles, gridDim.x, WARPS);
+    long long count = records;
+    if (cut.parted) {
+      count = lq_attn_count(mine, p.b.heads, cut, SHORT * WARPS);
+      for (int s = first + 1; s < behind; ++s) count += lq_attn_count(sequence(s), p.b.heads, cut, SHORT * WARPS);
+    }
+    long long up = count;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const long long v = __shfl_up_sync(0xffffffffu, up, d);
       if (lane >= d) up += v;
     }
+    __syncthreads();
     if (lane == 31) sm.prefix[warp] = up;
+    if (tid == 0) { sm.edge[0] = sm.edge[1] = cut.parted ? 0 : all; }
     __syncthreads();
-    long long begin = up - sum, total = 0;
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) {
-      if (i < warp) begin += sm.prefix[i];
-      total += sm.prefix[i];
-    }
-    share = max((long long)WARPS, lq_quotient(total + gridDim.x - 1, gridDim.x));       // at least a record for each warp
-    if (tid == 0) { sm.edge[0] = sm.edge[1] = total; }
-    __syncthreads();
-#pragma unroll 1
-    for (int i = 0; i < 2; ++i) {
-      const long long edge = (blockIdx.x + i) * share;
-      if (edge < begin || edge >= begin + sum) continue;
-      Place at = mine;
-      const long long there = lq_attn_edge(at, begin, edge, p.b.heads, SHORT * WARPS, sequence);
-      sm.edge[i] = there;
-      if (i == 0) {
-        if (there < total) lq_attn_walk(at, 0, p.b.heads, p.b.sequences, sequence);
+    long long begin = up - count;
+    for (int i = 0; i < warp; ++i) begin += sm.prefix[i];
+    if (cut.parted) {
+      if ((long long)blockIdx.x >= begin && (long long)blockIdx.x < begin + count) {
+        Place at = mine;
+        sm.edge[1] = lq_attn_part(at, begin, blockIdx.x, p.b.heads, SHORT * WARPS, cut, sm.part, sm.parts, sequence);
         sm.found = at;
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 2; ++i) {
+        const long long edge = (blockIdx.x + i) * cut.share;
+        if (edge < begin || edge >= begin + count) continue;
+        Place at = mine;
+        const long long there = lq_attn_edge(at, begin, edge, p.b.heads, SHORT * WARPS, sequence);
+        sm.edge[i] = there;
+        if (i == 0) {
+          if (there < all) lq_attn_walk(at, 0, p.b.heads, p.b.sequences, sequence);
+          sm.found = at;
+        }
       }
     }
     __syncthreads();
@@ -165,44 +191,40 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
   };
   if constexpr (!Smem::Q_HERE) load_q(here);               // (here and below: asked for ahead of the wait for something else)
 
-  // The warp's ring: records lo + warp, lo + warp + WARPS, ...  The page of the one that is next is known when it is asked for.
-  Place ahead = here;
-  int left = (int)((hi - lo - warp + WARPS - 1) / WARPS), slot = 0, page = -1, issued = 0;
+  // The warp's ring: records lo + warp, lo + warp + WARPS, ...  Where they lie is looked up for 32 of them at a time, one a lane.
+  Place ahead = here;                                      // of the first that has not been looked up
+  int left = (int)((hi - lo - warp + WARPS - 1) / WARPS), looked = 0, issued = 0;
+  long long mine = -1;                                     // the lane's record, -1: no page's, or of no token
+  if (left > 0) lq_attn_walk(ahead, warp, p.b.heads, p.b.sequences, sequence);
   const auto look = [&]() {
-    page = -1;
-    if (left > 0 && ahead.i < ahead.q.seen.count()) {
-      slot = lq_kv_slot(p.b, ahead.q.seen.block(ahead.i));
-      page = p.b.pages[(long long)ahead.s * p.b.page_stride + slot];
+    Place at = ahead;
+    mine = -1;
+    if (lane < left - looked && lq_attn_walk(at, lane * WARPS, p.b.heads, p.b.sequences, sequence) && at.i < at.q.seen.count()) {
+      mine = lq_kv_at(p.b, at.s, at.q.seen.block(at.i));
+      if (mine < 0) lq_kv_refuse(p.status);
+      else mine += at.head;
     }
+    __syncwarp();
+    looked += 32;
+    if (looked < left && !lq_attn_walk(ahead, 32 * WARPS, p.b.heads, p.b.sequences, sequence)) left = looked;
   };
-  const auto issue = [&]() {                               // (a record that is no page's, or of no token, is not fetched; its stage then stays empty)
-    if (left <= 0) return;
+  const auto issue = [&]() {                               // (what is not fetched leaves its stage empty)
+    if (issued >= left) return;
+    if (issued == looked) look();
+    const long long at = __shfl_sync(0xffffffffu, mine, issued & 31);
     if (lane == 0) {
-      long long at = -1;
-      if (ahead.i < ahead.q.seen.count()) {
-        at = lq_kv_at(p.b, ahead.q.seen.block(ahead.i), slot, page);
-        if (at < 0) lq_kv_refuse(p.status);
-      }
       const int st = issued % STAGES;
       const uint32_t bar = smem_u32(&sm.bars[warp][st]);
       sm.empty[warp][st] = at < 0;
       if (at >= 0) {
         mbar_expect_tx(bar, REC);
-        bulk_load(smem_u32(sm.ring[warp][st]), p.records + (at + ahead.head) * p.b.record, REC, bar);
+        bulk_load(smem_u32(sm.ring[warp][st]), p.records + at * p.b.record, REC, bar);
       } else {
         mbar_arrive(bar);
       }
     }
     ++issued;
-    if (--left > 0) {
-      if (!lq_attn_walk(ahead, WARPS, p.b.heads, p.b.sequences, sequence)) left = 0;
-      look();
-    }
   };
-  if (left > 0) {
-    if (!lq_attn_walk(ahead, warp, p.b.heads, p.b.sequences, sequence)) left = 0;
-    look();
-  }
   for (int i = 0; i < STAGES; ++i) issue();
 
   int taken = 0;
@@ -383,19 +405,18 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
       }
     }
     if (!whole) {
-      __threadfence();
-      __syncthreads();
+      int from = blockIdx.x - sm.part, parts = sm.parts;   // the blocks that have some of the tile
+      if (!cut.parted) {
+        from = (int)lq_quotient(tile_begin, cut.share);
+        parts = (int)lq_quotient(tile_begin + was.each - 1, cut.share) - from + 1;
+      }
+      __syncthreads();                                     // (behind this the count's release covers what all threads have written)
       if (tid == 0) {
-        const int from = (int)lq_quotient(tile_begin, share), to = (int)lq_quotient(tile_begin + was.each - 1, share);
-        sm.from = from;
-        sm.parts = to - from + 1;
-        sm.last = atomicAdd(&p.count[from], 1) == to - from;
+        sm.last = add_acq_rel(&p.count[from], 1) == parts - 1;
         if (sm.last) p.count[from] = 0;                    // (nobody else comes)
-        __threadfence();
       }
       __syncthreads();
       if (sm.last) {
-        const int from = sm.from, parts = sm.parts;
         for (int e = tid; e < rows * (DP / 4); e += THREADS) {
           const int row = e / (DP / 4), d = 4 * (e - row * (DP / 4));
           float m = -INFINITY, n = 0.f;

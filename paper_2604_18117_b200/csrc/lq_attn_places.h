@@ -64,3 +64,42 @@ LQ_HD long long lq_attn_edge(LqAttnPlace<SEQ>& at, long long from, long long edg
   }
   return edge;
 }
+
+// How records are shared out over `grid` blocks.  With few tiles (at most half the blocks) every tile that is not small is cut in equal parts for
+// blocks of their own: a block that has the end of one tile and the beginning of another joins twice, which took a fifth of a long sequence's time.  With
+// more of them blocks have neighbouring records, as even as can be.
+struct LqAttnCut {
+  bool parted;
+  long long share;                       // records of a block: the most, or exactly
+};
+LQ_HD LqAttnCut lq_attn_cut(long long records, long long tiles, int grid, int least) {
+  const bool parted = 2 * tiles <= grid;
+  const long long blocks = parted ? grid - tiles : grid, share = lq_quotient(records + blocks - 1, blocks);
+  return {parted, share < least ? least : share};
+}
+// parts of a tile (parted): together no more than there are blocks
+LQ_HD int lq_attn_parts(int each, const LqAttnCut& cut, int small) {
+  return each <= small ? 1 : (int)lq_quotient(each + cut.share - 1, cut.share);
+}
+// what is counted along the sequences: blocks, or records
+template <typename SEQ>
+LQ_HD long long lq_attn_count(const LqAttnPlace<SEQ>& at, int heads, const LqAttnCut& cut, int small) {
+  return cut.parted ? (long long)at.tiles * heads * (at.tiles > 0 ? lq_attn_parts(at.each, cut, small) : 0) : lq_attn_records(at, heads);
+}
+// Parted: the place where block `block` begins; the sequences from `at` on have the blocks from the from-th on.  Returns how many records it has; part:
+// which of its tile's parts it is.
+template <typename SEQ, typename Measure>
+LQ_HD int lq_attn_part(LqAttnPlace<SEQ>& at, long long from, long long block, int heads, int small, const LqAttnCut& cut, int& part, int& parts,
+                       const Measure& measure) {
+  while (block - from >= lq_attn_count(at, heads, cut, small)) {
+    from += lq_attn_count(at, heads, cut, small);
+    at = measure(at.s + 1);
+  }
+  parts = lq_attn_parts(at.each, cut, small);
+  const long long tile = lq_quotient(block - from, parts);
+  part = (int)(block - from - tile * parts);
+  at.head = (int)lq_quotient(tile, at.tiles);
+  at.tile = (int)(tile - (long long)at.head * at.tiles);
+  at.i = (int)lq_quotient((long long)at.each * part, parts);
+  return (int)lq_quotient((long long)at.each * (part + 1), parts) - at.i;
+}

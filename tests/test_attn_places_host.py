@@ -18,15 +18,27 @@ extern "C" int block(const int* tiles, const int* each, int sequences, int heads
   const auto measure = [&](int s) { Place p = {}; p.s = s; p.tiles = tiles[s]; p.each = tiles[s] ? each[s] : 0; return p; };
   long long total = 0;
   for (int s = 0; s < sequences; ++s) total += lq_attn_records(measure(s), heads);
-  const long long share = std::max((long long)warps, lq_quotient(total + grid - 1, grid));
-  *share_out = share;
+  long long all_tiles = 0;
+  for (int s = 0; s < sequences; ++s) all_tiles += (long long)tiles[s] * heads;
+  const LqAttnCut cut = lq_attn_cut(total, all_tiles, grid, warps);
+  *share_out = cut.parted ? 0 : cut.share;
+  const long long share = cut.share;
   Place found = {};
-  edges[0] = edges[1] = total;
+  edges[0] = edges[1] = cut.parted ? 0 : total;
+  edges[2] = 0; edges[3] = 1;
   const int chunk = (sequences + threads - 1) / threads;
   long long begin = 0;
   for (int first = 0; first < sequences; first += chunk) {           // a thread
     long long sum = 0;
-    for (int s = first; s < std::min(sequences, first + chunk); ++s) sum += lq_attn_records(measure(s), heads);
+    for (int s = first; s < std::min(sequences, first + chunk); ++s) sum += lq_attn_count(measure(s), heads, cut, small);
+    if (cut.parted && b >= begin && b < begin + sum) {
+      Place at = measure(first);
+      int part, parts;
+      edges[1] = lq_attn_part(at, begin, b, heads, small, cut, part, parts, measure);
+      edges[2] = part; edges[3] = parts;
+      found = at;
+    }
+    if (!cut.parted)
     for (int i = 0; i < 2; ++i) {
       const long long edge = (b + i) * share;
       if (edge < begin || edge >= begin + sum) continue;
@@ -69,19 +81,24 @@ def lib(tmp_path_factory):
 def shared_out(so, tiles, each, heads, warps, grid, small, threads):
     tiles, each = np.array(tiles, np.int32), np.array(each, np.int32)
     total = int((tiles.astype(np.int64) * each * heads).sum())
-    seen, owners, edges, share = {}, {}, (C.c_longlong * 2)(), C.c_longlong()
+    seen, owners, parts_of, edges, share = {}, {}, {}, (C.c_longlong * 4)(), C.c_longlong()
     out, ends = np.zeros((total + 1, 4), np.int32), 0
     for b in range(grid):
         n = so.block(tiles.ctypes.data_as(C.c_void_p), each.ctypes.data_as(C.c_void_p), len(tiles), heads, warps, grid, small, threads, b, edges, C.byref(share),
                      out.ctypes.data_as(C.c_void_p))
         assert n == max(0, edges[1] - edges[0]), (b, n, list(edges))
-        assert edges[0] >= ends
-        ends = max(ends, edges[1])
+        parted = share.value == 0
+        if parted:
+            parts_of.update({tuple(r[:3]): (b - edges[2], edges[3]) for r in out[:n].tolist()})
+            assert n == 0 or len({tuple(r[:3]) for r in out[:n].tolist()}) == 1          # of one tile
+        else:
+            assert edges[0] >= ends
+            ends = max(ends, edges[1])
         for s, h, t, i in out[:n].tolist():
             assert (s, h, t, i) not in seen
             seen[s, h, t, i] = b
             owners.setdefault((s, h, t), set()).add(b)
-    assert len(seen) == total and ends == total
+    assert len(seen) == total and (parted or ends == total)
     at = 0
     for s in range(len(tiles)):
         for h in range(heads):
@@ -90,6 +107,9 @@ def shared_out(so, tiles, each, heads, warps, grid, small, threads):
                 who = owners[s, h, t]
                 if each[s] <= small:
                     assert len(who) == 1
+                elif parted:
+                    first, parts = parts_of[s, h, t]
+                    assert who == set(range(first, first + parts))
                 elif len(who) > 1:                         # those that the joining block counts on
                     assert who == set(range(at // share.value, (at + each[s] - 1) // share.value + 1))
                 at += int(each[s])
