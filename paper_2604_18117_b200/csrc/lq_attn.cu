@@ -518,7 +518,7 @@ extern "C" lq_status lq_cache_attention(const lq_kvcache* C, int32_t layer, cons
   p.records = lq_kv_layer(C, layer);
   p.q = (const __half*)a->q; p.out = (__half*)a->out;
   p.q_row = a->q_row; p.q_head = a->q_head; p.out_row = a->out_row; p.out_head = a->out_head;
-  p.D = C->D; p.Dp = C->Dp; p.group = a->q_heads / C->heads;
+  p.D = C->D; p.group = a->q_heads / C->heads;
   p.causal = a->causal; p.window = a->window; p.sinks = a->sinks;
   p.scale = a->scale * 16.f * 1.44269504088896341f;        // (keys are opened as 2^-4 of themselves)
   p.part = C->d_part; p.count = C->d_count;

@@ -9,7 +9,7 @@ struct LqAttnParams {
   const __half* q;
   __half* out;
   long long q_row, q_head, out_row, out_head;
-  int D, Dp, group;                      // query heads of a head of keys and values
+  int D, group;                          // query heads of a head of keys and values
   int causal, window, sinks;
   float scale;                           // of the products of queries and stored keys, times log2 e
   float* part;

@@ -121,11 +121,11 @@ __global__ void __launch_bounds__(THREADS) lq_residual_kernel(const __grid_const
   int turn = 0, held = -1;
   grid_launch_dependents();
   grid_dependency_wait();
-  const int step = 32 * p.wide, last = min(p.groups, (int)(blockIdx.x + 1) * p.share);
+  const int step = 32 * p.wide, last = (int)min((long long)p.groups, (blockIdx.x + 1ll) * p.share);
   const int places = first < fours ? (fours - first + step - 1) / step : 0;
   const float4 *va = vectors + first, *vb = va + fours, *vc = vb + fours;
   constexpr int XB = XF32 ? 16 : 8, YB = YF32 ? 16 : 8, HB = HF32 ? 16 : 8;
-  for (int g = blockIdx.x * p.share; g < last; ++g) {
+  for (int g = (int)(blockIdx.x * (long long)p.share); g < last; ++g) {
     const int seq = g / p.seq_groups, in_seq = (g - seq * p.seq_groups) * per + warp / p.wide;
     const long long row = (long long)seq * p.seq_rows + in_seq;
     const int mine = in_seq < p.seq_rows ? places : 0;
