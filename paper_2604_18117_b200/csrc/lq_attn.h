@@ -15,7 +15,7 @@ struct LqAttnParams {
   float* part;
   int* count;
   int few, many;                         // sequences whose rows * group are in [few, many) are this launch's
-  int splits;                            // form for many rows: thread blocks that share out a tile's tokens
+  int whole, splits;                     // form for many rows: tiles with a thread block each; blocks that share out the tokens of each of the others
   float* tile_part;                      // [sms][Dp + 2][256]: what each of them leaves: sums by entry, maxima, sums of weights
   int4* tile_meta;                       // [sms]: of a tile: parts that it has, first row in the call, its place in the sequence's rows, how many
   int32_t* status;

@@ -245,7 +245,8 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
 
   // the block's sequence and tile of rows: blocks of a tile's heads follow each other, a sequence's last tiles (which see most) come first
   Task k = {};
-  const int part = blockIdx.x % p.splits, place = blockIdx.x / p.splits;
+  // (the first p.whole tiles have a block each, the others p.splits)
+  const int shared = (int)blockIdx.x - p.whole, part = shared < 0 ? 0 : shared % p.splits, place = shared < 0 ? (int)blockIdx.x : p.whole + shared / p.splits;
   k.head = place % p.b.heads;
   const int unit = place / p.b.heads;
   if (!p.b.row_start) {
@@ -294,13 +295,13 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
   if (k.s >= 0) {
     k.rows = min(2 * TILE, k.q.n * p.group - k.row0);
     k.seen = lq_seen(p, base + k.row0 / p.group, base + (k.row0 + k.rows - 1) / p.group, k.q.len);
-    const int all = (k.seen.count() + 3) / 4, each = max(MIN_TILES, (all + p.splits - 1) / p.splits);
+    const int all = (k.seen.count() + 3) / 4, each = shared < 0 ? max(1, all) : max(MIN_TILES, (all + p.splits - 1) / p.splits);
     k.parts = max(1, (all + each - 1) / each);
     k.first = part * each;
     k.tiles = max(0, min(each, all - k.first));
     if (part >= k.parts) k.rows = 0;                       // (nothing is left for this block)
   }
-  if (p.splits > 1 && part == 0 && tid == 0) p.tile_meta[place] = make_int4(k.parts, k.q.row, k.row0, k.rows);
+  if (shared >= 0 && p.splits > 1 && part == 0 && tid == 0) p.tile_meta[place - p.whole] = make_int4(k.parts, k.q.row, k.row0, k.rows);
   const int halves = k.rows > TILE ? 2 : 1, tiles = k.tiles;
   if (tid == 0) c.task = k;                                // (for code that has no registers for it)
   __syncthreads();
@@ -434,7 +435,7 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
       }
       if (tiles > 0 && wait(c.o_full[half], 0, LQ_STAGE_DRAIN)) tc_fence_after();
       if (task.parts > 1) {                                // for lq_attn_join_kernel
-        float* out = p.tile_part + (long long)blockIdx.x * (DP + 2) * (2 * TILE) + half * TILE + row;
+        float* out = p.tile_part + (long long)(blockIdx.x - p.whole) * (DP + 2) * (2 * TILE) + half * TILE + row;
         if (good)
 #pragma unroll 1
           for (int x = 0; x < DP; x += 16) {
@@ -639,7 +640,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) lq_attn_join_kernel(const __g
     }
   }
   const float by = l > 0.f ? 16.f / l : 0.f;
-  const int place = blockIdx.x % p.b.heads, r = meta.z + row, tok = r / p.group;
+  const int place = (p.whole + blockIdx.x) % p.b.heads, r = meta.z + row, tok = r / p.group;
   __half* out = p.out + (meta.y + tok) * p.out_row + (long long)(place * p.group + r - tok * p.group) * p.out_head;
 #pragma unroll
   for (int g = 0; g < NK; ++g)
@@ -674,12 +675,17 @@ lq_status lq_attn_tile_launch(const lq_kvcache* C, LqAttnParams p, cudaStream_t 
   const long long units = (p.b.row_start ? (long long)p.b.rows * p.group / (2 * TILE) + p.b.sequences
                                          : p.b.sequences * (((long long)p.b.each * p.group + 2 * TILE - 1) / (2 * TILE))) * C->heads;
   if (units > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
-  // where they leave SMs idle, as many thread blocks to a tile as there is room for
-  p.splits = (int)std::max(1ll, C->sms / units);
+  // Where the last of them leave SMs idle, as many thread blocks to each of these as there is room for, unless no sequence is long (us of 512 tiles, one
+  // block each / the last 68 shared by two: 4096 tokens, heads of 72 273 / 254; 4096 behind 4096, causal, heads of 128 448 / 422).
+  p.whole = (int)(units / C->sms * C->sms);
+  const int last = (int)(units - p.whole);
+  p.splits = last > 0 && (long long)p.b.page_stride * C->page_tokens >= 4 * MIN_TILES * KV ? C->sms / last : 1;
+  if (p.splits == 1) p.whole = (int)units;
   const cudaError_t e = with_size(C->Dp, [&](auto* kernel, auto* join) {
-    const cudaError_t first = lq_launch(kernel, (int)units * p.splits, THREADS, tile_smem(C->Dp), st, p);
-    if (first != cudaSuccess || p.splits == 1) return first;
-    return lq_launch_grid(join, dim3((unsigned)units, 2 * TILE / JOIN_ROWS), 32 * JOIN_WARPS, 1, 0, st, p);
+    const int split = (int)units - p.whole;
+    const cudaError_t first = lq_launch(kernel, p.whole + split * p.splits, THREADS, tile_smem(C->Dp), st, p);
+    if (first != cudaSuccess || split == 0) return first;
+    return lq_launch_grid(join, dim3((unsigned)split, 2 * TILE / JOIN_ROWS), 32 * JOIN_WARPS, 1, 0, st, p);
   });
   return lq_note_cuda(e) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
 }
