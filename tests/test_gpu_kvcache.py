@@ -452,6 +452,36 @@ def test_a_captured_step_goes_by_what_the_arrays_hold():
     c.close()
 
 
+def test_offsets_beyond_32_bits():
+    """Records behind 2^32 bytes, rows of queries and outputs behind 2^31 elements; prompts, single tokens, writing and reading."""
+    import torch
+    D, H, n_pages = 128, 4, 48000
+    h = B.lq_kvcache_create(2, n_pages, 64, H, D)           # 3.2 GB a layer
+    c = Cache(D, H, [300, 200], 64)
+    B.lq_kvcache_free(c.h)
+    c.h, c.layer = h, 1
+    c.pages = np.where(c.pages >= 0, n_pages - 1 - c.pages, -1).astype(np.int32)
+    c.pages_d = torch.from_numpy(c.pages).cuda()
+    c.append([300, 200])
+    c.check()
+    far = 1 << 24                                          # times 190 rows passes 2^31 elements
+    buf = torch.empty(2, 191 * far, dtype=torch.float16, device="cuda")
+    st = torch.cuda.current_stream().cuda_stream
+    for ns in ([150, 40], [1, 1]):
+        rows = sum(ns)
+        q = c.rng.standard_normal((rows, 4, D)).astype(np.float16)
+        qf, of = (torch.as_strided(x, (rows, 4, D), (far, D, 1), x.storage_offset()) for x in buf)
+        qf.copy_(torch.from_numpy(q).cuda())
+        b = c.batch(ns, c.len)
+        B.lq_cache_attention(c.h, 1, b, B.lq_attn(buf[0].data_ptr(), (far, D), buf[1].data_ptr(), (far, D), 4, 0.1), st)
+        got, at = of.double().cpu().numpy(), 0
+        for s, n in enumerate(ns):
+            want, err = attend(q[at:at + n].astype(np.float64), c.held[0][s][:c.len[s]], c.held[1][s][:c.len[s]], 0.1, c.len[s] - n, True, 0, 0)
+            assert (np.abs(got[at:at + n] - want) <= err).all(), s
+            at += n
+    c.close()
+
+
 def test_refusals():
     import torch
     code = lambda f, *a: _code(f, *a)

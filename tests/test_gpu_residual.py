@@ -120,6 +120,21 @@ def test_many_rows():
     run(6000, 2240, 3, "rms", "layer", fx="f32")
 
 
+def test_rows_far_apart():
+    """Rows behind 2^32 elements."""
+    import torch
+    C, far, M = 1152, (1 << 31) + 8, 3
+    buf = torch.empty(2 * far + C, dtype=torch.float16, device="cuda")
+    x = torch.as_strided(buf, (M, C), (far, 1))
+    ref = torch.randn(M, C, device="cuda").half()
+    x.copy_(ref)
+    h = torch.empty(M, C, device="cuda")
+    B.lq_residual_norm(B.lq_residual(M, C, x.data_ptr(), None, h.data_ptr(), norm=B.NORM_RMS, h_dtype=B.OUT_F32, strides=(far, C, C, C)),
+                       torch.cuda.current_stream().cuda_stream)
+    want, err = normed(ref.double().cpu().numpy(), np.zeros((M, C)), "rms", 1e-6)
+    assert (np.abs(h.double().cpu().numpy() - want) <= err + U * np.abs(want)).all()
+
+
 def test_rows_without_variance():
     run(5, 264, after="layer", norm="layer", flat=True, eps=1e-6)
 
