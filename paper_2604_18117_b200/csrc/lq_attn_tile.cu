@@ -9,6 +9,13 @@
 // of the other run, and O's product follows P 32 tokens at a time.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
 // there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are up to 2^8,
 // which halves and sums hold as well, and the last division takes care of it.
+//
+// B200, us: 4096 tokens behind 4096, 32 heads of 128 on 8 424 (970 TFLOP/s of visible pairs, 0.58 of the measured burst rate of a GEMM, 0.69 of the
+// sustained one); two images of 4096 tokens, 16 heads of 72 253 (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000
+// clocks where the tensor cores need 2048: the chain S -> weights -> O of either half (2400 clocks of weights, of which 1024 powers, and 1500 of
+// products and hand-overs) and shared memory, which the products' operands, opened codes and copies keep busy for 2560.  Timed and not kept: two threads a row
+// (16 warps: 441 for 430), the first weights by the last maximum while the new one is found (437), an eighth to a half of the powers by polynomials (431
+// to 502 for 445), core matrices without swizzle (no bank met twice, but 588 for 548).
 #include <math.h>
 
 #include <algorithm>
@@ -238,9 +245,6 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
     c.abort_flag = 0;
     mbar_init_fence();
   }
-  if (warp == MMA_WARP) tmem_alloc(smem_u32(&c.tmem), TMEM_COLS);
-  __syncthreads();                                         // (a kernel that starts early finds this block's tensor memory taken)
-  grid_launch_dependents();
   grid_dependency_wait();
 
   // the block's sequence and tile of rows: blocks of a tile's heads follow each other, a sequence's last tiles (which see most) come first
@@ -290,7 +294,6 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
     k.row0 = c.place[1];
     if (k.s >= 0) k.q = lq_seq(p.b, k.s);
   }
-  const uint32_t tmem = *const_cast<volatile uint32_t*>(&c.tmem);
   const int base = k.q.len - k.q.n;
   if (k.s >= 0) {
     k.rows = min(2 * TILE, k.q.n * p.group - k.row0);
@@ -302,9 +305,13 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
     if (part >= k.parts) k.rows = 0;                       // (nothing is left for this block)
   }
   if (shared >= 0 && p.splits > 1 && part == 0 && tid == 0) p.tile_meta[place - p.whole] = make_int4(k.parts, k.q.row, k.row0, k.rows);
-  const int halves = k.rows > TILE ? 2 : 1, tiles = k.tiles;
+  if (k.rows == 0) return;                                 // (a launch for a batch whose sequences may all have few rows costs little then)
+  if (warp == MMA_WARP) tmem_alloc(smem_u32(&c.tmem), TMEM_COLS);
   if (tid == 0) c.task = k;                                // (for code that has no registers for it)
   __syncthreads();
+  grid_launch_dependents();                                // (a kernel that starts early finds this block's tensor memory taken)
+  const uint32_t tmem = *const_cast<volatile uint32_t*>(&c.tmem);
+  const int halves = k.rows > TILE ? 2 : 1, tiles = k.tiles;
   bool good = true;
   const auto wait = [&](uint64_t& bar, int phase, int role) {
     // (without a call: the warps' registers are not those that the block was launched with)

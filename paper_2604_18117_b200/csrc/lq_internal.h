@@ -244,11 +244,12 @@ extern int g_lq_store_qb;    // option "store_qb": also write the branch activat
 // stream is still draining its last tiles.  Every kernel of this library executes griddepcontrol.wait after that set-up,
 // before it reads what an earlier kernel may write or writes global memory (weights, which no kernel writes, and the quantizer's
 // prefetch of X to the L2 come before it), and griddepcontrol.launch_dependents after the set-up, so that the chain
-// quantizer -> GEMM -> next quantizer overlaps its launch gaps and tails.  Three kernels differ:
+// quantizer -> GEMM -> next quantizer overlaps its launch gaps and tails.  Four kernels differ:
 //   lq_adapters_set_kernel   lets no dependent start early: what follows sees the adapter whole
 //   lq_adapters_down_kernel  lets its dependent start behind its own wait, and first sets a word of the map's (release, device scope)
 //   lq_adapters_up_kernel    reads the map, the factors and Y0 before its wait if it finds that word set (acquire), T and its rows'
 //                            scales behind it; its last act is to clear the word
+//   lq_attn_tile_kernel      lets its dependent start behind its own wait, once its block has its tensor memory (or nothing to do)
 // A kernel may read early only what it knows to be complete.  That it has started tells nothing: calls of distinct handles may come from
 // distinct threads to one stream, and the kernel right before it, which lets it start, need not be the one that its caller launched last.
 // The layer's kernels are persistent (the whole grid is resident at once), and a dependent of the others starts only when their last CTA

@@ -3,8 +3,13 @@
 //   a block of 32 tokens of a head has one step 2^e for its keys and one for its values, e the smallest integer in [-20, 9] with
 //   127 * 2^e >= the largest magnitude that was written to it;   code c = rint(x / 2^e) in [-127, 127]
 //
-// Tokens that come to a block that has some already may need a larger e'; the codes that are there become rint(c / 2^(e' - e)).  Powers of two
-// make both divisions exact, and every value c 2^e is a half (of 11 bits: c has 7).
+// Tokens that come to a block that has some already may need a larger e'; the codes that are there become rint(c / 2^(e' - e)).  Powers of two make
+// both divisions exact, and every value c 2^e is a half (of 11 bits: c has 7).
+//
+// Both kernels are the memory's: rows in and codes out, or the other way round, once.  Two warps have the keys of a head's block and two its values; rows go
+// through registers 16 bytes a lane and records through shared memory, where they change order (straight from rows to a record's places: 133 us
+// for 80).  B200: 32768 rows of 8 heads of 128 written in 46 us and read in 33, 0.68 and 0.93 of the measured copy rate of their bytes (written:
+// the blocks' two meetings, and registers for 28 warps an SM); single tokens of 32 sequences, written and read, 6.7 us, latency.
 #include <math.h>
 
 #include <algorithm>
