@@ -4,9 +4,9 @@
 //   S = Q K^T,   P = 2^(S c - m c),   O += P V,   l += P 1        over 128 tokens (four records) at a time, m a maximum of the row so far
 //
 // What bounds it is the tensor cores and what feeds them.  Seven warps open the records to halves in shared memory (two buffers of K and V, in
-// the core matrices of K-major operands; with the pads below no two lanes of a store meet in a bank); one thread issues the products; two
-// groups of four warps have 128 rows each, a row a thread, and take turns with the tensor cores: while one forms P of its rows, the products
-// of the other run, and O's product follows P 32 tokens at a time.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
+// swizzled rows, where no two lanes of a store meet in a bank); one thread issues the products; two groups of four warps have 128 rows each, a
+// row a thread, and take turns with the tensor cores: while one forms P of its rows, the products of the other run, and O's product follows P
+// 32 tokens at a time.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
 // there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are up to 2^8,
 // which halves and sums hold as well, and the last division takes care of it.
 //
@@ -15,7 +15,7 @@
 // clocks where the tensor cores need 2048: the chain S -> weights -> O of either half (2400 clocks of weights, of which 1024 powers, and 1500 of
 // products and hand-overs) and shared memory, which the products' operands, opened codes and copies keep busy for 2560.  Timed and not kept: two threads a row
 // (16 warps: 441 for 430), the first weights by the last maximum while the new one is found (437), an eighth to a half of the powers by polynomials (431
-// to 502 for 445), core matrices without swizzle (no bank met twice, but 588 for 548).
+// to 502 for 445); of the first form, which took 548, core matrices 16 and 32 bytes off boundaries of 128, whose stores met in no bank (588).
 #include <math.h>
 
 #include <algorithm>
