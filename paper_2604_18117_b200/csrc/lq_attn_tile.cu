@@ -372,14 +372,13 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         tmem_ld_wait();
 #pragma unroll
         for (int i = 0; i < 4; ++i) settled(v[i]);
-        // Of 32 tokens the weights, as they go to tensor memory, and their sum
+        // Of 32 tokens the weights, as they go to tensor memory, and what they add to the sum (taken to one number when all are handed over)
         const float2 scale2 = make_float2(scale, scale);
         uint32_t w[16];
-        float2 sum[2];
+        float2 sum[2] = {};
         const auto weigh = [&](const uint32_t (&v)[32]) {
           const float ref = m > -INFINITY ? -m : 0.f;
           const float2 ref2 = make_float2(ref, ref);
-          sum[0] = sum[1] = make_float2(0.f, 0.f);
 #pragma unroll
           for (int x = 0; x < 32; x += 2) {
             float2 e = __ffma2_rn(make_float2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), scale2, ref2);
@@ -432,13 +431,13 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           weigh(v[i]);
-          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
           tmem_st_16(ts + 16 * i, w);                      // (over columns of S, which has been read)
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&c.p_full[half][i]));
         }
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
       if (tiles > 0 && wait(c.o_full[half], 0, LQ_STAGE_DRAIN)) tc_fence_after();
       if (task.parts > 1) {                                // for lq_attn_join_kernel
