@@ -10,8 +10,8 @@
 // there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are up to 2^8,
 // which halves and sums hold as well, and the last division takes care of it.
 //
-// B200, us: 4096 tokens behind 4096, 32 heads of 128 on 8 424 (970 TFLOP/s of visible pairs, 0.58 of the measured burst rate of a GEMM, 0.69 of the
-// sustained one); two images of 4096 tokens, 16 heads of 72 253 (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000
+// B200, us: 4096 tokens behind 4096, 32 heads of 128 on 8 415 (994 TFLOP/s of visible pairs, 0.59 of the measured burst rate of a GEMM, 0.71 of the
+// sustained one); two images of 4096 tokens, 16 heads of 72 246 (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000
 // clocks where the tensor cores need 2048: the chain S -> weights -> O of either half (2400 clocks of weights, of which 1024 powers, and 1500 of
 // products and hand-overs) and shared memory, which the products' operands, opened codes and copies keep busy for 2560.  Timed and not kept: two threads a row
 // (16 warps: 441 for 430), the first weights by the last maximum while the new one is found (437), an eighth to a half of the powers by polynomials (431

@@ -8,8 +8,8 @@
 //
 // Both kernels are the memory's: rows in and codes out, or the other way round, once.  Two warps have the keys of a head's block and two its values; rows go
 // through registers 16 bytes a lane and records through shared memory, where they change order (straight from rows to a record's places: 133 us
-// for 80).  B200: 32768 rows of 8 heads of 128 written in 46 us and read in 33, 0.68 and 0.93 of the measured copy rate of their bytes (written:
-// the blocks' two meetings, and registers for 28 warps an SM); single tokens of 32 sequences, written and read, 6.7 us, latency.
+// for 79).  B200: 32768 rows of 8 heads of 128 written in 46 us and read in 34, 0.69 and 0.91 of the measured copy rate of their bytes (written:
+// the blocks' two meetings, and registers for 28 warps an SM); single tokens of 32 sequences, written and read, 6.5 us, latency.
 #include <math.h>
 
 #include <algorithm>
@@ -100,18 +100,33 @@ template <> struct Raw8<float> {
   }
 };
 
-// The sequence that row r belongs to: the last one that begins at or before it and has rows, found by the warp together.
-__device__ __forceinline__ int sequence_of(const LqBatch& b, int r, int lane) {
-  if (!b.row_start) return r / b.each;
+// The sequence that row r belongs to, the last one that begins at or before it and has rows, and its rows and tokens; found by the warp together, in
+// one trip to memory for up to 32 sequences (appends to ones of a single token, written and read, 6.7 -> 6.5 us).
+__device__ __forceinline__ int sequence_of(const LqBatch& b, int r, int lane, LqSeq& q) {
+  if (!b.row_start) {
+    const int s = r / b.each;
+    q = lq_seq(b, s);
+    return s;
+  }
   int lo = 0, n = b.sequences;           // the answer is in [lo, lo + n)
-  while (n > 1) {
+  while (n > 32) {
     const int step = (n + 31) / 32, at = lo + lane * step;
     const bool before = at < lo + n && b.row_start[at] <= r;
     const int last = 31 - __clz(__ballot_sync(0xffffffffu, before) | 1);
     lo += last * step;
     n = min(step, n - last * step);
   }
-  return lo;
+  LqSeq mine = {0, 0, 0};
+  bool before = false;
+  if (lane < n) {
+    mine = lq_seq(b, lo + lane);
+    before = b.row_start[lo + lane] <= r;
+  }
+  const int last = 31 - __clz(__ballot_sync(0xffffffffu, before) | 1);
+  q.row = __shfl_sync(0xffffffffu, mine.row, last);
+  q.n = __shfl_sync(0xffffffffu, mine.n, last);
+  q.len = __shfl_sync(0xffffffffu, mine.len, last);
+  return lo + last;
 }
 
 // A side of a record in shared memory, between rows and the order that it is kept in.  A thread turns units of four neighbouring tokens (a
@@ -144,8 +159,14 @@ __device__ __forceinline__ void sts_v2(uint32_t a, const uint2& v) { asm volatil
 
 // One block, keys or values, that has no tokens yet, two warps: tokens 0 .. n - 1 are rows of `in`, the others zeros.
 template <typename T, bool KEYS, int CHUNKS>
-__device__ __forceinline__ void fill_block(uint8_t* record, const T* in, long long row, int n, int D, int Dp, uint32_t image, float* tops) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 1, groups = (D + 15) / 16;
+__device__ __forceinline__ void fill_block(const RowsParams& p, int block, int slot, int page, int head, const T* in, long long row, int n, uint32_t image, float* tops) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 1, D = p.D, groups = (D + 15) / 16;
+  const long long found = lq_kv_at(p.b, block, slot, page);
+  if (found < 0) {
+    if (threadIdx.x == 0) lq_kv_refuse(p.status);
+    return;
+  }
+  uint8_t* record = p.records + (found + head) * p.b.record;
   Raw8<T> raw[CHUNKS][2][4];
   float top = 0.f;
 #pragma unroll
@@ -196,7 +217,7 @@ __device__ __forceinline__ void fill_block(uint8_t* record, const T* in, long lo
       }
     }
   meet();
-  uint4* to = reinterpret_cast<uint4*>(record + LQ_KV_HEAD + (KEYS ? 0 : lq_kv_side_bytes(Dp)));
+  uint4* to = reinterpret_cast<uint4*>(record + LQ_KV_HEAD + (KEYS ? 0 : lq_kv_side_bytes(p.Dp)));
   for (int i = threadIdx.x & 63; i < 32 * groups; i += 64) to[i] = lds_v4(image + piece<KEYS>(i) * 16);
   if ((threadIdx.x & 63) == 0) reinterpret_cast<int8_t*>(record)[KEYS ? 0 : 1] = (int8_t)e;
 }
@@ -263,9 +284,10 @@ __global__ void __launch_bounds__(THREADS) lq_kv_append_kernel(const __grid_cons
   int r = (int)(blockIdx.x / p.b.heads) * p.tile;
   const int end = min(p.b.rows - r, p.tile) + r;
   const T* in = reinterpret_cast<const T*>(side ? p.v : p.k) + head * p.head[side];
-  int s = sequence_of(p.b, r, lane);
-  while (r < end && s < p.b.sequences) {
-    const LqSeq q = lq_seq(p.b, s);
+  LqSeq q;
+  int s = sequence_of(p.b, r, lane, q);
+  for (bool known = true; r < end && s < p.b.sequences; known = false) {
+    if (!known) q = lq_seq(p.b, s);
     if (r < q.row || q.n == 0 || r >= q.row + q.n) {       // rows of no sequence lie in front (then r moves on), or the next sequence has it
       if (r < q.row) r = q.row;
       else ++s;
@@ -278,19 +300,20 @@ __global__ void __launch_bounds__(THREADS) lq_kv_append_kernel(const __grid_cons
     }
     const int at = q.len - q.n + (r - q.row), t0 = at % LQ_KV_BLOCK, t1 = min(LQ_KV_BLOCK, t0 + q.row + q.n - r);
     if (r == q.row || t0 == 0) {
-      const long long found = lq_kv_at(p.b, s, at / LQ_KV_BLOCK);
-      if (found < 0) {
-        if (threadIdx.x == 0) lq_kv_refuse(p.status);
+      const int block = at / LQ_KV_BLOCK, slot = lq_kv_slot(p.b, block), page = p.b.pages[(long long)s * p.b.page_stride + slot];
+      const T* rows = in + r * p.row[side];
+      if (t0 == 0) {
+        __syncthreads();                                   // (the images of the block before are read)
+        if (side == 0) fill_block<T, true, CHUNKS>(p, block, slot, page, head, rows, p.row[0], t1, smem_u32(images[0]), tops);
+        else fill_block<T, false, CHUNKS>(p, block, slot, page, head, rows, p.row[1], t1, smem_u32(images[1]), tops);
       } else {
-        uint8_t* record = p.records + (found + head) * p.b.record;
-        const T* rows = in + r * p.row[side];
-        if (t0 > 0) {
+        const long long found = lq_kv_at(p.b, block, slot, page);
+        if (found < 0) {
+          if (threadIdx.x == 0) lq_kv_refuse(p.status);
+        } else {
+          uint8_t* record = p.records + (found + head) * p.b.record;
           if (warp == 0) add_to_block<T, true>(record, rows, p.row[0], t0, t1, p.D, p.Dp);
           else if (warp == 2) add_to_block<T, false>(record, rows, p.row[1], t0, t1, p.D, p.Dp);
-        } else {
-          __syncthreads();                                 // (the images of the block before are read)
-          if (side == 0) fill_block<T, true, CHUNKS>(record, rows, p.row[0], t1, p.D, p.Dp, smem_u32(images[0]), tops);
-          else fill_block<T, false, CHUNKS>(record, rows, p.row[1], t1, p.D, p.Dp, smem_u32(images[1]), tops);
         }
       }
     }

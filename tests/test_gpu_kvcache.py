@@ -141,6 +141,18 @@ def test_one_row_of_every_sequence():
     c.close()
 
 
+@pytest.mark.parametrize("sequences", [1, 31, 32, 33, 64, 65, 1024, 1025, 2100])
+def test_rows_find_their_sequence(sequences):
+    """Sequences at the borders of what a warp looks through at once, some of them empty (the first and the last, and runs of more than a warp)."""
+    ns = [0 if sequences > 1 and (i in (0, sequences - 1) or i % 3 == 1 or 40 <= i < 110) else 1 + 31 * (i % 11 == 5) + 40 * (i % 13 == 2)
+          for i in range(sequences)]
+    c = Cache(8, 1, [1 + 2 * n for n in ns])
+    for n in (ns, [min(1, x) for x in ns], ns):
+        c.append(n)
+    c.check()
+    c.close()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_exponents_at_their_ends(dtype):
     """Borders of the exponent (127 2^e and the next number above), nothing but zeros, the smallest and largest magnitudes."""
