@@ -472,10 +472,6 @@ struct Form {
                                              (int)sizeof(Shared<NK, NT, WARPS, STAGES>))) == cudaSuccess;
   }
 };
-#ifndef W8
-#define W8 8
-#define S8 2
-#endif
 template <typename F>
 auto with_form(int Dp, bool narrow, const F& f) {
   switch (Dp) {
@@ -483,7 +479,7 @@ auto with_form(int Dp, bool narrow, const F& f) {
     case 80: return narrow ? f(Form<5, 1, 8, 3>()) : f(Form<5, 2, 8, 3>());
     case 96: return narrow ? f(Form<6, 1, 8, 3>()) : f(Form<6, 2, 8, 2>());
     case 112: return narrow ? f(Form<7, 1, 8, 2>()) : f(Form<7, 2, 8, 2>());
-    case 128: return narrow ? f(Form<8, 1, W8, S8>()) : f(Form<8, 2, 8, 2>());
+    case 128: return narrow ? f(Form<8, 1, 8, 2>()) : f(Form<8, 2, 8, 2>());
     case 192: return narrow ? f(Form<12, 1, 4, 3>()) : f(Form<12, 2, 4, 3>());
     default: return narrow ? f(Form<16, 1, 4, 2>()) : f(Form<16, 2, 4, 2>());
   }
