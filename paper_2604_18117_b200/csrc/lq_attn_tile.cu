@@ -6,16 +6,19 @@
 // What bounds it is the tensor cores and what feeds them.  Seven warps open the records to halves in shared memory (two buffers of K and V, in
 // swizzled rows, where no two lanes of a store meet in a bank); one thread issues the products; two groups of four warps have 128 rows each, a
 // row a thread, and take turns with the tensor cores: while one forms P of its rows, the products of the other run, and O's product follows P
-// 32 tokens at a time.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
+// 64 tokens at a time.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
 // there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are up to 2^8,
 // which halves and sums hold as well, and the last division takes care of it.
 //
-// B200, us: 4096 tokens behind 4096, 32 heads of 128 on 8 415 (994 TFLOP/s of visible pairs, 0.59 of the measured burst rate of a GEMM, 0.71 of the
-// sustained one); two images of 4096 tokens, 16 heads of 72 246 (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000
-// clocks where the tensor cores need 2048: the chain S -> weights -> O of either half (2400 clocks of weights, of which 1024 powers, and 1500 of
-// products and hand-overs) and shared memory, which the products' operands, opened codes and copies keep busy for 2560.  Timed and not kept: two threads a row
-// (16 warps: 441 for 430), the first weights by the last maximum while the new one is found (437), an eighth to a half of the powers by polynomials (431
-// to 502 for 445); of the first form, which took 548, core matrices 16 and 32 bytes off boundaries of 128, whose stores met in no bank (588).
+// B200, us: 4096 tokens behind 4096, 32 heads of 128 on 8 387 (1065 TFLOP/s of visible pairs, 0.64 of the measured burst rate of a GEMM, 0.76 of the
+// sustained one); two images of 4096 tokens, 16 heads of 72 241 (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000
+// clocks where the tensor cores need 2048: the chain S -> weights -> O of either half and its hand-overs.  Without powers it takes 0.99 of the time,
+// without maxima, sums and powers 0.96, without opening the records 0.95, with an eighth of S's product 0.84, with none of all that still 0.69.  So what
+// counts is how often there is something to wait for: P in one, two or four pieces 391, 387 and 415.  Timed and not kept: two threads a row (16 warps:
+// 441 for 430), the first weights by the last maximum while the new one is found (437), an eighth to a half of the powers by polynomials (431 to 502
+// for 445), S of 64 tokens twice so that the next one's product runs under a weighing (493, and 401 with a thread for the products of each half, but
+// images 257), issuing by lane 0 instead of an elected one (496 for 415); of the first form, which took 548, core matrices 16 and 32 bytes off
+// boundaries of 128, whose stores met in no bank (588).
 #include <math.h>
 
 #include <algorithm>
@@ -27,7 +30,7 @@ using namespace lqdev;
 
 namespace {
 
-constexpr int TILE = 128, KV = 128, SOFT_WARPS = 8, OPEN_WARPS = 7, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 32 * (MMA_WARP + 1);
+constexpr int TILE = 128, KV = 128, PIECES = 2, PIECE = KV / PIECES, SOFT_WARPS = 8, OPEN_WARPS = 7, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 32 * (MMA_WARP + 1);
 // Registers of a thread: as the block is launched (the kernel's bound, and what ptxas reports), and of the first kind and the others after setmaxnreg,
 // which takes from what the block was launched with and would wait for ever for more.
 constexpr int LAUNCH_REGS = 128, SOFT_REGS = 176, LEAN_REGS = 80;
@@ -54,7 +57,7 @@ struct Task {
 };
 
 struct Control {
-  uint64_t raw[OPEN_WARPS], q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2][4], o_full[2];
+  uint64_t raw[OPEN_WARPS], q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2][PIECES], o_full[2];
   uint32_t tmem;
   alignas(4) uint8_t missing[4][4];                 // of the last tiles: whether record i is no page's
   int abort_flag;
@@ -238,7 +241,7 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
       mbar_init(smem_u32(&c.k_empty[i]), 1);
       mbar_init(smem_u32(&c.v_empty[i]), 1);
       mbar_init(smem_u32(&c.s_full[i]), 1);
-      for (int x = 0; x < 4; ++x) mbar_init(smem_u32(&c.p_full[i][x]), 4);
+      for (int x = 0; x < PIECES; ++x) mbar_init(smem_u32(&c.p_full[i][x]), 4);
       mbar_init(smem_u32(&c.o_full[i]), 1);
     }
     for (int i = 0; i < OPEN_WARPS; ++i) mbar_init(smem_u32(&c.raw[i]), 1);
@@ -432,10 +435,11 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         for (int i = 0; i < 4; ++i) {
           weigh(v[i]);
           tmem_st_16(ts + 16 * i, w);                      // (over columns of S, which has been read)
+          if ((i + 1) % (PIECE / 32) != 0) continue;
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&c.p_full[half][i]));
+          if (lane == 0) mbar_arrive(smem_u32(&c.p_full[half][i / (PIECE / 32)]));
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
@@ -554,11 +558,11 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
           tc_mma<TC_F16>(tmem + COL_S + half * 128, make_smem_desc(a + x / 4 * TILE * 128 + x % 4 * 32), make_smem_desc(b + x / 4 * KV * 128 + x % 4 * 32), idesc_s,
                          x > 0);
       };
-      const auto product_o = [&](int half, int st, int piece, bool add) {          // 32 tokens
+      const auto product_o = [&](int half, int st, int piece, bool add) {          // of a piece
         const uint32_t b = smem_u32(sv + st * v_bytes(DP));
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int x = 2 * piece + y;
+        for (int y = 0; y < PIECE / 16; ++y) {
+          const int x = PIECE / 16 * piece + y;
           tc_mma_ta(tmem + COL_O + half * 128, tmem + COL_S + half * 128 + 8 * x, make_smem_desc(b + x / 4 * DP * 128 + x % 4 * 32), idesc_o, add || y > 0);
         }
       };
@@ -580,16 +584,16 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
           if (half == 0 && !wait(c.v_full[st], j >> 1, LQ_STAGE_MMA)) break;
           if (half == 0 && !last && !wait(c.k_full[next], (j + 1) >> 1, LQ_STAGE_MMA)) break;
 #pragma unroll
-          for (int x = 0; x < 3; ++x) {
+          for (int x = 0; x < PIECES - 1; ++x) {
             if (!wait(c.p_full[half][x], j, LQ_STAGE_MMA)) break;
             tc_fence_after();
             if (elect_one()) product_o(half, st, x, j > 0 || x > 0);
             __syncwarp();
           }
-          if (!wait(c.p_full[half][3], j, LQ_STAGE_MMA)) break;
+          if (!wait(c.p_full[half][PIECES - 1], j, LQ_STAGE_MMA)) break;
           tc_fence_after();
           if (elect_one()) {
-            product_o(half, st, 3, true);
+            product_o(half, st, PIECES - 1, true);
             if (half == halves - 1) tc_commit(smem_u32(&c.v_empty[st]));
             if (last) {
               tc_commit(smem_u32(&c.o_full[half]));
