@@ -12,7 +12,7 @@
 //
 // B200, us: 4096 tokens behind 4096, 32 heads of 128 on 8 387 (1065 TFLOP/s of visible pairs, 0.64 of the measured burst rate of a GEMM, 0.76 of the
 // sustained one); two images of 4096 tokens, 16 heads of 72 241 (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000
-// clocks where the tensor cores need 2048: the chain S -> weights -> O of either half and its hand-overs.  Without powers it takes 0.99 of the time,
+// clocks where the tensor cores need 2048: the chain S -> weights -> O of either half and its hand-overs.  With P in four pieces and no powers it took 0.99 of 415,
 // without maxima, sums and powers 0.96, without opening the records 0.95, with an eighth of S's product 0.84, with none of all that still 0.69.  So what
 // counts is how often there is something to wait for: P in one, two or four pieces 391, 387 and 415.  Timed and not kept: two threads a row (16 warps:
 // 441 for 430), the first weights by the last maximum while the new one is found (437), an eighth to a half of the powers by polynomials (431 to 502
