@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
   if (lo >= hi) return;
   Place here = sm.found;
 
-  const float scale = fmaxf(fabsf(p.scale), 1e-30f);       // (a scale of zero: all weights are one, and what is not seen stays -inf)
+  const float scale = lq_attn_scale(p);
   uint2 qb[Smem::Q_HERE ? 1 : NK][NT];
   const auto load_q = [&](const Place& at) {
     const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;              // of the signs of Q
@@ -250,7 +250,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
     }
     const int first_at = base + here.tile * ROWS / p.group, last_at = base + (here.tile * ROWS + rows - 1) / p.group;
     float o[NK][NT][4] = {};
-    float top[NT][2], sum[NT][2] = {};                     // top: what the weights are below, times scale; sum: of the lane's tokens
+    float top[NT][2], move[NT][2] = {}, sum[NT][2] = {};   // top: the rows' references; sum: of the lane's tokens
+    bool far = false;                                      // (some of the warp's rows' are)
 #pragma unroll
     for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
     // the warp's records are every WARPS-th of the block's
@@ -296,15 +297,16 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
                 if (!lq_sees(p, pos[n][x & 1], token0 + lq_kv_token(c8, 2 * a + (x >> 1)), here.q.rows.len)) s[a][n][x] = -INFINITY;
         }
         float high_s[NT][2];
-        bool grow = false;
+        bool grow = far;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
-            high_s[n][b] = scale * fmaxf(fmaxf(s[0][n][b], s[0][n][2 + b]), fmaxf(s[1][n][b], s[1][n][2 + b]));
-            grow = grow || high_s[n][b] > top[n][b] + GROWTH;
+            high_s[n][b] = fmaxf(fmaxf(s[0][n][b], s[0][n][2 + b]), fmaxf(s[1][n][b], s[1][n][2 + b]));
+            grow = grow || (high_s[n][b] - top[n][b]) * scale > GROWTH;
           }
         if (__any_sync(0xffffffffu, grow)) {
+          bool out = false;
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -314,17 +316,30 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
               for (int d = 4; d < 32; d *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
               m = fmaxf(m, top[n][b]);
               // (a row that has seen nothing yet has sums of zero)
-              const float by = top[n][b] == -INFINITY ? 1.f : ex2(top[n][b] - m);
+              const float by = top[n][b] == -INFINITY ? 1.f : ex2((top[n][b] - m) * scale);
               top[n][b] = m;
+              move[n][b] = lq_attn_move(m, scale);
+              out = out || lq_attn_far(m, scale);
               sum[n][b] *= by;
 #pragma unroll
               for (int g = 0; g < NK; ++g) { o[g][n][b] *= by; o[g][n][2 + b] *= by; }
             }
+          far = __any_sync(0xffffffffu, out);
+          if (far) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int b = 0; b < 2; ++b) {
+                const float off = lq_attn_far(top[n][b], scale) ? top[n][b] : 0.f;
+#pragma unroll
+                for (int a = 0; a < 2; ++a) { s[a][n][b] -= off; s[a][n][2 + b] -= off; }
+              }
+          }
         }
         uint2 w[2][NT];                                    // weights of 16 tokens: of words 2 a, of words 2 a + 1
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const float r0 = top[n][0] == -INFINITY ? 0.f : -top[n][0], r1 = top[n][1] == -INFINITY ? 0.f : -top[n][1];
+          const float r0 = move[n][0], r1 = move[n][1];
 #pragma unroll
           for (int a = 0; a < 2; ++a) {
             const float x0 = ex2(fmaf(s[a][n][0], scale, r0)), x1 = ex2(fmaf(s[a][n][1], scale, r1));
@@ -397,7 +412,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
 #pragma unroll
       for (int i = 0; i < WARPS; ++i) {
         if (tops[i] == -INFINITY) continue;
-        const float k = ex2(tops[i] - m);
+        const float k = ex2((tops[i] - m) * scale);
         const float4 v = *reinterpret_cast<const float4*>(&sm.sums[i][row][d]);
         n = fmaf(k, sm.total[i][row], n);
         x.x = fmaf(k, v.x, x.x); x.y = fmaf(k, v.y, x.y); x.z = fmaf(k, v.z, x.z); x.w = fmaf(k, v.w, x.w);
@@ -438,12 +453,12 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
               if (c + i >= parts) head[i].x = -INFINITY;
             }
             const float top = fmaxf(m, fmaxf(fmaxf(head[0].x, head[1].x), fmaxf(head[2].x, head[3].x)));
-            const float by = m == -INFINITY ? 0.f : ex2(m - top);
+            const float by = m == -INFINITY ? 0.f : ex2((m - top) * scale);
             n *= by; x.x *= by; x.y *= by; x.z *= by; x.w *= by;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               if (head[i].x == -INFINITY) continue;
-              const float k = ex2(head[i].x - top);
+              const float k = ex2((head[i].x - top) * scale);
               n = fmaf(k, head[i].y, n);
               x.x = fmaf(k, v[i].x, x.x); x.y = fmaf(k, v[i].y, x.y); x.z = fmaf(k, v[i].z, x.z); x.w = fmaf(k, v[i].w, x.w);
             }

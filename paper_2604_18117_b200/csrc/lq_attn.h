@@ -30,6 +30,15 @@ static inline int lq_attn_few(int sequences, int heads, int sms) { return 2ll * 
 lq_status lq_attn_tile_launch(const lq_kvcache* C, LqAttnParams p, cudaStream_t st);
 
 #ifdef __CUDACC__
+// A row's reference m is one of its products, as it is: the weight of product s is 2^((s - m) c).  Where c m is within LQ_ATTN_FAR, c s - c m in one
+// fused operation is that, but for the rounding of c m, at most 2^-15, which all weights below one m share.  Farther out half a step of c m is
+// added to every exponent, 16 and more from 2^28 on, and weights are infinite or nothing: there m is taken off the products first.
+constexpr float LQ_ATTN_FAR = 1024.f;
+__device__ __forceinline__ bool lq_attn_far(float m, float scale) { return m > -INFINITY && fabsf(m * scale) > LQ_ATTN_FAR; }
+// what c s is moved by, once m has been taken off s where it is far out; a row that has seen nothing yet has no m
+__device__ __forceinline__ float lq_attn_move(float m, float scale) { return m > -INFINITY && !lq_attn_far(m, scale) ? -m * scale : 0.f; }
+// c (its sign is the queries'); of a scale of zero: all weights are one, and what is not seen stays -inf
+__device__ __forceinline__ float lq_attn_scale(const LqAttnParams& p) { return fmaxf(fabsf(p.scale), 1e-30f); }
 // Tokens that any of the rows at places lo .. hi of a sequence may see, as blocks of 32: the first `sink` ones and those from `from` to `to` - 1;
 // the b-th of them, and how many.
 struct LqSeen {

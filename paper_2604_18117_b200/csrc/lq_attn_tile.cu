@@ -362,9 +362,10 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&c.q_full[half]));
       }
-      const float scale = fmaxf(fabsf(p.scale), 1e-30f);   // (a scale of zero: all weights are one, and what is covered stays -inf)
+      const float scale = lq_attn_scale(p);
       const uint32_t ts = tmem + ((uint32_t)(warp & 3) << 21) + COL_S + half * 128, to = ts + COL_O - COL_S;
-      float m = -INFINITY, l = 0.f;                        // m: what the weights are below, times scale
+      float m = -INFINITY, move = 0.f, l = 0.f;            // m: the row's reference
+      bool far = false;                                    // (some of the warp's rows' are)
       for (int j = 0; j < tiles; ++j) {
         if (!wait(c.s_full[half], j, LQ_STAGE_DRAIN)) break;
         tc_fence_after();
@@ -380,11 +381,10 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
         uint32_t w[16];
         float2 sum[2] = {};
         const auto weigh = [&](const uint32_t (&v)[32]) {
-          const float ref = m > -INFINITY ? -m : 0.f;
-          const float2 ref2 = make_float2(ref, ref);
+          const float2 move2 = make_float2(move, move);
 #pragma unroll
           for (int x = 0; x < 32; x += 2) {
-            float2 e = __ffma2_rn(make_float2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), scale2, ref2);
+            float2 e = __ffma2_rn(make_float2(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), scale2, move2);
             e.x = ex2(e.x); e.y = ex2(e.y);
             sum[x / 2 & 1] = __fadd2_rn(sum[x / 2 & 1], e);
             w[x / 2] = pack(e.x, e.y);
@@ -413,13 +413,13 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int x = 0; x < 32; x += 2) t[x / 2 & 3] = fmaxf(fmaxf(t[x / 2 & 3], __uint_as_float(v[i][x])), __uint_as_float(v[i][x + 1]));
-          top = scale * fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+          top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
         }
-        const bool grow = top > m + GROWTH || (m == -INFINITY && top > -INFINITY);
-        if (__any_sync(0xffffffffu, grow)) {
+        const bool grow = (top - m) * scale > GROWTH;      // (also of the first product that a row sees; not where both are -inf)
+        if (__any_sync(0xffffffffu, grow || far)) {
           // (a row that has seen nothing yet has sums of zero; its factor is one)
-          const float by = grow && m > -INFINITY ? ex2(m - top) : 1.f;
-          if (grow) { l *= by; m = top; }
+          const float by = grow && m > -INFINITY ? ex2((m - top) * scale) : 1.f;
+          if (grow) { l *= by; m = top; move = lq_attn_move(m, scale); }
           if (j > 0 && __any_sync(0xffffffffu, by != 1.f))
 #pragma unroll 1
             for (int x = 0; x < DP; x += 16) {
@@ -430,6 +430,14 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
               for (int y = 0; y < 16; ++y) u[y] = __float_as_uint(__uint_as_float(u[y]) * by);
               tmem_st_16(to + x, u);
             }
+          far = __any_sync(0xffffffffu, lq_attn_far(m, scale));
+          if (far) {
+            const float off = lq_attn_far(m, scale) ? m : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int x = 0; x < 32; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) - off);
+          }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -633,6 +641,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) lq_attn_join_kernel(const __g
   if (parts < 2 || row >= meta.w) return;
   const float* from = p.tile_part + (long long)blockIdx.x * p.splits * (DP + 2) * STEP + row;
   constexpr long long PART = (DP + 2) * STEP;
+  const float scale = lq_attn_scale(p);
   float m = -INFINITY, l = 0.f;
   for (int i = 0; i < parts; ++i) m = fmaxf(m, from[i * PART + DP * STEP]);
   const float ref = m > -INFINITY ? m : 0.f;
@@ -641,7 +650,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) lq_attn_join_kernel(const __g
   for (int g = 0; g < NK; ++g) o[g] = make_float2(0.f, 0.f);
   for (int i = 0; i < parts; ++i) {
     const float* at = from + i * PART;
-    const float by = ex2(at[DP * STEP] - ref);
+    const float by = ex2((at[DP * STEP] - ref) * scale);
     l = fmaf(by, at[(DP + 1) * STEP], l);
 #pragma unroll
     for (int g = 0; g < NK; ++g) {                         // entries 16 g + 2 warp and the next
