@@ -449,8 +449,8 @@ typedef struct {
 } lq_attn;
 
 /* Attention of the batch's rows over what the cache holds: out = sum_j w_j v_j / sum_j w_j, w_j = exp(scale q . k_j), j over the tokens that
- * the row sees.  Products on the tensor cores from halves, sums in fp32; weights are rounded to halves beside the values.  One token a
- * sequence, a few, whole prompts, or all of these in one batch.  No sum depends on the order of execution: equal calls give equal bits; a
+ * the row sees.  Products on the tensor cores from halves, sums in fp32; beside the values weights are rounded to halves, to 2^-11 of
+ * each down to 2^-21 of the largest and by at most 2^-32 of that below.  One token a sequence, a few, whole prompts, or all of these in one batch.  No sum depends on the order of execution: equal calls give equal bits; a
  * row may differ by rounding between calls of other batches.
  * rows * q_heads / kv_heads <= 2^30, rows * q_heads <= 2^34.  Attention calls of one cache, of any of its layers, share its workspace: they
  * must not overlap on the GPU (one stream, or events; graphs that were captured with one cache must not run side by side).

@@ -12,8 +12,8 @@
 // Within a block each warp takes every WARPS-th record, through a ring of its own in shared memory that bulk copies fill.  A record is opened
 // to halves in registers (a byte permutation and a packed subtraction for two codes), which are the first operands of m16n8k16 products: S^T =
 // K Q^T with 8 or 16 rows of Q as columns, so that no more products are made than rows ask for, and O^T = V^T W^T.  The rows' weights are
-// rounded to halves between the two (2^-11 of each) and turned round 8 x 8 at a time; sums, maxima and accumulators are fp32.  Accumulators
-// are only scaled when a row's maximum has grown by 8 or more (in powers of two): until then weights are up to 2^8.
+// rounded to halves between the two (lq_attn.h says what that keeps of small ones) and turned round 8 x 8 at a time; sums, maxima and accumulators are
+// fp32.  Accumulators are only scaled when a row's maximum has grown by 8 or more (in powers of two).
 //
 // B200, us in a graph of ten passes and TB/s of the visible codes: one token of 131072, 8 heads of 128, 32 queries 50.2, 5.3 (records stream at some
 // 7 TB/s once they do: 4 us of start, 2 to 3 of the join, the rest launch and end); 64 sequences of 1 to 8192 tokens 106, 5.1 (the same start and
@@ -31,7 +31,6 @@ using namespace lqdev;
 
 namespace {
 
-constexpr float GROWTH = 8.f;
 constexpr int SHORT = 4;                 // records a warp of a tile that is not shared out
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint2& b) {
@@ -303,7 +302,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) lq_attn_kernel(const __grid_con
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             high_s[n][b] = fmaxf(fmaxf(s[0][n][b], s[0][n][2 + b]), fmaxf(s[1][n][b], s[1][n][2 + b]));
-            grow = grow || (high_s[n][b] - top[n][b]) * scale > GROWTH;
+            grow = grow || (high_s[n][b] - top[n][b]) * scale > LQ_ATTN_GROWTH;
           }
         if (__any_sync(0xffffffffu, grow)) {
           bool out = false;

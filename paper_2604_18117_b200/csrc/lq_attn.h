@@ -33,10 +33,16 @@ lq_status lq_attn_tile_launch(const lq_kvcache* C, LqAttnParams p, cudaStream_t 
 // A row's reference m is one of its products, as it is: the weight of product s is 2^((s - m) c).  Where c m is within LQ_ATTN_FAR, c s - c m in one
 // fused operation is that, but for the rounding of c m, at most 2^-15, which all weights below one m share.  Farther out half a step of c m is
 // added to every exponent, 16 and more from 2^28 on, and weights are infinite or nothing: there m is taken off the products first.
-constexpr float LQ_ATTN_FAR = 1024.f;
+//
+// m is followed lazily, once a product is LQ_ATTN_GROWTH above it, and weights are all LQ_ATTN_LIFT powers of two larger than that: up to 2^15 as
+// halves (which go to 65504), so that small ones keep their 11 bits down to 2^-21 of m's, and are rounded by 2^-32 of it below.  (Without the lift
+// 100000 tokens that one outweighs by e^17 each were rounded up by half of what they weigh, by e^17.5 to nothing, while the sum had them.)
+constexpr float LQ_ATTN_FAR = 1024.f, LQ_ATTN_GROWTH = 8.f, LQ_ATTN_LIFT = 7.f;
 __device__ __forceinline__ bool lq_attn_far(float m, float scale) { return m > -INFINITY && fabsf(m * scale) > LQ_ATTN_FAR; }
 // what c s is moved by, once m has been taken off s where it is far out; a row that has seen nothing yet has no m
-__device__ __forceinline__ float lq_attn_move(float m, float scale) { return m > -INFINITY && !lq_attn_far(m, scale) ? -m * scale : 0.f; }
+__device__ __forceinline__ float lq_attn_move(float m, float scale) {
+  return m > -INFINITY && !lq_attn_far(m, scale) ? LQ_ATTN_LIFT - m * scale : LQ_ATTN_LIFT;
+}
 // c (its sign is the queries'); of a scale of zero: all weights are one, and what is not seen stays -inf
 __device__ __forceinline__ float lq_attn_scale(const LqAttnParams& p) { return fmaxf(fabsf(p.scale), 1e-30f); }
 // Tokens that any of the rows at places lo .. hi of a sequence may see, as blocks of 32: the first `sink` ones and those from `from` to `to` - 1;

@@ -7,8 +7,8 @@
 // swizzled rows, where no two lanes of a store meet in a bank); one thread issues the products; two groups of four warps have 128 rows each, a
 // row a thread, and take turns with the tensor cores: while one forms P of its rows, the products of the other run, and O's product follows P
 // 64 tokens at a time.  S and O stay in tensor memory.  P, as halves, takes the place of S and is the second product's A operand from
-// there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are up to 2^8,
-// which halves and sums hold as well, and the last division takes care of it.
+// there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are that much
+// larger, which halves and sums hold as well (lq_attn.h), and the last division takes care of it.
 //
 // B200, us: 4096 tokens behind 4096, 32 heads of 128 on 8 387 (1065 TFLOP/s of visible pairs, 0.64 of the measured burst rate of a GEMM, 0.76 of the
 // sustained one); two images of 4096 tokens, 16 heads of 72 241 (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000
@@ -37,7 +37,6 @@ constexpr int LAUNCH_REGS = 128, SOFT_REGS = 176, LEAN_REGS = 80;
 static_assert(SOFT_WARPS * SOFT_REGS + (OPEN_WARPS + 1) * LEAN_REGS <= THREADS / 32 * LAUNCH_REGS && THREADS % 128 == 0 && THREADS * LAUNCH_REGS <= 65536, "");
 constexpr int TMEM_COLS = 512;
 constexpr uint32_t COL_S = 0, COL_O = 256;                 // of the first 128 rows; the other's are 128 columns on
-constexpr float GROWTH = 8.f;
 constexpr int MIN_TILES = 4;             // of 128 tokens a thread block takes at least where a tile of rows is shared out
 
 // Operands are K-major rows of 128 bytes (64 halves), 128-byte swizzle; a wider K has panel after panel.  Q and K: rows are rows and tokens, 64
@@ -415,7 +414,7 @@ __global__ void __maxnreg__(LAUNCH_REGS) lq_attn_tile_kernel(const __grid_consta
             for (int x = 0; x < 32; x += 2) t[x / 2 & 3] = fmaxf(fmaxf(t[x / 2 & 3], __uint_as_float(v[i][x])), __uint_as_float(v[i][x + 1]));
           top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
         }
-        const bool grow = (top - m) * scale > GROWTH;      // (also of the first product that a row sees; not where both are -inf)
+        const bool grow = (top - m) * scale > LQ_ATTN_GROWTH;      // (also of the first product that a row sees; not where both are -inf)
         if (__any_sync(0xffffffffu, grow || far)) {
           // (a row that has seen nothing yet has sums of zero; its factor is one)
           const float by = grow && m > -INFINITY ? ex2((m - top) * scale) : 1.f;
