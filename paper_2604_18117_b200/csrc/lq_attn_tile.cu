@@ -110,9 +110,10 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// waits until all lanes have the value
+// Waits until all lanes' loads have come that v is made of, and holds back what follows: a fence hangs on the lanes' vote, so the vote's outcome, and with it
+// every lane's v, has to be there first.  (No lane has a v of zeros, whose codes would all be -128: the fence is not taken.)
 __device__ __forceinline__ void arrived(uint32_t v) {
-  asm volatile("{\n\t.reg .pred p;\n\t.reg .b32 r;\n\tsetp.ne.u32 p, %0, 0;\n\tvote.sync.ballot.b32 r, p, 0xffffffff;\n\t}" ::"r"(v) : "memory");
+  if (__ballot_sync(0xffffffffu, v != 0) == 0) fence_proxy_async();
 }
 __device__ __forceinline__ void sts_v2(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
 
@@ -125,7 +126,7 @@ __device__ __forceinline__ void open_keys(uint32_t from, uint32_t to, uint32_t h
   const int c8 = lane >> 2, t = lane & 3;
   const uint32_t high = lq_kv_high((int8_t)(head & 0xFF));
   const __half2 less = lq_kv_less(high);
-  uint32_t at[4];
+  uint32_t at[4], any = head;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = lq_kv_token(c8, i);
@@ -134,14 +135,13 @@ __device__ __forceinline__ void open_keys(uint32_t from, uint32_t to, uint32_t h
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     uint4 u[BATCH];
-    uint32_t any = 0;
 #pragma unroll
     for (int x = 0; x < BATCH; ++x)
       if (b * BATCH + x < NK) u[x] = lds_v4(from + 512 * (b * BATCH + x) + 16 * lane);
-    if (b == 1) {
 #pragma unroll
-      for (int x = 0; x < BATCH; ++x)
-        if (b * BATCH + x < NK) any |= u[x].w;
+    for (int x = 0; x < BATCH; ++x)
+      if (b * BATCH + x < NK) any |= u[x].w;
+    if (b == 1) {
       arrived(any);
       then();
     }
@@ -163,7 +163,7 @@ __device__ __forceinline__ void open_values(uint32_t from, uint32_t to, uint32_t
   const int c8 = lane >> 2, t = lane & 3;
   const uint32_t high = lq_kv_high((int8_t)(exponent & 0xFF));
   const __half2 less = lq_kv_less(high);
-  uint32_t at[4];
+  uint32_t at[4], any = exponent;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int chunk = 4 * upper + 2 * (i >> 1) + (t >> 1), row = 2 * c8 + (i & 1);
@@ -172,14 +172,13 @@ __device__ __forceinline__ void open_values(uint32_t from, uint32_t to, uint32_t
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     uint4 u[BATCH];
-    uint32_t any = 0;
 #pragma unroll
     for (int x = 0; x < BATCH; ++x)
       if (b * BATCH + x < NK) u[x] = lds_v4(from + 512 * (b * BATCH + x) + 16 * lane);
-    if (b == 1) {
 #pragma unroll
-      for (int x = 0; x < BATCH; ++x)
-        if (b * BATCH + x < NK) any |= u[x].w;
+    for (int x = 0; x < BATCH; ++x)
+      if (b * BATCH + x < NK) any |= u[x].w;
+    if (b == 1) {
       arrived(any);
       then();
     }
