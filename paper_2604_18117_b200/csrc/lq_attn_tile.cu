@@ -32,7 +32,7 @@ namespace {
 
 constexpr int TILE = 128, KV = 128, PIECES = 2, PIECE = KV / PIECES, SOFT_WARPS = 8, OPEN_WARPS = 7, MMA_WARP = SOFT_WARPS + OPEN_WARPS, THREADS = 32 * (MMA_WARP + 1);
 // Registers of a thread: as the block is launched (the kernel's bound, and what ptxas reports), and of the first kind and the others after setmaxnreg,
-// which takes from what the block was launched with and would wait for ever for more.
+// which takes from what the block was launched with and would wait for ever for more (every instance's own count is checked in lq_attn_tile_prepare).
 constexpr int LAUNCH_REGS = 128, SOFT_REGS = 176, LEAN_REGS = 80;
 static_assert(SOFT_WARPS * SOFT_REGS + (OPEN_WARPS + 1) * LEAN_REGS <= THREADS / 32 * LAUNCH_REGS && THREADS % 128 == 0 && THREADS * LAUNCH_REGS <= 65536, "");
 constexpr int TMEM_COLS = 512;
@@ -683,8 +683,11 @@ auto with_size(int Dp, const F& f) {
 
 lq_status lq_attn_tile_prepare(const lq_kvcache* C) {
   return with_size(C->Dp, [&](auto* kernel, auto*) {
-           return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tile_smem(C->Dp)));
-         }) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+    cudaFuncAttributes at;
+    if (lq_note_cuda(cudaFuncGetAttributes(&at, kernel)) != cudaSuccess) return LQ_ERR_CUDA;
+    if (at.numRegs < LAUNCH_REGS) return LQ_ERR_UNSUPPORTED;
+    return lq_note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tile_smem(C->Dp))) == cudaSuccess ? LQ_OK : LQ_ERR_CUDA;
+  });
 }
 
 lq_status lq_attn_tile_launch(const lq_kvcache* C, LqAttnParams p, cudaStream_t st) {
