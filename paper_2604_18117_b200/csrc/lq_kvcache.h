@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 
 #include "lq_internal.h"
+#include "lq_kv_rows.h"
 
 // A record holds 32 tokens of one head: 32 bytes that begin with the exponents of keys and values, the keys, the values.  Codes are kept as
 // bytes u = c + 128, in the order in which a warp of the attention kernels reads them as operands of m16n8k16 products, 16 bytes a lane
@@ -63,8 +64,9 @@ struct LqSeq {
 __device__ __forceinline__ LqSeq lq_seq(const LqBatch& b, int s) {
   LqSeq q;
   if (b.row_start) {
-    q.row = max(0, min(b.row_start[s], b.rows));
-    q.n = max(0, min(b.row_start[s + 1], b.rows) - q.row);
+    const LqRowRange r = lq_kv_rows(b.row_start[s], b.row_start[s + 1], b.rows);
+    q.row = r.row;
+    q.n = r.n;
   } else {
     q.row = s * b.each;
     q.n = b.each;

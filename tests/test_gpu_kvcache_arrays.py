@@ -1,0 +1,45 @@
+"""The arrays of a batch: what they may hold, and where they may lie."""
+import numpy as np
+import pytest
+
+from paper_2604_18117_b200 import binding as B
+
+from .test_gpu_kvcache import attend, filled
+
+pytestmark = pytest.mark.gpu
+
+LOW, HIGH = -2 ** 31, 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("many", [1, 60])
+def test_first_rows_that_are_none(many):
+    """Ends far below their starts, starts below zero, ends behind the call's rows: nothing but the call's rows is touched, and what the last sequence has for
+    itself is right."""
+    import torch
+    lens = [40, 10 * many, 100, 500]
+    c = filled(64, 2, lens, 32)
+    rows = 8 * many + 3
+    starts = [[5 * many, LOW, 6 * many, 6 * many, 8 * many], [LOW, LOW, LOW + 1, 6 * many, 8 * many], [HIGH, -1, 6 * many, 6 * many, 8 * many],
+              [HIGH, LOW, HIGH, 6 * many, 8 * many]]
+    for start in starts:
+        x = torch.randn(rows, 4, 64, dtype=torch.float16, device="cuda")
+        out = torch.full((rows + 64, 4, 64), 7.0, dtype=torch.float16, device="cuda")
+        sd, ld = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in (start, lens))
+        b = B.lq_kvbatch(4, rows, ld.data_ptr(), c.pages_d.data_ptr(), c.stride, sd.data_ptr())
+        st = torch.cuda.current_stream().cuda_stream
+        B.lq_cache_attention(c.h, 0, b, B.lq_attn(x.data_ptr(), (256, 64), out.data_ptr(), (256, 64), 4, 0.1), st)
+        torch.cuda.synchronize()
+        assert (out[rows:] == 7).all()
+        clamp = lambda v: min(max(v, 0), rows)
+        if any(clamp(a) < clamp(e) and clamp(e) > 6 * many for a, e in zip(start[:3], start[1:4])):
+            continue                                       # (another one has its rows too)
+        want, err = attend(x[6 * many:8 * many].double().cpu().numpy(), c.held[0][3][:500], c.held[1][3][:500], 0.1, 500 - 2 * many, True, 0, 0)
+        assert (np.abs(out[6 * many:8 * many].double().cpu().numpy() - want) <= err).all()
+        # the same to write: its last tokens, as they are there already
+        keys = torch.zeros(rows, 2, 2, 64, device="cuda")
+        for side in range(2):
+            keys[6 * many:8 * many, side] = torch.from_numpy(c.held[side][3][500 - 2 * many:500]).float()
+        B.lq_kvcache_append(c.h, 0, b, B.lq_kvrows(keys.data_ptr(), (0, 256, 64), keys[:, 1].data_ptr(), (0, 256, 64)), B.OUT_F32, st)
+        torch.cuda.synchronize()
+    B.lq_get_device_status(0)                              # (some of them do not fit their lengths)
+    B.lq_kvcache_free(c.h)
