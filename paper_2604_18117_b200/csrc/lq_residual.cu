@@ -290,7 +290,9 @@ extern "C" lq_status lq_residual_norm(const lq_residual* r, void* stream) {
   p.groups = p.seq_groups * (p.rows / p.seq_rows);
   const size_t smem = 3 * (size_t)p.features * sizeof(float);
   const auto launch = [&](auto* kernel) {
-    const cudaError_t c = smem > 47 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+    // (the widest call's: the limit is the kernel's, for all threads, and a call that set its own would lower it under another's launch)
+    const int most = 3 * LQ_MAX_K * (int)sizeof(float);
+    const cudaError_t c = smem > 47 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) : cudaSuccess;
     if (c != cudaSuccess) return c;
     // Neighbouring groups to a thread block, as many blocks as are resident at once: with seven and nine fours a lane two an SM (us of 32768 rows of
     // 2240, fp32 stream, with 2 / 3 / 4 / 8 / 16 blocks an SM: 151 / 184 / 153 / 158 / 175; of 8192 rows of 1152 14.9 / 19.5 / 16.7 / 19.7 / 19.6).
