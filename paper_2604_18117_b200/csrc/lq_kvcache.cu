@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(THREADS) lq_kv_append_kernel(const __grid_cons
       r = q.row + q.n;
       continue;
     }
-    const int at = q.len - q.n + (r - q.row), t0 = at % LQ_KV_BLOCK, t1 = min(LQ_KV_BLOCK, t0 + q.row + q.n - r);
+    const int at = q.len - q.n + (r - q.row), t0 = at % LQ_KV_BLOCK, t1 = min(LQ_KV_BLOCK, t0 + (q.row + q.n - r));
     if (r == q.row || t0 == 0) {
       const int block = at / LQ_KV_BLOCK, slot = lq_kv_slot(p.b, block), page = p.b.pages[(long long)s * p.b.page_stride + slot];
       const T* rows = in + r * p.row[side];
@@ -499,7 +499,7 @@ extern "C" lq_status lq_kvcache_append(lq_kvcache* C, int32_t layer, const lq_kv
   // Rows a thread block looks through: 32, as many as a block of tokens has, once that gives every SM eight; with fewer rows fewer, so that
   // single tokens of different sequences are not one's.
   p.tile = (int)std::max(1ll, std::min(32ll, (long long)C->heads * p.b.rows / (8ll * C->sms)));
-  const long long blocks = (long long)C->heads * lq_ceil_div(p.b.rows, p.tile);
+  const long long blocks = C->heads * (1ll + (p.b.rows - 1) / p.tile);
   if (blocks > 0x7fffffffll) return LQ_ERR_UNSUPPORTED;
   const auto launch = [&](auto* kernel) { return lq_launch(kernel, (int)blocks, THREADS, 0, (cudaStream_t)stream, p); };
   const cudaError_t e = dt == LQ_OUT_F16 ? (C->D <= 128 ? launch(lq_kv_append_kernel<__half, 1>) : launch(lq_kv_append_kernel<__half, 2>))

@@ -4,7 +4,7 @@ import pytest
 
 from paper_2604_18117_b200 import binding as B
 
-from .test_gpu_kvcache import attend, filled
+from .test_gpu_kvcache import Cache, attend, filled, write
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +43,28 @@ def test_first_rows_that_are_none(many):
         torch.cuda.synchronize()
     B.lq_get_device_status(0)                              # (some of them do not fit their lengths)
     B.lq_kvcache_free(c.h)
+
+
+@pytest.mark.parametrize("rows", [HIGH, HIGH - 30, HIGH - 31, HIGH - 32])
+def test_as_many_rows_as_there_are_numbers(rows):
+    """Calls of up to 2^31 - 1 rows, of which the first sequence begins far behind."""
+    import torch
+    c = Cache(16, 1, [60, 90], 32)
+    c.append([20, 3])
+    ns = [10, 39]
+    first = rows - sum(ns)
+    x = c.values(2 * sum(ns)).astype(np.float16)
+    buf = torch.from_numpy(x).cuda().view(sum(ns), 2, 16)
+    c.len = [a + n for a, n in zip(c.len, ns)]
+    sd, ld = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([first, first + ns[0], rows], c.len))
+    b = B.lq_kvbatch(2, rows, ld.data_ptr(), c.pages_d.data_ptr(), c.stride, sd.data_ptr())
+    k, v = (buf[:, i].data_ptr() - first * 64 for i in range(2))                # (where row 0 would lie)
+    B.lq_kvcache_append(c.h, 0, b, B.lq_kvrows(k, (0, 32, 16), v, (0, 32, 16)), B.OUT_F16, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for side in range(2):
+        at = 0
+        for s, n in enumerate(ns):
+            write(c.held[side][s], c.exps[side][s], x.reshape(sum(ns), 2, 1, 16)[at:at + n, side].astype(np.float64), c.len[s] - n)
+            at += n
+    c.check()
+    c.close()
