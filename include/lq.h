@@ -428,16 +428,16 @@ lq_status lq_kvcache_append(lq_kvcache* cache, int32_t layer, const lq_kvbatch* 
 /* Reads tokens begin .. length - 1 of each sequence, at most max_tokens of them, into rows 0, 1, .. of its part of the output; what lies
  * behind stays.  Values are exact in either type.  (Uses the batch's sequences, lengths and pages alone.)
  *   begin_dev  [sequences] int32, device, >= 0; NULL: from the first token on
- *   rows       k or v may be NULL (not wanted); no two entries on one place (INVALID_ARG; UNSUPPORTED where dimensions run through one
- *              another too often to tell)
+ *   rows       k or v may be NULL (not wanted); no two entries on one place and none on lengths, pages or begin_dev (INVALID_ARG;
+ *              UNSUPPORTED where dimensions run through one another too often to tell)
  * Asynchronous on `cuda_stream`. */
 lq_status lq_kvcache_read(const lq_kvcache* cache, int32_t layer, const lq_kvbatch* batch, const int32_t* begin_dev, int32_t max_tokens,
                           const lq_kvrows* rows, lq_out_dtype dtype, void* cuda_stream);
 
 typedef struct {
   const void* q;                           /* device, half, 16-byte aligned, finite: entry d of head h of row i at i * q_row + h * q_head + d */
-  void* out;                               /* the same, of what the row's head attends to; apart from q, no two entries on one place
-                                              (INVALID_ARG; UNSUPPORTED where it cannot be told)                      */
+  void* out;                               /* the same, of what the row's head attends to; apart from q and the batch's arrays, no two
+                                              entries on one place (INVALID_ARG; UNSUPPORTED where it cannot be told) */
   int64_t q_row, q_head;                   /* strides in elements, multiples of 8, below 2^40 in magnitude            */
   int64_t out_row, out_head;
   int32_t q_heads;                         /* a multiple of the cache's heads, up to 4096: heads h * q_heads / kv_heads and on share head h   */

@@ -528,7 +528,7 @@ extern "C" lq_status lq_cache_attention(const lq_kvcache* C, int32_t layer, cons
   const LqRuns q{(uintptr_t)a->q, {2 * a->q_row, 2 * a->q_head, 0}, {p.b.rows, a->q_heads, 1}, 2ll * C->D};
   const LqRuns out{(uintptr_t)a->out, {2 * a->out_row, 2 * a->out_head, 0}, {p.b.rows, a->q_heads, 1}, 2ll * C->D};
   const auto status = [](LqPlaces c) { return c == LQ_APART ? LQ_OK : c == LQ_SHARED ? LQ_ERR_INVALID_ARG : LQ_ERR_UNSUPPORTED; };
-  if ((s = status(lq_runs_collide(out))) != LQ_OK || (s = status(lq_runs_meet(out, q))) != LQ_OK) return s;
+  if ((s = status(lq_runs_collide(out))) != LQ_OK || (s = status(lq_runs_meet(out, q))) != LQ_OK || (s = status(lq_batch_meets(p.b, p.b.row_start, p.b.sequences + 1, out))) != LQ_OK) return s;
   LqDeviceGuard guard(C->device);
   if (!guard.ok) return LQ_ERR_CUDA;
   p.records = lq_kv_layer(C, layer);

@@ -432,6 +432,16 @@ lq_status lq_take_batch(const lq_kvcache* C, int32_t layer, const lq_kvbatch* b,
   return LQ_OK;
 }
 
+LqPlaces lq_batch_meets(const LqBatch& b, const int32_t* more, int entries, const LqRuns& out) {
+  const auto line = [](const int32_t* at, int64_t n) { return LqRuns{(uintptr_t)at, {0, 0, 0}, {1, 1, 1}, 4 * n}; };
+  const LqRuns arrays[3] = {line(b.length, b.sequences), line(b.pages, (int64_t)b.sequences * b.page_stride), line(more, entries)};
+  for (const LqRuns& a : arrays) {
+    const LqPlaces c = a.at ? lq_runs_meet(out, a) : LQ_APART;
+    if (c != LQ_APART) return c;
+  }
+  return LQ_APART;
+}
+
 extern "C" lq_status lq_kvcache_create(int32_t layers, int32_t pages, int32_t page_tokens, int32_t kv_heads, int32_t head_dim, int device,
                                        lq_kvcache** out) {
   if (!out || layers < 1 || pages < 1 || page_tokens < 1 || kv_heads < 1 || head_dim < 1) return LQ_ERR_INVALID_ARG;
@@ -518,7 +528,7 @@ extern "C" lq_status lq_kvcache_read(const lq_kvcache* C, int32_t layer, const l
   // (no sequence has more tokens than its row of pages)
   p.most = (int)std::min((long long)most, (long long)p.b.page_stride * C->page_tokens);
   p.blocks = (int)(((long long)p.most + 2 * LQ_KV_BLOCK - 2) / LQ_KV_BLOCK);
-  // no two entries of the outputs on one place
+  // no two entries of the outputs on one place, and none on the arrays
   LqRuns out[2];
   int n = 0;
   for (int i = 0; i < 2; ++i)
@@ -528,7 +538,7 @@ extern "C" lq_status lq_kvcache_read(const lq_kvcache* C, int32_t layer, const l
     }
   const auto status = [](LqPlaces c) { return c == LQ_APART ? LQ_OK : c == LQ_SHARED ? LQ_ERR_INVALID_ARG : LQ_ERR_UNSUPPORTED; };
   for (int i = 0; i < n; ++i)
-    if ((s = status(lq_runs_collide(out[i]))) != LQ_OK) return s;
+    if ((s = status(lq_runs_collide(out[i]))) != LQ_OK || (s = status(lq_batch_meets(p.b, begin, p.b.sequences, out[i]))) != LQ_OK) return s;
   if (n == 2 && (s = status(lq_runs_meet(out[0], out[1]))) != LQ_OK) return s;
   LqDeviceGuard guard(C->device);
   if (!guard.ok) return LQ_ERR_CUDA;

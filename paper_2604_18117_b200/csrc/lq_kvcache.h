@@ -4,6 +4,7 @@
 
 #include <cuda_fp16.h>
 
+#include "lq_heads_places.h"
 #include "lq_internal.h"
 #include "lq_kv_rows.h"
 
@@ -49,6 +50,9 @@ struct LqBatch {
 
 // checks a caller's batch against a cache; LQ_OK fills *out
 lq_status lq_take_batch(const lq_kvcache* C, int32_t layer, const lq_kvbatch* b, LqBatch* out);
+// whether an output lies on a batch's arrays, which blocks of a launch still read while others write theirs: lengths, pages, and
+// `entries` entries of one more (which may be NULL)
+LqPlaces lq_batch_meets(const LqBatch& b, const int32_t* more, int entries, const LqRuns& out);
 static inline uint8_t* lq_kv_layer(const lq_kvcache* C, int layer) {
   return C->d_records + (size_t)layer * C->pages * (C->page_tokens / LQ_KV_BLOCK) * C->heads * lq_kv_record_bytes(C->Dp);
 }

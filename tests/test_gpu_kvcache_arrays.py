@@ -68,3 +68,42 @@ def test_as_many_rows_as_there_are_numbers(rows):
             at += n
     c.check()
     c.close()
+
+
+def code(f, *a):
+    try:
+        f(*a)
+    except B.LqError as e:
+        return e.code
+    return 0
+
+
+def test_outputs_lie_on_no_array():
+    """An array of the batch, whole or its last entry, inside an output, in a gap of it and right behind it."""
+    import torch
+    c = B.lq_kvcache_create(1, 8, 32, 1, 64)
+    S = 4
+    buf = torch.zeros(4096, dtype=torch.float16, device="cuda")
+    other = torch.zeros(64, dtype=torch.int32, device="cuda")
+    q = torch.zeros(S * 64, dtype=torch.float16, device="cuda")
+    apart = {"length": other.data_ptr(), "pages": other.data_ptr() + 64, "start": other.data_ptr() + 128, "begin": other.data_ptr() + 192}
+    size = {"length": S, "pages": 2 * S, "start": S + 1, "begin": S}
+    out = buf.data_ptr() + 1024                            # rows of 64 halves, 192 apart: 128 bytes in 384
+    end = out + 3 * 384 + 128
+    for name in size:
+        n = 4 * size[name]
+        for at, want in ((out, 1), (out + 384 + 124, 1), (out - n + 4, 1), (end - 4, 1), (out + 128, 0), (out + 384 - n, 0), (out - n, 0), (end, 0)):
+            a = {**apart, name: at}
+            b = B.lq_kvbatch(S, S, a["length"], a["pages"], 2, a["start"])
+            o = B.lq_kvrows(out, (192, 64, 64), None, (0, 0, 0)), B.lq_kvrows(None, (0, 0, 0), out, (192, 64, 64))
+            if name != "begin":
+                assert code(B.lq_cache_attention, c, 0, b, B.lq_attn(q.data_ptr(), (64, 64), out, (192, 64), 1, 0.1)) == want, (name, at - out)
+            for r in o:
+                if name != "start":                          # (which reading does not use)
+                    assert code(B.lq_kvcache_read, c, 0, b, a["begin"], 1, r) == want, (name, at - out)
+                else:
+                    assert code(B.lq_kvcache_read, c, 0, b, a["begin"], 1, r) == 0
+    torch.cuda.synchronize()
+    B.lq_get_device_status(0)                              # (the arrays' zeros are lengths below their rows)
+    assert (buf == 0).all()
+    B.lq_kvcache_free(c)
