@@ -426,7 +426,8 @@ typedef struct {
 lq_status lq_kvcache_append(lq_kvcache* cache, int32_t layer, const lq_kvbatch* batch, const lq_kvrows* rows, lq_out_dtype dtype, void* cuda_stream);
 
 /* Reads tokens begin .. length - 1 of each sequence, at most max_tokens of them, into rows 0, 1, .. of its part of the output; what lies
- * behind stays.  Values are exact in either type.  (Uses the batch's sequences, lengths and pages alone.)
+ * behind stays.  Values are exact in either type.  Uses the batch's sequences, lengths and pages alone; rows and row_start have to be such as the
+ * other calls take, and what row_start points to is not read (rows = 0 and NULL will do).
  *   begin_dev  [sequences] int32, device, >= 0; NULL: from the first token on
  *   rows       k or v may be NULL (not wanted); no two entries on one place and none on lengths, pages or begin_dev (INVALID_ARG;
  *              UNSUPPORTED where dimensions run through one another too often to tell)

@@ -107,3 +107,21 @@ def test_outputs_lie_on_no_array():
     B.lq_get_device_status(0)                              # (the arrays' zeros are lengths below their rows)
     assert (buf == 0).all()
     B.lq_kvcache_free(c)
+
+
+def test_reading_wants_no_rows():
+    """Rows of none, first rows of none or anywhere: the same is read.  Rows that the sequences cannot share alike are refused here too."""
+    import torch
+    lens = [40, 10, 77]
+    c = filled(64, 2, lens, 32)
+    ld, wild = torch.tensor(lens, dtype=torch.int32, device="cuda"), torch.tensor([HIGH, LOW, -3, 5], dtype=torch.int32, device="cuda")
+    out = torch.zeros(3, 3, 77, 2, 64, device="cuda")
+    for i, (rows, start) in enumerate(((0, None), (6, None), (1000, wild.data_ptr()))):
+        r = B.lq_kvrows(out[i].data_ptr(), (77 * 128, 128, 64), None, (0, 0, 0))
+        B.lq_kvcache_read(c.h, 0, B.lq_kvbatch(3, rows, ld.data_ptr(), c.pages_d.data_ptr(), c.stride, start), None, 77, r, B.OUT_F32)
+    torch.cuda.synchronize()
+    for got in out.double().cpu().numpy():
+        for s, n in enumerate(lens):
+            assert np.array_equal(got[s, :n], c.held[0][s][:n]) and (got[s, n:] == 0).all()
+    assert code(B.lq_kvcache_read, c.h, 0, B.lq_kvbatch(3, 4, ld.data_ptr(), c.pages_d.data_ptr(), c.stride), None, 77, r, B.OUT_F32) == 1
+    c.close()
