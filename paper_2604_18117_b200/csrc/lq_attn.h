@@ -53,12 +53,13 @@ struct LqSeen {
   __device__ __forceinline__ int block(int b) const { return b < sink ? b : b - sink + from; }
 };
 __device__ __forceinline__ LqSeen lq_seen(const LqAttnParams& p, int lo, int hi, int len) {
-  LqSeen s{0, 0, (len + LQ_KV_BLOCK - 1) / LQ_KV_BLOCK};
+  const auto blocks = [](int tokens) { return (int)(((uint32_t)tokens + LQ_KV_BLOCK - 1) / LQ_KV_BLOCK); };
+  LqSeen s{0, 0, blocks(len)};
   if (p.causal) {
     s.to = hi / LQ_KV_BLOCK + 1;
     if (p.window > 0 && lo >= p.window) {
       s.from = (lo - p.window + 1) / LQ_KV_BLOCK;
-      s.sink = min(s.from, (min(p.sinks, len) + LQ_KV_BLOCK - 1) / LQ_KV_BLOCK);
+      s.sink = min(s.from, blocks(min(p.sinks, len)));
     }
   }
   return s;
