@@ -15,9 +15,11 @@
 // rounded to halves between the two (lq_attn.h says what that keeps of small ones) and turned round 8 x 8 at a time; sums, maxima and accumulators are
 // fp32.  Accumulators are only scaled when a row's maximum has grown by 8 or more (in powers of two).
 //
-// B200, us in a graph of ten passes and TB/s of the visible codes: one token of 131072, 8 heads of 128, 32 queries 50.2, 5.3 (records stream at some
-// 7 TB/s once they do: 4 us of start, 2 to 3 of the join, the rest launch and end); 64 sequences of 1 to 8192 tokens 106, 5.1 (the same start and
-// joins at three to six tiles a block); 24 times three tokens, window 1000, 2 heads of 80 14.9; one token of 300 6.8, a chain of latencies.
+// B200, us of passes back to back in graphs and TB/s of the visible codes: one token of 131072, 8 heads of 128, 32 queries 50.4, 5.3 (records stream at
+// some 7 TB/s once they do: 4 us of start, 2 to 3 of the join, the rest launch and end); 64 sequences of 1 to 8192 tokens 107.5, 5.0 (the same start
+// and joins at three to six tiles a block), with 4 heads of 256 for 16 queries 101, 5.3; 24 times three tokens, window 1000, 2 heads of 80 14.7; one token
+// of 300 6.6, a chain of latencies.  Prompts of heads above 128 entries, which have no other form: 2048 tokens of 4096, 16 heads on 4 of 256 931, 111
+// TFLOP/s.
 // With 16 rows where 8 would do (both products at twice the width) the long sequence took 89 us, with a ring of three, one or 16 warps' records
 // the same as with this one.
 #include <math.h>

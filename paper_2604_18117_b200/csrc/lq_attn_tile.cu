@@ -10,9 +10,11 @@
 // there.  O is only scaled when a row's maximum has grown by 8 or more (in powers of two) since it was last: until then weights are that much
 // larger, which halves and sums hold as well (lq_attn.h), and the last division takes care of it.
 //
-// B200, us: 4096 tokens behind 4096, 32 heads of 128 on 8 387 (1065 TFLOP/s of visible pairs, 0.64 of the measured burst rate of a GEMM, 0.76 of the
-// sustained one); two images of 4096 tokens, 16 heads of 72 241 (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000
-// clocks where the tensor cores need 2048: the chain S -> weights -> O of either half and its hand-overs.  With P in four pieces and no powers it took 0.99 of 415,
+// B200, us of passes back to back in graphs: 4096 tokens behind 4096, 32 heads of 128 on 8 414 at 1.83 GHz, which the power limit leaves (996 TFLOP/s of
+// visible pairs, 0.59 of the measured burst rate of a GEMM, 0.71 of the sustained one; the first ten passes after a pause 396 each); two images of 4096
+// tokens, 16 heads of 72 242 at 1.965 GHz (119 of them are the powers' at 16 a clock).  A tile of 128 tokens takes some 4000 clocks where the tensor
+// cores need 2048: the chain S -> weights -> O of either half and its hand-overs.  What follows is of ten passes after a pause, side by side in the builds
+// of their time, and good for comparison alone.  With P in four pieces and no powers it took 0.99 of 415,
 // without maxima, sums and powers 0.96, without opening the records 0.95, with an eighth of S's product 0.84, with none of all that still 0.69.  So what
 // counts is how often there is something to wait for: P in one, two or four pieces 391, 387 and 415.  Timed and not kept: two threads a row (16 warps:
 // 441 for 430), the first weights by the last maximum while the new one is found (437), an eighth to a half of the powers by polynomials (431 to 502

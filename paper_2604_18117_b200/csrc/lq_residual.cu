@@ -7,7 +7,7 @@
 // kept as they lie in memory until they are used, so that many rows are on their way.  What a row is multiplied with and what is added is
 // put together once for a sequence's rows of a thread block, in shared memory, and arithmetic goes two entries at a time: with five vectors
 // from global memory a row and entry by entry the issue of instructions took most of the time (32768 rows of 2240, fp32 stream: 369 us; now
-// 151 us, 5.8 TB/s, 0.89 of the measured copy rate).
+// 151 us, 5.8 TB/s, 0.89 of the measured copy rate, after a pause, and 154 back to back).
 // Variances are sums about the mean that is known; h is made of x' before that is rounded to its type.
 #include <cuda_fp16.h>
 #include <math.h>
@@ -295,7 +295,10 @@ extern "C" lq_status lq_residual_norm(const lq_residual* r, void* stream) {
     const cudaError_t c = smem > 47 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) : cudaSuccess;
     if (c != cudaSuccess) return c;
     // Neighbouring groups to a thread block, as many blocks as are resident at once: with seven and nine fours a lane two an SM (us of 32768 rows of
-    // 2240, fp32 stream, with 2 / 3 / 4 / 8 / 16 blocks an SM: 151 / 184 / 153 / 158 / 175; of 8192 rows of 1152 14.9 / 19.5 / 16.7 / 19.7 / 19.6).
+    // 2240, fp32 stream, with 2 / 3 / 4 / 8 / 16 blocks an SM: 151 / 184 / 153 / 158 / 175; of 8192 rows of 1152 14.9 / 19.5 / 16.7 / 19.7 / 19.6; with 2 / 3 /
+    // 4 / 8: 16384 rows of 4096, fp32 stream 147 / 182 / 151 / 159, fp16 117 / 145 / 122 / 128; 8192 of 8192, fp32 171 / 207 / 178 / 189, fp16 137 / 166 / 145 /
+    // 153; 20000 of 3200, fp16 121 / 149 / 125 / 133).  Of the other numbers one has been timed, five fours a lane (20000 rows of 5120, fp16: 237 / 179 /
+    // 223 / 197): three would be better there than the four that it takes.
     p.share = 1 + (p.groups - 1) / (sms * (held > 5 ? 2 : held > 2 ? 4 : 8));
     return lq_launch(kernel, 1 + (p.groups - 1) / p.share, THREADS, smem, (cudaStream_t)stream, p);
   };
