@@ -422,7 +422,7 @@ typedef struct {
 
 /* Writes the batch's rows, finite keys and values, as each sequence's last tokens: tokens length - n .. length - 1 of one with n rows
  * (length >= n).  A token that is the first of its 32 begins them anew.  Pages that are written belong to one sequence of the batch.
- * Asynchronous on `cuda_stream`. */
+ * kv_heads * ceil(rows / 32) < 2^31, else UNSUPPORTED.  Asynchronous on `cuda_stream`. */
 lq_status lq_kvcache_append(lq_kvcache* cache, int32_t layer, const lq_kvbatch* batch, const lq_kvrows* rows, lq_out_dtype dtype, void* cuda_stream);
 
 /* Reads tokens begin .. length - 1 of each sequence, at most max_tokens of them, into rows 0, 1, .. of its part of the output; what lies
@@ -431,6 +431,7 @@ lq_status lq_kvcache_append(lq_kvcache* cache, int32_t layer, const lq_kvbatch* 
  *   begin_dev  [sequences] int32, device, >= 0; NULL: from the first token on
  *   rows       k or v may be NULL (not wanted); no two entries on one place and none on lengths, pages or begin_dev (INVALID_ARG;
  *              UNSUPPORTED where dimensions run through one another too often to tell)
+ * kv_heads * sequences * (max_tokens / 32 + 2) < 2^31 (max_tokens, or page_stride * page_tokens where that is less), else UNSUPPORTED.
  * Asynchronous on `cuda_stream`. */
 lq_status lq_kvcache_read(const lq_kvcache* cache, int32_t layer, const lq_kvbatch* batch, const int32_t* begin_dev, int32_t max_tokens,
                           const lq_kvrows* rows, lq_out_dtype dtype, void* cuda_stream);

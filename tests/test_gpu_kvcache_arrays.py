@@ -125,3 +125,15 @@ def test_reading_wants_no_rows():
             assert np.array_equal(got[s, :n], c.held[0][s][:n]) and (got[s, n:] == 0).all()
     assert code(B.lq_kvcache_read, c.h, 0, B.lq_kvbatch(3, 4, ld.data_ptr(), c.pages_d.data_ptr(), c.stride), None, 77, r, B.OUT_F32) == 1
     c.close()
+
+
+def test_calls_of_more_thread_blocks_than_a_launch_has():
+    c = B.lq_kvcache_create(1, 1, 32, 4096, 8)
+    fake, far = 1 << 40, 1 << 50                           # (refused before anything is read)
+    rows = lambda seq: B.lq_kvrows(far, (seq, 4096 * 8, 8), None, (0, 0, 0))
+    b = lambda n, s=1, stride=1: B.lq_kvbatch(s, n, fake, fake + (1 << 20), stride)
+    both = B.lq_kvrows(far, (0, 0, 8), far, (0, 0, 8))
+    assert code(B.lq_kvcache_append, c, 0, b(1 << 24), both) == 2 and code(B.lq_kvcache_append, c, 0, b(HIGH), both) == 2
+    assert code(B.lq_kvcache_read, c, 0, b(0, 1, 1 << 20), None, 1 << 24, rows(0)) == 2
+    assert code(B.lq_kvcache_read, c, 0, b(0, 65535, 8), None, 256, rows(256 * 4096 * 8)) == 2
+    B.lq_kvcache_free(c)
